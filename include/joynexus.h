@@ -18,6 +18,12 @@
  *                          nothing is averaged across tenants)
  *   jn_tenant_experts_fwd_bwd the same for tenants whose action module is a
  *                          transformer expert reading each sample's backbone rows
+ *   jn_tenant_tokens_fwd_bwd the same for tenants that predict tokens: cross
+ *                          entropy over the tenant's vocabulary and its gradients
+ *   jn_tenant_tokens_decode the likeliest token of single rows (serving)
+ *   jn_qk_norm_rope        head norms and rotation of queries and keys, the step
+ *                          that jn_backbone_forward takes between projection and
+ *                          attention, with its gradients (jn_qk_norm_rope_bwd)
  *   jn_tenant_adamw_step   per-tenant AdamW update of the tenants' parameters
  *   jn_unpack              scatter packed rows back to the requests' own
  *                          padded buffers (the "split" by slices, App. A.3)
@@ -78,7 +84,8 @@ typedef enum jn_op {
   JN_OP_PACK = 1, JN_OP_RMSNORM = 2, JN_OP_GEMM_QKV = 3, JN_OP_ATTENTION = 4, JN_OP_GEMM_O = 5,
   JN_OP_GEMM_UP = 6, JN_OP_GEMM_DOWN = 7, JN_OP_POOL = 8, JN_OP_HEAD_FWD = 9, JN_OP_LOSS = 10,
   JN_OP_HEAD_BWD = 11, JN_OP_UNPACK = 12, JN_OP_EXPERT_GEMM = 13, JN_OP_EXPERT_ATTENTION = 14,
-  JN_OP_EXPERT_OTHER = 15, JN_OP_OPTIMIZER = 16, JN_OP_ROPE = 17
+  JN_OP_EXPERT_OTHER = 15, JN_OP_OPTIMIZER = 16, JN_OP_ROPE = 17, JN_OP_QK = 18, JN_OP_TOKEN_GEMM = 19,
+  JN_OP_TOKEN_OTHER = 20
 } jn_op;
 
 /* One traced kernel launch.  For GEMMs (M, N, K) is the launch shape
@@ -220,6 +227,8 @@ typedef struct jn_layer {
   const void* w_down;      /* bf16 [d][f]                                     */
   const void* g1;          /* bf16 [d] pre-attention RMSNorm gain             */
   const void* g2;          /* bf16 [d] pre-MLP RMSNorm gain                   */
+  const void* gq;          /* bf16 [hd] gains of the norms of every query and */
+  const void* gk;          /* key head, 16-byte aligned; both NULL: no norms  */
 } jn_layer;
 
 /* Frozen shared backbone: pre-RMSNorm transformer blocks
@@ -236,6 +245,14 @@ typedef struct jn_layer {
  *                 for i < hd/2 the pair (x_i, x_{i+hd/2}) of a row at
  *                 position p (its row inside its own sample, from 0) is
  *                 rotated by p * rope_theta^(-2i/hd); 0: no positions
+ *   gq, gk        (of every layer, or of none) q and k pass a norm of each head,
+ *                 x / sqrt(mean(x^2) + eps) * g over the head's hd elements,
+ *                 before the rotation
+ *   rope_axes     2 to 4: rows have that many positions (time, height, width of
+ *                 image and video patches), read from `pos`, and every pair
+ *                 turns by one of them: jn_qk_norm_rope below says which.
+ *                 0 or 1: one position, pos[row], or the row's own where pos
+ *                 is NULL
  * Arithmetic: bf16 GEMM / attention operands with fp32 accumulation, fp32
  * residual stream, fp32 norm / softmax / rotation math, bf16 stored
  * activations (q and k are stored rotated, rounded once more).
@@ -250,6 +267,12 @@ typedef struct jn_backbone {
   const void* gf;          /* bf16 [d] final RMSNorm gain              */
   int32_t causal;          /* 0 bidirectional, 1 causal                */
   float rope_theta;        /* 0 = no rotary embedding                  */
+  int32_t rope_axes;       /* 0 = 1                                    */
+  int32_t rope_interleaved;
+  int32_t rope_sections[4];
+  const int32_t* pos;      /* device int32 [T][rope_axes] of the packed rows
+                              (alignment rows: any value), or NULL; an
+                              inference plan reads it at every launch */
 } jn_backbone;
 
 /* Workspace bytes jn_backbone_forward needs for a batch of T rows. */
@@ -258,6 +281,48 @@ jn_status jn_backbone_workspace_size(const jn_backbone* bb, int32_t T, size_t* b
 /* hidden: device bf16 [T][d], written for every row (alignment rows zero). */
 jn_status jn_backbone_forward(jn_ctx* ctx, const jn_backbone* bb, const jn_packed* p,
                               void* hidden, void* ws, size_t ws_bytes);
+
+/* ------------------------------------- queries and keys: norm, rotation --- */
+
+/* Rows of a fused projection: n_heads query heads, then n_kv_heads key heads, of
+ * head_dim bf16 elements each, then whatever the caller holds there (values).
+ *   u = g x / sqrt(mean(x^2) + eps)   per head, g = gq or gk; u = x where both are NULL
+ *   y = the pairs (u_i, u_{i + hd/2}), i < hd/2, turned by pos[a(i)] * rope_theta^(-2i/hd)
+ * With one axis a(i) = 0.  With rope_axes = 2 .. 4, rope_sections[a] pairs belong
+ * to axis a and add up to hd/2: pairs 0, 1, ... in runs of the axes' lengths, or
+ * (rope_interleaved) dealt in turn, pair i to axis i mod rope_axes while that
+ * axis has had fewer than its pairs, else to axis 0.  Angles are formed in 64
+ * bits, so any int32 position (negative ones too) loses nothing; norms, rotation
+ * and sums are fp32; y and the input's gradient are rounded to bf16 once.
+ * rope_theta = 0: no rotation (then gq and gk are needed).
+ * head_dim: a multiple of 16 in [16, 256] (JN_EUNSUPPORTED).  Buffers and gains
+ * are 16-byte aligned and rows a multiple of 8 elements apart (JN_EUNSUPPORTED).
+ * rows may be 0. */
+typedef struct jn_qk_args {
+  int32_t rows, n_heads, n_kv_heads, head_dim;
+  int64_t ld_in;           /* elements between rows of the projection x */
+  int64_t ld_out;          /* elements between rows of y and of dy      */
+  int64_t ld_grad;         /* elements between rows of dx (jn_qk_norm_rope_bwd) */
+  const void* gq;          /* bf16 [head_dim], or both NULL                       */
+  const void* gk;
+  const int32_t* pos;      /* device int32 [rows][max(rope_axes, 1)]; unused without rotation */
+  float eps, rope_theta;
+  int32_t rope_axes, rope_interleaved;
+  int32_t rope_sections[4];
+} jn_qk_args;
+
+/* y = the rotated, normed query and key heads of every row of x; the columns
+ * behind them are not touched.  In place (y == x) where ld_out == ld_in; other
+ * overlaps are not allowed. */
+jn_status jn_qk_norm_rope(jn_ctx* ctx, const jn_qk_args* a, const void* x, void* y);
+
+/* Gradients: dx from the gradient dy of y (dx == dy or dx == x allowed where the
+ * strides are equal), and, with norms, the sums over all rows and heads dgq, dgk (fp32
+ * [head_dim], written, not added to).  x: the projection the forward read (not read
+ * without norms, may be NULL then).  The sums run in a fixed order. */
+jn_status jn_qk_norm_rope_workspace_size(const jn_qk_args* a, size_t* bytes);
+jn_status jn_qk_norm_rope_bwd(jn_ctx* ctx, const jn_qk_args* a, const void* x, const void* dy, void* dx,
+                              float* dgq, float* dgk, void* ws, size_t ws_bytes);
 
 /* --------------------------------------------------------------- heads --- */
 
@@ -399,6 +464,65 @@ jn_status jn_experts_workspace_size(const jn_packed* p, const jn_expert* ex, con
  * be 16-byte aligned. */
 jn_status jn_tenant_experts_fwd_bwd(jn_ctx* ctx, const jn_packed* p, const void* hidden, const jn_expert* ex,
                                     const jn_expert_io* io, int32_t G, void* ws, size_t ws_bytes);
+
+/* ---------------------------------------------------------- token heads --- */
+
+/* A tenant-private token head (VLM tenants of Sec. 5.2 that are trained on text or
+ * on discretised actions): logits z = W h of rows h of the shared feature. */
+typedef struct jn_token_head {
+  int32_t vocab;           /* 1 .. 2^24 */
+  int32_t reserved;
+  const void* W;           /* device bf16 [vocab][d], 16-byte aligned; tenants may share one */
+} jn_token_head;
+
+/* A tenant's targets: row rows[i] of the feature predicts token targets[i].  An
+ * entry whose row is outside [0, T) or whose token is outside [0, vocab) has no
+ * target (so lists can be padded with -1): logp 0, no gradient, not counted, and
+ * what the feature holds there is not looked at.  Entries may name a row twice.
+ * For row j of sample i of a packed batch the row is cu_seqlens[i] + j. */
+typedef struct jn_token_io {
+  int32_t n;               /* entries, 0 .. 2^20                                  */
+  int32_t reserved;
+  const int32_t* rows;     /* device int32 [n]                                    */
+  const int32_t* targets;  /* device int32 [n]                                    */
+  float* logp;             /* out: device fp32 [n], log softmax(z)[target]        */
+  float* loss;             /* out: device fp32 [1], mean of -logp over the targets, 0 without any */
+  void* dW;                /* out: device bf16 [vocab][d], dloss / dW             */
+  void* dh;                /* out: device bf16 [n][d], dloss / d(the entry's row), or NULL */
+} jn_token_io;
+
+/* Cross entropy of every tenant's targets over its own vocabulary, with gradients,
+ * in pieces of the vocabulary: the logits of one pass are reduced as they are formed
+ * and formed again for the gradients, so the workspace stays bounded (a piece of at
+ * most JN_TOKEN_PIECE_BYTES, 4 KB a target at d = 2048, and the columns' sums).
+ * Nothing is averaged across tenants.  hidden: device bf16 [T][d], d a multiple of 64
+ * in [64, 8192].  Precision: bf16 operands, fp32 accumulation, softmax statistics
+ * and loss; the logits' gradient is rounded to bf16 before it meets h and W, the
+ * results once.  Kernels only: the call may be captured into a HIP graph, whose
+ * replays read rows, targets, hidden and W as they are then.  Results are
+ * bitwise reproducible.  Errors enqueue nothing. */
+#define JN_TOKEN_PIECE_BYTES (256u << 20)
+jn_status jn_tokens_workspace_size(int32_t d, const jn_token_head* heads, const jn_token_io* io, int32_t G,
+                                   size_t* bytes);
+jn_status jn_tenant_tokens_fwd_bwd(jn_ctx* ctx, const void* hidden, int32_t T, int32_t d, const jn_token_head* heads,
+                                   const jn_token_io* io, int32_t G, void* ws, size_t ws_bytes);
+
+/* Greedy decoding of single rows: per entry the token of the largest logit (the
+ * lowest of equal ones) and its log-probability.  An entry whose row is outside
+ * [0, T) gets token -1 and logp 0.  Rows with NaN logits get some token of the
+ * vocabulary and a NaN logp. */
+typedef struct jn_token_pick {
+  int32_t n;               /* entries, 0 .. 2^20      */
+  int32_t reserved;
+  const int32_t* rows;     /* device int32 [n]        */
+  int32_t* token;          /* out: device int32 [n]   */
+  float* logp;             /* out: device fp32 [n]    */
+} jn_token_pick;
+
+jn_status jn_tokens_decode_workspace_size(int32_t d, const jn_token_head* heads, const jn_token_pick* io, int32_t G,
+                                          size_t* bytes);
+jn_status jn_tenant_tokens_decode(jn_ctx* ctx, const void* hidden, int32_t T, int32_t d, const jn_token_head* heads,
+                                  const jn_token_pick* io, int32_t G, void* ws, size_t ws_bytes);
 
 /* ---------------------------------------------------- tenant optimizer --- */
 

@@ -16,7 +16,8 @@ import numpy as np
 from . import _abi
 from ._abi import (EXPERT_LAYER_FIELDS, JN_OK, STATUS_NAMES, jn_adamw_tenant, jn_backbone, jn_expert, jn_expert_io,
                    jn_expert_layer, jn_expert_layer_grads, jn_head, jn_head_io, jn_layer, jn_pack_opts,
-                   jn_pack_sizes, jn_packed, jn_request, jn_tenant)
+                   jn_pack_sizes, jn_packed, jn_qk_args, jn_request, jn_tenant, jn_token_head, jn_token_io,
+                   jn_token_pick)
 
 _lib = _abi.load()
 
@@ -26,6 +27,9 @@ __all__ = [
     "jn_backbone_forward", "jn_heads_workspace_size", "jn_tenant_heads_fwd_bwd", "jn_tenant_heads_fwd_bwd_noalloc",
     "HEADS_SCRATCH_BYTES", "jn_unpack",
     "Expert", "ExpertIO", "jn_pack_tenant_sizes", "jn_experts_workspace_size", "jn_tenant_experts_fwd_bwd",
+    "QKNormRope", "jn_qk_norm_rope", "jn_qk_norm_rope_workspace_size", "jn_qk_norm_rope_bwd",
+    "TokenHead", "TokenIO", "TokenPick", "jn_tokens_workspace_size", "jn_tenant_tokens_fwd_bwd",
+    "jn_tokens_decode_workspace_size", "jn_tenant_tokens_decode",
     "AdamWTenant", "jn_adamw_workspace_size", "jn_tenant_adamw_step",
     "Collector", "InferPlan", "jn_infer_workspace_size",
     "lib_path",
@@ -204,11 +208,34 @@ def jn_pack_group(ctx: Context, reqs: Sequence[Request], tenants: Sequence[Tenan
 
 # ------------------------------------------------------------ backbone ------
 
+def _rope_fields(s, theta: float, sections, interleaved: bool):
+    sections = [int(x) for x in sections or ()]
+    if len(sections) > 4:
+        raise ValueError("at most four position axes")
+    s.rope_theta = float(theta)
+    s.rope_axes = len(sections)
+    s.rope_interleaved = 1 if interleaved else 0
+    s.rope_sections = (C.c_int32 * 4)(*(sections + [0] * (4 - len(sections))))
+
+
+def _positions(pos, rows: int, axes: int):
+    """Device pointer of int32 positions [rows, axes] ([rows] with one axis)."""
+    import torch
+    if pos is None:
+        return None
+    if pos.dtype != torch.int32 or not pos.is_contiguous() or pos.numel() != rows * axes:
+        raise TypeError(f"positions must be a contiguous int32 tensor of {rows} x {axes}")
+    return _ptr(pos)
+
+
 class Backbone:
-    """Device weights of the frozen backbone (lists of torch bf16 tensors)."""
+    """Device weights of the frozen backbone (lists of torch bf16 tensors).
+
+    A layer with head norms also has "gq" and "gk" (bf16 [head width]).  ``rope_sections``: pairs of every position
+    axis, for rows with several positions; ``set_positions`` then names the batch's."""
 
     def __init__(self, layers: List[dict], gf, n_heads: int, eps: float, n_kv_heads: int = 0, causal: bool = False,
-                 rope_theta: float = 0.0):
+                 rope_theta: float = 0.0, rope_sections: Sequence[int] = (), rope_interleaved: bool = False):
         self.layers = layers
         self.gf = gf
         self.n_heads = int(n_heads)
@@ -227,6 +254,8 @@ class Backbone:
             arr[i].w_down = _ptr(L["w_down"])
             arr[i].g1 = _ptr(L["g1"])
             arr[i].g2 = _ptr(L["g2"])
+            arr[i].gq = _ptr(L.get("gq"))
+            arr[i].gk = _ptr(L.get("gk"))
         self._arr = arr
         s = jn_backbone()
         s.n_layers = len(layers)
@@ -236,10 +265,17 @@ class Backbone:
         s.eps = self.eps
         s.n_kv_heads = self.n_kv_heads
         s.causal = 1 if self.causal else 0
-        s.rope_theta = self.rope_theta
+        _rope_fields(s, rope_theta, rope_sections, rope_interleaved)
         s.layers = C.cast(arr, C.POINTER(jn_layer))
         s.gf = _ptr(gf)
         self.struct = s
+        self.pos = None
+
+    def set_positions(self, pos):
+        """Positions of the packed rows of the batches that follow: device int32 [T, axes] (None: the rows' own)."""
+        axes = max(1, self.struct.rope_axes)
+        self.struct.pos = _positions(pos, pos.shape[0] if pos is not None else 0, axes)
+        self.pos = pos
 
 
 def jn_backbone_workspace_size(bb: Backbone, T: int) -> int:
@@ -251,6 +287,62 @@ def jn_backbone_workspace_size(bb: Backbone, T: int) -> int:
 def jn_backbone_forward(ctx: Context, bb: Backbone, packed: Packed, hidden, ws):
     _check(_lib.jn_backbone_forward(ctx.handle, C.byref(bb.struct), C.byref(packed.struct), _ptr(hidden),
                                     _ptr(ws), ws.numel() * ws.element_size()), ctx)
+
+
+# --------------------------------------- queries and keys: norm, rotation ---
+
+class QKNormRope:
+    """Head norms (``gq``, ``gk``: device bf16 [head_dim], or both None) and rotation (``theta`` > 0) of the query and
+    key heads of fused rows; ``sections``: pairs of every position axis, none for a single axis."""
+
+    def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, eps: float = 1e-6, gq=None, gk=None,
+                 theta: float = 0.0, sections: Sequence[int] = (), interleaved: bool = False):
+        self.gq, self.gk = gq, gk
+        s = jn_qk_args()
+        s.n_heads, s.n_kv_heads, s.head_dim = int(n_heads), int(n_kv_heads), int(head_dim)
+        s.eps = float(eps)
+        s.gq, s.gk = _ptr(gq), _ptr(gk)
+        _rope_fields(s, theta, sections, interleaved)
+        self.struct = s
+
+    def at(self, rows: int, pos, x=None, y=None, dx=None):
+        """The C arguments for rows of x, y (or its gradient) and dx."""
+        s = jn_qk_args.from_buffer_copy(self.struct)
+        s.rows = int(rows)
+        s.pos = _positions(pos, rows, max(1, s.rope_axes))
+        width = (s.n_heads + s.n_kv_heads) * s.head_dim
+        s.ld_in, s.ld_out, s.ld_grad = (_row_stride(t, rows, width) for t in (x, y, dx))
+        return s
+
+
+def _row_stride(t, rows: int, width: int) -> int:
+    """Elements between the rows of a bf16 [rows, >= width] tensor."""
+    import torch
+    if t is None:
+        return (width + 7) // 8 * 8
+    if t.dtype != torch.bfloat16 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] < width or t.stride(1) != 1:
+        raise TypeError(f"rows must be a bfloat16 tensor [{rows}, >= {width}] with adjacent columns")
+    return t.stride(0) if rows > 1 else max(t.stride(0), t.shape[1])
+
+
+def jn_qk_norm_rope(ctx: Context, qk: QKNormRope, x, pos, y):
+    a = qk.at(x.shape[0], pos, x, y)
+    _check(_lib.jn_qk_norm_rope(ctx.handle, C.byref(a), _ptr(x), _ptr(y)), ctx)
+
+
+def jn_qk_norm_rope_workspace_size(qk: QKNormRope, rows: int) -> int:
+    n = C.c_size_t()
+    a = jn_qk_args.from_buffer_copy(qk.struct)
+    a.rows = int(rows)
+    _check(_lib.jn_qk_norm_rope_workspace_size(C.byref(a), C.byref(n)), what="jn_qk_norm_rope_workspace_size")
+    return int(n.value)
+
+
+def jn_qk_norm_rope_bwd(ctx: Context, qk: QKNormRope, x, pos, dy, dx, dgq, dgk, ws):
+    """``x``, ``dgq``, ``dgk`` and ``ws`` may be None without norms."""
+    a = qk.at(dy.shape[0], pos, x, dy, dx)
+    _check(_lib.jn_qk_norm_rope_bwd(ctx.handle, C.byref(a), _ptr(x), _ptr(dy), _ptr(dx), _ptr(dgq), _ptr(dgk),
+                                    _ptr(ws), ws.numel() * ws.element_size() if ws is not None else 0), ctx)
 
 
 # --------------------------------------------------------------- heads ------
@@ -406,6 +498,105 @@ def jn_tenant_experts_fwd_bwd(ctx: Context, packed: Packed, hidden, ex: Sequence
     ea, ia = _expert_arrays(ex, ios)
     _check(_lib.jn_tenant_experts_fwd_bwd(ctx.handle, C.byref(packed.struct), _ptr(hidden), ea, ia, len(ex),
                                           _ptr(ws), ws.numel() * ws.element_size()), ctx)
+
+
+# --------------------------------------------------------- token heads ------
+
+def _entries(name: str, t, dtype, n: int):
+    if t is None or t.dtype != dtype or not t.is_contiguous() or t.numel() != n:
+        raise TypeError(f"{name} must be a contiguous {dtype} tensor of {n} elements")
+    return _ptr(t)
+
+
+class TokenHead:
+    """A tenant's token head: device bf16 W [vocab, d]."""
+
+    def __init__(self, W):
+        import torch
+        if W.dtype != torch.bfloat16 or W.dim() != 2 or not W.is_contiguous():
+            raise TypeError("W must be a contiguous bfloat16 tensor [vocab, d]")
+        self.W = W
+        s = jn_token_head()
+        s.vocab = int(W.shape[0])
+        s.W = _ptr(W)
+        self.struct = s
+
+
+class TokenIO:
+    """A tenant's targets (device int32 ``rows`` and ``targets`` [n]) and outputs: fp32 logp [n] and loss [1], bf16 dW
+    [vocab, d] and, optionally, dh [n, d]."""
+
+    def __init__(self, rows, targets, logp, loss, dW, dh=None):
+        import torch
+        self.rows, self.targets, self.logp, self.loss, self.dW, self.dh = rows, targets, logp, loss, dW, dh
+        s = jn_token_io()
+        n = s.n = int(rows.numel())
+        s.rows = _entries("rows", rows, torch.int32, n)
+        s.targets = _entries("targets", targets, torch.int32, n)
+        s.logp = _entries("logp", logp, torch.float32, n)
+        s.loss = _entries("loss", loss, torch.float32, 1)
+        s.dW = _entries("dW", dW, torch.bfloat16, dW.numel())
+        s.dh = _entries("dh", dh, torch.bfloat16, n * int(dW.shape[1])) if dh is not None else None
+        self.struct = s
+
+
+class TokenPick:
+    """Rows to decode (device int32 [n]) and outputs: token int32 [n], logp fp32 [n]."""
+
+    def __init__(self, rows, token, logp):
+        import torch
+        self.rows, self.token, self.logp = rows, token, logp
+        s = jn_token_pick()
+        n = s.n = int(rows.numel())
+        s.rows = _entries("rows", rows, torch.int32, n)
+        s.token = _entries("token", token, torch.int32, n)
+        s.logp = _entries("logp", logp, torch.float32, n)
+        self.struct = s
+
+
+def _token_arrays(heads: Sequence[TokenHead], ios: Sequence):
+    if len(heads) != len(ios) or not heads:
+        raise ValueError("one entry per token head")
+    d = int(heads[0].W.shape[1])
+    for h, io in zip(heads, ios):
+        if int(h.W.shape[1]) != d or (isinstance(io, TokenIO) and tuple(io.dW.shape) != tuple(h.W.shape)):
+            raise TypeError("token heads of one call share d, and dW has its W's shape")
+    c = jn_token_io if isinstance(ios[0], TokenIO) else jn_token_pick
+    return d, (jn_token_head * len(heads))(*[h.struct for h in heads]), (c * len(ios))(*[x.struct for x in ios])
+
+
+def _feature(hidden, d: int) -> int:
+    import torch
+    if hidden.dtype != torch.bfloat16 or hidden.dim() != 2 or not hidden.is_contiguous() or hidden.shape[1] != d:
+        raise TypeError(f"hidden must be a contiguous bfloat16 tensor [T, {d}]")
+    return int(hidden.shape[0])
+
+
+def jn_tokens_workspace_size(heads: Sequence[TokenHead], ios: Sequence[TokenIO]) -> int:
+    d, ha, ia = _token_arrays(heads, ios)
+    n = C.c_size_t()
+    _check(_lib.jn_tokens_workspace_size(d, ha, ia, len(heads), C.byref(n)), what="jn_tokens_workspace_size")
+    return int(n.value)
+
+
+def jn_tenant_tokens_fwd_bwd(ctx: Context, hidden, heads: Sequence[TokenHead], ios: Sequence[TokenIO], ws):
+    d, ha, ia = _token_arrays(heads, ios)
+    _check(_lib.jn_tenant_tokens_fwd_bwd(ctx.handle, _ptr(hidden), _feature(hidden, d), d, ha, ia, len(heads),
+                                         _ptr(ws), ws.numel() * ws.element_size()), ctx)
+
+
+def jn_tokens_decode_workspace_size(heads: Sequence[TokenHead], picks: Sequence[TokenPick]) -> int:
+    d, ha, ia = _token_arrays(heads, picks)
+    n = C.c_size_t()
+    _check(_lib.jn_tokens_decode_workspace_size(d, ha, ia, len(heads), C.byref(n)),
+           what="jn_tokens_decode_workspace_size")
+    return int(n.value)
+
+
+def jn_tenant_tokens_decode(ctx: Context, hidden, heads: Sequence[TokenHead], picks: Sequence[TokenPick], ws):
+    d, ha, ia = _token_arrays(heads, picks)
+    _check(_lib.jn_tenant_tokens_decode(ctx.handle, _ptr(hidden), _feature(hidden, d), d, ha, ia, len(heads),
+                                        _ptr(ws), ws.numel() * ws.element_size()), ctx)
 
 
 # ---------------------------------------------------- tenant optimizer ------

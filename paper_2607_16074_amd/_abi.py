@@ -25,6 +25,9 @@ EXPORTS = (
     "jn_backbone_workspace_size", "jn_backbone_forward",
     "jn_heads_workspace_size", "jn_tenant_heads_fwd_bwd", "jn_tenant_heads_fwd_bwd_noalloc",
     "jn_pack_tenant_sizes", "jn_experts_workspace_size", "jn_tenant_experts_fwd_bwd",
+    "jn_qk_norm_rope", "jn_qk_norm_rope_workspace_size", "jn_qk_norm_rope_bwd",
+    "jn_tokens_workspace_size", "jn_tenant_tokens_fwd_bwd",
+    "jn_tokens_decode_workspace_size", "jn_tenant_tokens_decode",
     "jn_adamw_workspace_size", "jn_tenant_adamw_step",
     "jn_unpack",
     "jn_collector_create", "jn_collector_destroy", "jn_collector_submit", "jn_collector_poll",
@@ -36,7 +39,8 @@ EXPORTS = (
 
 OPS = {1: "pack", 2: "rmsnorm", 3: "gemm_qkv", 4: "attention", 5: "gemm_o", 6: "gemm_up", 7: "gemm_down",
        8: "pool", 9: "head_fwd", 10: "loss", 11: "head_bwd", 12: "unpack", 13: "expert_gemm",
-       14: "expert_attention", 15: "expert_other", 16: "optimizer", 17: "rope"}
+       14: "expert_attention", 15: "expert_other", 16: "optimizer", 17: "rope", 18: "qk_norm_rope",
+       19: "token_gemm", 20: "token_other"}
 
 
 class jn_trace_entry(C.Structure):
@@ -85,13 +89,35 @@ class jn_packed(C.Structure):
 
 class jn_layer(C.Structure):
     _fields_ = [("wqkv", C.c_void_p), ("wo", C.c_void_p), ("w_up", C.c_void_p), ("w_gate", C.c_void_p),
-                ("w_down", C.c_void_p), ("g1", C.c_void_p), ("g2", C.c_void_p)]
+                ("w_down", C.c_void_p), ("g1", C.c_void_p), ("g2", C.c_void_p), ("gq", C.c_void_p), ("gk", C.c_void_p)]
 
 
 class jn_backbone(C.Structure):
     _fields_ = [("n_layers", C.c_int32), ("d", C.c_int32), ("n_heads", C.c_int32), ("ffn", C.c_int32),
                 ("eps", C.c_float), ("n_kv_heads", C.c_int32), ("layers", C.POINTER(jn_layer)), ("gf", C.c_void_p),
-                ("causal", C.c_int32), ("rope_theta", C.c_float)]
+                ("causal", C.c_int32), ("rope_theta", C.c_float), ("rope_axes", C.c_int32),
+                ("rope_interleaved", C.c_int32), ("rope_sections", C.c_int32 * 4), ("pos", C.c_void_p)]
+
+
+class jn_qk_args(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("ld_in", C.c_int64), ("ld_out", C.c_int64), ("ld_grad", C.c_int64), ("gq", C.c_void_p), ("gk", C.c_void_p),
+                ("pos", C.c_void_p), ("eps", C.c_float), ("rope_theta", C.c_float), ("rope_axes", C.c_int32),
+                ("rope_interleaved", C.c_int32), ("rope_sections", C.c_int32 * 4)]
+
+
+class jn_token_head(C.Structure):
+    _fields_ = [("vocab", C.c_int32), ("reserved", C.c_int32), ("W", C.c_void_p)]
+
+
+class jn_token_io(C.Structure):
+    _fields_ = [("n", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_void_p), ("targets", C.c_void_p),
+                ("logp", C.c_void_p), ("loss", C.c_void_p), ("dW", C.c_void_p), ("dh", C.c_void_p)]
+
+
+class jn_token_pick(C.Structure):
+    _fields_ = [("n", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_void_p), ("token", C.c_void_p),
+                ("logp", C.c_void_p)]
 
 
 class jn_head(C.Structure):
@@ -176,6 +202,17 @@ def load(path: str = LIB_PATH) -> C.CDLL:
                                                 P(C.c_size_t)]),
         "jn_tenant_experts_fwd_bwd": (C.c_int, [V, P(jn_packed), V, P(jn_expert), P(jn_expert_io), C.c_int32, V,
                                                 C.c_size_t]),
+        "jn_qk_norm_rope": (C.c_int, [V, P(jn_qk_args), V, V]),
+        "jn_qk_norm_rope_workspace_size": (C.c_int, [P(jn_qk_args), P(C.c_size_t)]),
+        "jn_qk_norm_rope_bwd": (C.c_int, [V, P(jn_qk_args), V, V, V, V, V, V, C.c_size_t]),
+        "jn_tokens_workspace_size": (C.c_int, [C.c_int32, P(jn_token_head), P(jn_token_io), C.c_int32,
+                                               P(C.c_size_t)]),
+        "jn_tenant_tokens_fwd_bwd": (C.c_int, [V, V, C.c_int32, C.c_int32, P(jn_token_head), P(jn_token_io),
+                                               C.c_int32, V, C.c_size_t]),
+        "jn_tokens_decode_workspace_size": (C.c_int, [C.c_int32, P(jn_token_head), P(jn_token_pick), C.c_int32,
+                                                      P(C.c_size_t)]),
+        "jn_tenant_tokens_decode": (C.c_int, [V, V, C.c_int32, C.c_int32, P(jn_token_head), P(jn_token_pick),
+                                              C.c_int32, V, C.c_size_t]),
         "jn_adamw_workspace_size": (C.c_int, [P(jn_adamw_tenant), C.c_int32, P(C.c_size_t)]),
         "jn_tenant_adamw_step": (C.c_int, [V, P(jn_adamw_tenant), C.c_int32, V, C.c_size_t]),
         "jn_unpack": (C.c_int, [V, P(jn_packed), P(jn_request), C.c_int32, V, C.c_size_t, P(V)]),

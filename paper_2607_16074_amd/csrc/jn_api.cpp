@@ -593,6 +593,40 @@ BbLayout bb_layout(const jn_backbone* bb, int64_t T) {
   return L;
 }
 
+jn_status check_axes(jn_ctx* c, int32_t axes, int32_t interleaved, const int32_t* sections, int32_t hd) {
+  if (axes < 0 || axes > 4 || (interleaved != 0 && interleaved != 1))
+    return fail(c, JN_EINVAL, "rope_axes must be 0 to 4 and rope_interleaved 0 or 1");
+  if (axes <= 1) return JN_OK;
+  int64_t sum = 0;
+  for (int32_t a = 0; a < axes; ++a) {
+    // of the pairs dealt in turn, axis a > 0 is offered a, a + axes, ... below hd/2
+    const int32_t offered = hd / 2 > a ? (hd / 2 - a + axes - 1) / axes : 0;
+    if (sections[a] < 0 || (interleaved && a > 0 && sections[a] > offered))
+      return fail(c, JN_EINVAL, "rope_sections[%d] = %d is not possible", a, sections[a]);
+    sum += sections[a];
+  }
+  if (sum != hd / 2) return fail(c, JN_EINVAL, "rope_sections add up to %lld of %d pairs", (long long)sum, hd / 2);
+  return JN_OK;
+}
+
+// Frequencies and axes of a head's pairs, as jn_qk_norm_rope says.
+void qk_pairs(QkShape* q, float theta, int32_t axes, int32_t interleaved, const int32_t* sections) {
+  const double turn = 6.283185307179586476925286766559;
+  int32_t run = 0, left = axes > 1 ? sections[0] : q->hd / 2;
+  for (int32_t i = 0; i < q->hd / 2; ++i) {
+    q->freq[i] = std::pow((double)theta, -2.0 * i / q->hd) / turn;
+    if (axes > 1 && interleaved) {
+      const int32_t a = i % axes;
+      q->axis[i] = (uint8_t)(i / axes < sections[a] ? a : 0);
+    } else {
+      while (left == 0) left = sections[++run];
+      --left;
+      q->axis[i] = (uint8_t)run;
+    }
+  }
+  q->axes = axes > 1 ? axes : 1;
+}
+
 jn_status check_backbone(jn_ctx* c, const jn_backbone* bb) {
   if (!bb || !bb->layers || !bb->gf) return fail(c, JN_EINVAL, "null backbone");
   if (bb->n_layers < 1 || bb->d < 1 || bb->n_heads < 1 || bb->ffn < 1)
@@ -610,12 +644,20 @@ jn_status check_backbone(jn_ctx* c, const jn_backbone* bb) {
     return fail(c, JN_EINVAL, "n_kv_heads %d must divide n_heads %d", bb->n_kv_heads, bb->n_heads);
   if (bb->causal != 0 && bb->causal != 1) return fail(c, JN_EINVAL, "causal must be 0 or 1");
   if (!(bb->rope_theta >= 0.f) || std::isinf(bb->rope_theta)) return fail(c, JN_EINVAL, "rope_theta must be >= 0");
+  const jn_status st = check_axes(c, bb->rope_axes, bb->rope_interleaved, bb->rope_sections, hd);
+  if (st != JN_OK) return st;
+  if (bb->rope_axes > 1 && (!(bb->rope_theta > 0.f) || !bb->pos))
+    return fail(c, JN_EINVAL, "%d position axes need rope_theta > 0 and pos", bb->rope_axes);
   bool glu = bb->layers[0].w_gate != nullptr;
   for (int l = 0; l < bb->n_layers; ++l) {
     const jn_layer& L = bb->layers[l];
     if (!L.wqkv || !L.wo || !L.w_up || !L.w_down || !L.g1 || !L.g2)
       return fail(c, JN_EINVAL, "layer %d has a null weight", l);
     if ((L.w_gate != nullptr) != glu) return fail(c, JN_EINVAL, "layer %d mixes GELU and GeGLU MLPs", l);
+    if ((L.gq != nullptr) != (bb->layers[0].gq != nullptr) || (L.gk != nullptr) != (L.gq != nullptr))
+      return fail(c, JN_EINVAL, "layer %d: head norms need both gains, in every layer or in none", l);
+    if (((uintptr_t)L.gq | (uintptr_t)L.gk) % 16 != 0)
+      return fail(c, JN_EUNSUPPORTED, "layer %d head gains not 16-byte aligned", l);
     const void* ps[] = {L.wqkv, L.wo, L.w_up, L.w_down, L.w_gate};
     for (const void* q : ps)
       if (q && ((uintptr_t)q) % 16 != 0) return fail(c, JN_EUNSUPPORTED, "layer %d weight not 16-byte aligned", l);
@@ -680,6 +722,22 @@ jn_status jn_backbone_forward(jn_ctx* c, const jn_backbone* bb, const jn_packed*
     return S > 1 ? launch_rmsnorm_split(s, x, (const float*)sp, S, g, out, T, d, bb->eps)
                  : launch_rmsnorm_f32in(s, x, g, out, T, d, bb->eps);
   };
+  // Head norms, several position axes or positions of the caller's: one pass over
+  // q and k; a plain rotation by the row's own position keeps its kernel and its bits
+  const bool qk = bb->layers[0].gq != nullptr || (bb->rope_theta > 0.f && bb->pos);
+  QkShape shape{};
+  if (qk) {
+    shape.rows = T;
+    shape.heads = bb->n_heads;
+    shape.kv = kvh;
+    shape.hd = hd;
+    shape.ldx = shape.ldy = nqkv;
+    shape.eps = bb->eps;
+    if (bb->rope_theta > 0.f) {
+      shape.pos = bb->pos ? bb->pos : p->token_pos;
+      qk_pairs(&shape, bb->rope_theta, bb->rope_axes, bb->rope_interleaved, bb->rope_sections);
+    }
+  }
   for (int l = 0; l < bb->n_layers; ++l) {
     const jn_layer& Ly = bb->layers[l];
     if (l == 0)
@@ -688,7 +746,12 @@ jn_status jn_backbone_forward(jn_ctx* c, const jn_backbone* bb, const jn_packed*
       JN_TRACED(c, JN_OP_RMSNORM, T, d, 0, norm(sd, Ly.g1, h), "rmsnorm");
     JN_TRACED(c, JN_OP_GEMM_QKV, T, nqkv, d,
               launch_gemm(s, EPI_BF16, h, d, Ly.wqkv, nullptr, d, qkv, nqkv, T, nqkv, d, sp, spb), "gemm qkv");
-    if (bb->rope_theta > 0.f)
+    if (qk) {
+      shape.gq = (const uint16_t*)Ly.gq;
+      shape.gk = (const uint16_t*)Ly.gk;
+      JN_TRACED(c, JN_OP_QK, T, (bb->n_heads + kvh) * hd, 0,
+                launch_qk_fwd(s, shape, (const uint16_t*)qkv, (uint16_t*)qkv), "head norms and rotation");
+    } else if (bb->rope_theta > 0.f)
       JN_TRACED(c, JN_OP_ROPE, T, (bb->n_heads + kvh) * hd, 0,
                 launch_rope(s, qkv, nqkv, p->token_pos, T, bb->n_heads + kvh, hd, bb->rope_theta), "rope");
     JN_TRACED(c, JN_OP_ATTENTION, T, d, bb->n_heads,
@@ -709,6 +772,442 @@ jn_status jn_backbone_forward(jn_ctx* c, const jn_backbone* bb, const jn_packed*
   }
   JN_TRACED(c, JN_OP_RMSNORM, T, d, 0, norm(sd, bb->gf, hidden), "final rmsnorm");
   return JN_OK;
+}
+
+// --------------------------------------- queries and keys: norm, rotation ---
+
+extern "C++" {
+namespace {
+
+// Allocations of the host's own may fail: nothing is thrown out of a C entry.
+template <typename F>
+jn_status guarded(jn_ctx* c, F&& f) {
+  try {
+    return f();
+  } catch (const std::bad_alloc&) {
+    return c ? fail(c, JN_ENOSPACE, "out of host memory") : JN_ENOSPACE;
+  }
+}
+
+// Launches go to the context's stream, which belongs to its device.
+jn_status check_device(jn_ctx* c) {
+  int dev = -1;
+  JN_HIP(c, hipGetDevice(&dev), "hipGetDevice");
+  if (dev != c->device) return fail(c, JN_EINVAL, "device %d is current, the context is of device %d", dev, c->device);
+  return JN_OK;
+}
+
+jn_status qk_shape(jn_ctx* c, const jn_qk_args* a, bool back, QkShape* q) {
+  if (!a) return fail(c, JN_EINVAL, "null arguments");
+  if (a->rows < 0 || a->n_heads < 0 || a->n_kv_heads < 0 || (int64_t)a->n_heads + a->n_kv_heads < 1)
+    return fail(c, JN_EINVAL, "rows must be >= 0 and there must be a head");
+  if (a->head_dim < 16 || a->head_dim > 256 || a->head_dim % 16 != 0)
+    return fail(c, JN_EUNSUPPORTED, "head_dim %d not a multiple of 16 in [16, 256]", a->head_dim);
+  const int64_t heads = (int64_t)a->n_heads + a->n_kv_heads, width = heads * a->head_dim;
+  if (heads > 65536) return fail(c, JN_ESHAPE, "%lld heads", (long long)heads);
+  if (a->rows >= (1 << 28)) return fail(c, JN_ESHAPE, "%d rows exceed one launch's grid", a->rows);
+  const bool reads = !back || a->gq != nullptr;  // x
+  const int64_t ld_in = reads ? a->ld_in : width, ld_grad = back ? a->ld_grad : width;
+  if (std::min({ld_in, a->ld_out, ld_grad}) < width)
+    return fail(c, JN_EINVAL, "rows of %lld elements hold no %lld", (long long)std::min({ld_in, a->ld_out, ld_grad}),
+                (long long)width);
+  if ((ld_in | a->ld_out | ld_grad) % 8 != 0) return fail(c, JN_EUNSUPPORTED, "row strides not multiples of 8");
+  if ((a->gq == nullptr) != (a->gk == nullptr)) return fail(c, JN_EINVAL, "norms need both gains");
+  if (((uintptr_t)a->gq | (uintptr_t)a->gk) % 16 != 0) return fail(c, JN_EUNSUPPORTED, "gains not 16-byte aligned");
+  if (a->gq && !(a->eps > 0.f)) return fail(c, JN_EINVAL, "eps must be > 0");
+  if (!(a->rope_theta >= 0.f) || std::isinf(a->rope_theta)) return fail(c, JN_EINVAL, "rope_theta must be >= 0");
+  if (!a->gq && !(a->rope_theta > 0.f)) return fail(c, JN_EINVAL, "neither norms nor a rotation");
+  const jn_status st = check_axes(c, a->rope_axes, a->rope_interleaved, a->rope_sections, a->head_dim);
+  if (st != JN_OK) return st;
+  if (a->rope_theta > 0.f && a->rows > 0 && (!a->pos || (uintptr_t)a->pos % 4 != 0))
+    return fail(c, JN_EINVAL, "a rotation needs positions");
+  *q = QkShape{};
+  q->rows = a->rows;
+  q->heads = a->n_heads;
+  q->kv = a->n_kv_heads;
+  q->hd = a->head_dim;
+  q->ldx = ld_in;
+  q->ldy = a->ld_out;
+  q->ldd = ld_grad;
+  q->gq = (const uint16_t*)a->gq;
+  q->gk = (const uint16_t*)a->gk;
+  q->eps = a->eps;
+  if (a->rope_theta > 0.f) {
+    q->pos = a->pos;
+    qk_pairs(q, a->rope_theta, a->rope_axes, a->rope_interleaved, a->rope_sections);
+  }
+  return JN_OK;
+}
+
+}  // namespace
+}
+
+jn_status jn_qk_norm_rope(jn_ctx* c, const jn_qk_args* a, const void* x, void* y) {
+  if (!c) return JN_EINVAL;
+  QkShape q;
+  jn_status st = qk_shape(c, a, false, &q);
+  if (st != JN_OK) return st;
+  if (a->rows == 0) return JN_OK;
+  if (!x || !y) return fail(c, JN_EINVAL, "null rows");
+  if (((uintptr_t)x | (uintptr_t)y) % 16 != 0) return fail(c, JN_EUNSUPPORTED, "rows not 16-byte aligned");
+  if (x == y && a->ld_in != a->ld_out) return fail(c, JN_EINVAL, "in place with two strides");
+  if ((st = check_device(c)) != JN_OK) return st;
+  JN_TRACED(c, JN_OP_QK, a->rows, (a->n_heads + a->n_kv_heads) * a->head_dim, 0,
+            launch_qk_fwd(c->stream, q, (const uint16_t*)x, (uint16_t*)y), "head norms and rotation");
+  return JN_OK;
+}
+
+jn_status jn_qk_norm_rope_workspace_size(const jn_qk_args* a, size_t* bytes) {
+  if (!a || !bytes || a->rows < 0 || a->head_dim < 1 || a->head_dim > 256) return JN_EINVAL;
+  *bytes = a->gq ? (size_t)qk_bwd_blocks(a->rows) * 2 * a->head_dim * sizeof(float) : 0;
+  return JN_OK;
+}
+
+jn_status jn_qk_norm_rope_bwd(jn_ctx* c, const jn_qk_args* a, const void* x, const void* dy, void* dx, float* dgq,
+                              float* dgk, void* ws, size_t ws_bytes) {
+  if (!c) return JN_EINVAL;
+  QkShape q;
+  jn_status st = qk_shape(c, a, true, &q);
+  if (st != JN_OK) return st;
+  const bool norm = a->gq != nullptr;
+  if (a->rows > 0 && (!dy || !dx || (norm && !x))) return fail(c, JN_EINVAL, "null rows");
+  if (((uintptr_t)x | (uintptr_t)dy | (uintptr_t)dx) % 16 != 0)
+    return fail(c, JN_EUNSUPPORTED, "rows not 16-byte aligned");
+  if (a->rows > 0 && ((dx == dy && q.ldd != q.ldy) || (norm && dx == x && q.ldd != q.ldx)))
+    return fail(c, JN_EINVAL, "in place with two strides");
+  if (norm && (!dgq || !dgk || ((uintptr_t)dgq | (uintptr_t)dgk) % 4 != 0))
+    return fail(c, JN_EINVAL, "norms need dgq and dgk");
+  size_t need = 0;
+  jn_qk_norm_rope_workspace_size(a, &need);
+  if (need > 0 && (!ws || ws_bytes < need)) return fail(c, JN_ENOSPACE, "workspace %zu B < %zu B", ws ? ws_bytes : 0, need);
+  if (need > 0 && (uintptr_t)ws % 16 != 0) return fail(c, JN_EUNSUPPORTED, "workspace not 16-byte aligned");
+  if ((st = check_device(c)) != JN_OK) return st;
+  if (a->rows == 0 && !norm) return JN_OK;
+  JN_TRACED(c, JN_OP_QK, a->rows, (a->n_heads + a->n_kv_heads) * a->head_dim, 1,
+            launch_qk_bwd(c->stream, q, (const uint16_t*)x, (const uint16_t*)dy, (uint16_t*)dx, (float*)ws, dgq, dgk),
+            "head norm and rotation gradients");
+  return JN_OK;
+}
+
+// ----------------------------------------------------------- token heads ---
+
+extern "C++" {
+namespace {
+
+constexpr int64_t kTokPieceBytes = JN_TOKEN_PIECE_BYTES;
+
+struct TokSet {  // one grouped launch
+  int epi = 0, trans = 0;
+  size_t at = 0;  // of its problems in the table
+  int32_t n = 0;
+  TokTiles tiles;
+};
+
+// Workspace offsets, the device table (descriptors, then the problems of every
+// launch) and the launches of a token-head call.  With `ws` null only the sizes.
+struct TokPlan {
+  int32_t N = 0;
+  size_t table = 0, h = 0, labels = 0, zlab = 0, inv = 0, rows = 0, part = 0, index = 0, piece = 0, acc = 0, total = 0;
+  bool dh = false, split = false;  // row gradients wanted; they are summed over pieces
+  std::vector<char> bytes;
+  TokSet scores;
+  std::vector<TokSet> pieces;  // logit gradients, weight gradients and, wanted, row gradients of every piece
+};
+
+inline int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
+
+// The entries as the plan reads them, training and decoding alike.
+struct TokEntry {
+  int32_t n;
+  const int32_t *rows, *targets;
+  float *logp, *loss;
+  int32_t* token;
+  void *dW, *dh;
+};
+
+jn_status check_tokens(jn_ctx* c, int32_t d, const jn_token_head* heads, const std::vector<TokEntry>& io, bool train) {
+  if (d < 64 || d > 8192 || d % 64 != 0) return fail(c, JN_EUNSUPPORTED, "d %d not a multiple of 64 in [64, 8192]", d);
+  int64_t N = 0;
+  for (size_t g = 0; g < io.size(); ++g) {
+    const TokEntry& e = io[g];
+    if (heads[g].vocab < 1 || heads[g].vocab > (1 << 24))
+      return fail(c, JN_ESHAPE, "tenant %zu: vocabulary of %d", g, heads[g].vocab);
+    if (e.n < 0 || e.n > (1 << 20)) return fail(c, JN_ESHAPE, "tenant %zu: %d entries", g, e.n);
+    N += e.n;
+    if (2 * ((int64_t)e.n + 64) * d > 0x7fffffff)
+      return fail(c, JN_ESHAPE, "tenant %zu: %d entries of %d features exceed 2 GiB", g, e.n, d);
+    if (!heads[g].W || (train && (!e.dW || !e.loss))) return fail(c, JN_EINVAL, "tenant %zu: null weight or output", g);
+    if (((uintptr_t)heads[g].W | (uintptr_t)e.dW | (uintptr_t)e.dh) % 16 != 0)
+      return fail(c, JN_EUNSUPPORTED, "tenant %zu: W, dW and dh must be 16-byte aligned", g);
+    if (e.n > 0 && (!e.rows || !e.logp || (train ? !e.targets : !e.token)))
+      return fail(c, JN_EINVAL, "tenant %zu: null entries", g);
+    if (((uintptr_t)e.rows | (uintptr_t)e.targets | (uintptr_t)e.logp | (uintptr_t)e.loss | (uintptr_t)e.token) % 4 != 0)
+      return fail(c, JN_EUNSUPPORTED, "tenant %zu: entries must be 4-byte aligned", g);
+  }
+  if (N > (1 << 24)) return fail(c, JN_ESHAPE, "%lld entries", (long long)N);
+  return JN_OK;
+}
+
+jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std::vector<TokEntry>& io, bool train,
+                     char* ws, TokPlan* P) {
+  const int32_t G = (int32_t)io.size();
+  int64_t N = 0, logits = 0;
+  std::vector<int32_t> first(G);
+  for (int32_t g = 0; g < G; ++g) {
+    first[g] = (int32_t)N;
+    N += io[g].n;
+    logits += (int64_t)io[g].n * up(heads[g].vocab, 64);
+    P->dh = P->dh || (io[g].dh != nullptr && io[g].n > 0);
+  }
+  P->N = (int32_t)N;
+  // pieces of the vocabulary, as many for every tenant, in whole ring tiles
+  const int64_t K = train && N > 0 ? std::max<int64_t>(1, (2 * logits + kTokPieceBytes - 1) / kTokPieceBytes) : 0;
+  std::vector<int64_t> width(G), pat(G);
+  int64_t piece = 0, pieces = 0;
+  for (int32_t g = 0; g < G; ++g) {
+    if (io[g].n == 0 || K == 0) continue;
+    width[g] = std::min<int64_t>(up((heads[g].vocab + K - 1) / K, 256), up(heads[g].vocab, 64));
+    const int64_t most = 0x7fffffff / (2 * d) / 256 * 256 - 256;  // a transposed panel of W within 32-bit offsets
+    width[g] = std::min(width[g], most);
+    pat[g] = piece;
+    piece += up(2 * io[g].n * width[g], 256);
+    pieces = std::max(pieces, (heads[g].vocab + width[g] - 1) / width[g]);
+  }
+  P->split = P->dh && pieces > 1;
+  // the products, sized first with their pointers left open
+  std::vector<GemmArgs> probs;
+  auto add = [&](TokSet* set, int epi, int trans, std::vector<GemmArgs>& v) -> jn_status {
+    set->epi = epi;
+    set->trans = trans;
+    set->n = (int32_t)v.size();
+    set->at = probs.size();
+    set->tiles = gemm_tokens_prepare(epi, trans, v.data(), set->n);
+    if (set->tiles.total < 0) return fail(c, JN_ESHAPE, "a product of the token heads exceeds one launch's grid");
+    probs.insert(probs.end(), v.begin(), v.end());
+    return JN_OK;
+  };
+  std::vector<GemmArgs> v;
+  std::vector<int32_t> blocks(G);
+  std::vector<int64_t> parts(G);
+  int64_t all_parts = 0;
+  for (int32_t g = 0; g < G; ++g) {
+    if (io[g].n == 0) continue;
+    GemmArgs q{};
+    q.W = (const uint16_t*)heads[g].W;
+    q.ldx = q.ldw = d;
+    q.ldc = io[g].n;
+    q.M = io[g].n;
+    q.N = heads[g].vocab;
+    q.K = d;
+    v.push_back(q);
+  }
+  if (!v.empty()) {
+    jn_status st = add(&P->scores, train ? EPI_SOFTMAX : EPI_GREEDY, 0, v);
+    if (st != JN_OK) return st;
+    const int32_t block = gemm_tokens_block(P->scores.tiles.shape);
+    for (int32_t g = 0; g < G; ++g) {
+      if (io[g].n == 0) continue;
+      blocks[g] = tok_blocks(heads[g].vocab, block);
+      parts[g] = all_parts;
+      all_parts += (int64_t)blocks[g] * io[g].n;
+    }
+  }
+  size_t o = 0;
+  auto take = [&](int64_t bytes) {
+    const size_t at = o;
+    o = align_up(o + (size_t)bytes, 256);
+    return at;
+  };
+  P->h = take(2 * N * d);
+  P->labels = take(4 * N);
+  P->inv = take(4 * (int64_t)G);
+  if (train) {
+    P->zlab = take(4 * N);
+    P->rows = take((int64_t)sizeof(TokRow) * N);
+    // the parts are joined before the first piece is written
+    P->part = P->piece = take(std::max<int64_t>((int64_t)sizeof(TokPart) * all_parts, piece));
+    if (P->split) P->acc = take(4 * N * d);
+  } else {
+    P->part = take((int64_t)sizeof(TokPart) * all_parts);
+    P->index = take(4 * all_parts);
+  }
+  int32_t j = 0;
+  for (int32_t g = 0; g < G; ++g) {
+    if (io[g].n == 0) continue;
+    GemmArgs& q = probs[P->scores.at + j++];
+    q.X = (const uint16_t*)(ws + P->h) + (int64_t)first[g] * d;
+    q.C = ws + P->part + sizeof(TokPart) * parts[g];
+    if (train) {
+      q.W2 = (const uint16_t*)(ws + P->labels + 4 * (size_t)first[g]);
+      q.aux = (float*)(ws + P->zlab) + first[g];
+    } else {
+      q.aux = (float*)(ws + P->index) + parts[g];
+    }
+  }
+  for (int64_t k = 0; k < pieces; ++k) {
+    std::vector<GemmArgs> dz, dw, dx;
+    for (int32_t g = 0; g < G; ++g) {
+      const int64_t v0 = k * width[g];
+      if (io[g].n == 0 || v0 >= heads[g].vocab) continue;
+      const int32_t n = io[g].n, cols = (int32_t)std::min(width[g], heads[g].vocab - v0);
+      uint16_t* const grad = (uint16_t*)(ws + P->piece + pat[g]);
+      const uint16_t* const rows = (const uint16_t*)(ws + P->h) + (int64_t)first[g] * d;
+      const uint16_t* const W = (const uint16_t*)heads[g].W + v0 * d;
+      GemmArgs q{};
+      q.X = rows;
+      q.W = W;
+      q.C = grad;
+      q.aux = (float*)(ws + P->rows + sizeof(TokRow) * first[g]);
+      q.ldx = q.ldw = d;
+      q.ldc = up(cols, 64);
+      q.M = n;
+      q.N = cols;
+      q.K = d;
+      q.split_c = v0;
+      dz.push_back(q);
+      GemmArgs w{};  // dW piece = grad^T rows
+      w.X = grad;
+      w.W = rows;
+      w.C = (uint16_t*)io[g].dW + v0 * d;
+      w.aux = (float*)(ws + P->inv) + g;
+      w.ldx = up(cols, 64);
+      w.ldw = w.ldc = d;
+      w.M = cols;
+      w.N = d;
+      w.K = n;
+      dw.push_back(w);
+      if (!io[g].dh) continue;
+      GemmArgs r{};  // dh (+)= grad W piece
+      r.X = grad;
+      r.W = W;
+      r.aux = P->split ? nullptr : w.aux;  // (a residual add without aux is in place)
+      r.C = P->split ? (void*)((float*)(ws + P->acc) + (int64_t)first[g] * d) : io[g].dh;
+      r.ldx = up(cols, 64);
+      r.ldw = r.ldc = d;
+      r.M = n;
+      r.N = d;
+      r.K = cols;
+      dx.push_back(r);
+    }
+    TokSet a, b, e;
+    jn_status st = add(&a, EPI_DLOGIT, 0, dz);
+    if (st == JN_OK) st = add(&b, EPI_SCALED_BF16, GEMM_TRANS_X | GEMM_TRANS_W, dw);
+    if (st == JN_OK && !dx.empty())
+      st = add(&e, !P->split ? EPI_SCALED_BF16 : k == 0 ? EPI_F32 : EPI_RESID_F32, GEMM_TRANS_W, dx);
+    if (st != JN_OK) return st;
+    P->pieces.push_back(a);
+    P->pieces.push_back(b);
+    if (!dx.empty()) P->pieces.push_back(e);
+  }
+  // descriptors, then problems
+  P->table = take((int64_t)(sizeof(TokDesc) * G + sizeof(GemmArgs) * probs.size()));
+  P->total = o;
+  P->bytes.resize(sizeof(TokDesc) * G + sizeof(GemmArgs) * probs.size());
+  TokDesc* const desc = (TokDesc*)P->bytes.data();
+  for (int32_t g = 0; g < G; ++g)
+    desc[g] = TokDesc{io[g].rows, io[g].targets, io[g].logp, io[g].loss, io[g].token,
+                      P->split ? (uint16_t*)io[g].dh : nullptr, (const TokPart*)(ws + P->part) + parts[g],
+                      (const int32_t*)(ws + P->index) + parts[g], io[g].n, first[g], heads[g].vocab, blocks[g]};
+  if (!probs.empty()) std::memcpy(P->bytes.data() + sizeof(TokDesc) * G, probs.data(), sizeof(GemmArgs) * probs.size());
+  return JN_OK;
+}
+
+jn_status tokens_run(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const jn_token_head* heads,
+                     const std::vector<TokEntry>& io, bool train, void* ws, size_t ws_bytes) {
+  const int32_t G = (int32_t)io.size();
+  jn_status st = check_tokens(c, d, heads, io, train);
+  if (st != JN_OK) return st;
+  TokPlan P;
+  if ((st = token_plan(c, d, heads, io, train, (char*)ws, &P)) != JN_OK) return st;
+  if (T < 0 || (T > 0 && !hidden)) return fail(c, JN_EINVAL, "null feature or negative rows");
+  if (!ws || ws_bytes < P.total) return fail(c, JN_ENOSPACE, "workspace %zu B < %zu B", ws ? ws_bytes : 0, P.total);
+  if ((uintptr_t)ws % 256 != 0 || (uintptr_t)hidden % 16 != 0)
+    return fail(c, JN_EUNSUPPORTED, "workspace must be 256-byte and the feature 16-byte aligned");
+  if ((st = check_device(c)) != JN_OK) return st;
+  if (P.N == 0 && !train) return JN_OK;
+  hipStream_t s = c->stream;
+  char* const w = (char*)ws;
+  const TokDesc* const desc = (const TokDesc*)(w + P.table);
+  const GemmArgs* const probs = (const GemmArgs*)(desc + G);
+  uint16_t* const h = (uint16_t*)(w + P.h);
+  int32_t* const labels = (int32_t*)(w + P.labels);
+  float* const inv = (float*)(w + P.inv);
+  float* const zlab = (float*)(w + P.zlab);
+  auto product = [&](const TokSet& t) { return launch_gemm_tokens(s, t.epi, t.trans, probs + t.at, t.n, t.tiles); };
+  JN_HIP(c, launch_tok_table(s, w + P.table, P.bytes.data(), P.bytes.size()), "token table");
+  JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 0,
+            launch_tok_gather(s, desc, G, P.N, hidden, T, d, h, labels, train ? inv : nullptr), "token rows");
+  if (P.scores.n > 0)
+    JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, heads[0].vocab, d, product(P.scores), "token scores");
+  if (!train) {
+    JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, heads[0].vocab, 0, launch_tok_pick(s, desc, G, P.N, labels), "token pick");
+    return JN_OK;
+  }
+  if (P.N > 0)
+    JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, heads[0].vocab, 0,
+              launch_tok_join(s, desc, G, P.N, labels, zlab, (TokRow*)(w + P.rows)), "token softmax");
+  for (const TokSet& t : P.pieces)
+    JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, heads[0].vocab, d, product(t), "token gradients");
+  for (int32_t g = 0; g < G; ++g)
+    if (io[g].n == 0)
+      JN_HIP(c, launch_tok_zero(s, io[g].dW, 2 * (size_t)heads[g].vocab * d), "empty tenant's gradient");
+  JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 1,
+            launch_tok_finish(s, desc, G, P.N, inv, P.split ? (const float*)(w + P.acc) : nullptr, d), "token loss");
+  return JN_OK;
+}
+
+std::vector<TokEntry> entries(const jn_token_io* io, int32_t G) {
+  std::vector<TokEntry> v(G);
+  for (int32_t g = 0; g < G; ++g)
+    v[g] = TokEntry{io[g].n, io[g].rows, io[g].targets, io[g].logp, io[g].loss, nullptr, io[g].dW, io[g].dh};
+  return v;
+}
+
+std::vector<TokEntry> entries(const jn_token_pick* io, int32_t G) {
+  std::vector<TokEntry> v(G);
+  for (int32_t g = 0; g < G; ++g)
+    v[g] = TokEntry{io[g].n, io[g].rows, nullptr, io[g].logp, nullptr, io[g].token, nullptr, nullptr};
+  return v;
+}
+
+template <typename IO>
+jn_status tokens_size(int32_t d, const jn_token_head* heads, const IO* io, int32_t G, bool train, size_t* bytes) {
+  if (!heads || !io || !bytes || G < 1 || G > (1 << 16)) return JN_EINVAL;
+  return guarded(nullptr, [&]() {
+    const std::vector<TokEntry> e = entries(io, G);
+    jn_status st = check_tokens(nullptr, d, heads, e, train);
+    if (st != JN_OK) return st;
+    TokPlan P;
+    if ((st = token_plan(nullptr, d, heads, e, train, nullptr, &P)) == JN_OK) *bytes = P.total;
+    return st;
+  });
+}
+
+}  // namespace
+}
+
+jn_status jn_tokens_workspace_size(int32_t d, const jn_token_head* heads, const jn_token_io* io, int32_t G,
+                                   size_t* bytes) {
+  return tokens_size(d, heads, io, G, true, bytes);
+}
+
+jn_status jn_tenant_tokens_fwd_bwd(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const jn_token_head* heads,
+                                   const jn_token_io* io, int32_t G, void* ws, size_t ws_bytes) {
+  if (!c) return JN_EINVAL;
+  if (!heads || !io || G < 1 || G > (1 << 16)) return fail(c, JN_EINVAL, "null token heads or no tenant");
+  return guarded(c, [&]() { return tokens_run(c, hidden, T, d, heads, entries(io, G), true, ws, ws_bytes); });
+}
+
+jn_status jn_tokens_decode_workspace_size(int32_t d, const jn_token_head* heads, const jn_token_pick* io, int32_t G,
+                                          size_t* bytes) {
+  return tokens_size(d, heads, io, G, false, bytes);
+}
+
+jn_status jn_tenant_tokens_decode(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const jn_token_head* heads,
+                                  const jn_token_pick* io, int32_t G, void* ws, size_t ws_bytes) {
+  if (!c) return JN_EINVAL;
+  if (!heads || !io || G < 1 || G > (1 << 16)) return fail(c, JN_EINVAL, "null token heads or no tenant");
+  return guarded(c, [&]() { return tokens_run(c, hidden, T, d, heads, entries(io, G), false, ws, ws_bytes); });
 }
 
 // ----------------------------------------------------------------- heads ---

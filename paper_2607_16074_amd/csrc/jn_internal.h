@@ -75,6 +75,27 @@ hipError_t launch_rmsnorm_f32in(hipStream_t s, const float* x, const void* g, vo
 hipError_t launch_rmsnorm_split(hipStream_t s, float* x, const float* part, int32_t S, const void* g, void* h,
                                 int32_t rows, int32_t d, float eps);
 
+// Head norms and rotation of the q and k heads of rows of x (jn_qk_norm_rope):
+// gq null: no norm; pos null: no rotation.  Passed to the kernels by value.
+struct QkShape {
+  int32_t rows, heads, kv, hd;
+  int64_t ldx, ldy, ldd;        // elements between rows: input, rotated rows, gradient of the input
+  const uint16_t* gq;
+  const uint16_t* gk;
+  const int32_t* pos;           // [rows][axes]
+  float eps;
+  int32_t axes;
+  double freq[128];             // turns per position of pair i
+  uint8_t axis[128];            // its position axis
+};
+constexpr int32_t kQkFewRows = 1024;    // below, a row's heads are shared by several wavefronts
+constexpr int32_t kQkBwdBlocks = 1024;  // most workgroups of the gradient, hence of its partial gain sums
+int32_t qk_bwd_blocks(int32_t rows);
+hipError_t launch_qk_fwd(hipStream_t s, const QkShape& a, const uint16_t* x, uint16_t* y);
+// part: [qk_bwd_blocks][2][hd]; rows may be 0 (gain gradients become zero).
+hipError_t launch_qk_bwd(hipStream_t s, const QkShape& a, const uint16_t* x, const uint16_t* dy, uint16_t* dx,
+                         float* part, float* dgq, float* dgk);
+
 enum GemmEpi : int32_t {
   EPI_BF16 = 0,          // C bf16 = acc
   EPI_GELU_BF16 = 1,     // C bf16 = gelu(acc)
@@ -82,7 +103,12 @@ enum GemmEpi : int32_t {
   EPI_GEGLU_BF16 = 3,    // weights gate|up interleaved at load; C bf16 = gelu(gate) * up
   EPI_F32 = 4,           // C fp32 = acc
   EPI_GELU_SAVE = 5,     // aux fp32 = acc; C bf16 = gelu(acc)
-  EPI_GELUGRAD_BF16 = 6  // C bf16 = acc * gelu'(aux fp32)
+  EPI_GELUGRAD_BF16 = 6, // C bf16 = acc * gelu'(aux fp32)
+  // token heads (launch_gemm_tokens): columns are a vocabulary, rows targets
+  EPI_SOFTMAX = 7,       // C TokPart [column block][M] of the block's columns; aux[m] = acc of column labels[m]
+  EPI_GREEDY = 8,        // the same with the columns' indices in `aux` (int32 [column block][M]), no labels
+  EPI_DLOGIT = 9,        // C bf16 = softmax gradient from the rows' TokRow (aux), zero in columns N .. ldc - 1
+  EPI_SCALED_BF16 = 10   // C bf16 = acc * aux[0]
 };
 
 // Operand layouts of a grouped problem (GemmArgs::trans): X stored [K][M]
@@ -94,7 +120,7 @@ constexpr int GEMM_TRANS_X = 1, GEMM_TRANS_W = 2;
 struct GemmArgs {
   const uint16_t* X;
   const uint16_t* W;
-  const uint16_t* W2;   // GeGLU up weights
+  const uint16_t* W2;   // GeGLU up weights; EPI_SOFTMAX: labels, int32 [M] (no column: outside [0, N))
   void* C;
   float* aux;           // GELU pre-activation (saved or read); residual source (null: C)
   int64_t ldx, ldw, ldc, ldaux;
@@ -102,7 +128,8 @@ struct GemmArgs {
   int32_t tiles_m, tiles_n, tile_start;  // filled by the launchers
   int32_t trans;        // GEMM_TRANS_* bits (grouped launches only)
   int64_t split_c;      // split-K: elements between the fp32 partial outputs of
-                        // consecutive K ranges; 0 when unsplit
+                        // consecutive K ranges; 0 when unsplit.  EPI_DLOGIT:
+                        // the vocabulary's index of column 0
 };
 
 // Grouped launch over nprob problems sharing one epilogue: the host fills
@@ -127,6 +154,37 @@ hipError_t launch_gemm_grouped(hipStream_t s, int epi, const GemmArgs* dprobs, i
 bool gemm_grad_pair_ok(int epi, int dshape, int wshape, int32_t wtiles);
 hipError_t launch_gemm_grad_pair(hipStream_t s, int epi, const GemmArgs* dprobs, int32_t nd, int32_t td,
                                  const GemmArgs* wprobs, int32_t nw, int32_t tw);
+
+// Softmax of a row over some columns: their largest value and the sum of
+// exp(z - largest) over the others (the largest is left out, so that log1p of the
+// sum keeps the log-probabilities of sure rows).  No column: {-inf, 0}.
+struct TokPart {
+  float m, rest;
+};
+// A target row as its logits' gradient needs it: p = exp2(z log2(e) - lse2), times
+// `live` (0 or 1), and `own` = p - 1 from logp in the target's column.  Dividing by
+// the number of targets is left to the products' results: bf16 holds the gradient
+// of an unlikely target, nearly -1 in every row, all but exactly, while a common
+// factor's rounding would be off by the same half step in all of them.
+struct TokRow {
+  float lse2, live, own;
+  int32_t label;        // -1: the row has no target, and live and own are 0
+};
+
+// Grouped launches of a token head's products, as above but with any N for
+// EPI_SOFTMAX, EPI_GREEDY and EPI_DLOGIT (trans 0), and any K with GEMM_TRANS_W
+// where the columns K .. of X up to a multiple of 64 are zeros (EPI_SCALED_BF16,
+// EPI_F32, EPI_RESID_F32) or with both operands transposed (EPI_SCALED_BF16).  prepare: tile
+// ranges and shape, or a total of -1.  Column blocks of EPI_SOFTMAX and EPI_GREEDY are
+// gemm_tokens_block(shape) columns, tok_blocks of them per problem.
+struct TokTiles {
+  int32_t total = -1, shape = 0;
+};
+TokTiles gemm_tokens_prepare(int epi, int trans, GemmArgs* probs, int32_t nprob);
+int32_t gemm_tokens_block(int shape);
+inline int32_t tok_blocks(int32_t vocab, int32_t block) { return (vocab + 2 * block - 1) / (2 * block) * 2; }
+hipError_t launch_gemm_tokens(hipStream_t s, int epi, int trans, const GemmArgs* dprobs, int32_t nprob,
+                              const TokTiles& t);
 
 // C[M][N] (+)= epi(A[M][K] * B[N][K]^T); A, B bf16 row-major with leading
 // dims lda, ldb (elements); for EPI_GEGLU_BF16, B is w_gate and B2 is w_up,
@@ -220,6 +278,36 @@ struct HeadLaunch {
 };
 hipError_t launch_head_gemm(hipStream_t s, const HeadGemm* descs, const HeadTile* tiles, const HeadLaunch& n,
                             int32_t tms, const int32_t* tenant_sample_off, bool forward);
+
+// ---- token heads (k_heads.hip) ----
+// A tenant of a token-head call; its targets are rows [first, first + n) of the
+// call's.  Device table, as are the problems of its products.
+struct TokDesc {
+  const int32_t* rows;     // [n] rows of the shared feature
+  const int32_t* targets;  // [n], null when decoding
+  float* logp;             // [n]
+  float* loss;             // [1]
+  int32_t* token;          // [n], decoding
+  uint16_t* dh;            // [n][d] or null
+  const TokPart* part;     // [blocks][n]
+  const int32_t* index;    // [blocks][n], decoding
+  int32_t n, first, vocab, blocks;
+};
+// Table bytes by value in kernel arguments: no staging memory, so that a captured
+// call replays.
+hipError_t launch_tok_table(hipStream_t s, void* dst, const void* src, size_t bytes);
+// h[i] = hidden[row of target i], zeros where it has none; labels[i] its token or
+// -1 (decoding: 0 where the row exists); inv[g] = 1 / targets of tenant g.
+hipError_t launch_tok_gather(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const void* hidden, int32_t T,
+                             int32_t width, uint16_t* h, int32_t* labels, float* inv);
+// Parts of every row joined: logp, and the rows' TokRow; decoding: token and logp.
+hipError_t launch_tok_join(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const int32_t* labels,
+                           const float* zlab, TokRow* rows);
+hipError_t launch_tok_pick(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const int32_t* labels);
+// loss[g] = -(sum of logp) inv[g], and dh = acc inv[g] (acc null: dh is written already).
+hipError_t launch_tok_finish(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const float* inv, const float* acc,
+                             int32_t width);
+hipError_t launch_tok_zero(hipStream_t s, void* p, size_t bytes);
 
 // ---- action expert (k_expert.hip) ----
 // dst[r][c] = cvt(src[r][c]) for r < src_rows, c < src_cols, else 0; r < rows, c < cols.

@@ -183,7 +183,11 @@ __global__ __launch_bounds__(256) void splitk_reduce_kernel(const float* __restr
 // mostly idle): 21.1 -> 19.8, 25.3 -> 23.9, 21.4 -> 20.4 and 33.7 -> 24.0 us.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-constexpr bool epi_bf16(int epi) { return epi == EPI_BF16 || epi == EPI_GELU_BF16 || epi == EPI_GEGLU_BF16; }
+constexpr bool epi_bf16(int epi) {
+  return epi == EPI_BF16 || epi == EPI_GELU_BF16 || epi == EPI_GEGLU_BF16 || epi == EPI_DLOGIT ||
+         epi == EPI_SCALED_BF16;
+}
+constexpr bool epi_softmax(int epi) { return epi == EPI_SOFTMAX || epi == EPI_GREEDY; }
 constexpr bool epi_reads(int epi) { return epi == EPI_RESID_F32 || epi == EPI_GELUGRAD_BF16; }
 
 // Sizes of the 16-bit epilogue of a wave's part.
@@ -209,6 +213,16 @@ __device__ __forceinline__ void epilogue_bf16(const GemmArgs& g, const f32x4 (&a
   uint16_t* C = reinterpret_cast<uint16_t*>(g.C) + (int64_t)m * g.ldc + n;
   const int64_t step = RI * g.ldc;
   auto swz = [](int r) { return CH == 16 ? r & 15 : (r / (16 / CH)) & (CH - 1); };
+  const float alpha = EPI == EPI_SCALED_BF16 ? g.aux[0] : 1.f;
+  TokRow tr[EPI == EPI_DLOGIT ? TM : 1];
+  if constexpr (EPI == EPI_DLOGIT) {
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int32_t r = m0 + 16 * j + row;
+      tr[j] = reinterpret_cast<const TokRow*>(g.aux)[WHOLE ? r : min(r, g.M - 1)];
+      tr[j].label = tr[j].label < 0 ? -1 : tr[j].label - (int32_t)g.split_c - n0 - 4 * quad;  // from the lane's first column
+    }
+  }
   auto put = [&](int j) __attribute__((always_inline)) {  // blocks j .. j + NB - 1
 #pragma unroll
     for (int jj = 0; jj < NB; ++jj) {
@@ -218,7 +232,16 @@ __device__ __forceinline__ void epilogue_bf16(const GemmArgs& g, const f32x4 (&a
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float a = acc[i][j + jj][e];
-          v[e] = GLU ? gelu_fast_f(a) * acc[i + (GLU ? 1 : 0)][j + jj][e] : EPI == EPI_GELU_BF16 ? gelu_fast_f(a) : a;
+          if constexpr (EPI == EPI_DLOGIT) {
+            const TokRow& t = tr[j + jj];
+            v[e] = __builtin_amdgcn_exp2f(fmaf(a, 1.4426950408889634f, -t.lse2)) * t.live;
+            if (t.label == 16 * i + e) v[e] = t.own;
+            if (!WHOLE && n0 + 16 * i + 4 * quad + e >= g.N) v[e] = 0.f;
+          } else if constexpr (EPI == EPI_SCALED_BF16) {
+            v[e] = a * alpha;
+          } else {
+            v[e] = GLU ? gelu_fast_f(a) * acc[i + (GLU ? 1 : 0)][j + jj][e] : EPI == EPI_GELU_BF16 ? gelu_fast_f(a) : a;
+          }
         }
         const int chunk = 2 * (GLU ? i / 2 : i) + (quad >> 1);
         *reinterpret_cast<u32x2*>(stage + (16 * jj + row) * WC + (chunk ^ swz(row)) * 8 + (quad & 1) * 4) =
@@ -236,7 +259,8 @@ __device__ __forceinline__ void epilogue_bf16(const GemmArgs& g, const f32x4 (&a
     if (j + NB < TM) put(j + NB);  // (a wave's LDS operations stay in order)
 #pragma unroll
     for (int it = 0; it < NI; ++it)
-      if ((NB * 16 % RI == 0 || RI * it + rr < NB * 16) && (WHOLE || (m + 16 * j + RI * it < g.M && n < g.N)))
+      if ((NB * 16 % RI == 0 || RI * it + rr < NB * 16) &&
+          (WHOLE || (m + 16 * j + RI * it < g.M && n < (EPI == EPI_DLOGIT ? (int32_t)g.ldc : g.N))))
         *reinterpret_cast<u32x4*>(C + it * step) = v[it];
     C += NB * 16 * g.ldc;
   }
@@ -314,6 +338,82 @@ __device__ __forceinline__ void epilogue_f32(const GemmArgs& g, const f32x4 (&ac
   }
 }
 
+// Two parts of a softmax joined.
+__device__ __forceinline__ void tok_join(float& m, float& rest, float m2, float rest2) {
+  const float hi = __builtin_elementwise_maximum(m, m2), lo = __builtin_elementwise_minimum(m, m2);
+  const float base = hi == -INFINITY ? 0.f : hi;
+  const float small = 1.f + (m >= m2 ? rest2 : rest);
+  rest = (m >= m2 ? rest : rest2) + small * __builtin_amdgcn_exp2f((lo - base) * 1.4426950408889634f);
+  m = hi;
+}
+
+// Softmax parts of the wave's columns, one TokPart per token (and, GREEDY, the
+// lowest column of the largest value).  A lane owns 4 TN columns of a token:
+// rounds of pairwise maxima and minima leave the largest in v[0] and every
+// other value once among the minima, in as many operations as the sum with
+// the largest in it would take.  NaN comes through (IEEE maximum, minimum).
+template <int EPI, int TN, int TM, bool WHOLE>
+__device__ __forceinline__ void epilogue_softmax(const GemmArgs& g, const f32x4 (&acc)[TN][TM], int32_t m0, int32_t n0,
+                                                 int lane) {
+  constexpr int NV = 4 * TN;
+  static_assert((NV & (NV - 1)) == 0, "rounds of halves");
+  const int quad = lane >> 4, row = lane & 15;
+  const int64_t block = n0 / (16 * TN);
+  const int32_t own = n0 + 4 * quad;  // the lane's first column
+#pragma unroll
+  for (int j = 0; j < TM; ++j) {
+    const int32_t r = m0 + 16 * j + row;
+    const bool in = WHOLE || r < g.M;
+    float v[NV];
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * i + e] = WHOLE || own + 16 * i + e < g.N ? acc[i][j][e] : -INFINITY;
+    if constexpr (EPI == EPI_SOFTMAX) {
+      const int32_t label = in ? reinterpret_cast<const int32_t*>(g.W2)[r] - own : -1;
+      const bool here = label >= 0 && label < 16 * TN && (label & 15) < 4 && own + label < g.N;
+      if (__builtin_amdgcn_ballot_w64(here) != 0) {
+        float z = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) z = label == 16 * (k >> 2) + (k & 3) ? v[k] : z;
+        if (here) g.aux[r] = z;
+      }
+    }
+    // v[0 .. h) the winners so far, v[h .. 2h) what lost to them
+#pragma unroll
+    for (int h = NV / 2; h >= 1; h >>= 1)
+#pragma unroll
+      for (int k = 0; k < h; ++k) {
+        const float a = v[k], b = v[k + h];
+        v[k] = __builtin_elementwise_maximum(a, b);
+        v[k + h] = __builtin_elementwise_minimum(a, b);
+      }
+    float m = v[0], rest = 0.f;
+    const float base = (m == -INFINITY ? 0.f : m) * -1.4426950408889634f;
+#pragma unroll
+    for (int k = 1; k < NV; ++k) rest += __builtin_amdgcn_exp2f(fmaf(v[k], 1.4426950408889634f, base));
+    int32_t at = 0x7fffffff;
+    if constexpr (EPI == EPI_GREEDY) {
+#pragma unroll
+      for (int k = NV - 1; k >= 0; --k)
+        if ((WHOLE || own + 16 * (k >> 2) + (k & 3) < g.N) && acc[k >> 2][j][k & 3] == m) at = own + 16 * (k >> 2) + (k & 3);
+    }
+#pragma unroll
+    for (int o = 16; o <= 32; o <<= 1) {
+      const float m2 = __shfl_xor(m, o, kWave), rest2 = __shfl_xor(rest, o, kWave);
+      if constexpr (EPI == EPI_GREEDY) {
+        const int32_t at2 = __shfl_xor(at, o, kWave);
+        at = m2 > m ? at2 : m2 == m ? min(at, at2) : at;
+      }
+      tok_join(m, rest, m2, rest2);
+    }
+    if (quad == 0 && in) {
+      reinterpret_cast<TokPart*>(g.C)[block * g.ldc + r] = TokPart{m, rest};
+      if constexpr (EPI == EPI_GREEDY) reinterpret_cast<int32_t*>(g.aux)[block * g.ldc + r] = at;
+    }
+  }
+}
+
 // stage: 8 KB of the wave's own.  Returns whether the part lay inside the
 // output.  ONCE: fp32 results that no kernel reads next (weight gradients), stored
 // non-temporally so that the caches keep what the next launches read (16
@@ -323,7 +423,12 @@ __device__ __forceinline__ bool gemm_epilogue(const GemmArgs& g, const f32x4 (&a
                                               int32_t m0, int32_t n0, int lane) {
   const bool whole = m0 + 16 * TM <= g.M && n0 + (EPI == EPI_GEGLU_BF16 ? 8 : 16) * TN <= g.N;
   asm volatile("" : "+v"(lane));  // lane offsets are formed here, not held in registers through a loop over tiles
-  if constexpr (epi_bf16(EPI)) {
+  if constexpr (epi_softmax(EPI)) {
+    if (whole)
+      epilogue_softmax<EPI, TN, TM, true>(g, acc, m0, n0, lane);
+    else
+      epilogue_softmax<EPI, TN, TM, false>(g, acc, m0, n0, lane);
+  } else if constexpr (epi_bf16(EPI)) {
     if (whole)
       epilogue_bf16<EPI, TN, TM, true>(g, acc, stage, m0, n0, lane);
     else
@@ -1495,6 +1600,99 @@ hipError_t launch_gemm_grad_pair(hipStream_t s, int epi, const GemmArgs* dprobs,
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
+}
+
+// ---- products of the token heads ----
+
+int32_t gemm_tokens_block(int shape) { return kShapes[shape].bn / 2; }
+
+// Shapes that are launched: a transposed operand's tile side is a multiple of
+// 128, and a softmax part's columns per lane a power of two.
+static bool tokens_shape_ok(int trans, int t) {
+  if (t == 0) return true;
+  return trans == (GEMM_TRANS_X | GEMM_TRANS_W) ? t == k128Shape : trans == GEMM_TRANS_W ? t == 4 : t == 4 || t == 5;
+}
+
+TokTiles gemm_tokens_prepare(int epi, int trans, GemmArgs* probs, int32_t nprob) {
+  TokTiles out;
+  double best = 1e300;
+  for (int t = 0; t <= k128Shape; ++t) {
+    if (!tokens_shape_ok(trans, t)) continue;
+    int64_t tiles = 0, work = 0;
+    for (int32_t p = 0; p < nprob; ++p) {
+      const int64_t n = (int64_t)((probs[p].M + kShapes[t].bm - 1) / kShapes[t].bm) *
+                        ((probs[p].N + kShapes[t].bn - 1) / kShapes[t].bn);
+      tiles += n;
+      work += n * ((probs[p].K + kBK - 1) / kBK);
+    }
+    if (tiles <= 0 || tiles > (int64_t)kMostBlocks) continue;
+    const double us = tiles_time(epi == EPI_DLOGIT ? EPI_GELU_BF16 : epi, tiles, (double)work / tiles, t);
+    if (us < best * 0.999) {
+      best = us;
+      out.shape = t;
+      out.total = (int32_t)tiles;
+    }
+  }
+  if (out.total < 0) return out;
+  const TileShape& T = kShapes[out.shape];
+  int32_t at = 0;
+  for (int32_t p = 0; p < nprob; ++p) {
+    GemmArgs& g = probs[p];
+    if (g.M <= 0 || g.N <= 0 || g.K <= 0 || (trans == 0 && g.K % kBK != 0) || (trans != 0 && g.N % 32 != 0)) {
+      out.total = -1;
+      return out;
+    }
+    g.trans = trans;
+    g.tiles_m = (g.M + T.bm - 1) / T.bm;
+    g.tiles_n = (g.N + T.bn - 1) / T.bn;
+    g.tile_start = at;
+    at += g.tiles_m * g.tiles_n;
+  }
+  return out;
+}
+
+template <int EPI, int TR>
+static hipError_t launch_tokens(hipStream_t s, const GemmArgs* p, int32_t n, const TokTiles& t) {
+  constexpr int BOTH = GEMM_TRANS_X | GEMM_TRANS_W;
+  const dim3 block(256), flex((unsigned)((t.total + 7) / 8 * 8));
+  if (t.shape == 0) {
+    const int32_t chain = ring_chain(t.total);
+    gemm_grouped_ring_kernel<EPI, TR><<<dim3(ring_groups(t.total, chain)), block, 0, s>>>(p, n, t.total, chain);
+    return hipGetLastError();
+  }
+  if constexpr (TR == BOTH) {
+    if (t.shape != k128Shape) return hipErrorInvalidValue;
+    gemm_grouped_flex_kernel<128, 128, 3, 2, EPI, TR, 2, false><<<flex, block, 0, s>>>(p, n, t.total, false);
+    return hipGetLastError();
+  } else {
+    if (t.shape == 4) {
+      gemm_grouped_flex_kernel<128, 96, 4, 4, EPI, TR, 1, false><<<flex, block, 0, s>>>(p, n, t.total, false);
+      return hipGetLastError();
+    }
+    if constexpr (TR == 0) {
+      if (t.shape == 5) {
+        gemm_grouped_flex_kernel<64, 96, 4, 4, EPI, TR, 2, false><<<flex, block, 0, s>>>(p, n, t.total, false);
+        return hipGetLastError();
+      }
+    }
+    return hipErrorInvalidValue;
+  }
+}
+
+hipError_t launch_gemm_tokens(hipStream_t s, int epi, int trans, const GemmArgs* dprobs, int32_t nprob,
+                              const TokTiles& t) {
+  if (nprob <= 0 || t.total <= 0) return hipErrorInvalidValue;
+  switch (epi * 4 + trans) {
+    case EPI_SOFTMAX * 4: return launch_tokens<EPI_SOFTMAX, 0>(s, dprobs, nprob, t);
+    case EPI_GREEDY * 4: return launch_tokens<EPI_GREEDY, 0>(s, dprobs, nprob, t);
+    case EPI_DLOGIT * 4: return launch_tokens<EPI_DLOGIT, 0>(s, dprobs, nprob, t);
+    case EPI_SCALED_BF16 * 4 + GEMM_TRANS_W: return launch_tokens<EPI_SCALED_BF16, GEMM_TRANS_W>(s, dprobs, nprob, t);
+    case EPI_F32 * 4 + GEMM_TRANS_W: return launch_tokens<EPI_F32, GEMM_TRANS_W>(s, dprobs, nprob, t);
+    case EPI_RESID_F32 * 4 + GEMM_TRANS_W: return launch_tokens<EPI_RESID_F32, GEMM_TRANS_W>(s, dprobs, nprob, t);
+    case EPI_SCALED_BF16 * 4 + (GEMM_TRANS_X | GEMM_TRANS_W):
+      return launch_tokens<EPI_SCALED_BF16, GEMM_TRANS_X | GEMM_TRANS_W>(s, dprobs, nprob, t);
+    default: return hipErrorInvalidValue;
+  }
 }
 
 }  // namespace jnx

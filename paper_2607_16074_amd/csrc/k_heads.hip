@@ -8,6 +8,7 @@
 //              read from the device maps, so the host needs no per-tenant counts
 // Every reduction runs in a fixed order: results are bitwise reproducible.
 #include <algorithm>
+#include <cstring>
 
 #include "jn_device.h"
 #include "jn_internal.h"
@@ -551,6 +552,214 @@ hipError_t launch_head_gemm(hipStream_t s, const HeadGemm* descs, const HeadTile
     tm0 += rows;
     if (e != hipSuccess || n.nrow == 0 || tm0 >= tms) return e;
   }
+}
+
+// ------------------------------------------------------------ token heads ---
+// The small kernels around a token head's products (k_gemm.hip): targets in, the
+// softmax parts of a row's columns joined, results out.
+
+constexpr int kTableWords = 896;
+struct TableWords {
+  uint32_t w[kTableWords];
+};
+__global__ __launch_bounds__(256) void tok_table_kernel(uint32_t* __restrict__ dst, TableWords t, int32_t n) {
+  for (int32_t i = threadIdx.x; i < n; i += 256) dst[i] = t.w[i];
+}
+
+hipError_t launch_tok_table(hipStream_t s, void* dst, const void* src, size_t bytes) {
+  TableWords t{};
+  for (size_t at = 0; at < bytes; at += sizeof t.w) {
+    const size_t n = std::min(bytes - at, sizeof t.w);
+    std::memcpy(t.w, static_cast<const char*>(src) + at, n);
+    tok_table_kernel<<<1, 256, 0, s>>>(reinterpret_cast<uint32_t*>(static_cast<char*>(dst) + at), t,
+                                       (int32_t)((n + 3) / 4));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+// Last tenant whose targets start at or before i; tenants without any share a
+// start with the next one.
+__device__ __forceinline__ int32_t tok_tenant(const TokDesc* __restrict__ d, int32_t G, int32_t i) {
+  int32_t lo = 0, hi = G - 1;
+  while (lo < hi) {
+    const int32_t mid = (lo + hi + 1) >> 1;
+    if (d[mid].first <= i) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+// One wavefront per target: rows without a target become zeros here, whatever the
+// feature holds there, so that nothing behind this reads them.  The last G
+// workgroups count the targets of a tenant each.
+typedef uint32_t u32x4t __attribute__((ext_vector_type(4)));
+__global__ __launch_bounds__(256) void tok_gather_kernel(const TokDesc* __restrict__ desc, int32_t G, int32_t N,
+                                                         const u32x4t* __restrict__ hidden, int32_t T, int32_t chunks,
+                                                         u32x4t* __restrict__ h, int32_t* __restrict__ labels,
+                                                         float* __restrict__ inv) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int32_t blocks = gridDim.x - (inv ? G : 0);
+  if ((int32_t)blockIdx.x >= blocks) {
+    const TokDesc d = desc[blockIdx.x - blocks];
+    __shared__ int32_t part[4];
+    int32_t n = 0;
+    for (int32_t i = threadIdx.x; i < d.n; i += 256) {
+      const int32_t r = d.rows[i], t = d.targets[i];
+      n += r >= 0 && r < T && t >= 0 && t < d.vocab;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, kWave);
+    if (lane == 0) part[w] = n;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      n = part[0] + part[1] + part[2] + part[3];
+      inv[blockIdx.x - blocks] = n > 0 ? 1.f / (float)n : 0.f;
+    }
+    return;
+  }
+  const int32_t i = blockIdx.x * 4 + w;
+  if (i >= N) return;
+  const TokDesc d = desc[tok_tenant(desc, G, i)];
+  const int32_t r = d.rows[i - d.first], t = d.targets ? d.targets[i - d.first] : 0;
+  const bool live = r >= 0 && r < T && t >= 0 && t < d.vocab;
+  if (lane == 0) labels[i] = live ? t : -1;
+  for (int32_t c = lane; c < chunks; c += 64)
+    h[(int64_t)i * chunks + c] = live ? hidden[(int64_t)r * chunks + c] : u32x4t{0, 0, 0, 0};
+}
+
+hipError_t launch_tok_gather(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const void* hidden, int32_t T,
+                             int32_t width, uint16_t* h, int32_t* labels, float* inv) {
+  tok_gather_kernel<<<(N + 3) / 4 + (inv ? G : 0), 256, 0, s>>>(d, G, N, static_cast<const u32x4t*>(hidden), T,
+                                                                width / 8, reinterpret_cast<u32x4t*>(h), labels, inv);
+  return hipGetLastError();
+}
+
+// Parts {m, rest} of two sets of columns joined (TokPart).
+__device__ __forceinline__ void part_join(float& m, float& rest, float m2, float rest2) {
+  const float hi = __builtin_elementwise_maximum(m, m2), lo = __builtin_elementwise_minimum(m, m2);
+  const float base = hi == -INFINITY ? 0.f : hi;
+  const bool first = m >= m2;
+  rest = (first ? rest : rest2) + (1.f + (first ? rest2 : rest)) * __builtin_amdgcn_exp2f((lo - base) * 1.4426950408889634f);
+  m = hi;
+}
+
+// 16 rows per workgroup, read as runs of 16 parts (128 bytes) of a column block,
+// 64 blocks at a time; joined in a fixed order.
+constexpr int kJoinThreads = 1024, kJoinWaves = kJoinThreads / 64;
+template <bool PICK>
+__global__ __launch_bounds__(kJoinThreads) void tok_join_kernel(const TokDesc* __restrict__ desc, int32_t G, int32_t N,
+                                                                const int32_t* __restrict__ labels,
+                                                                const float* __restrict__ zlab,
+                                                                TokRow* __restrict__ rows) {
+  __shared__ float sm[kJoinWaves][16], sr[kJoinWaves][16];
+  __shared__ int32_t sa[PICK ? kJoinWaves : 1][16];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int32_t i = blockIdx.x * 16 + (lane & 15);
+  const TokDesc d = desc[tok_tenant(desc, G, min(i, N - 1))];
+  float m = -INFINITY, rest = 0.f;
+  int32_t at = 0x7fffffff;
+  auto join = [&](float m2, float rest2, int32_t at2) __attribute__((always_inline)) {
+    if constexpr (PICK) at = m2 > m ? at2 : m2 == m ? min(at, at2) : at;
+    // an empty side ({-inf, 0}) counts no value
+    if (m == -INFINITY && rest == 0.f) {
+      m = m2;
+      rest = rest2;
+    } else if (!(m2 == -INFINITY && rest2 == 0.f)) {
+      part_join(m, rest, m2, rest2);
+    }
+  };
+  if (i < N) {
+    const int64_t col = i - d.first;
+#pragma unroll 4
+    for (int32_t b = w * 4 + (lane >> 4); b < d.blocks; b += 4 * kJoinWaves) {
+      const TokPart p = d.part[(int64_t)b * d.n + col];
+      join(p.m, p.rest, PICK ? d.index[(int64_t)b * d.n + col] : 0);
+    }
+  }
+#pragma unroll
+  for (int o = 16; o <= 32; o <<= 1) {
+    const float m2 = __shfl_xor(m, o, kWave), rest2 = __shfl_xor(rest, o, kWave);
+    const int32_t at2 = PICK ? __shfl_xor(at, o, kWave) : 0;
+    join(m2, rest2, at2);
+  }
+  if (lane < 16) {
+    sm[w][lane] = m;
+    sr[w][lane] = rest;
+    if constexpr (PICK) sa[w][lane] = at;
+  }
+  __syncthreads();
+  if (threadIdx.x >= 16 || i >= N) return;
+  for (int k = 1; k < kJoinWaves; ++k) join(sm[k][lane], sr[k][lane], PICK ? sa[k][lane] : 0);
+  const int32_t label = labels[i];
+  const float tail = log1pf(rest);
+  if constexpr (PICK) {
+    // (a row of NaN has no largest value: any token of the vocabulary)
+    d.token[i - d.first] = label < 0 ? -1 : min(at, d.vocab - 1);
+    d.logp[i - d.first] = label < 0 ? 0.f : -tail + 0.f * m;
+  } else {
+    const float logp = label < 0 ? 0.f : (zlab[i] - m) - tail;
+    d.logp[i - d.first] = logp;
+    rows[i] = TokRow{label < 0 ? 0.f : (m + tail) * 1.4426950408889634f, label < 0 ? 0.f : 1.f, expm1f(logp), label};
+  }
+}
+
+hipError_t launch_tok_join(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const int32_t* labels,
+                           const float* zlab, TokRow* rows) {
+  tok_join_kernel<false><<<(N + 15) / 16, kJoinThreads, 0, s>>>(d, G, N, labels, zlab, rows);
+  return hipGetLastError();
+}
+
+hipError_t launch_tok_pick(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const int32_t* labels) {
+  tok_join_kernel<true><<<(N + 15) / 16, kJoinThreads, 0, s>>>(d, G, N, labels, nullptr, nullptr);
+  return hipGetLastError();
+}
+
+// The first G workgroups sum a tenant's logp each; the others scale acc and round it to dh,
+// eight elements a thread.
+__global__ __launch_bounds__(256) void tok_finish_kernel(const TokDesc* __restrict__ desc, int32_t G, int32_t N,
+                                                         const float* __restrict__ inv, const float4* __restrict__ acc,
+                                                         int32_t chunks) {
+  if ((int32_t)blockIdx.x < G) {
+    const TokDesc d = desc[blockIdx.x];
+    __shared__ float part[4];
+    float v = 0.f;
+    for (int32_t i = threadIdx.x; i < d.n; i += 256) v += d.logp[i];
+    v = wave_sum(v);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    if (threadIdx.x == 0) d.loss[0] = -((part[0] + part[1]) + (part[2] + part[3])) * inv[blockIdx.x];
+    return;
+  }
+  const int64_t e = (int64_t)(blockIdx.x - G) * 256 + threadIdx.x;
+  const int32_t i = (int32_t)min(e / chunks, (int64_t)N), c = (int32_t)(e - (int64_t)i * chunks);
+  if (i >= N) return;
+  const int32_t t = tok_tenant(desc, G, i);
+  const TokDesc d = desc[t];
+  if (!d.dh) return;
+  const float4 a = acc[2 * e], b = acc[2 * e + 1];
+  const float k = inv[t];
+  reinterpret_cast<uint4*>(d.dh)[(int64_t)(i - d.first) * chunks + c] = make_uint4(
+      pack_bf2(a.x * k, a.y * k), pack_bf2(a.z * k, a.w * k), pack_bf2(b.x * k, b.y * k), pack_bf2(b.z * k, b.w * k));
+}
+
+hipError_t launch_tok_finish(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const float* inv, const float* acc,
+                             int32_t width) {
+  const int64_t more = acc ? ((int64_t)N * (width / 8) + 255) / 256 : 0;
+  tok_finish_kernel<<<(unsigned)(G + more), 256, 0, s>>>(d, G, N, inv, reinterpret_cast<const float4*>(acc), width / 8);
+  return hipGetLastError();
+}
+
+__global__ __launch_bounds__(256) void tok_zero_kernel(u32x4t* __restrict__ p, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
+    p[i] = u32x4t{0, 0, 0, 0};
+}
+
+hipError_t launch_tok_zero(hipStream_t s, void* p, size_t bytes) {
+  const int64_t n = (int64_t)(bytes / 16);
+  if (n == 0) return hipSuccess;
+  tok_zero_kernel<<<(unsigned)std::min<int64_t>((n + 255) / 256, 4096), 256, 0, s>>>(static_cast<u32x4t*>(p), n);
+  return hipGetLastError();
 }
 
 }  // namespace jnx

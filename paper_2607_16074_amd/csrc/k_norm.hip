@@ -1,6 +1,7 @@
 // RMSNorm over rows of the packed batch: one wavefront per row, the row held
 // in registers between the sum-of-squares pass and the scaling pass, a
 // butterfly wave reduction (deterministic order), fp32 math, bf16 output.
+#include <algorithm>
 #include <type_traits>
 
 #include "jn_device.h"
@@ -234,6 +235,319 @@ hipError_t launch_rmsnorm_bf16in(hipStream_t s, const void* x_bf16, float* x_out
 hipError_t launch_rmsnorm_f32in(hipStream_t s, const float* x, const void* g, void* h, int32_t rows, int32_t d,
                                 float eps) {
   return launch_rms<false>(s, x, nullptr, g, h, rows, d, eps);
+}
+
+// ------------------------------------- head norms and rotary positions ---
+// Queries and keys of a fused q | k | v row, per head x of hd elements:
+//   y = R(u), u = g x r, r = 1 / sqrt(mean(x^2) + eps)        (NORM; else u = x)
+// R turns the pair (u_i, u_{i + hd/2}) by pos[axis(i)] * theta^(-2i/hd).  Its
+// gradients, with du = R^T dy and xh = x r:
+//   dx = r (g du - xh mean(xh g du)),   dg = sum over rows and heads of du xh
+//
+// One wavefront per row (or per part of a row's heads, where rows are few).
+// P2 lanes hold a head: lane q its elements 8q .. 8q + 7 of both halves, so
+// that a pair lies in one lane and every access is 16 bytes, and the 64 / P2
+// heads of one step are reduced together by log2 P2 lane exchanges.  A row's
+// sines and cosines are formed once, one pair per lane, and shared through
+// LDS.  Angles: turns = pos * f in 64 bits (f = theta^(-2i/hd) / 2 pi), of
+// which the whole turns are dropped before anything is rounded to 32 bits, so
+// positions of any size lose nothing; then sincospi.  Everything else is fp32;
+// y and dx are rounded to bf16 once.
+constexpr int kQkStep = 4;  // head steps whose loads are issued together
+
+template <int P2>
+__device__ __forceinline__ float head_sum(float v) {
+#pragma unroll
+  for (int o = 1; o < P2; o <<= 1) v += __shfl_xor(v, o, kWave);
+  return v;
+}
+
+__device__ __forceinline__ void unpack8(const uint4& q, float* v) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    v[2 * k] = __uint_as_float(w[k] << 16);
+    v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+  }
+}
+
+__device__ __forceinline__ uint4 pack8(const float* v) {
+  return make_uint4(pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3]), pack_bf2(v[4], v[5]), pack_bf2(v[6], v[7]));
+}
+
+// Sines and cosines of a row's pairs into the wave's line [2][128]: cosines, sines.
+__device__ __forceinline__ void row_turns(const QkShape& a, int64_t row, int lane, float* line) {
+  const int half = a.hd >> 1;
+  __builtin_amdgcn_wave_barrier();  // the line's last readers are done (a wave's LDS operations stay in order)
+  for (int i = lane; i < half; i += 64) {
+    const double t = (double)a.pos[row * a.axes + a.axis[i]] * a.freq[i];
+    float sn, cs;
+    sincospif((float)(2.0 * (t - rint(t))), &sn, &cs);
+    line[i] = cs;
+    line[128 + i] = sn;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+__device__ __forceinline__ void lane_turns(const float* line, int q, float* cs, float* sn) {
+#pragma unroll
+  for (int k = 0; k < 8; k += 4) {
+    *reinterpret_cast<float4*>(cs + k) = *reinterpret_cast<const float4*>(line + 8 * q + k);
+    *reinterpret_cast<float4*>(sn + k) = *reinterpret_cast<const float4*>(line + 128 + 8 * q + k);
+  }
+}
+
+// x and y may be the same rows: a lane reads what it writes before it does.
+template <int P2, bool NORM, bool ROPE>
+__global__ __launch_bounds__(256) void qk_fwd_kernel(QkShape a, const uint16_t* x, uint16_t* y, int32_t parts) {
+  __shared__ __attribute__((aligned(16))) float lines[4][256];
+  constexpr int PER = 64 / P2;  // heads per step
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, q = lane % P2, slot = lane / P2;
+  const int64_t item = (int64_t)blockIdx.x * 4 + w;
+  const int64_t row = item / parts;
+  if (row >= a.rows) return;
+  const int heads = a.heads + a.kv, half = a.hd >> 1;
+  const int steps = (heads + PER - 1) / PER, part = (int)(item - row * parts);
+  const int s0 = steps * part / parts, s1 = steps * (part + 1) / parts;
+  const bool live = 8 * q < half;
+  float cs[8], sn[8];
+  if constexpr (ROPE) {
+    row_turns(a, row, lane, lines[w]);
+    lane_turns(lines[w], live ? q : 0, cs, sn);
+  }
+  uint4 g[2][2];  // gains of queries and keys, both halves
+  if constexpr (NORM) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint16_t* p = (k ? a.gk : a.gq) + (live ? 8 * q : 0);
+      g[k][0] = *reinterpret_cast<const uint4*>(p);
+      g[k][1] = *reinterpret_cast<const uint4*>(p + half);
+    }
+  }
+  const uint16_t* xr = x + row * a.ldx + 8 * q;
+  uint16_t* yr = y + row * a.ldy + 8 * q;
+  for (int s = s0; s < s1; s += kQkStep) {
+    uint4 v[kQkStep][2];
+#pragma unroll
+    for (int j = 0; j < kQkStep; ++j) {
+      const int h = (s + j) * PER + slot;
+      v[j][0] = v[j][1] = make_uint4(0, 0, 0, 0);
+      if (s + j < s1 && live && h < heads) {
+        v[j][0] = *reinterpret_cast<const uint4*>(xr + h * a.hd);
+        v[j][1] = *reinterpret_cast<const uint4*>(xr + h * a.hd + half);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kQkStep; ++j) {
+      if (s + j >= s1) break;
+      const int h = (s + j) * PER + slot;
+      float u[16];
+      unpack8(v[j][0], u);
+      unpack8(v[j][1], u + 8);
+      if constexpr (NORM) {
+        float ss = 0.f, gv[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) ss = fmaf(u[k], u[k], ss);
+        const float r = rsqrtf(head_sum<P2>(ss) / (float)a.hd + a.eps);
+        const bool key = h >= a.heads;
+        unpack8(key ? g[1][0] : g[0][0], gv);
+        unpack8(key ? g[1][1] : g[0][1], gv + 8);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) u[k] = u[k] * r * gv[k];
+      }
+      if constexpr (ROPE) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float p = u[k], o = u[8 + k];
+          u[k] = p * cs[k] - o * sn[k];
+          u[8 + k] = o * cs[k] + p * sn[k];
+        }
+      }
+      if (live && h < heads) {
+        *reinterpret_cast<uint4*>(yr + h * a.hd) = pack8(u);
+        *reinterpret_cast<uint4*>(yr + h * a.hd + half) = pack8(u + 8);
+      }
+    }
+  }
+}
+
+// Workgroups walk rows in steps of the grid; each leaves its sums of du xh in
+// part [workgroup][2][hd], queries then keys, which qk_gain_kernel adds in
+// order.  dx may be the rows of x or of dy.
+template <int P2, bool NORM, bool ROPE>
+__global__ __launch_bounds__(256) void qk_bwd_kernel(QkShape a, const uint16_t* x, const uint16_t* dy,
+                                                     uint16_t* dx, float* __restrict__ part) {
+  __shared__ __attribute__((aligned(16))) float lines[4][256];
+  __shared__ float sums[NORM ? 4 : 1][2][256];
+  constexpr int PER = 64 / P2;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, q = lane % P2, slot = lane / P2;
+  const int heads = a.heads + a.kv, half = a.hd >> 1, steps = (heads + PER - 1) / PER;
+  const bool live = 8 * q < half;
+  uint4 g[2][2];
+  float dg[2][16];
+  if constexpr (NORM) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint16_t* p = (k ? a.gk : a.gq) + (live ? 8 * q : 0);
+      g[k][0] = *reinterpret_cast<const uint4*>(p);
+      g[k][1] = *reinterpret_cast<const uint4*>(p + half);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) dg[k][i] = 0.f;
+    }
+  }
+  for (int64_t row = (int64_t)blockIdx.x * 4 + w; row < a.rows; row += (int64_t)gridDim.x * 4) {
+    float cs[8], sn[8];
+    if constexpr (ROPE) {
+      row_turns(a, row, lane, lines[w]);
+      lane_turns(lines[w], live ? q : 0, cs, sn);
+    }
+    const uint16_t* xr = x + row * a.ldx + 8 * q;
+    const uint16_t* yr = dy + row * a.ldy + 8 * q;
+    uint16_t* dr = dx + row * a.ldd + 8 * q;
+    for (int s = 0; s < steps; s += 2) {
+      uint4 v[2][4];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int h = (s + j) * PER + slot;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[j][k] = make_uint4(0, 0, 0, 0);
+        if (live && h < heads) {
+          if constexpr (NORM) {
+            v[j][0] = *reinterpret_cast<const uint4*>(xr + h * a.hd);
+            v[j][1] = *reinterpret_cast<const uint4*>(xr + h * a.hd + half);
+          }
+          v[j][2] = *reinterpret_cast<const uint4*>(yr + h * a.hd);
+          v[j][3] = *reinterpret_cast<const uint4*>(yr + h * a.hd + half);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (s + j >= steps) break;
+        const int h = (s + j) * PER + slot;
+        float du[16];
+        unpack8(v[j][2], du);
+        unpack8(v[j][3], du + 8);
+        if constexpr (ROPE) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float p = du[k], o = du[8 + k];
+            du[k] = p * cs[k] + o * sn[k];
+            du[8 + k] = o * cs[k] - p * sn[k];
+          }
+        }
+        if constexpr (NORM) {
+          float xh[16], gv[16], ss = 0.f, dot = 0.f;
+          unpack8(v[j][0], xh);
+          unpack8(v[j][1], xh + 8);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) ss = fmaf(xh[k], xh[k], ss);
+          const float r = rsqrtf(head_sum<P2>(ss) / (float)a.hd + a.eps);
+          const bool key = h >= a.heads;
+          unpack8(key ? g[1][0] : g[0][0], gv);
+          unpack8(key ? g[1][1] : g[0][1], gv + 8);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            xh[k] *= r;
+            const float t = du[k] * xh[k];
+            dg[0][k] += key ? 0.f : t;  // (lanes without a head hold zeros)
+            dg[1][k] += key ? t : 0.f;
+            dot = fmaf(t, gv[k], dot);
+          }
+          const float c = head_sum<P2>(dot) / (float)a.hd;
+#pragma unroll
+          for (int k = 0; k < 16; ++k) du[k] = r * (gv[k] * du[k] - xh[k] * c);
+        }
+        if (live && h < heads) {
+          *reinterpret_cast<uint4*>(dr + h * a.hd) = pack8(du);
+          *reinterpret_cast<uint4*>(dr + h * a.hd + half) = pack8(du + 8);
+        }
+      }
+    }
+  }
+  if constexpr (NORM) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float v = dg[k][i];
+#pragma unroll
+        for (int o = P2; o < 64; o <<= 1) v += __shfl_xor(v, o, kWave);
+        if (slot == 0 && live) sums[w][k][8 * q + (i < 8 ? i : half + i - 8)] = v;
+      }
+    __syncthreads();
+    for (int e = threadIdx.x; e < 2 * a.hd; e += 256) {
+      const int k = e >= a.hd, c = e - k * a.hd;
+      part[(int64_t)blockIdx.x * 2 * a.hd + e] = (sums[0][k][c] + sums[1][k][c]) + (sums[2][k][c] + sums[3][k][c]);
+    }
+  }
+}
+
+// dgq | dgk = the sums of `blocks` workgroups, 16 columns per workgroup here.
+__global__ __launch_bounds__(256) void qk_gain_kernel(const float* __restrict__ part, int32_t blocks, int32_t hd,
+                                                      float* __restrict__ dgq, float* __restrict__ dgk) {
+  __shared__ float lds[16][17];
+  const int c = threadIdx.x & 15, k = threadIdx.x >> 4, e = blockIdx.x * 16 + c;
+  float v = 0.f;
+  for (int32_t b = k; b < blocks; b += 16) v += part[(int64_t)b * 2 * hd + e];
+  lds[k][c] = v;
+  __syncthreads();
+  if (k == 0) {
+    v = lds[0][c];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) v += lds[i][c];
+    if (e < hd) dgq[e] = v; else dgk[e - hd] = v;
+  }
+}
+
+// Calls f<P2, NORM, ROPE>() for the shape.
+template <typename F>
+static hipError_t with_qk(const QkShape& a, F&& f) {
+  auto go = [&](auto p2) {
+    const bool norm = a.gq != nullptr, rope = a.pos != nullptr;
+    if (norm && rope) return f(p2, std::true_type(), std::true_type());
+    if (norm) return f(p2, std::true_type(), std::false_type());
+    return f(p2, std::false_type(), std::true_type());
+  };
+  if (a.hd <= 16) return go(std::integral_constant<int, 1>());
+  if (a.hd <= 32) return go(std::integral_constant<int, 2>());
+  if (a.hd <= 64) return go(std::integral_constant<int, 4>());
+  if (a.hd <= 128) return go(std::integral_constant<int, 8>());
+  return go(std::integral_constant<int, 16>());
+}
+
+static bool qk_ok(const QkShape& a) {
+  return a.rows >= 1 && a.hd >= 16 && a.hd <= 256 && a.hd % 16 == 0 && (a.gq || a.pos) && !a.gq == !a.gk;
+}
+
+hipError_t launch_qk_fwd(hipStream_t s, const QkShape& a, const uint16_t* x, uint16_t* y) {
+  if (!qk_ok(a)) return hipErrorInvalidValue;
+  return with_qk(a, [&](auto p2, auto norm, auto rope) {
+    constexpr int PER = 64 / decltype(p2)::value;
+    const int32_t steps = (a.heads + a.kv + PER - 1) / PER;
+    const int32_t parts = a.rows < kQkFewRows ? steps : 1;
+    const int64_t blocks = ((int64_t)a.rows * parts + 3) / 4;
+    qk_fwd_kernel<p2(), norm(), rope()><<<(unsigned)blocks, 256, 0, s>>>(a, x, y, parts);
+    return hipGetLastError();
+  });
+}
+
+int32_t qk_bwd_blocks(int32_t rows) { return std::min((rows + 3) / 4, kQkBwdBlocks); }
+
+hipError_t launch_qk_bwd(hipStream_t s, const QkShape& a, const uint16_t* x, const uint16_t* dy, uint16_t* dx,
+                         float* part, float* dgq, float* dgk) {
+  const int32_t blocks = qk_bwd_blocks(a.rows);
+  if (a.rows > 0) {
+    if (!qk_ok(a)) return hipErrorInvalidValue;
+    const hipError_t e = with_qk(a, [&](auto p2, auto norm, auto rope) {
+      qk_bwd_kernel<p2(), norm(), rope()><<<blocks, 256, 0, s>>>(a, x, dy, dx, part);
+      return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
+  }
+  if (!a.gq) return hipSuccess;
+  qk_gain_kernel<<<2 * a.hd / 16, 256, 0, s>>>(part, blocks, a.hd, dgq, dgk);
+  return hipGetLastError();
 }
 
 }  // namespace jnx
