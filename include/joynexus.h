@@ -492,16 +492,17 @@ typedef struct jn_token_io {
 } jn_token_io;
 
 /* Cross entropy of every tenant's targets over its own vocabulary, with gradients,
- * in pieces of the vocabulary: the logits of one pass are reduced as they are formed
- * and formed again for the gradients, so the workspace stays bounded (a piece of at
- * most JN_TOKEN_PIECE_BYTES, 4 KB a target at d = 2048, and the columns' sums).
+ * in pieces of the vocabulary: logits are reduced to the softmax's sums as they are
+ * formed, and one piece of them, of about JN_TOKEN_PIECE_BYTES at most, is kept as
+ * bf16 exponentials; the other pieces are formed again for the gradients.  So the
+ * workspace does not grow with vocabulary times targets.
  * Nothing is averaged across tenants.  hidden: device bf16 [T][d], d a multiple of 64
  * in [64, 8192].  Precision: bf16 operands, fp32 accumulation, softmax statistics
  * and loss; the logits' gradient is rounded to bf16 before it meets h and W, the
  * results once.  Kernels only: the call may be captured into a HIP graph, whose
  * replays read rows, targets, hidden and W as they are then.  Results are
  * bitwise reproducible.  Errors enqueue nothing. */
-#define JN_TOKEN_PIECE_BYTES (256u << 20)
+#define JN_TOKEN_PIECE_BYTES (1u << 30)
 jn_status jn_tokens_workspace_size(int32_t d, const jn_token_head* heads, const jn_token_io* io, int32_t G,
                                    size_t* bytes);
 jn_status jn_tenant_tokens_fwd_bwd(jn_ctx* ctx, const void* hidden, int32_t T, int32_t d, const jn_token_head* heads,

@@ -52,6 +52,18 @@ def _check(st: int, ctx: "Context" = None, what: str = ""):
         raise JNError(st, msg or what)
 
 
+_torch = None
+
+
+def _dtypes():
+    """torch, imported at its first use."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
 def _ptr(t) -> int:
     """Device pointer of a torch tensor (or an int)."""
     if t is None:
@@ -220,12 +232,11 @@ def _rope_fields(s, theta: float, sections, interleaved: bool):
 
 def _positions(pos, rows: int, axes: int):
     """Device pointer of int32 positions [rows, axes] ([rows] with one axis)."""
-    import torch
     if pos is None:
         return None
-    if pos.dtype != torch.int32 or not pos.is_contiguous() or pos.numel() != rows * axes:
+    if pos.dtype is not _dtypes().int32 or not pos.is_contiguous() or pos.numel() != rows * axes:
         raise TypeError(f"positions must be a contiguous int32 tensor of {rows} x {axes}")
-    return _ptr(pos)
+    return pos.data_ptr()
 
 
 class Backbone:
@@ -305,29 +316,37 @@ class QKNormRope:
         _rope_fields(s, theta, sections, interleaved)
         self.struct = s
 
+        self.axes = max(1, s.rope_axes)
+        self.width = (s.n_heads + s.n_kv_heads) * s.head_dim
+
     def at(self, rows: int, pos, x=None, y=None, dx=None):
         """The C arguments for rows of x, y (or its gradient) and dx."""
         s = jn_qk_args.from_buffer_copy(self.struct)
-        s.rows = int(rows)
-        s.pos = _positions(pos, rows, max(1, s.rope_axes))
-        width = (s.n_heads + s.n_kv_heads) * s.head_dim
-        s.ld_in, s.ld_out, s.ld_grad = (_row_stride(t, rows, width) for t in (x, y, dx))
+        s.rows = rows
+        s.pos = _positions(pos, rows, self.axes)
+        if x is not None:
+            s.ld_in = _row_stride(x, rows, self.width)
+        if y is not None:
+            s.ld_out = _row_stride(y, rows, self.width)
+        if dx is not None:
+            s.ld_grad = _row_stride(dx, rows, self.width)
         return s
 
 
 def _row_stride(t, rows: int, width: int) -> int:
     """Elements between the rows of a bf16 [rows, >= width] tensor."""
-    import torch
-    if t is None:
-        return (width + 7) // 8 * 8
-    if t.dtype != torch.bfloat16 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] < width or t.stride(1) != 1:
-        raise TypeError(f"rows must be a bfloat16 tensor [{rows}, >= {width}] with adjacent columns")
-    return t.stride(0) if rows > 1 else max(t.stride(0), t.shape[1])
+    shape = t.shape
+    if t.dtype is not _dtypes().bfloat16 or len(shape) != 2 or shape[0] != rows or shape[1] < width:
+        raise TypeError(f"rows must be a bfloat16 tensor [{rows}, >= {width}]")
+    ld, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        raise TypeError("the columns of a row must be adjacent")
+    return ld if rows > 1 else max(ld, shape[1])
 
 
 def jn_qk_norm_rope(ctx: Context, qk: QKNormRope, x, pos, y):
     a = qk.at(x.shape[0], pos, x, y)
-    _check(_lib.jn_qk_norm_rope(ctx.handle, C.byref(a), _ptr(x), _ptr(y)), ctx)
+    _check(_lib.jn_qk_norm_rope(ctx.handle, a, x.data_ptr(), y.data_ptr()), ctx)
 
 
 def jn_qk_norm_rope_workspace_size(qk: QKNormRope, rows: int) -> int:
@@ -338,11 +357,23 @@ def jn_qk_norm_rope_workspace_size(qk: QKNormRope, rows: int) -> int:
     return int(n.value)
 
 
+def _gain(t, qk: QKNormRope):
+    if t is None:
+        return None
+    if t.dtype is not _dtypes().float32 or t.numel() != qk.struct.head_dim or not t.is_contiguous():
+        raise TypeError("gain gradients must be contiguous float32 tensors [head_dim]")
+    return t.data_ptr()
+
+
+def _bytes(ws) -> int:
+    return ws.numel() * ws.element_size() if ws is not None else 0
+
+
 def jn_qk_norm_rope_bwd(ctx: Context, qk: QKNormRope, x, pos, dy, dx, dgq, dgk, ws):
     """``x``, ``dgq``, ``dgk`` and ``ws`` may be None without norms."""
     a = qk.at(dy.shape[0], pos, x, dy, dx)
-    _check(_lib.jn_qk_norm_rope_bwd(ctx.handle, C.byref(a), _ptr(x), _ptr(dy), _ptr(dx), _ptr(dgq), _ptr(dgk),
-                                    _ptr(ws), ws.numel() * ws.element_size() if ws is not None else 0), ctx)
+    _check(_lib.jn_qk_norm_rope_bwd(ctx.handle, a, _ptr(x), dy.data_ptr(), dx.data_ptr(), _gain(dgq, qk), _gain(dgk, qk),
+                                    _ptr(ws), _bytes(ws)), ctx)
 
 
 # --------------------------------------------------------------- heads ------
@@ -503,22 +534,20 @@ def jn_tenant_experts_fwd_bwd(ctx: Context, packed: Packed, hidden, ex: Sequence
 # --------------------------------------------------------- token heads ------
 
 def _entries(name: str, t, dtype, n: int):
-    if t is None or t.dtype != dtype or not t.is_contiguous() or t.numel() != n:
+    if t is None or t.dtype is not dtype or not t.is_contiguous() or t.numel() != n:
         raise TypeError(f"{name} must be a contiguous {dtype} tensor of {n} elements")
-    return _ptr(t)
+    return t.data_ptr()
 
 
 class TokenHead:
     """A tenant's token head: device bf16 W [vocab, d]."""
 
     def __init__(self, W):
-        import torch
-        if W.dtype != torch.bfloat16 or W.dim() != 2 or not W.is_contiguous():
+        if W.dtype is not _dtypes().bfloat16 or W.dim() != 2 or not W.is_contiguous():
             raise TypeError("W must be a contiguous bfloat16 tensor [vocab, d]")
-        self.W = W
+        self.W, self.shape = W, tuple(W.shape)
         s = jn_token_head()
-        s.vocab = int(W.shape[0])
-        s.W = _ptr(W)
+        s.vocab, s.W = int(W.shape[0]), W.data_ptr()
         self.struct = s
 
 
@@ -526,77 +555,80 @@ class TokenIO:
     """A tenant's targets (device int32 ``rows`` and ``targets`` [n]) and outputs: fp32 logp [n] and loss [1], bf16 dW
     [vocab, d] and, optionally, dh [n, d]."""
 
+    STRUCT = jn_token_io
+
     def __init__(self, rows, targets, logp, loss, dW, dh=None):
-        import torch
+        t = _dtypes()
         self.rows, self.targets, self.logp, self.loss, self.dW, self.dh = rows, targets, logp, loss, dW, dh
+        self.shape = tuple(dW.shape)  # of its head
         s = jn_token_io()
         n = s.n = int(rows.numel())
-        s.rows = _entries("rows", rows, torch.int32, n)
-        s.targets = _entries("targets", targets, torch.int32, n)
-        s.logp = _entries("logp", logp, torch.float32, n)
-        s.loss = _entries("loss", loss, torch.float32, 1)
-        s.dW = _entries("dW", dW, torch.bfloat16, dW.numel())
-        s.dh = _entries("dh", dh, torch.bfloat16, n * int(dW.shape[1])) if dh is not None else None
+        s.rows = _entries("rows", rows, t.int32, n)
+        s.targets = _entries("targets", targets, t.int32, n)
+        s.logp = _entries("logp", logp, t.float32, n)
+        s.loss = _entries("loss", loss, t.float32, 1)
+        s.dW = _entries("dW", dW, t.bfloat16, dW.numel())
+        s.dh = _entries("dh", dh, t.bfloat16, n * int(dW.shape[1])) if dh is not None else None
         self.struct = s
 
 
 class TokenPick:
     """Rows to decode (device int32 [n]) and outputs: token int32 [n], logp fp32 [n]."""
 
+    STRUCT = jn_token_pick
+    shape = None
+
     def __init__(self, rows, token, logp):
-        import torch
+        t = _dtypes()
         self.rows, self.token, self.logp = rows, token, logp
         s = jn_token_pick()
         n = s.n = int(rows.numel())
-        s.rows = _entries("rows", rows, torch.int32, n)
-        s.token = _entries("token", token, torch.int32, n)
-        s.logp = _entries("logp", logp, torch.float32, n)
+        s.rows = _entries("rows", rows, t.int32, n)
+        s.token = _entries("token", token, t.int32, n)
+        s.logp = _entries("logp", logp, t.float32, n)
         self.struct = s
 
 
-def _token_arrays(heads: Sequence[TokenHead], ios: Sequence):
-    if len(heads) != len(ios) or not heads:
+def _token_arrays(heads: Sequence[TokenHead], ios: Sequence, kind):
+    G = len(heads)
+    if G != len(ios) or G == 0:
         raise ValueError("one entry per token head")
-    d = int(heads[0].W.shape[1])
+    d = heads[0].shape[1]
     for h, io in zip(heads, ios):
-        if int(h.W.shape[1]) != d or (isinstance(io, TokenIO) and tuple(io.dW.shape) != tuple(h.W.shape)):
+        if h.shape[1] != d or (io.shape is not None and io.shape != h.shape) or type(io) is not kind:
             raise TypeError("token heads of one call share d, and dW has its W's shape")
-    c = jn_token_io if isinstance(ios[0], TokenIO) else jn_token_pick
-    return d, (jn_token_head * len(heads))(*[h.struct for h in heads]), (c * len(ios))(*[x.struct for x in ios])
+    return d, G, (jn_token_head * G)(*[h.struct for h in heads]), (kind.STRUCT * G)(*[x.struct for x in ios])
 
 
-def _feature(hidden, d: int) -> int:
-    import torch
-    if hidden.dtype != torch.bfloat16 or hidden.dim() != 2 or not hidden.is_contiguous() or hidden.shape[1] != d:
+def _tokens_size(call, heads, ios, kind) -> int:
+    d, G, ha, ia = _token_arrays(heads, ios, kind)
+    n = C.c_size_t()
+    _check(call(d, ha, ia, G, C.byref(n)), what=call.__name__)
+    return int(n.value)
+
+
+def _tokens_call(call, ctx: Context, hidden, heads, ios, kind, ws):
+    d, G, ha, ia = _token_arrays(heads, ios, kind)
+    shape = hidden.shape
+    if hidden.dtype is not _dtypes().bfloat16 or len(shape) != 2 or shape[1] != d or not hidden.is_contiguous():
         raise TypeError(f"hidden must be a contiguous bfloat16 tensor [T, {d}]")
-    return int(hidden.shape[0])
+    _check(call(ctx.handle, hidden.data_ptr(), shape[0], d, ha, ia, G, _ptr(ws), _bytes(ws)), ctx)
 
 
 def jn_tokens_workspace_size(heads: Sequence[TokenHead], ios: Sequence[TokenIO]) -> int:
-    d, ha, ia = _token_arrays(heads, ios)
-    n = C.c_size_t()
-    _check(_lib.jn_tokens_workspace_size(d, ha, ia, len(heads), C.byref(n)), what="jn_tokens_workspace_size")
-    return int(n.value)
+    return _tokens_size(_lib.jn_tokens_workspace_size, heads, ios, TokenIO)
 
 
 def jn_tenant_tokens_fwd_bwd(ctx: Context, hidden, heads: Sequence[TokenHead], ios: Sequence[TokenIO], ws):
-    d, ha, ia = _token_arrays(heads, ios)
-    _check(_lib.jn_tenant_tokens_fwd_bwd(ctx.handle, _ptr(hidden), _feature(hidden, d), d, ha, ia, len(heads),
-                                         _ptr(ws), ws.numel() * ws.element_size()), ctx)
+    _tokens_call(_lib.jn_tenant_tokens_fwd_bwd, ctx, hidden, heads, ios, TokenIO, ws)
 
 
 def jn_tokens_decode_workspace_size(heads: Sequence[TokenHead], picks: Sequence[TokenPick]) -> int:
-    d, ha, ia = _token_arrays(heads, picks)
-    n = C.c_size_t()
-    _check(_lib.jn_tokens_decode_workspace_size(d, ha, ia, len(heads), C.byref(n)),
-           what="jn_tokens_decode_workspace_size")
-    return int(n.value)
+    return _tokens_size(_lib.jn_tokens_decode_workspace_size, heads, picks, TokenPick)
 
 
 def jn_tenant_tokens_decode(ctx: Context, hidden, heads: Sequence[TokenHead], picks: Sequence[TokenPick], ws):
-    d, ha, ia = _token_arrays(heads, picks)
-    _check(_lib.jn_tenant_tokens_decode(ctx.handle, _ptr(hidden), _feature(hidden, d), d, ha, ia, len(heads),
-                                        _ptr(ws), ws.numel() * ws.element_size()), ctx)
+    _tokens_call(_lib.jn_tenant_tokens_decode, ctx, hidden, heads, picks, TokenPick, ws)
 
 
 # ---------------------------------------------------- tenant optimizer ------

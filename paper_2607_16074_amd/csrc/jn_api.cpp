@@ -613,8 +613,10 @@ jn_status check_axes(jn_ctx* c, int32_t axes, int32_t interleaved, const int32_t
 void qk_pairs(QkShape* q, float theta, int32_t axes, int32_t interleaved, const int32_t* sections) {
   const double turn = 6.283185307179586476925286766559;
   int32_t run = 0, left = axes > 1 ? sections[0] : q->hd / 2;
+  // a power for every 8th pair, and at most 7 products from it (8 x 2^-53)
+  const double step = std::pow((double)theta, -2.0 / q->hd);
   for (int32_t i = 0; i < q->hd / 2; ++i) {
-    q->freq[i] = std::pow((double)theta, -2.0 * i / q->hd) / turn;
+    q->freq[i] = i % 8 == 0 ? std::pow((double)theta, -2.0 * i / q->hd) / turn : q->freq[i - 1] * step;
     if (axes > 1 && interleaved) {
       const int32_t a = i % axes;
       q->axis[i] = (uint8_t)(i / axes < sections[a] ? a : 0);
@@ -905,13 +907,17 @@ struct TokSet {  // one grouped launch
 
 // Workspace offsets, the device table (descriptors, then the problems of every
 // launch) and the launches of a token-head call.  With `ws` null only the sizes.
+struct TokPiece {
+  TokSet grad, weights, rows;  // logit gradients (none for the kept piece), dW, dh
+};
 struct TokPlan {
-  int32_t N = 0;
+  int32_t N = 0, grad_blocks = 0;
+  int64_t zero8 = 0;
   size_t table = 0, h = 0, labels = 0, zlab = 0, inv = 0, rows = 0, part = 0, index = 0, piece = 0, acc = 0, total = 0;
-  bool dh = false, split = false;  // row gradients wanted; they are summed over pieces
+  bool planes = false;  // row gradients are summed from fp32 planes
   std::vector<char> bytes;
-  TokSet scores;
-  std::vector<TokSet> pieces;  // logit gradients, weight gradients and, wanted, row gradients of every piece
+  TokSet scores, more;  // of the kept piece (all columns when decoding), and of the columns behind it
+  std::vector<TokPiece> pieces;
 };
 
 inline int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
@@ -944,72 +950,55 @@ jn_status check_tokens(jn_ctx* c, int32_t d, const jn_token_head* heads, const s
     if (((uintptr_t)e.rows | (uintptr_t)e.targets | (uintptr_t)e.logp | (uintptr_t)e.loss | (uintptr_t)e.token) % 4 != 0)
       return fail(c, JN_EUNSUPPORTED, "tenant %zu: entries must be 4-byte aligned", g);
   }
-  if (N > (1 << 24)) return fail(c, JN_ESHAPE, "%lld entries", (long long)N);
+  if (N > (1 << 21)) return fail(c, JN_ESHAPE, "%lld entries", (long long)N);
   return JN_OK;
 }
+
+// K ranges of the row gradients' products: with few rows their tiles leave most
+// CUs idle for as long as the vocabulary is.  Ranges of 512 columns at least; the
+// planes' sum reads 4 bytes an element and plane at the copy rate (4.8 TB/s).
+constexpr int32_t kTokMostRanges = 16;
+int64_t range_columns(int64_t cols, int32_t S) { return std::max<int64_t>(512, up((cols + S - 1) / S, 64)); }
 
 jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std::vector<TokEntry>& io, bool train,
                      char* ws, TokPlan* P) {
   const int32_t G = (int32_t)io.size();
   int64_t N = 0, logits = 0;
-  std::vector<int32_t> first(G);
+  bool dh = false;
+  std::vector<TokDesc> desc(G);
+  std::vector<int64_t> width(G), pat(G);
   for (int32_t g = 0; g < G; ++g) {
-    first[g] = (int32_t)N;
+    desc[g].rows = io[g].rows;
+    desc[g].targets = io[g].targets;
+    desc[g].logp = io[g].logp;
+    desc[g].loss = io[g].loss;
+    desc[g].token = io[g].token;
+    desc[g].n = io[g].n;
+    desc[g].vocab = heads[g].vocab;
+    desc[g].first = (int32_t)N;
     N += io[g].n;
     logits += (int64_t)io[g].n * up(heads[g].vocab, 64);
-    P->dh = P->dh || (io[g].dh != nullptr && io[g].n > 0);
+    dh = dh || (io[g].dh != nullptr && io[g].n > 0);
+    if (train && io[g].n == 0) {
+      desc[g].zero = (uint16_t*)io[g].dW;
+      desc[g].zero_n8 = (int64_t)heads[g].vocab * d / 8;
+      P->zero8 += desc[g].zero_n8;
+    }
   }
   P->N = (int32_t)N;
   // pieces of the vocabulary, as many for every tenant, in whole ring tiles
-  const int64_t K = train && N > 0 ? std::max<int64_t>(1, (2 * logits + kTokPieceBytes - 1) / kTokPieceBytes) : 0;
-  std::vector<int64_t> width(G), pat(G);
+  const int64_t K = std::max<int64_t>(1, (2 * logits + kTokPieceBytes - 1) / kTokPieceBytes);
   int64_t piece = 0, pieces = 0;
   for (int32_t g = 0; g < G; ++g) {
-    if (io[g].n == 0 || K == 0) continue;
-    width[g] = std::min<int64_t>(up((heads[g].vocab + K - 1) / K, 256), up(heads[g].vocab, 64));
-    const int64_t most = 0x7fffffff / (2 * d) / 256 * 256 - 256;  // a transposed panel of W within 32-bit offsets
-    width[g] = std::min(width[g], most);
-    pat[g] = piece;
-    piece += up(2 * io[g].n * width[g], 256);
-    pieces = std::max(pieces, (heads[g].vocab + width[g] - 1) / width[g]);
-  }
-  P->split = P->dh && pieces > 1;
-  // the products, sized first with their pointers left open
-  std::vector<GemmArgs> probs;
-  auto add = [&](TokSet* set, int epi, int trans, std::vector<GemmArgs>& v) -> jn_status {
-    set->epi = epi;
-    set->trans = trans;
-    set->n = (int32_t)v.size();
-    set->at = probs.size();
-    set->tiles = gemm_tokens_prepare(epi, trans, v.data(), set->n);
-    if (set->tiles.total < 0) return fail(c, JN_ESHAPE, "a product of the token heads exceeds one launch's grid");
-    probs.insert(probs.end(), v.begin(), v.end());
-    return JN_OK;
-  };
-  std::vector<GemmArgs> v;
-  std::vector<int32_t> blocks(G);
-  std::vector<int64_t> parts(G);
-  int64_t all_parts = 0;
-  for (int32_t g = 0; g < G; ++g) {
     if (io[g].n == 0) continue;
-    GemmArgs q{};
-    q.W = (const uint16_t*)heads[g].W;
-    q.ldx = q.ldw = d;
-    q.ldc = io[g].n;
-    q.M = io[g].n;
-    q.N = heads[g].vocab;
-    q.K = d;
-    v.push_back(q);
-  }
-  if (!v.empty()) {
-    jn_status st = add(&P->scores, train ? EPI_SOFTMAX : EPI_GREEDY, 0, v);
-    if (st != JN_OK) return st;
-    const int32_t block = gemm_tokens_block(P->scores.tiles.shape);
-    for (int32_t g = 0; g < G; ++g) {
-      if (io[g].n == 0) continue;
-      blocks[g] = tok_blocks(heads[g].vocab, block);
-      parts[g] = all_parts;
-      all_parts += (int64_t)blocks[g] * io[g].n;
+    width[g] = heads[g].vocab;
+    if (train) {
+      width[g] = std::min<int64_t>(up((heads[g].vocab + K - 1) / K, 256), up(heads[g].vocab, 64));
+      const int64_t most = 0x7fffffff / (2 * d) / 256 * 256 - 256;  // a transposed panel of W within 32-bit offsets
+      width[g] = std::min(width[g], most);
+      pat[g] = piece;
+      piece += up(2 * io[g].n * width[g], 256);
+      pieces = std::max(pieces, (heads[g].vocab + width[g] - 1) / width[g]);
     }
   }
   size_t o = 0;
@@ -1021,27 +1010,125 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
   P->h = take(2 * N * d);
   P->labels = take(4 * N);
   P->inv = take(4 * (int64_t)G);
-  if (train) {
-    P->zlab = take(4 * N);
-    P->rows = take((int64_t)sizeof(TokRow) * N);
-    // the parts are joined before the first piece is written
-    P->part = P->piece = take(std::max<int64_t>((int64_t)sizeof(TokPart) * all_parts, piece));
-    if (P->split) P->acc = take(4 * N * d);
-  } else {
-    P->part = take((int64_t)sizeof(TokPart) * all_parts);
-    P->index = take(4 * all_parts);
+  P->zlab = take(train ? 4 * N : 0);
+  P->rows = take(train ? (int64_t)sizeof(TokRow) * N : 0);
+  P->piece = take(piece);
+
+  std::vector<GemmArgs> probs;
+  auto add = [&](TokSet* set, int epi, int trans, std::vector<GemmArgs>& v) -> jn_status {
+    if (v.empty()) return JN_OK;
+    set->epi = epi;
+    set->trans = trans;
+    set->n = (int32_t)v.size();
+    set->at = probs.size();
+    set->tiles = gemm_tokens_prepare(epi, trans, v.data(), set->n);
+    if (set->tiles.total < 0) return fail(c, JN_ESHAPE, "a product of the token heads exceeds one launch's grid");
+    probs.insert(probs.end(), v.begin(), v.end());
+    return JN_OK;
+  };
+  // logits: columns [0, width) and [width, vocab); their parts follow each other
+  for (int32_t k = 0; k < 2; ++k) {
+    std::vector<GemmArgs> v;
+    std::vector<int32_t> who;
+    for (int32_t g = 0; g < G; ++g) {
+      const int64_t v0 = k == 0 ? 0 : width[g], cols = k == 0 ? std::min<int64_t>(width[g], heads[g].vocab) : heads[g].vocab - v0;
+      if (k == 0) desc[g].grad_block = P->grad_blocks;  // (ascending, for the kernel's search)
+      if (io[g].n == 0 || cols <= 0) continue;
+      GemmArgs q{};
+      q.X = (const uint16_t*)(ws + P->h) + (int64_t)desc[g].first * d;
+      q.W = (const uint16_t*)heads[g].W + v0 * d;
+      q.ldx = q.ldw = d;
+      q.ldc = io[g].n;
+      q.M = io[g].n;
+      q.N = (int32_t)cols;
+      q.K = d;
+      q.split_c = v0;
+      if (train) {
+        q.W2 = (const uint16_t*)(ws + P->labels + 4 * (size_t)desc[g].first);
+        q.aux = (float*)(ws + P->zlab) + desc[g].first;
+        if (k == 0) {
+          desc[g].keep = (uint16_t*)(ws + P->piece + pat[g]);
+          desc[g].kept = (int32_t)cols;
+          desc[g].kept_n8 = (int32_t)(up(cols, 64) / 8);
+          P->grad_blocks += io[g].n * ((desc[g].kept_n8 + 255) / 256);
+          q.C = desc[g].keep;
+          q.ldc = up(cols, 64);
+        }
+      }
+      v.push_back(q);
+      who.push_back(g);
+    }
+    TokSet* const set = k == 0 ? &P->scores : &P->more;
+    const jn_status st = add(set, !train ? EPI_GREEDY : k == 0 ? EPI_SOFTMAX_KEEP : EPI_SOFTMAX, 0, v);
+    if (st != JN_OK) return st;
+    for (size_t j = 0; j < who.size(); ++j) {
+      TokDesc& q = desc[who[j]];
+      const int32_t block = gemm_tokens_block(set->tiles.shape);
+      if (k == 0) q.width = block;
+      q.blocks += tok_blocks(v[j].N, block);
+    }
   }
-  int32_t j = 0;
+  int64_t all_parts = 0;
+  std::vector<int64_t> parts(G);
+  for (int32_t g = 0; g < G; ++g) {
+    parts[g] = all_parts;
+    all_parts += (int64_t)desc[g].blocks * io[g].n;
+  }
+  P->part = take((int64_t)sizeof(TokPart) * all_parts);
+  P->index = take(train ? 0 : 4 * all_parts);
+  for (int32_t g = 0; g < G; ++g) {
+    desc[g].part = (const TokPart*)(ws + P->part) + parts[g];
+    if (!train) desc[g].index = (const int32_t*)(ws + P->index) + parts[g];
+  }
+  int32_t j = 0, j2 = 0;
   for (int32_t g = 0; g < G; ++g) {
     if (io[g].n == 0) continue;
     GemmArgs& q = probs[P->scores.at + j++];
-    q.X = (const uint16_t*)(ws + P->h) + (int64_t)first[g] * d;
-    q.C = ws + P->part + sizeof(TokPart) * parts[g];
-    if (train) {
-      q.W2 = (const uint16_t*)(ws + P->labels + 4 * (size_t)first[g]);
-      q.aux = (float*)(ws + P->zlab) + first[g];
-    } else {
-      q.aux = (float*)(ws + P->index) + parts[g];
+    const int32_t own = tok_blocks(q.N, gemm_tokens_block(P->scores.tiles.shape));
+    if (!train) {
+      q.C = (void*)desc[g].part;
+      q.aux = (float*)desc[g].index;
+      continue;
+    }
+    q.part = (void*)desc[g].part;
+    if (width[g] < heads[g].vocab) probs[P->more.at + j2++].C = (void*)(desc[g].part + (int64_t)own * io[g].n);
+  }
+  // gradients, piece by piece
+  int32_t S = 1;
+  if (dh) {
+    double best = 1e300;
+    for (int32_t t = 1; t <= kTokMostRanges; ++t) {
+      std::vector<GemmArgs> v;
+      for (int32_t g = 0; g < G; ++g) {
+        if (io[g].n == 0 || !io[g].dh) continue;
+        const int64_t cols = desc[g].kept, step = range_columns(cols, t);
+        for (int64_t at = 0; at < cols; at += step) {
+          GemmArgs q{};
+          q.M = io[g].n;
+          q.N = d;
+          q.K = (int32_t)std::min(step, cols - at);
+          v.push_back(q);
+        }
+      }
+      const bool sum = t > 1 || pieces > 1;
+      const TokTiles f = gemm_tokens_prepare(sum ? EPI_F32 : EPI_BF16, GEMM_TRANS_W, v.data(), (int32_t)v.size());
+      const double us = f.us + (sum ? 5.0 + 4e-6 * t * (double)N * d / 4.8 : 0.0);
+      if (f.total > 0 && us < best * 0.98) {
+        best = us;
+        S = t;
+      }
+    }
+    int32_t most = 0;
+    for (int32_t g = 0; g < G; ++g)
+      if (io[g].n > 0 && io[g].dh) {
+        const int64_t step = range_columns(desc[g].kept, S);
+        desc[g].planes = (int32_t)((desc[g].kept + step - 1) / step);
+        most = std::max(most, desc[g].planes);
+      }
+    P->planes = pieces > 1 || most > 1;
+    if (P->planes) {
+      P->acc = take(4 * most * N * d);
+      for (int32_t g = 0; g < G; ++g) desc[g].dh = (uint16_t*)io[g].dh;
     }
   }
   for (int64_t k = 0; k < pieces; ++k) {
@@ -1051,25 +1138,28 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
       if (io[g].n == 0 || v0 >= heads[g].vocab) continue;
       const int32_t n = io[g].n, cols = (int32_t)std::min(width[g], heads[g].vocab - v0);
       uint16_t* const grad = (uint16_t*)(ws + P->piece + pat[g]);
-      const uint16_t* const rows = (const uint16_t*)(ws + P->h) + (int64_t)first[g] * d;
+      const uint16_t* const rows = (const uint16_t*)(ws + P->h) + (int64_t)desc[g].first * d;
       const uint16_t* const W = (const uint16_t*)heads[g].W + v0 * d;
-      GemmArgs q{};
-      q.X = rows;
-      q.W = W;
-      q.C = grad;
-      q.aux = (float*)(ws + P->rows + sizeof(TokRow) * first[g]);
-      q.ldx = q.ldw = d;
-      q.ldc = up(cols, 64);
-      q.M = n;
-      q.N = cols;
-      q.K = d;
-      q.split_c = v0;
-      dz.push_back(q);
+      float* const inv = (float*)(ws + P->inv) + g;
+      if (k > 0) {
+        GemmArgs q{};
+        q.X = rows;
+        q.W = W;
+        q.C = grad;
+        q.aux = (float*)(ws + P->rows + sizeof(TokRow) * desc[g].first);
+        q.ldx = q.ldw = d;
+        q.ldc = up(cols, 64);
+        q.M = n;
+        q.N = cols;
+        q.K = d;
+        q.split_c = v0;
+        dz.push_back(q);
+      }
       GemmArgs w{};  // dW piece = grad^T rows
       w.X = grad;
       w.W = rows;
       w.C = (uint16_t*)io[g].dW + v0 * d;
-      w.aux = (float*)(ws + P->inv) + g;
+      w.aux = inv;
       w.ldx = up(cols, 64);
       w.ldw = w.ldc = d;
       w.M = cols;
@@ -1077,83 +1167,271 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
       w.K = n;
       dw.push_back(w);
       if (!io[g].dh) continue;
-      GemmArgs r{};  // dh (+)= grad W piece
-      r.X = grad;
-      r.W = W;
-      r.aux = P->split ? nullptr : w.aux;  // (a residual add without aux is in place)
-      r.C = P->split ? (void*)((float*)(ws + P->acc) + (int64_t)first[g] * d) : io[g].dh;
-      r.ldx = up(cols, 64);
-      r.ldw = r.ldc = d;
-      r.M = n;
-      r.N = d;
-      r.K = cols;
-      dx.push_back(r);
+      const int64_t step = P->planes ? range_columns(desc[g].kept, S) : cols;
+      for (int64_t at = 0, s = 0; at < cols; at += step, ++s) {
+        GemmArgs r{};  // dh (+)= grad W piece
+        r.X = grad + at;
+        r.W = W + at * d;
+        r.aux = P->planes ? nullptr : inv;  // (a residual add without aux is in place)
+        r.C = P->planes ? (void*)((float*)(ws + P->acc) + (s * N + desc[g].first) * d) : io[g].dh;
+        r.ldx = up(cols, 64);
+        r.ldw = r.ldc = d;
+        r.M = n;
+        r.N = d;
+        r.K = (int32_t)std::min(step, cols - at);
+        dx.push_back(r);
+      }
     }
-    TokSet a, b, e;
-    jn_status st = add(&a, EPI_DLOGIT, 0, dz);
-    if (st == JN_OK) st = add(&b, EPI_SCALED_BF16, GEMM_TRANS_X | GEMM_TRANS_W, dw);
-    if (st == JN_OK && !dx.empty())
-      st = add(&e, !P->split ? EPI_SCALED_BF16 : k == 0 ? EPI_F32 : EPI_RESID_F32, GEMM_TRANS_W, dx);
+    TokPiece p;
+    jn_status st = add(&p.grad, EPI_DLOGIT, 0, dz);
+    if (st == JN_OK) st = add(&p.weights, EPI_SCALED_BF16, GEMM_TRANS_X | GEMM_TRANS_W, dw);
+    if (st == JN_OK) st = add(&p.rows, !P->planes ? EPI_SCALED_BF16 : k == 0 ? EPI_F32 : EPI_RESID_F32, GEMM_TRANS_W, dx);
     if (st != JN_OK) return st;
-    P->pieces.push_back(a);
-    P->pieces.push_back(b);
-    if (!dx.empty()) P->pieces.push_back(e);
+    P->pieces.push_back(p);
   }
   // descriptors, then problems
-  P->table = take((int64_t)(sizeof(TokDesc) * G + sizeof(GemmArgs) * probs.size()));
+  const size_t db = sizeof(TokDesc) * G, pb = sizeof(GemmArgs) * probs.size();
+  P->table = take((int64_t)(db + pb));
   P->total = o;
-  P->bytes.resize(sizeof(TokDesc) * G + sizeof(GemmArgs) * probs.size());
-  TokDesc* const desc = (TokDesc*)P->bytes.data();
-  for (int32_t g = 0; g < G; ++g)
-    desc[g] = TokDesc{io[g].rows, io[g].targets, io[g].logp, io[g].loss, io[g].token,
-                      P->split ? (uint16_t*)io[g].dh : nullptr, (const TokPart*)(ws + P->part) + parts[g],
-                      (const int32_t*)(ws + P->index) + parts[g], io[g].n, first[g], heads[g].vocab, blocks[g]};
-  if (!probs.empty()) std::memcpy(P->bytes.data() + sizeof(TokDesc) * G, probs.data(), sizeof(GemmArgs) * probs.size());
+  P->bytes.resize(db + pb);
+  std::memcpy(P->bytes.data(), desc.data(), db);
+  if (pb > 0) std::memcpy(P->bytes.data() + db, probs.data(), pb);
   return JN_OK;
 }
 
-jn_status tokens_run(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const jn_token_head* heads,
-                     const std::vector<TokEntry>& io, bool train, void* ws, size_t ws_bytes) {
+// Tenants of few rows: launches of up to kSmallTenants, workgroups by vocabulary.
+struct SmallPlan {
+  std::vector<TokSmallSet> sets;
+  std::vector<int32_t> wgs, gwgs;  // of every set
+  int32_t ldz = 16, N = 0;
+  size_t table = 0, inv = 0, acc = 0, total = 0;
+  std::vector<char> bytes;         // descriptors and problems of the row gradients
+  TokSet rows;
+};
+
+jn_status small_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std::vector<TokEntry>& io, bool train,
+                     char* ws, SmallPlan* P) {
   const int32_t G = (int32_t)io.size();
-  jn_status st = check_tokens(c, d, heads, io, train);
-  if (st != JN_OK) return st;
-  TokPlan P;
-  if ((st = token_plan(c, d, heads, io, train, (char*)ws, &P)) != JN_OK) return st;
-  if (T < 0 || (T > 0 && !hidden)) return fail(c, JN_EINVAL, "null feature or negative rows");
-  if (!ws || ws_bytes < P.total) return fail(c, JN_ENOSPACE, "workspace %zu B < %zu B", ws ? ws_bytes : 0, P.total);
-  if ((uintptr_t)ws % 256 != 0 || (uintptr_t)hidden % 16 != 0)
-    return fail(c, JN_EUNSUPPORTED, "workspace must be 256-byte and the feature 16-byte aligned");
-  if ((st = check_device(c)) != JN_OK) return st;
-  if (P.N == 0 && !train) return JN_OK;
+  size_t o = 0;
+  auto take = [&](int64_t bytes) {
+    const size_t at = o;
+    o = align_up(o + (size_t)bytes, 256);
+    return at;
+  };
+  int32_t most = 1;
+  for (const TokEntry& e : io) most = std::max(most, e.n);
+  P->ldz = most > 32 ? 64 : most > 16 ? 32 : 16;
+  P->inv = take(4 * (int64_t)G);
+  std::vector<TokDesc> desc(G);
+  std::vector<GemmArgs> dx;
+  int64_t N = 0;
+  for (int32_t g = 0; g < G; ++g) {
+    desc[g].n = io[g].n;
+    desc[g].first = (int32_t)N;
+    desc[g].dh = io[g].n > 0 ? (uint16_t*)io[g].dh : nullptr;
+    N += io[g].n;
+  }
+  P->N = (int32_t)N;
+  const int64_t score_rows = small_score_rows(d), grad_rows = small_grad_rows(d);
+  for (int32_t g0 = 0; g0 < G; g0 += kSmallTenants) {
+    TokSmallSet set{};
+    set.G = std::min(G - g0, kSmallTenants);
+    int64_t all = 0, live = 0;
+    for (int32_t k = 0; k < set.G; ++k) {
+      all += heads[g0 + k].vocab;
+      live += io[g0 + k].n > 0 ? heads[g0 + k].vocab : 0;
+    }
+    int32_t wgs = 0, gwgs = 0;
+    for (int32_t k = 0; k < set.G; ++k) {
+      const TokEntry& e = io[g0 + k];
+      const int64_t V = heads[g0 + k].vocab;
+      TokSmall& t = set.t[k];
+      t.rows = e.rows;
+      t.targets = e.targets;
+      t.W = (const uint16_t*)heads[g0 + k].W;
+      t.logp = e.logp;
+      t.loss = e.loss;
+      t.token = e.token;
+      t.dW = (uint16_t*)e.dW;
+      t.n = e.n;
+      t.vocab = (int32_t)V;
+      t.inv = (float*)(ws + P->inv) + g0 + k;
+      // workgroups by share, never more than there are steps
+      auto share = [&](int64_t of, int64_t rows) {
+        const int64_t steps = (V + rows - 1) / rows;
+        return (int32_t)std::max<int64_t>(1, std::min(steps, kSmallGroups * V / std::max<int64_t>(of, 1)));
+      };
+      t.wg0 = wgs;
+      t.wgs = e.n > 0 ? share(live, score_rows) : 0;
+      wgs += t.wgs;
+      t.part = (TokPart*)(ws + take((int64_t)sizeof(TokPart) * t.wgs * e.n));
+      if (!train) {
+        t.index = (int32_t*)(ws + take(4 * (int64_t)t.wgs * e.n));
+        continue;
+      }
+      t.gwg0 = gwgs;
+      t.gwgs = share(all, grad_rows);
+      gwgs += t.gwgs;
+      t.zlab = (float*)(ws + take(4 * (int64_t)e.n));
+      if (e.n > 0) t.z = (float*)(ws + take(4 * V * P->ldz));
+      if (!desc[g0 + k].dh) continue;
+      t.grad = (uint16_t*)(ws + take(2 * V * P->ldz));
+    }
+    P->sets.push_back(set);
+    P->wgs.push_back(wgs);
+    P->gwgs.push_back(gwgs);
+  }
+  // dh = grad^T W over ranges of the vocabulary, as many as fill the CUs
+  int64_t tiles = 0, planes = 0;
+  for (int32_t g = 0; g < G; ++g)
+    if (desc[g].dh) tiles += (d + 127) / 128;
+  if (tiles > 0) {
+    const int64_t most_cols = 0x7fffffff / (2 * d) / 256 * 256 - 256;  // a panel of W within 32-bit offsets
+    for (int32_t g = 0; g < G; ++g) {
+      if (!desc[g].dh) continue;
+      const int64_t V = heads[g].vocab, S = std::max<int64_t>(1, 2 * kSmallGroups / tiles);
+      const int64_t step = std::min(range_columns(V, (int32_t)S), most_cols);
+      desc[g].planes = (int32_t)((V + step - 1) / step);
+      planes = std::max<int64_t>(planes, desc[g].planes);
+      for (int64_t at = 0; at < V; at += step) {
+        GemmArgs r{};
+        r.X = P->sets[g / kSmallTenants].t[g % kSmallTenants].grad + at * P->ldz;
+        r.W = (const uint16_t*)heads[g].W + at * d;
+        r.C = (void*)((at / step * N + desc[g].first) * d * 4);  // (of the planes, below)
+        r.ldx = P->ldz;
+        r.ldw = r.ldc = d;
+        r.M = io[g].n;
+        r.N = d;
+        r.K = (int32_t)std::min(step, V - at);
+        dx.push_back(r);
+      }
+    }
+    P->acc = take(4 * planes * N * d);
+    for (GemmArgs& r : dx) r.C = ws + P->acc + (size_t)r.C;
+    P->rows.epi = EPI_F32;
+    P->rows.trans = GEMM_TRANS_X | GEMM_TRANS_W;
+    P->rows.n = (int32_t)dx.size();
+    P->rows.tiles = gemm_tokens_prepare(P->rows.epi, P->rows.trans, dx.data(), P->rows.n);
+    if (P->rows.tiles.total < 0) return fail(c, JN_ESHAPE, "a product of the token heads exceeds one launch's grid");
+    const size_t db = sizeof(TokDesc) * G, pb = sizeof(GemmArgs) * dx.size();
+    P->table = take((int64_t)(db + pb));
+    P->bytes.resize(db + pb);
+    std::memcpy(P->bytes.data(), desc.data(), db);
+    std::memcpy(P->bytes.data() + db, dx.data(), pb);
+  }
+  P->total = o;
+  return JN_OK;
+}
+
+// A call's tenants by the path they take.
+struct TokSplit {
+  std::vector<jn_token_head> heads, small_heads;
+  std::vector<TokEntry> io, small_io;
+  TokPlan big;
+  SmallPlan small;
+  size_t total = 0;
+};
+
+jn_status split_tokens(jn_ctx* c, int32_t d, const jn_token_head* heads, const std::vector<TokEntry>& io, bool train,
+                       char* ws, TokSplit* P) {
+  bool big = false;
+  for (const TokEntry& e : io) big = big || e.n > tok_small_rows(d);
+  for (size_t g = 0; g < io.size(); ++g) {
+    if (io[g].n == 0 && !train) continue;
+    const bool few = io[g].n == 0 ? !big : io[g].n <= tok_small_rows(d);
+    (few ? P->small_heads : P->heads).push_back(heads[g]);
+    (few ? P->small_io : P->io).push_back(io[g]);
+  }
+  if (!P->io.empty()) {
+    const jn_status st = token_plan(c, d, P->heads.data(), P->io, train, ws, &P->big);
+    if (st != JN_OK) return st;
+  }
+  P->total = P->big.total;
+  if (!P->small_io.empty()) {
+    const jn_status st = small_plan(c, d, P->small_heads.data(), P->small_io, train, ws + P->total, &P->small);
+    if (st != JN_OK) return st;
+  }
+  P->total += P->small.total;
+  return JN_OK;
+}
+
+jn_status run_big(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const TokPlan& P, int32_t G, bool train, char* w) {
   hipStream_t s = c->stream;
-  char* const w = (char*)ws;
   const TokDesc* const desc = (const TokDesc*)(w + P.table);
   const GemmArgs* const probs = (const GemmArgs*)(desc + G);
+  const int32_t V = ((const TokDesc*)P.bytes.data())[0].vocab;
   uint16_t* const h = (uint16_t*)(w + P.h);
   int32_t* const labels = (int32_t*)(w + P.labels);
   float* const inv = (float*)(w + P.inv);
   float* const zlab = (float*)(w + P.zlab);
   auto product = [&](const TokSet& t) { return launch_gemm_tokens(s, t.epi, t.trans, probs + t.at, t.n, t.tiles); };
-  JN_HIP(c, launch_tok_table(s, w + P.table, P.bytes.data(), P.bytes.size()), "token table");
   JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 0,
-            launch_tok_gather(s, desc, G, P.N, hidden, T, d, h, labels, train ? inv : nullptr), "token rows");
-  if (P.scores.n > 0)
-    JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, heads[0].vocab, d, product(P.scores), "token scores");
+            launch_tok_gather(s, w + P.table, P.bytes.data(), P.bytes.size(), G, P.N, hidden, T, d, h, labels,
+                              train ? inv : nullptr),
+            "token rows");
+  for (const TokSet* t : {&P.scores, &P.more})
+    if (t->n > 0) JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, product(*t), "token scores");
   if (!train) {
-    JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, heads[0].vocab, 0, launch_tok_pick(s, desc, G, P.N, labels), "token pick");
+    JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, V, 0, launch_tok_pick(s, desc, G, P.N, labels), "token pick");
     return JN_OK;
   }
-  if (P.N > 0)
-    JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, heads[0].vocab, 0,
-              launch_tok_join(s, desc, G, P.N, labels, zlab, (TokRow*)(w + P.rows)), "token softmax");
-  for (const TokSet& t : P.pieces)
-    JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, heads[0].vocab, d, product(t), "token gradients");
-  for (int32_t g = 0; g < G; ++g)
-    if (io[g].n == 0)
-      JN_HIP(c, launch_tok_zero(s, io[g].dW, 2 * (size_t)heads[g].vocab * d), "empty tenant's gradient");
-  JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 1,
-            launch_tok_finish(s, desc, G, P.N, inv, P.split ? (const float*)(w + P.acc) : nullptr, d), "token loss");
+  JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, V, 0, launch_tok_join(s, desc, G, P.N, labels, zlab, (TokRow*)(w + P.rows)),
+            "token softmax");
+  JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, V, 1,
+            launch_tok_grad(s, desc, G, P.N, inv, (const TokRow*)(w + P.rows), P.grad_blocks, P.zero8),
+            "token logit gradients");
+  for (const TokPiece& p : P.pieces)
+    for (const TokSet* t : {&p.grad, &p.weights, &p.rows})
+      if (t->n > 0) JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, product(*t), "token gradients");
+  if (P.planes)
+    JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 1, launch_tok_rows(s, desc, G, P.N, inv, (const float*)(w + P.acc), d),
+              "token row gradients");
   return JN_OK;
+}
+
+jn_status run_small(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const SmallPlan& P, int32_t G, bool train,
+                    char* w) {
+  hipStream_t s = c->stream;
+  for (size_t k = 0; k < P.sets.size(); ++k) {
+    const TokSmallSet& set = P.sets[k];
+    const int32_t V = set.t[0].vocab;
+    if (P.wgs[k] > 0)
+      JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, launch_small_scores(s, set, P.wgs[k], P.ldz, hidden, T, d), "token scores");
+    if (train)
+      JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, launch_small_grads(s, set, P.gwgs[k], P.ldz, hidden, T, d),
+                "token gradients");
+    else
+      JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, V, 0, launch_small_pick(s, set, P.ldz, T), "token pick");
+  }
+  if (P.rows.n == 0) return JN_OK;
+  const TokDesc* const desc = (const TokDesc*)(w + P.table);
+  JN_HIP(c, launch_tok_table(s, w + P.table, P.bytes.data(), P.bytes.size()), "token table");
+  JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, d, 0,
+            launch_gemm_tokens(s, P.rows.epi, P.rows.trans, (const GemmArgs*)(desc + G), P.rows.n, P.rows.tiles),
+            "token gradients");
+  JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 1,
+            launch_tok_rows(s, desc, G, P.N, (const float*)(w + P.inv), (const float*)(w + P.acc), d),
+            "token row gradients");
+  return JN_OK;
+}
+
+jn_status tokens_run(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const jn_token_head* heads,
+                     const std::vector<TokEntry>& io, bool train, void* ws, size_t ws_bytes) {
+  jn_status st = check_tokens(c, d, heads, io, train);
+  if (st != JN_OK) return st;
+  TokSplit P;
+  if ((st = split_tokens(c, d, heads, io, train, (char*)ws, &P)) != JN_OK) return st;
+  if (T < 0 || (T > 0 && !hidden)) return fail(c, JN_EINVAL, "null feature or negative rows");
+  if (P.total > 0 && (!ws || ws_bytes < P.total))
+    return fail(c, JN_ENOSPACE, "workspace %zu B < %zu B", ws ? ws_bytes : 0, P.total);
+  if ((uintptr_t)ws % 256 != 0 || (uintptr_t)hidden % 16 != 0)
+    return fail(c, JN_EUNSUPPORTED, "workspace must be 256-byte and the feature 16-byte aligned");
+  if ((st = check_device(c)) != JN_OK) return st;
+  char* const w = (char*)ws;
+  if (!P.io.empty() && (st = run_big(c, hidden, T, d, P.big, (int32_t)P.io.size(), train, w)) != JN_OK) return st;
+  if (!P.small_io.empty())
+    st = run_small(c, hidden, T, d, P.small, (int32_t)P.small_io.size(), train, w + P.big.total);
+  return st;
 }
 
 std::vector<TokEntry> entries(const jn_token_io* io, int32_t G) {
@@ -1177,8 +1455,8 @@ jn_status tokens_size(int32_t d, const jn_token_head* heads, const IO* io, int32
     const std::vector<TokEntry> e = entries(io, G);
     jn_status st = check_tokens(nullptr, d, heads, e, train);
     if (st != JN_OK) return st;
-    TokPlan P;
-    if ((st = token_plan(nullptr, d, heads, e, train, nullptr, &P)) == JN_OK) *bytes = P.total;
+    TokSplit P;
+    if ((st = split_tokens(nullptr, d, heads, e, train, nullptr, &P)) == JN_OK) *bytes = P.total;
     return st;
   });
 }

@@ -108,7 +108,8 @@ enum GemmEpi : int32_t {
   EPI_SOFTMAX = 7,       // C TokPart [column block][M] of the block's columns; aux[m] = acc of column labels[m]
   EPI_GREEDY = 8,        // the same with the columns' indices in `aux` (int32 [column block][M]), no labels
   EPI_DLOGIT = 9,        // C bf16 = softmax gradient from the rows' TokRow (aux), zero in columns N .. ldc - 1
-  EPI_SCALED_BF16 = 10   // C bf16 = acc * aux[0]
+  EPI_SCALED_BF16 = 10,  // C bf16 = acc * aux[0]
+  EPI_SOFTMAX_KEEP = 11  // EPI_SOFTMAX with the parts at `part`; C bf16 = exp(acc - m) of the block's part
 };
 
 // Operand layouts of a grouped problem (GemmArgs::trans): X stored [K][M]
@@ -130,6 +131,7 @@ struct GemmArgs {
   int64_t split_c;      // split-K: elements between the fp32 partial outputs of
                         // consecutive K ranges; 0 when unsplit.  EPI_DLOGIT:
                         // the vocabulary's index of column 0
+  void* part;           // EPI_SOFTMAX_KEEP: TokPart [column block][M]
 };
 
 // Grouped launch over nprob problems sharing one epilogue: the host fills
@@ -179,6 +181,7 @@ struct TokRow {
 // gemm_tokens_block(shape) columns, tok_blocks of them per problem.
 struct TokTiles {
   int32_t total = -1, shape = 0;
+  double us = 0;        // estimate
 };
 TokTiles gemm_tokens_prepare(int epi, int trans, GemmArgs* probs, int32_t nprob);
 int32_t gemm_tokens_block(int shape);
@@ -281,7 +284,9 @@ hipError_t launch_head_gemm(hipStream_t s, const HeadGemm* descs, const HeadTile
 
 // ---- token heads (k_heads.hip) ----
 // A tenant of a token-head call; its targets are rows [first, first + n) of the
-// call's.  Device table, as are the problems of its products.
+// call's.  Device table, as are the problems of its products.  The kept logits
+// are columns [0, kept) of the vocabulary, in parts of `width` columns, kept_n8
+// groups of 8 to a row.
 struct TokDesc {
   const int32_t* rows;     // [n] rows of the shared feature
   const int32_t* targets;  // [n], null when decoding
@@ -291,23 +296,75 @@ struct TokDesc {
   uint16_t* dh;            // [n][d] or null
   const TokPart* part;     // [blocks][n]
   const int32_t* index;    // [blocks][n], decoding
+  uint16_t* keep;          // [n][8 kept_n8]
+  uint16_t* zero;          // dW of a tenant without entries, else null
+  int64_t zero_n8;
   int32_t n, first, vocab, blocks;
+  int32_t kept, width, kept_n8;
+  int32_t grad_block;      // first workgroup of launch_tok_grad, ceil(kept_n8 / 256) to an entry
+  int32_t planes, reserved;  // of dh
 };
-// Table bytes by value in kernel arguments: no staging memory, so that a captured
-// call replays.
-hipError_t launch_tok_table(hipStream_t s, void* dst, const void* src, size_t bytes);
-// h[i] = hidden[row of target i], zeros where it has none; labels[i] its token or
-// -1 (decoding: 0 where the row exists); inv[g] = 1 / targets of tenant g.
-hipError_t launch_tok_gather(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const void* hidden, int32_t T,
-                             int32_t width, uint16_t* h, int32_t* labels, float* inv);
+// The call's table at `dst` (G descriptors, then the problems), h[i] = hidden[row
+// of target i], zeros where it has none; labels[i] its token or -1 (decoding: 0
+// where the row exists); inv[g] = 1 / targets of tenant g.  The table travels by
+// value in kernel arguments: no staging memory, so that a captured call replays.
+hipError_t launch_tok_gather(hipStream_t s, void* dst, const void* table, size_t bytes, int32_t G, int32_t N,
+                             const void* hidden, int32_t T, int32_t width, uint16_t* h, int32_t* labels, float* inv);
 // Parts of every row joined: logp, and the rows' TokRow; decoding: token and logp.
 hipError_t launch_tok_join(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const int32_t* labels,
                            const float* zlab, TokRow* rows);
 hipError_t launch_tok_pick(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const int32_t* labels);
-// loss[g] = -(sum of logp) inv[g], and dh = acc inv[g] (acc null: dh is written already).
-hipError_t launch_tok_finish(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const float* inv, const float* acc,
-                             int32_t width);
-hipError_t launch_tok_zero(hipStream_t s, void* p, size_t bytes);
+// The kept logits' exponentials to their gradient, in place, and loss[g] = -(sum
+// of logp) inv[g]; zeros for dW of tenants without entries.
+hipError_t launch_tok_grad(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const float* inv, const TokRow* rows,
+                           int32_t blocks, int64_t zero8);
+// The device table by itself, for calls whose first launch is another one.
+hipError_t launch_tok_table(hipStream_t s, void* dst, const void* table, size_t bytes);
+// Tenants of few rows (tok_small_rows), by value in kernel arguments.  Logits:
+// launch_small_scores streams W once past the rows' fragments in registers and
+// leaves one part per workgroup and row, and, training, z fp32 [vocab][ldz].
+// launch_small_grads joins the parts (every workgroup for itself), writes logp and
+// loss, and streams dW out once; grad: bf16 [vocab][ldz], the logits' gradient,
+// where row gradients are wanted.  launch_small_pick joins them for decoding.
+struct TokSmall {
+  const int32_t* rows;
+  const int32_t* targets;  // null when decoding
+  const uint16_t* W;
+  float* logp;
+  float* loss;
+  int32_t* token;
+  uint16_t* dW;
+  TokPart* part;           // [wgs][n]
+  int32_t* index;          // [wgs][n], decoding
+  float* z;
+  float* zlab;             // [n], z of the target
+  uint16_t* grad;          // or null
+  float* inv;              // out: 1 / targets
+  int32_t n, vocab;
+  int32_t wg0, wgs;        // workgroups of the scores
+  int32_t gwg0, gwgs;      // and of the gradients
+};
+constexpr int32_t kSmallTenants = 24;  // of one launch
+constexpr int32_t kSmallGroups = 256;  // workgroups of a launch, about: one per CU
+template <int C>
+struct TokSmallArgs {
+  TokSmall t[C];
+  int32_t G;
+};
+typedef TokSmallArgs<kSmallTenants> TokSmallSet;
+// Most rows of a tenant: their fragments stay in 128 registers of a lane.
+inline int32_t tok_small_rows(int32_t d) { return d <= 2048 ? 64 : d <= 4096 ? 32 : 16; }
+// Vocabulary rows of a workgroup's step, scores and gradients.
+int32_t small_score_rows(int32_t d);
+int32_t small_grad_rows(int32_t d);
+hipError_t launch_small_scores(hipStream_t s, const TokSmallSet& set, int32_t wgs, int32_t ldz, const void* hidden,
+                               int32_t T, int32_t d);
+hipError_t launch_small_grads(hipStream_t s, const TokSmallSet& set, int32_t wgs, int32_t ldz, const void* hidden,
+                              int32_t T, int32_t d);
+hipError_t launch_small_pick(hipStream_t s, const TokSmallSet& set, int32_t ldz, int32_t T);
+// dh = (acc[0] + acc[1] + ...) inv[g], planes of [N][width].
+hipError_t launch_tok_rows(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const float* inv, const float* acc,
+                           int32_t width);
 
 // ---- action expert (k_expert.hip) ----
 // dst[r][c] = cvt(src[r][c]) for r < src_rows, c < src_cols, else 0; r < rows, c < cols.

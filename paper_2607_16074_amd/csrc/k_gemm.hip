@@ -185,9 +185,10 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr bool epi_bf16(int epi) {
   return epi == EPI_BF16 || epi == EPI_GELU_BF16 || epi == EPI_GEGLU_BF16 || epi == EPI_DLOGIT ||
-         epi == EPI_SCALED_BF16;
+         epi == EPI_SCALED_BF16 || epi == EPI_SOFTMAX_KEEP;
 }
-constexpr bool epi_softmax(int epi) { return epi == EPI_SOFTMAX || epi == EPI_GREEDY; }
+constexpr bool epi_softmax(int epi) { return epi == EPI_SOFTMAX || epi == EPI_GREEDY || epi == EPI_SOFTMAX_KEEP; }
+constexpr bool epi_exp(int epi) { return epi == EPI_DLOGIT || epi == EPI_SOFTMAX_KEEP; }
 constexpr bool epi_reads(int epi) { return epi == EPI_RESID_F32 || epi == EPI_GELUGRAD_BF16; }
 
 // Sizes of the 16-bit epilogue of a wave's part.
@@ -204,7 +205,7 @@ struct Epi16 {
 
 template <int EPI, int TN, int TM, bool WHOLE>
 __device__ __forceinline__ void epilogue_bf16(const GemmArgs& g, const f32x4 (&acc)[TN][TM], uint16_t* stage,
-                                              int32_t m0, int32_t n0, int lane) {
+                                              int32_t m0, int32_t n0, int lane, const float* top = nullptr) {
   using E = Epi16<EPI, TN, TM>;
   constexpr bool GLU = E::GLU;
   constexpr int WC = E::WC, CH = E::CH, RI = E::RI, NB = E::NB, NI = E::NI;
@@ -237,6 +238,9 @@ __device__ __forceinline__ void epilogue_bf16(const GemmArgs& g, const f32x4 (&a
             v[e] = __builtin_amdgcn_exp2f(fmaf(a, 1.4426950408889634f, -t.lse2)) * t.live;
             if (t.label == 16 * i + e) v[e] = t.own;
             if (!WHOLE && n0 + 16 * i + 4 * quad + e >= g.N) v[e] = 0.f;
+          } else if constexpr (EPI == EPI_SOFTMAX_KEEP) {
+            v[e] = __builtin_amdgcn_exp2f(fmaf(a, 1.4426950408889634f, top[j + jj]));
+            if (!WHOLE && n0 + 16 * i + 4 * quad + e >= g.N) v[e] = 0.f;
           } else if constexpr (EPI == EPI_SCALED_BF16) {
             v[e] = a * alpha;
           } else {
@@ -260,7 +264,7 @@ __device__ __forceinline__ void epilogue_bf16(const GemmArgs& g, const f32x4 (&a
 #pragma unroll
     for (int it = 0; it < NI; ++it)
       if ((NB * 16 % RI == 0 || RI * it + rr < NB * 16) &&
-          (WHOLE || (m + 16 * j + RI * it < g.M && n < (EPI == EPI_DLOGIT ? (int32_t)g.ldc : g.N))))
+          (WHOLE || (m + 16 * j + RI * it < g.M && n < (epi_exp(EPI) ? (int32_t)g.ldc : g.N))))
         *reinterpret_cast<u32x4*>(C + it * step) = v[it];
     C += NB * 16 * g.ldc;
   }
@@ -354,7 +358,7 @@ __device__ __forceinline__ void tok_join(float& m, float& rest, float m2, float 
 // the largest in it would take.  NaN comes through (IEEE maximum, minimum).
 template <int EPI, int TN, int TM, bool WHOLE>
 __device__ __forceinline__ void epilogue_softmax(const GemmArgs& g, const f32x4 (&acc)[TN][TM], int32_t m0, int32_t n0,
-                                                 int lane) {
+                                                 int lane, float* top = nullptr) {
   constexpr int NV = 4 * TN;
   static_assert((NV & (NV - 1)) == 0, "rounds of halves");
   const int quad = lane >> 4, row = lane & 15;
@@ -369,8 +373,8 @@ __device__ __forceinline__ void epilogue_softmax(const GemmArgs& g, const f32x4 
     for (int i = 0; i < TN; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[4 * i + e] = WHOLE || own + 16 * i + e < g.N ? acc[i][j][e] : -INFINITY;
-    if constexpr (EPI == EPI_SOFTMAX) {
-      const int32_t label = in ? reinterpret_cast<const int32_t*>(g.W2)[r] - own : -1;
+    if constexpr (EPI != EPI_GREEDY) {
+      const int32_t label = in ? reinterpret_cast<const int32_t*>(g.W2)[r] - (int32_t)g.split_c - own : -1;
       const bool here = label >= 0 && label < 16 * TN && (label & 15) < 4 && own + label < g.N;
       if (__builtin_amdgcn_ballot_w64(here) != 0) {
         float z = 0.f;
@@ -407,7 +411,10 @@ __device__ __forceinline__ void epilogue_softmax(const GemmArgs& g, const f32x4 
       }
       tok_join(m, rest, m2, rest2);
     }
-    if (quad == 0 && in) {
+    if constexpr (EPI == EPI_SOFTMAX_KEEP) {
+      top[j] = (m == -INFINITY ? 0.f : m) * -1.4426950408889634f;
+      if (quad == 0 && in) reinterpret_cast<TokPart*>(g.part)[block * g.M + r] = TokPart{m, rest};
+    } else if (quad == 0 && in) {
       reinterpret_cast<TokPart*>(g.C)[block * g.ldc + r] = TokPart{m, rest};
       if constexpr (EPI == EPI_GREEDY) reinterpret_cast<int32_t*>(g.aux)[block * g.ldc + r] = at;
     }
@@ -423,7 +430,16 @@ __device__ __forceinline__ bool gemm_epilogue(const GemmArgs& g, const f32x4 (&a
                                               int32_t m0, int32_t n0, int lane) {
   const bool whole = m0 + 16 * TM <= g.M && n0 + (EPI == EPI_GEGLU_BF16 ? 8 : 16) * TN <= g.N;
   asm volatile("" : "+v"(lane));  // lane offsets are formed here, not held in registers through a loop over tiles
-  if constexpr (epi_softmax(EPI)) {
+  if constexpr (EPI == EPI_SOFTMAX_KEEP) {
+    float top[TM];
+    if (whole) {
+      epilogue_softmax<EPI, TN, TM, true>(g, acc, m0, n0, lane, top);
+      epilogue_bf16<EPI, TN, TM, true>(g, acc, stage, m0, n0, lane, top);
+    } else {
+      epilogue_softmax<EPI, TN, TM, false>(g, acc, m0, n0, lane, top);
+      epilogue_bf16<EPI, TN, TM, false>(g, acc, stage, m0, n0, lane, top);
+    }
+  } else if constexpr (epi_softmax(EPI)) {
     if (whole)
       epilogue_softmax<EPI, TN, TM, true>(g, acc, m0, n0, lane);
     else
@@ -1626,9 +1642,10 @@ TokTiles gemm_tokens_prepare(int epi, int trans, GemmArgs* probs, int32_t nprob)
       work += n * ((probs[p].K + kBK - 1) / kBK);
     }
     if (tiles <= 0 || tiles > (int64_t)kMostBlocks) continue;
-    const double us = tiles_time(epi == EPI_DLOGIT ? EPI_GELU_BF16 : epi, tiles, (double)work / tiles, t);
+    const double us = tiles_time(epi == EPI_DLOGIT || epi == EPI_SOFTMAX_KEEP ? EPI_GELU_BF16 : epi, tiles, (double)work / tiles, t);
     if (us < best * 0.999) {
       best = us;
+      out.us = us;
       out.shape = t;
       out.total = (int32_t)tiles;
     }
@@ -1684,11 +1701,14 @@ hipError_t launch_gemm_tokens(hipStream_t s, int epi, int trans, const GemmArgs*
   if (nprob <= 0 || t.total <= 0) return hipErrorInvalidValue;
   switch (epi * 4 + trans) {
     case EPI_SOFTMAX * 4: return launch_tokens<EPI_SOFTMAX, 0>(s, dprobs, nprob, t);
+    case EPI_SOFTMAX_KEEP * 4: return launch_tokens<EPI_SOFTMAX_KEEP, 0>(s, dprobs, nprob, t);
     case EPI_GREEDY * 4: return launch_tokens<EPI_GREEDY, 0>(s, dprobs, nprob, t);
     case EPI_DLOGIT * 4: return launch_tokens<EPI_DLOGIT, 0>(s, dprobs, nprob, t);
     case EPI_SCALED_BF16 * 4 + GEMM_TRANS_W: return launch_tokens<EPI_SCALED_BF16, GEMM_TRANS_W>(s, dprobs, nprob, t);
     case EPI_F32 * 4 + GEMM_TRANS_W: return launch_tokens<EPI_F32, GEMM_TRANS_W>(s, dprobs, nprob, t);
     case EPI_RESID_F32 * 4 + GEMM_TRANS_W: return launch_tokens<EPI_RESID_F32, GEMM_TRANS_W>(s, dprobs, nprob, t);
+    case EPI_F32 * 4 + (GEMM_TRANS_X | GEMM_TRANS_W):
+      return launch_tokens<EPI_F32, GEMM_TRANS_X | GEMM_TRANS_W>(s, dprobs, nprob, t);
     case EPI_SCALED_BF16 * 4 + (GEMM_TRANS_X | GEMM_TRANS_W):
       return launch_tokens<EPI_SCALED_BF16, GEMM_TRANS_X | GEMM_TRANS_W>(s, dprobs, nprob, t);
     default: return hipErrorInvalidValue;

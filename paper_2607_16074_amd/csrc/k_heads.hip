@@ -9,6 +9,7 @@
 // Every reduction runs in a fixed order: results are bitwise reproducible.
 #include <algorithm>
 #include <cstring>
+#include <type_traits>
 
 #include "jn_device.h"
 #include "jn_internal.h"
@@ -558,27 +559,6 @@ hipError_t launch_head_gemm(hipStream_t s, const HeadGemm* descs, const HeadTile
 // The small kernels around a token head's products (k_gemm.hip): targets in, the
 // softmax parts of a row's columns joined, results out.
 
-constexpr int kTableWords = 896;
-struct TableWords {
-  uint32_t w[kTableWords];
-};
-__global__ __launch_bounds__(256) void tok_table_kernel(uint32_t* __restrict__ dst, TableWords t, int32_t n) {
-  for (int32_t i = threadIdx.x; i < n; i += 256) dst[i] = t.w[i];
-}
-
-hipError_t launch_tok_table(hipStream_t s, void* dst, const void* src, size_t bytes) {
-  TableWords t{};
-  for (size_t at = 0; at < bytes; at += sizeof t.w) {
-    const size_t n = std::min(bytes - at, sizeof t.w);
-    std::memcpy(t.w, static_cast<const char*>(src) + at, n);
-    tok_table_kernel<<<1, 256, 0, s>>>(reinterpret_cast<uint32_t*>(static_cast<char*>(dst) + at), t,
-                                       (int32_t)((n + 3) / 4));
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
-}
-
 // Last tenant whose targets start at or before i; tenants without any share a
 // start with the next one.
 __device__ __forceinline__ int32_t tok_tenant(const TokDesc* __restrict__ d, int32_t G, int32_t i) {
@@ -591,22 +571,38 @@ __device__ __forceinline__ int32_t tok_tenant(const TokDesc* __restrict__ d, int
 }
 
 // One wavefront per target: rows without a target become zeros here, whatever the
-// feature holds there, so that nothing behind this reads them.  The last G
-// workgroups count the targets of a tenant each.
+// feature holds there, so that nothing behind this reads them.  The G workgroups
+// behind them count the targets of a tenant each, the last one lays the table
+// down.  BYVAL: the descriptors are at the start of the table's bytes, else
+// (larger tables, laid down before) in device memory.
+constexpr size_t kTableBytes = 3584;
+struct alignas(16) TokTable {
+  uint32_t w[kTableBytes / 4];
+};
+__global__ __launch_bounds__(256) void tok_table_kernel(uint32_t* __restrict__ dst, TokTable t, int32_t n) {
+  for (int32_t i = threadIdx.x; i < n; i += 256) dst[i] = t.w[i];
+}
+
 typedef uint32_t u32x4t __attribute__((ext_vector_type(4)));
-__global__ __launch_bounds__(256) void tok_gather_kernel(const TokDesc* __restrict__ desc, int32_t G, int32_t N,
-                                                         const u32x4t* __restrict__ hidden, int32_t T, int32_t chunks,
-                                                         u32x4t* __restrict__ h, int32_t* __restrict__ labels,
-                                                         float* __restrict__ inv) {
+template <bool BYVAL>
+__global__ __launch_bounds__(256) void tok_gather_kernel(uint32_t* __restrict__ dst, TokTable t, int32_t words, int32_t G,
+                                                         int32_t N, const u32x4t* __restrict__ hidden, int32_t T,
+                                                         int32_t chunks, u32x4t* __restrict__ h,
+                                                         int32_t* __restrict__ labels, float* __restrict__ inv) {
+  const TokDesc* const desc = reinterpret_cast<const TokDesc*>(BYVAL ? t.w : dst);
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int32_t blocks = gridDim.x - (inv ? G : 0);
-  if ((int32_t)blockIdx.x >= blocks) {
-    const TokDesc d = desc[blockIdx.x - blocks];
+  const int32_t rows = (N + 3) / 4;
+  if ((int32_t)blockIdx.x >= rows + (inv ? G : 0)) {
+    for (int32_t i = threadIdx.x; i < words; i += 256) dst[i] = t.w[i];
+    return;
+  }
+  if ((int32_t)blockIdx.x >= rows) {
+    const TokDesc& d = desc[blockIdx.x - rows];
     __shared__ int32_t part[4];
     int32_t n = 0;
     for (int32_t i = threadIdx.x; i < d.n; i += 256) {
-      const int32_t r = d.rows[i], t = d.targets[i];
-      n += r >= 0 && r < T && t >= 0 && t < d.vocab;
+      const int32_t r = d.rows[i], at = d.targets[i];
+      n += r >= 0 && r < T && at >= 0 && at < d.vocab;
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, kWave);
@@ -614,25 +610,48 @@ __global__ __launch_bounds__(256) void tok_gather_kernel(const TokDesc* __restri
     __syncthreads();
     if (threadIdx.x == 0) {
       n = part[0] + part[1] + part[2] + part[3];
-      inv[blockIdx.x - blocks] = n > 0 ? 1.f / (float)n : 0.f;
+      inv[blockIdx.x - rows] = n > 0 ? 1.f / (float)n : 0.f;
     }
     return;
   }
-  const int32_t i = blockIdx.x * 4 + w;
+  const int32_t i = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + w);
   if (i >= N) return;
-  const TokDesc d = desc[tok_tenant(desc, G, i)];
-  const int32_t r = d.rows[i - d.first], t = d.targets ? d.targets[i - d.first] : 0;
-  const bool live = r >= 0 && r < T && t >= 0 && t < d.vocab;
-  if (lane == 0) labels[i] = live ? t : -1;
+  const TokDesc& d = desc[tok_tenant(desc, G, i)];
+  const int32_t r = d.rows[i - d.first], at = d.targets ? d.targets[i - d.first] : 0;
+  const bool live = r >= 0 && r < T && at >= 0 && at < d.vocab;
+  if (lane == 0) labels[i] = live ? at : -1;
   for (int32_t c = lane; c < chunks; c += 64)
     h[(int64_t)i * chunks + c] = live ? hidden[(int64_t)r * chunks + c] : u32x4t{0, 0, 0, 0};
 }
 
-hipError_t launch_tok_gather(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const void* hidden, int32_t T,
-                             int32_t width, uint16_t* h, int32_t* labels, float* inv) {
-  tok_gather_kernel<<<(N + 3) / 4 + (inv ? G : 0), 256, 0, s>>>(d, G, N, static_cast<const u32x4t*>(hidden), T,
-                                                                width / 8, reinterpret_cast<u32x4t*>(h), labels, inv);
-  return hipGetLastError();
+hipError_t launch_tok_table(hipStream_t s, void* dst, const void* table, size_t bytes) {
+  TokTable t{};
+  for (size_t at = 0; at < bytes; at += kTableBytes) {
+    const size_t n = std::min(bytes - at, kTableBytes);
+    std::memcpy(t.w, static_cast<const char*>(table) + at, n);
+    tok_table_kernel<<<1, 256, 0, s>>>(static_cast<uint32_t*>(dst) + at / 4, t, (int32_t)(n / 4));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_tok_gather(hipStream_t s, void* dst, const void* table, size_t bytes, int32_t G, int32_t N,
+                             const void* hidden, int32_t T, int32_t width, uint16_t* h, int32_t* labels, float* inv) {
+  TokTable t{};
+  uint32_t* const to = static_cast<uint32_t*>(dst);
+  const unsigned blocks = (N + 3) / 4 + (inv ? G : 0);
+  auto go = [&](auto byval, int32_t words) {
+    tok_gather_kernel<byval()><<<blocks + (words > 0), 256, 0, s>>>(
+        to, t, words, G, N, static_cast<const u32x4t*>(hidden), T, width / 8, reinterpret_cast<u32x4t*>(h), labels, inv);
+    return hipGetLastError();
+  };
+  if (bytes <= kTableBytes) {
+    std::memcpy(t.w, table, bytes);
+    return go(std::true_type(), (int32_t)(bytes / 4));
+  }
+  const hipError_t e = launch_tok_table(s, dst, table, bytes);
+  return e != hipSuccess ? e : go(std::false_type(), 0);
 }
 
 // Parts {m, rest} of two sets of columns joined (TokPart).
@@ -642,6 +661,16 @@ __device__ __forceinline__ void part_join(float& m, float& rest, float m2, float
   const bool first = m >= m2;
   rest = (first ? rest : rest2) + (1.f + (first ? rest2 : rest)) * __builtin_amdgcn_exp2f((lo - base) * 1.4426950408889634f);
   m = hi;
+}
+
+// The same where a side may be empty ({-inf, 0}: no value).
+__device__ __forceinline__ void part_merge(float& m, float& rest, float m2, float rest2) {
+  if (m == -INFINITY && rest == 0.f) {
+    m = m2;
+    rest = rest2;
+  } else if (!(m2 == -INFINITY && rest2 == 0.f)) {
+    part_join(m, rest, m2, rest2);
+  }
 }
 
 // 16 rows per workgroup, read as runs of 16 parts (128 bytes) of a column block,
@@ -661,13 +690,7 @@ __global__ __launch_bounds__(kJoinThreads) void tok_join_kernel(const TokDesc* _
   int32_t at = 0x7fffffff;
   auto join = [&](float m2, float rest2, int32_t at2) __attribute__((always_inline)) {
     if constexpr (PICK) at = m2 > m ? at2 : m2 == m ? min(at, at2) : at;
-    // an empty side ({-inf, 0}) counts no value
-    if (m == -INFINITY && rest == 0.f) {
-      m = m2;
-      rest = rest2;
-    } else if (!(m2 == -INFINITY && rest2 == 0.f)) {
-      part_join(m, rest, m2, rest2);
-    }
+    part_merge(m, rest, m2, rest2);
   };
   if (i < N) {
     const int64_t col = i - d.first;
@@ -715,51 +738,541 @@ hipError_t launch_tok_pick(hipStream_t s, const TokDesc* d, int32_t G, int32_t N
   return hipGetLastError();
 }
 
-// The first G workgroups sum a tenant's logp each; the others scale acc and round it to dh,
-// eight elements a thread.
-__global__ __launch_bounds__(256) void tok_finish_kernel(const TokDesc* __restrict__ desc, int32_t G, int32_t N,
-                                                         const float* __restrict__ inv, const float4* __restrict__ acc,
-                                                         int32_t chunks) {
-  if ((int32_t)blockIdx.x < G) {
-    const TokDesc d = desc[blockIdx.x];
+// The kept exponentials e = exp(z - m) of column blocks to the logits' gradient
+// p - 1: p = e exp(m - lse), `own` in the target's column; 8 columns a thread.  The
+// next G workgroups sum a tenant's logp each, those behind them clear dW of
+// tenants without entries.
+__global__ __launch_bounds__(256) void tok_grad_kernel(const TokDesc* __restrict__ desc, int32_t G, int32_t N,
+                                                       const float* __restrict__ inv, const TokRow* __restrict__ rows,
+                                                       int32_t blocks, int32_t zeros) {
+  int32_t b = blockIdx.x;
+  if (b < blocks) {
+    int32_t lo = 0, hi = G - 1;  // as tok_tenant
+    while (lo < hi) {
+      const int32_t mid = (lo + hi + 1) >> 1;
+      if (desc[mid].grad_block <= b) lo = mid; else hi = mid - 1;
+    }
+    const TokDesc& d = desc[lo];
+    const int32_t per = (d.kept_n8 + 255) / 256, n = (b - d.grad_block) / per, i = d.first + n;
+    const int32_t c = (b - d.grad_block - n * per) * 256 + threadIdx.x;
+    if (c >= d.kept_n8) return;
+    const TokRow row = rows[i];
+    uint4* const at = reinterpret_cast<uint4*>(d.keep) + (int64_t)n * d.kept_n8 + c;
+    const int32_t v0 = 8 * c;
+    const float m = d.part[(int64_t)(v0 / d.width) * d.n + n].m;
+    // (a block without a column has m = -inf and zeros)
+    const float f = v0 < d.kept ? __builtin_amdgcn_exp2f(fmaf(m, 1.4426950408889634f, -row.lse2)) * row.live : 0.f;
+    const uint4 q = *at;
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[2 * k] = __uint_as_float(w[k] << 16) * f;
+      v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u) * f;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = row.label == v0 + k ? row.own : v[k];
+    *at = make_uint4(pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3]), pack_bf2(v[4], v[5]), pack_bf2(v[6], v[7]));
+    return;
+  }
+  b -= blocks;
+  if (b < G) {
+    const TokDesc& d = desc[b];
     __shared__ float part[4];
     float v = 0.f;
     for (int32_t i = threadIdx.x; i < d.n; i += 256) v += d.logp[i];
     v = wave_sum(v);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
     __syncthreads();
-    if (threadIdx.x == 0) d.loss[0] = -((part[0] + part[1]) + (part[2] + part[3])) * inv[blockIdx.x];
+    if (threadIdx.x == 0) d.loss[0] = -((part[0] + part[1]) + (part[2] + part[3])) * inv[b];
     return;
   }
-  const int64_t e = (int64_t)(blockIdx.x - G) * 256 + threadIdx.x;
-  const int32_t i = (int32_t)min(e / chunks, (int64_t)N), c = (int32_t)(e - (int64_t)i * chunks);
-  if (i >= N) return;
-  const int32_t t = tok_tenant(desc, G, i);
-  const TokDesc d = desc[t];
+  for (int32_t g = 0; g < G; ++g)
+    if (desc[g].zero)
+      for (int64_t e = (int64_t)(b - G) * 256 + threadIdx.x; e < desc[g].zero_n8; e += (int64_t)zeros * 256)
+        reinterpret_cast<uint4*>(desc[g].zero)[e] = make_uint4(0, 0, 0, 0);
+}
+
+hipError_t launch_tok_grad(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const float* inv, const TokRow* rows,
+                           int32_t blocks, int64_t zero8) {
+  const int32_t zeros = (int32_t)std::min<int64_t>((zero8 + 1023) / 1024, 2048);
+  tok_grad_kernel<<<(unsigned)(blocks + G + zeros), 256, 0, s>>>(d, G, N, inv, rows, blocks, zeros);
+  return hipGetLastError();
+}
+
+// Eight elements of dh per thread.
+__global__ __launch_bounds__(256) void tok_rows_kernel(const TokDesc* __restrict__ desc, int32_t G, int32_t N,
+                                                       const float* __restrict__ inv, const float4* __restrict__ acc,
+                                                       int32_t chunks) {
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, plane = (int64_t)N * chunks;
+  if (e >= plane) return;
+  const int32_t i = (int32_t)(e / chunks), c = (int32_t)(e - (int64_t)i * chunks), t = tok_tenant(desc, G, i);
+  const TokDesc& d = desc[t];
   if (!d.dh) return;
-  const float4 a = acc[2 * e], b = acc[2 * e + 1];
-  const float k = inv[t];
+  float4 a = acc[2 * e], b = acc[2 * e + 1];
+#pragma unroll 4
+  for (int32_t k = 1; k < d.planes; ++k) {
+    const float4 x = acc[2 * (k * plane + e)], y = acc[2 * (k * plane + e) + 1];
+    a = make_float4(a.x + x.x, a.y + x.y, a.z + x.z, a.w + x.w);
+    b = make_float4(b.x + y.x, b.y + y.y, b.z + y.z, b.w + y.w);
+  }
+  const float f = inv[t];
   reinterpret_cast<uint4*>(d.dh)[(int64_t)(i - d.first) * chunks + c] = make_uint4(
-      pack_bf2(a.x * k, a.y * k), pack_bf2(a.z * k, a.w * k), pack_bf2(b.x * k, b.y * k), pack_bf2(b.z * k, b.w * k));
+      pack_bf2(a.x * f, a.y * f), pack_bf2(a.z * f, a.w * f), pack_bf2(b.x * f, b.y * f), pack_bf2(b.z * f, b.w * f));
 }
 
-hipError_t launch_tok_finish(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const float* inv, const float* acc,
-                             int32_t width) {
-  const int64_t more = acc ? ((int64_t)N * (width / 8) + 255) / 256 : 0;
-  tok_finish_kernel<<<(unsigned)(G + more), 256, 0, s>>>(d, G, N, inv, reinterpret_cast<const float4*>(acc), width / 8);
+hipError_t launch_tok_rows(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const float* inv, const float* acc,
+                           int32_t width) {
+  const int64_t blocks = ((int64_t)N * (width / 8) + 255) / 256;
+  tok_rows_kernel<<<(unsigned)blocks, 256, 0, s>>>(d, G, N, inv, reinterpret_cast<const float4*>(acc), width / 8);
   return hipGetLastError();
 }
 
-__global__ __launch_bounds__(256) void tok_zero_kernel(u32x4t* __restrict__ p, int64_t n) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
-    p[i] = u32x4t{0, 0, 0, 0};
+// ---- tenants of few rows ----
+// With up to 64 rows a call is bound by memory, W in and dW out once each, and the
+// smallest ones by their launches.
+
+typedef __bf16 bf16x8h __attribute__((ext_vector_type(8)));
+typedef float f32x4h __attribute__((ext_vector_type(4)));
+constexpr int kSmallThreads = 512;
+constexpr float kLog2e = 1.4426950408889634f;
+
+// LDS written before is read behind it; loads from memory stay in flight.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <int C>
+__device__ __forceinline__ int32_t small_tenant(const TokSmallArgs<C>& s, int32_t wg, bool grads) {
+  int32_t g = 0;
+  while (g + 1 < s.G && (grads ? s.t[g + 1].gwg0 : s.t[g + 1].wg0) <= wg) ++g;
+  return g;
 }
 
-hipError_t launch_tok_zero(hipStream_t s, void* p, size_t bytes) {
-  const int64_t n = (int64_t)(bytes / 16);
-  if (n == 0) return hipSuccess;
-  tok_zero_kernel<<<(unsigned)std::min<int64_t>((n + 255) / 256, 4096), 256, 0, s>>>(static_cast<u32x4t*>(p), n);
-  return hipGetLastError();
+// The feature's row of entry i, or -1 where it has no target.
+__device__ __forceinline__ int32_t small_row(const TokSmall& d, int32_t i, int32_t T) {
+  if (i >= d.n) return -1;
+  const int32_t r = d.rows[i], at = d.targets ? d.targets[i] : 0;
+  return r >= 0 && r < T && at >= 0 && at < d.vocab ? r : -1;
+}
+
+// z = W h for up to 16 NB rows.  8 wavefronts: WK share the contraction (at most 8
+// CH steps of 32 each, whose row fragments stay in registers for the whole
+// launch) and 8 / WK take 16 vocabulary rows each; W goes straight from memory to
+// the matrix cores' operands, 8 loads of 1 KB a wavefront ahead of the 8 in use
+// (128 KB of a CU in flight), and is read by nobody twice.  The shares are added
+// in LDS, in pairs, which also rounds less than one long chain of additions.
+// Every thread then owns one row and some of the vocabulary's, and keeps a running
+// maximum and the sum of the others' exponentials, as TokPart.
+template <int WK, int CH, int NB, int C>
+__global__ __launch_bounds__(kSmallThreads, 2) void small_scores_kernel(TokSmallArgs<C> set, int32_t ldz,
+                                                                        const uint16_t* __restrict__ hidden, int32_t T,
+                                                                        int32_t width) {
+  constexpr int WV = 8 / WK, TOK = 16 * NB, LD = TOK + 4, ROWS = 16 * WV, PER = kSmallThreads / TOK;
+  __shared__ __attribute__((aligned(16))) float red[2][8][16 * LD];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wk = w % WK, wv = w / WK, quad = lane >> 4, row = lane & 15;
+  const TokSmall& d = set.t[small_tenant(set, blockIdx.x, false)];
+  const int32_t V = d.vocab, n = d.n, wg = blockIdx.x - d.wg0;
+  const int32_t blocks = (V + ROWS - 1) / ROWS;
+  const int32_t b0 = (int32_t)((int64_t)blocks * wg / d.wgs), b1 = (int32_t)((int64_t)blocks * (wg + 1) / d.wgs);
+  const int32_t S = width / 32, s0 = S * wk / WK, ns = S * (wk + 1) / WK - s0;
+  bf16x8h w0[8], w1[8];
+  auto fetch = [&](bf16x8h(&to)[8], int32_t b, int c) __attribute__((always_inline)) {
+    const int32_t v = min((b * WV + wv) * 16 + row, V - 1);
+    const uint16_t* const p = d.W + (int64_t)v * width + (s0 + 8 * c) * 32 + 8 * quad;
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+      if (8 * c + s < ns) to[s] = *reinterpret_cast<const bf16x8h*>(p + 32 * s);
+  };
+#pragma unroll
+  for (int s = 0; s < 8; ++s) w0[s] = w1[s] = bf16x8h{};
+  if (b0 < b1) fetch(w0, b0, 0);
+  bf16x8h x[8 * CH][NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    const int32_t r = small_row(d, 16 * j + row, T);
+    const uint16_t* const p = hidden + (int64_t)max(r, 0) * width + s0 * 32 + 8 * quad;
+#pragma unroll
+    for (int s = 0; s < 8 * CH; ++s) {
+      x[s][j] = bf16x8h{};
+      if (r >= 0 && s < ns) x[s][j] = *reinterpret_cast<const bf16x8h*>(p + 32 * s);
+    }
+  }
+  const int32_t tok = threadIdx.x % TOK;
+  const int32_t label = d.targets && tok < n ? d.targets[tok] : -1;
+  float m = -INFINITY, rest = 0.f;
+  int32_t at = 0x7fffffff;
+  f32x4h acc[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) acc[j] = f32x4h{0.f, 0.f, 0.f, 0.f};
+  int buf = 0;
+  // chunk c of block b, from `use`; the next one into `next`
+  auto chunk = [&](auto c_, bf16x8h(&use)[8], bf16x8h(&next)[8], int32_t b) __attribute__((always_inline)) {
+    constexpr int c = decltype(c_)::value;
+    if (c + 1 < CH)
+      fetch(next, b, c + 1);
+    else if (b + 1 < b1)
+      fetch(next, b + 1, 0);
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(use[s], x[8 * c + s][j], acc[j], 0, 0, 0);
+    if (c + 1 < CH) return;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) red[buf][w][(4 * quad + e) * LD + 16 * j + row] = acc[j][e];
+      acc[j] = f32x4h{0.f, 0.f, 0.f, 0.f};
+    }
+    lds_barrier();
+#pragma unroll
+    for (int u = 0; u < (ROWS + PER - 1) / PER; ++u) {
+      const int32_t r = threadIdx.x / TOK + u * PER;
+      if (ROWS % PER != 0 && r >= ROWS) break;
+      float p[WK];
+#pragma unroll
+      for (int k = 0; k < WK; ++k) p[k] = red[buf][(r >> 4) * WK + k][(r & 15) * LD + tok];
+#pragma unroll
+      for (int h = 1; h < WK; h <<= 1)
+#pragma unroll
+        for (int k = 0; k < WK; k += 2 * h) p[k] += p[k + h];
+      const float z = p[0];
+      const int32_t v = b * ROWS + r;
+      if (v >= V) continue;
+      if (d.z) d.z[(int64_t)v * ldz + tok] = z;
+      if (v == label) d.zlab[tok] = z;
+      const float e = __builtin_amdgcn_exp2f(-fabsf(z - m) * kLog2e);
+      if (z > m) {
+        rest = (rest + 1.f) * e;  // (from -inf: e = 0)
+        m = z;
+        at = v;
+      } else {
+        rest += e;
+      }
+    }
+    buf ^= 1;
+  };
+  if constexpr (CH == 1) {
+    for (int32_t b = b0; b < b1; b += 2) {
+      chunk(std::integral_constant<int, 0>(), w0, w1, b);
+      if (b + 1 < b1) chunk(std::integral_constant<int, 0>(), w1, w0, b + 1);
+    }
+  } else {
+    for (int32_t b = b0; b < b1; ++b) {
+      chunk(std::integral_constant<int, 0>(), w0, w1, b);
+      chunk(std::integral_constant<int, 1>(), w1, w0, b);
+      if constexpr (CH == 4) {
+        chunk(std::integral_constant<int, 2>(), w0, w1, b);
+        chunk(std::integral_constant<int, 3>(), w1, w0, b);
+      }
+    }
+  }
+  // the lanes of a row, then its wavefronts
+  auto join = [&](float m2, float rest2, int32_t at2) __attribute__((always_inline)) {
+    at = m2 > m ? at2 : m2 == m ? min(at, at2) : at;
+    part_merge(m, rest, m2, rest2);
+  };
+#pragma unroll
+  for (int o = TOK; o < 64; o <<= 1) {
+    const float m2 = __shfl_xor(m, o, kWave), rest2 = __shfl_xor(rest, o, kWave);
+    join(m2, rest2, __shfl_xor(at, o, kWave));
+  }
+  lds_barrier();  // the last step's shares are read
+  float* const sm = red[0][0];
+  float* const sr = sm + 8 * TOK;
+  int32_t* const sa = reinterpret_cast<int32_t*>(sr + 8 * TOK);
+  static_assert(3 * 8 * TOK <= 2 * 8 * 16 * LD, "joins in the same memory");
+  if (lane < TOK) {
+    sm[w * TOK + lane] = m;
+    sr[w * TOK + lane] = rest;
+    sa[w * TOK + lane] = at;
+  }
+  lds_barrier();
+  if (threadIdx.x >= TOK || tok >= n) return;
+#pragma unroll
+  for (int k = 1; k < 8; ++k) join(sm[k * TOK + tok], sr[k * TOK + tok], sa[k * TOK + tok]);
+  d.part[(int64_t)wg * n + tok] = TokPart{m, rest};
+  if (d.index) d.index[(int64_t)wg * n + tok] = at;
+}
+
+// Parts of TOK rows from row `first` on joined by a workgroup: thread t < TOK ends
+// with row first + t's.
+template <int TOK>
+struct SmallJoin {
+  float m[8][TOK], rest[8][TOK];
+  int32_t at[8][TOK];
+};
+template <int TOK>
+__device__ __forceinline__ void small_join(const TokSmall& d, int32_t first, float& m, float& rest, int32_t& at,
+                                           SmallJoin<TOK>& l) {
+  constexpr int PER = kSmallThreads / TOK;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, t = threadIdx.x % TOK;
+  const int32_t tok = first + t;
+  m = -INFINITY;
+  rest = 0.f;
+  at = 0x7fffffff;
+  auto join = [&](float m2, float rest2, int32_t at2) __attribute__((always_inline)) {
+    at = m2 > m ? at2 : m2 == m ? min(at, at2) : at;
+    part_merge(m, rest, m2, rest2);
+  };
+  if (tok < d.n) {
+#pragma unroll 8
+    for (int32_t p = threadIdx.x / TOK; p < d.wgs; p += PER) {
+      const TokPart q = d.part[(int64_t)p * d.n + tok];
+      join(q.m, q.rest, d.index ? d.index[(int64_t)p * d.n + tok] : 0);
+    }
+  }
+#pragma unroll
+  for (int o = TOK; o < 64; o <<= 1) {
+    const float m2 = __shfl_xor(m, o, kWave), rest2 = __shfl_xor(rest, o, kWave);
+    join(m2, rest2, __shfl_xor(at, o, kWave));
+  }
+  if (lane < TOK) {
+    l.m[w][t] = m;
+    l.rest[w][t] = rest;
+    l.at[w][t] = at;
+  }
+  lds_barrier();
+  if (threadIdx.x < TOK) {
+#pragma unroll
+    for (int k = 1; k < 8; ++k) join(l.m[k][t], l.rest[k][t], l.at[k][t]);
+  }
+}
+
+// 16 rows per workgroup.
+template <int C>
+__global__ __launch_bounds__(kSmallThreads) void small_pick_kernel(TokSmallArgs<C> set, int32_t T) {
+  __shared__ SmallJoin<16> l;
+  const TokSmall& d = set.t[blockIdx.x];
+  const int32_t first = 16 * blockIdx.y;
+  if (first >= d.n) return;
+  float m, rest;
+  int32_t at;
+  const int32_t i = first + threadIdx.x;
+  const bool live = threadIdx.x < 16 && small_row(d, i, T) >= 0;
+  small_join<16>(d, first, m, rest, at, l);
+  if (threadIdx.x >= 16 || i >= d.n) return;
+  // (a row of NaN has no largest value: any token of the vocabulary)
+  d.token[i] = live ? min(at, d.vocab - 1) : -1;
+  d.logp[i] = live ? -log1pf(rest) + 0.f * m : 0.f;
+}
+
+// dW = dz^T H / count for up to 32 NS rows: the contraction is the rows, so one or
+// two matrix instructions make 16 vocabulary rows x 16 columns, and the kernel is
+// bound by writing dW.  A lane's fragments of H^T stay in registers: it reads 8
+// columns (16 bytes) of 8 rows and turns them, so that fragment j of a group of 128
+// columns holds columns 8 i + j of row i of the instruction, and the 8 results of
+// a lane for one of its 4 rows are 8 adjacent columns: one 16-byte store.  dz is
+// formed from z and the rows' joined sums by every wavefront for itself, rounded to
+// bf16 unscaled (TokRow).  blockIdx.y: 2,048 columns each.
+template <int GP, int NS, int C>
+__global__ __launch_bounds__(kSmallThreads, 2) void small_grads_kernel(TokSmallArgs<C> set, int32_t ldz,
+                                                                       const uint16_t* __restrict__ hidden, int32_t T,
+                                                                       int32_t width) {
+  __shared__ SmallJoin<32 * NS> l;
+  __shared__ __attribute__((aligned(16))) float lse[64], own[64];
+  __shared__ __attribute__((aligned(16))) int32_t lab[64];
+  __shared__ float scale;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int quad = lane >> 4, col = lane & 15;
+  const TokSmall& d = set.t[small_tenant(set, blockIdx.x, true)];
+  const int32_t V = d.vocab, wg = blockIdx.x - d.gwg0, n = d.n;
+  // column groups of this slice, and how many wavefronts share them
+  const int32_t g0 = 16 * blockIdx.y, groups = min((width + 127) / 128 - g0, 16);
+  const int32_t WC = groups > 4 ? 8 : groups > 2 ? 4 : groups, WV = 8 / WC, wc = w % WC, wv = w / WC;
+  const int32_t mine = small_row(d, lane, T);  // of row `lane`
+  uint4 q[GP][NS][8];
+#pragma unroll
+  for (int s = 0; s < NS; ++s)
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      const int32_t r = __shfl(mine, 32 * s + 8 * quad + t, kWave);
+#pragma unroll
+      for (int p = 0; p < GP; ++p) {
+        const int32_t k = 128 * (g0 + wc + 8 * p) + 8 * col;
+        q[p][s][t] = make_uint4(0, 0, 0, 0);
+        if (r >= 0 && k < width) q[p][s][t] = *reinterpret_cast<const uint4*>(hidden + (int64_t)r * width + k);
+      }
+    }
+  {
+    float m, rest;
+    int32_t at;
+    const bool live = mine >= 0;
+    const float zl = w == 0 && live ? d.zlab[lane] : 0.f;
+    const int32_t label = w == 0 && live ? d.targets[lane] : -1;
+    small_join<32 * NS>(d, 0, m, rest, at, l);
+    if (w == 0) {
+      // (of 32 rows the upper lanes have none)
+      const float tail = log1pf(rest), logp = live ? (zl - m) - tail : 0.f;
+      lse[lane] = live ? (m + tail) * kLog2e : INFINITY;  // (no target: z = 0, and p = 0)
+      own[lane] = expm1f(logp);
+      lab[lane] = label;
+      const int32_t count = __popcll(__builtin_amdgcn_ballot_w64(live));
+      const float inv = count > 0 ? 1.f / (float)count : 0.f, sum = wave_sum(logp);
+      if (wg == 0 && blockIdx.y == 0) {
+        if (lane < n) d.logp[lane] = logp;
+        if (lane == 0) {
+          d.loss[0] = -sum * inv;
+          *d.inv = inv;
+        }
+      }
+      if (lane == 0) scale = inv;
+    }
+    lds_barrier();
+  }
+  bf16x8h h[GP][NS][8];
+#pragma unroll
+  for (int p = 0; p < GP; ++p)
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        uint32_t f[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const uint32_t lo = reinterpret_cast<const uint32_t*>(&q[p][s][2 * t])[j >> 1];
+          const uint32_t hi = reinterpret_cast<const uint32_t*>(&q[p][s][2 * t + 1])[j >> 1];
+          f[t] = __builtin_amdgcn_perm(hi, lo, (j & 1) ? 0x07060302u : 0x05040100u);
+        }
+        h[p][s][j] = __builtin_bit_cast(bf16x8h, make_uint4(f[0], f[1], f[2], f[3]));
+      }
+  float l2[NS][8], ow[NS][8];
+  int32_t lb[NS][8];
+#pragma unroll
+  for (int s = 0; s < NS; ++s)
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      l2[s][t] = lse[32 * s + 8 * quad + t];
+      ow[s][t] = own[32 * s + 8 * quad + t];
+      lb[s][t] = lab[32 * s + 8 * quad + t];
+    }
+  const float inv = scale;
+  const int32_t blocks = (V + 16 * WV - 1) / (16 * WV);
+  const int32_t b0 = (int32_t)((int64_t)blocks * wg / d.gwgs), b1 = (int32_t)((int64_t)blocks * (wg + 1) / d.gwgs);
+  float4 z[NS][2];
+  auto fetch = [&](int32_t b) __attribute__((always_inline)) {
+    const int32_t v = min((b * WV + wv) * 16 + col, V - 1);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      z[s][0] = z[s][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (n > 0 && 32 * s + 8 * quad < ldz) {
+        const float4* const p = reinterpret_cast<const float4*>(d.z + (int64_t)v * ldz + 32 * s + 8 * quad);
+        z[s][0] = p[0];
+        z[s][1] = p[1];
+      }
+    }
+  };
+  if (b0 < b1) fetch(b0);
+  for (int32_t b = b0; b < b1; ++b) {
+    const int32_t v = (b * WV + wv) * 16 + col;
+    bf16x8h g[NS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      float p[8] = {z[s][0].x, z[s][0].y, z[s][0].z, z[s][0].w, z[s][1].x, z[s][1].y, z[s][1].z, z[s][1].w};
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        p[t] = __builtin_amdgcn_exp2f(fmaf(p[t], kLog2e, -l2[s][t]));
+        p[t] = lb[s][t] == v ? ow[s][t] : p[t];
+      }
+      const uint4 q = make_uint4(pack_bf2(p[0], p[1]), pack_bf2(p[2], p[3]), pack_bf2(p[4], p[5]), pack_bf2(p[6], p[7]));
+      g[s] = __builtin_bit_cast(bf16x8h, q);
+      if (d.grad && wc == 0 && blockIdx.y == 0 && v < V && 32 * s + 8 * quad < ldz)
+        *reinterpret_cast<uint4*>(d.grad + (int64_t)v * ldz + 32 * s + 8 * quad) = q;
+    }
+    if (b + 1 < b1) fetch(b + 1);
+#pragma unroll
+    for (int p = 0; p < GP; ++p) {
+      f32x4h a[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        a[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h[p][0][j], g[0], f32x4h{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+        if constexpr (NS == 2) a[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h[p][1][j], g[1], a[j], 0, 0, 0);
+      }
+      const int32_t k = 128 * (g0 + wc + 8 * p) + 32 * quad;
+      if (v < V && wc + 8 * p < groups) {
+        uint4* const to = reinterpret_cast<uint4*>(d.dW + (int64_t)v * width + k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (k + 8 * e < width)
+            to[e] = make_uint4(pack_bf2(a[0][e] * inv, a[1][e] * inv), pack_bf2(a[2][e] * inv, a[3][e] * inv),
+                               pack_bf2(a[4][e] * inv, a[5][e] * inv), pack_bf2(a[6][e] * inv, a[7][e] * inv));
+      }
+    }
+  }
+}
+
+static int small_share(int32_t d) { return d <= 256 ? 1 : d <= 512 ? 2 : d <= 1024 ? 4 : 8; }  // WK
+int32_t small_score_rows(int32_t d) { return 16 * (8 / small_share(d)); }
+int32_t small_grad_rows(int32_t d) {
+  const int32_t groups = (d + 127) / 128;
+  return 16 * (groups > 4 ? 1 : groups > 2 ? 2 : 8 / groups);
+}
+
+// Kernel arguments of two tenants take 0.3 KB, of kSmallTenants 3 KB.
+template <typename F>
+static hipError_t with_tenants(const TokSmallSet& set, F&& f) {
+  if (set.G > 2) return f(set);
+  TokSmallArgs<2> few;
+  few.t[0] = set.t[0];
+  few.t[1] = set.t[1];
+  few.G = set.G;
+  return f(few);
+}
+
+hipError_t launch_small_scores(hipStream_t s, const TokSmallSet& all, int32_t wgs, int32_t ldz, const void* hidden,
+                               int32_t T, int32_t d) {
+  const uint16_t* const h = static_cast<const uint16_t*>(hidden);
+  if (d > 8192 || d % 64 != 0) return hipErrorInvalidValue;
+  return with_tenants(all, [&](const auto& set) {
+    constexpr int C = sizeof(set.t) / sizeof(set.t[0]);
+    auto go = [&](auto wk, auto ch, auto nb) {
+      small_scores_kernel<wk(), ch(), nb(), C><<<wgs, kSmallThreads, 0, s>>>(set, ldz, h, T, d);
+      return hipGetLastError();
+    };
+    auto rows = [&](auto wk, auto ch) {
+      if (ldz == 16) return go(wk, ch, std::integral_constant<int, 1>());
+      if constexpr (decltype(ch)::value <= 2)
+        if (ldz == 32) return go(wk, ch, std::integral_constant<int, 2>());
+      if constexpr (decltype(ch)::value == 1)
+        if (ldz == 64) return go(wk, ch, std::integral_constant<int, 4>());
+      return hipErrorInvalidValue;
+    };
+    const auto one = std::integral_constant<int, 1>();
+    switch (small_share(d)) {
+      case 1: return rows(std::integral_constant<int, 1>(), one);
+      case 2: return rows(std::integral_constant<int, 2>(), one);
+      case 4: return rows(std::integral_constant<int, 4>(), one);
+      default:
+        if (d <= 2048) return rows(std::integral_constant<int, 8>(), one);
+        if (d <= 4096) return rows(std::integral_constant<int, 8>(), std::integral_constant<int, 2>());
+        return rows(std::integral_constant<int, 8>(), std::integral_constant<int, 4>());
+    }
+  });
+}
+
+hipError_t launch_small_grads(hipStream_t s, const TokSmallSet& all, int32_t wgs, int32_t ldz, const void* hidden,
+                              int32_t T, int32_t d) {
+  const uint16_t* const h = static_cast<const uint16_t*>(hidden);
+  const dim3 grid(wgs, (d + 2047) / 2048);
+  return with_tenants(all, [&](const auto& set) {
+    constexpr int C = sizeof(set.t) / sizeof(set.t[0]);
+    auto go = [&](auto gp, auto ns) {
+      small_grads_kernel<gp(), ns(), C><<<grid, kSmallThreads, 0, s>>>(set, ldz, h, T, d);
+      return hipGetLastError();
+    };
+    auto steps = [&](auto gp) {
+      return ldz > 32 ? go(gp, std::integral_constant<int, 2>()) : go(gp, std::integral_constant<int, 1>());
+    };
+    return d <= 1024 ? steps(std::integral_constant<int, 1>()) : steps(std::integral_constant<int, 2>());
+  });
+}
+
+hipError_t launch_small_pick(hipStream_t s, const TokSmallSet& all, int32_t ldz, int32_t T) {
+  return with_tenants(all, [&](const auto& set) {
+    constexpr int C = sizeof(set.t) / sizeof(set.t[0]);
+    small_pick_kernel<C><<<dim3(set.G, ldz / 16), kSmallThreads, 0, s>>>(set, T);
+    return hipGetLastError();
+  });
 }
 
 }  // namespace jnx
