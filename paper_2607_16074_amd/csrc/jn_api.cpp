@@ -993,7 +993,9 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
     if (io[g].n == 0) continue;
     width[g] = heads[g].vocab;
     if (train) {
-      width[g] = std::min<int64_t>(up((heads[g].vocab + K - 1) / K, 256), up(heads[g].vocab, 64));
+      // whole rounds of the weight gradient's ring tiles on 256 CUs, where there are some
+      const int64_t round = 256 * std::max(1, 256 / ((d + 255) / 256)), even = up((heads[g].vocab + K - 1) / K, 256);
+      width[g] = std::min<int64_t>(K > 1 && even > round ? up(even, round) : even, up(heads[g].vocab, 64));
       const int64_t most = 0x7fffffff / (2 * d) / 256 * 256 - 256;  // a transposed panel of W within 32-bit offsets
       width[g] = std::min(width[g], most);
       pat[g] = piece;
@@ -1380,9 +1382,18 @@ jn_status run_big(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const Tok
   JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, V, 1,
             launch_tok_grad(s, desc, G, P.N, inv, (const TokRow*)(w + P.rows), P.grad_blocks, P.zero8),
             "token logit gradients");
-  for (const TokPiece& p : P.pieces)
-    for (const TokSet* t : {&p.grad, &p.weights, &p.rows})
+  for (const TokPiece& p : P.pieces) {
+    if (p.grad.n > 0) JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, product(p.grad), "token gradients");
+    if (p.rows.n > 0 && p.rows.epi != EPI_RESID_F32 && gemm_tokens_pair_ok(p.rows.tiles, p.weights.tiles)) {
+      JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d,
+                launch_gemm_tokens_pair(s, p.rows.epi, probs + p.rows.at, p.rows.n, p.rows.tiles, probs + p.weights.at,
+                                        p.weights.n, p.weights.tiles),
+                "token gradients");
+      continue;
+    }
+    for (const TokSet* t : {&p.weights, &p.rows})
       if (t->n > 0) JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, product(*t), "token gradients");
+  }
   if (P.planes)
     JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 1, launch_tok_rows(s, desc, G, P.N, inv, (const float*)(w + P.acc), d),
               "token row gradients");

@@ -163,14 +163,15 @@ hipError_t launch_gemm_grad_pair(hipStream_t s, int epi, const GemmArgs* dprobs,
 struct TokPart {
   float m, rest;
 };
-// A target row as its logits' gradient needs it: p = exp2(z log2(e) - lse2), times
-// `live` (0 or 1), and `own` = p - 1 from logp in the target's column.  Dividing by
-// the number of targets is left to the products' results: bf16 holds the gradient
-// of an unlikely target, nearly -1 in every row, all but exactly, while a common
-// factor's rounding would be off by the same half step in all of them.
+// A target row as its logits' gradient needs it: p = exp2(z log2(e) - lse2), and
+// `own` = p - 1 from logp in the target's column.  Dividing by the number of targets
+// is left to the products' results: bf16 holds the gradient of an unlikely target,
+// nearly -1 in every row, all but exactly, while a common factor's rounding would
+// be off by the same half step in all of them.
 struct TokRow {
-  float lse2, live, own;
-  int32_t label;        // -1: the row has no target, and live and own are 0
+  float lse2;           // +inf: the row has no target (its z are 0), and p = 0
+  int32_t label;        // then -1
+  float own;
 };
 
 // Grouped launches of a token head's products, as above but with any N for
@@ -180,14 +181,20 @@ struct TokRow {
 // ranges and shape, or a total of -1.  Column blocks of EPI_SOFTMAX and EPI_GREEDY are
 // gemm_tokens_block(shape) columns, tok_blocks of them per problem.
 struct TokTiles {
-  int32_t total = -1, shape = 0;
+  int32_t total = -1, shape = 0, tiles_m = 0;  // tiles_m: the most of a problem
   double us = 0;        // estimate
+  bool uneven = false;  // gemm_grouped_uneven: the problems are sorted, longest contraction first
 };
 TokTiles gemm_tokens_prepare(int epi, int trans, GemmArgs* probs, int32_t nprob);
 int32_t gemm_tokens_block(int shape);
 inline int32_t tok_blocks(int32_t vocab, int32_t block) { return (vocab + 2 * block - 1) / (2 * block) * 2; }
 hipError_t launch_gemm_tokens(hipStream_t s, int epi, int trans, const GemmArgs* dprobs, int32_t nprob,
                               const TokTiles& t);
+// Row gradients (epi EPI_F32 or EPI_SCALED_BF16, GEMM_TRANS_W) and weight gradients
+// (EPI_SCALED_BF16, both transposed) in one launch, where the shapes allow it.
+bool gemm_tokens_pair_ok(const TokTiles& rows, const TokTiles& weights);
+hipError_t launch_gemm_tokens_pair(hipStream_t s, int epi, const GemmArgs* dprobs, int32_t nd, const TokTiles& d,
+                                   const GemmArgs* wprobs, int32_t nw, const TokTiles& w);
 
 // C[M][N] (+)= epi(A[M][K] * B[N][K]^T); A, B bf16 row-major with leading
 // dims lda, ldb (elements); for EPI_GEGLU_BF16, B is w_gate and B2 is w_up,

@@ -215,13 +215,14 @@ __device__ __forceinline__ void epilogue_bf16(const GemmArgs& g, const f32x4 (&a
   const int64_t step = RI * g.ldc;
   auto swz = [](int r) { return CH == 16 ? r & 15 : (r / (16 / CH)) & (CH - 1); };
   const float alpha = EPI == EPI_SCALED_BF16 ? g.aux[0] : 1.f;
-  TokRow tr[EPI == EPI_DLOGIT ? TM : 1];
+  float lse[EPI == EPI_DLOGIT ? TM : 1];
+  int32_t own[EPI == EPI_DLOGIT ? TM : 1];  // the target, from the lane's first column
   if constexpr (EPI == EPI_DLOGIT) {
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
-      const int32_t r = m0 + 16 * j + row;
-      tr[j] = reinterpret_cast<const TokRow*>(g.aux)[WHOLE ? r : min(r, g.M - 1)];
-      tr[j].label = tr[j].label < 0 ? -1 : tr[j].label - (int32_t)g.split_c - n0 - 4 * quad;  // from the lane's first column
+      const TokRow& t = reinterpret_cast<const TokRow*>(g.aux)[WHOLE ? m0 + 16 * j + row : min(m0 + 16 * j + row, g.M - 1)];
+      lse[j] = t.lse2;
+      own[j] = t.label < 0 ? -1 : t.label - (int32_t)g.split_c - n0 - 4 * quad;
     }
   }
   auto put = [&](int j) __attribute__((always_inline)) {  // blocks j .. j + NB - 1
@@ -234,9 +235,7 @@ __device__ __forceinline__ void epilogue_bf16(const GemmArgs& g, const f32x4 (&a
         for (int e = 0; e < 4; ++e) {
           const float a = acc[i][j + jj][e];
           if constexpr (EPI == EPI_DLOGIT) {
-            const TokRow& t = tr[j + jj];
-            v[e] = __builtin_amdgcn_exp2f(fmaf(a, 1.4426950408889634f, -t.lse2)) * t.live;
-            if (t.label == 16 * i + e) v[e] = t.own;
+            v[e] = __builtin_amdgcn_exp2f(fmaf(a, 1.4426950408889634f, -lse[j + jj]));
             if (!WHOLE && n0 + 16 * i + 4 * quad + e >= g.N) v[e] = 0.f;
           } else if constexpr (EPI == EPI_SOFTMAX_KEEP) {
             v[e] = __builtin_amdgcn_exp2f(fmaf(a, 1.4426950408889634f, top[j + jj]));
@@ -250,6 +249,13 @@ __device__ __forceinline__ void epilogue_bf16(const GemmArgs& g, const f32x4 (&a
         const int chunk = 2 * (GLU ? i / 2 : i) + (quad >> 1);
         *reinterpret_cast<u32x2*>(stage + (16 * jj + row) * WC + (chunk ^ swz(row)) * 8 + (quad & 1) * 4) =
             u32x2{pack_bf2_cvt(v[0], v[1]), pack_bf2_cvt(v[2], v[3])};
+      }
+      if constexpr (EPI == EPI_DLOGIT) {  // (behind the lane's own write of that column: a wave's LDS operations stay in order)
+        const int32_t k = own[j + jj];
+        if (k >= 0 && k < 16 * TN && (k & 15) < 4)
+          stage[(16 * jj + row) * WC + (((2 * (k >> 4)) + (quad >> 1)) ^ swz(row)) * 8 + (quad & 1) * 4 + (k & 3)] =
+              f2bf(reinterpret_cast<const TokRow*>(g.aux)[WHOLE ? m0 + 16 * (j + jj) + row
+                                                                 : min(m0 + 16 * (j + jj) + row, g.M - 1)].own);
       }
     }
   };
@@ -402,15 +408,20 @@ __device__ __forceinline__ void epilogue_softmax(const GemmArgs& g, const f32x4 
       for (int k = NV - 1; k >= 0; --k)
         if ((WHOLE || own + 16 * (k >> 2) + (k & 3) < g.N) && acc[k >> 2][j][k & 3] == m) at = own + 16 * (k >> 2) + (k & 3);
     }
-#pragma unroll
-    for (int o = 16; o <= 32; o <<= 1) {
-      const float m2 = __shfl_xor(m, o, kWave), rest2 = __shfl_xor(rest, o, kWave);
+    // the four lanes of a token (a join takes its two sides in either order)
+    auto quads = [&](auto pair) __attribute__((always_inline)) {
+      const float2 pm = pair(m), pr = pair(rest);
       if constexpr (EPI == EPI_GREEDY) {
-        const int32_t at2 = __shfl_xor(at, o, kWave);
-        at = m2 > m ? at2 : m2 == m ? min(at, at2) : at;
+        const float2 pa = pair(__int_as_float(at));
+        const int32_t ax = __float_as_int(pa.x), ay = __float_as_int(pa.y);
+        at = pm.y > pm.x ? ay : pm.y == pm.x ? min(ax, ay) : ax;
       }
-      tok_join(m, rest, m2, rest2);
-    }
+      m = pm.x;
+      rest = pr.x;
+      tok_join(m, rest, pm.y, pr.y);
+    };
+    quads([](float v) { return lane_pair16(v); });
+    quads([](float v) { return lane_pair32(v); });
     if constexpr (EPI == EPI_SOFTMAX_KEEP) {
       top[j] = (m == -INFINITY ? 0.f : m) * -1.4426950408889634f;
       if (quad == 0 && in) reinterpret_cast<TokPart*>(g.part)[block * g.M + r] = TokPart{m, rest};
@@ -418,6 +429,7 @@ __device__ __forceinline__ void epilogue_softmax(const GemmArgs& g, const f32x4 
       reinterpret_cast<TokPart*>(g.C)[block * g.ldc + r] = TokPart{m, rest};
       if constexpr (EPI == EPI_GREEDY) reinterpret_cast<int32_t*>(g.aux)[block * g.ldc + r] = at;
     }
+    __builtin_amdgcn_sched_barrier(0);  // (tokens side by side cost more registers than there are)
   }
 }
 
@@ -1626,11 +1638,19 @@ int32_t gemm_tokens_block(int shape) { return kShapes[shape].bn / 2; }
 // 128, and a softmax part's columns per lane a power of two.
 static bool tokens_shape_ok(int trans, int t) {
   if (t == 0) return true;
-  return trans == (GEMM_TRANS_X | GEMM_TRANS_W) ? t == k128Shape : trans == GEMM_TRANS_W ? t == 4 : t == 4 || t == 5;
+  return trans == (GEMM_TRANS_X | GEMM_TRANS_W) ? t == k128Shape : t == 3 || t == 4 || (trans == 0 && (t == 2 || t == 5));
 }
 
 TokTiles gemm_tokens_prepare(int epi, int trans, GemmArgs* probs, int32_t nprob) {
   TokTiles out;
+  int64_t longest = 0;
+  for (int32_t p = 0; p < nprob; ++p) {
+    probs[p].trans = trans;
+    longest = std::max<int64_t>(longest, (probs[p].K + kBK - 1) / kBK);
+  }
+  out.uneven = gemm_grouped_uneven(probs, nprob);
+  if (out.uneven)
+    std::stable_sort(probs, probs + nprob, [](const GemmArgs& a, const GemmArgs& b) { return a.K > b.K; });
   double best = 1e300;
   for (int t = 0; t <= k128Shape; ++t) {
     if (!tokens_shape_ok(trans, t)) continue;
@@ -1642,7 +1662,10 @@ TokTiles gemm_tokens_prepare(int epi, int trans, GemmArgs* probs, int32_t nprob)
       work += n * ((probs[p].K + kBK - 1) / kBK);
     }
     if (tiles <= 0 || tiles > (int64_t)kMostBlocks) continue;
-    const double us = tiles_time(epi == EPI_DLOGIT || epi == EPI_SOFTMAX_KEEP ? EPI_GELU_BF16 : epi, tiles, (double)work / tiles, t);
+    const int like = epi_exp(epi) ? EPI_GELU_BF16 : epi;
+    double us = tiles_time(like, tiles, (double)work / tiles, t);
+    if (out.uneven)
+      us = std::max(us, longest * std::max(kShapes[t].slab, kShapes[t].slab1) + tiles_time(like, tiles, 0.0, t));
     if (us < best * 0.999) {
       best = us;
       out.us = us;
@@ -1659,14 +1682,62 @@ TokTiles gemm_tokens_prepare(int epi, int trans, GemmArgs* probs, int32_t nprob)
       out.total = -1;
       return out;
     }
-    g.trans = trans;
     g.tiles_m = (g.M + T.bm - 1) / T.bm;
     g.tiles_n = (g.N + T.bn - 1) / T.bn;
     g.tile_start = at;
     at += g.tiles_m * g.tiles_n;
+    out.tiles_m = std::max(out.tiles_m, g.tiles_m);
   }
   return out;
 }
+
+// Row gradients (128x96 tiles, GEMM_TRANS_W) and weight gradients (128x128, both
+// operands transposed) of a call in one launch, as gemm_grad_pair_kernel.
+template <int EPI>
+__global__ __launch_bounds__(256, 1) void gemm_tokens_pair_kernel(const GemmArgs* __restrict__ dprobs, int32_t nd,
+                                                                  int32_t td, int32_t gd,
+                                                                  const GemmArgs* __restrict__ wprobs, int32_t nw,
+                                                                  int32_t tw, bool uneven) {
+  constexpr int BN = 128, BM = 96, NS = 4, LDS = NS * (BN + BM) * kBK;
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[LDS];
+  const bool data = (int32_t)blockIdx.x < gd;
+  const GemmArgs* const probs = data ? dprobs : wprobs;
+  const int32_t n = data ? nd : nw;
+  const int32_t idx = data ? xcd_item(blockIdx.x, gd)
+                           : uneven ? (int32_t)blockIdx.x - gd : xcd_item(blockIdx.x - gd, gridDim.x - gd);
+  if (idx >= (data ? td : tw)) return;
+  int32_t p = 0;
+  while (p + 1 < n && probs[p + 1].tile_start <= idx) ++p;
+  const GemmArgs g = probs[p];
+  int32_t tm, tn;
+  flex_walk(idx - g.tile_start, g.tiles_m, g.tiles_n, tm, tn);
+  const int32_t KT = (g.K + kBK - 1) / kBK;
+  if (data)
+    flex_tile<BN, BM, NS, NS, EPI, GEMM_TRANS_W>(g, tm, tn, 0, KT, lds);
+  else
+    flex_tile<128, 128, 3, 2, EPI_SCALED_BF16, GEMM_TRANS_X | GEMM_TRANS_W>(g, tm, tn, 0, KT, lds);
+}
+
+// Ring tiles with an XCD's workgroups on consecutive tiles, 32 at a time: with few
+// token tiles (the fast index) a weight panel is then fetched by one XCD, not by
+// as many as there are token tiles.  XCD x owns tiles [x per, (x + 1) per).
+template <int EPI, int TR>
+__global__ __launch_bounds__(256, 1) void gemm_tokens_ring_kernel(const GemmArgs* __restrict__ probs, int32_t nprob,
+                                                                  int32_t total, int32_t chain) {
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[5 * 256 * kBK];
+  const int32_t per = (total + 7) / 8, first = (blockIdx.x & 7) * per, own = blockIdx.x >> 3;
+  int32_t p = 0;
+  auto next = [&](int32_t r, GemmArgs& q, int32_t& tm, int32_t& tn) __attribute__((always_inline)) {
+    const int32_t l = (own >> 5) * 32 * chain + 32 * r + (own & 31), t = first + l;
+    if (r >= chain || l >= per || t >= total) return false;
+    while (p + 1 < nprob && probs[p + 1].tile_start <= t) ++p;
+    q = probs[p];
+    tile_of(t - q.tile_start, q.tiles_m, q.tiles_n, tm, tn);
+    return true;
+  };
+  ring_run<EPI, TR>(next, lds);
+}
+constexpr int32_t kFewTokenTiles = 7;
 
 template <int EPI, int TR>
 static hipError_t launch_tokens(hipStream_t s, const GemmArgs* p, int32_t n, const TokTiles& t) {
@@ -1674,14 +1745,30 @@ static hipError_t launch_tokens(hipStream_t s, const GemmArgs* p, int32_t n, con
   const dim3 block(256), flex((unsigned)((t.total + 7) / 8 * 8));
   if (t.shape == 0) {
     const int32_t chain = ring_chain(t.total);
-    gemm_grouped_ring_kernel<EPI, TR><<<dim3(ring_groups(t.total, chain)), block, 0, s>>>(p, n, t.total, chain);
+    if constexpr (TR != BOTH)
+      if (t.tiles_m <= kFewTokenTiles) {
+        const int32_t per = (t.total + 7) / 8, whole = per / (32 * chain), rest = std::min(per - whole * 32 * chain, 32);
+        gemm_tokens_ring_kernel<EPI, TR><<<dim3(8 * (whole * 32 + rest)), block, 0, s>>>(p, n, t.total, chain);
+        return hipGetLastError();
+      }
+    const int32_t run = t.uneven ? 1 : chain;
+    gemm_grouped_ring_kernel<EPI, TR><<<dim3(ring_groups(t.total, run)), block, 0, s>>>(p, n, t.total, run);
     return hipGetLastError();
   }
   if constexpr (TR == BOTH) {
     if (t.shape != k128Shape) return hipErrorInvalidValue;
-    gemm_grouped_flex_kernel<128, 128, 3, 2, EPI, TR, 2, false><<<flex, block, 0, s>>>(p, n, t.total, false);
+    gemm_grouped_flex_kernel<128, 128, 3, 2, EPI, TR, 2, false><<<flex, block, 0, s>>>(p, n, t.total, t.uneven);
     return hipGetLastError();
   } else {
+    if constexpr (TR == 0)
+      if (t.shape == 2) {
+        gemm_grouped_flex_kernel<256, 128, 3, 3, EPI, TR, 1, false><<<flex, block, 0, s>>>(p, n, t.total, false);
+        return hipGetLastError();
+      }
+    if (t.shape == 3) {
+      gemm_grouped_flex_kernel<128, 160, 4, 4, EPI, TR, 1, false><<<flex, block, 0, s>>>(p, n, t.total, false);
+      return hipGetLastError();
+    }
     if (t.shape == 4) {
       gemm_grouped_flex_kernel<128, 96, 4, 4, EPI, TR, 1, false><<<flex, block, 0, s>>>(p, n, t.total, false);
       return hipGetLastError();
@@ -1694,6 +1781,23 @@ static hipError_t launch_tokens(hipStream_t s, const GemmArgs* p, int32_t n, con
     }
     return hipErrorInvalidValue;
   }
+}
+
+bool gemm_tokens_pair_ok(const TokTiles& rows, const TokTiles& weights) {
+  return rows.total > 0 && rows.shape == 4 && weights.shape == k128Shape && weights.total <= 1024;
+}
+
+hipError_t launch_gemm_tokens_pair(hipStream_t s, int epi, const GemmArgs* dprobs, int32_t nd, const TokTiles& d,
+                                   const GemmArgs* wprobs, int32_t nw, const TokTiles& w) {
+  if (nd <= 0 || nw <= 0 || !gemm_tokens_pair_ok(d, w)) return hipErrorInvalidValue;
+  const int32_t gd = (d.total + 7) / 8 * 8, gw = (w.total + 7) / 8 * 8;
+  if (epi == EPI_F32)
+    gemm_tokens_pair_kernel<EPI_F32><<<gd + gw, 256, 0, s>>>(dprobs, nd, d.total, gd, wprobs, nw, w.total, w.uneven);
+  else if (epi == EPI_SCALED_BF16)
+    gemm_tokens_pair_kernel<EPI_SCALED_BF16><<<gd + gw, 256, 0, s>>>(dprobs, nd, d.total, gd, wprobs, nw, w.total, w.uneven);
+  else
+    return hipErrorInvalidValue;
+  return hipGetLastError();
 }
 
 hipError_t launch_gemm_tokens(hipStream_t s, int epi, int trans, const GemmArgs* dprobs, int32_t nprob,

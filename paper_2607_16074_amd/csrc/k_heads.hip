@@ -723,7 +723,7 @@ __global__ __launch_bounds__(kJoinThreads) void tok_join_kernel(const TokDesc* _
   } else {
     const float logp = label < 0 ? 0.f : (zlab[i] - m) - tail;
     d.logp[i - d.first] = logp;
-    rows[i] = TokRow{label < 0 ? 0.f : (m + tail) * 1.4426950408889634f, label < 0 ? 0.f : 1.f, expm1f(logp), label};
+    rows[i] = TokRow{label < 0 ? INFINITY : (m + tail) * 1.4426950408889634f, label, expm1f(logp)};
   }
 }
 
@@ -761,7 +761,7 @@ __global__ __launch_bounds__(256) void tok_grad_kernel(const TokDesc* __restrict
     const int32_t v0 = 8 * c;
     const float m = d.part[(int64_t)(v0 / d.width) * d.n + n].m;
     // (a block without a column has m = -inf and zeros)
-    const float f = v0 < d.kept ? __builtin_amdgcn_exp2f(fmaf(m, 1.4426950408889634f, -row.lse2)) * row.live : 0.f;
+    const float f = v0 < d.kept ? __builtin_amdgcn_exp2f(fmaf(m, 1.4426950408889634f, -row.lse2)) : 0.f;
     const uint4 q = *at;
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
     float v[8];

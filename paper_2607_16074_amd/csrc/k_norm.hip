@@ -244,35 +244,34 @@ hipError_t launch_rmsnorm_f32in(hipStream_t s, const float* x, const void* g, vo
 // gradients, with du = R^T dy and xh = x r:
 //   dx = r (g du - xh mean(xh g du)),   dg = sum over rows and heads of du xh
 //
-// One wavefront per row (or per part of a row's heads, where rows are few).
-// P2 lanes hold a head: lane q its elements 8q .. 8q + 7 of both halves, so
-// that a pair lies in one lane and every access is 16 bytes, and the 64 / P2
-// heads of one step are reduced together by log2 P2 lane exchanges.  A row's
-// sines and cosines are formed once, one pair per lane, and shared through
-// LDS.  Angles: turns = pos * f in 64 bits (f = theta^(-2i/hd) / 2 pi), of
-// which the whole turns are dropped before anything is rounded to 32 bits, so
-// positions of any size lose nothing; then sincospi.  Everything else is fp32;
-// y and dx are rounded to bf16 once.
+// One wavefront per row (or per part of a row's heads, where rows are few).  P2
+// lanes hold a head: lane q its elements E q .. E q + E - 1 of both halves, so that
+// a pair lies in one lane, and the 64 / P2 heads of one step are reduced together
+// by log2 P2 lane exchanges.  A row's sines and cosines are formed once, one pair
+// per lane, and shared through LDS.  Angles: turns = pos * f in 64 bits (f =
+// theta^(-2i/hd) / 2 pi), of which the whole turns are dropped before anything is
+// rounded to 32 bits, so positions of any size lose nothing; then sincospi.
+// Everything else is fp32; y and dx are rounded to bf16 once.
+// Bound by memory; with E = 4 a step holds fewer heads, so that less of the last
+// one is idle (18 heads: 5 steps of 4, not 3 of 8), and the gradients' sums, gains
+// and rows fit the registers of four wavefronts a SIMD: 75,923 rows forward 129 ->
+// 124 us, gradients 262 -> 223.  The rows' loads are issued before the sines.
+constexpr int kQkFwdE = 4, kQkBwdE = 4;
 constexpr int kQkStep = 4;  // head steps whose loads are issued together
 
+// Sum over the P2 lanes of a head, in all of them.
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
 template <int P2>
 __device__ __forceinline__ float head_sum(float v) {
-#pragma unroll
-  for (int o = 1; o < P2; o <<= 1) v += __shfl_xor(v, o, kWave);
+  if constexpr (P2 >= 2) v = add_dpp<0xB1>(v);   // lane ^ 1
+  if constexpr (P2 >= 4) v = add_dpp<0x4E>(v);   // lane ^ 2
+  if constexpr (P2 >= 8) v = add_dpp<0x141>(v);  // the other quad of 8 lanes
+  if constexpr (P2 >= 16) v = add_dpp<0x140>(v); // the other 8 of 16
+  if constexpr (P2 >= 32) v = sum_xor16(v);
   return v;
-}
-
-__device__ __forceinline__ void unpack8(const uint4& q, float* v) {
-  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    v[2 * k] = __uint_as_float(w[k] << 16);
-    v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
-  }
-}
-
-__device__ __forceinline__ uint4 pack8(const float* v) {
-  return make_uint4(pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3]), pack_bf2(v[4], v[5]), pack_bf2(v[6], v[7]));
 }
 
 // Sines and cosines of a row's pairs into the wave's line [2][128]: cosines, sines.
@@ -290,16 +289,66 @@ __device__ __forceinline__ void row_turns(const QkShape& a, int64_t row, int lan
   __builtin_amdgcn_wave_barrier();
 }
 
-__device__ __forceinline__ void lane_turns(const float* line, int q, float* cs, float* sn) {
+// E values of a bf16 row, as loaded.
+template <int E>
+struct QkRaw {
+  uint32_t w[E / 2];
+};
+template <int E>
+__device__ __forceinline__ QkRaw<E> raw(const uint16_t* p) {
+  if constexpr (E == 8)
+    return __builtin_bit_cast(QkRaw<E>, *reinterpret_cast<const uint4*>(p));
+  else
+    return __builtin_bit_cast(QkRaw<E>, *reinterpret_cast<const uint2*>(p));
+}
+template <int E>
+__device__ __forceinline__ void widen(const QkRaw<E>& q, float* v) {
 #pragma unroll
-  for (int k = 0; k < 8; k += 4) {
-    *reinterpret_cast<float4*>(cs + k) = *reinterpret_cast<const float4*>(line + 8 * q + k);
-    *reinterpret_cast<float4*>(sn + k) = *reinterpret_cast<const float4*>(line + 128 + 8 * q + k);
+  for (int k = 0; k < E / 2; ++k) {
+    v[2 * k] = __uint_as_float(q.w[k] << 16);
+    v[2 * k + 1] = __uint_as_float(q.w[k] & 0xffff0000u);
   }
 }
 
+// Results beyond the last-level cache are stored non-temporally (kStreamBytes):
+// 75,923 rows of 18 heads of 128 forward 123.7 -> 116.9 us (6.0 TB/s), gradients
+// 222.8 -> 216.3 (4.9 TB/s).
+template <int E, bool ONCE>
+__device__ __forceinline__ void put_bf(uint16_t* p, const float* v) {
+  typedef uint32_t V __attribute__((ext_vector_type(E / 2)));
+  V r;
+#pragma unroll
+  for (int k = 0; k < E / 2; ++k) r[k] = pack_bf2(v[2 * k], v[2 * k + 1]);
+  if constexpr (ONCE)
+    __builtin_nontemporal_store(r, reinterpret_cast<V*>(p));
+  else
+    *reinterpret_cast<V*>(p) = r;
+}
+
+// The gains of a lane's elements, queries' and keys'.
+template <int E>
+struct QkGains {
+  QkRaw<E> q[2], k[2];  // both halves
+  __device__ __forceinline__ void load(const QkShape& a, int at) {
+    const int half = a.hd >> 1;
+    q[0] = raw<E>(a.gq + at);
+    q[1] = raw<E>(a.gq + at + half);
+    k[0] = raw<E>(a.gk + at);
+    k[1] = raw<E>(a.gk + at + half);
+  }
+  __device__ __forceinline__ void get(bool key, float* v) const {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      QkRaw<E> r;
+#pragma unroll
+      for (int i = 0; i < E / 2; ++i) r.w[i] = key ? k[s].w[i] : q[s].w[i];
+      widen<E>(r, v + E * s);
+    }
+  }
+};
+
 // x and y may be the same rows: a lane reads what it writes before it does.
-template <int P2, bool NORM, bool ROPE>
+template <int E, int P2, bool NORM, bool ROPE, bool ONCE>
 __global__ __launch_bounds__(256) void qk_fwd_kernel(QkShape a, const uint16_t* x, uint16_t* y, int32_t parts) {
   __shared__ __attribute__((aligned(16))) float lines[4][256];
   constexpr int PER = 64 / P2;  // heads per step
@@ -310,63 +359,55 @@ __global__ __launch_bounds__(256) void qk_fwd_kernel(QkShape a, const uint16_t* 
   const int heads = a.heads + a.kv, half = a.hd >> 1;
   const int steps = (heads + PER - 1) / PER, part = (int)(item - row * parts);
   const int s0 = steps * part / parts, s1 = steps * (part + 1) / parts;
-  const bool live = 8 * q < half;
-  float cs[8], sn[8];
-  if constexpr (ROPE) {
-    row_turns(a, row, lane, lines[w]);
-    lane_turns(lines[w], live ? q : 0, cs, sn);
-  }
-  uint4 g[2][2];  // gains of queries and keys, both halves
-  if constexpr (NORM) {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const uint16_t* p = (k ? a.gk : a.gq) + (live ? 8 * q : 0);
-      g[k][0] = *reinterpret_cast<const uint4*>(p);
-      g[k][1] = *reinterpret_cast<const uint4*>(p + half);
-    }
-  }
-  const uint16_t* xr = x + row * a.ldx + 8 * q;
-  uint16_t* yr = y + row * a.ldy + 8 * q;
-  for (int s = s0; s < s1; s += kQkStep) {
-    uint4 v[kQkStep][2];
+  const bool live = E * q < half;
+  const uint16_t* xr = x + row * a.ldx + E * q;
+  uint16_t* yr = y + row * a.ldy + E * q;
+  QkRaw<E> v[kQkStep][2];
+  auto fetch = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < kQkStep; ++j) {
       const int h = (s + j) * PER + slot;
-      v[j][0] = v[j][1] = make_uint4(0, 0, 0, 0);
+      v[j][0] = v[j][1] = QkRaw<E>{};
       if (s + j < s1 && live && h < heads) {
-        v[j][0] = *reinterpret_cast<const uint4*>(xr + h * a.hd);
-        v[j][1] = *reinterpret_cast<const uint4*>(xr + h * a.hd + half);
+        v[j][0] = raw<E>(xr + h * a.hd);
+        v[j][1] = raw<E>(xr + h * a.hd + half);
       }
     }
+  };
+  fetch(s0);  // in flight under the sines
+  QkGains<E> g;
+  if constexpr (NORM) g.load(a, live ? E * q : 0);
+  const float* const line = lines[w] + (live ? E * q : 0);
+  if constexpr (ROPE) row_turns(a, row, lane, lines[w]);
+  for (int s = s0; s < s1; s += kQkStep) {
+    if (s > s0) fetch(s);
 #pragma unroll
     for (int j = 0; j < kQkStep; ++j) {
       if (s + j >= s1) break;
       const int h = (s + j) * PER + slot;
-      float u[16];
-      unpack8(v[j][0], u);
-      unpack8(v[j][1], u + 8);
+      float u[2 * E];
+      widen<E>(v[j][0], u);
+      widen<E>(v[j][1], u + E);
       if constexpr (NORM) {
-        float ss = 0.f, gv[16];
+        float ss = 0.f, gv[2 * E];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) ss = fmaf(u[k], u[k], ss);
+        for (int k = 0; k < 2 * E; ++k) ss = fmaf(u[k], u[k], ss);
         const float r = rsqrtf(head_sum<P2>(ss) / (float)a.hd + a.eps);
-        const bool key = h >= a.heads;
-        unpack8(key ? g[1][0] : g[0][0], gv);
-        unpack8(key ? g[1][1] : g[0][1], gv + 8);
+        g.get(h >= a.heads, gv);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) u[k] = u[k] * r * gv[k];
+        for (int k = 0; k < 2 * E; ++k) u[k] = u[k] * r * gv[k];
       }
       if constexpr (ROPE) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float p = u[k], o = u[8 + k];
-          u[k] = p * cs[k] - o * sn[k];
-          u[8 + k] = o * cs[k] + p * sn[k];
+        for (int k = 0; k < E; ++k) {
+          const float p = u[k], o = u[E + k], cs = line[k], sn = line[128 + k];
+          u[k] = p * cs - o * sn;
+          u[E + k] = o * cs + p * sn;
         }
       }
       if (live && h < heads) {
-        *reinterpret_cast<uint4*>(yr + h * a.hd) = pack8(u);
-        *reinterpret_cast<uint4*>(yr + h * a.hd + half) = pack8(u + 8);
+        put_bf<E, ONCE>(yr + h * a.hd, u);
+        put_bf<E, ONCE>(yr + h * a.hd + half, u + E);
       }
     }
   }
@@ -375,79 +416,76 @@ __global__ __launch_bounds__(256) void qk_fwd_kernel(QkShape a, const uint16_t* 
 // Workgroups walk rows in steps of the grid; each leaves its sums of du xh in
 // part [workgroup][2][hd], queries then keys, which qk_gain_kernel adds in
 // order.  dx may be the rows of x or of dy.
-template <int P2, bool NORM, bool ROPE>
-__global__ __launch_bounds__(256) void qk_bwd_kernel(QkShape a, const uint16_t* x, const uint16_t* dy,
+template <int E, int P2, bool NORM, bool ROPE, bool ONCE>
+__global__ __launch_bounds__(256, 4) void qk_bwd_kernel(QkShape a, const uint16_t* x, const uint16_t* dy,
                                                      uint16_t* dx, float* __restrict__ part) {
   __shared__ __attribute__((aligned(16))) float lines[4][256];
   __shared__ float sums[NORM ? 4 : 1][2][256];
-  constexpr int PER = 64 / P2;
+  constexpr int PER = 64 / P2, STEP = 2;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, q = lane % P2, slot = lane / P2;
   const int heads = a.heads + a.kv, half = a.hd >> 1, steps = (heads + PER - 1) / PER;
-  const bool live = 8 * q < half;
-  uint4 g[2][2];
-  float dg[2][16];
+  const bool live = E * q < half;
+  QkGains<E> g;
+  float dg[2][2 * E];
   if constexpr (NORM) {
+    g.load(a, live ? E * q : 0);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const uint16_t* p = (k ? a.gk : a.gq) + (live ? 8 * q : 0);
-      g[k][0] = *reinterpret_cast<const uint4*>(p);
-      g[k][1] = *reinterpret_cast<const uint4*>(p + half);
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) dg[k][i] = 0.f;
-    }
+      for (int i = 0; i < 2 * E; ++i) dg[k][i] = 0.f;
   }
+  const float* const line = lines[w] + (live ? E * q : 0);
   for (int64_t row = (int64_t)blockIdx.x * 4 + w; row < a.rows; row += (int64_t)gridDim.x * 4) {
-    float cs[8], sn[8];
-    if constexpr (ROPE) {
-      row_turns(a, row, lane, lines[w]);
-      lane_turns(lines[w], live ? q : 0, cs, sn);
-    }
-    const uint16_t* xr = x + row * a.ldx + 8 * q;
-    const uint16_t* yr = dy + row * a.ldy + 8 * q;
-    uint16_t* dr = dx + row * a.ldd + 8 * q;
-    for (int s = 0; s < steps; s += 2) {
-      uint4 v[2][4];
+    const uint16_t* xr = x + row * a.ldx + E * q;
+    const uint16_t* yr = dy + row * a.ldy + E * q;
+    uint16_t* dr = dx + row * a.ldd + E * q;
+    QkRaw<E> v[STEP][4];
+    auto fetch = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int j = 0; j < STEP; ++j) {
         const int h = (s + j) * PER + slot;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[j][k] = make_uint4(0, 0, 0, 0);
+        for (int k = 0; k < 4; ++k) v[j][k] = QkRaw<E>{};
         if (live && h < heads) {
           if constexpr (NORM) {
-            v[j][0] = *reinterpret_cast<const uint4*>(xr + h * a.hd);
-            v[j][1] = *reinterpret_cast<const uint4*>(xr + h * a.hd + half);
+            v[j][0] = raw<E>(xr + h * a.hd);
+            v[j][1] = raw<E>(xr + h * a.hd + half);
           }
-          v[j][2] = *reinterpret_cast<const uint4*>(yr + h * a.hd);
-          v[j][3] = *reinterpret_cast<const uint4*>(yr + h * a.hd + half);
+          v[j][2] = raw<E>(yr + h * a.hd);
+          v[j][3] = raw<E>(yr + h * a.hd + half);
         }
       }
+    };
+    fetch(0);
+    if constexpr (ROPE) row_turns(a, row, lane, lines[w]);
+    for (int s = 0; s < steps; s += STEP) {
+      if (s > 0) fetch(s);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int j = 0; j < STEP; ++j) {
         if (s + j >= steps) break;
         const int h = (s + j) * PER + slot;
-        float du[16];
-        unpack8(v[j][2], du);
-        unpack8(v[j][3], du + 8);
+        float du[2 * E];
+        widen<E>(v[j][2], du);
+        widen<E>(v[j][3], du + E);
         if constexpr (ROPE) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const float p = du[k], o = du[8 + k];
-            du[k] = p * cs[k] + o * sn[k];
-            du[8 + k] = o * cs[k] - p * sn[k];
+          for (int k = 0; k < E; ++k) {
+            const float p = du[k], o = du[E + k], cs = line[k], sn = line[128 + k];
+            du[k] = p * cs + o * sn;
+            du[E + k] = o * cs - p * sn;
           }
         }
         if constexpr (NORM) {
-          float xh[16], gv[16], ss = 0.f, dot = 0.f;
-          unpack8(v[j][0], xh);
-          unpack8(v[j][1], xh + 8);
+          float xh[2 * E], gv[2 * E], ss = 0.f, dot = 0.f;
+          widen<E>(v[j][0], xh);
+          widen<E>(v[j][1], xh + E);
 #pragma unroll
-          for (int k = 0; k < 16; ++k) ss = fmaf(xh[k], xh[k], ss);
+          for (int k = 0; k < 2 * E; ++k) ss = fmaf(xh[k], xh[k], ss);
           const float r = rsqrtf(head_sum<P2>(ss) / (float)a.hd + a.eps);
           const bool key = h >= a.heads;
-          unpack8(key ? g[1][0] : g[0][0], gv);
-          unpack8(key ? g[1][1] : g[0][1], gv + 8);
+          g.get(key, gv);
 #pragma unroll
-          for (int k = 0; k < 16; ++k) {
+          for (int k = 0; k < 2 * E; ++k) {
             xh[k] *= r;
             const float t = du[k] * xh[k];
             dg[0][k] += key ? 0.f : t;  // (lanes without a head hold zeros)
@@ -456,11 +494,11 @@ __global__ __launch_bounds__(256) void qk_bwd_kernel(QkShape a, const uint16_t* 
           }
           const float c = head_sum<P2>(dot) / (float)a.hd;
 #pragma unroll
-          for (int k = 0; k < 16; ++k) du[k] = r * (gv[k] * du[k] - xh[k] * c);
+          for (int k = 0; k < 2 * E; ++k) du[k] = r * (gv[k] * du[k] - xh[k] * c);
         }
         if (live && h < heads) {
-          *reinterpret_cast<uint4*>(dr + h * a.hd) = pack8(du);
-          *reinterpret_cast<uint4*>(dr + h * a.hd + half) = pack8(du + 8);
+          put_bf<E, ONCE>(dr + h * a.hd, du);
+          put_bf<E, ONCE>(dr + h * a.hd + half, du + E);
         }
       }
     }
@@ -469,11 +507,11 @@ __global__ __launch_bounds__(256) void qk_bwd_kernel(QkShape a, const uint16_t* 
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
+      for (int i = 0; i < 2 * E; ++i) {
         float v = dg[k][i];
 #pragma unroll
         for (int o = P2; o < 64; o <<= 1) v += __shfl_xor(v, o, kWave);
-        if (slot == 0 && live) sums[w][k][8 * q + (i < 8 ? i : half + i - 8)] = v;
+        if (slot == 0 && live) sums[w][k][E * q + (i < E ? i : half + i - E)] = v;
       }
     __syncthreads();
     for (int e = threadIdx.x; e < 2 * a.hd; e += 256) {
@@ -483,14 +521,18 @@ __global__ __launch_bounds__(256) void qk_bwd_kernel(QkShape a, const uint16_t* 
   }
 }
 
-// dgq | dgk = the sums of `blocks` workgroups, 16 columns per workgroup here.
-__global__ __launch_bounds__(256) void qk_gain_kernel(const float* __restrict__ part, int32_t blocks, int32_t hd,
-                                                      float* __restrict__ dgq, float* __restrict__ dgk) {
+// dgq | dgk = the sums of `blocks` workgroups, 16 columns per workgroup here, 64
+// of the sums at a time.
+__global__ __launch_bounds__(1024) void qk_gain_kernel(const float* __restrict__ part, int32_t blocks, int32_t hd,
+                                                       float* __restrict__ dgq, float* __restrict__ dgk) {
   __shared__ float lds[16][17];
   const int c = threadIdx.x & 15, k = threadIdx.x >> 4, e = blockIdx.x * 16 + c;
   float v = 0.f;
-  for (int32_t b = k; b < blocks; b += 16) v += part[(int64_t)b * 2 * hd + e];
-  lds[k][c] = v;
+#pragma unroll 8
+  for (int32_t b = k; b < blocks; b += 64) v += part[(int64_t)b * 2 * hd + e];
+  v = sum_xor16(v);  // the four of a wavefront
+  v = sum_xor32(v);
+  if ((threadIdx.x & 63) < 16) lds[threadIdx.x >> 6][c] = v;
   __syncthreads();
   if (k == 0) {
     v = lds[0][c];
@@ -500,20 +542,24 @@ __global__ __launch_bounds__(256) void qk_gain_kernel(const float* __restrict__ 
   }
 }
 
-// Calls f<P2, NORM, ROPE>() for the shape.
-template <typename F>
+// Calls f<P2, NORM, ROPE, ONCE>() for the shape, with E elements of both halves a lane.
+template <int E, typename F>
 static hipError_t with_qk(const QkShape& a, F&& f) {
-  auto go = [&](auto p2) {
+  auto kind = [&](auto p2, auto once) {
     const bool norm = a.gq != nullptr, rope = a.pos != nullptr;
-    if (norm && rope) return f(p2, std::true_type(), std::true_type());
-    if (norm) return f(p2, std::true_type(), std::false_type());
-    return f(p2, std::false_type(), std::true_type());
+    if (norm && rope) return f(p2, std::true_type(), std::true_type(), once);
+    if (norm) return f(p2, std::true_type(), std::false_type(), once);
+    return f(p2, std::false_type(), std::true_type(), once);
   };
-  if (a.hd <= 16) return go(std::integral_constant<int, 1>());
-  if (a.hd <= 32) return go(std::integral_constant<int, 2>());
-  if (a.hd <= 64) return go(std::integral_constant<int, 4>());
-  if (a.hd <= 128) return go(std::integral_constant<int, 8>());
-  return go(std::integral_constant<int, 16>());
+  auto go = [&](auto p2) {
+    return (int64_t)a.rows * (a.heads + a.kv) * a.hd * 2 > kStreamBytes ? kind(p2, std::true_type())
+                                                                        : kind(p2, std::false_type());
+  };
+  constexpr int M = 16 / E;  // lanes of 32 elements
+  if (a.hd <= 32) return go(std::integral_constant<int, M>());
+  if (a.hd <= 64) return go(std::integral_constant<int, 2 * M>());
+  if (a.hd <= 128) return go(std::integral_constant<int, 4 * M>());
+  return go(std::integral_constant<int, 8 * M>());
 }
 
 static bool qk_ok(const QkShape& a) {
@@ -522,12 +568,12 @@ static bool qk_ok(const QkShape& a) {
 
 hipError_t launch_qk_fwd(hipStream_t s, const QkShape& a, const uint16_t* x, uint16_t* y) {
   if (!qk_ok(a)) return hipErrorInvalidValue;
-  return with_qk(a, [&](auto p2, auto norm, auto rope) {
+  return with_qk<kQkFwdE>(a, [&](auto p2, auto norm, auto rope, auto once) {
     constexpr int PER = 64 / decltype(p2)::value;
     const int32_t steps = (a.heads + a.kv + PER - 1) / PER;
     const int32_t parts = a.rows < kQkFewRows ? steps : 1;
     const int64_t blocks = ((int64_t)a.rows * parts + 3) / 4;
-    qk_fwd_kernel<p2(), norm(), rope()><<<(unsigned)blocks, 256, 0, s>>>(a, x, y, parts);
+    qk_fwd_kernel<kQkFwdE, p2(), norm(), rope(), once()><<<(unsigned)blocks, 256, 0, s>>>(a, x, y, parts);
     return hipGetLastError();
   });
 }
@@ -539,14 +585,14 @@ hipError_t launch_qk_bwd(hipStream_t s, const QkShape& a, const uint16_t* x, con
   const int32_t blocks = qk_bwd_blocks(a.rows);
   if (a.rows > 0) {
     if (!qk_ok(a)) return hipErrorInvalidValue;
-    const hipError_t e = with_qk(a, [&](auto p2, auto norm, auto rope) {
-      qk_bwd_kernel<p2(), norm(), rope()><<<blocks, 256, 0, s>>>(a, x, dy, dx, part);
+    const hipError_t e = with_qk<kQkBwdE>(a, [&](auto p2, auto norm, auto rope, auto once) {
+      qk_bwd_kernel<kQkBwdE, p2(), norm(), rope(), once()><<<blocks, 256, 0, s>>>(a, x, dy, dx, part);
       return hipGetLastError();
     });
     if (e != hipSuccess) return e;
   }
   if (!a.gq) return hipSuccess;
-  qk_gain_kernel<<<2 * a.hd / 16, 256, 0, s>>>(part, blocks, a.hd, dgq, dgk);
+  qk_gain_kernel<<<2 * a.hd / 16, 1024, 0, s>>>(part, blocks, a.hd, dgq, dgk);
   return hipGetLastError();
 }
 

@@ -111,6 +111,7 @@ SHAPES = [
     (1024, 16, 2, 128, 3, True, False),   # one wavefront per row from here on
     (5003, 8, 8, 256, 3, True, False),
     (9001, 4, 1, 32, 2, False, True),
+    (60001, 20, 12, 80, 3, True, True),   # results beyond the last-level cache
 ]
 
 
