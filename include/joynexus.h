@@ -482,12 +482,13 @@ typedef struct jn_token_head {
  * For row j of sample i of a packed batch the row is cu_seqlens[i] + j. */
 typedef struct jn_token_io {
   int32_t n;               /* entries, 0 .. 2^20                                  */
-  int32_t reserved;
+  int32_t dw_f32;          /* 0: dW is bf16; 1: fp32, as jn_tenant_adamw_step reads it
+                              (all tenants of a call alike)                       */
   const int32_t* rows;     /* device int32 [n]                                    */
   const int32_t* targets;  /* device int32 [n]                                    */
   float* logp;             /* out: device fp32 [n], log softmax(z)[target]        */
   float* loss;             /* out: device fp32 [1], mean of -logp over the targets, 0 without any */
-  void* dW;                /* out: device bf16 [vocab][d], dloss / dW             */
+  void* dW;                /* out: device bf16 or fp32 [vocab][d], dloss / dW     */
   void* dh;                /* out: device bf16 [n][d], dloss / d(the entry's row), or NULL */
 } jn_token_io;
 
@@ -498,8 +499,8 @@ typedef struct jn_token_io {
  * workspace does not grow with vocabulary times targets.
  * Nothing is averaged across tenants.  hidden: device bf16 [T][d], d a multiple of 64
  * in [64, 8192].  Precision: bf16 operands, fp32 accumulation, softmax statistics
- * and loss; the logits' gradient is rounded to bf16 before it meets h and W, the
- * results once.  Kernels only: the call may be captured into a HIP graph, whose
+ * and loss; the logits' gradient is rounded to bf16 before it meets h and W (as the
+ * action experts' are), bf16 results once.  Kernels only: the call may be captured into a HIP graph, whose
  * replays read rows, targets, hidden and W as they are then.  Results are
  * bitwise reproducible.  Errors enqueue nothing. */
 #define JN_TOKEN_PIECE_BYTES (1u << 30)

@@ -552,8 +552,8 @@ class TokenHead:
 
 
 class TokenIO:
-    """A tenant's targets (device int32 ``rows`` and ``targets`` [n]) and outputs: fp32 logp [n] and loss [1], bf16 dW
-    [vocab, d] and, optionally, dh [n, d]."""
+    """A tenant's targets (device int32 ``rows`` and ``targets`` [n]) and outputs: fp32 logp [n] and loss [1], bf16 or
+    fp32 dW [vocab, d] and, optionally, bf16 dh [n, d]."""
 
     STRUCT = jn_token_io
 
@@ -567,7 +567,8 @@ class TokenIO:
         s.targets = _entries("targets", targets, t.int32, n)
         s.logp = _entries("logp", logp, t.float32, n)
         s.loss = _entries("loss", loss, t.float32, 1)
-        s.dW = _entries("dW", dW, t.bfloat16, dW.numel())
+        s.dw_f32 = 1 if dW.dtype is t.float32 else 0
+        s.dW = _entries("dW", dW, t.float32 if s.dw_f32 else t.bfloat16, dW.numel())
         s.dh = _entries("dh", dh, t.bfloat16, n * int(dW.shape[1])) if dh is not None else None
         self.struct = s
 

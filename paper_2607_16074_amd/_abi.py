@@ -111,7 +111,7 @@ class jn_token_head(C.Structure):
 
 
 class jn_token_io(C.Structure):
-    _fields_ = [("n", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_void_p), ("targets", C.c_void_p),
+    _fields_ = [("n", C.c_int32), ("dw_f32", C.c_int32), ("rows", C.c_void_p), ("targets", C.c_void_p),
                 ("logp", C.c_void_p), ("loss", C.c_void_p), ("dW", C.c_void_p), ("dh", C.c_void_p)]
 
 

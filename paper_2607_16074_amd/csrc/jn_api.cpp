@@ -929,6 +929,7 @@ struct TokEntry {
   float *logp, *loss;
   int32_t* token;
   void *dW, *dh;
+  int32_t f32;  // dW
 };
 
 jn_status check_tokens(jn_ctx* c, int32_t d, const jn_token_head* heads, const std::vector<TokEntry>& io, bool train) {
@@ -938,6 +939,8 @@ jn_status check_tokens(jn_ctx* c, int32_t d, const jn_token_head* heads, const s
     const TokEntry& e = io[g];
     if (heads[g].vocab < 1 || heads[g].vocab > (1 << 24))
       return fail(c, JN_ESHAPE, "tenant %zu: vocabulary of %d", g, heads[g].vocab);
+    if ((e.f32 != 0 && e.f32 != 1) || e.f32 != io[0].f32)
+      return fail(c, JN_EINVAL, "tenant %zu: dw_f32 must be 0 or 1, the same for every tenant", g);
     if (e.n < 0 || e.n > (1 << 20)) return fail(c, JN_ESHAPE, "tenant %zu: %d entries", g, e.n);
     N += e.n;
     if (2 * ((int64_t)e.n + 64) * d > 0x7fffffff)
@@ -981,7 +984,7 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
     dh = dh || (io[g].dh != nullptr && io[g].n > 0);
     if (train && io[g].n == 0) {
       desc[g].zero = (uint16_t*)io[g].dW;
-      desc[g].zero_n8 = (int64_t)heads[g].vocab * d / 8;
+      desc[g].zero_n8 = (int64_t)heads[g].vocab * d / (io[g].f32 ? 4 : 8);
       P->zero8 += desc[g].zero_n8;
     }
   }
@@ -1160,7 +1163,7 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
       GemmArgs w{};  // dW piece = grad^T rows
       w.X = grad;
       w.W = rows;
-      w.C = (uint16_t*)io[g].dW + v0 * d;
+      w.C = (char*)io[g].dW + (io[g].f32 ? 4 : 2) * v0 * d;
       w.aux = inv;
       w.ldx = up(cols, 64);
       w.ldw = w.ldc = d;
@@ -1186,7 +1189,7 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
     }
     TokPiece p;
     jn_status st = add(&p.grad, EPI_DLOGIT, 0, dz);
-    if (st == JN_OK) st = add(&p.weights, EPI_SCALED_BF16, GEMM_TRANS_X | GEMM_TRANS_W, dw);
+    if (st == JN_OK) st = add(&p.weights, io[0].f32 ? EPI_SCALED_F32 : EPI_SCALED_BF16, GEMM_TRANS_X | GEMM_TRANS_W, dw);
     if (st == JN_OK) st = add(&p.rows, !P->planes ? EPI_SCALED_BF16 : k == 0 ? EPI_F32 : EPI_RESID_F32, GEMM_TRANS_W, dx);
     if (st != JN_OK) return st;
     P->pieces.push_back(p);
@@ -1205,7 +1208,7 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
 struct SmallPlan {
   std::vector<TokSmallSet> sets;
   std::vector<int32_t> wgs, gwgs;  // of every set
-  int32_t ldz = 16, N = 0;
+  int32_t ldz = 16, N = 0, f32 = 0;
   size_t table = 0, inv = 0, acc = 0, total = 0;
   std::vector<char> bytes;         // descriptors and problems of the row gradients
   TokSet rows;
@@ -1223,6 +1226,7 @@ jn_status small_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
   int32_t most = 1;
   for (const TokEntry& e : io) most = std::max(most, e.n);
   P->ldz = most > 32 ? 64 : most > 16 ? 32 : 16;
+  P->f32 = io[0].f32;
   P->inv = take(4 * (int64_t)G);
   std::vector<TokDesc> desc(G);
   std::vector<GemmArgs> dx;
@@ -1254,7 +1258,7 @@ jn_status small_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
       t.logp = e.logp;
       t.loss = e.loss;
       t.token = e.token;
-      t.dW = (uint16_t*)e.dW;
+      t.dW = e.dW;
       t.n = e.n;
       t.vocab = (int32_t)V;
       t.inv = (float*)(ws + P->inv) + g0 + k;
@@ -1386,8 +1390,8 @@ jn_status run_big(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const Tok
     if (p.grad.n > 0) JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, product(p.grad), "token gradients");
     if (p.rows.n > 0 && p.rows.epi != EPI_RESID_F32 && gemm_tokens_pair_ok(p.rows.tiles, p.weights.tiles)) {
       JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d,
-                launch_gemm_tokens_pair(s, p.rows.epi, probs + p.rows.at, p.rows.n, p.rows.tiles, probs + p.weights.at,
-                                        p.weights.n, p.weights.tiles),
+                launch_gemm_tokens_pair(s, p.rows.epi, probs + p.rows.at, p.rows.n, p.rows.tiles, p.weights.epi,
+                                        probs + p.weights.at, p.weights.n, p.weights.tiles),
                 "token gradients");
       continue;
     }
@@ -1409,7 +1413,7 @@ jn_status run_small(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const S
     if (P.wgs[k] > 0)
       JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, launch_small_scores(s, set, P.wgs[k], P.ldz, hidden, T, d), "token scores");
     if (train)
-      JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, launch_small_grads(s, set, P.gwgs[k], P.ldz, hidden, T, d),
+      JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, launch_small_grads(s, set, P.gwgs[k], P.ldz, hidden, T, d, P.f32 != 0),
                 "token gradients");
     else
       JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, V, 0, launch_small_pick(s, set, P.ldz, T), "token pick");
@@ -1448,14 +1452,15 @@ jn_status tokens_run(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const 
 std::vector<TokEntry> entries(const jn_token_io* io, int32_t G) {
   std::vector<TokEntry> v(G);
   for (int32_t g = 0; g < G; ++g)
-    v[g] = TokEntry{io[g].n, io[g].rows, io[g].targets, io[g].logp, io[g].loss, nullptr, io[g].dW, io[g].dh};
+    v[g] = TokEntry{io[g].n, io[g].rows, io[g].targets, io[g].logp, io[g].loss, nullptr, io[g].dW, io[g].dh,
+                    io[g].dw_f32};
   return v;
 }
 
 std::vector<TokEntry> entries(const jn_token_pick* io, int32_t G) {
   std::vector<TokEntry> v(G);
   for (int32_t g = 0; g < G; ++g)
-    v[g] = TokEntry{io[g].n, io[g].rows, nullptr, io[g].logp, nullptr, io[g].token, nullptr, nullptr};
+    v[g] = TokEntry{io[g].n, io[g].rows, nullptr, io[g].logp, nullptr, io[g].token, nullptr, nullptr, 0};
   return v;
 }
 

@@ -109,6 +109,7 @@ enum GemmEpi : int32_t {
   EPI_GREEDY = 8,        // the same with the columns' indices in `aux` (int32 [column block][M]), no labels
   EPI_DLOGIT = 9,        // C bf16 = softmax gradient from the rows' TokRow (aux), zero in columns N .. ldc - 1
   EPI_SCALED_BF16 = 10,  // C bf16 = acc * aux[0]
+  EPI_SCALED_F32 = 12,   // C fp32 = acc * aux[0]
   EPI_SOFTMAX_KEEP = 11  // EPI_SOFTMAX with the parts at `part`; C bf16 = exp(acc - m) of the block's part
 };
 
@@ -177,7 +178,8 @@ struct TokRow {
 // Grouped launches of a token head's products, as above but with any N for
 // EPI_SOFTMAX, EPI_GREEDY and EPI_DLOGIT (trans 0), and any K with GEMM_TRANS_W
 // where the columns K .. of X up to a multiple of 64 are zeros (EPI_SCALED_BF16,
-// EPI_F32, EPI_RESID_F32) or with both operands transposed (EPI_SCALED_BF16).  prepare: tile
+// EPI_F32, EPI_RESID_F32) or with both operands transposed (EPI_SCALED_BF16,
+// EPI_SCALED_F32, EPI_F32).  prepare: tile
 // ranges and shape, or a total of -1.  Column blocks of EPI_SOFTMAX and EPI_GREEDY are
 // gemm_tokens_block(shape) columns, tok_blocks of them per problem.
 struct TokTiles {
@@ -190,11 +192,12 @@ int32_t gemm_tokens_block(int shape);
 inline int32_t tok_blocks(int32_t vocab, int32_t block) { return (vocab + 2 * block - 1) / (2 * block) * 2; }
 hipError_t launch_gemm_tokens(hipStream_t s, int epi, int trans, const GemmArgs* dprobs, int32_t nprob,
                               const TokTiles& t);
-// Row gradients (epi EPI_F32 or EPI_SCALED_BF16, GEMM_TRANS_W) and weight gradients
-// (EPI_SCALED_BF16, both transposed) in one launch, where the shapes allow it.
+// Row gradients (depi EPI_F32 or EPI_SCALED_BF16, GEMM_TRANS_W) and weight gradients
+// (wepi EPI_SCALED_BF16 or EPI_SCALED_F32, both transposed) in one launch, where
+// the shapes allow it.
 bool gemm_tokens_pair_ok(const TokTiles& rows, const TokTiles& weights);
-hipError_t launch_gemm_tokens_pair(hipStream_t s, int epi, const GemmArgs* dprobs, int32_t nd, const TokTiles& d,
-                                   const GemmArgs* wprobs, int32_t nw, const TokTiles& w);
+hipError_t launch_gemm_tokens_pair(hipStream_t s, int depi, const GemmArgs* dprobs, int32_t nd, const TokTiles& d,
+                                   int wepi, const GemmArgs* wprobs, int32_t nw, const TokTiles& w);
 
 // C[M][N] (+)= epi(A[M][K] * B[N][K]^T); A, B bf16 row-major with leading
 // dims lda, ldb (elements); for EPI_GEGLU_BF16, B is w_gate and B2 is w_up,
@@ -305,7 +308,7 @@ struct TokDesc {
   const int32_t* index;    // [blocks][n], decoding
   uint16_t* keep;          // [n][8 kept_n8]
   uint16_t* zero;          // dW of a tenant without entries, else null
-  int64_t zero_n8;
+  int64_t zero_n8;         // its 16-byte groups
   int32_t n, first, vocab, blocks;
   int32_t kept, width, kept_n8;
   int32_t grad_block;      // first workgroup of launch_tok_grad, ceil(kept_n8 / 256) to an entry
@@ -340,7 +343,7 @@ struct TokSmall {
   float* logp;
   float* loss;
   int32_t* token;
-  uint16_t* dW;
+  void* dW;                // bf16 or fp32
   TokPart* part;           // [wgs][n]
   int32_t* index;          // [wgs][n], decoding
   float* z;
@@ -367,7 +370,7 @@ int32_t small_grad_rows(int32_t d);
 hipError_t launch_small_scores(hipStream_t s, const TokSmallSet& set, int32_t wgs, int32_t ldz, const void* hidden,
                                int32_t T, int32_t d);
 hipError_t launch_small_grads(hipStream_t s, const TokSmallSet& set, int32_t wgs, int32_t ldz, const void* hidden,
-                              int32_t T, int32_t d);
+                              int32_t T, int32_t d, bool f32);
 hipError_t launch_small_pick(hipStream_t s, const TokSmallSet& set, int32_t ldz, int32_t T);
 // dh = (acc[0] + acc[1] + ...) inv[g], planes of [N][width].
 hipError_t launch_tok_rows(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const float* inv, const float* acc,

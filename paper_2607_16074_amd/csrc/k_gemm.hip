@@ -322,8 +322,8 @@ __device__ __forceinline__ void epilogue_f32(const GemmArgs& g, const f32x4 (&ac
     for (int it = 0; it < NI; ++it) {
       if (!WHOLE && !(m + 16 * j + RI * it < g.M && n < g.N)) continue;
       const int64_t at = base + 16 * j * g.ldc + it * step;
-      const f32x4 a = v[it];
-      if constexpr (EPI == EPI_F32 || EPI == EPI_RESID_F32) {
+      const f32x4 a = EPI == EPI_SCALED_F32 ? v[it] * g.aux[0] : v[it];
+      if constexpr (EPI == EPI_F32 || EPI == EPI_RESID_F32 || EPI == EPI_SCALED_F32) {
         f32x4* const p = reinterpret_cast<f32x4*>(reinterpret_cast<float*>(g.C) + at);
         if constexpr (ONCE)
           __builtin_nontemporal_store(a, p);
@@ -1662,7 +1662,7 @@ TokTiles gemm_tokens_prepare(int epi, int trans, GemmArgs* probs, int32_t nprob)
       work += n * ((probs[p].K + kBK - 1) / kBK);
     }
     if (tiles <= 0 || tiles > (int64_t)kMostBlocks) continue;
-    const int like = epi_exp(epi) ? EPI_GELU_BF16 : epi;
+    const int like = epi_exp(epi) ? EPI_GELU_BF16 : epi == EPI_SCALED_F32 ? EPI_F32 : epi;
     double us = tiles_time(like, tiles, (double)work / tiles, t);
     if (out.uneven)
       us = std::max(us, longest * std::max(kShapes[t].slab, kShapes[t].slab1) + tiles_time(like, tiles, 0.0, t));
@@ -1693,7 +1693,7 @@ TokTiles gemm_tokens_prepare(int epi, int trans, GemmArgs* probs, int32_t nprob)
 
 // Row gradients (128x96 tiles, GEMM_TRANS_W) and weight gradients (128x128, both
 // operands transposed) of a call in one launch, as gemm_grad_pair_kernel.
-template <int EPI>
+template <int EPI, int WEPI>
 __global__ __launch_bounds__(256, 1) void gemm_tokens_pair_kernel(const GemmArgs* __restrict__ dprobs, int32_t nd,
                                                                   int32_t td, int32_t gd,
                                                                   const GemmArgs* __restrict__ wprobs, int32_t nw,
@@ -1715,7 +1715,7 @@ __global__ __launch_bounds__(256, 1) void gemm_tokens_pair_kernel(const GemmArgs
   if (data)
     flex_tile<BN, BM, NS, NS, EPI, GEMM_TRANS_W>(g, tm, tn, 0, KT, lds);
   else
-    flex_tile<128, 128, 3, 2, EPI_SCALED_BF16, GEMM_TRANS_X | GEMM_TRANS_W>(g, tm, tn, 0, KT, lds);
+    flex_tile<128, 128, 3, 2, WEPI, GEMM_TRANS_X | GEMM_TRANS_W>(g, tm, tn, 0, KT, lds);
 }
 
 // Ring tiles with an XCD's workgroups on consecutive tiles, 32 at a time: with few
@@ -1787,16 +1787,23 @@ bool gemm_tokens_pair_ok(const TokTiles& rows, const TokTiles& weights) {
   return rows.total > 0 && rows.shape == 4 && weights.shape == k128Shape && weights.total <= 1024;
 }
 
-hipError_t launch_gemm_tokens_pair(hipStream_t s, int epi, const GemmArgs* dprobs, int32_t nd, const TokTiles& d,
-                                   const GemmArgs* wprobs, int32_t nw, const TokTiles& w) {
+hipError_t launch_gemm_tokens_pair(hipStream_t s, int depi, const GemmArgs* dprobs, int32_t nd, const TokTiles& d,
+                                   int wepi, const GemmArgs* wprobs, int32_t nw, const TokTiles& w) {
   if (nd <= 0 || nw <= 0 || !gemm_tokens_pair_ok(d, w)) return hipErrorInvalidValue;
   const int32_t gd = (d.total + 7) / 8 * 8, gw = (w.total + 7) / 8 * 8;
-  if (epi == EPI_F32)
-    gemm_tokens_pair_kernel<EPI_F32><<<gd + gw, 256, 0, s>>>(dprobs, nd, d.total, gd, wprobs, nw, w.total, w.uneven);
-  else if (epi == EPI_SCALED_BF16)
-    gemm_tokens_pair_kernel<EPI_SCALED_BF16><<<gd + gw, 256, 0, s>>>(dprobs, nd, d.total, gd, wprobs, nw, w.total, w.uneven);
+#define JN_PAIR(D, W) \
+  gemm_tokens_pair_kernel<D, W><<<gd + gw, 256, 0, s>>>(dprobs, nd, d.total, gd, wprobs, nw, w.total, w.uneven)
+  if (depi == EPI_F32 && wepi == EPI_SCALED_BF16)
+    JN_PAIR(EPI_F32, EPI_SCALED_BF16);
+  else if (depi == EPI_SCALED_BF16 && wepi == EPI_SCALED_BF16)
+    JN_PAIR(EPI_SCALED_BF16, EPI_SCALED_BF16);
+  else if (depi == EPI_F32 && wepi == EPI_SCALED_F32)
+    JN_PAIR(EPI_F32, EPI_SCALED_F32);
+  else if (depi == EPI_SCALED_BF16 && wepi == EPI_SCALED_F32)
+    JN_PAIR(EPI_SCALED_BF16, EPI_SCALED_F32);
   else
     return hipErrorInvalidValue;
+#undef JN_PAIR
   return hipGetLastError();
 }
 
@@ -1813,6 +1820,8 @@ hipError_t launch_gemm_tokens(hipStream_t s, int epi, int trans, const GemmArgs*
     case EPI_RESID_F32 * 4 + GEMM_TRANS_W: return launch_tokens<EPI_RESID_F32, GEMM_TRANS_W>(s, dprobs, nprob, t);
     case EPI_F32 * 4 + (GEMM_TRANS_X | GEMM_TRANS_W):
       return launch_tokens<EPI_F32, GEMM_TRANS_X | GEMM_TRANS_W>(s, dprobs, nprob, t);
+    case EPI_SCALED_F32 * 4 + (GEMM_TRANS_X | GEMM_TRANS_W):
+      return launch_tokens<EPI_SCALED_F32, GEMM_TRANS_X | GEMM_TRANS_W>(s, dprobs, nprob, t);
     case EPI_SCALED_BF16 * 4 + (GEMM_TRANS_X | GEMM_TRANS_W):
       return launch_tokens<EPI_SCALED_BF16, GEMM_TRANS_X | GEMM_TRANS_W>(s, dprobs, nprob, t);
     default: return hipErrorInvalidValue;

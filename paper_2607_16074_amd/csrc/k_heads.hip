@@ -1065,7 +1065,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_pick_kernel(TokSmallArgs<
 // a lane for one of its 4 rows are 8 adjacent columns: one 16-byte store.  dz is
 // formed from z and the rows' joined sums by every wavefront for itself, rounded to
 // bf16 unscaled (TokRow).  blockIdx.y: 2,048 columns each.
-template <int GP, int NS, int C>
+template <int GP, int NS, int C, bool F32>
 __global__ __launch_bounds__(kSmallThreads, 2) void small_grads_kernel(TokSmallArgs<C> set, int32_t ldz,
                                                                        const uint16_t* __restrict__ hidden, int32_t T,
                                                                        int32_t width) {
@@ -1190,12 +1190,20 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_grads_kernel(TokSmallA
       }
       const int32_t k = 128 * (g0 + wc + 8 * p) + 32 * quad;
       if (v < V && wc + 8 * p < groups) {
-        uint4* const to = reinterpret_cast<uint4*>(d.dW + (int64_t)v * width + k);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (k + 8 * e < width)
-            to[e] = make_uint4(pack_bf2(a[0][e] * inv, a[1][e] * inv), pack_bf2(a[2][e] * inv, a[3][e] * inv),
-                               pack_bf2(a[4][e] * inv, a[5][e] * inv), pack_bf2(a[6][e] * inv, a[7][e] * inv));
+        for (int e = 0; e < 4; ++e) {
+          if (k + 8 * e >= width) continue;
+          const int64_t at = (int64_t)v * width + k + 8 * e;
+          if constexpr (F32) {
+            float4* const to = reinterpret_cast<float4*>(static_cast<float*>(d.dW) + at);
+            to[0] = make_float4(a[0][e] * inv, a[1][e] * inv, a[2][e] * inv, a[3][e] * inv);
+            to[1] = make_float4(a[4][e] * inv, a[5][e] * inv, a[6][e] * inv, a[7][e] * inv);
+          } else {
+            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(d.dW) + at) =
+                make_uint4(pack_bf2(a[0][e] * inv, a[1][e] * inv), pack_bf2(a[2][e] * inv, a[3][e] * inv),
+                           pack_bf2(a[4][e] * inv, a[5][e] * inv), pack_bf2(a[6][e] * inv, a[7][e] * inv));
+          }
+        }
       }
     }
   }
@@ -1251,13 +1259,16 @@ hipError_t launch_small_scores(hipStream_t s, const TokSmallSet& all, int32_t wg
 }
 
 hipError_t launch_small_grads(hipStream_t s, const TokSmallSet& all, int32_t wgs, int32_t ldz, const void* hidden,
-                              int32_t T, int32_t d) {
+                              int32_t T, int32_t d, bool f32) {
   const uint16_t* const h = static_cast<const uint16_t*>(hidden);
   const dim3 grid(wgs, (d + 2047) / 2048);
   return with_tenants(all, [&](const auto& set) {
     constexpr int C = sizeof(set.t) / sizeof(set.t[0]);
     auto go = [&](auto gp, auto ns) {
-      small_grads_kernel<gp(), ns(), C><<<grid, kSmallThreads, 0, s>>>(set, ldz, h, T, d);
+      if (f32)
+        small_grads_kernel<gp(), ns(), C, true><<<grid, kSmallThreads, 0, s>>>(set, ldz, h, T, d);
+      else
+        small_grads_kernel<gp(), ns(), C, false><<<grid, kSmallThreads, 0, s>>>(set, ldz, h, T, d);
       return hipGetLastError();
     };
     auto steps = [&](auto gp) {

@@ -23,12 +23,12 @@ def draw(n, v, d, T, seed, scale=1.0):
 
 
 class Tenant:
-    def __init__(self, lib, W, rows, targets, dh):
+    def __init__(self, lib, W, rows, targets, dh, f32=False):
         n, (v, d) = rows.numel(), W.shape
         self.W, self.rows, self.targets = W, rows, targets
         self.logp = torch.full((n + 4,), 9.0, device="cuda")
         self.loss = torch.full((2,), 9.0, device="cuda")
-        self.dW = torch.full((v * d + 16,), 9.0, dtype=torch.bfloat16, device="cuda")
+        self.dW = torch.full((v * d + 16,), 9.0, dtype=torch.float32 if f32 else torch.bfloat16, device="cuda")
         self.dh = torch.full((n * d + 16,), 9.0, dtype=torch.bfloat16, device="cuda") if dh else None
         self.head = lib.TokenHead(W)
         self.io = lib.TokenIO(rows, targets, self.logp[:n], self.loss[:1], self.dW[: v * d].view(v, d),
@@ -70,6 +70,7 @@ class Tenant:
             if margin and ref.numel() and count > 1:
                 margin(what, rel, 1e-2)
 
+        # (an fp32 dW misses the last rounding only: the same bar holds)
         within(self.dW[: v * d].view(v, d), dz.T @ h, terms.T @ h.abs(), "dW")
         if self.dh is not None:
             within(self.dh[: n * d].view(n, d), dz @ w, terms @ w.abs(), "dh")
@@ -97,6 +98,9 @@ CASES = [
     (1, 1, 64), (1, 2, 64), (1, 7, 128), (2, 64, 64), (5, 63, 128), (7, 256, 768), (1, 1024, 768), (33, 65, 192),
     (95, 127, 64), (96, 128, 64), (97, 129, 64), (130, 1000, 320), (255, 2049, 128), (700, 513, 2048), (64, 5001, 2048),
     (513, 8193, 256), (2048, 4096, 512), (2300, 9001, 192), (20, 40001, 64),
+    # few rows at every width the streaming kernels split differently, and one row more than they take
+    (16, 700, 576), (17, 700, 1024), (32, 333, 1088), (64, 999, 2048), (65, 999, 2048), (33, 500, 2176), (32, 500, 4096),
+    (16, 300, 4160), (16, 300, 8192), (17, 300, 8192),
 ]
 
 
@@ -119,6 +123,27 @@ def test_pieces_of_the_vocabulary(lib, margin):
     step(lib, lib.Context(), hidden, [b, a, c])
     for t in (a, b, c):
         t.check(hidden, margin)
+
+
+@pytest.mark.parametrize("case", [(1, 300, 64), (7, 256, 768), (50, 777, 2176), (300, 1003, 320), (2048, 4096, 512)],
+                         ids=lambda c: "-".join(map(str, c)))
+def test_fp32_weight_gradients(lib, case):
+    """The same products without the last rounding: rounded, they are the bf16 result bit for bit."""
+    n, v, d = case
+    hidden = feature(max(3, 2 * n), d)
+    args = draw(n, v, d, hidden.shape[0], 15)
+    for dh in (False, True):
+        a, b = Tenant(lib, *args, dh), Tenant(lib, *args, dh, f32=True)
+        empty = [Tenant(lib, *draw(0, 77, d, 4, 16), False, f32=x) for x in (False, True)]
+        ctx = lib.Context()
+        step(lib, ctx, hidden, [a, empty[0]])
+        step(lib, ctx, hidden, [b, empty[1]])
+        b.check(hidden)
+        assert torch.equal(b.dW[: v * d].to(torch.bfloat16), a.dW[: v * d]) and torch.equal(a.logp, b.logp)
+        for e in empty:
+            e.check(hidden)
+    with pytest.raises(lib.JNError):
+        lib.jn_tokens_workspace_size([a.head, b.head], [a.io, b.io])
 
 
 def test_tenants_of_unequal_sizes(lib):
