@@ -501,8 +501,10 @@ typedef struct jn_token_io {
  * in [64, 8192].  Precision: bf16 operands, fp32 accumulation, softmax statistics
  * and loss; the logits' gradient is rounded to bf16 before it meets h and W (as the
  * action experts' are), bf16 results once.  Kernels only: the call may be captured into a HIP graph, whose
- * replays read rows, targets, hidden and W as they are then.  Results are
- * bitwise reproducible.  Errors enqueue nothing. */
+ * replays read rows, targets, hidden and W as they are then.  A call's results are
+ * bitwise reproducible; a tenant's may differ in their last bits with the group it
+ * is called in, whose sizes choose the launches' shapes and the pieces.  Errors
+ * enqueue nothing. */
 #define JN_TOKEN_PIECE_BYTES (1u << 30)
 jn_status jn_tokens_workspace_size(int32_t d, const jn_token_head* heads, const jn_token_io* io, int32_t G,
                                    size_t* bytes);

@@ -284,8 +284,9 @@ class Backbone:
 
     def set_positions(self, pos):
         """Positions of the packed rows of the batches that follow: device int32 [T, axes] (None: the rows' own)."""
-        axes = max(1, self.struct.rope_axes)
-        self.struct.pos = _positions(pos, pos.shape[0] if pos is not None else 0, axes)
+        if pos is not None and pos.dim() != 2:
+            raise TypeError("positions must be [T, axes]")
+        self.struct.pos = _positions(pos, pos.shape[0] if pos is not None else 0, max(1, self.struct.rope_axes))
         self.pos = pos
 
 
@@ -295,7 +296,14 @@ def jn_backbone_workspace_size(bb: Backbone, T: int) -> int:
     return int(n.value)
 
 
+def _check_positions(bb: Backbone, T: int):
+    pos = getattr(bb, "pos", None)  # (anything with a `struct` may stand for a backbone)
+    if pos is not None and pos.shape[0] != T:
+        raise ValueError(f"the backbone's positions are of {pos.shape[0]} rows, the batch has {T}")
+
+
 def jn_backbone_forward(ctx: Context, bb: Backbone, packed: Packed, hidden, ws):
+    _check_positions(bb, packed.struct.T)
     _check(_lib.jn_backbone_forward(ctx.handle, C.byref(bb.struct), C.byref(packed.struct), _ptr(hidden),
                                     _ptr(ws), ws.numel() * ws.element_size()), ctx)
 
@@ -750,6 +758,9 @@ class InferPlan:
 
     def __init__(self, ctx: Context, reqs: Sequence[Request], tenants: Sequence[Tenant], d: int, align: int,
                  bb: Backbone, heads: Sequence[Head], actions: Sequence, ws):
+        pos = getattr(bb, "pos", None)
+        if pos is not None:
+            _check_positions(bb, jn_pack_plan(reqs, tenants, d, align).T)
         ra, keep = _requests(reqs)
         ha, _ = _head_arrays(heads)
         o = _opts(d, align)
@@ -760,7 +771,7 @@ class InferPlan:
                                          C.byref(h)), ctx)
         self.handle = h
         self.ctx = ctx
-        self._keep = (reqs, bb, heads, actions, ws)
+        self._keep = (reqs, bb, pos, heads, actions, ws)
 
     def packed(self):
         """(jn_packed struct, hidden device pointer) of the plan's batch."""

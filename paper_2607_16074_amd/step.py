@@ -7,12 +7,15 @@ tenant's head, allocates the buffers a given group of requests needs once
     jn_pack_group -> jn_backbone_forward -> jn_tenant_heads_fwd_bwd -> jn_unpack
 
 (``jn_tenant_experts_fwd_bwd`` in place of the heads call when the group's
-tenants carry action experts)
+tenants carry action experts, ``jn_tenant_tokens_fwd_bwd`` when they predict
+tokens)
 
 on one stream (``run``) with no allocation and no host synchronisation.
 ``InferStep`` is the inference-side counterpart: one physical batch made
 resident by ``jn_infer_plan_create`` (pack, shared encode, split, forward-only
 decode), launched eagerly or replayed as a captured HIP graph.
+``DecodeStep`` is the token-predicting tenants' counterpart: the likeliest next
+token behind every sample's last row.
 ``isolated_runs`` builds one such step per tenant over the same device
 weights: the serial-execution comparator of grouped execution, using the
 same kernels and the same tile rule.
@@ -24,9 +27,11 @@ from typing import Dict, List, Optional, Sequence
 import numpy as np
 
 from . import (EXPERT_LAYER_FIELDS, AdamWTenant, Backbone, Context, Expert, ExpertIO, Head, HeadIO, InferPlan,
-               Request, Tenant, jn_adamw_workspace_size, jn_infer_workspace_size, jn_backbone_forward, jn_backbone_workspace_size, jn_experts_workspace_size,
-               jn_heads_workspace_size, jn_pack_group, jn_pack_plan, jn_pack_tenant_sizes, jn_tenant_adamw_step,
-               jn_tenant_experts_fwd_bwd, jn_tenant_heads_fwd_bwd, jn_unpack)
+               Request, Tenant, TokenHead, TokenIO, TokenPick, jn_adamw_workspace_size, jn_infer_workspace_size,
+               jn_backbone_forward, jn_backbone_workspace_size, jn_experts_workspace_size, jn_heads_workspace_size,
+               jn_pack_group, jn_pack_maps_host, jn_pack_plan, jn_pack_tenant_sizes, jn_tenant_adamw_step,
+               jn_tenant_experts_fwd_bwd, jn_tenant_heads_fwd_bwd, jn_tenant_tokens_decode, jn_tenant_tokens_fwd_bwd,
+               jn_tokens_decode_workspace_size, jn_tokens_workspace_size, jn_unpack)
 
 
 def _dev_bf16(bits: np.ndarray, device):
@@ -40,14 +45,43 @@ def _dev_f32(a: np.ndarray, device):
     return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(device)
 
 
+def _dev_i32(a: np.ndarray, device):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(device)
+
+
+def packed_positions(requests: Sequence[Request], maps: dict, positions: Sequence[np.ndarray]) -> np.ndarray:
+    """Positions of the packed rows, int32 [T, axes], from the requests' own ([n, max_len, axes] each); zeros in
+    alignment rows.  ``maps``: ``jn_pack_maps_host`` of the requests."""
+    axes = positions[0].shape[-1]
+    out = np.zeros((maps["T"], axes), np.int32)
+    for i in range(maps["N"]):
+        r, j, n, at = (int(maps[k][i]) for k in ("sample_request", "sample_local", "seqlens", "cu_seqlens"))
+        out[at: at + n] = positions[r][j, :n]
+    return out
+
+
+def target_rows(maps: dict, slot: int, sample: np.ndarray, row: np.ndarray) -> np.ndarray:
+    """Rows of the packed feature of (sample, row) pairs, samples in tenant ``slot``'s arrival order; -1 where the pair
+    names no valid row (no target)."""
+    first, end = int(maps["tenant_sample_off"][slot]), int(maps["tenant_sample_off"][slot + 1])
+    sample, row = np.asarray(sample, np.int64), np.asarray(row, np.int64)
+    ok = (sample >= 0) & (sample < end - first)
+    i = maps["tenant_perm"][first + np.where(ok, sample, 0)]
+    ok &= (row >= 0) & (row < maps["seqlens"][i])
+    return np.where(ok, maps["cu_seqlens"][i] + row, -1).astype(np.int32)
+
+
 class Model:
-    """Device weights: frozen backbone + per-tenant heads or action experts."""
+    """Device weights: frozen backbone + per-tenant heads, action experts or token heads."""
 
     def __init__(self, backbone: Backbone, heads: List[Optional[Head]], tenant_meta: List[dict], prefix_sig: int,
-                 experts: Optional[List[Optional[Expert]]] = None):
+                 experts: Optional[List[Optional[Expert]]] = None,
+                 token_heads: Optional[List[Optional[TokenHead]]] = None):
         self.backbone = backbone
         self.heads = heads
         self.experts = experts or [None] * len(heads)
+        self.token_heads = token_heads or [None] * len(heads)
         self.tenant_meta = tenant_meta  # action_dim, chunk per tenant
         self.prefix_sig = prefix_sig
 
@@ -55,13 +89,17 @@ class Model:
     def from_arrays(cls, layers: List[dict], gf: np.ndarray, n_heads: int, eps: float,
                     heads: List[Optional[list]], tenant_meta: List[dict], prefix_sig: int, device="cuda",
                     experts: Optional[List[Optional[dict]]] = None, n_kv_heads: int = 0, causal: bool = False,
-                    rope_theta: float = 0.0):
+                    rope_theta: float = 0.0, rope_sections: Sequence[int] = (), rope_interleaved: bool = False,
+                    token_heads: Optional[List[Optional[np.ndarray]]] = None):
         """``layers``: per layer dict of bf16 bit arrays; ``heads``: per tenant
         list of (W fp32 [out,in], b fp32 [out]) or None; ``experts``: per
         tenant None or a dict of bf16 bit arrays (w_in, w_out, gf, layers)
-        with ``tenant_meta[g]["expert_heads"]`` attention heads."""
+        with ``tenant_meta[g]["expert_heads"]`` attention heads;
+        ``token_heads``: per tenant None or bf16 bits [vocab, d]."""
         dl = [{k: _dev_bf16(v, device) for k, v in L.items()} for L in layers]
-        bb = Backbone(dl, _dev_bf16(gf, device), n_heads, eps, n_kv_heads, causal, rope_theta)
+        bb = Backbone(dl, _dev_bf16(gf, device), n_heads, eps, n_kv_heads, causal, rope_theta, rope_sections,
+                      rope_interleaved)
+        ts = [TokenHead(_dev_bf16(w, device)) if w is not None else None for w in token_heads or [None] * len(heads)]
         hs, xs = [], []
         for g, layers_g in enumerate(heads):
             if layers_g is None:
@@ -79,15 +117,20 @@ class Model:
                                  _dev_bf16(e["gf"], device), xl, tenant_meta[g]["expert_heads"],
                                  tenant_meta[g]["chunk"], bb.d, eps,
                                  _dev_bf16(e["w_time"], device) if "w_time" in e else None))
-        return cls(bb, hs, tenant_meta, prefix_sig, xs)
+        return cls(bb, hs, tenant_meta, prefix_sig, xs, ts)
 
 
 class GroupStep:
-    """One group of requests over a subset of tenants, buffers allocated once."""
+    """One group of requests over a subset of tenants, buffers allocated once.
+
+    Token-predicting tenants: ``targets[g]`` is a triple of int arrays (sample in the tenant's arrival order, its row,
+    the token that row predicts).  ``positions``: per request int [n, max_len, axes], for backbones whose rows have
+    several position axes."""
 
     def __init__(self, model: Model, requests: Sequence[Request], targets: Dict[int, np.ndarray],
                  tenants: Sequence[int], align: int = 1, ctx: Optional[Context] = None, device="cuda",
-                 noisy: Optional[Dict[int, np.ndarray]] = None, flow_t: Optional[Dict[int, np.ndarray]] = None):
+                 noisy: Optional[Dict[int, np.ndarray]] = None, flow_t: Optional[Dict[int, np.ndarray]] = None,
+                 positions: Optional[Sequence[np.ndarray]] = None):
         import torch
         self.model = model
         self.ctx = ctx or Context()
@@ -108,6 +151,12 @@ class GroupStep:
         self.use_experts = self.experts[0] is not None
         if any((x is not None) != self.use_experts for x in self.experts):
             raise ValueError("a group mixes expert tenants with MLP-head tenants")
+        self.token_heads = [model.token_heads[g] for g in self.tenants]
+        self.use_tokens = self.token_heads[0] is not None
+        if any((x is not None) != self.use_tokens for x in self.token_heads):
+            raise ValueError("a group mixes token-predicting tenants with others")
+        host = jn_pack_maps_host(self.requests, self.table, d, align) if self.use_tokens or positions is not None else None
+        self.pos = _dev_i32(packed_positions(self.requests, host, positions), device) if positions is not None else None
         self.heads = [model.heads[g] for g in self.tenants]
         self.pooled = torch.empty((self.N, d), dtype=torch.float32, device=device)
         self.out_hidden = [torch.empty((r.n, r.max_len, d), dtype=torch.bfloat16, device=device) for r in self.requests]
@@ -131,6 +180,14 @@ class GroupStep:
                                          f32(e.w_time) if e.w_time is not None else None))
             self.hd_ws = torch.empty(jn_experts_workspace_size(self.packed, self.experts, self.ios), dtype=torch.uint8,
                                      device=device)
+        elif self.use_tokens:
+            for k, g in enumerate(self.tenants):
+                sample, row, token = targets[g]
+                f32 = lambda *n: torch.empty(n, dtype=torch.float32, device=device)  # noqa: E731
+                self.ios.append(TokenIO(_dev_i32(target_rows(host, k, sample, row), device), _dev_i32(token, device),
+                                        f32(len(token)), f32(1), f32(*model.token_heads[g].shape)))
+            self.hd_ws = torch.empty(jn_tokens_workspace_size(self.token_heads, self.ios), dtype=torch.uint8,
+                                     device=device)
         else:
             for k, g in enumerate(self.tenants):
                 h = model.heads[g]
@@ -151,11 +208,14 @@ class GroupStep:
         self.packed = jn_pack_group(self.ctx, self.requests, self.table, d, self.align, self.maps, self.tokens)
 
     def backbone(self):
+        self.model.backbone.set_positions(self.pos)
         jn_backbone_forward(self.ctx, self.model.backbone, self.packed, self.hidden, self.bb_ws)
 
     def heads_fwd_bwd(self):
         if self.use_experts:
             jn_tenant_experts_fwd_bwd(self.ctx, self.packed, self.hidden, self.experts, self.ios, self.hd_ws)
+        elif self.use_tokens:
+            jn_tenant_tokens_fwd_bwd(self.ctx, self.hidden, self.token_heads, self.ios, self.hd_ws)
         else:
             jn_tenant_heads_fwd_bwd(self.ctx, self.packed, self.hidden, self.heads, self.ios, self.hd_ws,
                                     self.pooled)
@@ -213,12 +273,55 @@ class InferStep:
         self.stream.synchronize()
 
 
+class DecodeStep:
+    """The likeliest next token behind the last row of every sample of token-predicting tenants: pack, shared backbone,
+    ``jn_tenant_tokens_decode``.  ``tokens[k]`` (int32) and ``logp[k]`` are tenant ``tenants[k]``'s, in its arrival
+    order.  ``run`` may be called again with new observations and ``pos`` in the same buffers."""
+
+    def __init__(self, model: Model, requests: Sequence[Request], tenants: Sequence[int], align: int = 1,
+                 ctx: Optional[Context] = None, device="cuda", positions: Optional[Sequence[np.ndarray]] = None):
+        import torch
+        self.model = model
+        self.ctx = ctx or Context()
+        self.tenants = list(tenants)
+        slot = {g: k for k, g in enumerate(self.tenants)}
+        self.requests = [Request(slot[r.tenant], r.embeds, r.lengths, r.max_len) for r in requests]
+        self.align, d = align, model.backbone.d
+        self.table = [Tenant(model.prefix_sig, d) for _ in self.tenants]
+        self.heads = [model.token_heads[g] for g in self.tenants]
+        if any(h is None for h in self.heads):
+            raise ValueError("DecodeStep serves token-predicting tenants")
+        sz = jn_pack_plan(self.requests, self.table, d, align)
+        host = jn_pack_maps_host(self.requests, self.table, d, align)
+        self.pos = _dev_i32(packed_positions(self.requests, host, positions), device) if positions is not None else None
+        self.maps = torch.empty(int(sz.map_bytes), dtype=torch.uint8, device=device)
+        self.packed_tokens = torch.empty((sz.T, d), dtype=torch.bfloat16, device=device)
+        self.hidden = torch.empty((sz.T, d), dtype=torch.bfloat16, device=device)
+        self.bb_ws = torch.empty(jn_backbone_workspace_size(model.backbone, sz.T), dtype=torch.uint8, device=device)
+        self.picks = []
+        for k in range(len(self.tenants)):
+            i = host["tenant_perm"][host["tenant_sample_off"][k]: host["tenant_sample_off"][k + 1]]
+            rows = _dev_i32(host["cu_seqlens"][i] + host["seqlens"][i] - 1, device)
+            self.picks.append(TokenPick(rows, torch.empty(len(i), dtype=torch.int32, device=device),
+                                        torch.empty(len(i), dtype=torch.float32, device=device)))
+        self.tokens, self.logp = [p.token for p in self.picks], [p.logp for p in self.picks]
+        self.ws = torch.empty(jn_tokens_decode_workspace_size(self.heads, self.picks), dtype=torch.uint8, device=device)
+
+    def run(self):
+        d = self.model.backbone.d
+        packed = jn_pack_group(self.ctx, self.requests, self.table, d, self.align, self.maps, self.packed_tokens)
+        self.model.backbone.set_positions(self.pos)
+        jn_backbone_forward(self.ctx, self.model.backbone, packed, self.hidden, self.bb_ws)
+        jn_tenant_tokens_decode(self.ctx, self.hidden, self.heads, self.picks, self.ws)
+
+
 class TenantOptimizer:
     """Per-tenant AdamW over the tenants of one ``GroupStep``: after the
     group's tenant stage, ``step()`` updates every tenant's own parameters
     from its own gradients in one launch and advances only those tenants'
-    versions.  MLP heads are updated in place (fp32); an action expert keeps
-    fp32 master weights here and its bf16 weights receive the rounded update.
+    versions.  MLP heads are updated in place (fp32); an action expert or token
+    head keeps fp32 master weights here and its bf16 weights receive the rounded
+    update.
     Moments start at zero."""
 
     def __init__(self, group: "GroupStep", lr: float = 1e-4, betas=(0.9, 0.999), eps: float = 1e-8,
@@ -238,6 +341,9 @@ class TenantOptimizer:
                     pairs += [(L[n], Lg[n]) for n in EXPERT_LAYER_FIELDS]
                 masters = [w.float().contiguous() for w, _ in pairs]
                 self.sets.append((masters, [gr for _, gr in pairs], [w for w, _ in pairs]))
+            elif group.use_tokens:
+                W = group.token_heads[k].W
+                self.sets.append(([W.float().contiguous()], [group.ios[k].dW], [W]))
             else:
                 h, io = group.heads[k], group.ios[k]
                 self.sets.append((list(h.W) + list(h.b), list(io.dW) + list(io.db), None))
