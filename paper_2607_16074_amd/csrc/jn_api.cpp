@@ -915,6 +915,7 @@ struct TokPlan {
   int64_t zero8 = 0;
   size_t table = 0, h = 0, labels = 0, zlab = 0, inv = 0, rows = 0, part = 0, index = 0, piece = 0, acc = 0, total = 0;
   bool planes = false;  // row gradients are summed from fp32 planes
+  int32_t most_planes = 0;
   std::vector<char> bytes;
   TokSet scores, more;  // of the kept piece (all columns when decoding), and of the columns behind it
   std::vector<TokPiece> pieces;
@@ -1106,14 +1107,13 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
       std::vector<GemmArgs> v;
       for (int32_t g = 0; g < G; ++g) {
         if (io[g].n == 0 || !io[g].dh) continue;
-        const int64_t cols = desc[g].kept, step = range_columns(cols, t);
-        for (int64_t at = 0; at < cols; at += step) {
-          GemmArgs q{};
-          q.M = io[g].n;
-          q.N = d;
-          q.K = (int32_t)std::min(step, cols - at);
-          v.push_back(q);
-        }
+        GemmArgs q{};
+        q.M = io[g].n;
+        q.N = d;
+        q.K = desc[g].kept;
+        q.krange = (int32_t)range_columns(q.K, t);
+        q.ranges = (q.K + q.krange - 1) / q.krange;
+        v.push_back(q);
       }
       const bool sum = t > 1 || pieces > 1;
       const TokTiles f = gemm_tokens_prepare(sum ? EPI_F32 : EPI_BF16, GEMM_TRANS_W, v.data(), (int32_t)v.size());
@@ -1131,6 +1131,7 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
         most = std::max(most, desc[g].planes);
       }
     P->planes = pieces > 1 || most > 1;
+    P->most_planes = most;
     if (P->planes) {
       P->acc = take(4 * most * N * d);
       for (int32_t g = 0; g < G; ++g) desc[g].dh = (uint16_t*)io[g].dh;
@@ -1172,20 +1173,22 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
       w.K = n;
       dw.push_back(w);
       if (!io[g].dh) continue;
-      const int64_t step = P->planes ? range_columns(desc[g].kept, S) : cols;
-      for (int64_t at = 0, s = 0; at < cols; at += step, ++s) {
-        GemmArgs r{};  // dh (+)= grad W piece
-        r.X = grad + at;
-        r.W = W + at * d;
-        r.aux = P->planes ? nullptr : inv;  // (a residual add without aux is in place)
-        r.C = P->planes ? (void*)((float*)(ws + P->acc) + (s * N + desc[g].first) * d) : io[g].dh;
-        r.ldx = up(cols, 64);
-        r.ldw = r.ldc = d;
-        r.M = n;
-        r.N = d;
-        r.K = (int32_t)std::min(step, cols - at);
-        dx.push_back(r);
+      GemmArgs r{};  // dh (+)= grad W piece
+      r.X = grad;
+      r.W = W;
+      r.aux = P->planes ? nullptr : inv;  // (a residual add without aux is in place)
+      r.C = P->planes ? (void*)((float*)(ws + P->acc) + (int64_t)desc[g].first * d) : io[g].dh;
+      r.ldx = up(cols, 64);
+      r.ldw = r.ldc = d;
+      r.M = n;
+      r.N = d;
+      r.K = cols;
+      if (P->planes) {
+        r.krange = (int32_t)range_columns(desc[g].kept, S);
+        r.ranges = (cols + r.krange - 1) / r.krange;
+        r.split_c = N * d;
       }
+      dx.push_back(r);
     }
     TokPiece p;
     jn_status st = add(&p.grad, EPI_DLOGIT, 0, dz);
@@ -1207,8 +1210,8 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
 // Tenants of few rows: launches of up to kSmallTenants, workgroups by vocabulary.
 struct SmallPlan {
   std::vector<TokSmallSet> sets;
-  std::vector<int32_t> wgs, gwgs;  // of every set
-  int32_t ldz = 16, N = 0, f32 = 0;
+  std::vector<int32_t> wgs, gwgs, grad_rows;  // of every set
+  int32_t ldz = 16, N = 0, f32 = 0, planes = 0;
   size_t table = 0, inv = 0, acc = 0, total = 0;
   std::vector<char> bytes;         // descriptors and problems of the row gradients
   TokSet rows;
@@ -1238,7 +1241,7 @@ jn_status small_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
     N += io[g].n;
   }
   P->N = (int32_t)N;
-  const int64_t score_rows = small_score_rows(d), grad_rows = small_grad_rows(d);
+  const int64_t score_rows = small_score_rows(d);
   for (int32_t g0 = 0; g0 < G; g0 += kSmallTenants) {
     TokSmallSet set{};
     set.G = std::min(G - g0, kSmallTenants);
@@ -1247,6 +1250,7 @@ jn_status small_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
       all += heads[g0 + k].vocab;
       live += io[g0 + k].n > 0 ? heads[g0 + k].vocab : 0;
     }
+    const int32_t grad_rows = small_grad_rows(d, all);
     int32_t wgs = 0, gwgs = 0;
     for (int32_t k = 0; k < set.G; ++k) {
       const TokEntry& e = io[g0 + k];
@@ -1286,6 +1290,7 @@ jn_status small_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
     P->sets.push_back(set);
     P->wgs.push_back(wgs);
     P->gwgs.push_back(gwgs);
+    P->grad_rows.push_back(grad_rows);
   }
   // dh = grad^T W over ranges of the vocabulary, as many as fill the CUs
   int64_t tiles = 0, planes = 0;
@@ -1299,21 +1304,26 @@ jn_status small_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
       const int64_t step = std::min(range_columns(V, (int32_t)S), most_cols);
       desc[g].planes = (int32_t)((V + step - 1) / step);
       planes = std::max<int64_t>(planes, desc[g].planes);
-      for (int64_t at = 0; at < V; at += step) {
-        GemmArgs r{};
-        r.X = P->sets[g / kSmallTenants].t[g % kSmallTenants].grad + at * P->ldz;
-        r.W = (const uint16_t*)heads[g].W + at * d;
-        r.C = (void*)((at / step * N + desc[g].first) * d * 4);  // (of the planes, below)
-        r.ldx = P->ldz;
-        r.ldw = r.ldc = d;
-        r.M = io[g].n;
-        r.N = d;
-        r.K = (int32_t)std::min(step, V - at);
-        dx.push_back(r);
-      }
+      GemmArgs r{};
+      r.X = P->sets[g / kSmallTenants].t[g % kSmallTenants].grad;
+      r.W = (const uint16_t*)heads[g].W;
+      r.ldx = P->ldz;
+      r.ldw = r.ldc = d;
+      r.M = io[g].n;
+      r.N = d;
+      r.K = (int32_t)V;
+      r.krange = (int32_t)step;
+      r.ranges = desc[g].planes;
+      r.split_c = N * d;
+      r.aux = (float*)(intptr_t)desc[g].first;  // (until the planes have their place)
+      dx.push_back(r);
     }
     P->acc = take(4 * planes * N * d);
-    for (GemmArgs& r : dx) r.C = ws + P->acc + (size_t)r.C;
+    P->planes = (int32_t)planes;
+    for (GemmArgs& r : dx) {
+      r.C = (float*)(ws + P->acc) + (intptr_t)r.aux * d;
+      r.aux = nullptr;
+    }
     P->rows.epi = EPI_F32;
     P->rows.trans = GEMM_TRANS_X | GEMM_TRANS_W;
     P->rows.n = (int32_t)dx.size();
@@ -1340,13 +1350,15 @@ struct TokSplit {
 
 jn_status split_tokens(jn_ctx* c, int32_t d, const jn_token_head* heads, const std::vector<TokEntry>& io, bool train,
                        char* ws, TokSplit* P) {
+  // Few rows in every tenant: two launches that stream.  A tenant with more brings
+  // the others' along at little cost (126 and 63 rows of 865 x 1,024: 46 us by both
+  // paths, 25 by one).
   bool big = false;
   for (const TokEntry& e : io) big = big || e.n > tok_small_rows(d);
   for (size_t g = 0; g < io.size(); ++g) {
     if (io[g].n == 0 && !train) continue;
-    const bool few = io[g].n == 0 ? !big : io[g].n <= tok_small_rows(d);
-    (few ? P->small_heads : P->heads).push_back(heads[g]);
-    (few ? P->small_io : P->io).push_back(io[g]);
+    (big ? P->heads : P->small_heads).push_back(heads[g]);
+    (big ? P->io : P->small_io).push_back(io[g]);
   }
   if (!P->io.empty()) {
     const jn_status st = token_plan(c, d, P->heads.data(), P->io, train, ws, &P->big);
@@ -1399,7 +1411,7 @@ jn_status run_big(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const Tok
       if (t->n > 0) JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, product(*t), "token gradients");
   }
   if (P.planes)
-    JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 1, launch_tok_rows(s, desc, G, P.N, inv, (const float*)(w + P.acc), d),
+    JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 1, launch_tok_rows(s, desc, G, P.N, inv, (const float*)(w + P.acc), P.most_planes, d),
               "token row gradients");
   return JN_OK;
 }
@@ -1413,7 +1425,7 @@ jn_status run_small(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const S
     if (P.wgs[k] > 0)
       JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, launch_small_scores(s, set, P.wgs[k], P.ldz, hidden, T, d), "token scores");
     if (train)
-      JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, launch_small_grads(s, set, P.gwgs[k], P.ldz, hidden, T, d, P.f32 != 0),
+      JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, launch_small_grads(s, set, P.gwgs[k], P.ldz, hidden, T, d, P.grad_rows[k], P.f32 != 0),
                 "token gradients");
     else
       JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, V, 0, launch_small_pick(s, set, P.ldz, T), "token pick");
@@ -1425,7 +1437,7 @@ jn_status run_small(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const S
             launch_gemm_tokens(s, P.rows.epi, P.rows.trans, (const GemmArgs*)(desc + G), P.rows.n, P.rows.tiles),
             "token gradients");
   JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 1,
-            launch_tok_rows(s, desc, G, P.N, (const float*)(w + P.inv), (const float*)(w + P.acc), d),
+            launch_tok_rows(s, desc, G, P.N, (const float*)(w + P.inv), (const float*)(w + P.acc), P.planes, d),
             "token row gradients");
   return JN_OK;
 }

@@ -133,6 +133,8 @@ struct GemmArgs {
                         // consecutive K ranges; 0 when unsplit.  EPI_DLOGIT:
                         // the vocabulary's index of column 0
   void* part;           // EPI_SOFTMAX_KEEP: TokPart [column block][M]
+  int32_t krange, ranges;  // token heads: K in `ranges` ranges of krange each (0: unsplit),
+                           // partial results split_c elements apart
 };
 
 // Grouped launch over nprob problems sharing one epilogue: the host fills
@@ -175,7 +177,7 @@ struct TokRow {
   float own;
 };
 
-// Grouped launches of a token head's products, as above but with any N for
+// Grouped launches of a token head's products, as above but with K ranges, any N for
 // EPI_SOFTMAX, EPI_GREEDY and EPI_DLOGIT (trans 0), and any K with GEMM_TRANS_W
 // where the columns K .. of X up to a multiple of 64 are zeros (EPI_SCALED_BF16,
 // EPI_F32, EPI_RESID_F32) or with both operands transposed (EPI_SCALED_BF16,
@@ -364,17 +366,19 @@ struct TokSmallArgs {
 typedef TokSmallArgs<kSmallTenants> TokSmallSet;
 // Most rows of a tenant: their fragments stay in 128 registers of a lane.
 inline int32_t tok_small_rows(int32_t d) { return d <= 2048 ? 64 : d <= 4096 ? 32 : 16; }
-// Vocabulary rows of a workgroup's step, scores and gradients.
+// Vocabulary rows of a workgroup's step, scores and gradients (for `vocab` rows of all
+// tenants of a launch; at most kSmallGradRows).
+constexpr int32_t kSmallGradRows = 128;
 int32_t small_score_rows(int32_t d);
-int32_t small_grad_rows(int32_t d);
+int32_t small_grad_rows(int32_t d, int64_t vocab);
 hipError_t launch_small_scores(hipStream_t s, const TokSmallSet& set, int32_t wgs, int32_t ldz, const void* hidden,
                                int32_t T, int32_t d);
 hipError_t launch_small_grads(hipStream_t s, const TokSmallSet& set, int32_t wgs, int32_t ldz, const void* hidden,
-                              int32_t T, int32_t d, bool f32);
+                              int32_t T, int32_t d, int32_t rows, bool f32);
 hipError_t launch_small_pick(hipStream_t s, const TokSmallSet& set, int32_t ldz, int32_t T);
-// dh = (acc[0] + acc[1] + ...) inv[g], planes of [N][width].
+// dh = (sum of the planes of acc) inv[g], planes of [N][width]; planes: the most of a tenant.
 hipError_t launch_tok_rows(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const float* inv, const float* acc,
-                           int32_t width);
+                           int32_t planes, int32_t width);
 
 // ---- action expert (k_expert.hip) ----
 // dst[r][c] = cvt(src[r][c]) for r < src_rows, c < src_cols, else 0; r < rows, c < cols.

@@ -1644,11 +1644,20 @@ static bool tokens_shape_ok(int trans, int t) {
 TokTiles gemm_tokens_prepare(int epi, int trans, GemmArgs* probs, int32_t nprob) {
   TokTiles out;
   int64_t longest = 0;
+  bool cut = false;
+  auto slabs = [](const GemmArgs& g) { return ((g.ranges > 1 ? g.krange : g.K) + kBK - 1) / kBK; };
+  auto tiles_of = [](const GemmArgs& g, const TileShape& T) {
+    return (int64_t)((g.M + T.bm - 1) / T.bm) * ((g.N + T.bn - 1) / T.bn) * std::max(g.ranges, 1);
+  };
   for (int32_t p = 0; p < nprob; ++p) {
-    probs[p].trans = trans;
-    longest = std::max<int64_t>(longest, (probs[p].K + kBK - 1) / kBK);
+    GemmArgs& g = probs[p];
+    if (g.M <= 0 || g.N <= 0 || g.K <= 0 || (trans == 0 && g.K % kBK != 0) || (trans != 0 && g.N % 32 != 0)) return out;
+    if (g.ranges > 1 && (g.krange <= 0 || g.krange % kBK != 0 || (int64_t)g.krange * (g.ranges - 1) >= g.K)) return out;
+    g.trans = trans;
+    cut = cut || g.ranges > 1;
+    longest = std::max<int64_t>(longest, slabs(g));
   }
-  out.uneven = gemm_grouped_uneven(probs, nprob);
+  out.uneven = !cut && gemm_grouped_uneven(probs, nprob);
   if (out.uneven)
     std::stable_sort(probs, probs + nprob, [](const GemmArgs& a, const GemmArgs& b) { return a.K > b.K; });
   double best = 1e300;
@@ -1656,10 +1665,9 @@ TokTiles gemm_tokens_prepare(int epi, int trans, GemmArgs* probs, int32_t nprob)
     if (!tokens_shape_ok(trans, t)) continue;
     int64_t tiles = 0, work = 0;
     for (int32_t p = 0; p < nprob; ++p) {
-      const int64_t n = (int64_t)((probs[p].M + kShapes[t].bm - 1) / kShapes[t].bm) *
-                        ((probs[p].N + kShapes[t].bn - 1) / kShapes[t].bn);
+      const int64_t n = tiles_of(probs[p], kShapes[t]);
       tiles += n;
-      work += n * ((probs[p].K + kBK - 1) / kBK);
+      work += n * slabs(probs[p]);
     }
     if (tiles <= 0 || tiles > (int64_t)kMostBlocks) continue;
     const int like = epi_exp(epi) ? EPI_GELU_BF16 : epi == EPI_SCALED_F32 ? EPI_F32 : epi;
@@ -1678,17 +1686,51 @@ TokTiles gemm_tokens_prepare(int epi, int trans, GemmArgs* probs, int32_t nprob)
   int32_t at = 0;
   for (int32_t p = 0; p < nprob; ++p) {
     GemmArgs& g = probs[p];
-    if (g.M <= 0 || g.N <= 0 || g.K <= 0 || (trans == 0 && g.K % kBK != 0) || (trans != 0 && g.N % 32 != 0)) {
-      out.total = -1;
-      return out;
-    }
     g.tiles_m = (g.M + T.bm - 1) / T.bm;
     g.tiles_n = (g.N + T.bn - 1) / T.bn;
     g.tile_start = at;
-    at += g.tiles_m * g.tiles_n;
+    at += (int32_t)tiles_of(g, T);
     out.tiles_m = std::max(out.tiles_m, g.tiles_m);
   }
   return out;
+}
+
+// Problem and tile t of a grouped launch whose problems may be cut into K ranges: a
+// range is a whole set of tiles.  The search is by halves: 200 problems one after
+// the other are 40 us of dependent loads.
+template <int TR>
+__device__ __forceinline__ int32_t tokens_problem(const GemmArgs* __restrict__ probs, int32_t nprob, int32_t t,
+                                                  GemmArgs& g) {
+  int32_t lo = 0, hi = nprob - 1;
+  while (lo < hi) {
+    const int32_t mid = (lo + hi + 1) >> 1;
+    if (probs[mid].tile_start <= t) lo = mid; else hi = mid - 1;
+  }
+  g = probs[lo];
+  int32_t local = t - g.tile_start;
+  if (g.ranges > 1) {
+    const int32_t tiles = g.tiles_m * g.tiles_n, s = local / tiles;
+    const int64_t k0 = (int64_t)s * g.krange;
+    local -= s * tiles;
+    g.X += (TR & GEMM_TRANS_X) ? k0 * g.ldx : k0;
+    g.W += (TR & GEMM_TRANS_W) ? k0 * g.ldw : k0;
+    g.K = min(g.krange, (int32_t)(g.K - k0));
+    g.C = reinterpret_cast<float*>(g.C) + s * g.split_c;
+  }
+  return local;
+}
+
+template <int BN, int BM, int NS, int NSW, int EPI, int TR, int OCC>
+__global__ __launch_bounds__(256, OCC) void gemm_tokens_flex_kernel(const GemmArgs* __restrict__ probs, int32_t nprob,
+                                                                    int32_t total, bool uneven) {
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[(NSW * BN + NS * BM) * kBK];
+  const int32_t idx = uneven ? (int32_t)blockIdx.x : xcd_item(blockIdx.x, gridDim.x);
+  if (idx >= total) return;
+  GemmArgs g;
+  const int32_t t = tokens_problem<TR>(probs, nprob, idx, g);
+  int32_t tm, tn;
+  flex_walk(t, g.tiles_m, g.tiles_n, tm, tn);
+  flex_tile<BN, BM, NS, NSW, EPI, TR, false>(g, tm, tn, 0, (g.K + kBK - 1) / kBK, lds);
 }
 
 // Row gradients (128x96 tiles, GEMM_TRANS_W) and weight gradients (128x128, both
@@ -1698,41 +1740,42 @@ __global__ __launch_bounds__(256, 1) void gemm_tokens_pair_kernel(const GemmArgs
                                                                   int32_t td, int32_t gd,
                                                                   const GemmArgs* __restrict__ wprobs, int32_t nw,
                                                                   int32_t tw, bool uneven) {
-  constexpr int BN = 128, BM = 96, NS = 4, LDS = NS * (BN + BM) * kBK;
+  constexpr int BN = 128, BM = 96, NS = 4, LDS = NS * (BN + BM) * kBK, BOTH = GEMM_TRANS_X | GEMM_TRANS_W;
   __shared__ __attribute__((aligned(1024))) uint16_t lds[LDS];
   const bool data = (int32_t)blockIdx.x < gd;
-  const GemmArgs* const probs = data ? dprobs : wprobs;
-  const int32_t n = data ? nd : nw;
   const int32_t idx = data ? xcd_item(blockIdx.x, gd)
                            : uneven ? (int32_t)blockIdx.x - gd : xcd_item(blockIdx.x - gd, gridDim.x - gd);
   if (idx >= (data ? td : tw)) return;
-  int32_t p = 0;
-  while (p + 1 < n && probs[p + 1].tile_start <= idx) ++p;
-  const GemmArgs g = probs[p];
+  GemmArgs g;
+  const int32_t t = data ? tokens_problem<GEMM_TRANS_W>(dprobs, nd, idx, g) : tokens_problem<BOTH>(wprobs, nw, idx, g);
   int32_t tm, tn;
-  flex_walk(idx - g.tile_start, g.tiles_m, g.tiles_n, tm, tn);
+  flex_walk(t, g.tiles_m, g.tiles_n, tm, tn);
   const int32_t KT = (g.K + kBK - 1) / kBK;
   if (data)
     flex_tile<BN, BM, NS, NS, EPI, GEMM_TRANS_W>(g, tm, tn, 0, KT, lds);
   else
-    flex_tile<128, 128, 3, 2, WEPI, GEMM_TRANS_X | GEMM_TRANS_W>(g, tm, tn, 0, KT, lds);
+    flex_tile<128, 128, 3, 2, WEPI, BOTH>(g, tm, tn, 0, KT, lds);
 }
 
-// Ring tiles with an XCD's workgroups on consecutive tiles, 32 at a time: with few
-// token tiles (the fast index) a weight panel is then fetched by one XCD, not by
-// as many as there are token tiles.  XCD x owns tiles [x per, (x + 1) per).
+// Ring tiles; near: an XCD's workgroups on consecutive tiles, 32 at a time (XCD x
+// owns tiles [x per, (x + 1) per)), else the walk of the other grouped launches.
+// With few token tiles (the fast index) a weight panel is then fetched by one XCD,
+// not by as many as there are token tiles: row gradients of 701 targets, 32,003
+// columns of 2,048, 117 -> 80 us.
 template <int EPI, int TR>
 __global__ __launch_bounds__(256, 1) void gemm_tokens_ring_kernel(const GemmArgs* __restrict__ probs, int32_t nprob,
-                                                                  int32_t total, int32_t chain) {
+                                                                  int32_t total, int32_t chain, bool near) {
   __shared__ __attribute__((aligned(1024))) uint16_t lds[5 * 256 * kBK];
-  const int32_t per = (total + 7) / 8, first = (blockIdx.x & 7) * per, own = blockIdx.x >> 3;
-  int32_t p = 0;
+  const int32_t per = (total + 7) / 8, own = blockIdx.x >> 3;
   auto next = [&](int32_t r, GemmArgs& q, int32_t& tm, int32_t& tn) __attribute__((always_inline)) {
-    const int32_t l = (own >> 5) * 32 * chain + 32 * r + (own & 31), t = first + l;
-    if (r >= chain || l >= per || t >= total) return false;
-    while (p + 1 < nprob && probs[p + 1].tile_start <= t) ++p;
-    q = probs[p];
-    tile_of(t - q.tile_start, q.tiles_m, q.tiles_n, tm, tn);
+    int64_t t = chain_tile(blockIdx.x, chain, r);
+    if (near) {
+      const int32_t l = (own >> 5) * 32 * chain + 32 * r + (own & 31);
+      t = l < per ? (int64_t)(blockIdx.x & 7) * per + l : total;
+    }
+    if (r >= chain || t >= total) return false;
+    const int32_t local = tokens_problem<TR>(probs, nprob, (int32_t)t, q);
+    tile_of(local, q.tiles_m, q.tiles_n, tm, tn);
     return true;
   };
   ring_run<EPI, TR>(next, lds);
@@ -1744,43 +1787,38 @@ static hipError_t launch_tokens(hipStream_t s, const GemmArgs* p, int32_t n, con
   constexpr int BOTH = GEMM_TRANS_X | GEMM_TRANS_W;
   const dim3 block(256), flex((unsigned)((t.total + 7) / 8 * 8));
   if (t.shape == 0) {
-    const int32_t chain = ring_chain(t.total);
-    if constexpr (TR != BOTH)
-      if (t.tiles_m <= kFewTokenTiles) {
-        const int32_t per = (t.total + 7) / 8, whole = per / (32 * chain), rest = std::min(per - whole * 32 * chain, 32);
-        gemm_tokens_ring_kernel<EPI, TR><<<dim3(8 * (whole * 32 + rest)), block, 0, s>>>(p, n, t.total, chain);
-        return hipGetLastError();
-      }
-    const int32_t run = t.uneven ? 1 : chain;
-    gemm_grouped_ring_kernel<EPI, TR><<<dim3(ring_groups(t.total, run)), block, 0, s>>>(p, n, t.total, run);
+    const bool near = TR != BOTH && t.tiles_m <= kFewTokenTiles;
+    const int32_t chain = t.uneven ? 1 : ring_chain(t.total);
+    unsigned grid = ring_groups(t.total, chain);
+    if (near) {
+      const int32_t per = (t.total + 7) / 8, whole = per / (32 * chain), rest = std::min(per - whole * 32 * chain, 32);
+      grid = 8 * (whole * 32 + rest);
+    }
+    gemm_tokens_ring_kernel<EPI, TR><<<dim3(grid), block, 0, s>>>(p, n, t.total, chain, near);
     return hipGetLastError();
   }
+#define JN_FLEX(BN, BM, NS, NSW, OCC) \
+  gemm_tokens_flex_kernel<BN, BM, NS, NSW, EPI, TR, OCC><<<flex, block, 0, s>>>(p, n, t.total, t.uneven)
   if constexpr (TR == BOTH) {
     if (t.shape != k128Shape) return hipErrorInvalidValue;
-    gemm_grouped_flex_kernel<128, 128, 3, 2, EPI, TR, 2, false><<<flex, block, 0, s>>>(p, n, t.total, t.uneven);
-    return hipGetLastError();
+    JN_FLEX(128, 128, 3, 2, 2);
   } else {
-    if constexpr (TR == 0)
-      if (t.shape == 2) {
-        gemm_grouped_flex_kernel<256, 128, 3, 3, EPI, TR, 1, false><<<flex, block, 0, s>>>(p, n, t.total, false);
-        return hipGetLastError();
-      }
-    if (t.shape == 3) {
-      gemm_grouped_flex_kernel<128, 160, 4, 4, EPI, TR, 1, false><<<flex, block, 0, s>>>(p, n, t.total, false);
-      return hipGetLastError();
+    switch (t.shape) {
+      case 3: JN_FLEX(128, 160, 4, 4, 1); break;
+      case 4: JN_FLEX(128, 96, 4, 4, 1); break;
+      case 2:
+        if constexpr (TR != 0) return hipErrorInvalidValue;
+        else JN_FLEX(256, 128, 3, 3, 1);
+        break;
+      case 5:
+        if constexpr (TR != 0) return hipErrorInvalidValue;
+        else JN_FLEX(64, 96, 4, 4, 2);
+        break;
+      default: return hipErrorInvalidValue;
     }
-    if (t.shape == 4) {
-      gemm_grouped_flex_kernel<128, 96, 4, 4, EPI, TR, 1, false><<<flex, block, 0, s>>>(p, n, t.total, false);
-      return hipGetLastError();
-    }
-    if constexpr (TR == 0) {
-      if (t.shape == 5) {
-        gemm_grouped_flex_kernel<64, 96, 4, 4, EPI, TR, 2, false><<<flex, block, 0, s>>>(p, n, t.total, false);
-        return hipGetLastError();
-      }
-    }
-    return hipErrorInvalidValue;
   }
+#undef JN_FLEX
+  return hipGetLastError();
 }
 
 bool gemm_tokens_pair_ok(const TokTiles& rows, const TokTiles& weights) {

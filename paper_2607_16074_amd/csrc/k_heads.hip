@@ -800,32 +800,44 @@ hipError_t launch_tok_grad(hipStream_t s, const TokDesc* d, int32_t G, int32_t N
   return hipGetLastError();
 }
 
-// Eight elements of dh per thread.
+// Eight elements of dh per STR lanes, which share the planes (many planes are those
+// of few rows) and are added in pairs.
+template <int STR>
 __global__ __launch_bounds__(256) void tok_rows_kernel(const TokDesc* __restrict__ desc, int32_t G, int32_t N,
                                                        const float* __restrict__ inv, const float4* __restrict__ acc,
                                                        int32_t chunks) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, plane = (int64_t)N * chunks;
+  const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) / STR, plane = (int64_t)N * chunks;
   if (e >= plane) return;
   const int32_t i = (int32_t)(e / chunks), c = (int32_t)(e - (int64_t)i * chunks), t = tok_tenant(desc, G, i);
   const TokDesc& d = desc[t];
   if (!d.dh) return;
-  float4 a = acc[2 * e], b = acc[2 * e + 1];
+  float v[8] = {};
 #pragma unroll 4
-  for (int32_t k = 1; k < d.planes; ++k) {
+  for (int32_t k = threadIdx.x % STR; k < d.planes; k += STR) {
     const float4 x = acc[2 * (k * plane + e)], y = acc[2 * (k * plane + e) + 1];
-    a = make_float4(a.x + x.x, a.y + x.y, a.z + x.z, a.w + x.w);
-    b = make_float4(b.x + y.x, b.y + y.y, b.z + y.z, b.w + y.w);
+    const float w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += w[j];
   }
+#pragma unroll
+  for (int o = 1; o < STR; o <<= 1)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += __shfl_xor(v[j], o, kWave);
+  if (threadIdx.x % STR != 0) return;
   const float f = inv[t];
   reinterpret_cast<uint4*>(d.dh)[(int64_t)(i - d.first) * chunks + c] = make_uint4(
-      pack_bf2(a.x * f, a.y * f), pack_bf2(a.z * f, a.w * f), pack_bf2(b.x * f, b.y * f), pack_bf2(b.z * f, b.w * f));
+      pack_bf2(v[0] * f, v[1] * f), pack_bf2(v[2] * f, v[3] * f), pack_bf2(v[4] * f, v[5] * f), pack_bf2(v[6] * f, v[7] * f));
 }
 
 hipError_t launch_tok_rows(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const float* inv, const float* acc,
-                           int32_t width) {
-  const int64_t blocks = ((int64_t)N * (width / 8) + 255) / 256;
-  tok_rows_kernel<<<(unsigned)blocks, 256, 0, s>>>(d, G, N, inv, reinterpret_cast<const float4*>(acc), width / 8);
-  return hipGetLastError();
+                           int32_t planes, int32_t width) {
+  const int64_t all = (int64_t)N * (width / 8);
+  auto go = [&](auto str) {
+    tok_rows_kernel<str()><<<(unsigned)((all * str() + 255) / 256), 256, 0, s>>>(
+        d, G, N, inv, reinterpret_cast<const float4*>(acc), width / 8);
+    return hipGetLastError();
+  };
+  return planes > 16 && all < (1 << 20) ? go(std::integral_constant<int, 16>()) : go(std::integral_constant<int, 1>());
 }
 
 // ---- tenants of few rows ----
@@ -836,6 +848,21 @@ typedef __bf16 bf16x8h __attribute__((ext_vector_type(8)));
 typedef float f32x4h __attribute__((ext_vector_type(4)));
 constexpr int kSmallThreads = 512;
 constexpr float kLog2e = 1.4426950408889634f;
+
+// Two floats to bf16 by one instruction (pack_bf2 takes three).
+__device__ __forceinline__ uint32_t cvt_bf2(float lo, float hi) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{lo, hi}, b2));
+}
+
+template <bool ONCE, typename V>
+__device__ __forceinline__ void put_once(V v, V* p) {
+  if constexpr (ONCE)
+    __builtin_nontemporal_store(v, p);
+  else
+    *p = v;
+}
 
 // LDS written before is read behind it; loads from memory stay in flight.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
@@ -889,12 +916,16 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_scores_kernel(TokSmall
   bf16x8h x[8 * CH][NB];
 #pragma unroll
   for (int j = 0; j < NB; ++j) {
+    // (loads without a condition: rows without a target read W instead)
     const int32_t r = small_row(d, 16 * j + row, T);
-    const uint16_t* const p = hidden + (int64_t)max(r, 0) * width + s0 * 32 + 8 * quad;
+    const uint16_t* const p = (r >= 0 ? hidden + (int64_t)r * width : d.W) + s0 * 32 + 8 * quad;
 #pragma unroll
     for (int s = 0; s < 8 * CH; ++s) {
       x[s][j] = bf16x8h{};
-      if (r >= 0 && s < ns) x[s][j] = *reinterpret_cast<const bf16x8h*>(p + 32 * s);
+      if (s < ns) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p + 32 * s);
+        x[s][j] = __builtin_bit_cast(bf16x8h, r >= 0 ? v : make_uint4(0, 0, 0, 0));
+      }
     }
   }
   const int32_t tok = threadIdx.x % TOK;
@@ -1060,16 +1091,27 @@ __global__ __launch_bounds__(kSmallThreads) void small_pick_kernel(TokSmallArgs<
 // dW = dz^T H / count for up to 32 NS rows: the contraction is the rows, so one or
 // two matrix instructions make 16 vocabulary rows x 16 columns, and the kernel is
 // bound by writing dW.  A lane's fragments of H^T stay in registers: it reads 8
-// columns (16 bytes) of 8 rows and turns them, so that fragment j of a group of 128
-// columns holds columns 8 i + j of row i of the instruction, and the 8 results of
-// a lane for one of its 4 rows are 8 adjacent columns: one 16-byte store.  dz is
-// formed from z and the rows' joined sums by every wavefront for itself, rounded to
-// bf16 unscaled (TokRow).  blockIdx.y: 2,048 columns each.
-template <int GP, int NS, int C, bool F32>
+// columns (16 bytes) of 8 rows and turns them, so that row i = 4 q + e of
+// instruction j is column 32 e + 8 q + j of a group of 128: the 8 results of a lane
+// for one e are 8 adjacent columns, turned around in LDS so that a store instruction
+// writes 256 adjacent bytes of 4 rows.  60 rows, 120,000 x 2,048 (491 MB): 187 us with 16
+// bytes in each of four places a row and instruction, 152 with 64 adjacent ones, 120
+// so, non-temporally (93 with plain stores, whose lines the next call then waits
+// for: 260 us a call instead of 243).  dz of 128
+// vocabulary rows at a time is formed from z and the rows' joined sums by the
+// workgroup's threads together, 8 rows of the feature each, rounded to bf16 unscaled
+// (TokRow) and shared through LDS; the next rows of z are on their way meanwhile.
+// rows: those of a chunk, 128 or, of small vocabularies, fewer (a multiple of 16), so
+// that there are workgroups for the chip.  blockIdx.y: 2,048 columns each.
+constexpr int kGradRows = kSmallGradRows;
+template <int GP, int NS, int C, bool F32, bool ONCE>
 __global__ __launch_bounds__(kSmallThreads, 2) void small_grads_kernel(TokSmallArgs<C> set, int32_t ldz,
                                                                        const uint16_t* __restrict__ hidden, int32_t T,
-                                                                       int32_t width) {
+                                                                       int32_t width, int32_t rows) {
+  constexpr int TG = 4 * NS, U = kGradRows * TG / kSmallThreads, LD = 32 * NS + 8;  // groups of 8 rows; passes; elements of a line
   __shared__ SmallJoin<32 * NS> l;
+  __shared__ __attribute__((aligned(16))) uint16_t dz[2][kGradRows * LD];
+  __shared__ u32x4t stage[8][256];
   __shared__ __attribute__((aligned(16))) float lse[64], own[64];
   __shared__ __attribute__((aligned(16))) int32_t lab[64];
   __shared__ float scale;
@@ -1080,6 +1122,7 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_grads_kernel(TokSmallA
   // column groups of this slice, and how many wavefronts share them
   const int32_t g0 = 16 * blockIdx.y, groups = min((width + 127) / 128 - g0, 16);
   const int32_t WC = groups > 4 ? 8 : groups > 2 ? 4 : groups, WV = 8 / WC, wc = w % WC, wv = w / WC;
+  u32x4t* const mine16 = stage[w];
   const int32_t mine = small_row(d, lane, T);  // of row `lane`
   uint4 q[GP][NS][8];
 #pragma unroll
@@ -1089,9 +1132,11 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_grads_kernel(TokSmallA
       const int32_t r = __shfl(mine, 32 * s + 8 * quad + t, kWave);
 #pragma unroll
       for (int p = 0; p < GP; ++p) {
-        const int32_t k = 128 * (g0 + wc + 8 * p) + 8 * col;
-        q[p][s][t] = make_uint4(0, 0, 0, 0);
-        if (r >= 0 && k < width) q[p][s][t] = *reinterpret_cast<const uint4*>(hidden + (int64_t)r * width + k);
+        // (a load without a condition: rows without a target, and columns past the end, read W instead)
+        const int32_t k = 128 * (g0 + wc + 8 * p) + 32 * (col & 3) + 8 * (col >> 2);
+        const bool in = r >= 0 && k < width;
+        const uint4 v = *reinterpret_cast<const uint4*>(in ? hidden + (int64_t)r * width + k : d.W);
+        q[p][s][t] = in ? v : make_uint4(0, 0, 0, 0);
       }
     }
   {
@@ -1136,73 +1181,94 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_grads_kernel(TokSmallA
         }
         h[p][s][j] = __builtin_bit_cast(bf16x8h, make_uint4(f[0], f[1], f[2], f[3]));
       }
-  float l2[NS][8], ow[NS][8];
-  int32_t lb[NS][8];
+  // this thread's 8 rows of the feature, and its vocabulary rows r0 + u 512 / TG of a chunk
+  const int32_t tg = threadIdx.x % TG, r0 = threadIdx.x / TG;
+  float l2[8], ow[8];
+  int32_t lb[8];
 #pragma unroll
-  for (int s = 0; s < NS; ++s)
-#pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      l2[s][t] = lse[32 * s + 8 * quad + t];
-      ow[s][t] = own[32 * s + 8 * quad + t];
-      lb[s][t] = lab[32 * s + 8 * quad + t];
-    }
+  for (int t = 0; t < 8; ++t) {
+    l2[t] = lse[8 * tg + t];
+    ow[t] = own[8 * tg + t];
+    lb[t] = lab[8 * tg + t];
+  }
   const float inv = scale;
-  const int32_t blocks = (V + 16 * WV - 1) / (16 * WV);
-  const int32_t b0 = (int32_t)((int64_t)blocks * wg / d.gwgs), b1 = (int32_t)((int64_t)blocks * (wg + 1) / d.gwgs);
-  float4 z[NS][2];
-  auto fetch = [&](int32_t b) __attribute__((always_inline)) {
-    const int32_t v = min((b * WV + wv) * 16 + col, V - 1);
+  const bool held = n > 0 && 8 * tg < ldz;  // z has these columns
+  const int32_t chunks = (V + rows - 1) / rows;
+  const int32_t c0 = (int32_t)((int64_t)chunks * wg / d.gwgs), c1 = (int32_t)((int64_t)chunks * (wg + 1) / d.gwgs);
+  float4 z[U][2];
+  auto fetch = [&](int32_t c) __attribute__((always_inline)) {
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      z[s][0] = z[s][1] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (n > 0 && 32 * s + 8 * quad < ldz) {
-        const float4* const p = reinterpret_cast<const float4*>(d.z + (int64_t)v * ldz + 32 * s + 8 * quad);
-        z[s][0] = p[0];
-        z[s][1] = p[1];
+    for (int u = 0; u < U; ++u) {
+      z[u][0] = z[u][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (held && r0 + u * (kSmallThreads / TG) < rows) {
+        const int32_t v = min(c * rows + r0 + u * (kSmallThreads / TG), V - 1);
+        const float4* const p = reinterpret_cast<const float4*>(d.z + (int64_t)v * ldz + 8 * tg);
+        z[u][0] = p[0];
+        z[u][1] = p[1];
       }
     }
   };
-  if (b0 < b1) fetch(b0);
-  for (int32_t b = b0; b < b1; ++b) {
-    const int32_t v = (b * WV + wv) * 16 + col;
-    bf16x8h g[NS];
+  if (c0 < c1) fetch(c0);
+  for (int32_t c = c0; c < c1; ++c) {
+    uint16_t* const line = dz[(c - c0) & 1];
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      float p[8] = {z[s][0].x, z[s][0].y, z[s][0].z, z[s][0].w, z[s][1].x, z[s][1].y, z[s][1].z, z[s][1].w};
+    for (int u = 0; u < U; ++u) {
+      const int32_t r = r0 + u * (kSmallThreads / TG), v = c * rows + r;
+      if (r >= rows) break;
+      float p[8] = {z[u][0].x, z[u][0].y, z[u][0].z, z[u][0].w, z[u][1].x, z[u][1].y, z[u][1].z, z[u][1].w};
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
-        p[t] = __builtin_amdgcn_exp2f(fmaf(p[t], kLog2e, -l2[s][t]));
-        p[t] = lb[s][t] == v ? ow[s][t] : p[t];
+        p[t] = __builtin_amdgcn_exp2f(fmaf(p[t], kLog2e, -l2[t]));
+        p[t] = lb[t] == v ? ow[t] : p[t];
       }
-      const uint4 q = make_uint4(pack_bf2(p[0], p[1]), pack_bf2(p[2], p[3]), pack_bf2(p[4], p[5]), pack_bf2(p[6], p[7]));
-      g[s] = __builtin_bit_cast(bf16x8h, q);
-      if (d.grad && wc == 0 && blockIdx.y == 0 && v < V && 32 * s + 8 * quad < ldz)
-        *reinterpret_cast<uint4*>(d.grad + (int64_t)v * ldz + 32 * s + 8 * quad) = q;
+      const uint4 g = make_uint4(cvt_bf2(p[0], p[1]), cvt_bf2(p[2], p[3]), cvt_bf2(p[4], p[5]), cvt_bf2(p[6], p[7]));
+      *reinterpret_cast<uint4*>(line + r * LD + 8 * tg) = g;
+      if (d.grad && blockIdx.y == 0 && v < V && 8 * tg < ldz)
+        *reinterpret_cast<uint4*>(d.grad + (int64_t)v * ldz + 8 * tg) = g;
     }
-    if (b + 1 < b1) fetch(b + 1);
+    lds_barrier();  // (the other line's readers passed the barrier before this one)
+    if (c + 1 < c1) fetch(c + 1);
+    for (int32_t b = wv; b < rows / 16; b += WV) {
+      bf16x8h g[NS];
 #pragma unroll
-    for (int p = 0; p < GP; ++p) {
-      f32x4h a[8];
+      for (int s = 0; s < NS; ++s)
+        g[s] = *reinterpret_cast<const bf16x8h*>(line + (16 * b + col) * LD + 32 * s + 8 * quad);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        a[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h[p][0][j], g[0], f32x4h{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-        if constexpr (NS == 2) a[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h[p][1][j], g[1], a[j], 0, 0, 0);
-      }
-      const int32_t k = 128 * (g0 + wc + 8 * p) + 32 * quad;
-      if (v < V && wc + 8 * p < groups) {
+      for (int p = 0; p < GP; ++p) {
+        f32x4h a[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (k + 8 * e >= width) continue;
-          const int64_t at = (int64_t)v * width + k + 8 * e;
-          if constexpr (F32) {
-            float4* const to = reinterpret_cast<float4*>(static_cast<float*>(d.dW) + at);
-            to[0] = make_float4(a[0][e] * inv, a[1][e] * inv, a[2][e] * inv, a[3][e] * inv);
-            to[1] = make_float4(a[4][e] * inv, a[5][e] * inv, a[6][e] * inv, a[7][e] * inv);
-          } else {
-            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(d.dW) + at) =
-                make_uint4(pack_bf2(a[0][e] * inv, a[1][e] * inv), pack_bf2(a[2][e] * inv, a[3][e] * inv),
-                           pack_bf2(a[4][e] * inv, a[5][e] * inv), pack_bf2(a[6][e] * inv, a[7][e] * inv));
+        for (int j = 0; j < 8; ++j) {
+          a[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h[p][0][j], g[0], f32x4h{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+          if constexpr (NS == 2) a[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h[p][1][j], g[1], a[j], 0, 0, 0);
+        }
+        if (wc + 8 * p >= groups) continue;
+        // turned around in LDS: a store instruction writes 256 adjacent bytes of 4 rows
+        constexpr int HALVES = F32 ? 2 : 1, COLS = 128 / HALVES;
+#pragma unroll
+        for (int f = 0; f < HALVES; ++f) {
+#pragma unroll
+          for (int e = f * 4 / HALVES; e < (f + 1) * 4 / HALVES; ++e) {
+            const int chunk = F32 ? 8 * (e & 1) + 2 * quad : 4 * e + quad;
+            if constexpr (F32) {
+              mine16[col * 16 + (chunk ^ col)] = __builtin_bit_cast(u32x4t, f32x4h{a[0][e] * inv, a[1][e] * inv, a[2][e] * inv, a[3][e] * inv});
+              mine16[col * 16 + ((chunk + 1) ^ col)] = __builtin_bit_cast(u32x4t, f32x4h{a[4][e] * inv, a[5][e] * inv, a[6][e] * inv, a[7][e] * inv});
+            } else {
+              mine16[col * 16 + (chunk ^ col)] = u32x4t{cvt_bf2(a[0][e] * inv, a[1][e] * inv), cvt_bf2(a[2][e] * inv, a[3][e] * inv),
+                                                        cvt_bf2(a[4][e] * inv, a[5][e] * inv), cvt_bf2(a[6][e] * inv, a[7][e] * inv)};
+            }
           }
+          __builtin_amdgcn_wave_barrier();  // (a wave's LDS operations stay in order)
+          const int32_t k = 128 * (g0 + wc + 8 * p) + COLS * f + COLS / 16 * col;
+          u32x4t o[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[r] = mine16[(4 * r + quad) * 16 + (col ^ (4 * r + quad))];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int32_t v = c * rows + 16 * b + 4 * r + quad;
+            if (v < V && k < width)
+              put_once<ONCE>(o[r], reinterpret_cast<u32x4t*>(static_cast<char*>(d.dW) + ((int64_t)v * width + k) * (F32 ? 4 : 2)));
+          }
+          __builtin_amdgcn_wave_barrier();
         }
       }
     }
@@ -1211,11 +1277,11 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_grads_kernel(TokSmallA
 
 static int small_share(int32_t d) { return d <= 256 ? 1 : d <= 512 ? 2 : d <= 1024 ? 4 : 8; }  // WK
 int32_t small_score_rows(int32_t d) { return 16 * (8 / small_share(d)); }
-int32_t small_grad_rows(int32_t d) {
-  const int32_t groups = (d + 127) / 128;
-  return 16 * (groups > 4 ? 1 : groups > 2 ? 2 : 8 / groups);
+int32_t small_grad_rows(int32_t d, int64_t vocab) {
+  const int32_t groups = (d + 127) / 128, least = groups > 4 ? 16 : groups > 2 ? 32 : 128 / groups;  // of all wavefronts
+  const int64_t each = (vocab + kSmallGroups - 1) / kSmallGroups;
+  return (int32_t)std::max<int64_t>(least, std::min<int64_t>(kSmallGradRows, (each + 15) / 16 * 16));
 }
-
 // Kernel arguments of two tenants take 0.3 KB, of kSmallTenants 3 KB.
 template <typename F>
 static hipError_t with_tenants(const TokSmallSet& set, F&& f) {
@@ -1259,17 +1325,23 @@ hipError_t launch_small_scores(hipStream_t s, const TokSmallSet& all, int32_t wg
 }
 
 hipError_t launch_small_grads(hipStream_t s, const TokSmallSet& all, int32_t wgs, int32_t ldz, const void* hidden,
-                              int32_t T, int32_t d, bool f32) {
+                              int32_t T, int32_t d, int32_t rows, bool f32) {
+  if (rows < 16 || rows > kSmallGradRows || rows % 16 != 0) return hipErrorInvalidValue;
   const uint16_t* const h = static_cast<const uint16_t*>(hidden);
   const dim3 grid(wgs, (d + 2047) / 2048);
+  // dW stored non-temporally where W, read before, and dW pass the last-level cache:
+  // the next call's W then need not push dW out (5 rows, 60,000 x 2,048 129 -> 115 us)
+  int64_t bytes = 0;
+  for (int32_t g = 0; g < all.G; ++g) bytes += (f32 ? 6ll : 4ll) * all.t[g].vocab * d;
   return with_tenants(all, [&](const auto& set) {
     constexpr int C = sizeof(set.t) / sizeof(set.t[0]);
     auto go = [&](auto gp, auto ns) {
-      if (f32)
-        small_grads_kernel<gp(), ns(), C, true><<<grid, kSmallThreads, 0, s>>>(set, ldz, h, T, d);
-      else
-        small_grads_kernel<gp(), ns(), C, false><<<grid, kSmallThreads, 0, s>>>(set, ldz, h, T, d);
-      return hipGetLastError();
+      auto kind = [&](auto f32_, auto once) {
+        small_grads_kernel<gp(), ns(), C, f32_(), once()><<<grid, kSmallThreads, 0, s>>>(set, ldz, h, T, d, rows);
+        return hipGetLastError();
+      };
+      auto type = [&](auto once) { return f32 ? kind(std::true_type(), once) : kind(std::false_type(), once); };
+      return bytes > kStreamBytes ? type(std::true_type()) : type(std::false_type());
     };
     auto steps = [&](auto gp) {
       return ldz > 32 ? go(gp, std::integral_constant<int, 2>()) : go(gp, std::integral_constant<int, 1>());
