@@ -18,6 +18,13 @@ __device__ __forceinline__ uint32_t pack_bf2(float lo, float hi) {
   return (uint32_t)f2bf(lo) | ((uint32_t)f2bf(hi) << 16);
 }
 
+// The same by one instruction (pack_bf2 takes three).
+__device__ __forceinline__ uint32_t cvt_bf2(float lo, float hi) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{lo, hi}, b2));
+}
+
 // ds_read_b64_tr_b16 at LDS address p + OFF bytes (in each 16-lane group,
 // lane i receives element i % 4 of the 8-byte chunks that lanes 4e + i / 4
 // address, e = 0..3), issued as inline assembly.  The compiler's wait

@@ -849,13 +849,6 @@ typedef float f32x4h __attribute__((ext_vector_type(4)));
 constexpr int kSmallThreads = 512;
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Two floats to bf16 by one instruction (pack_bf2 takes three).
-__device__ __forceinline__ uint32_t cvt_bf2(float lo, float hi) {
-  typedef float f2 __attribute__((ext_vector_type(2)));
-  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{lo, hi}, b2));
-}
-
 template <bool ONCE, typename V>
 __device__ __forceinline__ void put_once(V v, V* p) {
   if constexpr (ONCE)

@@ -255,7 +255,13 @@ hipError_t launch_rmsnorm_f32in(hipStream_t s, const float* x, const void* g, vo
 // Bound by memory; with E = 4 a step holds fewer heads, so that less of the last
 // one is idle (18 heads: 5 steps of 4, not 3 of 8), and the gradients' sums, gains
 // and rows fit the registers of four wavefronts a SIMD: 75,923 rows forward 129 ->
-// 124 us, gradients 262 -> 223.  The rows' loads are issued before the sines.
+// 124 us, gradients 262 -> 223.  The rows' loads are issued before the sines.  A
+// vector instruction takes four cycles, so instructions count too: with the row
+// and the step's offsets in scalar registers, 1 / hd multiplied in, the keys' gains
+// chosen and their sums taken apart only in steps that hold keys, 160 -> 110 a step
+// forward and 215 -> 155 backward, where they were 66 % of the time: 217 -> 193 us
+// (5.4 TB/s; forward 116, 6.0 TB/s).  The next two steps' loads in flight under
+// each step, over the ends of rows, measured the same 193.
 constexpr int kQkFwdE = 4, kQkBwdE = 4;
 constexpr int kQkStep = 4;  // head steps whose loads are issued together
 
@@ -312,13 +318,13 @@ __device__ __forceinline__ void widen(const QkRaw<E>& q, float* v) {
 
 // Results beyond the last-level cache are stored non-temporally (kStreamBytes):
 // 75,923 rows of 18 heads of 128 forward 123.7 -> 116.9 us (6.0 TB/s), gradients
-// 222.8 -> 216.3 (4.9 TB/s).
+// 222.8 -> 216.3.
 template <int E, bool ONCE>
 __device__ __forceinline__ void put_bf(uint16_t* p, const float* v) {
   typedef uint32_t V __attribute__((ext_vector_type(E / 2)));
   V r;
 #pragma unroll
-  for (int k = 0; k < E / 2; ++k) r[k] = pack_bf2(v[2 * k], v[2 * k + 1]);
+  for (int k = 0; k < E / 2; ++k) r[k] = cvt_bf2(v[2 * k], v[2 * k + 1]);
   if constexpr (ONCE)
     __builtin_nontemporal_store(r, reinterpret_cast<V*>(p));
   else
@@ -336,13 +342,19 @@ struct QkGains {
     k[0] = raw<E>(a.gk + at);
     k[1] = raw<E>(a.gk + at + half);
   }
-  __device__ __forceinline__ void get(bool key, float* v) const {
+  // any: whether a head of the step is a key (for the whole wavefront)
+  __device__ __forceinline__ void get(bool any, bool key, float* v) const {
+    if (!any) {
+      widen<E>(q[0], v);
+      widen<E>(q[1], v + E);
+    } else {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      QkRaw<E> r;
+      for (int s = 0; s < 2; ++s) {
+        QkRaw<E> r;
 #pragma unroll
-      for (int i = 0; i < E / 2; ++i) r.w[i] = key ? k[s].w[i] : q[s].w[i];
-      widen<E>(r, v + E * s);
+        for (int i = 0; i < E / 2; ++i) r.w[i] = key ? k[s].w[i] : q[s].w[i];
+        widen<E>(r, v + E * s);
+      }
     }
   }
 };
@@ -352,7 +364,7 @@ template <int E, int P2, bool NORM, bool ROPE, bool ONCE>
 __global__ __launch_bounds__(256) void qk_fwd_kernel(QkShape a, const uint16_t* x, uint16_t* y, int32_t parts) {
   __shared__ __attribute__((aligned(16))) float lines[4][256];
   constexpr int PER = 64 / P2;  // heads per step
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, q = lane % P2, slot = lane / P2;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane % P2, slot = lane / P2;
   const int64_t item = (int64_t)blockIdx.x * 4 + w;
   const int64_t row = item / parts;
   if (row >= a.rows) return;
@@ -360,8 +372,9 @@ __global__ __launch_bounds__(256) void qk_fwd_kernel(QkShape a, const uint16_t* 
   const int steps = (heads + PER - 1) / PER, part = (int)(item - row * parts);
   const int s0 = steps * part / parts, s1 = steps * (part + 1) / parts;
   const bool live = E * q < half;
-  const uint16_t* xr = x + row * a.ldx + E * q;
-  uint16_t* yr = y + row * a.ldy + E * q;
+  const uint32_t mine = slot * a.hd + E * q;
+  const uint16_t* const xr = x + row * a.ldx;
+  uint16_t* const yr = y + row * a.ldy;
   QkRaw<E> v[kQkStep][2];
   auto fetch = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
@@ -369,8 +382,9 @@ __global__ __launch_bounds__(256) void qk_fwd_kernel(QkShape a, const uint16_t* 
       const int h = (s + j) * PER + slot;
       v[j][0] = v[j][1] = QkRaw<E>{};
       if (s + j < s1 && live && h < heads) {
-        v[j][0] = raw<E>(xr + h * a.hd);
-        v[j][1] = raw<E>(xr + h * a.hd + half);
+        const uint16_t* const at = xr + (s + j) * PER * a.hd;
+        v[j][0] = raw<E>(at + mine);
+        v[j][1] = raw<E>(at + half + mine);
       }
     }
   };
@@ -378,6 +392,7 @@ __global__ __launch_bounds__(256) void qk_fwd_kernel(QkShape a, const uint16_t* 
   QkGains<E> g;
   if constexpr (NORM) g.load(a, live ? E * q : 0);
   const float* const line = lines[w] + (live ? E * q : 0);
+  const float part_of = 1.f / (float)a.hd;
   if constexpr (ROPE) row_turns(a, row, lane, lines[w]);
   for (int s = s0; s < s1; s += kQkStep) {
     if (s > s0) fetch(s);
@@ -392,8 +407,8 @@ __global__ __launch_bounds__(256) void qk_fwd_kernel(QkShape a, const uint16_t* 
         float ss = 0.f, gv[2 * E];
 #pragma unroll
         for (int k = 0; k < 2 * E; ++k) ss = fmaf(u[k], u[k], ss);
-        const float r = rsqrtf(head_sum<P2>(ss) / (float)a.hd + a.eps);
-        g.get(h >= a.heads, gv);
+        const float r = rsqrtf(fmaf(head_sum<P2>(ss), part_of, a.eps));
+        g.get((s + j + 1) * PER > a.heads, h >= a.heads, gv);
 #pragma unroll
         for (int k = 0; k < 2 * E; ++k) u[k] = u[k] * r * gv[k];
       }
@@ -406,8 +421,9 @@ __global__ __launch_bounds__(256) void qk_fwd_kernel(QkShape a, const uint16_t* 
         }
       }
       if (live && h < heads) {
-        put_bf<E, ONCE>(yr + h * a.hd, u);
-        put_bf<E, ONCE>(yr + h * a.hd + half, u + E);
+        uint16_t* const at = yr + (s + j) * PER * a.hd;
+        put_bf<E, ONCE>(at + mine, u);
+        put_bf<E, ONCE>(at + half + mine, u + E);
       }
     }
   }
@@ -422,7 +438,7 @@ __global__ __launch_bounds__(256, 4) void qk_bwd_kernel(QkShape a, const uint16_
   __shared__ __attribute__((aligned(16))) float lines[4][256];
   __shared__ float sums[NORM ? 4 : 1][2][256];
   constexpr int PER = 64 / P2, STEP = 2;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, q = lane % P2, slot = lane / P2;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane % P2, slot = lane / P2;
   const int heads = a.heads + a.kv, half = a.hd >> 1, steps = (heads + PER - 1) / PER;
   const bool live = E * q < half;
   QkGains<E> g;
@@ -435,10 +451,12 @@ __global__ __launch_bounds__(256, 4) void qk_bwd_kernel(QkShape a, const uint16_
       for (int i = 0; i < 2 * E; ++i) dg[k][i] = 0.f;
   }
   const float* const line = lines[w] + (live ? E * q : 0);
+  const uint32_t mine = slot * a.hd + E * q;
+  const float part_of = 1.f / (float)a.hd;
   for (int64_t row = (int64_t)blockIdx.x * 4 + w; row < a.rows; row += (int64_t)gridDim.x * 4) {
-    const uint16_t* xr = x + row * a.ldx + E * q;
-    const uint16_t* yr = dy + row * a.ldy + E * q;
-    uint16_t* dr = dx + row * a.ldd + E * q;
+    const uint16_t* const xr = x + row * a.ldx;
+    const uint16_t* const yr = dy + row * a.ldy;
+    uint16_t* const dr = dx + row * a.ldd;
     QkRaw<E> v[STEP][4];
     auto fetch = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
@@ -447,12 +465,13 @@ __global__ __launch_bounds__(256, 4) void qk_bwd_kernel(QkShape a, const uint16_
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[j][k] = QkRaw<E>{};
         if (live && h < heads) {
+          const int at = (s + j) * PER * a.hd;
           if constexpr (NORM) {
-            v[j][0] = raw<E>(xr + h * a.hd);
-            v[j][1] = raw<E>(xr + h * a.hd + half);
+            v[j][0] = raw<E>(xr + at + mine);
+            v[j][1] = raw<E>(xr + at + half + mine);
           }
-          v[j][2] = raw<E>(yr + h * a.hd);
-          v[j][3] = raw<E>(yr + h * a.hd + half);
+          v[j][2] = raw<E>(yr + at + mine);
+          v[j][3] = raw<E>(yr + at + half + mine);
         }
       }
     };
@@ -476,29 +495,38 @@ __global__ __launch_bounds__(256, 4) void qk_bwd_kernel(QkShape a, const uint16_
           }
         }
         if constexpr (NORM) {
-          float xh[2 * E], gv[2 * E], ss = 0.f, dot = 0.f;
-          widen<E>(v[j][0], xh);
-          widen<E>(v[j][1], xh + E);
-#pragma unroll
-          for (int k = 0; k < 2 * E; ++k) ss = fmaf(xh[k], xh[k], ss);
-          const float r = rsqrtf(head_sum<P2>(ss) / (float)a.hd + a.eps);
-          const bool key = h >= a.heads;
-          g.get(key, gv);
+          // with t = g du: mean(xh t) = r mean(x t), dx = r (t - x r mean(xh t))
+          float xv[2 * E], gv[2 * E], ss = 0.f, dot = 0.f;
+          widen<E>(v[j][0], xv);
+          widen<E>(v[j][1], xv + E);
+          const bool any = (s + j + 1) * PER > a.heads, key = h >= a.heads;
+          g.get(any, key, gv);
 #pragma unroll
           for (int k = 0; k < 2 * E; ++k) {
-            xh[k] *= r;
-            const float t = du[k] * xh[k];
-            dg[0][k] += key ? 0.f : t;  // (lanes without a head hold zeros)
-            dg[1][k] += key ? t : 0.f;
-            dot = fmaf(t, gv[k], dot);
+            ss = fmaf(xv[k], xv[k], ss);
+            gv[k] *= du[k];
+            dot = fmaf(xv[k], gv[k], dot);
           }
-          const float c = head_sum<P2>(dot) / (float)a.hd;
+          const float r = rsqrtf(fmaf(head_sum<P2>(ss), part_of, a.eps));
+          if (!any) {
 #pragma unroll
-          for (int k = 0; k < 2 * E; ++k) du[k] = r * (gv[k] * du[k] - xh[k] * c);
+            for (int k = 0; k < 2 * E; ++k) dg[0][k] = fmaf(du[k], xv[k] * r, dg[0][k]);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 2 * E; ++k) {
+              const float t = du[k] * (xv[k] * r);
+              dg[0][k] += key ? 0.f : t;  // (lanes without a head hold zeros)
+              dg[1][k] += key ? t : 0.f;
+            }
+          }
+          const float c = r * (r * head_sum<P2>(dot) * part_of);
+#pragma unroll
+          for (int k = 0; k < 2 * E; ++k) du[k] = r * fmaf(-xv[k], c, gv[k]);
         }
         if (live && h < heads) {
-          put_bf<E, ONCE>(dr + h * a.hd, du);
-          put_bf<E, ONCE>(dr + h * a.hd + half, du + E);
+          uint16_t* const at = dr + (s + j) * PER * a.hd;
+          put_bf<E, ONCE>(at + mine, du);
+          put_bf<E, ONCE>(at + half + mine, du + E);
         }
       }
     }
