@@ -1734,14 +1734,17 @@ __global__ __launch_bounds__(256, OCC) void gemm_tokens_flex_kernel(const GemmAr
 }
 
 // Row gradients (128x96 tiles, GEMM_TRANS_W) and weight gradients (128x128, both
-// operands transposed) of a call in one launch, as gemm_grad_pair_kernel.
+// operands transposed) of a call in one launch, two workgroups a CU: eight tenants,
+// 2,003 targets, 2,049 x 768 61 us a call (65 with one a CU and a stage more of the
+// 128x96 tiles, 69 as two launches); 900 targets, 8,000 x 768 131 (144 as two); one
+// tenant, 80, 160,000 x 1,024 306 (334); 100, 100,000 x 768 176 (180).
 template <int EPI, int WEPI>
-__global__ __launch_bounds__(256, 1) void gemm_tokens_pair_kernel(const GemmArgs* __restrict__ dprobs, int32_t nd,
+__global__ __launch_bounds__(256, 2) void gemm_tokens_pair_kernel(const GemmArgs* __restrict__ dprobs, int32_t nd,
                                                                   int32_t td, int32_t gd,
                                                                   const GemmArgs* __restrict__ wprobs, int32_t nw,
                                                                   int32_t tw, bool uneven) {
-  constexpr int BN = 128, BM = 96, NS = 4, LDS = NS * (BN + BM) * kBK, BOTH = GEMM_TRANS_X | GEMM_TRANS_W;
-  __shared__ __attribute__((aligned(1024))) uint16_t lds[LDS];
+  constexpr int BOTH = GEMM_TRANS_X | GEMM_TRANS_W;
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[5 * 128 * kBK];
   const bool data = (int32_t)blockIdx.x < gd;
   const int32_t idx = data ? xcd_item(blockIdx.x, gd)
                            : uneven ? (int32_t)blockIdx.x - gd : xcd_item(blockIdx.x - gd, gridDim.x - gd);
@@ -1752,7 +1755,7 @@ __global__ __launch_bounds__(256, 1) void gemm_tokens_pair_kernel(const GemmArgs
   flex_walk(t, g.tiles_m, g.tiles_n, tm, tn);
   const int32_t KT = (g.K + kBK - 1) / kBK;
   if (data)
-    flex_tile<BN, BM, NS, NS, EPI, GEMM_TRANS_W>(g, tm, tn, 0, KT, lds);
+    flex_tile<128, 96, 3, 2, EPI, GEMM_TRANS_W>(g, tm, tn, 0, KT, lds);
   else
     flex_tile<128, 128, 3, 2, WEPI, BOTH>(g, tm, tn, 0, KT, lds);
 }
@@ -1822,7 +1825,7 @@ static hipError_t launch_tokens(hipStream_t s, const GemmArgs* p, int32_t n, con
 }
 
 bool gemm_tokens_pair_ok(const TokTiles& rows, const TokTiles& weights) {
-  return rows.total > 0 && rows.shape == 4 && weights.shape == k128Shape && weights.total <= 1024;
+  return rows.total > 0 && rows.shape == 4 && weights.shape == k128Shape;
 }
 
 hipError_t launch_gemm_tokens_pair(hipStream_t s, int depi, const GemmArgs* dprobs, int32_t nd, const TokTiles& d,
