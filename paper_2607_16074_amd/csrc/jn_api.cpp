@@ -1207,6 +1207,9 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
   return JN_OK;
 }
 
+// Elements of a vocabulary row's logits where no tenant has more than `most` entries.
+int32_t small_ldz(int32_t most) { return most > 32 ? 64 : most > 16 ? 32 : 16; }
+
 // Tenants of few rows: launches of up to kSmallTenants, workgroups by vocabulary.
 struct SmallPlan {
   std::vector<TokSmallSet> sets;
@@ -1228,7 +1231,7 @@ jn_status small_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
   };
   int32_t most = 1;
   for (const TokEntry& e : io) most = std::max(most, e.n);
-  P->ldz = most > 32 ? 64 : most > 16 ? 32 : 16;
+  P->ldz = small_ldz(most);
   P->f32 = io[0].f32;
   P->inv = take(4 * (int64_t)G);
   std::vector<TokDesc> desc(G);
@@ -1352,9 +1355,15 @@ jn_status split_tokens(jn_ctx* c, int32_t d, const jn_token_head* heads, const s
                        char* ws, TokSplit* P) {
   // Few rows in every tenant: two launches that stream.  A tenant with more brings
   // the others' along at little cost (126 and 63 rows of 865 x 1,024: 46 us by both
-  // paths, 25 by one).
-  bool big = false;
-  for (const TokEntry& e : io) big = big || e.n > tok_small_rows(d);
+  // paths, 25 by one).  The streaming launches keep all logits in fp32, and where
+  // a row gradient is asked for their gradients in bf16: up to a piece's bytes.
+  int32_t most = 1;
+  for (const TokEntry& e : io) most = std::max(most, e.n);
+  int64_t kept = 0;
+  if (train)
+    for (size_t g = 0; g < io.size(); ++g)
+      if (io[g].n > 0) kept += (io[g].dh ? 6ll : 4ll) * heads[g].vocab * small_ldz(most);
+  const bool big = most > tok_small_rows(d) || kept > kTokPieceBytes;
   for (size_t g = 0; g < io.size(); ++g) {
     if (io[g].n == 0 && !train) continue;
     (big ? P->heads : P->small_heads).push_back(heads[g]);

@@ -40,6 +40,10 @@ def test_sizes_of_workspaces(lib):
     # one piece (up to a whole round of tiles more: 65,536 columns here would be; 256 it is below a round), 8 bytes a
     # part of 128 columns, and the rows
     assert n < (1 << 30) * 1.05 + 8 * 20000 * (120001 / 64 + 8) + 20000 * 64 * 8 + (1 << 20)
+    # tenants of few rows keep whole logits only up to a piece: 40 of them, 64 rows of 120,001 each
+    few = [lib.TokenIO(i32(64), i32(64), torch.zeros(64), torch.zeros(1), big.W, bf(64, 64)) for _ in range(40)]
+    assert lib.jn_tokens_workspace_size([big] * 20, few[:20]) < (1 << 30) * 1.05
+    assert lib.jn_tokens_workspace_size([big] * 40, few) < (1 << 30) * 1.35
     pick = lib.TokenPick(i32(3), i32(3), torch.zeros(3))
     assert lib.jn_tokens_decode_workspace_size([small], [pick]) < 1 << 16
     with pytest.raises(lib.JNError):

@@ -125,6 +125,15 @@ def test_pieces_of_the_vocabulary(lib, margin):
         t.check(hidden, margin)
 
 
+def test_few_rows_of_a_vocabulary_beyond_a_piece(lib):
+    """33 rows whose logits in fp32 are more than the workspace may hold: not the streaming launches."""
+    hidden = feature(40, 64)
+    t = Tenant(lib, *draw(33, 4300001, 64, 40, 38), True)
+    assert lib.jn_tokens_workspace_size([t.head], [t.io]) < 1 << 30
+    step(lib, lib.Context(), hidden, [t])
+    t.check(hidden)
+
+
 @pytest.mark.parametrize("case", [(1, 300, 64), (7, 256, 768), (50, 777, 2176), (300, 1003, 320), (2048, 4096, 512)],
                          ids=lambda c: "-".join(map(str, c)))
 def test_fp32_weight_gradients(lib, case):
