@@ -18,8 +18,12 @@ __device__ __forceinline__ uint32_t pack_bf2(float lo, float hi) {
   return (uint32_t)f2bf(lo) | ((uint32_t)f2bf(hi) << 16);
 }
 
-// The same by one instruction (pack_bf2 takes three).
-__device__ __forceinline__ uint32_t cvt_bf2(float lo, float hi) {
+// Two floats -> two bf16 (round to nearest even) by one v_cvt_pk_bf16_f32;
+// pack_bf2 converts each value alone and merges them with a shift and an
+// OR.  Same bits.  Not in the staged epilogue of the QKV kernel: there the packed
+// form changed the register allocation of the main loop (operand fragments moved
+// through the accumulation registers, 16% slower).
+__device__ __forceinline__ uint32_t pack_bf2_cvt(float lo, float hi) {
   typedef float f2 __attribute__((ext_vector_type(2)));
   typedef __bf16 b2 __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{lo, hi}, b2));

@@ -97,17 +97,6 @@ __device__ __forceinline__ const uint16_t* weight_row(const uint16_t* W, const u
   }
 }
 
-// Two floats -> two bf16 (round to nearest even) by one v_cvt_pk_bf16_f32;
-// pack_bf2 converts each value alone and merges them with a shift and an
-// OR.  Same bits.  Used in the GeGLU epilogue only: in the QKV kernel's staged
-// epilogue the packed form changed the register allocation of the main loop
-// (operand fragments moved through the accumulation registers, 16% slower).
-typedef float gemm_f32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 gemm_bf16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t pack_bf2_cvt(float lo, float hi) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(gemm_f32x2{lo, hi}, gemm_bf16x2));
-}
-
 // Largest divisor of `rows` that is at most `most`.
 constexpr int row_batch(int rows, int most) {
   int b = most < rows ? most : rows;
@@ -247,8 +236,10 @@ __device__ __forceinline__ void epilogue_bf16(const GemmArgs& g, const f32x4 (&a
           }
         }
         const int chunk = 2 * (GLU ? i / 2 : i) + (quad >> 1);
-        *reinterpret_cast<u32x2*>(stage + (16 * jj + row) * WC + (chunk ^ swz(row)) * 8 + (quad & 1) * 4) =
-            u32x2{pack_bf2_cvt(v[0], v[1]), pack_bf2_cvt(v[2], v[3])};
+        u32x2 two{pack_bf2_cvt(v[0], v[1]), pack_bf2_cvt(v[2], v[3])};
+        if constexpr (EPI == EPI_DLOGIT)  // (no target: zeros also where W is not finite)
+          if (lse[j + jj] == INFINITY) two = u32x2{0u, 0u};
+        *reinterpret_cast<u32x2*>(stage + (16 * jj + row) * WC + (chunk ^ swz(row)) * 8 + (quad & 1) * 4) = two;
       }
       if constexpr (EPI == EPI_DLOGIT) {  // (behind the lane's own write of that column: a wave's LDS operations stay in order)
         const int32_t k = own[j + jj];

@@ -758,6 +758,10 @@ __global__ __launch_bounds__(256) void tok_grad_kernel(const TokDesc* __restrict
     if (c >= d.kept_n8) return;
     const TokRow row = rows[i];
     uint4* const at = reinterpret_cast<uint4*>(d.keep) + (int64_t)n * d.kept_n8 + c;
+    if (row.label < 0) {  // (whatever W made of the zeros in its place)
+      *at = make_uint4(0, 0, 0, 0);
+      return;
+    }
     const int32_t v0 = 8 * c;
     const float m = d.part[(int64_t)(v0 / d.width) * d.n + n].m;
     // (a block without a column has m = -inf and zeros)
@@ -971,7 +975,7 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_scores_kernel(TokSmall
         m = z;
         at = v;
       } else {
-        rest += e;
+        rest += z == -INFINITY ? 0.f : e;  // (as the first of a thread's values: e = NaN)
       }
     }
     buf ^= 1;
@@ -1212,9 +1216,9 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_grads_kernel(TokSmallA
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
         p[t] = __builtin_amdgcn_exp2f(fmaf(p[t], kLog2e, -l2[t]));
-        p[t] = lb[t] == v ? ow[t] : p[t];
+        p[t] = lb[t] == v ? ow[t] : l2[t] == INFINITY ? 0.f : p[t];  // (also where W is not finite)
       }
-      const uint4 g = make_uint4(cvt_bf2(p[0], p[1]), cvt_bf2(p[2], p[3]), cvt_bf2(p[4], p[5]), cvt_bf2(p[6], p[7]));
+      const uint4 g = make_uint4(pack_bf2_cvt(p[0], p[1]), pack_bf2_cvt(p[2], p[3]), pack_bf2_cvt(p[4], p[5]), pack_bf2_cvt(p[6], p[7]));
       *reinterpret_cast<uint4*>(line + r * LD + 8 * tg) = g;
       if (d.grad && blockIdx.y == 0 && v < V && 8 * tg < ldz)
         *reinterpret_cast<uint4*>(d.grad + (int64_t)v * ldz + 8 * tg) = g;
@@ -1246,8 +1250,8 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_grads_kernel(TokSmallA
               mine16[col * 16 + (chunk ^ col)] = __builtin_bit_cast(u32x4t, f32x4h{a[0][e] * inv, a[1][e] * inv, a[2][e] * inv, a[3][e] * inv});
               mine16[col * 16 + ((chunk + 1) ^ col)] = __builtin_bit_cast(u32x4t, f32x4h{a[4][e] * inv, a[5][e] * inv, a[6][e] * inv, a[7][e] * inv});
             } else {
-              mine16[col * 16 + (chunk ^ col)] = u32x4t{cvt_bf2(a[0][e] * inv, a[1][e] * inv), cvt_bf2(a[2][e] * inv, a[3][e] * inv),
-                                                        cvt_bf2(a[4][e] * inv, a[5][e] * inv), cvt_bf2(a[6][e] * inv, a[7][e] * inv)};
+              mine16[col * 16 + (chunk ^ col)] = u32x4t{pack_bf2_cvt(a[0][e] * inv, a[1][e] * inv), pack_bf2_cvt(a[2][e] * inv, a[3][e] * inv),
+                                                        pack_bf2_cvt(a[4][e] * inv, a[5][e] * inv), pack_bf2_cvt(a[6][e] * inv, a[7][e] * inv)};
             }
           }
           __builtin_amdgcn_wave_barrier();  // (a wave's LDS operations stay in order)

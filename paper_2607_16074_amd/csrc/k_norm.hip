@@ -324,7 +324,7 @@ __device__ __forceinline__ void put_bf(uint16_t* p, const float* v) {
   typedef uint32_t V __attribute__((ext_vector_type(E / 2)));
   V r;
 #pragma unroll
-  for (int k = 0; k < E / 2; ++k) r[k] = cvt_bf2(v[2 * k], v[2 * k + 1]);
+  for (int k = 0; k < E / 2; ++k) r[k] = pack_bf2_cvt(v[2 * k], v[2 * k + 1]);
   if constexpr (ONCE)
     __builtin_nontemporal_store(r, reinterpret_cast<V*>(p));
   else
@@ -606,7 +606,9 @@ hipError_t launch_qk_fwd(hipStream_t s, const QkShape& a, const uint16_t* x, uin
   });
 }
 
-int32_t qk_bwd_blocks(int32_t rows) { return std::min((rows + 3) / 4, kQkBwdBlocks); }
+int32_t qk_bwd_blocks(int32_t rows) {
+  return (int32_t)std::min<int64_t>(((int64_t)rows + 3) / 4, kQkBwdBlocks);
+}
 
 hipError_t launch_qk_bwd(hipStream_t s, const QkShape& a, const uint16_t* x, const uint16_t* dy, uint16_t* dx,
                          float* part, float* dgq, float* dgk) {

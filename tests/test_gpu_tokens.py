@@ -251,6 +251,51 @@ def test_nan_of_a_target_is_not_hidden(lib):
     assert bad.tolist() == [False, False, True, False, False, False] and bool(t.loss[:1].isnan())
 
 
+@pytest.mark.parametrize("n", [3, 40, 200])
+def test_a_token_of_no_probability(lib, n):
+    """Logits of -inf (a row of W of -inf where the feature is positive, else 0): as if the vocabulary held no such token."""
+    d, v, ban = 128, 600, 0
+    hidden = feature(n, d)
+    hidden[:, 0] = 1.0
+    W, rows, targets = draw(n, v, d, n, 36)
+    targets.clamp_(min=1)
+    W[ban] = 0.0
+    W[ban, 0] = float("-inf")
+    t = Tenant(lib, W, rows, targets, False)
+    step(lib, lib.Context(), hidden, [t])
+    assert bool((t.dW[:d] == 0).all())
+    rest = Tenant(lib, W[1:].contiguous(), rows, targets - 1, False)
+    rest.logp.copy_(t.logp)
+    rest.loss.copy_(t.loss)
+    rest.dW.copy_(t.dW[d:])
+    rest.check(hidden)
+    pick = Pick(lib, W, rows)
+    decode(lib, lib.Context(), hidden, [pick])
+    assert bool((pick.token[:n] != ban).all()) and bool(torch.isfinite(pick.logp[:n]).all())
+
+
+@pytest.mark.parametrize("n,v,ban", [(5, 600, 0), (64, 600, 300), (200, 600, 1), (2000, 300007, 3), (2000, 300007, 300001)])
+def test_a_token_of_no_probability_and_rows_without_a_target(lib, n, v, ban):
+    """As above; an entry without a target meets the infinity with nothing and gets no gradient."""
+    d = 64
+    hidden = feature(n, d)
+    hidden[:, 0] = 1.0
+    W, rows, targets = draw(n, v, d, n, 37)
+    targets[targets == ban] = 7
+    rows[1], targets[2], rows[n - 1] = -1, -1, n
+    W[ban] = 0.0
+    W[ban, 0] = float("-inf")
+    t = Tenant(lib, W, rows, targets, False)
+    step(lib, lib.Context(), hidden, [t])
+    assert bool((t.dW[ban * d: (ban + 1) * d] == 0).all())
+    keep = torch.arange(v, device="cuda") != ban
+    rest = Tenant(lib, W[keep], rows, torch.where(targets > ban, targets - 1, targets), False)
+    rest.logp.copy_(t.logp)
+    rest.loss.copy_(t.loss)
+    rest.dW.copy_(torch.cat([t.dW[: v * d].view(v, d)[keep].reshape(-1), t.dW[v * d:]]))
+    rest.check(hidden)
+
+
 def test_same_bits_twice_and_on_another_stream(lib):
     hidden = feature(800, 256)
     a = Tenant(lib, *draw(500, 3001, 256, 800, 35), True)
