@@ -299,7 +299,7 @@ jn_status jn_backbone_forward(jn_ctx* ctx, const jn_backbone* bb, const jn_packe
  * are 16-byte aligned and rows a multiple of 8 elements apart (JN_EUNSUPPORTED).
  * rows may be 0. */
 typedef struct jn_qk_args {
-  int32_t rows, n_heads, n_kv_heads, head_dim;
+  int32_t rows, n_heads, n_kv_heads, head_dim;   /* rows < 2^26 - 3 */
   int64_t ld_in;           /* elements between rows of the projection x */
   int64_t ld_out;          /* elements between rows of y and of dy      */
   int64_t ld_grad;         /* elements between rows of dx (jn_qk_norm_rope_bwd) */

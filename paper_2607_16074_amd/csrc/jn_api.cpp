@@ -807,7 +807,7 @@ jn_status qk_shape(jn_ctx* c, const jn_qk_args* a, bool back, QkShape* q) {
     return fail(c, JN_EUNSUPPORTED, "head_dim %d not a multiple of 16 in [16, 256]", a->head_dim);
   const int64_t heads = (int64_t)a->n_heads + a->n_kv_heads, width = heads * a->head_dim;
   if (heads > 65536) return fail(c, JN_ESHAPE, "%lld heads", (long long)heads);
-  if (a->rows >= (1 << 28)) return fail(c, JN_ESHAPE, "%d rows exceed one launch's grid", a->rows);
+  if (a->rows > (1 << 26) - 4) return fail(c, JN_ESHAPE, "%d rows exceed one launch's grid", a->rows);
   const bool reads = !back || a->gq != nullptr;  // x
   const int64_t ld_in = reads ? a->ld_in : width, ld_grad = back ? a->ld_grad : width;
   if (std::min({ld_in, a->ld_out, ld_grad}) < width)

@@ -85,6 +85,7 @@ void check_qk(jn_ctx* c) {
       CHECK(jn_qk_norm_rope_bwd(c, &b, at(3), at(4), at(7), (float*)at(5), (float*)at(6), at(8), 1u << 30) == want);
     };
     refused(JN_EINVAL, [](jn_qk_args& b) { b.rows = -1; });
+    refused(JN_ESHAPE, [](jn_qk_args& b) { b.rows = (1 << 26) - 3; });  // 2^32 threads in one launch
     refused(JN_EINVAL, [](jn_qk_args& b) { b.n_heads = b.n_kv_heads = 0; });
     refused(JN_EUNSUPPORTED, [](jn_qk_args& b) { b.head_dim += 8; });
     refused(JN_EUNSUPPORTED, [](jn_qk_args& b) { b.head_dim = 272; });
