@@ -960,8 +960,9 @@ jn_status check_tokens(jn_ctx* c, int32_t d, const jn_token_head* heads, const s
 
 // K ranges of the row gradients' products: with few rows their tiles leave most
 // CUs idle for as long as the vocabulary is.  Ranges of 512 columns at least; the
-// planes' sum reads 4 bytes an element and plane at the copy rate (4.8 TB/s).
-constexpr int32_t kTokMostRanges = 16;
+// planes' sum reads 4 bytes an element and plane at the copy rate (4.8 TB/s).  100
+// rows, 100,000 x 128: up to 8 ranges 138 us, 16 96, 32 75, 64 66.
+constexpr int32_t kTokRanges[] = {1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15, 16, 20, 24, 28, 32, 40, 48, 64};
 int64_t range_columns(int64_t cols, int32_t S) { return std::max<int64_t>(512, up((cols + S - 1) / S, 64)); }
 
 jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std::vector<TokEntry>& io, bool train,
@@ -1103,7 +1104,7 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
   int32_t S = 1;
   if (dh) {
     double best = 1e300;
-    for (int32_t t = 1; t <= kTokMostRanges; ++t) {
+    for (const int32_t t : kTokRanges) {
       std::vector<GemmArgs> v;
       for (int32_t g = 0; g < G; ++g) {
         if (io[g].n == 0 || !io[g].dh) continue;
@@ -1351,19 +1352,40 @@ struct TokSplit {
   size_t total = 0;
 };
 
-jn_status split_tokens(jn_ctx* c, int32_t d, const jn_token_head* heads, const std::vector<TokEntry>& io, bool train,
-                       char* ws, TokSplit* P) {
-  // Few rows in every tenant: two launches that stream.  A tenant with more brings
-  // the others' along at little cost (126 and 63 rows of 865 x 1,024: 46 us by both
-  // paths, 25 by one).  The streaming launches keep all logits in fp32, and where
-  // a row gradient is asked for their gradients in bf16: up to a piece's bytes.
+// Few rows in every tenant: launches that stream W, two without row gradients
+// (else five).  A tenant with more rows brings the others' along at little cost
+// (126 and 63 rows of 865 x 1,024: 46 us by both paths, 25 by one).  Training, the
+// streaming launches keep all logits in fp32, and with row gradients their
+// gradients in bf16: up to a piece's bytes.  Where W is small, latencies decide, and
+// the products' tiles work on more rows at a time.  Streaming and not, one tenant,
+// us, without row gradients: 32 rows of 4,000 x 768 21.2 and 23.7, of 120,000 x 2,048
+// 219 and 315; 64 rows of 256 x 2,048 22.9 and 25.4, 4,000 x 2,048 37.3 and 30.3,
+// 32,003 x 768 49.9 and 49.7, x 2,048 86 and 94.  With: 32 rows of 32,003 x 128
+// 41.0 and 34.3, 120,000 x 128 55.6 and 63.1, 32,003 x 2,048 114 and 119; 64 rows of
+// that 133 and 126, 120,000 x 768 159 and 165.  Decoding, 1 row of 1,024 x 768 11.7
+// and 14.5, 64 of 32,003 x 2,048 44.5 and 48.8.
+bool tokens_stream(int32_t d, const jn_token_head* heads, const std::vector<TokEntry>& io, bool train) {
   int32_t most = 1;
   for (const TokEntry& e : io) most = std::max(most, e.n);
-  int64_t kept = 0;
-  if (train)
-    for (size_t g = 0; g < io.size(); ++g)
-      if (io[g].n > 0) kept += (io[g].dh ? 6ll : 4ll) * heads[g].vocab * small_ldz(most);
-  const bool big = most > tok_small_rows(d) || kept > kTokPieceBytes;
+  if (most > tok_small_rows(d)) return false;
+  if (!train) return true;
+  int64_t kept = 0, elements = 0;
+  bool dh = false;
+  for (size_t g = 0; g < io.size(); ++g) {
+    if (io[g].n == 0) continue;
+    kept += (io[g].dh ? 6ll : 4ll) * heads[g].vocab * small_ldz(most);
+    elements += (int64_t)heads[g].vocab * d;
+    dh = dh || io[g].dh;
+  }
+  if (kept > kTokPieceBytes) return false;
+  const bool few = most <= 32;
+  if (dh) return elements > (few ? 3 << 22 : 1 << 26);
+  return few || elements <= 1 << 20 || elements > 3 << 22;
+}
+
+jn_status split_tokens(jn_ctx* c, int32_t d, const jn_token_head* heads, const std::vector<TokEntry>& io, bool train,
+                       char* ws, TokSplit* P) {
+  const bool big = !tokens_stream(d, heads, io, train);
   for (size_t g = 0; g < io.size(); ++g) {
     if (io[g].n == 0 && !train) continue;
     (big ? P->heads : P->small_heads).push_back(heads[g]);

@@ -1755,7 +1755,9 @@ __global__ __launch_bounds__(256, 2) void gemm_tokens_pair_kernel(const GemmArgs
 // owns tiles [x per, (x + 1) per)), else the walk of the other grouped launches.
 // With few token tiles (the fast index) a weight panel is then fetched by one XCD,
 // not by as many as there are token tiles: row gradients of 701 targets, 32,003
-// columns of 2,048, 117 -> 80 us.
+// columns of 2,048, 117 -> 80 us.  Calls of 32,003 x 2,048 with 3 token tiles 360 ->
+// 326 us, 7 754 -> 650, 8 747 -> 715, 12 and 16 the same; 32 token tiles of 160,001 x
+// 2,048 14.4 -> 15.3 ms.
 template <int EPI, int TR>
 __global__ __launch_bounds__(256, 1) void gemm_tokens_ring_kernel(const GemmArgs* __restrict__ probs, int32_t nprob,
                                                                   int32_t total, int32_t chain, bool near) {
@@ -1774,7 +1776,7 @@ __global__ __launch_bounds__(256, 1) void gemm_tokens_ring_kernel(const GemmArgs
   };
   ring_run<EPI, TR>(next, lds);
 }
-constexpr int32_t kFewTokenTiles = 7;
+constexpr int32_t kFewTokenTiles = 16;
 
 template <int EPI, int TR>
 static hipError_t launch_tokens(hipStream_t s, const GemmArgs* p, int32_t n, const TokTiles& t) {

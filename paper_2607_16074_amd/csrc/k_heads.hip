@@ -805,7 +805,8 @@ hipError_t launch_tok_grad(hipStream_t s, const TokDesc* d, int32_t G, int32_t N
 }
 
 // Eight elements of dh per STR lanes, which share the planes (many planes are those
-// of few rows) and are added in pairs.
+// of few rows) and are added in pairs: 60 rows, 120,000 x 128 110 -> 76 us a call, 5
+// rows, 60,000 x 2,048 163 -> 159; 701 rows of 10 planes, 32,003 x 2,048 330 -> 339.
 template <int STR>
 __global__ __launch_bounds__(256) void tok_rows_kernel(const TokDesc* __restrict__ desc, int32_t G, int32_t N,
                                                        const float* __restrict__ inv, const float4* __restrict__ acc,

@@ -125,6 +125,28 @@ def test_pieces_of_the_vocabulary(lib, margin):
         t.check(hidden, margin)
 
 
+@pytest.mark.parametrize("case", [(5, 100001, 128), (32, 20003, 1024), (40, 35003, 2048), (33, 600011, 128),
+                                  (16, 1601, 8192), (17, 3203, 4160), (1, 197003, 64)], ids=lambda c: "-".join(map(str, c)))
+def test_row_gradients_of_few_rows_and_large_heads(lib, case):
+    """Row gradients behind the streaming launches, at both of their row counts and every width."""
+    n, v, d = case
+    hidden = feature(n + 3, d)
+    t = Tenant(lib, *draw(n, v, d, n + 3, 41), True)
+    if n > 2:
+        t.rows[1], t.targets[2] = -1, v
+    step(lib, lib.Context(), hidden, [t])
+    t.check(hidden)
+
+
+def test_row_gradients_of_few_rows_and_many_heads(lib):
+    hidden = feature(50, 192)
+    ts = [Tenant(lib, *draw(n, v, 192, 50, 42 + k), dh)
+          for k, (n, v, dh) in enumerate([(9, 40003, True), (0, 77, True), (31, 30001, False), (1, 1, True), (16, 9001, True)])]
+    step(lib, lib.Context(), hidden, ts)
+    for t in ts:
+        t.check(hidden)
+
+
 def test_few_rows_of_a_vocabulary_beyond_a_piece(lib):
     """33 rows whose logits in fp32 are more than the workspace may hold: not the streaming launches."""
     hidden = feature(40, 64)
