@@ -985,7 +985,7 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
     logits += (int64_t)io[g].n * up(heads[g].vocab, 64);
     dh = dh || (io[g].dh != nullptr && io[g].n > 0);
     if (train && io[g].n == 0) {
-      desc[g].zero = (uint16_t*)io[g].dW;
+      desc[g].keep = (uint16_t*)io[g].dW;
       desc[g].zero_n8 = (int64_t)heads[g].vocab * d / (io[g].f32 ? 4 : 8);
       P->zero8 += desc[g].zero_n8;
     }
@@ -1056,8 +1056,7 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
         if (k == 0) {
           desc[g].keep = (uint16_t*)(ws + P->piece + pat[g]);
           desc[g].kept = (int32_t)cols;
-          desc[g].kept_n8 = (int32_t)(up(cols, 64) / 8);
-          P->grad_blocks += io[g].n * ((desc[g].kept_n8 + 255) / 256);
+          P->grad_blocks += io[g].n * ((desc[g].kept_n8() + 255) / 256);
           q.C = desc[g].keep;
           q.ldc = up(cols, 64);
         }

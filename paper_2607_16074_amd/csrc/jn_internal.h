@@ -314,14 +314,16 @@ struct TokDesc {
   uint16_t* dh;            // [n][d] or null
   const TokPart* part;     // [blocks][n]
   const int32_t* index;    // [blocks][n], decoding
-  uint16_t* keep;          // [n][8 kept_n8]
-  uint16_t* zero;          // dW of a tenant without entries, else null
-  int64_t zero_n8;         // its 16-byte groups
+  uint16_t* keep;          // [n][8 kept_n8()]; a tenant without entries: its dW, to be cleared
+  int64_t zero_n8;         // 16-byte groups of that, else 0
   int32_t n, first, vocab, blocks;
-  int32_t kept, width, kept_n8;
-  int32_t grad_block;      // first workgroup of launch_tok_grad, ceil(kept_n8 / 256) to an entry
-  int32_t planes, reserved;  // of dh
+  int32_t kept, width;
+  int32_t grad_block;      // first workgroup of launch_tok_grad, ceil(kept_n8() / 256) to an entry
+  int32_t planes;          // of dh
+  __host__ __device__ int32_t kept_n8() const { return (kept + 63) / 64 * 8; }
 };
+// (eight tenants' descriptors and problems, with row gradients, in one launch's arguments: kTableBytes)
+static_assert(8 * sizeof(TokDesc) + 24 * sizeof(GemmArgs) <= 4000, "token tables");
 // The call's table at `dst` (G descriptors, then the problems), h[i] = hidden[row
 // of target i], zeros where it has none; labels[i] its token or -1 (decoding: 0
 // where the row exists); inv[g] = 1 / targets of tenant g.  The table travels by

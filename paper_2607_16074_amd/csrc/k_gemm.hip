@@ -1726,7 +1726,7 @@ __global__ __launch_bounds__(256, OCC) void gemm_tokens_flex_kernel(const GemmAr
 
 // Row gradients (128x96 tiles, GEMM_TRANS_W) and weight gradients (128x128, both
 // operands transposed) of a call in one launch, two workgroups a CU: eight tenants,
-// 2,003 targets, 2,049 x 768 61 us a call (65 with one a CU and a stage more of the
+// 2,003 targets, 2,049 x 768 61 us a call then (65 with one a CU and a stage more of the
 // 128x96 tiles, 69 as two launches); 900 targets, 8,000 x 768 131 (144 as two); one
 // tenant, 80, 160,000 x 1,024 306 (334); 100, 100,000 x 768 176 (180).
 template <int EPI, int WEPI>

@@ -574,8 +574,8 @@ __device__ __forceinline__ int32_t tok_tenant(const TokDesc* __restrict__ d, int
 // feature holds there, so that nothing behind this reads them.  The G workgroups
 // behind them count the targets of a tenant each, the last one lays the table
 // down.  BYVAL: the descriptors are at the start of the table's bytes, else
-// (larger tables, laid down before) in device memory.
-constexpr size_t kTableBytes = 3584;
+// (larger tables, laid down before, another launch) in device memory.
+constexpr size_t kTableBytes = 4000;  // a launch's arguments hold 4 KB
 struct alignas(16) TokTable {
   uint32_t w[kTableBytes / 4];
 };
@@ -753,11 +753,11 @@ __global__ __launch_bounds__(256) void tok_grad_kernel(const TokDesc* __restrict
       if (desc[mid].grad_block <= b) lo = mid; else hi = mid - 1;
     }
     const TokDesc& d = desc[lo];
-    const int32_t per = (d.kept_n8 + 255) / 256, n = (b - d.grad_block) / per, i = d.first + n;
+    const int32_t per = (d.kept_n8() + 255) / 256, n = (b - d.grad_block) / per, i = d.first + n;
     const int32_t c = (b - d.grad_block - n * per) * 256 + threadIdx.x;
-    if (c >= d.kept_n8) return;
+    if (c >= d.kept_n8()) return;
     const TokRow row = rows[i];
-    uint4* const at = reinterpret_cast<uint4*>(d.keep) + (int64_t)n * d.kept_n8 + c;
+    uint4* const at = reinterpret_cast<uint4*>(d.keep) + (int64_t)n * d.kept_n8() + c;
     if (row.label < 0) {  // (whatever W made of the zeros in its place)
       *at = make_uint4(0, 0, 0, 0);
       return;
@@ -792,9 +792,9 @@ __global__ __launch_bounds__(256) void tok_grad_kernel(const TokDesc* __restrict
     return;
   }
   for (int32_t g = 0; g < G; ++g)
-    if (desc[g].zero)
+    if (desc[g].zero_n8 > 0)
       for (int64_t e = (int64_t)(b - G) * 256 + threadIdx.x; e < desc[g].zero_n8; e += (int64_t)zeros * 256)
-        reinterpret_cast<uint4*>(desc[g].zero)[e] = make_uint4(0, 0, 0, 0);
+        reinterpret_cast<uint4*>(desc[g].keep)[e] = make_uint4(0, 0, 0, 0);
 }
 
 hipError_t launch_tok_grad(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const float* inv, const TokRow* rows,
