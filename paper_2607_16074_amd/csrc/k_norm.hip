@@ -431,12 +431,14 @@ __global__ __launch_bounds__(256) void qk_fwd_kernel(QkShape a, const uint16_t* 
 
 // Workgroups walk rows in steps of the grid; each leaves its sums of du xh in
 // part [workgroup][2][hd], queries then keys, which qk_gain_kernel adds in
-// order.  dx may be the rows of x or of dy.
-template <int E, int P2, bool NORM, bool ROPE, bool ONCE>
-__global__ __launch_bounds__(256, 4) void qk_bwd_kernel(QkShape a, const uint16_t* x, const uint16_t* dy,
-                                                     uint16_t* dx, float* __restrict__ part) {
-  __shared__ __attribute__((aligned(16))) float lines[4][256];
-  __shared__ float sums[NORM ? 4 : 1][2][256];
+// order.  dx may be the rows of x or of dy.  With few rows (qk_one) one
+// workgroup of 16 wavefronts takes them all, and its sums are the gradients.
+template <int E, int P2, bool NORM, bool ROPE, bool ONCE, int W>
+__global__ __launch_bounds__(64 * W, 4) void qk_bwd_kernel(QkShape a, const uint16_t* x, const uint16_t* dy,
+                                                        uint16_t* dx, float* __restrict__ part,
+                                                        float* __restrict__ dgq, float* __restrict__ dgk) {
+  __shared__ __attribute__((aligned(16))) float lines[W][256];
+  __shared__ float sums[NORM ? W : 1][2][256];
   constexpr int PER = 64 / P2, STEP = 2;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane % P2, slot = lane / P2;
   const int heads = a.heads + a.kv, half = a.hd >> 1, steps = (heads + PER - 1) / PER;
@@ -453,7 +455,7 @@ __global__ __launch_bounds__(256, 4) void qk_bwd_kernel(QkShape a, const uint16_
   const float* const line = lines[w] + (live ? E * q : 0);
   const uint32_t mine = slot * a.hd + E * q;
   const float part_of = 1.f / (float)a.hd;
-  for (int64_t row = (int64_t)blockIdx.x * 4 + w; row < a.rows; row += (int64_t)gridDim.x * 4) {
+  for (int64_t row = (int64_t)blockIdx.x * W + w; row < a.rows; row += (int64_t)gridDim.x * W) {
     const uint16_t* const xr = x + row * a.ldx;
     const uint16_t* const yr = dy + row * a.ldy;
     uint16_t* const dr = dx + row * a.ldd;
@@ -542,9 +544,16 @@ __global__ __launch_bounds__(256, 4) void qk_bwd_kernel(QkShape a, const uint16_
         if (slot == 0 && live) sums[w][k][E * q + (i < E ? i : half + i - E)] = v;
       }
     __syncthreads();
-    for (int e = threadIdx.x; e < 2 * a.hd; e += 256) {
+    for (int e = threadIdx.x; e < 2 * a.hd; e += 64 * W) {
       const int k = e >= a.hd, c = e - k * a.hd;
-      part[(int64_t)blockIdx.x * 2 * a.hd + e] = (sums[0][k][c] + sums[1][k][c]) + (sums[2][k][c] + sums[3][k][c]);
+      float v = 0.f;
+#pragma unroll
+      for (int i = 0; i < W; i += 4)
+        v += (sums[i][k][c] + sums[i + 1][k][c]) + (sums[i + 2][k][c] + sums[i + 3][k][c]);
+      if constexpr (W == 4)
+        part[(int64_t)blockIdx.x * 2 * a.hd + e] = v;
+      else
+        (k ? dgk : dgq)[c] = v;
     }
   }
 }
@@ -570,6 +579,14 @@ __global__ __launch_bounds__(1024) void qk_gain_kernel(const float* __restrict__
   }
 }
 
+// Whether the rows written are past the last-level cache.
+static bool qk_streams(const QkShape& a) { return (int64_t)a.rows * (a.heads + a.kv) * a.hd * 2 > kStreamBytes; }
+
+// Gradients of few rows by one workgroup: one launch instead of two, on one CU.  18
+// heads of 128: 1 and 8 rows 9.4 -> 6.9 us a call, 16 (37 k elements) 9.3 -> 8.7,
+// 24 9.4 -> 10.5; 16 heads of 256: 8 rows (33 k) 10.1 -> 9.1, 16 10.1 -> 12.4.
+static bool qk_one(const QkShape& a) { return (int64_t)a.rows * (a.heads + a.kv) * a.hd <= 1 << 15; }
+
 // Calls f<P2, NORM, ROPE, ONCE>() for the shape, with E elements of both halves a lane.
 template <int E, typename F>
 static hipError_t with_qk(const QkShape& a, F&& f) {
@@ -580,8 +597,7 @@ static hipError_t with_qk(const QkShape& a, F&& f) {
     return f(p2, std::false_type(), std::true_type(), once);
   };
   auto go = [&](auto p2) {
-    return (int64_t)a.rows * (a.heads + a.kv) * a.hd * 2 > kStreamBytes ? kind(p2, std::true_type())
-                                                                        : kind(p2, std::false_type());
+    return qk_streams(a) ? kind(p2, std::true_type()) : kind(p2, std::false_type());
   };
   constexpr int M = 16 / E;  // lanes of 32 elements
   if (a.hd <= 32) return go(std::integral_constant<int, M>());
@@ -616,10 +632,17 @@ hipError_t launch_qk_bwd(hipStream_t s, const QkShape& a, const uint16_t* x, con
   if (a.rows > 0) {
     if (!qk_ok(a)) return hipErrorInvalidValue;
     const hipError_t e = with_qk<kQkBwdE>(a, [&](auto p2, auto norm, auto rope, auto once) {
-      qk_bwd_kernel<kQkBwdE, p2(), norm(), rope(), once()><<<blocks, 256, 0, s>>>(a, x, dy, dx, part);
+      if constexpr (norm() && !once()) {
+        if (qk_one(a)) {
+          qk_bwd_kernel<kQkBwdE, p2(), norm(), rope(), once(), 16><<<1, 1024, 0, s>>>(a, x, dy, dx, part, dgq, dgk);
+          return hipGetLastError();
+        }
+      }
+      qk_bwd_kernel<kQkBwdE, p2(), norm(), rope(), once(), 4><<<blocks, 256, 0, s>>>(a, x, dy, dx, part, dgq, dgk);
       return hipGetLastError();
     });
     if (e != hipSuccess) return e;
+    if (a.gq && qk_one(a)) return hipSuccess;
   }
   if (!a.gq) return hipSuccess;
   qk_gain_kernel<<<2 * a.hd / 16, 1024, 0, s>>>(part, blocks, a.hd, dgq, dgk);
