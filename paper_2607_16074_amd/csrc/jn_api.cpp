@@ -992,15 +992,18 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
   }
   P->N = (int32_t)N;
   // pieces of the vocabulary, as many for every tenant, in whole ring tiles
-  const int64_t K = std::max<int64_t>(1, (2 * logits + kTokPieceBytes - 1) / kTokPieceBytes);
+  // (the same share of every tenant's vocabulary, as large as the kept piece may be:
+  // the columns behind it are formed twice; 8,192 rows of 70,000 x 1,024 3,680 us with
+  // halves, 3,506 so; 5,000 of 120,000 x 128, whose products are short, 1,637 and 1,685)
+  const double share = std::min(1.0, (double)kTokPieceBytes / (2.0 * std::max<int64_t>(logits, 1)));
   int64_t piece = 0, pieces = 0;
   for (int32_t g = 0; g < G; ++g) {
     if (io[g].n == 0) continue;
     width[g] = heads[g].vocab;
     if (train) {
       // whole rounds of the weight gradient's ring tiles on 256 CUs, where there are some
-      const int64_t round = 256 * std::max(1, 256 / ((d + 255) / 256)), even = up((heads[g].vocab + K - 1) / K, 256);
-      width[g] = std::min<int64_t>(K > 1 && even > round ? up(even, round) : even, up(heads[g].vocab, 64));
+      const int64_t round = 256 * std::max(1, 256 / ((d + 255) / 256)), even = up((int64_t)std::ceil(heads[g].vocab * share), 256);
+      width[g] = std::min<int64_t>(share < 1.0 && even > round ? (even + round / 2) / round * round : even, up(heads[g].vocab, 64));
       const int64_t most = 0x7fffffff / (2 * d) / 256 * 256 - 256;  // a transposed panel of W within 32-bit offsets
       width[g] = std::min(width[g], most);
       pat[g] = piece;
