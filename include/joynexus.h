@@ -501,7 +501,8 @@ typedef struct jn_token_io {
  * Nothing is averaged across tenants.  hidden: device bf16 [T][d], d a multiple of 64
  * in [64, 8192].  Precision: bf16 operands, fp32 accumulation, softmax statistics
  * and loss; the logits' gradient is rounded to bf16 before it meets h and W (as the
- * action experts' are), bf16 results once.  Kernels only: the call may be captured into a HIP graph, whose
+ * action experts' are) or, where every tenant of the call has few entries (the streaming
+ * launches, at most 64), kept as two bf16 that are off by 2^-16 of it; bf16 results once.  Kernels only: the call may be captured into a HIP graph, whose
  * replays read rows, targets, hidden and W as they are then.  A call's results are
  * bitwise reproducible; a tenant's may differ in their last bits with the group it
  * is called in, whose sizes choose the launches' shapes and the pieces.  Errors

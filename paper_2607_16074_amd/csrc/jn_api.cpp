@@ -1291,19 +1291,21 @@ jn_status small_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
       t.zlab = (float*)(ws + take(4 * (int64_t)e.n));
       if (e.n > 0) t.z = (float*)(ws + take(4 * V * P->ldz));
       if (!desc[g0 + k].dh) continue;
-      t.grad = (uint16_t*)(ws + take(2 * V * P->ldz));
+      t.grad = (uint16_t*)(ws + take(4 * V * P->ldz));
     }
     P->sets.push_back(set);
     P->wgs.push_back(wgs);
     P->gwgs.push_back(gwgs);
     P->grad_rows.push_back(grad_rows);
   }
-  // dh = grad^T W over ranges of the vocabulary, as many as fill the CUs
+  // dh = grad^T W over ranges of the vocabulary, as many as fill the CUs, of both
+  // halves of an entry's gradient in one tile (at most 128 rows)
   int64_t tiles = 0, planes = 0;
   for (int32_t g = 0; g < G; ++g)
     if (desc[g].dh) tiles += (d + 127) / 128;
   if (tiles > 0) {
-    const int64_t most_cols = 0x7fffffff / (2 * d) / 256 * 256 - 256;  // a panel of W within 32-bit offsets
+    const int64_t widest = std::max(d, 2 * P->ldz);
+    const int64_t most_cols = 0x7fffffff / (2 * widest) / 256 * 256 - 256;  // panels of W and grad within 32-bit offsets
     for (int32_t g = 0; g < G; ++g) {
       if (!desc[g].dh) continue;
       const int64_t V = heads[g].vocab, S = std::max<int64_t>(1, 2 * kSmallGroups / tiles);
@@ -1313,18 +1315,18 @@ jn_status small_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
       GemmArgs r{};
       r.X = P->sets[g / kSmallTenants].t[g % kSmallTenants].grad;
       r.W = (const uint16_t*)heads[g].W;
-      r.ldx = P->ldz;
+      r.ldx = 2 * P->ldz;
       r.ldw = r.ldc = d;
-      r.M = io[g].n;
+      r.M = 2 * io[g].n;
       r.N = d;
       r.K = (int32_t)V;
       r.krange = (int32_t)step;
       r.ranges = desc[g].planes;
-      r.split_c = N * d;
-      r.aux = (float*)(intptr_t)desc[g].first;  // (until the planes have their place)
+      r.split_c = 2 * N * d;
+      r.aux = (float*)(intptr_t)(2 * desc[g].first);  // (until the planes have their place)
       dx.push_back(r);
     }
-    P->acc = take(4 * planes * N * d);
+    P->acc = take(8 * planes * N * d);
     P->planes = (int32_t)planes;
     for (GemmArgs& r : dx) {
       r.C = (float*)(ws + P->acc) + (intptr_t)r.aux * d;
@@ -1358,7 +1360,7 @@ struct TokSplit {
 // (else five).  A tenant with more rows brings the others' along at little cost
 // (126 and 63 rows of 865 x 1,024: 46 us by both paths, 25 by one).  Training, the
 // streaming launches keep all logits in fp32, and with row gradients their
-// gradients in bf16: up to a piece's bytes.  Where W is small, latencies decide, and
+// gradients as two bf16: up to a piece's bytes.  Where W is small, latencies decide, and
 // the products' tiles work on more rows at a time.  Streaming and not, one tenant,
 // us, without row gradients: 32 rows of 4,000 x 768 21.2 and 23.7, of 120,000 x 2,048
 // 219 and 315; 64 rows of 256 x 2,048 22.9 and 25.4, 4,000 x 2,048 37.3 and 30.3,
@@ -1375,7 +1377,7 @@ bool tokens_stream(int32_t d, const jn_token_head* heads, const std::vector<TokE
   bool dh = false;
   for (size_t g = 0; g < io.size(); ++g) {
     if (io[g].n == 0) continue;
-    kept += (io[g].dh ? 6ll : 4ll) * heads[g].vocab * small_ldz(most);
+    kept += (io[g].dh ? 8ll : 4ll) * heads[g].vocab * small_ldz(most);
     elements += (int64_t)heads[g].vocab * d;
     dh = dh || io[g].dh;
   }
@@ -1444,7 +1446,7 @@ jn_status run_big(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const Tok
       if (t->n > 0) JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, product(*t), "token gradients");
   }
   if (P.planes)
-    JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 1, launch_tok_rows(s, desc, G, P.N, inv, (const float*)(w + P.acc), P.most_planes, d),
+    JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 1, launch_tok_rows(s, desc, G, P.N, inv, (const float*)(w + P.acc), P.most_planes, d, false),
               "token row gradients");
   return JN_OK;
 }
@@ -1470,7 +1472,7 @@ jn_status run_small(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const S
             launch_gemm_tokens(s, P.rows.epi, P.rows.trans, (const GemmArgs*)(desc + G), P.rows.n, P.rows.tiles),
             "token gradients");
   JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 1,
-            launch_tok_rows(s, desc, G, P.N, (const float*)(w + P.inv), (const float*)(w + P.acc), P.planes, d),
+            launch_tok_rows(s, desc, G, P.N, (const float*)(w + P.inv), (const float*)(w + P.acc), P.planes, d, true),
             "token row gradients");
   return JN_OK;
 }

@@ -344,8 +344,9 @@ hipError_t launch_tok_table(hipStream_t s, void* dst, const void* table, size_t 
 // launch_small_scores streams W once past the rows' fragments in registers and
 // leaves one part per workgroup and row, and, training, z fp32 [vocab][ldz].
 // launch_small_grads joins the parts (every workgroup for itself), writes logp and
-// loss, and streams dW out once; grad: bf16 [vocab][ldz], the logits' gradient,
-// where row gradients are wanted.  launch_small_pick joins them for decoding.
+// loss, and streams dW out once; grad: bf16 [vocab][2 ldz], the logits' gradient,
+// where row gradients are wanted, of every row two bf16 that add up to it (the
+// nearest one and the rest).  launch_small_pick joins them for decoding.
 struct TokSmall {
   const int32_t* rows;
   const int32_t* targets;  // null when decoding
@@ -384,9 +385,10 @@ hipError_t launch_small_scores(hipStream_t s, const TokSmallSet& set, int32_t wg
 hipError_t launch_small_grads(hipStream_t s, const TokSmallSet& set, int32_t wgs, int32_t ldz, const void* hidden,
                               int32_t T, int32_t d, int32_t rows, bool f32);
 hipError_t launch_small_pick(hipStream_t s, const TokSmallSet& set, int32_t ldz, int32_t T);
-// dh = (sum of the planes of acc) inv[g], planes of [N][width]; planes: the most of a tenant.
+// dh = (sum of the planes of acc) inv[g], planes of [N][width], or (pairs) of two
+// such rows for each, one after the other; planes: the most of a tenant.
 hipError_t launch_tok_rows(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const float* inv, const float* acc,
-                           int32_t planes, int32_t width);
+                           int32_t planes, int32_t width, bool pairs);
 
 // ---- action expert (k_expert.hip) ----
 // dst[r][c] = cvt(src[r][c]) for r < src_rows, c < src_cols, else 0; r < rows, c < cols.

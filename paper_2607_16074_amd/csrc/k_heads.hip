@@ -804,10 +804,11 @@ hipError_t launch_tok_grad(hipStream_t s, const TokDesc* d, int32_t G, int32_t N
   return hipGetLastError();
 }
 
-// Eight elements of dh per STR lanes, which share the planes (many planes are those
+// Eight elements of dh per STR lanes, the sum of the planes' PARTS rows of an entry
+// (two where its logits' gradient is two bf16); they share the planes (many planes are those
 // of few rows) and are added in pairs: 60 rows, 120,000 x 128 110 -> 76 us a call, 5
 // rows, 60,000 x 2,048 163 -> 159; 701 rows of 10 planes, 32,003 x 2,048 330 -> 339.
-template <int STR>
+template <int STR, int PARTS>
 __global__ __launch_bounds__(256) void tok_rows_kernel(const TokDesc* __restrict__ desc, int32_t G, int32_t N,
                                                        const float* __restrict__ inv, const float4* __restrict__ acc,
                                                        int32_t chunks) {
@@ -819,10 +820,14 @@ __global__ __launch_bounds__(256) void tok_rows_kernel(const TokDesc* __restrict
   float v[8] = {};
 #pragma unroll 4
   for (int32_t k = threadIdx.x % STR; k < d.planes; k += STR) {
-    const float4 x = acc[2 * (k * plane + e)], y = acc[2 * (k * plane + e) + 1];
-    const float w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] += w[j];
+    for (int part = 0; part < PARTS; ++part) {
+      const float4* const at = acc + 2 * (PARTS * (k * plane + (int64_t)i * chunks) + (int64_t)part * chunks + c);
+      const float4 x = at[0], y = at[1];
+      const float w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += w[j];
+    }
   }
 #pragma unroll
   for (int o = 1; o < STR; o <<= 1)
@@ -835,14 +840,17 @@ __global__ __launch_bounds__(256) void tok_rows_kernel(const TokDesc* __restrict
 }
 
 hipError_t launch_tok_rows(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const float* inv, const float* acc,
-                           int32_t planes, int32_t width) {
+                           int32_t planes, int32_t width, bool pairs) {
   const int64_t all = (int64_t)N * (width / 8);
-  auto go = [&](auto str) {
-    tok_rows_kernel<str()><<<(unsigned)((all * str() + 255) / 256), 256, 0, s>>>(
+  auto go = [&](auto str, auto parts) {
+    tok_rows_kernel<str(), parts()><<<(unsigned)((all * str() + 255) / 256), 256, 0, s>>>(
         d, G, N, inv, reinterpret_cast<const float4*>(acc), width / 8);
     return hipGetLastError();
   };
-  return planes > 16 && all < (1 << 20) ? go(std::integral_constant<int, 16>()) : go(std::integral_constant<int, 1>());
+  auto rows = [&](auto str) {
+    return pairs ? go(str, std::integral_constant<int, 2>()) : go(str, std::integral_constant<int, 1>());
+  };
+  return planes > 16 && all < (1 << 20) ? rows(std::integral_constant<int, 16>()) : rows(std::integral_constant<int, 1>());
 }
 
 // ---- tenants of few rows ----
@@ -1097,8 +1105,13 @@ __global__ __launch_bounds__(kSmallThreads) void small_pick_kernel(TokSmallArgs<
 // so, non-temporally (93 with plain stores, whose lines the next call then waits
 // for: 260 us a call instead of 243).  dz of 128
 // vocabulary rows at a time is formed from z and the rows' joined sums by the
-// workgroup's threads together, 8 rows of the feature each, rounded to bf16 unscaled
-// (TokRow) and shared through LDS; the next rows of z are on their way meanwhile.
+// workgroup's threads together, 8 rows of the feature each, and shared through LDS as
+// two bf16, the nearest one and what is left: a row of dW is made of few terms here, of
+// one where a tenant has one target, and one bf16's rounding would stay in an fp32 dW
+// (up to 2^-8 of it; two hold 2^-16).  A second matrix instruction takes the rest: 60
+// rows, 120,000 x 2,048 236 -> 238 us a call, 5 rows, 60,000 x 2,048 with row gradients
+// 158 -> 160, 60 of 120,000 x 2,048 346 -> 360.  The next rows of z are on their way
+// meanwhile.
 // rows: those of a chunk, 128 or, of small vocabularies, fewer (a multiple of 16), so
 // that there are workgroups for the chip.  blockIdx.y: 2,048 columns each.
 constexpr int kGradRows = kSmallGradRows;
@@ -1108,7 +1121,7 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_grads_kernel(TokSmallA
                                                                        int32_t width, int32_t rows) {
   constexpr int TG = 4 * NS, U = kGradRows * TG / kSmallThreads, LD = 32 * NS + 8;  // groups of 8 rows; passes; elements of a line
   __shared__ SmallJoin<32 * NS> l;
-  __shared__ __attribute__((aligned(16))) uint16_t dz[2][kGradRows * LD];
+  __shared__ __attribute__((aligned(16))) uint16_t dz[2][2][kGradRows * LD];  // of two chunks: nearest, rest
   __shared__ u32x4t stage[8][256];
   __shared__ __attribute__((aligned(16))) float lse[64], own[64];
   __shared__ __attribute__((aligned(16))) int32_t lab[64];
@@ -1208,7 +1221,8 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_grads_kernel(TokSmallA
   };
   if (c0 < c1) fetch(c0);
   for (int32_t c = c0; c < c1; ++c) {
-    uint16_t* const line = dz[(c - c0) & 1];
+    uint16_t* const line = dz[(c - c0) & 1][0];
+    uint16_t* const rest = dz[(c - c0) & 1][1];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int32_t r = r0 + u * (kSmallThreads / TG), v = c * rows + r;
@@ -1219,26 +1233,43 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_grads_kernel(TokSmallA
         p[t] = __builtin_amdgcn_exp2f(fmaf(p[t], kLog2e, -l2[t]));
         p[t] = lb[t] == v ? ow[t] : l2[t] == INFINITY ? 0.f : p[t];  // (also where W is not finite)
       }
-      const uint4 g = make_uint4(pack_bf2_cvt(p[0], p[1]), pack_bf2_cvt(p[2], p[3]), pack_bf2_cvt(p[4], p[5]), pack_bf2_cvt(p[6], p[7]));
-      *reinterpret_cast<uint4*>(line + r * LD + 8 * tg) = g;
-      if (d.grad && blockIdx.y == 0 && v < V && 8 * tg < ldz)
-        *reinterpret_cast<uint4*>(d.grad + (int64_t)v * ldz + 8 * tg) = g;
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        hi[t] = pack_bf2_cvt(p[2 * t], p[2 * t + 1]);
+        lo[t] = pack_bf2_cvt(p[2 * t] - __uint_as_float(hi[t] << 16), p[2 * t + 1] - __uint_as_float(hi[t] & 0xffff0000u));
+      }
+      *reinterpret_cast<uint4*>(line + r * LD + 8 * tg) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      *reinterpret_cast<uint4*>(rest + r * LD + 8 * tg) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      if (d.grad && blockIdx.y == 0 && v < V && 8 * tg < ldz) {
+        uint32_t w[8];  // both of a row side by side
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          w[2 * t] = __builtin_amdgcn_perm(lo[t], hi[t], 0x05040100u);
+          w[2 * t + 1] = __builtin_amdgcn_perm(lo[t], hi[t], 0x07060302u);
+        }
+        uint4* const to = reinterpret_cast<uint4*>(d.grad + 2 * ((int64_t)v * ldz + 8 * tg));
+        to[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        to[1] = make_uint4(w[4], w[5], w[6], w[7]);
+      }
     }
     lds_barrier();  // (the other line's readers passed the barrier before this one)
     if (c + 1 < c1) fetch(c + 1);
     for (int32_t b = wv; b < rows / 16; b += WV) {
-      bf16x8h g[NS];
-#pragma unroll
-      for (int s = 0; s < NS; ++s)
-        g[s] = *reinterpret_cast<const bf16x8h*>(line + (16 * b + col) * LD + 32 * s + 8 * quad);
 #pragma unroll
       for (int p = 0; p < GP; ++p) {
         f32x4h a[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          a[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h[p][0][j], g[0], f32x4h{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-          if constexpr (NS == 2) a[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h[p][1][j], g[1], a[j], 0, 0, 0);
-        }
+        for (int j = 0; j < 8; ++j) a[j] = f32x4h{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int s = 0; s < NS; ++s) {
+            __builtin_amdgcn_sched_barrier(0);  // (one fragment of dz at a time: more spill)
+            const bf16x8h g = *reinterpret_cast<const bf16x8h*>((part ? line : rest) + (16 * b + col) * LD + 32 * s + 8 * quad);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) a[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h[p][s][j], g, a[j], 0, 0, 0);
+          }
         if (wc + 8 * p >= groups) continue;
         // turned around in LDS: a store instruction writes 256 adjacent bytes of 4 rows
         constexpr int HALVES = F32 ? 2 : 1, COLS = 128 / HALVES;
