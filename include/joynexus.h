@@ -494,8 +494,8 @@ typedef struct jn_token_io {
 
 /* Cross entropy of every tenant's targets over its own vocabulary, with gradients,
  * in pieces of the vocabulary: logits are reduced to the softmax's sums as they are
- * formed, and one piece of them, of about JN_TOKEN_PIECE_BYTES at most, is kept as
- * bf16 exponentials; the other pieces are formed again for the gradients.  So of the
+ * formed, and one piece of them, of about JN_TOKEN_PIECE_BYTES at most, is kept in
+ * 16 bits (to 2^-10.5 of the exponential); the other pieces are formed again for the gradients.  So of the
  * workspace only the softmax's sums grow with vocabulary times targets, a sixteenth to
  * a thirty-second of what the logits would take in bf16.
  * Nothing is averaged across tenants.  hidden: device bf16 [T][d], d a multiple of 64

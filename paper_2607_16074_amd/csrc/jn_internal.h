@@ -116,7 +116,8 @@ enum GemmEpi : int32_t {
   EPI_DLOGIT = 9,        // C bf16 = softmax gradient from the rows' TokRow (aux), zero in columns N .. ldc - 1
   EPI_SCALED_BF16 = 10,  // C bf16 = acc * aux[0]
   EPI_SCALED_F32 = 12,   // C fp32 = acc * aux[0]
-  EPI_SOFTMAX_KEEP = 11  // EPI_SOFTMAX with the parts at `part`; C bf16 = exp(acc - m) of the block's part
+  EPI_SOFTMAX_KEEP = 11  // EPI_SOFTMAX with the parts at `part`; C uint16 = acc as its distance below the
+                         // block's largest, in steps (kKeepSteps)
 };
 
 // Operand layouts of a grouped problem (GemmArgs::trans): X stored [K][M]
@@ -172,6 +173,12 @@ hipError_t launch_gemm_grad_pair(hipStream_t s, int epi, const GemmArgs* dprobs,
 struct TokPart {
   float m, rest;
 };
+// A kept logit z: (m - z) log2(e) in steps of 1/512 in 16 bits, m its part's largest, so
+// that exp(z - m) is off by 2^-10.5 of it at every magnitude; beyond 2^-128 of the
+// largest it is nothing.  The exponential itself in bf16 would be off by 2^-8, and then
+// be rounded a second time as the gradient that is made of it.
+constexpr float kKeepSteps = 512.f;
+constexpr uint32_t kKeepNone = 65535;
 // A target row as its logits' gradient needs it: p = exp2(z log2(e) - lse2), and
 // `own` = p - 1 from logp in the target's column.  Dividing by the number of targets
 // is left to the products' results: bf16 holds the gradient of an unlikely target,
@@ -303,8 +310,8 @@ hipError_t launch_head_gemm(hipStream_t s, const HeadGemm* descs, const HeadTile
 // ---- token heads (k_heads.hip) ----
 // A tenant of a token-head call; its targets are rows [first, first + n) of the
 // call's.  Device table, as are the problems of its products.  The kept logits
-// are columns [0, kept) of the vocabulary, in parts of `width` columns, kept_n8
-// groups of 8 to a row.
+// (kKeepSteps) are columns [0, kept) of the vocabulary, in parts of `width` columns,
+// kept_n8 groups of 8 to a row.
 struct TokDesc {
   const int32_t* rows;     // [n] rows of the shared feature
   const int32_t* targets;  // [n], null when decoding
@@ -334,7 +341,7 @@ hipError_t launch_tok_gather(hipStream_t s, void* dst, const void* table, size_t
 hipError_t launch_tok_join(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const int32_t* labels,
                            const float* zlab, TokRow* rows);
 hipError_t launch_tok_pick(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const int32_t* labels);
-// The kept logits' exponentials to their gradient, in place, and loss[g] = -(sum
+// The kept logits to their gradient in bf16, in place, and loss[g] = -(sum
 // of logp) inv[g]; zeros for dW of tenants without entries.
 hipError_t launch_tok_grad(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const float* inv, const TokRow* rows,
                            int32_t blocks, int64_t zero8);

@@ -227,8 +227,9 @@ __device__ __forceinline__ void epilogue_bf16(const GemmArgs& g, const f32x4 (&a
             v[e] = __builtin_amdgcn_exp2f(fmaf(a, 1.4426950408889634f, -lse[j + jj]));
             if (!WHOLE && n0 + 16 * i + 4 * quad + e >= g.N) v[e] = 0.f;
           } else if constexpr (EPI == EPI_SOFTMAX_KEEP) {
-            v[e] = __builtin_amdgcn_exp2f(fmaf(a, 1.4426950408889634f, top[j + jj]));
-            if (!WHOLE && n0 + 16 * i + 4 * quad + e >= g.N) v[e] = 0.f;
+            // (+ 0.5: cut off below; NaN, of a row whose sums are NaN then, becomes kKeepNone)
+            v[e] = fminf(fmaf(a - top[j + jj], -1.4426950408889634f * kKeepSteps, 0.5f), (float)kKeepNone);
+            if (!WHOLE && n0 + 16 * i + 4 * quad + e >= g.N) v[e] = (float)kKeepNone;
           } else if constexpr (EPI == EPI_SCALED_BF16) {
             v[e] = a * alpha;
           } else {
@@ -236,7 +237,11 @@ __device__ __forceinline__ void epilogue_bf16(const GemmArgs& g, const f32x4 (&a
           }
         }
         const int chunk = 2 * (GLU ? i / 2 : i) + (quad >> 1);
-        u32x2 two{pack_bf2_cvt(v[0], v[1]), pack_bf2_cvt(v[2], v[3])};
+        u32x2 two;
+        if constexpr (EPI == EPI_SOFTMAX_KEEP)
+          two = u32x2{(uint32_t)v[0] | (uint32_t)v[1] << 16, (uint32_t)v[2] | (uint32_t)v[3] << 16};
+        else
+          two = u32x2{pack_bf2_cvt(v[0], v[1]), pack_bf2_cvt(v[2], v[3])};
         if constexpr (EPI == EPI_DLOGIT)  // (no target: zeros also where W is not finite)
           if (lse[j + jj] == INFINITY) two = u32x2{0u, 0u};
         *reinterpret_cast<u32x2*>(stage + (16 * jj + row) * WC + (chunk ^ swz(row)) * 8 + (quad & 1) * 4) = two;
@@ -414,7 +419,7 @@ __device__ __forceinline__ void epilogue_softmax(const GemmArgs& g, const f32x4 
     quads([](float v) { return lane_pair16(v); });
     quads([](float v) { return lane_pair32(v); });
     if constexpr (EPI == EPI_SOFTMAX_KEEP) {
-      top[j] = (m == -INFINITY ? 0.f : m) * -1.4426950408889634f;
+      top[j] = m;
       if (quad == 0 && in) reinterpret_cast<TokPart*>(g.part)[block * g.M + r] = TokPart{m, rest};
     } else if (quad == 0 && in) {
       reinterpret_cast<TokPart*>(g.C)[block * g.ldc + r] = TokPart{m, rest};

@@ -738,8 +738,8 @@ hipError_t launch_tok_pick(hipStream_t s, const TokDesc* d, int32_t G, int32_t N
   return hipGetLastError();
 }
 
-// The kept exponentials e = exp(z - m) of column blocks to the logits' gradient
-// p - 1: p = e exp(m - lse), `own` in the target's column; 8 columns a thread.  The
+// The kept logits (kKeepSteps) to their gradient p - 1: p = exp(z - m) exp(m - lse),
+// `own` in the target's column, rounded to bf16 here and nowhere else; 8 columns a thread.  The
 // next G workgroups sum a tenant's logp each, those behind them clear dW of
 // tenants without entries.
 __global__ __launch_bounds__(256) void tok_grad_kernel(const TokDesc* __restrict__ desc, int32_t G, int32_t N,
@@ -764,15 +764,15 @@ __global__ __launch_bounds__(256) void tok_grad_kernel(const TokDesc* __restrict
     }
     const int32_t v0 = 8 * c;
     const float m = d.part[(int64_t)(v0 / d.width) * d.n + n].m;
-    // (a block without a column has m = -inf and zeros)
-    const float f = v0 < d.kept ? __builtin_amdgcn_exp2f(fmaf(m, 1.4426950408889634f, -row.lse2)) : 0.f;
+    // (a block without a column has m = -inf)
+    const float f = v0 < d.kept ? fmaf(m, 1.4426950408889634f, -row.lse2) : -INFINITY;
     const uint4 q = *at;
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
     float v[8];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      v[2 * k] = __uint_as_float(w[k] << 16) * f;
-      v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u) * f;
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t u = k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffffu;
+      v[k] = __builtin_amdgcn_exp2f(u == kKeepNone ? -INFINITY + f : fmaf((float)u, -1.f / kKeepSteps, f));
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = row.label == v0 + k ? row.own : v[k];

@@ -26,8 +26,8 @@ def problem(lib, n, v, d, dh, f32, live=None, seed=80):
     return Tenant(lib, W, rows, targets, dh, f32), hidden
 
 
-def check(t, hidden, rounding, adds=640):
-    """`rounding`: of dz, relative."""
+def check(t, hidden, rounding, adds=640, adds_dh=None):
+    """`rounding`: of dz, relative; `adds`: the longest sum of dW, and of dh where nothing else is said."""
     n, (v, d) = t.rows.numel(), t.W.shape
     y, live = t.targets.long().clamp(min=0)[:, None], (t.targets >= 0)[:, None]
     h, w = torch.where(live, hidden.double(), 0.0), t.W.double()
@@ -36,17 +36,18 @@ def check(t, hidden, rounding, adds=640):
     p = torch.softmax(z, 1)
     count = int(live.sum())
     dz = torch.where(live, p.scatter_add(1, y, torch.full((n, 1), -1.0, dtype=torch.float64, device="cuda")), 0.0) / count
-    err = dz.abs() * (rounding + (adds + 8) * 2.0 ** -24)
+    err = dz.abs() * (rounding + 8 * 2.0 ** -24)
     err += torch.where(live, p, 0.0) * (2 * D + 2.0 ** -21 * (1 + z.abs().amax(1, keepdim=True))) / count
+    sums = [err + adds * 2.0 ** -24 * dz.abs() for adds in (adds, adds_dh or adds)]
 
     def within(got, ref, spread, what):
         own = 0.0 if got.dtype is torch.float32 else BF
         o, b = (got.double() - ref).abs(), own * ref.abs() + (1 + own) * spread + 1e-37
         assert bool((o <= b).all()), (what, float((o / b).max()))
 
-    within(t.dW[: v * d].view(v, d), dz.T @ h, err.T @ h.abs(), "dW")
+    within(t.dW[: v * d].view(v, d), dz.T @ h, sums[0].T @ h.abs(), "dW")
     if t.dh is not None:
-        within(t.dh[: n * d].view(n, d), dz @ w, err @ w.abs(), "dh")
+        within(t.dh[: n * d].view(n, d), dz @ w, sums[1] @ w.abs(), "dh")
 
 
 @pytest.mark.parametrize("f32", [True, False], ids=["fp32", "bf16"])
@@ -67,3 +68,15 @@ def test_few_rows_keep_dz_in_row_gradients(lib, case):
     step(lib, lib.Context(), hidden, [t])
     # sums over ranges of 512 to 4,160 columns, then over up to 256 of them
     check(t, hidden, 2.0 ** -16, 4500)
+
+
+@pytest.mark.parametrize("f32", [True, False], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("case", [(100, 3001, 64, 1), (100, 3001, 64, 100), (300, 2049, 128, 3), (700, 8193, 64, 2),
+                                  (2000, 300007, 64, 1)], ids=lambda c: "-".join(map(str, c)))
+def test_dz_of_many_rows_is_rounded_once(lib, case, f32):
+    """Groups of more rows: dz to bf16 (2^-8) from logits kept in 16 bits (ln 2 / 1024 < 2^-10 of the exponential) or formed
+    again.  One or a few targets, so that the weight gradients show single terms."""
+    n, v, d, live = case
+    t, hidden = problem(lib, n, v, d, True, f32, live)
+    step(lib, lib.Context(), hidden, [t])
+    check(t, hidden, BF + 2.0 ** -10, n, v)
