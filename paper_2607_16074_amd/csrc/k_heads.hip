@@ -913,8 +913,12 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_scores_kernel(TokSmall
     const int32_t v = min((b * WV + wv) * 16 + row, V - 1);
     const uint16_t* const p = d.W + (int64_t)v * width + (s0 + 8 * c) * 32 + 8 * quad;
 #pragma unroll
-    for (int s = 0; s < 8; ++s)
-      if (8 * c + s < ns) to[s] = *reinterpret_cast<const bf16x8h*>(p + 32 * s);
+    for (int s = 0; s < 8; ++s) {
+      if (8 * c + s < ns)
+        to[s] = *reinterpret_cast<const bf16x8h*>(p + 32 * s);
+      else if constexpr (CH > 2)  // (else zeros from the start: a register takes one chunk; with 0 * inf a product too many shows)
+        to[s] = bf16x8h{};
+    }
   };
 #pragma unroll
   for (int s = 0; s < 8; ++s) w0[s] = w1[s] = bf16x8h{};
