@@ -1180,6 +1180,7 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
       r.X = grad;
       r.W = W;
       r.aux = P->planes ? nullptr : inv;  // (a residual add without aux is in place)
+      r.W2 = (const uint16_t*)(ws + P->labels + 4 * (size_t)desc[g].first);
       r.C = P->planes ? (void*)((float*)(ws + P->acc) + (int64_t)desc[g].first * d) : io[g].dh;
       r.ldx = up(cols, 64);
       r.ldw = r.ldc = d;
@@ -1196,7 +1197,7 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
     TokPiece p;
     jn_status st = add(&p.grad, EPI_DLOGIT, 0, dz);
     if (st == JN_OK) st = add(&p.weights, io[0].f32 ? EPI_SCALED_F32 : EPI_SCALED_BF16, GEMM_TRANS_X | GEMM_TRANS_W, dw);
-    if (st == JN_OK) st = add(&p.rows, !P->planes ? EPI_SCALED_BF16 : k == 0 ? EPI_F32 : EPI_RESID_F32, GEMM_TRANS_W, dx);
+    if (st == JN_OK) st = add(&p.rows, !P->planes ? EPI_ROWS_BF16 : k == 0 ? EPI_F32 : EPI_RESID_F32, GEMM_TRANS_W, dx);
     if (st != JN_OK) return st;
     P->pieces.push_back(p);
   }
@@ -1241,7 +1242,10 @@ jn_status small_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
   std::vector<GemmArgs> dx;
   int64_t N = 0;
   for (int32_t g = 0; g < G; ++g) {
+    desc[g].rows = io[g].rows;
+    desc[g].targets = io[g].targets;
     desc[g].n = io[g].n;
+    desc[g].vocab = heads[g].vocab;
     desc[g].first = (int32_t)N;
     desc[g].dh = io[g].n > 0 ? (uint16_t*)io[g].dh : nullptr;
     N += io[g].n;
@@ -1446,7 +1450,7 @@ jn_status run_big(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const Tok
       if (t->n > 0) JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, product(*t), "token gradients");
   }
   if (P.planes)
-    JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 1, launch_tok_rows(s, desc, G, P.N, inv, (const float*)(w + P.acc), P.most_planes, d, false),
+    JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 1, launch_tok_rows(s, desc, G, P.N, T, inv, (const float*)(w + P.acc), P.most_planes, d, false),
               "token row gradients");
   return JN_OK;
 }
@@ -1472,7 +1476,7 @@ jn_status run_small(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const S
             launch_gemm_tokens(s, P.rows.epi, P.rows.trans, (const GemmArgs*)(desc + G), P.rows.n, P.rows.tiles),
             "token gradients");
   JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 1,
-            launch_tok_rows(s, desc, G, P.N, (const float*)(w + P.inv), (const float*)(w + P.acc), P.planes, d, true),
+            launch_tok_rows(s, desc, G, P.N, T, (const float*)(w + P.inv), (const float*)(w + P.acc), P.planes, d, true),
             "token row gradients");
   return JN_OK;
 }

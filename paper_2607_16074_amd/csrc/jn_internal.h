@@ -116,6 +116,7 @@ enum GemmEpi : int32_t {
   EPI_DLOGIT = 9,        // C bf16 = softmax gradient from the rows' TokRow (aux), zero in columns N .. ldc - 1
   EPI_SCALED_BF16 = 10,  // C bf16 = acc * aux[0]
   EPI_SCALED_F32 = 12,   // C fp32 = acc * aux[0]
+  EPI_ROWS_BF16 = 13,    // EPI_SCALED_BF16 with zeros in rows whose label (W2) is negative, whatever acc is there
   EPI_SOFTMAX_KEEP = 11  // EPI_SOFTMAX with the parts at `part`; C uint16 = acc as its distance below the
                          // block's largest, in steps (kKeepSteps)
 };
@@ -129,7 +130,7 @@ constexpr int GEMM_TRANS_X = 1, GEMM_TRANS_W = 2;
 struct GemmArgs {
   const uint16_t* X;
   const uint16_t* W;
-  const uint16_t* W2;   // GeGLU up weights; EPI_SOFTMAX: labels, int32 [M] (no column: outside [0, N))
+  const uint16_t* W2;   // GeGLU up weights; EPI_SOFTMAX, EPI_ROWS_BF16: labels, int32 [M] (no column: outside [0, N))
   void* C;
   float* aux;           // GELU pre-activation (saved or read); residual source (null: C)
   int64_t ldx, ldw, ldc, ldaux;
@@ -192,7 +193,7 @@ struct TokRow {
 
 // Grouped launches of a token head's products, as above but with K ranges, any N for
 // EPI_SOFTMAX, EPI_GREEDY and EPI_DLOGIT (trans 0), and any K with GEMM_TRANS_W
-// where the columns K .. of X up to a multiple of 64 are zeros (EPI_SCALED_BF16,
+// where the columns K .. of X up to a multiple of 64 are zeros (EPI_ROWS_BF16,
 // EPI_F32, EPI_RESID_F32) or with both operands transposed (EPI_SCALED_BF16,
 // EPI_SCALED_F32, EPI_F32).  prepare: tile
 // ranges and shape, or a total of -1.  Column blocks of EPI_SOFTMAX and EPI_GREEDY are
@@ -207,7 +208,7 @@ int32_t gemm_tokens_block(int shape);
 inline int32_t tok_blocks(int32_t vocab, int32_t block) { return (vocab + 2 * block - 1) / (2 * block) * 2; }
 hipError_t launch_gemm_tokens(hipStream_t s, int epi, int trans, const GemmArgs* dprobs, int32_t nprob,
                               const TokTiles& t);
-// Row gradients (depi EPI_F32 or EPI_SCALED_BF16, GEMM_TRANS_W) and weight gradients
+// Row gradients (depi EPI_F32 or EPI_ROWS_BF16, GEMM_TRANS_W) and weight gradients
 // (wepi EPI_SCALED_BF16 or EPI_SCALED_F32, both transposed) in one launch, where
 // the shapes allow it.
 bool gemm_tokens_pair_ok(const TokTiles& rows, const TokTiles& weights);
@@ -393,9 +394,10 @@ hipError_t launch_small_grads(hipStream_t s, const TokSmallSet& set, int32_t wgs
                               int32_t T, int32_t d, int32_t rows, bool f32);
 hipError_t launch_small_pick(hipStream_t s, const TokSmallSet& set, int32_t ldz, int32_t T);
 // dh = (sum of the planes of acc) inv[g], planes of [N][width], or (pairs) of two
-// such rows for each, one after the other; planes: the most of a tenant.
-hipError_t launch_tok_rows(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const float* inv, const float* acc,
-                           int32_t planes, int32_t width, bool pairs);
+// such rows for each, one after the other, and zeros for entries without a target, whose
+// products are 0 * W and NaN where W is not finite; planes: the most of a tenant.
+hipError_t launch_tok_rows(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, int32_t T, const float* inv,
+                           const float* acc, int32_t planes, int32_t width, bool pairs);
 
 // ---- action expert (k_expert.hip) ----
 // dst[r][c] = cvt(src[r][c]) for r < src_rows, c < src_cols, else 0; r < rows, c < cols.

@@ -174,7 +174,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr bool epi_bf16(int epi) {
   return epi == EPI_BF16 || epi == EPI_GELU_BF16 || epi == EPI_GEGLU_BF16 || epi == EPI_DLOGIT ||
-         epi == EPI_SCALED_BF16 || epi == EPI_SOFTMAX_KEEP;
+         epi == EPI_SCALED_BF16 || epi == EPI_ROWS_BF16 || epi == EPI_SOFTMAX_KEEP;
 }
 constexpr bool epi_softmax(int epi) { return epi == EPI_SOFTMAX || epi == EPI_GREEDY || epi == EPI_SOFTMAX_KEEP; }
 constexpr bool epi_exp(int epi) { return epi == EPI_DLOGIT || epi == EPI_SOFTMAX_KEEP; }
@@ -203,7 +203,12 @@ __device__ __forceinline__ void epilogue_bf16(const GemmArgs& g, const f32x4 (&a
   uint16_t* C = reinterpret_cast<uint16_t*>(g.C) + (int64_t)m * g.ldc + n;
   const int64_t step = RI * g.ldc;
   auto swz = [](int r) { return CH == 16 ? r & 15 : (r / (16 / CH)) & (CH - 1); };
-  const float alpha = EPI == EPI_SCALED_BF16 ? g.aux[0] : 1.f;
+  const float alpha = EPI == EPI_SCALED_BF16 || EPI == EPI_ROWS_BF16 ? g.aux[0] : 1.f;
+  int32_t label[EPI == EPI_ROWS_BF16 ? TM : 1];
+  if constexpr (EPI == EPI_ROWS_BF16)
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+      label[j] = reinterpret_cast<const int32_t*>(g.W2)[WHOLE ? m0 + 16 * j + row : min(m0 + 16 * j + row, g.M - 1)];
   float lse[EPI == EPI_DLOGIT ? TM : 1];
   int32_t own[EPI == EPI_DLOGIT ? TM : 1];  // the target, from the lane's first column
   if constexpr (EPI == EPI_DLOGIT) {
@@ -230,7 +235,7 @@ __device__ __forceinline__ void epilogue_bf16(const GemmArgs& g, const f32x4 (&a
             // (+ 0.5: cut off below; NaN, of a row whose sums are NaN then, becomes kKeepNone)
             v[e] = fminf(fmaf(a - top[j + jj], -1.4426950408889634f * kKeepSteps, 0.5f), (float)kKeepNone);
             if (!WHOLE && n0 + 16 * i + 4 * quad + e >= g.N) v[e] = (float)kKeepNone;
-          } else if constexpr (EPI == EPI_SCALED_BF16) {
+          } else if constexpr (EPI == EPI_SCALED_BF16 || EPI == EPI_ROWS_BF16) {
             v[e] = a * alpha;
           } else {
             v[e] = GLU ? gelu_fast_f(a) * acc[i + (GLU ? 1 : 0)][j + jj][e] : EPI == EPI_GELU_BF16 ? gelu_fast_f(a) : a;
@@ -244,6 +249,8 @@ __device__ __forceinline__ void epilogue_bf16(const GemmArgs& g, const f32x4 (&a
           two = u32x2{pack_bf2_cvt(v[0], v[1]), pack_bf2_cvt(v[2], v[3])};
         if constexpr (EPI == EPI_DLOGIT)  // (no target: zeros also where W is not finite)
           if (lse[j + jj] == INFINITY) two = u32x2{0u, 0u};
+        if constexpr (EPI == EPI_ROWS_BF16)
+          if (label[j + jj] < 0) two = u32x2{0u, 0u};
         *reinterpret_cast<u32x2*>(stage + (16 * jj + row) * WC + (chunk ^ swz(row)) * 8 + (quad & 1) * 4) = two;
       }
       if constexpr (EPI == EPI_DLOGIT) {  // (behind the lane's own write of that column: a wave's LDS operations stay in order)
@@ -1666,7 +1673,7 @@ TokTiles gemm_tokens_prepare(int epi, int trans, GemmArgs* probs, int32_t nprob)
       work += n * slabs(probs[p]);
     }
     if (tiles <= 0 || tiles > (int64_t)kMostBlocks) continue;
-    const int like = epi_exp(epi) ? EPI_GELU_BF16 : epi == EPI_SCALED_F32 ? EPI_F32 : epi;
+    const int like = epi_exp(epi) ? EPI_GELU_BF16 : epi == EPI_SCALED_F32 ? EPI_F32 : epi == EPI_ROWS_BF16 ? EPI_SCALED_BF16 : epi;
     double us = tiles_time(like, tiles, (double)work / tiles, t);
     if (out.uneven)
       us = std::max(us, longest * std::max(kShapes[t].slab, kShapes[t].slab1) + tiles_time(like, tiles, 0.0, t));
@@ -1834,12 +1841,12 @@ hipError_t launch_gemm_tokens_pair(hipStream_t s, int depi, const GemmArgs* dpro
   gemm_tokens_pair_kernel<D, W><<<gd + gw, 256, 0, s>>>(dprobs, nd, d.total, gd, wprobs, nw, w.total, w.uneven)
   if (depi == EPI_F32 && wepi == EPI_SCALED_BF16)
     JN_PAIR(EPI_F32, EPI_SCALED_BF16);
-  else if (depi == EPI_SCALED_BF16 && wepi == EPI_SCALED_BF16)
-    JN_PAIR(EPI_SCALED_BF16, EPI_SCALED_BF16);
+  else if (depi == EPI_ROWS_BF16 && wepi == EPI_SCALED_BF16)
+    JN_PAIR(EPI_ROWS_BF16, EPI_SCALED_BF16);
   else if (depi == EPI_F32 && wepi == EPI_SCALED_F32)
     JN_PAIR(EPI_F32, EPI_SCALED_F32);
-  else if (depi == EPI_SCALED_BF16 && wepi == EPI_SCALED_F32)
-    JN_PAIR(EPI_SCALED_BF16, EPI_SCALED_F32);
+  else if (depi == EPI_ROWS_BF16 && wepi == EPI_SCALED_F32)
+    JN_PAIR(EPI_ROWS_BF16, EPI_SCALED_F32);
   else
     return hipErrorInvalidValue;
 #undef JN_PAIR
@@ -1854,7 +1861,7 @@ hipError_t launch_gemm_tokens(hipStream_t s, int epi, int trans, const GemmArgs*
     case EPI_SOFTMAX_KEEP * 4: return launch_tokens<EPI_SOFTMAX_KEEP, 0>(s, dprobs, nprob, t);
     case EPI_GREEDY * 4: return launch_tokens<EPI_GREEDY, 0>(s, dprobs, nprob, t);
     case EPI_DLOGIT * 4: return launch_tokens<EPI_DLOGIT, 0>(s, dprobs, nprob, t);
-    case EPI_SCALED_BF16 * 4 + GEMM_TRANS_W: return launch_tokens<EPI_SCALED_BF16, GEMM_TRANS_W>(s, dprobs, nprob, t);
+    case EPI_ROWS_BF16 * 4 + GEMM_TRANS_W: return launch_tokens<EPI_ROWS_BF16, GEMM_TRANS_W>(s, dprobs, nprob, t);
     case EPI_F32 * 4 + GEMM_TRANS_W: return launch_tokens<EPI_F32, GEMM_TRANS_W>(s, dprobs, nprob, t);
     case EPI_RESID_F32 * 4 + GEMM_TRANS_W: return launch_tokens<EPI_RESID_F32, GEMM_TRANS_W>(s, dprobs, nprob, t);
     case EPI_F32 * 4 + (GEMM_TRANS_X | GEMM_TRANS_W):

@@ -810,13 +810,15 @@ hipError_t launch_tok_grad(hipStream_t s, const TokDesc* d, int32_t G, int32_t N
 // rows, 60,000 x 2,048 163 -> 159; 701 rows of 10 planes, 32,003 x 2,048 330 -> 339.
 template <int STR, int PARTS>
 __global__ __launch_bounds__(256) void tok_rows_kernel(const TokDesc* __restrict__ desc, int32_t G, int32_t N,
-                                                       const float* __restrict__ inv, const float4* __restrict__ acc,
+                                                       int32_t T, const float* __restrict__ inv, const float4* __restrict__ acc,
                                                        int32_t chunks) {
   const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) / STR, plane = (int64_t)N * chunks;
   if (e >= plane) return;
   const int32_t i = (int32_t)(e / chunks), c = (int32_t)(e - (int64_t)i * chunks), t = tok_tenant(desc, G, i);
   const TokDesc& d = desc[t];
   if (!d.dh) return;
+  const int32_t r = d.rows[i - d.first], to = d.targets[i - d.first];
+  const bool live = r >= 0 && r < T && to >= 0 && to < d.vocab;
   float v[8] = {};
 #pragma unroll 4
   for (int32_t k = threadIdx.x % STR; k < d.planes; k += STR) {
@@ -835,16 +837,18 @@ __global__ __launch_bounds__(256) void tok_rows_kernel(const TokDesc* __restrict
     for (int j = 0; j < 8; ++j) v[j] += __shfl_xor(v[j], o, kWave);
   if (threadIdx.x % STR != 0) return;
   const float f = inv[t];
-  reinterpret_cast<uint4*>(d.dh)[(int64_t)(i - d.first) * chunks + c] = make_uint4(
-      pack_bf2(v[0] * f, v[1] * f), pack_bf2(v[2] * f, v[3] * f), pack_bf2(v[4] * f, v[5] * f), pack_bf2(v[6] * f, v[7] * f));
+  reinterpret_cast<uint4*>(d.dh)[(int64_t)(i - d.first) * chunks + c] =
+      live ? make_uint4(pack_bf2(v[0] * f, v[1] * f), pack_bf2(v[2] * f, v[3] * f), pack_bf2(v[4] * f, v[5] * f),
+                        pack_bf2(v[6] * f, v[7] * f))
+           : make_uint4(0, 0, 0, 0);
 }
 
-hipError_t launch_tok_rows(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, const float* inv, const float* acc,
-                           int32_t planes, int32_t width, bool pairs) {
+hipError_t launch_tok_rows(hipStream_t s, const TokDesc* d, int32_t G, int32_t N, int32_t T, const float* inv,
+                           const float* acc, int32_t planes, int32_t width, bool pairs) {
   const int64_t all = (int64_t)N * (width / 8);
   auto go = [&](auto str, auto parts) {
     tok_rows_kernel<str(), parts()><<<(unsigned)((all * str() + 255) / 256), 256, 0, s>>>(
-        d, G, N, inv, reinterpret_cast<const float4*>(acc), width / 8);
+        d, G, N, T, inv, reinterpret_cast<const float4*>(acc), width / 8);
     return hipGetLastError();
   };
   auto rows = [&](auto str) {

@@ -38,3 +38,26 @@ def test_a_token_of_no_probability_in_wide_heads(lib, d):
         pick = Pick(lib, W, rows)
         decode(lib, lib.Context(), hidden, [pick])
         assert bool((pick.token[:n] != ban).all()) and bool(torch.isfinite(pick.logp[:n]).all()), k
+
+
+@pytest.mark.parametrize("value", ["-inf", "inf", "nan"])
+@pytest.mark.parametrize("case", [(20, 100003, 128), (40, 530001, 128), (20, 600, 64), (100, 400, 64), (300, 3001, 128),
+                                  (200, 20001, 256), (2000, 300007, 64)], ids=lambda c: "-".join(map(str, c)))
+def test_row_gradients_of_entries_without_a_target(lib, case, value):
+    """Their gradient is zero whatever W holds: behind the streaming launches, of one plane, of several, of several pieces."""
+    n, v, d = case
+    hidden = feature(n, d)
+    hidden[:, 0] = 1.0
+    W, rows, targets = draw(n, v, d, n, 91)
+    rows[1], targets[2], rows[n - 1], targets[n // 2] = -1, -1, n, v
+    W[v // 3] = 0.0
+    W[v // 3, 0] = float(value)
+    W[v - 2, 5] = float(value)
+    for f32 in (False, True):
+        t = Tenant(lib, W, rows, targets, True, f32)
+        step(lib, lib.Context(), hidden, [t])
+        dead = (rows < 0) | (rows >= n) | (targets < 0) | (targets >= v)
+        assert int(dead.sum()) == 4
+        dh = t.dh[: n * d].view(n, d)
+        assert bool((dh[dead] == 0).all()) and bool((t.logp[:n][dead] == 0).all())
+        assert bool(dh[~dead].isnan().any())  # (a live row's product with an infinity is what the formula says)
