@@ -186,8 +186,8 @@ constexpr uint32_t kKeepNone = 65535;
 // nearly -1 in every row, all but exactly, while a common factor's rounding would
 // be off by the same half step in all of them.
 struct TokRow {
-  float lse2;           // +inf: the row has no target (its z are 0), and p = 0
-  int32_t label;        // then -1
+  float lse2;           // (+inf where the row has no target, and where a logit is)
+  int32_t label;        // -1: no target, and p = 0
   float own;
 };
 

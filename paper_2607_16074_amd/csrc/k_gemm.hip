@@ -210,13 +210,14 @@ __device__ __forceinline__ void epilogue_bf16(const GemmArgs& g, const f32x4 (&a
     for (int j = 0; j < TM; ++j)
       label[j] = reinterpret_cast<const int32_t*>(g.W2)[WHOLE ? m0 + 16 * j + row : min(m0 + 16 * j + row, g.M - 1)];
   float lse[EPI == EPI_DLOGIT ? TM : 1];
-  int32_t own[EPI == EPI_DLOGIT ? TM : 1];  // the target, from the lane's first column
+  int32_t own[EPI == EPI_DLOGIT ? TM : 1];  // the target, from the lane's first column; kNoTarget: none
+  constexpr int32_t kNoTarget = -0x7fffffff - 1;
   if constexpr (EPI == EPI_DLOGIT) {
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
       const TokRow& t = reinterpret_cast<const TokRow*>(g.aux)[WHOLE ? m0 + 16 * j + row : min(m0 + 16 * j + row, g.M - 1)];
       lse[j] = t.lse2;
-      own[j] = t.label < 0 ? -1 : t.label - (int32_t)g.split_c - n0 - 4 * quad;
+      own[j] = t.label < 0 ? kNoTarget : t.label - (int32_t)g.split_c - n0 - 4 * quad;
     }
   }
   auto put = [&](int j) __attribute__((always_inline)) {  // blocks j .. j + NB - 1
@@ -247,8 +248,8 @@ __device__ __forceinline__ void epilogue_bf16(const GemmArgs& g, const f32x4 (&a
           two = u32x2{(uint32_t)v[0] | (uint32_t)v[1] << 16, (uint32_t)v[2] | (uint32_t)v[3] << 16};
         else
           two = u32x2{pack_bf2_cvt(v[0], v[1]), pack_bf2_cvt(v[2], v[3])};
-        if constexpr (EPI == EPI_DLOGIT)  // (no target: zeros also where W is not finite)
-          if (lse[j + jj] == INFINITY) two = u32x2{0u, 0u};
+        if constexpr (EPI == EPI_DLOGIT)  // (zeros also where W is not finite; a target's infinite logit is no such row)
+          if (own[j + jj] == kNoTarget) two = u32x2{0u, 0u};
         if constexpr (EPI == EPI_ROWS_BF16)
           if (label[j + jj] < 0) two = u32x2{0u, 0u};
         *reinterpret_cast<u32x2*>(stage + (16 * jj + row) * WC + (chunk ^ swz(row)) * 8 + (quad & 1) * 4) = two;

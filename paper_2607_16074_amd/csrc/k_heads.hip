@@ -1239,7 +1239,7 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_grads_kernel(TokSmallA
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
         p[t] = __builtin_amdgcn_exp2f(fmaf(p[t], kLog2e, -l2[t]));
-        p[t] = lb[t] == v ? ow[t] : l2[t] == INFINITY ? 0.f : p[t];  // (also where W is not finite)
+        p[t] = lb[t] == v ? ow[t] : lb[t] < 0 ? 0.f : p[t];  // (no target: zeros also where W is not finite)
       }
       uint32_t hi[4], lo[4];
 #pragma unroll

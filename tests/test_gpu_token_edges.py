@@ -61,3 +61,28 @@ def test_row_gradients_of_entries_without_a_target(lib, case, value):
         dh = t.dh[: n * d].view(n, d)
         assert bool((dh[dead] == 0).all()) and bool((t.logp[:n][dead] == 0).all())
         assert bool(dh[~dead].isnan().any())  # (a live row's product with an infinity is what the formula says)
+
+
+@pytest.mark.parametrize("case", [(5, 600, 64, 300), (40, 100003, 128, 7), (100, 600, 64, 300), (2000, 300007, 64, 3),
+                                  (2000, 300007, 64, 300001)], ids=lambda c: "-".join(map(str, c)))
+def test_an_infinite_logit_of_a_target_is_not_hidden(lib, case):
+    """Such a row has no softmax: its loss is infinite, and its gradient does not read as that of a row without a target,
+    nor reach other tokens' rows where the infinite token's block is not theirs."""
+    n, v, d, bad = case
+    hidden = feature(n, d)
+    hidden[:, 0] = 0.0
+    hidden[1, 0] = 1.0  # the others meet the infinity with 0 * inf, so they have no target
+    W, rows, targets = draw(n, v, d, n, 92)
+    rows.copy_(torch.arange(n))
+    targets[targets == bad] = 0
+    targets[0], targets[2:] = -1, -1
+    W[bad] = 0.0
+    W[bad, 0] = float("inf")
+    t = Tenant(lib, W, rows, targets, False, True)
+    step(lib, lib.Context(), hidden, [t])
+    assert float(t.loss[0]) == float("inf") and float(t.logp[1]) == -float("inf")
+    dW = t.dW[: v * d].view(v, d)
+    assert bool(dW[bad].isnan().all())
+    far = (bad + v // 2) % v
+    y = int(targets[1])
+    assert bool(torch.isfinite(dW[far]).all()) and (abs(y - bad) <= 256 or bool((dW[y] == -hidden[1].float()).all()))
