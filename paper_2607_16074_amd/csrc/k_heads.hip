@@ -945,7 +945,9 @@ __global__ __launch_bounds__(kSmallThreads, 2) void small_scores_kernel(TokSmall
   const int32_t tok = threadIdx.x % TOK;
   const int32_t label = d.targets && tok < n ? d.targets[tok] : -1;
   float m = -INFINITY, rest = 0.f;
-  int32_t at = 0x7fffffff;
+  // the thread's first token, so that logits that are all -inf pick their lowest
+  const int32_t first = threadIdx.x / TOK;
+  int32_t at = first < ROWS && b0 < b1 && b0 * ROWS + first < V ? b0 * ROWS + first : 0x7fffffff;
   f32x4h acc[NB];
 #pragma unroll
   for (int j = 0; j < NB; ++j) acc[j] = f32x4h{0.f, 0.f, 0.f, 0.f};

@@ -86,3 +86,24 @@ def test_an_infinite_logit_of_a_target_is_not_hidden(lib, case):
     far = (bad + v // 2) % v
     y = int(targets[1])
     assert bool(torch.isfinite(dW[far]).all()) and (abs(y - bad) <= 256 or bool((dW[y] == -hidden[1].float()).all()))
+
+
+@pytest.mark.parametrize("case", [(1, 1, 64), (5, 37, 64), (16, 301, 768), (64, 1003, 2048), (16, 700, 8192), (3, 20001, 320),
+                                  (100, 301, 64), (70, 20001, 128)], ids=lambda c: "-".join(map(str, c)))
+def test_decode_of_equal_infinite_logits_takes_the_lowest(lib, case):
+    """All logits -inf, or all but the last ones: still the lowest of equal ones."""
+    n, v, d = case
+    hidden = feature(n, d)
+    hidden[:, 0] = 1.0
+    W, rows, _ = draw(n, v, d, n, 93)
+    rows.copy_(torch.arange(n))
+    W[:] = 0.0
+    W[:, 0] = float("-inf")
+    pick = Pick(lib, W, rows)
+    decode(lib, lib.Context(), hidden, [pick])
+    assert bool((pick.token[:n] == 0).all()) and bool(pick.logp[:n].isnan().all())
+    if v > 2:
+        W[v - 2:, 0] = 1.0
+        decode(lib, lib.Context(), hidden, [pick])
+        assert bool((pick.token[:n] == v - 2).all())
+        assert float((pick.logp[:n] + 0.6931472).abs().max()) < 1e-6
