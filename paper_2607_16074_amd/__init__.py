@@ -243,7 +243,8 @@ class Backbone:
     """Device weights of the frozen backbone (lists of torch bf16 tensors).
 
     A layer with head norms also has "gq" and "gk" (bf16 [head width]).  ``rope_sections``: pairs of every position
-    axis, for rows with several positions; ``set_positions`` then names the batch's."""
+    axis, for rows with several positions.  Positions belong to a batch: the calls take them as ``pos``, and nothing
+    here writes those of ``set_positions``, which stand for calls that give none."""
 
     def __init__(self, layers: List[dict], gf, n_heads: int, eps: float, n_kv_heads: int = 0, causal: bool = False,
                  rope_theta: float = 0.0, rope_sections: Sequence[int] = (), rope_interleaved: bool = False):
@@ -283,7 +284,7 @@ class Backbone:
         self.pos = None
 
     def set_positions(self, pos):
-        """Positions of the packed rows of the batches that follow: device int32 [T, axes] (None: the rows' own)."""
+        """Positions of the packed rows of calls that give none: device int32 [T, axes] (None: the rows' own)."""
         if pos is not None and pos.dim() != 2:
             raise TypeError("positions must be [T, axes]")
         self.struct.pos = _positions(pos, pos.shape[0] if pos is not None else 0, max(1, self.struct.rope_axes))
@@ -296,16 +297,24 @@ def jn_backbone_workspace_size(bb: Backbone, T: int) -> int:
     return int(n.value)
 
 
-def _check_positions(bb: Backbone, T: int):
-    pos = getattr(bb, "pos", None)  # (anything with a `struct` may stand for a backbone)
-    if pos is not None and pos.shape[0] != T:
-        raise ValueError(f"the backbone's positions are of {pos.shape[0]} rows, the batch has {T}")
+def _backbone_of(bb: Backbone, T: int, pos):
+    """The C struct for a batch of T rows at ``pos``, a copy where that is not the backbone's own."""
+    own = getattr(bb, "pos", None)  # (anything with a `struct` may stand for a backbone)
+    if pos is None:
+        if own is not None and own.shape[0] != T:
+            raise ValueError(f"the backbone's positions are of {own.shape[0]} rows, the batch has {T}")
+        return bb.struct
+    if pos.dim() != 2 or pos.shape[0] != T:
+        raise ValueError(f"positions must be [{T}, axes], not {tuple(pos.shape)}")
+    s = jn_backbone.from_buffer_copy(bb.struct)
+    s.pos = _positions(pos, T, max(1, s.rope_axes))
+    return s
 
 
-def jn_backbone_forward(ctx: Context, bb: Backbone, packed: Packed, hidden, ws):
-    _check_positions(bb, packed.struct.T)
-    _check(_lib.jn_backbone_forward(ctx.handle, C.byref(bb.struct), C.byref(packed.struct), _ptr(hidden),
-                                    _ptr(ws), ws.numel() * ws.element_size()), ctx)
+def jn_backbone_forward(ctx: Context, bb: Backbone, packed: Packed, hidden, ws, pos=None):
+    """``pos``: device int32 [T, axes], positions of the batch's packed rows (None: as ``Backbone.set_positions`` says)."""
+    _check(_lib.jn_backbone_forward(ctx.handle, C.byref(_backbone_of(bb, packed.struct.T, pos)), C.byref(packed.struct),
+                                    _ptr(hidden), _ptr(ws), ws.numel() * ws.element_size()), ctx)
 
 
 # --------------------------------------- queries and keys: norm, rotation ---
@@ -742,32 +751,35 @@ class Collector:
 
 
 def jn_infer_workspace_size(reqs: Sequence[Request], tenants: Sequence[Tenant], d: int, align: int, bb: Backbone,
-                            heads: Sequence[Head]) -> int:
+                            heads: Sequence[Head], pos=None) -> int:
     ra, keep = _requests(reqs)
     ha, _ = _head_arrays(heads)
     o = _opts(d, align)
     n = C.c_size_t()
+    s = bb.struct if pos is None else _backbone_of(bb, jn_pack_plan(reqs, tenants, d, align).T, pos)
     _check(_lib.jn_infer_workspace_size(ra, len(reqs), _tenants(tenants), len(tenants), C.byref(o),
-                                        C.byref(bb.struct), ha, C.byref(n)), what="jn_infer_workspace_size")
+                                        C.byref(s), ha, C.byref(n)), what="jn_infer_workspace_size")
     return int(n.value)
 
 
 class InferPlan:
     """``jn_infer_plan_*``: a resident decode-only step over one physical batch
-    (device buffers stay referenced here for the plan's lifetime)."""
+    (device buffers stay referenced here for the plan's lifetime; ``pos`` as in
+    ``jn_backbone_forward``, read at every launch)."""
 
     def __init__(self, ctx: Context, reqs: Sequence[Request], tenants: Sequence[Tenant], d: int, align: int,
-                 bb: Backbone, heads: Sequence[Head], actions: Sequence, ws):
-        pos = getattr(bb, "pos", None)
-        if pos is not None:
-            _check_positions(bb, jn_pack_plan(reqs, tenants, d, align).T)
+                 bb: Backbone, heads: Sequence[Head], actions: Sequence, ws, pos=None):
+        s = bb.struct
+        if pos is not None or getattr(bb, "pos", None) is not None:
+            s = _backbone_of(bb, jn_pack_plan(reqs, tenants, d, align).T, pos)
+            pos = bb.pos if pos is None else pos
         ra, keep = _requests(reqs)
         ha, _ = _head_arrays(heads)
         o = _opts(d, align)
         acts = (C.c_void_p * len(actions))(*[_ptr(a) for a in actions])
         h = C.c_void_p()
         _check(_lib.jn_infer_plan_create(ctx.handle, ra, len(reqs), _tenants(tenants), len(tenants), C.byref(o),
-                                         C.byref(bb.struct), ha, acts, _ptr(ws), ws.numel() * ws.element_size(),
+                                         C.byref(s), ha, acts, _ptr(ws), ws.numel() * ws.element_size(),
                                          C.byref(h)), ctx)
         self.handle = h
         self.ctx = ctx

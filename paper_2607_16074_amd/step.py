@@ -125,7 +125,7 @@ class GroupStep:
 
     Token-predicting tenants: ``targets[g]`` is a triple of int arrays (sample in the tenant's arrival order, its row,
     the token that row predicts).  ``positions``: per request int [n, max_len, axes], for backbones whose rows have
-    several position axes."""
+    several position axes; the step's own, whatever other steps of the model have."""
 
     def __init__(self, model: Model, requests: Sequence[Request], targets: Dict[int, np.ndarray],
                  tenants: Sequence[int], align: int = 1, ctx: Optional[Context] = None, device="cuda",
@@ -208,8 +208,7 @@ class GroupStep:
         self.packed = jn_pack_group(self.ctx, self.requests, self.table, d, self.align, self.maps, self.tokens)
 
     def backbone(self):
-        self.model.backbone.set_positions(self.pos)
-        jn_backbone_forward(self.ctx, self.model.backbone, self.packed, self.hidden, self.bb_ws)
+        jn_backbone_forward(self.ctx, self.model.backbone, self.packed, self.hidden, self.bb_ws, self.pos)
 
     def heads_fwd_bwd(self):
         if self.use_experts:
@@ -236,10 +235,11 @@ class InferStep:
     its own (graph capture needs a non-null stream): ``launch`` enqueues the
     kernels, ``capture`` records one launch into a HIP graph, ``replay``
     launches that graph.  ``actions[k]`` is tenant ``tenants[k]``'s output,
-    rows in its arrival order."""
+    rows in its arrival order.  ``positions`` as in ``GroupStep``; ``pos``, the
+    packed rows' own, is read at every launch."""
 
     def __init__(self, model: Model, requests: Sequence[Request], tenants: Sequence[int], align: int = 1,
-                 device="cuda", stream=None):
+                 device="cuda", stream=None, positions: Optional[Sequence[np.ndarray]] = None):
         import torch
         self.model = model
         self.stream = stream if stream is not None else torch.cuda.Stream(device=device)
@@ -254,11 +254,15 @@ class InferStep:
             raise ValueError("InferStep serves MLP-head tenants")
         self.actions = [torch.empty((int(sum(r.n for r in self.requests if r.tenant == k)), int(h.dims[-1])),
                                     dtype=torch.float32, device=device) for k, h in enumerate(self.heads)]
-        nbytes = jn_infer_workspace_size(self.requests, self.table, d, align, model.backbone, self.heads)
+        self.pos = None
+        if positions is not None:
+            host = jn_pack_maps_host(self.requests, self.table, d, align)
+            self.pos = _dev_i32(packed_positions(self.requests, host, positions), device)
+        nbytes = jn_infer_workspace_size(self.requests, self.table, d, align, model.backbone, self.heads, self.pos)
         self.ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
         torch.cuda.synchronize()
         self.plan = InferPlan(self.ctx, self.requests, self.table, d, align, model.backbone, self.heads,
-                              self.actions, self.ws)
+                              self.actions, self.ws, self.pos)
 
     def launch(self):
         self.plan.launch()
@@ -310,8 +314,7 @@ class DecodeStep:
     def run(self):
         d = self.model.backbone.d
         packed = jn_pack_group(self.ctx, self.requests, self.table, d, self.align, self.maps, self.packed_tokens)
-        self.model.backbone.set_positions(self.pos)
-        jn_backbone_forward(self.ctx, self.model.backbone, packed, self.hidden, self.bb_ws)
+        jn_backbone_forward(self.ctx, self.model.backbone, packed, self.hidden, self.bb_ws, self.pos)
         jn_tenant_tokens_decode(self.ctx, self.hidden, self.heads, self.picks, self.ws)
 
 
@@ -367,13 +370,15 @@ class TenantOptimizer:
 
 def isolated_runs(model: Model, requests: Sequence[Request], targets: Dict[int, np.ndarray],
                   tenants: Sequence[int], align: int = 1, ctx: Optional[Context] = None, device="cuda",
-                  noisy: Optional[Dict[int, np.ndarray]] = None, flow_t: Optional[Dict[int, np.ndarray]] = None):
-    """One ``GroupStep`` per tenant (its own requests only), sharing the weights."""
+                  noisy: Optional[Dict[int, np.ndarray]] = None, flow_t: Optional[Dict[int, np.ndarray]] = None,
+                  positions: Optional[Sequence[np.ndarray]] = None):
+    """One ``GroupStep`` per tenant (its own requests and their positions only), sharing the weights."""
     ctx = ctx or Context()
     out = []
     for g in tenants:
-        reqs = [r for r in requests if r.tenant == g]
-        out.append(GroupStep(model, reqs, targets, [g], align, ctx, device, noisy, flow_t))
+        mine = [k for k, r in enumerate(requests) if r.tenant == g]
+        out.append(GroupStep(model, [requests[k] for k in mine], targets, [g], align, ctx, device, noisy, flow_t,
+                             [positions[k] for k in mine] if positions is not None else None))
     return out
 
 
