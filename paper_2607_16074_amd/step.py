@@ -66,10 +66,11 @@ def target_rows(maps: dict, slot: int, sample: np.ndarray, row: np.ndarray) -> n
     names no valid row (no target)."""
     first, end = int(maps["tenant_sample_off"][slot]), int(maps["tenant_sample_off"][slot + 1])
     sample, row = np.asarray(sample, np.int64), np.asarray(row, np.int64)
-    ok = (sample >= 0) & (sample < end - first)
-    i = maps["tenant_perm"][first + np.where(ok, sample, 0)]
-    ok &= (row >= 0) & (row < maps["seqlens"][i])
-    return np.where(ok, maps["cu_seqlens"][i] + row, -1).astype(np.int32)
+    out = np.full(np.broadcast(sample, row).shape, -1, np.int32)
+    ok = (sample >= 0) & (sample < end - first) & (row >= 0)
+    i = maps["tenant_perm"][first + sample[ok]]
+    out[ok] = np.where(row[ok] < maps["seqlens"][i], maps["cu_seqlens"][i] + row[ok], -1)
+    return out
 
 
 class Model:
