@@ -650,6 +650,7 @@ jn_status check_backbone(jn_ctx* c, const jn_backbone* bb) {
   if (st != JN_OK) return st;
   if (bb->rope_axes > 1 && (!(bb->rope_theta > 0.f) || !bb->pos))
     return fail(c, JN_EINVAL, "%d position axes need rope_theta > 0 and pos", bb->rope_axes);
+  if (bb->rope_theta > 0.f && (uintptr_t)bb->pos % 4 != 0) return fail(c, JN_EINVAL, "pos not 4-byte aligned");
   bool glu = bb->layers[0].w_gate != nullptr;
   for (int l = 0; l < bb->n_layers; ++l) {
     const jn_layer& L = bb->layers[l];

@@ -113,3 +113,21 @@ def test_positions_of_another_size_are_refused(lib, calls):
         with pytest.raises(error):
             lib.jn_backbone_forward(st.ctx, m.backbone, st.packed, st.hidden, st.bb_ws, bad)
     assert calls == []
+
+
+def test_misaligned_positions_are_refused(lib):
+    m = model(lib)
+    heads = [lib.Head([torch.zeros(2, D)], [torch.zeros(2)], 2, 1) for _ in range(2)]
+    table, reqs = [lib.Tenant(7, D)] * 2, requests(lib)
+    pos = torch.zeros(14, 3, dtype=torch.int32)
+
+    def size():
+        return lib.jn_infer_workspace_size(reqs, table, D, 1, m.backbone, heads)
+
+    m.backbone.set_positions(pos)
+    assert size() > 0
+    for off in (1, 2, 3):
+        m.backbone.struct.pos = pos.data_ptr() + off
+        with pytest.raises(lib.JNError) as e:
+            size()
+        assert e.value.status == lib._abi.JN_EINVAL
