@@ -969,7 +969,7 @@ int64_t range_columns(int64_t cols, int32_t S) { return std::max<int64_t>(512, u
 jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std::vector<TokEntry>& io, bool train,
                      char* ws, TokPlan* P) {
   const int32_t G = (int32_t)io.size();
-  int64_t N = 0, logits = 0;
+  int64_t N = 0;
   bool dh = false;
   std::vector<TokDesc> desc(G);
   std::vector<int64_t> width(G), pat(G);
@@ -983,7 +983,6 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
     desc[g].vocab = heads[g].vocab;
     desc[g].first = (int32_t)N;
     N += io[g].n;
-    logits += (int64_t)io[g].n * up(heads[g].vocab, 64);
     dh = dh || (io[g].dh != nullptr && io[g].n > 0);
     if (train && io[g].n == 0) {
       desc[g].keep = (uint16_t*)io[g].dW;
@@ -992,19 +991,31 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
     }
   }
   P->N = (int32_t)N;
-  // pieces of the vocabulary, as many for every tenant, in whole ring tiles
-  // (the same share of every tenant's vocabulary, as large as the kept piece may be:
-  // the columns behind it are formed twice; 8,192 rows of 70,000 x 1,024 3,680 us with
-  // halves, 3,506 so; 5,000 of 120,000 x 128, whose products are short, 1,637 and 1,685)
-  const double share = std::min(1.0, (double)kTokPieceBytes / (2.0 * std::max<int64_t>(logits, 1)));
+  // pieces of the vocabulary: 256 columns (a ring tile) of every tenant, which 2^21
+  // entries' budget holds, and the same share of the rest of every vocabulary, in whole
+  // tiles; as large as the kept piece may be and no larger
+  // (the columns behind it are formed twice; 8,192 rows of 70,000 x 1,024 3,680 us with
+  // halves, 3,506 so)
+  auto columns = [&](int32_t g) { return up(heads[g].vocab, 64); };
+  auto least = [&](int32_t g) { return std::min<int64_t>(columns(g), 256); };
+  int64_t budget = kTokPieceBytes / 2, beyond = 0;
+  for (int32_t g = 0; g < G; ++g) {
+    budget -= io[g].n * least(g);
+    beyond += io[g].n * (columns(g) - least(g));
+  }
+  const bool whole = beyond <= budget;
+  const double share = whole ? 1.0 : (double)budget / beyond;
   int64_t piece = 0, pieces = 0;
   for (int32_t g = 0; g < G; ++g) {
     if (io[g].n == 0) continue;
     width[g] = heads[g].vocab;
     if (train) {
+      width[g] = whole ? columns(g) : least(g) + (int64_t)((columns(g) - least(g)) * share) / 256 * 256;
       // whole rounds of the weight gradient's ring tiles on 256 CUs, where there are some
-      const int64_t round = 256 * std::max(1, 256 / ((d + 255) / 256)), even = up((int64_t)std::ceil(heads[g].vocab * share), 256);
-      width[g] = std::min<int64_t>(share < 1.0 && even > round ? (even + round / 2) / round * round : even, up(heads[g].vocab, 64));
+      // (5,447 rows of 200,000 x 128 2,615 us without, 2,513 so; 5,000 of 160,001 x 1,024
+      // 5,540 and 5,280; 7,000 of 160,001 x 768 6,070 and 6,090)
+      const int64_t round = 256 * std::max(1, 256 / ((d + 255) / 256));
+      if (!whole && width[g] > round) width[g] = width[g] / round * round;
       const int64_t most = 0x7fffffff / (2 * d) / 256 * 256 - 256;  // a transposed panel of W within 32-bit offsets
       width[g] = std::min(width[g], most);
       pat[g] = piece;
