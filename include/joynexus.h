@@ -44,6 +44,8 @@
  *   - "host" arrays are read during the call and may be reused on return.
  *   - One context per stream and per host thread; contexts share nothing.
  *   - Weight matrices are row-major [out][in].
+ *   - Structs carry no size or version: callers are built against the header of the
+ *     library they load, and set fields they do not use to zero.
  */
 #ifndef JOYNEXUS_H
 #define JOYNEXUS_H
@@ -481,7 +483,8 @@ typedef struct jn_token_head {
  * what the feature holds there is not looked at.  Entries may name a row twice.
  * For row j of sample i of a packed batch the row is cu_seqlens[i] + j. */
 typedef struct jn_token_io {
-  int32_t n;               /* entries, 0 .. 2^20                                  */
+  int32_t n;               /* entries, 0 .. 2^20, with (n + 64) d < 2^30; at most 2^21 in
+                              all tenants of a call (JN_ESHAPE)                   */
   int32_t dw_f32;          /* 0: dW is bf16; 1: fp32, as jn_tenant_adamw_step reads it
                               (all tenants of a call alike)                       */
   const int32_t* rows;     /* device int32 [n]                                    */
@@ -494,19 +497,23 @@ typedef struct jn_token_io {
 
 /* Cross entropy of every tenant's targets over its own vocabulary, with gradients,
  * in pieces of the vocabulary: logits are reduced to the softmax's sums as they are
- * formed, and one piece of them, of about JN_TOKEN_PIECE_BYTES at most, is kept in
- * 16 bits (to 2^-10.5 of the exponential); the other pieces are formed again for the gradients.  So of the
- * workspace only the softmax's sums grow with vocabulary times targets, a sixteenth to
- * a thirty-second of what the logits would take in bf16.
+ * formed, and one piece of them, of JN_TOKEN_PIECE_BYTES at most, is kept in 16 bits (to
+ * 2^-10.5 of the exponential); the other pieces are formed again for the gradients.  So of
+ * the workspace only the softmax's sums grow with vocabulary times targets, 8 bytes for
+ * 128 to 32 columns: a thirty-second to an eighth of what the logits would take in bf16.
+ * Calls whose tenants all have few entries (at most 64, by d and vocabulary) may keep every
+ * logit instead: 16, 32 or 64 fp32 a row of the vocabulary, and with dh as many bytes again,
+ * in JN_TOKEN_PIECE_BYTES at most.
  * Nothing is averaged across tenants.  hidden: device bf16 [T][d], d a multiple of 64
  * in [64, 8192].  Precision: bf16 operands, fp32 accumulation, softmax statistics
  * and loss; the logits' gradient is rounded to bf16 before it meets h and W (as the
  * action experts' are) or, where every tenant of the call has few entries (the streaming
- * launches, at most 64), kept as two bf16 that are off by 2^-16 of it; bf16 results once.  Kernels only: the call may be captured into a HIP graph, whose
- * replays read rows, targets, hidden and W as they are then.  A call's results are
- * bitwise reproducible; a tenant's may differ in their last bits with the group it
- * is called in, whose sizes choose the launches' shapes and the pieces.  Errors
- * enqueue nothing. */
+ * launches, at most 64), kept as two bf16 that are off by 2^-16 of it; bf16 results once.
+ * Kernels only: the call may be captured into a HIP graph, whose replays read rows,
+ * targets, hidden and W as they are then.  A call's results are bitwise reproducible; a
+ * tenant's may differ with the group it is called in, whose sizes choose the launches and
+ * with them the order of sums and how the logits' gradient is rounded.  Errors enqueue
+ * nothing. */
 #define JN_TOKEN_PIECE_BYTES (1u << 30)
 jn_status jn_tokens_workspace_size(int32_t d, const jn_token_head* heads, const jn_token_io* io, int32_t G,
                                    size_t* bytes);
@@ -518,7 +525,7 @@ jn_status jn_tenant_tokens_fwd_bwd(jn_ctx* ctx, const void* hidden, int32_t T, i
  * [0, T) gets token -1 and logp 0.  Rows with NaN logits get some token of the
  * vocabulary and a NaN logp. */
 typedef struct jn_token_pick {
-  int32_t n;               /* entries, 0 .. 2^20      */
+  int32_t n;               /* entries, as jn_token_io's */
   int32_t reserved;
   const int32_t* rows;     /* device int32 [n]        */
   int32_t* token;          /* out: device int32 [n]   */
