@@ -91,8 +91,9 @@ typedef enum jn_op {
 } jn_op;
 
 /* One traced kernel launch.  For GEMMs (M, N, K) is the launch shape
- * (N counts gate and up rows for GeGLU); for the other kernels M is the
- * number of rows touched and N the row width. */
+ * (N counts gate and up rows for GeGLU; of a token launch over several tenants
+ * M is their rows' sum, N and K means over these rows); for the other kernels M is
+ * the number of rows touched and N the row width. */
 typedef struct jn_trace_entry {
   int32_t op, M, N, K;
   float ms;               /* device time between the bracketing events */

@@ -904,7 +904,21 @@ struct TokSet {  // one grouped launch
   size_t at = 0;  // of its problems in the table
   int32_t n = 0;
   TokTiles tiles;
+  int32_t M = 0, N = 0, K = 0;  // traced shape: rows of all problems, means over them
 };
+
+// The traced shape of a set's problems.
+void trace_shape(TokSet* set, const std::vector<GemmArgs>& v) {
+  double m = 0, n = 0, k = 0;
+  for (const GemmArgs& g : v) {
+    m += g.M;
+    n += (double)g.M * g.N;
+    k += (double)g.M * g.K;
+  }
+  set->M = (int32_t)std::min(m, 2147483647.0);
+  set->N = (int32_t)std::lround(n / m);
+  set->K = (int32_t)std::lround(k / m);
+}
 
 // Workspace offsets, the device table (descriptors, then the problems of every
 // launch) and the launches of a token-head call.  With `ws` null only the sizes.
@@ -912,7 +926,7 @@ struct TokPiece {
   TokSet grad, weights, rows;  // logit gradients (none for the kept piece), dW, dh
 };
 struct TokPlan {
-  int32_t N = 0, grad_blocks = 0;
+  int32_t N = 0, grad_blocks = 0, vocab = 0;  // vocab: its mean over the entries
   int64_t zero8 = 0;
   size_t table = 0, h = 0, labels = 0, zlab = 0, inv = 0, rows = 0, part = 0, index = 0, piece = 0, acc = 0, total = 0;
   bool planes = false;  // row gradients are summed from fp32 planes
@@ -959,6 +973,16 @@ jn_status check_tokens(jn_ctx* c, int32_t d, const jn_token_head* heads, const s
   return JN_OK;
 }
 
+// The tenants' vocabulary, its mean over their entries (traced).
+int32_t mean_vocab(const jn_token_head* heads, const TokEntry* io, int32_t G) {
+  double n = 0, nv = 0;
+  for (int32_t g = 0; g < G; ++g) {
+    n += io[g].n;
+    nv += (double)io[g].n * heads[g].vocab;
+  }
+  return n > 0 ? (int32_t)std::lround(nv / n) : 0;
+}
+
 // K ranges of the row gradients' products: with few rows their tiles leave most
 // CUs idle for as long as the vocabulary is.  Ranges of 512 columns at least; the
 // planes' sum reads 4 bytes an element and plane at the copy rate (4.8 TB/s).  100
@@ -991,6 +1015,7 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
     }
   }
   P->N = (int32_t)N;
+  P->vocab = mean_vocab(heads, io.data(), G);
   // pieces of the vocabulary: 256 columns (a ring tile) of every tenant, which 2^21
   // entries' budget holds, and the same share of the rest of every vocabulary, in whole
   // tiles; as large as the kept piece may be and no larger
@@ -1043,6 +1068,7 @@ jn_status token_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
     set->trans = trans;
     set->n = (int32_t)v.size();
     set->at = probs.size();
+    trace_shape(set, v);
     set->tiles = gemm_tokens_prepare(epi, trans, v.data(), set->n);
     if (set->tiles.total < 0) return fail(c, JN_ESHAPE, "a product of the token heads exceeds one launch's grid");
     probs.insert(probs.end(), v.begin(), v.end());
@@ -1229,7 +1255,7 @@ int32_t small_ldz(int32_t most) { return most > 32 ? 64 : most > 16 ? 32 : 16; }
 // Tenants of few rows: launches of up to kSmallTenants, workgroups by vocabulary.
 struct SmallPlan {
   std::vector<TokSmallSet> sets;
-  std::vector<int32_t> wgs, gwgs, grad_rows;  // of every set
+  std::vector<int32_t> wgs, gwgs, grad_rows, entries, vocab;  // of every set; vocab: its mean over the entries
   int32_t ldz = 16, N = 0, f32 = 0, planes = 0;
   size_t table = 0, inv = 0, acc = 0, total = 0;
   std::vector<char> bytes;         // descriptors and problems of the row gradients
@@ -1310,6 +1336,9 @@ jn_status small_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
       t.grad = (uint16_t*)(ws + take(4 * V * P->ldz));
     }
     P->sets.push_back(set);
+    P->vocab.push_back(mean_vocab(heads + g0, io.data() + g0, set.G));
+    P->entries.push_back(0);
+    for (int32_t k = 0; k < set.G; ++k) P->entries.back() += io[g0 + k].n;
     P->wgs.push_back(wgs);
     P->gwgs.push_back(gwgs);
     P->grad_rows.push_back(grad_rows);
@@ -1351,6 +1380,7 @@ jn_status small_plan(jn_ctx* c, int32_t d, const jn_token_head* heads, const std
     P->rows.epi = EPI_F32;
     P->rows.trans = GEMM_TRANS_X | GEMM_TRANS_W;
     P->rows.n = (int32_t)dx.size();
+    trace_shape(&P->rows, dx);
     P->rows.tiles = gemm_tokens_prepare(P->rows.epi, P->rows.trans, dx.data(), P->rows.n);
     if (P->rows.tiles.total < 0) return fail(c, JN_ESHAPE, "a product of the token heads exceeds one launch's grid");
     const size_t db = sizeof(TokDesc) * G, pb = sizeof(GemmArgs) * dx.size();
@@ -1428,7 +1458,7 @@ jn_status run_big(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const Tok
   hipStream_t s = c->stream;
   const TokDesc* const desc = (const TokDesc*)(w + P.table);
   const GemmArgs* const probs = (const GemmArgs*)(desc + G);
-  const int32_t V = ((const TokDesc*)P.bytes.data())[0].vocab;
+  const int32_t V = P.vocab;
   uint16_t* const h = (uint16_t*)(w + P.h);
   int32_t* const labels = (int32_t*)(w + P.labels);
   float* const inv = (float*)(w + P.inv);
@@ -1439,7 +1469,7 @@ jn_status run_big(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const Tok
                               train ? inv : nullptr),
             "token rows");
   for (const TokSet* t : {&P.scores, &P.more})
-    if (t->n > 0) JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, product(*t), "token scores");
+    if (t->n > 0) JN_TRACED(c, JN_OP_TOKEN_GEMM, t->M, t->N, t->K, product(*t), "token scores");
   if (!train) {
     JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, V, 0, launch_tok_pick(s, desc, G, P.N, labels), "token pick");
     return JN_OK;
@@ -1450,16 +1480,18 @@ jn_status run_big(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const Tok
             launch_tok_grad(s, desc, G, P.N, inv, (const TokRow*)(w + P.rows), P.grad_blocks, P.zero8),
             "token logit gradients");
   for (const TokPiece& p : P.pieces) {
-    if (p.grad.n > 0) JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, product(p.grad), "token gradients");
+    if (p.grad.n > 0) JN_TRACED(c, JN_OP_TOKEN_GEMM, p.grad.M, p.grad.N, p.grad.K, product(p.grad), "token gradients");
     if (p.rows.n > 0 && p.rows.epi != EPI_RESID_F32 && gemm_tokens_pair_ok(p.rows.tiles, p.weights.tiles)) {
-      JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d,
+      // (both products' operations on the weight gradient's rows)
+      const double rows = (double)p.rows.M * p.rows.K / p.weights.M;
+      JN_TRACED(c, JN_OP_TOKEN_GEMM, p.weights.M, d, p.weights.K + (int32_t)std::lround(rows),
                 launch_gemm_tokens_pair(s, p.rows.epi, probs + p.rows.at, p.rows.n, p.rows.tiles, p.weights.epi,
                                         probs + p.weights.at, p.weights.n, p.weights.tiles),
                 "token gradients");
       continue;
     }
     for (const TokSet* t : {&p.weights, &p.rows})
-      if (t->n > 0) JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, product(*t), "token gradients");
+      if (t->n > 0) JN_TRACED(c, JN_OP_TOKEN_GEMM, t->M, t->N, t->K, product(*t), "token gradients");
   }
   if (P.planes)
     JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 1, launch_tok_rows(s, desc, G, P.N, T, inv, (const float*)(w + P.acc), P.most_planes, d, false),
@@ -1472,19 +1504,19 @@ jn_status run_small(jn_ctx* c, const void* hidden, int32_t T, int32_t d, const S
   hipStream_t s = c->stream;
   for (size_t k = 0; k < P.sets.size(); ++k) {
     const TokSmallSet& set = P.sets[k];
-    const int32_t V = set.t[0].vocab;
+    const int32_t V = P.vocab[k], N = P.entries[k];
     if (P.wgs[k] > 0)
-      JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, launch_small_scores(s, set, P.wgs[k], P.ldz, hidden, T, d), "token scores");
+      JN_TRACED(c, JN_OP_TOKEN_GEMM, N, V, d, launch_small_scores(s, set, P.wgs[k], P.ldz, hidden, T, d), "token scores");
     if (train)
-      JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, V, d, launch_small_grads(s, set, P.gwgs[k], P.ldz, hidden, T, d, P.grad_rows[k], P.f32 != 0),
+      JN_TRACED(c, JN_OP_TOKEN_GEMM, N, V, d, launch_small_grads(s, set, P.gwgs[k], P.ldz, hidden, T, d, P.grad_rows[k], P.f32 != 0),
                 "token gradients");
     else
-      JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, V, 0, launch_small_pick(s, set, P.ldz, T), "token pick");
+      JN_TRACED(c, JN_OP_TOKEN_OTHER, N, V, 0, launch_small_pick(s, set, P.ldz, T), "token pick");
   }
   if (P.rows.n == 0) return JN_OK;
   const TokDesc* const desc = (const TokDesc*)(w + P.table);
   JN_HIP(c, launch_tok_table(s, w + P.table, P.bytes.data(), P.bytes.size()), "token table");
-  JN_TRACED(c, JN_OP_TOKEN_GEMM, P.N, d, 0,
+  JN_TRACED(c, JN_OP_TOKEN_GEMM, P.rows.M, P.rows.N, P.rows.K,
             launch_gemm_tokens(s, P.rows.epi, P.rows.trans, (const GemmArgs*)(desc + G), P.rows.n, P.rows.tiles),
             "token gradients");
   JN_TRACED(c, JN_OP_TOKEN_OTHER, P.N, d, 1,
