@@ -358,7 +358,7 @@ def _row_stride(t, rows: int, width: int) -> int:
     ld, one = t.stride()
     if one != 1 and shape[1] > 1:
         raise TypeError("the columns of a row must be adjacent")
-    return ld if rows > 1 else max(ld, shape[1])
+    return ld if rows > 1 else (max(ld, shape[1]) + 7) // 8 * 8  # (of one row any: nothing is that far away)
 
 
 def jn_qk_norm_rope(ctx: Context, qk: QKNormRope, x, pos, y):

@@ -1,7 +1,10 @@
 """Steps of one model, each with positions of its own: what one step ran with reaches no other."""
+from types import SimpleNamespace
+
 import pytest
 import torch
 
+from test_gpu_token_bits import check
 from test_gpu_token_step import Problem
 
 pytestmark = pytest.mark.gpu
@@ -79,3 +82,31 @@ def test_isolated_runs_of_a_group_with_positions(lib):
         mine = [k for k, t in enumerate(p.tenant) if t == g]
         assert all(torch.equal(one.out_hidden[j], st.out_hidden[k]) for j, k in enumerate(mine))
     p.check_hidden(st)
+
+
+def test_weight_gradients_grouped_and_isolated(lib):
+    """Element by element, each against the definition: no small row hides behind a large one."""
+    p = Problem(seed=14)
+    st = p.jstep.GroupStep(p.model, p.requests, p.targets, [0, 1], positions=p.positions)
+    iso = p.jstep.isolated_runs(p.model, p.requests, p.targets, [0, 1], ctx=st.ctx, positions=p.positions)
+    for step, k, g in ((st, 0, 0), (st, 1, 1), (iso[0], 0, 0), (iso[1], 0, 1)):
+        step.run()
+        torch.cuda.synchronize()
+        io, rows = step.ios[k], step.ios[k].rows.long()
+        assert io.dW.dtype is torch.float32 and int((rows < 0).sum()) == 2
+        t = SimpleNamespace(rows=io.rows, W=step.token_heads[k].W, targets=torch.where(rows < 0, -1, io.targets), dh=None,
+                            dW=io.dW.flatten())
+        check(t, step.hidden[rows.clamp(min=0)], 2.0 ** -16)
+
+
+def test_one_row_between_others(lib):
+    """Rows of odd widths, where there is one of them."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn(1, 3 * 64 + 5, generator=g, device="cuda").to(torch.bfloat16)
+    pos = torch.full((1,), 9, dtype=torch.int32, device="cuda")
+    qk = lib.QKNormRope(2, 1, 64, theta=1e4)
+    y, z = torch.full((1, 197), 7.0, dtype=torch.bfloat16, device="cuda"), torch.empty(1, 192, dtype=torch.bfloat16, device="cuda")
+    ctx = lib.Context()
+    lib.jn_qk_norm_rope(ctx, qk, x, pos, y)
+    lib.jn_qk_norm_rope(ctx, qk, x[:, :192].contiguous(), pos, z)
+    assert torch.equal(y[:, :192], z) and bool((y[:, 192:] == 7.0).all())
