@@ -1408,12 +1408,13 @@ struct TokSplit {
 // streaming launches keep all logits in fp32, and with row gradients their
 // gradients as two bf16: up to a piece's bytes.  Where W is small, latencies decide, and
 // the products' tiles work on more rows at a time.  Streaming and not, one tenant,
-// us, without row gradients: 32 rows of 4,000 x 768 21.2 and 23.7, of 120,000 x 2,048
-// 219 and 315; 64 rows of 256 x 2,048 22.9 and 25.4, 4,000 x 2,048 37.3 and 30.3,
-// 32,003 x 768 49.9 and 49.7, x 2,048 86 and 94.  With: 32 rows of 32,003 x 128
-// 41.0 and 34.3, 120,000 x 128 55.6 and 63.1, 32,003 x 2,048 114 and 119; 64 rows of
-// that 133 and 126, 120,000 x 768 159 and 165.  Decoding, 1 row of 1,024 x 768 11.7
-// and 14.5, 64 of 32,003 x 2,048 44.5 and 48.8.
+// us, without row gradients: 32 rows of 4,000 x 768 21.5 and 23.6, of 120,000 x 2,048
+// 218 and 317; 64 rows of 256 x 2,048 23.9 and 25.6, 4,000 x 2,048 39.0 and 30.3,
+// 32,003 x 768 52.6 and 49.0, x 2,048 90.0 and 90.3.  With: 32 rows of 32,003 x 128
+// 43.6 and 34.8, 120,000 x 128 63.0 and 64.5, 32,003 x 2,048 126 and 123; 5 of 60,000 x
+// 2,048 162 and 201; 64 rows of 32,003 x 2,048 144 and 127, 120,000 x 768 170 and 167,
+// 60,000 x 2,048 195 and 210.  Decoding, 1 row of 1,024 x 768 11.7 and 14.5, 64 of
+// 32,003 x 2,048 44.5 and 48.8.
 bool tokens_stream(int32_t d, const jn_token_head* heads, const std::vector<TokEntry>& io, bool train) {
   int32_t most = 1;
   for (const TokEntry& e : io) most = std::max(most, e.n);

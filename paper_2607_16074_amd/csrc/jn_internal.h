@@ -184,7 +184,9 @@ constexpr uint32_t kKeepNone = 65535;
 // `own` = p - 1 from logp in the target's column.  Dividing by the number of targets
 // is left to the products' results: bf16 holds the gradient of an unlikely target,
 // nearly -1 in every row, all but exactly, while a common factor's rounding would
-// be off by the same half step in all of them.
+// be off by the same half step in all of them.  One bf16, as the matrix cores' rate
+// has it: two (as the streaming launches hold it, whose time is W's) would double the
+// two products that these calls' time is, and over many rows the roundings average out.
 struct TokRow {
   float lse2;           // (+inf where the row has no target, and where a logit is)
   int32_t label;        // -1: no target, and p = 0
