@@ -65,8 +65,8 @@ def target_rows(maps: dict, slot: int, sample: np.ndarray, row: np.ndarray) -> n
     """Rows of the packed feature of (sample, row) pairs, samples in tenant ``slot``'s arrival order; -1 where the pair
     names no valid row (no target)."""
     first, end = int(maps["tenant_sample_off"][slot]), int(maps["tenant_sample_off"][slot + 1])
-    sample, row = np.asarray(sample, np.int64), np.asarray(row, np.int64)
-    out = np.full(np.broadcast(sample, row).shape, -1, np.int32)
+    sample, row = np.broadcast_arrays(np.asarray(sample, np.int64), np.asarray(row, np.int64))
+    out = np.full(sample.shape, -1, np.int32)
     ok = (sample >= 0) & (sample < end - first) & (row >= 0)
     i = maps["tenant_perm"][first + sample[ok]]
     out[ok] = np.where(row[ok] < maps["seqlens"][i], maps["cu_seqlens"][i] + row[ok], -1)

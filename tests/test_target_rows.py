@@ -18,3 +18,13 @@ def test_tenants_without_samples(lib, slot):
     assert step.target_rows(maps, slot, none, none).shape == (0,)
     far = np.array([2 ** 40, -2 ** 40, 0])
     assert step.target_rows(maps, slot, far, np.array([0, 0, 2 ** 40])).tolist() == [-1] * 3
+
+
+def test_one_sample_and_many_rows(lib):
+    from paper_2607_16074_amd import step
+    maps = {"tenant_sample_off": np.array([0, 0, 3]), "tenant_perm": np.array([0, 1, 2]), "seqlens": np.array([3, 5, 2]),
+            "cu_seqlens": np.array([0, 4, 12, 16])}
+    assert step.target_rows(maps, 1, 1, np.arange(-1, 6)).tolist() == [-1, 4, 5, 6, 7, 8, -1]
+    assert step.target_rows(maps, 1, np.array([[0], [2]]), np.arange(3)).tolist() == [[0, 1, 2], [12, 13, -1]]
+    assert step.target_rows(maps, 1, [2, 0], [1, 9]).tolist() == [13, -1]
+    assert int(step.target_rows(maps, 1, 2, 1)) == 13 and int(step.target_rows(maps, 0, 0, 0)) == -1
