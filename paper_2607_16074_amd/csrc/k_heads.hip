@@ -805,9 +805,10 @@ hipError_t launch_tok_grad(hipStream_t s, const TokDesc* d, int32_t G, int32_t N
 }
 
 // Eight elements of dh per STR lanes, the sum of the planes' PARTS rows of an entry
-// (two where its logits' gradient is two bf16); they share the planes (many planes are those
-// of few rows) and are added in pairs: 60 rows, 120,000 x 128 110 -> 76 us a call, 5
-// rows, 60,000 x 2,048 163 -> 159; 701 rows of 10 planes, 32,003 x 2,048 330 -> 339.
+// (two where its logits' gradient is two bf16); they share the planes (many planes
+// are those of few rows) and are added in pairs, against one lane each: 60 rows, 120,000 x
+// 128 74 -> 70 us a call, 20 of 100,003 x 128 147 -> 58, 5 of 60,000 x 2,048 176 -> 162;
+// 701 rows of 10 planes, 32,003 x 2,048 330 -> 339.
 template <int STR, int PARTS>
 __global__ __launch_bounds__(256) void tok_rows_kernel(const TokDesc* __restrict__ desc, int32_t G, int32_t N,
                                                        int32_t T, const float* __restrict__ inv, const float4* __restrict__ acc,
