@@ -345,7 +345,7 @@ def _verify_plain(t: dict):
         else:
             qx = q[first + cur, x].double()
             stands = tried & (u * qx * left < (px - a * qx).clamp(min=0))
-            fails = tried & ~stands
+            fails = tried & ~stands & (left > 0)
             before = torch.where(fails, a, before)
             a = torch.where(fails, a + left, a)
             left = torch.where(fails, rest(a).sum(1), left)
