@@ -398,17 +398,19 @@ def _call(s: dict):
         ws = torch.empty(jn.jn_tokens_verify_workspace_size(ios), dtype=torch.uint8, device=DEV)
         return lambda: jn.jn_tenant_tokens_verify(ctx, ios, ws), res
     cache = jn.KVCache(s["k"], s["v"])
-    batch = jn.KVBatch(s["pages"], s["past"], s["cu"], c["rows"], c["new"], s["parents"], c.get("mask") == "whole")
+    rows = c["rows"] if s["parents"] is None else c["live"]  # (every row of a call with trees has its parent)
+    batch = jn.KVBatch(s["pages"], s["past"], s["cu"], rows, c["new"], s["parents"], c.get("mask") == "whole")
     if c["kind"] == "keep":
         return (lambda: jn.jn_kv_keep(ctx, cache, batch, s["path"], s["count"], s["behind"]),
                 {"k": s["k"], "v": s["v"], "past": s["behind"]})
     if c["kind"] == "append":
         qk = jn.QKNormRope(c["heads"], c["kv"], c["hd"], EPS, s["gq"], s["gk"], c["theta"],
                            _sections(c) if s["pos"] is not None else ())
-        return (lambda: jn.jn_kv_append(ctx, cache, 0, batch, qk, s["x"], s["pos"], s["q"]),
+        pos = s["pos"][:rows] if s["pos"] is not None else None
+        return (lambda: jn.jn_kv_append(ctx, cache, 0, batch, qk, s["x"][:rows], pos, s["q"][:rows]),
                 {"q": s["q"], "k": s["k"], "v": s["v"]})
     ws = torch.empty(jn.jn_kv_attention_workspace_size(cache, batch, c["heads"]), dtype=torch.uint8, device=DEV)
-    return lambda: jn.jn_kv_attention(ctx, cache, 0, batch, c["heads"], s["q"], s["out"], ws), s["out"]
+    return lambda: jn.jn_kv_attention(ctx, cache, 0, batch, c["heads"], s["q"][:rows], s["out"][:rows], ws), s["out"]
 
 
 _contexts: dict = {}
