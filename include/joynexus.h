@@ -21,6 +21,12 @@
  *   jn_tenant_tokens_fwd_bwd the same for tenants that predict tokens: cross
  *                          entropy over the tenant's vocabulary and its gradients
  *   jn_tenant_tokens_decode the likeliest token of single rows (serving)
+ *   jn_kv_append, jn_kv_attention, jn_kv_keep, jn_backbone_extend
+ *                          the same backbone row by row: keys and values of
+ *                          earlier rows lie in a paged cache, and new rows (a
+ *                          token, a tree of drafted ones, a piece of a prompt)
+ *                          are appended to it and attend over it
+ *   jn_tenant_tokens_verify which drafted tokens stand, and the token after them
  *   jn_qk_norm_rope        head norms and rotation of queries and keys, the step
  *                          that jn_backbone_forward takes between projection and
  *                          attention, with its gradients (jn_qk_norm_rope_bwd)
@@ -87,7 +93,7 @@ typedef enum jn_op {
   JN_OP_GEMM_UP = 6, JN_OP_GEMM_DOWN = 7, JN_OP_POOL = 8, JN_OP_HEAD_FWD = 9, JN_OP_LOSS = 10,
   JN_OP_HEAD_BWD = 11, JN_OP_UNPACK = 12, JN_OP_EXPERT_GEMM = 13, JN_OP_EXPERT_ATTENTION = 14,
   JN_OP_EXPERT_OTHER = 15, JN_OP_OPTIMIZER = 16, JN_OP_ROPE = 17, JN_OP_QK = 18, JN_OP_TOKEN_GEMM = 19,
-  JN_OP_TOKEN_OTHER = 20
+  JN_OP_TOKEN_OTHER = 20, JN_OP_KV_APPEND = 21, JN_OP_KV_ATTENTION = 22, JN_OP_KV_KEEP = 23, JN_OP_TOKEN_VERIFY = 24
 } jn_op;
 
 /* One traced kernel launch.  For GEMMs (M, N, K) is the launch shape
@@ -327,6 +333,103 @@ jn_status jn_qk_norm_rope_workspace_size(const jn_qk_args* a, size_t* bytes);
 jn_status jn_qk_norm_rope_bwd(jn_ctx* ctx, const jn_qk_args* a, const void* x, const void* dy, void* dx,
                               float* dgq, float* dgk, void* ws, size_t ws_bytes);
 
+/* --------------------------------------- keys and values of earlier rows --- */
+
+/* A paged cache of keys and values: element e of key head h in row r of page g of
+ * layer l is k[l * ld_layer + g * ld_page + (h * page_size + r) * head_dim + e], values
+ * alike.  Pages are shared by all sequences; which holds what is the caller's to say. */
+typedef struct jn_kv_cache {
+  int32_t n_layers, n_pages;
+  int32_t page_size;       /* rows of a page: 16, 32, 64, 128 or 256 (JN_EUNSUPPORTED) */
+  int32_t n_kv_heads;
+  int32_t head_dim;        /* a multiple of 16 in [16, 256]; for attention 32, 64, 128 or 256 (JN_EUNSUPPORTED) */
+  int32_t reserved;
+  int64_t ld_page;         /* elements between pages, >= n_kv_heads * page_size * head_dim  */
+  int64_t ld_layer;        /* elements between layers: layer after layer (>= n_pages * ld_page) or the
+                              layers of a page together (ld_page >= n_layers * ld_layer); unused with one layer.
+                              Both multiples of 8 (JN_EUNSUPPORTED)                         */
+  void* k;                 /* device bf16, 16-byte aligned */
+  void* v;
+} jn_kv_cache;
+
+/* New rows of cached sequences.  Sequence s has past[s] rows in the cache; its new
+ * ones are rows cu_rows[s] .. cu_rows[s + 1] - 1 of the call, of which row j is place
+ * past[s] + j of the sequence, which is row (place % page_size) of page
+ * pages[s][place / page_size].  All device arrays are read when the kernels run, so a
+ * captured call follows them.  What they hold is bounded there: cu_rows is taken
+ * within [0, rows], at most max_new rows of a sequence, past within [0, max_pages *
+ * page_size]; a place behind max_pages pages, or in a page outside [0, n_pages), is
+ * neither written nor seen.  Rows behind the last sequence's are not touched.  Pages that
+ * two sequences of a call write are the caller's mistake; reading one together is not.
+ *   whole     1: the new rows of a sequence see each other (and the cached ones);
+ *             0: each sees the earlier ones and itself
+ *   parents   (or NULL, and whole 0) the new rows are trees: row j sees itself, and what
+ *             row parents[cu_rows[s] + j] of the sequence (an index in it) sees.  Where that
+ *             is not an earlier row (-1 is usual) it hangs on the cached rows. */
+#define JN_KV_TREE_ROWS 256
+typedef struct jn_kv_batch {
+  int32_t n_seqs;          /* 0 .. 65535                                        */
+  int32_t max_pages;       /* >= 1; max_pages * page_size <= 2^30 (JN_ESHAPE)   */
+  int32_t rows;            /* rows of the call, 0 .. 2^26 - 4 (JN_ESHAPE)       */
+  int32_t max_new;         /* >= 1: the most new rows of a sequence; with parents at most
+                              JN_KV_TREE_ROWS (JN_EUNSUPPORTED)                 */
+  int32_t whole;
+  int32_t reserved;
+  const int32_t* pages;    /* device int32 [n_seqs][max_pages] */
+  const int32_t* past;     /* device int32 [n_seqs]            */
+  const int32_t* cu_rows;  /* device int32 [n_seqs + 1], ascending */
+  const int32_t* parents;  /* device int32 [rows]              */
+} jn_kv_batch;
+
+/* Appends the new rows' keys and values to a layer of the cache: rows of x are
+ * [n_heads query | n_kv_heads key | n_kv_heads value] heads; queries and keys pass
+ * norms and rotation as jn_qk_norm_rope says (or neither: gq, gk NULL and rope_theta
+ * 0), queries go to rows of q, keys and values to their places.  a: rows, n_kv_heads
+ * and head_dim as the batch's and the cache's; ld_in of x, ld_out of q; pos NULL (one
+ * axis): past[s] + j, or past[s] + the row's depth in its tree.  q: device bf16, may be x
+ * where ld_in == ld_out, or NULL with n_heads 0. */
+jn_status jn_kv_append(jn_ctx* ctx, const jn_kv_cache* cache, int32_t layer, const jn_kv_batch* b, const jn_qk_args* a,
+                       const void* x, void* q);
+
+typedef struct jn_kv_attn {
+  int32_t n_heads;         /* a multiple of the cache's n_kv_heads: query head h reads
+                              key head h / (n_heads / n_kv_heads)                   */
+  float scale;             /* of the scores, finite and >= 0; 0: 1 / sqrt(head_dim) */
+  int64_t ld_q, ld_out;    /* elements between rows, multiples of 8 (JN_EUNSUPPORTED) */
+} jn_kv_attn;
+
+/* out = softmax(scale q k^T) v of every new row (whose keys and values are in the
+ * cache) over the rows that it sees: all cached ones, and the new ones that jn_kv_batch
+ * names.  Rows that see nothing, and rows whose every score is -inf, are zeros; what the
+ * cache holds in places that a row does not see, NaN too, leaves it alone.  Precision:
+ * as jn_backbone_forward's attention (bf16 operands, fp32 scores, statistics and sums,
+ * probabilities rounded to bf16), bf16 results.  q: device bf16, rows of n_heads heads; out
+ * alike, another buffer.  Results are bitwise reproducible; a sequence's may differ with
+ * the batch it is called in, whose lengths decide where the work is split. */
+jn_status jn_kv_attention_workspace_size(const jn_kv_cache* cache, const jn_kv_batch* b, const jn_kv_attn* a,
+                                         size_t* bytes);
+jn_status jn_kv_attention(jn_ctx* ctx, const jn_kv_cache* cache, int32_t layer, const jn_kv_batch* b,
+                          const jn_kv_attn* a, const void* q, void* out, void* ws, size_t ws_bytes);
+
+/* Keeps a branch of every sequence's new rows, in all layers: keys and values of new
+ * row path[s][k] move to place past[s] + k for k < n_path[s] (n_path taken within [0,
+ * max_path]), and past_out[s] = past[s] + n_path[s] (past_out may be past, or NULL).
+ * A path ascends, path[s][k] >= k, as those of jn_tenant_tokens_verify do; an entry outside
+ * k .. max_new - 1, or below an earlier one, moves nothing. */
+jn_status jn_kv_keep(jn_ctx* ctx, const jn_kv_cache* cache, const jn_kv_batch* b, const int32_t* path, int32_t max_path,
+                     const int32_t* n_path, int32_t* past_out);
+
+/* jn_backbone_forward over new rows of cached sequences: embeds (device bf16
+ * [rows][d]) pass the layers, every layer appends its keys and values to its layer of
+ * the cache and attends over them.  bb: pos [rows][rope_axes] or NULL as in
+ * jn_kv_append; with causal 0 the batch is `whole`, with 1 it is not.  The cache has bb's
+ * layers, key heads and head width (JN_EINCOMPAT).  hidden: device bf16 [rows][d]; its
+ * rows behind the last sequence's hold nothing of meaning. */
+jn_status jn_backbone_extend_workspace_size(const jn_backbone* bb, const jn_kv_cache* cache, const jn_kv_batch* b,
+                                            size_t* bytes);
+jn_status jn_backbone_extend(jn_ctx* ctx, const jn_backbone* bb, const jn_kv_cache* cache, const jn_kv_batch* b,
+                             const void* embeds, void* hidden, void* ws, size_t ws_bytes);
+
 /* --------------------------------------------------------------- heads --- */
 
 /* A tenant-private MLP action head: y = W_L gelu(... gelu(W_1 p + b_1) ...) + b_L
@@ -537,6 +640,46 @@ jn_status jn_tokens_decode_workspace_size(int32_t d, const jn_token_head* heads,
                                           size_t* bytes);
 jn_status jn_tenant_tokens_decode(jn_ctx* ctx, const void* hidden, int32_t T, int32_t d, const jn_token_head* heads,
                                   const jn_token_pick* io, int32_t G, void* ws, size_t ws_bytes);
+
+/* Verification of drafted tokens.  A tree's nodes are rows cu_nodes[t] ..
+ * cu_nodes[t + 1] - 1 (taken within [0, n], at most max_path of a chain and
+ * JN_KV_TREE_ROWS of a tree): node 0 is a token that stands, and a node's children, the nodes
+ * whose parents entry names it (NULL: node j - 1), are drafts of the token behind it.
+ * From node 0 on, the children x of the last standing node c are tried in their order,
+ * with the node's number u, until one stands and is the last:
+ *   drawn drafts (q: the probabilities that children were drawn from, independently),
+ *     with a = 0, T = 1 at first:  x stands if u q[c][x] T < max(p[c][x] - a q[c][x], 0),
+ *     else a += T, T = sum_i max(p[c][i] - a q[c][i], 0);
+ *   picked drafts (q NULL), with T = 1:  x stands if u T < p[c][x], else T -= p[c][x] and
+ *     p[c][x] counts as 0 from there on;
+ *   likeliest tokens (p NULL): x stands if x == greedy[c].
+ * So a standing token's chance is the target's p.  Behind the last standing node comes
+ * `next`: the lowest token i with sum_{k <= i} w_k > r sum_k w_k for the tree's number r, w
+ * what is left of p[c] (its max(p - a q, 0), or p without the rejected tokens; the w before
+ * the last rejection where that leaves nothing), or greedy[c]; -1 where no w is positive.  A
+ * node 0 alone draws a token from p.  Weights that are NaN or negative count as 0; children
+ * whose token is outside [0, vocab) are passed over.  Products and sums are formed in 64 bits, in a fixed order. */
+typedef struct jn_token_verify {
+  int32_t n_trees, n;      /* n: nodes of all trees, with n * vocab < 2^40 (JN_ESHAPE) */
+  int32_t vocab;           /* 1 .. 2^24 */
+  int32_t max_path;        /* >= 1 */
+  int64_t ld_p, ld_q;      /* elements between rows of p and q, >= vocab */
+  const int32_t* cu_nodes; /* device int32 [n_trees + 1], ascending */
+  const int32_t* parents;  /* device int32 [n] or NULL: indices in the tree, earlier than the node's own
+                              (a node without such a parent is not reached) */
+  const int32_t* tokens;   /* device int32 [n]; node 0's is not looked at */
+  const float* p;          /* device fp32 [n][ld_p] or NULL: the target's probabilities behind each node */
+  const float* q;          /* device fp32 [n][ld_q] or NULL: the draft's */
+  const int32_t* greedy;   /* device int32 [n], where p is NULL */
+  const float* u;          /* device fp32 [n], in [0, 1); node 0's is not looked at; where p is not NULL */
+  const float* r;          /* device fp32 [n_trees], in [0, 1); where p is not NULL */
+  int32_t* path;           /* out: device int32 [n_trees][max_path], standing nodes, -1 behind them */
+  int32_t* n_path;         /* out: device int32 [n_trees] (at most max_path: the walk ends there) */
+  int32_t* next;           /* out: device int32 [n_trees]; of a tree without nodes -1, and n_path 0 */
+} jn_token_verify;
+
+jn_status jn_tokens_verify_workspace_size(const jn_token_verify* v, int32_t G, size_t* bytes);
+jn_status jn_tenant_tokens_verify(jn_ctx* ctx, const jn_token_verify* v, int32_t G, void* ws, size_t ws_bytes);
 
 /* ---------------------------------------------------- tenant optimizer --- */
 

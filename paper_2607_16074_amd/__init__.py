@@ -16,8 +16,8 @@ import numpy as np
 from . import _abi
 from ._abi import (EXPERT_LAYER_FIELDS, JN_OK, STATUS_NAMES, jn_adamw_tenant, jn_backbone, jn_expert, jn_expert_io,
                    jn_expert_layer, jn_expert_layer_grads, jn_head, jn_head_io, jn_layer, jn_pack_opts,
-                   jn_pack_sizes, jn_packed, jn_qk_args, jn_request, jn_tenant, jn_token_head, jn_token_io,
-                   jn_token_pick)
+                   jn_kv_attn, jn_kv_batch, jn_kv_cache, jn_pack_sizes, jn_packed, jn_qk_args, jn_request, jn_tenant,
+                   jn_token_head, jn_token_io, jn_token_pick, jn_token_verify)
 
 _lib = _abi.load()
 
@@ -28,6 +28,9 @@ __all__ = [
     "HEADS_SCRATCH_BYTES", "jn_unpack",
     "Expert", "ExpertIO", "jn_pack_tenant_sizes", "jn_experts_workspace_size", "jn_tenant_experts_fwd_bwd",
     "QKNormRope", "jn_qk_norm_rope", "jn_qk_norm_rope_workspace_size", "jn_qk_norm_rope_bwd",
+    "KVCache", "KVBatch", "jn_kv_append", "jn_kv_attention_workspace_size", "jn_kv_attention", "jn_kv_keep",
+    "jn_backbone_extend_workspace_size", "jn_backbone_extend",
+    "TokenVerify", "jn_tokens_verify_workspace_size", "jn_tenant_tokens_verify",
     "TokenHead", "TokenIO", "TokenPick", "jn_tokens_workspace_size", "jn_tenant_tokens_fwd_bwd",
     "jn_tokens_decode_workspace_size", "jn_tenant_tokens_decode",
     "AdamWTenant", "jn_adamw_workspace_size", "jn_tenant_adamw_step",
@@ -393,6 +396,117 @@ def jn_qk_norm_rope_bwd(ctx: Context, qk: QKNormRope, x, pos, dy, dx, dgq, dgk, 
                                     _ptr(ws), _bytes(ws)), ctx)
 
 
+# ----------------------------------------- keys and values of earlier rows ---
+
+def _entries(name: str, t, dtype, n: int):
+    if t is None or t.dtype is not dtype or not t.is_contiguous() or t.numel() != n:
+        raise TypeError(f"{name} must be a contiguous {dtype} tensor of {n} elements")
+    return t.data_ptr()
+
+
+class KVCache:
+    """A paged cache: device bf16 ``k`` and ``v`` [layers, pages, key heads, page size, head width], of equal strides,
+    where heads, rows and elements of a page lie together."""
+
+    def __init__(self, k, v):
+        t = _dtypes()
+        if k.dtype is not t.bfloat16 or v.dtype is not t.bfloat16 or k.dim() != 5 or v.shape != k.shape:
+            raise TypeError("k and v must be bfloat16 tensors [layers, pages, heads, page size, head width]")
+        layers, pages, kv, size, hd = k.shape
+        ld_layer, ld_page, *inner = k.stride()
+        if inner != [size * hd, hd, 1] or v.stride() != k.stride():
+            raise TypeError("a page's heads and rows must lie together, in both caches alike")
+        self.k, self.v = k, v
+        s = jn_kv_cache()
+        s.n_layers, s.n_pages, s.page_size, s.n_kv_heads, s.head_dim = layers, pages, size, kv, hd
+        # (of one page or layer any distance: nothing is that far away)
+        s.ld_page = ld_page if pages > 1 else max(ld_page, kv * size * hd)
+        s.ld_layer = ld_layer
+        s.k, s.v = k.data_ptr(), v.data_ptr()
+        self.struct = s
+
+
+class KVBatch:
+    """New rows of cached sequences, all device int32: ``pages`` [sequences, pages of each], ``past`` (cached rows) and
+    ``cu_rows`` [sequences + 1]; ``rows`` of a call, at most ``max_new`` of a sequence.  ``parents`` [rows]: trees (indices in
+    the sequence's new rows); ``whole``: its new rows all see each other."""
+
+    def __init__(self, pages, past, cu_rows, rows: int, max_new: int, parents=None, whole: bool = False):
+        t = _dtypes()
+        if pages.dim() != 2:
+            raise TypeError("pages must be [sequences, pages of each]")
+        n, per = pages.shape
+        self.pages, self.past, self.cu_rows, self.parents = pages, past, cu_rows, parents
+        s = jn_kv_batch()
+        s.n_seqs, s.max_pages, s.rows, s.max_new, s.whole = int(n), int(per), int(rows), int(max_new), 1 if whole else 0
+        s.pages = _entries("pages", pages, t.int32, n * per)
+        s.past = _entries("past", past, t.int32, n)
+        s.cu_rows = _entries("cu_rows", cu_rows, t.int32, n + 1)
+        s.parents = _entries("parents", parents, t.int32, s.rows) if parents is not None else None
+        self.struct = s
+
+
+def jn_kv_append(ctx: Context, cache: KVCache, layer: int, batch: KVBatch, qk: QKNormRope, x, pos, q):
+    """Rows of ``x`` (query, key and value heads): norms and rotation as ``qk`` says, keys and values to the cache,
+    queries to ``q`` (``x`` itself, another, or None without query heads).  ``pos`` None: the rows' own places."""
+    rows, s = batch.struct.rows, qk.struct
+    a = jn_qk_args.from_buffer_copy(s)
+    a.rows = rows
+    a.pos = _positions(pos, rows, qk.axes)
+    a.ld_in = _row_stride(x, rows, qk.width + s.n_kv_heads * s.head_dim)
+    if q is not None:
+        a.ld_out = _row_stride(q, rows, s.n_heads * s.head_dim)
+    _check(_lib.jn_kv_append(ctx.handle, C.byref(cache.struct), layer, C.byref(batch.struct), a, x.data_ptr(), _ptr(q)), ctx)
+
+
+def _kv_attn(cache: KVCache, n_heads: int, scale: float):
+    a = jn_kv_attn()
+    a.n_heads, a.scale = int(n_heads), float(scale)
+    a.ld_q = a.ld_out = a.n_heads * cache.struct.head_dim
+    return a
+
+
+def jn_kv_attention_workspace_size(cache: KVCache, batch: KVBatch, n_heads: int) -> int:
+    n = C.c_size_t()
+    _check(_lib.jn_kv_attention_workspace_size(C.byref(cache.struct), C.byref(batch.struct), _kv_attn(cache, n_heads, 0.0),
+                                               C.byref(n)), what="jn_kv_attention_workspace_size")
+    return int(n.value)
+
+
+def jn_kv_attention(ctx: Context, cache: KVCache, layer: int, batch: KVBatch, n_heads: int, q, out, ws, scale: float = 0.0):
+    """``q`` and ``out``: bf16 [rows, >= n_heads x head width]; ``scale`` 0: 1 / sqrt(head width)."""
+    a, rows = _kv_attn(cache, n_heads, scale), batch.struct.rows
+    a.ld_q, a.ld_out = _row_stride(q, rows, a.ld_q), _row_stride(out, rows, a.ld_out)
+    _check(_lib.jn_kv_attention(ctx.handle, C.byref(cache.struct), layer, C.byref(batch.struct), a, q.data_ptr(),
+                                out.data_ptr(), _ptr(ws), _bytes(ws)), ctx)
+
+
+def jn_kv_keep(ctx: Context, cache: KVCache, batch: KVBatch, path, n_path, past_out=None):
+    """``path`` int32 [sequences, most rows], ``n_path`` [sequences]; ``past_out`` [sequences]: the new ``past``."""
+    t, n = _dtypes(), batch.struct.n_seqs
+    if path.dim() != 2:
+        raise TypeError("path must be [sequences, most rows]")
+    most = int(path.shape[1])
+    _check(_lib.jn_kv_keep(ctx.handle, C.byref(cache.struct), C.byref(batch.struct), _entries("path", path, t.int32, n * most),
+                           most, _entries("n_path", n_path, t.int32, n),
+                           _entries("past_out", past_out, t.int32, n) if past_out is not None else None), ctx)
+
+
+def jn_backbone_extend_workspace_size(bb: Backbone, cache: KVCache, batch: KVBatch, pos=None) -> int:
+    n = C.c_size_t()
+    _check(_lib.jn_backbone_extend_workspace_size(C.byref(_backbone_of(bb, batch.struct.rows, pos)), C.byref(cache.struct),
+                                                  C.byref(batch.struct), C.byref(n)), what="jn_backbone_extend_workspace_size")
+    return int(n.value)
+
+
+def jn_backbone_extend(ctx: Context, bb: Backbone, cache: KVCache, batch: KVBatch, embeds, hidden, ws, pos=None):
+    """``embeds`` and ``hidden``: contiguous bf16 [rows, d]; ``pos`` as in ``jn_backbone_forward``."""
+    t, rows = _dtypes(), batch.struct.rows
+    _check(_lib.jn_backbone_extend(ctx.handle, C.byref(_backbone_of(bb, rows, pos)), C.byref(cache.struct),
+                                   C.byref(batch.struct), _entries("embeds", embeds, t.bfloat16, rows * bb.d),
+                                   _entries("hidden", hidden, t.bfloat16, rows * bb.d), _ptr(ws), _bytes(ws)), ctx)
+
+
 # --------------------------------------------------------------- heads ------
 
 class Head:
@@ -550,12 +664,6 @@ def jn_tenant_experts_fwd_bwd(ctx: Context, packed: Packed, hidden, ex: Sequence
 
 # --------------------------------------------------------- token heads ------
 
-def _entries(name: str, t, dtype, n: int):
-    if t is None or t.dtype is not dtype or not t.is_contiguous() or t.numel() != n:
-        raise TypeError(f"{name} must be a contiguous {dtype} tensor of {n} elements")
-    return t.data_ptr()
-
-
 class TokenHead:
     """A tenant's token head: device bf16 W [vocab, d]."""
 
@@ -647,6 +755,63 @@ def jn_tokens_decode_workspace_size(heads: Sequence[TokenHead], picks: Sequence[
 
 def jn_tenant_tokens_decode(ctx: Context, hidden, heads: Sequence[TokenHead], picks: Sequence[TokenPick], ws):
     _tokens_call(_lib.jn_tenant_tokens_decode, ctx, hidden, heads, picks, TokenPick, ws)
+
+
+class TokenVerify:
+    """A tenant's trees of drafted tokens (device int32 ``cu_nodes`` [trees + 1], ``tokens`` and ``parents`` [n], no
+    parents: chains) and what they are held against: fp32 ``p`` [n, vocab] with the numbers ``u`` [n] and ``r`` [trees]
+    and, where the drafts were drawn, their ``q`` [n, vocab]; or the likeliest tokens ``greedy`` [n].  Outputs, int32:
+    ``path`` [trees, most nodes], ``n_path`` and ``next`` [trees]."""
+
+    def __init__(self, cu_nodes, tokens, path, n_path, next, p=None, greedy=None, q=None, u=None, r=None, parents=None,
+                 vocab: int = None):
+        t = _dtypes()
+        self.buffers = (cu_nodes, tokens, path, n_path, next, p, greedy, q, u, r, parents)
+        s = jn_token_verify()
+        n, trees = s.n, s.n_trees = int(tokens.numel()), int(cu_nodes.numel()) - 1
+        if trees < 0 or path.dim() != 2:
+            raise TypeError("cu_nodes must be [trees + 1], path [trees, most nodes]")
+        s.max_path = int(path.shape[1])
+        rows = lambda name, x: self._rows(name, x, n, t)  # noqa: E731
+        if p is not None:
+            s.p, s.ld_p = rows("p", p)
+            s.u, s.r = _entries("u", u, t.float32, n), _entries("r", r, t.float32, trees)
+        if q is not None:
+            s.q, s.ld_q = rows("q", q)
+        if (p is None and vocab is None) or (p is not None and q is not None and p.shape != q.shape):
+            raise TypeError("p and q must be of one vocabulary; without p it is to be named")
+        s.vocab = int(vocab if vocab is not None else p.shape[1])
+        if p is not None and s.vocab > p.shape[1]:
+            raise TypeError(f"p holds {p.shape[1]} probabilities, not {s.vocab}")
+        s.cu_nodes = _entries("cu_nodes", cu_nodes, t.int32, trees + 1)
+        s.tokens = _entries("tokens", tokens, t.int32, n)
+        s.greedy = _entries("greedy", greedy, t.int32, n) if greedy is not None else None
+        s.parents = _entries("parents", parents, t.int32, n) if parents is not None else None
+        s.path = _entries("path", path, t.int32, trees * s.max_path)
+        s.n_path, s.next = _entries("n_path", n_path, t.int32, trees), _entries("next", next, t.int32, trees)
+        self.struct = s
+
+    @staticmethod
+    def _rows(name, x, n, t):
+        if x.dtype is not t.float32 or x.dim() != 2 or x.shape[0] != n or (x.stride(1) != 1 and x.shape[1] > 1):
+            raise TypeError(f"{name} must be a float32 tensor [{n}, vocab] of adjacent columns")
+        if n > 1 and x.stride(0) < x.shape[1]:
+            raise TypeError(f"rows of {name} overlap")
+        return x.data_ptr(), x.stride(0) if n > 1 else x.shape[1]
+
+
+def _verify_array(ios: Sequence[TokenVerify]):
+    return (jn_token_verify * len(ios))(*[x.struct for x in ios]), len(ios)
+
+
+def jn_tokens_verify_workspace_size(ios: Sequence[TokenVerify]) -> int:
+    n = C.c_size_t()
+    _check(_lib.jn_tokens_verify_workspace_size(*_verify_array(ios), C.byref(n)), what="jn_tokens_verify_workspace_size")
+    return int(n.value)
+
+
+def jn_tenant_tokens_verify(ctx: Context, ios: Sequence[TokenVerify], ws):
+    _check(_lib.jn_tenant_tokens_verify(ctx.handle, *_verify_array(ios), _ptr(ws), _bytes(ws)), ctx)
 
 
 # ---------------------------------------------------- tenant optimizer ------

@@ -28,6 +28,9 @@ EXPORTS = (
     "jn_qk_norm_rope", "jn_qk_norm_rope_workspace_size", "jn_qk_norm_rope_bwd",
     "jn_tokens_workspace_size", "jn_tenant_tokens_fwd_bwd",
     "jn_tokens_decode_workspace_size", "jn_tenant_tokens_decode",
+    "jn_kv_append", "jn_kv_attention_workspace_size", "jn_kv_attention", "jn_kv_keep",
+    "jn_backbone_extend_workspace_size", "jn_backbone_extend",
+    "jn_tokens_verify_workspace_size", "jn_tenant_tokens_verify",
     "jn_adamw_workspace_size", "jn_tenant_adamw_step",
     "jn_unpack",
     "jn_collector_create", "jn_collector_destroy", "jn_collector_submit", "jn_collector_poll",
@@ -40,7 +43,7 @@ EXPORTS = (
 OPS = {1: "pack", 2: "rmsnorm", 3: "gemm_qkv", 4: "attention", 5: "gemm_o", 6: "gemm_up", 7: "gemm_down",
        8: "pool", 9: "head_fwd", 10: "loss", 11: "head_bwd", 12: "unpack", 13: "expert_gemm",
        14: "expert_attention", 15: "expert_other", 16: "optimizer", 17: "rope", 18: "qk_norm_rope",
-       19: "token_gemm", 20: "token_other"}
+       19: "token_gemm", 20: "token_other", 21: "kv_append", 22: "kv_attention", 23: "kv_keep", 24: "token_verify"}
 
 
 class jn_trace_entry(C.Structure):
@@ -118,6 +121,29 @@ class jn_token_io(C.Structure):
 class jn_token_pick(C.Structure):
     _fields_ = [("n", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_void_p), ("token", C.c_void_p),
                 ("logp", C.c_void_p)]
+
+
+class jn_kv_cache(C.Structure):
+    _fields_ = [("n_layers", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("reserved", C.c_int32), ("ld_page", C.c_int64), ("ld_layer", C.c_int64),
+                ("k", C.c_void_p), ("v", C.c_void_p)]
+
+
+class jn_kv_batch(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("rows", C.c_int32), ("max_new", C.c_int32),
+                ("whole", C.c_int32), ("reserved", C.c_int32), ("pages", C.c_void_p), ("past", C.c_void_p),
+                ("cu_rows", C.c_void_p), ("parents", C.c_void_p)]
+
+
+class jn_kv_attn(C.Structure):
+    _fields_ = [("n_heads", C.c_int32), ("scale", C.c_float), ("ld_q", C.c_int64), ("ld_out", C.c_int64)]
+
+
+class jn_token_verify(C.Structure):
+    _fields_ = [("n_trees", C.c_int32), ("n", C.c_int32), ("vocab", C.c_int32), ("max_path", C.c_int32),
+                ("ld_p", C.c_int64), ("ld_q", C.c_int64), ("cu_nodes", C.c_void_p), ("parents", C.c_void_p),
+                ("tokens", C.c_void_p), ("p", C.c_void_p), ("q", C.c_void_p), ("greedy", C.c_void_p), ("u", C.c_void_p),
+                ("r", C.c_void_p), ("path", C.c_void_p), ("n_path", C.c_void_p), ("next", C.c_void_p)]
 
 
 class jn_head(C.Structure):
@@ -213,6 +239,14 @@ def load(path: str = LIB_PATH) -> C.CDLL:
                                                       P(C.c_size_t)]),
         "jn_tenant_tokens_decode": (C.c_int, [V, V, C.c_int32, C.c_int32, P(jn_token_head), P(jn_token_pick),
                                               C.c_int32, V, C.c_size_t]),
+        "jn_kv_append": (C.c_int, [V, P(jn_kv_cache), C.c_int32, P(jn_kv_batch), P(jn_qk_args), V, V]),
+        "jn_kv_attention_workspace_size": (C.c_int, [P(jn_kv_cache), P(jn_kv_batch), P(jn_kv_attn), P(C.c_size_t)]),
+        "jn_kv_attention": (C.c_int, [V, P(jn_kv_cache), C.c_int32, P(jn_kv_batch), P(jn_kv_attn), V, V, V, C.c_size_t]),
+        "jn_kv_keep": (C.c_int, [V, P(jn_kv_cache), P(jn_kv_batch), V, C.c_int32, V, V]),
+        "jn_backbone_extend_workspace_size": (C.c_int, [P(jn_backbone), P(jn_kv_cache), P(jn_kv_batch), P(C.c_size_t)]),
+        "jn_backbone_extend": (C.c_int, [V, P(jn_backbone), P(jn_kv_cache), P(jn_kv_batch), V, V, V, C.c_size_t]),
+        "jn_tokens_verify_workspace_size": (C.c_int, [P(jn_token_verify), C.c_int32, P(C.c_size_t)]),
+        "jn_tenant_tokens_verify": (C.c_int, [V, P(jn_token_verify), C.c_int32, V, C.c_size_t]),
         "jn_adamw_workspace_size": (C.c_int, [P(jn_adamw_tenant), C.c_int32, P(C.c_size_t)]),
         "jn_tenant_adamw_step": (C.c_int, [V, P(jn_adamw_tenant), C.c_int32, V, C.c_size_t]),
         "jn_unpack": (C.c_int, [V, P(jn_packed), P(jn_request), C.c_int32, V, C.c_size_t, P(V)]),

@@ -676,35 +676,14 @@ jn_status jn_backbone_workspace_size(const jn_backbone* bb, int32_t T, size_t* b
   return JN_OK;
 }
 
-jn_status jn_backbone_forward(jn_ctx* c, const jn_backbone* bb, const jn_packed* p, void* hidden, void* ws,
-                              size_t ws_bytes) {
-  if (!c) return JN_EINVAL;
-  jn_status st = check_backbone(c, bb);
-  if (st != JN_OK) return st;
-  if (!valid_packed(p) || !p->tokens) return fail(c, JN_EINVAL, "invalid packed batch");
-  if (p->d != bb->d) return fail(c, JN_EINCOMPAT, "packed width %d != backbone width %d", p->d, bb->d);
-  if (!hidden || !ws) return fail(c, JN_EINVAL, "null hidden or workspace");
-  BbLayout L = bb_layout(bb, p->T);
-  if (ws_bytes < L.total) return fail(c, JN_ENOSPACE, "workspace %zu B < %zu B", ws_bytes, L.total);
-  if (((uintptr_t)ws) % 256 != 0 || ((uintptr_t)hidden) % 16 != 0)
-    return fail(c, JN_EUNSUPPORTED, "workspace must be 256-byte and hidden 16-byte aligned");
-
-  const int32_t T = p->T, d = bb->d, f = bb->ffn;
-  {
-    // launch-size limits, checked before anything is enqueued: a dispatch
-    // holds at most 2^32 - 1 work-items, and the attention grid at most 2^30
-    // workgroups.  GEMM: batches near the bound below (rows x columns / 32 work-
-    // items) run on tiles of at least 64x128 per 256 threads, which stay under it;
-    // the smaller tiles are planned for short launches only
-    const int64_t kv = bb->n_kv_heads ? bb->n_kv_heads : bb->n_heads;
-    const int64_t nmax = std::max<int64_t>((bb->n_heads + 2 * kv) * (d / bb->n_heads),
-                                           (bb->layers[0].w_gate ? 2 : 1) * (int64_t)f);
-    const int64_t gemm_items = ((int64_t)T + 127) / 128 * ((nmax + 127) / 128) * 512;
-    const int64_t qtiles = ((int64_t)p->max_seqlen + 127) / 128;
-    const int64_t attn_blocks = ((int64_t)p->N * kv + 7) / 8 * 8 * (bb->n_heads / kv) * qtiles;
-    if (gemm_items >= (1ll << 32) || attn_blocks > (1ll << 30))
-      return fail(c, JN_ESHAPE, "batch of %d rows / %d samples exceeds one launch's grid", T, p->N);
-  }
+// The layers over T rows; between(l, qkv, att) enqueues what stands between a layer's
+// fused projection and its output projection.
+extern "C++" {
+namespace {
+template <typename F>
+jn_status backbone_layers(jn_ctx* c, const jn_backbone* bb, int32_t T, const void* rows, void* hidden, void* ws,
+                          const BbLayout& L, F&& between) {
+  const int32_t d = bb->d, f = bb->ffn;
   char* w = (char*)ws;
   float* x = (float*)(w + L.x);
   void* h = w + L.h;
@@ -725,42 +704,16 @@ jn_status jn_backbone_forward(jn_ctx* c, const jn_backbone* bb, const jn_packed*
     return S > 1 ? launch_rmsnorm_split(s, x, (const float*)sp, S, g, out, T, d, bb->eps)
                  : launch_rmsnorm_f32in(s, x, g, out, T, d, bb->eps);
   };
-  // Head norms, several position axes or positions of the caller's: one pass over
-  // q and k; a plain rotation by the row's own position keeps its kernel and its bits
-  const bool qk = bb->layers[0].gq != nullptr || (bb->rope_theta > 0.f && bb->pos);
-  QkShape shape{};
-  if (qk) {
-    shape.rows = T;
-    shape.heads = bb->n_heads;
-    shape.kv = kvh;
-    shape.hd = hd;
-    shape.ldx = shape.ldy = nqkv;
-    shape.eps = bb->eps;
-    if (bb->rope_theta > 0.f) {
-      shape.pos = bb->pos ? bb->pos : p->token_pos;
-      qk_pairs(&shape, bb->rope_theta, bb->rope_axes, bb->rope_interleaved, bb->rope_sections);
-    }
-  }
   for (int l = 0; l < bb->n_layers; ++l) {
     const jn_layer& Ly = bb->layers[l];
     if (l == 0)
-      JN_TRACED(c, JN_OP_RMSNORM, T, d, 0, launch_rmsnorm_bf16in(s, p->tokens, x, Ly.g1, h, T, d, bb->eps), "rmsnorm");
+      JN_TRACED(c, JN_OP_RMSNORM, T, d, 0, launch_rmsnorm_bf16in(s, rows, x, Ly.g1, h, T, d, bb->eps), "rmsnorm");
     else
       JN_TRACED(c, JN_OP_RMSNORM, T, d, 0, norm(sd, Ly.g1, h), "rmsnorm");
     JN_TRACED(c, JN_OP_GEMM_QKV, T, nqkv, d,
               launch_gemm(s, EPI_BF16, h, d, Ly.wqkv, nullptr, d, qkv, nqkv, T, nqkv, d, sp, spb), "gemm qkv");
-    if (qk) {
-      shape.gq = (const uint16_t*)Ly.gq;
-      shape.gk = (const uint16_t*)Ly.gk;
-      JN_TRACED(c, JN_OP_QK, T, (bb->n_heads + kvh) * hd, 0,
-                launch_qk_fwd(s, shape, (const uint16_t*)qkv, (uint16_t*)qkv), "head norms and rotation");
-    } else if (bb->rope_theta > 0.f)
-      JN_TRACED(c, JN_OP_ROPE, T, (bb->n_heads + kvh) * hd, 0,
-                launch_rope(s, qkv, nqkv, p->token_pos, T, bb->n_heads + kvh, hd, bb->rope_theta), "rope");
-    JN_TRACED(c, JN_OP_ATTENTION, T, d, bb->n_heads,
-              launch_attention(s, qkv, att, p->seqlens, p->cu_seqlens, p->N, d, bb->n_heads, kvh, bb->causal != 0,
-                               p->max_seqlen, p->align),
-              "attention");
+    const jn_status st = between(l, qkv, att);
+    if (st != JN_OK) return st;
     JN_TRACED(c, JN_OP_GEMM_O, T, d, d,
               launch_gemm(s, EPI_RESID_F32, att, d, Ly.wo, nullptr, d, x, d, T, d, d, sp, spb, true), "gemm o");
     JN_TRACED(c, JN_OP_RMSNORM, T, d, 0, norm(so, Ly.g2, h), "rmsnorm");
@@ -775,6 +728,76 @@ jn_status jn_backbone_forward(jn_ctx* c, const jn_backbone* bb, const jn_packed*
   }
   JN_TRACED(c, JN_OP_RMSNORM, T, d, 0, norm(sd, bb->gf, hidden), "final rmsnorm");
   return JN_OK;
+}
+}  // namespace
+}
+
+// Launch-size limits of T rows, checked before anything is enqueued: a dispatch
+// holds at most 2^32 - 1 work-items.  GEMM: batches near the bound below (rows x
+// columns / 32 work-items) run on tiles of at least 64x128 per 256 threads, which
+// stay under it; the smaller tiles are planned for short launches only.
+static bool backbone_fits(const jn_backbone* bb, int64_t T) {
+  const int64_t kv = bb->n_kv_heads ? bb->n_kv_heads : bb->n_heads;
+  const int64_t nmax = std::max<int64_t>((bb->n_heads + 2 * kv) * (bb->d / bb->n_heads),
+                                         (bb->layers[0].w_gate ? 2 : 1) * (int64_t)bb->ffn);
+  return (T + 127) / 128 * ((nmax + 127) / 128) * 512 < (1ll << 32);
+}
+
+jn_status jn_backbone_forward(jn_ctx* c, const jn_backbone* bb, const jn_packed* p, void* hidden, void* ws,
+                              size_t ws_bytes) {
+  if (!c) return JN_EINVAL;
+  jn_status st = check_backbone(c, bb);
+  if (st != JN_OK) return st;
+  if (!valid_packed(p) || !p->tokens) return fail(c, JN_EINVAL, "invalid packed batch");
+  if (p->d != bb->d) return fail(c, JN_EINCOMPAT, "packed width %d != backbone width %d", p->d, bb->d);
+  if (!hidden || !ws) return fail(c, JN_EINVAL, "null hidden or workspace");
+  BbLayout L = bb_layout(bb, p->T);
+  if (ws_bytes < L.total) return fail(c, JN_ENOSPACE, "workspace %zu B < %zu B", ws_bytes, L.total);
+  if (((uintptr_t)ws) % 256 != 0 || ((uintptr_t)hidden) % 16 != 0)
+    return fail(c, JN_EUNSUPPORTED, "workspace must be 256-byte and hidden 16-byte aligned");
+
+  const int32_t T = p->T, d = bb->d;
+  // (the attention grid holds at most 2^30 workgroups)
+  const int64_t kv = bb->n_kv_heads ? bb->n_kv_heads : bb->n_heads;
+  const int64_t qtiles = ((int64_t)p->max_seqlen + 127) / 128;
+  const int64_t attn_blocks = ((int64_t)p->N * kv + 7) / 8 * 8 * (bb->n_heads / kv) * qtiles;
+  if (!backbone_fits(bb, T) || attn_blocks > (1ll << 30))
+    return fail(c, JN_ESHAPE, "batch of %d rows / %d samples exceeds one launch's grid", T, p->N);
+  // Head norms, several position axes or positions of the caller's: one pass over
+  // q and k; a plain rotation by the row's own position keeps its kernel and its bits
+  const int32_t hd = d / bb->n_heads, kvh = bb->n_kv_heads ? bb->n_kv_heads : bb->n_heads;
+  const int32_t nqkv = (bb->n_heads + 2 * kvh) * hd;
+  hipStream_t s = c->stream;
+  const bool qk = bb->layers[0].gq != nullptr || (bb->rope_theta > 0.f && bb->pos);
+  QkShape shape{};
+  if (qk) {
+    shape.rows = T;
+    shape.heads = bb->n_heads;
+    shape.kv = kvh;
+    shape.hd = hd;
+    shape.ldx = shape.ldy = nqkv;
+    shape.eps = bb->eps;
+    if (bb->rope_theta > 0.f) {
+      shape.pos = bb->pos ? bb->pos : p->token_pos;
+      qk_pairs(&shape, bb->rope_theta, bb->rope_axes, bb->rope_interleaved, bb->rope_sections);
+    }
+  }
+  return backbone_layers(c, bb, T, p->tokens, hidden, ws, L, [&](int l, void* qkv, void* att) -> jn_status {
+    const jn_layer& Ly = bb->layers[l];
+    if (qk) {
+      shape.gq = (const uint16_t*)Ly.gq;
+      shape.gk = (const uint16_t*)Ly.gk;
+      JN_TRACED(c, JN_OP_QK, T, (bb->n_heads + kvh) * hd, 0,
+                launch_qk_fwd(s, shape, (const uint16_t*)qkv, (uint16_t*)qkv), "head norms and rotation");
+    } else if (bb->rope_theta > 0.f)
+      JN_TRACED(c, JN_OP_ROPE, T, (bb->n_heads + kvh) * hd, 0,
+                launch_rope(s, qkv, nqkv, p->token_pos, T, bb->n_heads + kvh, hd, bb->rope_theta), "rope");
+    JN_TRACED(c, JN_OP_ATTENTION, T, d, bb->n_heads,
+              launch_attention(s, qkv, att, p->seqlens, p->cu_seqlens, p->N, d, bb->n_heads, kvh, bb->causal != 0,
+                               p->max_seqlen, p->align),
+              "attention");
+    return JN_OK;
+  });
 }
 
 // --------------------------------------- queries and keys: norm, rotation ---
@@ -890,6 +913,315 @@ jn_status jn_qk_norm_rope_bwd(jn_ctx* c, const jn_qk_args* a, const void* x, con
             launch_qk_bwd(c->stream, q, (const uint16_t*)x, (const uint16_t*)dy, (uint16_t*)dx, (float*)ws, dgq, dgk),
             "head norm and rotation gradients");
   return JN_OK;
+}
+
+// ----------------------------------------- keys and values of earlier rows ---
+
+extern "C++" {
+namespace {
+
+int32_t log2_of(int32_t x) {
+  int32_t k = 0;
+  while ((1 << k) < x) ++k;
+  return k;
+}
+
+jn_status kv_cache(jn_ctx* c, const jn_kv_cache* k, int32_t layer, KvCache* out) {
+  if (!k) return fail(c, JN_EINVAL, "null cache");
+  if (k->n_layers < 1 || k->n_pages < 1 || k->n_kv_heads < 1) return fail(c, JN_EINVAL, "cache sizes must be positive");
+  if (layer < 0 || layer >= k->n_layers) return fail(c, JN_ESHAPE, "layer %d of %d", layer, k->n_layers);
+  if (k->page_size < 16 || k->page_size > 256 || (k->page_size & (k->page_size - 1)) != 0)
+    return fail(c, JN_EUNSUPPORTED, "pages of %d rows, not 16, 32, 64, 128 or 256", k->page_size);
+  if (k->head_dim < 16 || k->head_dim > 256 || k->head_dim % 16 != 0)
+    return fail(c, JN_EUNSUPPORTED, "head_dim %d not a multiple of 16 in [16, 256]", k->head_dim);
+  if (k->n_kv_heads > 65536) return fail(c, JN_ESHAPE, "%d key heads", k->n_kv_heads);
+  const int64_t page = (int64_t)k->n_kv_heads * k->page_size * k->head_dim;
+  if (k->ld_page < page || k->ld_page > INT64_MAX / 4 / k->n_pages)
+    return fail(c, JN_EINVAL, "pages of %lld elements are %lld apart", (long long)page, (long long)k->ld_page);
+  if (k->n_layers > 1) {
+    const bool after = k->ld_layer >= k->n_pages * k->ld_page;
+    const bool within = k->ld_layer >= page && k->ld_layer <= k->ld_page / k->n_layers;
+    if ((!after && !within) || k->ld_layer > INT64_MAX / 4 / k->n_layers)
+      return fail(c, JN_EINVAL, "layers %lld elements apart overlap", (long long)k->ld_layer);
+  }
+  if (k->ld_page % 8 != 0 || (k->n_layers > 1 && k->ld_layer % 8 != 0))
+    return fail(c, JN_EUNSUPPORTED, "strides of the cache not multiples of 8");
+  if (!k->k || !k->v || k->k == k->v) return fail(c, JN_EINVAL, "keys and values need buffers of their own");
+  if (((uintptr_t)k->k | (uintptr_t)k->v) % 16 != 0) return fail(c, JN_EUNSUPPORTED, "cache not 16-byte aligned");
+  *out = KvCache{};
+  out->ld_layer = k->n_layers > 1 ? k->ld_layer : 0;
+  out->k = (uint16_t*)k->k + layer * out->ld_layer;
+  out->v = (uint16_t*)k->v + layer * out->ld_layer;
+  out->ld_page = k->ld_page;
+  out->n_layers = k->n_layers;
+  out->n_pages = k->n_pages;
+  out->page_log2 = log2_of(k->page_size);
+  out->kv = k->n_kv_heads;
+  out->hd = k->head_dim;
+  return JN_OK;
+}
+
+jn_status kv_batch(jn_ctx* c, const jn_kv_batch* b, const jn_kv_cache* k, KvBatch* out) {
+  if (!b) return fail(c, JN_EINVAL, "null batch");
+  if (b->n_seqs < 0 || b->rows < 0 || b->max_pages < 1 || b->max_new < 1 || (b->whole != 0 && b->whole != 1))
+    return fail(c, JN_EINVAL, "batch of %d sequences, %d rows, %d pages, %d new", b->n_seqs, b->rows, b->max_pages, b->max_new);
+  if (b->n_seqs > 65535 || b->rows > (1 << 26) - 4) return fail(c, JN_ESHAPE, "%d sequences, %d rows", b->n_seqs, b->rows);
+  if ((int64_t)b->max_pages * k->page_size > 1 << 30)
+    return fail(c, JN_ESHAPE, "%d pages of %d rows in a sequence", b->max_pages, k->page_size);
+  if (b->n_seqs > 0 && (!b->pages || !b->past || !b->cu_rows)) return fail(c, JN_EINVAL, "null batch table");
+  if (((uintptr_t)b->pages | (uintptr_t)b->past | (uintptr_t)b->cu_rows | (uintptr_t)b->parents) % 4 != 0)
+    return fail(c, JN_EINVAL, "batch tables not 4-byte aligned");
+  if (b->parents && b->whole) return fail(c, JN_EINVAL, "a tree's rows do not see the whole of it");
+  if (b->parents && b->max_new > JN_KV_TREE_ROWS)
+    return fail(c, JN_EUNSUPPORTED, "trees of %d rows, more than %d", b->max_new, JN_KV_TREE_ROWS);
+  *out = KvBatch{};
+  out->pages = b->pages;
+  out->past = b->past;
+  out->cu = b->cu_rows;
+  out->parents = b->parents;
+  out->n_seqs = b->n_seqs;
+  out->max_pages = b->max_pages;
+  out->rows = b->rows;
+  out->max_new = b->max_new;
+  out->places = b->max_pages * k->page_size;
+  out->whole = b->whole;
+  return JN_OK;
+}
+
+// The arguments of an append, and whether it rotates.
+jn_status kv_rows(jn_ctx* c, const KvCache& k, const KvBatch& b, const jn_qk_args* a, QkShape* q) {
+  if (!a) return fail(c, JN_EINVAL, "null arguments");
+  if (a->rows != b.rows || a->n_kv_heads != k.kv || a->head_dim != k.hd)
+    return fail(c, JN_EINVAL, "rows, key heads or head width differ from the batch's and the cache's");
+  if (a->n_heads < 0 || a->n_heads > 65536) return fail(c, JN_ESHAPE, "%d query heads", a->n_heads);
+  const int64_t width = ((int64_t)a->n_heads + 2 * a->n_kv_heads) * a->head_dim;
+  if (a->ld_in < width || (a->n_heads > 0 && a->ld_out < (int64_t)a->n_heads * a->head_dim))
+    return fail(c, JN_EINVAL, "rows hold no %lld elements, or those of q no queries", (long long)width);
+  if (a->ld_in % 8 != 0 || (a->n_heads > 0 && a->ld_out % 8 != 0))
+    return fail(c, JN_EUNSUPPORTED, "row strides not multiples of 8");
+  if ((a->gq == nullptr) != (a->gk == nullptr)) return fail(c, JN_EINVAL, "norms need both gains");
+  if (((uintptr_t)a->gq | (uintptr_t)a->gk) % 16 != 0) return fail(c, JN_EUNSUPPORTED, "gains not 16-byte aligned");
+  if (a->gq && !(a->eps > 0.f)) return fail(c, JN_EINVAL, "eps must be > 0");
+  if (!(a->rope_theta >= 0.f) || std::isinf(a->rope_theta)) return fail(c, JN_EINVAL, "rope_theta must be >= 0");
+  const jn_status st = check_axes(c, a->rope_axes, a->rope_interleaved, a->rope_sections, a->head_dim);
+  if (st != JN_OK) return st;
+  if (a->rope_theta > 0.f && a->rope_axes > 1 && a->rows > 0 && !a->pos)
+    return fail(c, JN_EINVAL, "%d position axes need pos", a->rope_axes);
+  if ((uintptr_t)a->pos % 4 != 0) return fail(c, JN_EINVAL, "pos not 4-byte aligned");
+  *q = QkShape{};
+  q->rows = a->rows;
+  q->heads = a->n_heads;
+  q->kv = a->n_kv_heads;
+  q->hd = a->head_dim;
+  q->ldx = a->ld_in;
+  q->ldy = a->ld_out;
+  q->gq = (const uint16_t*)a->gq;
+  q->gk = (const uint16_t*)a->gk;
+  q->eps = a->eps;
+  if (a->rope_theta > 0.f) {
+    q->pos = a->pos;
+    qk_pairs(q, a->rope_theta, a->rope_axes, a->rope_interleaved, a->rope_sections);
+  }
+  return JN_OK;
+}
+
+jn_status kv_attn(jn_ctx* c, const KvCache& k, const KvBatch& b, const jn_kv_attn* a, KvAttn* out) {
+  if (!a) return fail(c, JN_EINVAL, "null arguments");
+  if (k.hd != 32 && k.hd != 64 && k.hd != 128 && k.hd != 256)
+    return fail(c, JN_EUNSUPPORTED, "head_dim %d not in {32,64,128,256}", k.hd);
+  if (a->n_heads < 1 || a->n_heads % k.kv != 0)
+    return fail(c, JN_EINVAL, "%d query heads over %d key heads", a->n_heads, k.kv);
+  if (a->n_heads > 65536) return fail(c, JN_ESHAPE, "%d query heads", a->n_heads);
+  const int64_t width = (int64_t)a->n_heads * k.hd;
+  if (a->ld_q < width || a->ld_out < width) return fail(c, JN_EINVAL, "rows hold no %lld elements", (long long)width);
+  if ((a->ld_q | a->ld_out) % 8 != 0) return fail(c, JN_EUNSUPPORTED, "row strides not multiples of 8");
+  if (!(a->scale >= 0.f) || std::isinf(a->scale)) return fail(c, JN_EINVAL, "scale must be finite and >= 0");
+  // query tiles of a launch, for the smallest tile (16 rows)
+  const int64_t tiles = ((int64_t)std::min(b.max_new, std::max(b.rows, 1)) * (a->n_heads / k.kv) + 15) / 16;
+  if (tiles * k.kv * std::max(b.n_seqs, 1) > kMostBlocks)
+    return fail(c, JN_ESHAPE, "%d sequences of %d new rows exceed one launch's grid", b.n_seqs, b.max_new);
+  *out = KvAttn{};
+  out->ldq = a->ld_q;
+  out->ldo = a->ld_out;
+  out->heads = a->n_heads;
+  out->scale_log2 = 1.4426950408889634f * (a->scale > 0.f ? a->scale : 1.f / sqrtf((float)k.hd));
+  return JN_OK;
+}
+
+}  // namespace
+}
+
+jn_status jn_kv_append(jn_ctx* c, const jn_kv_cache* cache, int32_t layer, const jn_kv_batch* batch, const jn_qk_args* a,
+                       const void* x, void* q) {
+  if (!c) return JN_EINVAL;
+  KvCache k;
+  KvBatch b;
+  QkShape shape;
+  jn_status st = kv_cache(c, cache, layer, &k);
+  if (st == JN_OK) st = kv_batch(c, batch, cache, &b);
+  if (st == JN_OK) st = kv_rows(c, k, b, a, &shape);
+  if (st != JN_OK) return st;
+  if (b.rows == 0 || b.n_seqs == 0) return JN_OK;
+  if (!x || (a->n_heads > 0 && !q)) return fail(c, JN_EINVAL, "null rows");
+  if (((uintptr_t)x | (uintptr_t)q) % 16 != 0) return fail(c, JN_EUNSUPPORTED, "rows not 16-byte aligned");
+  if (x == q && a->ld_in != a->ld_out) return fail(c, JN_EINVAL, "in place with two strides");
+  if ((st = check_device(c)) != JN_OK) return st;
+  JN_TRACED(c, JN_OP_KV_APPEND, b.rows, (a->n_heads + 2 * k.kv) * k.hd, 0,
+            launch_kv_append(c->stream, k, b, shape, a->rope_theta > 0.f, (const uint16_t*)x, (uint16_t*)q),
+            "keys and values to the cache");
+  return JN_OK;
+}
+
+jn_status jn_kv_attention_workspace_size(const jn_kv_cache* cache, const jn_kv_batch* batch, const jn_kv_attn* a,
+                                         size_t* bytes) {
+  KvCache k;
+  KvBatch b;
+  KvAttn at;
+  if (!bytes) return JN_EINVAL;
+  jn_status st = kv_cache(nullptr, cache, 0, &k);
+  if (st == JN_OK) st = kv_batch(nullptr, batch, cache, &b);
+  if (st == JN_OK) st = kv_attn(nullptr, k, b, a, &at);
+  if (st == JN_OK) *bytes = b.rows > 0 && b.n_seqs > 0 ? kv_attention_bytes(k, b, at.heads) : 0;
+  return st;
+}
+
+jn_status jn_kv_attention(jn_ctx* c, const jn_kv_cache* cache, int32_t layer, const jn_kv_batch* batch,
+                          const jn_kv_attn* a, const void* q, void* out, void* ws, size_t ws_bytes) {
+  if (!c) return JN_EINVAL;
+  KvCache k;
+  KvBatch b;
+  KvAttn at;
+  jn_status st = kv_cache(c, cache, layer, &k);
+  if (st == JN_OK) st = kv_batch(c, batch, cache, &b);
+  if (st == JN_OK) st = kv_attn(c, k, b, a, &at);
+  if (st != JN_OK) return st;
+  if (b.rows == 0 || b.n_seqs == 0) return JN_OK;
+  if (!q || !out || q == out) return fail(c, JN_EINVAL, "queries and results need buffers of their own");
+  if (((uintptr_t)q | (uintptr_t)out) % 16 != 0) return fail(c, JN_EUNSUPPORTED, "rows not 16-byte aligned");
+  const size_t need = kv_attention_bytes(k, b, at.heads);
+  if (need > 0 && (!ws || ws_bytes < need)) return fail(c, JN_ENOSPACE, "workspace %zu B < %zu B", ws ? ws_bytes : 0, need);
+  if (need > 0 && (uintptr_t)ws % 256 != 0) return fail(c, JN_EUNSUPPORTED, "workspace not 256-byte aligned");
+  if ((st = check_device(c)) != JN_OK) return st;
+  at.q = (const uint16_t*)q;
+  at.out = (uint16_t*)out;
+  JN_TRACED(c, JN_OP_KV_ATTENTION, b.rows, at.heads * k.hd, at.heads, launch_kv_attention(c->stream, k, b, at, ws),
+            "attention over the cache");
+  return JN_OK;
+}
+
+jn_status jn_kv_keep(jn_ctx* c, const jn_kv_cache* cache, const jn_kv_batch* batch, const int32_t* path, int32_t max_path,
+                     const int32_t* n_path, int32_t* past_out) {
+  if (!c) return JN_EINVAL;
+  KvCache k;
+  KvBatch b;
+  jn_status st = kv_cache(c, cache, 0, &k);
+  if (st == JN_OK) st = kv_batch(c, batch, cache, &b);
+  if (st != JN_OK) return st;
+  if (max_path < 1) return fail(c, JN_EINVAL, "paths of %d rows", max_path);
+  if (((uintptr_t)path | (uintptr_t)n_path | (uintptr_t)past_out) % 4 != 0)
+    return fail(c, JN_EINVAL, "paths not 4-byte aligned");
+  if (b.n_seqs == 0) return JN_OK;
+  if (!path || !n_path) return fail(c, JN_EINVAL, "null paths");
+  if (kv_keep_blocks(k) * b.n_seqs > kMostBlocks)
+    return fail(c, JN_ESHAPE, "%d sequences of %d layers exceed one launch's grid", b.n_seqs, k.n_layers);
+  if ((st = check_device(c)) != JN_OK) return st;
+  JN_TRACED(c, JN_OP_KV_KEEP, b.n_seqs, k.n_layers * k.kv * k.hd, 0,
+            launch_kv_keep(c->stream, k, b, path, max_path, n_path, past_out), "kept rows of the cache");
+  return JN_OK;
+}
+
+extern "C++" {
+namespace {
+
+// What jn_backbone_extend adds to a backbone's workspace: its attention's.
+struct ExtendPlan {
+  KvCache k;
+  KvBatch b;
+  KvAttn at;
+  QkShape shape;
+  jn_qk_args args;
+  BbLayout L;
+  size_t attn, total;
+};
+
+jn_status extend_plan(jn_ctx* c, const jn_backbone* bb, const jn_kv_cache* cache, const jn_kv_batch* batch,
+                      ExtendPlan* P) {
+  jn_status st = check_backbone(c, bb);
+  if (st == JN_OK) st = kv_cache(c, cache, 0, &P->k);
+  if (st == JN_OK) st = kv_batch(c, batch, cache, &P->b);
+  if (st != JN_OK) return st;
+  const int32_t hd = bb->d / bb->n_heads, kv = bb->n_kv_heads ? bb->n_kv_heads : bb->n_heads;
+  if (P->k.n_layers != bb->n_layers || P->k.kv != kv || P->k.hd != hd)
+    return fail(c, JN_EINCOMPAT, "cache of %d layers, %d heads of %d; backbone of %d, %d, %d", P->k.n_layers, P->k.kv,
+                P->k.hd, bb->n_layers, kv, hd);
+  if (P->b.whole == bb->causal) return fail(c, JN_EINVAL, "a causal backbone's rows do not see later ones, the others do");
+  P->args = jn_qk_args{};
+  P->args.rows = P->b.rows;
+  P->args.n_heads = bb->n_heads;
+  P->args.n_kv_heads = kv;
+  P->args.head_dim = hd;
+  P->args.ld_in = P->args.ld_out = (int64_t)(bb->n_heads + 2 * kv) * hd;
+  P->args.gq = bb->layers[0].gq;
+  P->args.gk = bb->layers[0].gk;
+  P->args.pos = bb->pos;
+  P->args.eps = bb->eps;
+  P->args.rope_theta = bb->rope_theta;
+  P->args.rope_axes = bb->rope_axes;
+  P->args.rope_interleaved = bb->rope_interleaved;
+  std::copy(bb->rope_sections, bb->rope_sections + 4, P->args.rope_sections);
+  const jn_kv_attn a{bb->n_heads, 0.f, P->args.ld_in, bb->d};
+  st = kv_rows(c, P->k, P->b, &P->args, &P->shape);
+  if (st == JN_OK) st = kv_attn(c, P->k, P->b, &a, &P->at);
+  if (st != JN_OK) return st;
+  if (!backbone_fits(bb, P->b.rows)) return fail(c, JN_ESHAPE, "batch of %d rows exceeds one launch's grid", P->b.rows);
+  const bool empty = P->b.rows == 0 || P->b.n_seqs == 0;
+  P->L = bb_layout(bb, P->b.rows);
+  P->attn = P->L.total;
+  P->total = P->attn + (empty ? 0 : kv_attention_bytes(P->k, P->b, bb->n_heads));
+  return JN_OK;
+}
+
+}  // namespace
+}
+
+jn_status jn_backbone_extend_workspace_size(const jn_backbone* bb, const jn_kv_cache* cache, const jn_kv_batch* batch,
+                                            size_t* bytes) {
+  if (!bytes) return JN_EINVAL;
+  ExtendPlan P;
+  const jn_status st = extend_plan(nullptr, bb, cache, batch, &P);
+  if (st == JN_OK) *bytes = P.total;
+  return st;
+}
+
+jn_status jn_backbone_extend(jn_ctx* c, const jn_backbone* bb, const jn_kv_cache* cache, const jn_kv_batch* batch,
+                             const void* embeds, void* hidden, void* ws, size_t ws_bytes) {
+  if (!c) return JN_EINVAL;
+  ExtendPlan P;
+  jn_status st = extend_plan(c, bb, cache, batch, &P);
+  if (st != JN_OK) return st;
+  if (P.b.rows == 0 || P.b.n_seqs == 0) return JN_OK;
+  if (!embeds || !hidden || !ws) return fail(c, JN_EINVAL, "null rows or workspace");
+  if (ws_bytes < P.total) return fail(c, JN_ENOSPACE, "workspace %zu B < %zu B", ws_bytes, P.total);
+  if ((uintptr_t)ws % 256 != 0 || ((uintptr_t)embeds | (uintptr_t)hidden) % 16 != 0)
+    return fail(c, JN_EUNSUPPORTED, "workspace must be 256-byte, embeds and hidden 16-byte aligned");
+  if ((st = check_device(c)) != JN_OK) return st;
+  const int32_t T = P.b.rows, d = bb->d;
+  hipStream_t s = c->stream;
+  return backbone_layers(c, bb, T, embeds, hidden, ws, P.L, [&](int l, void* qkv, void* att) -> jn_status {
+    KvCache k = P.k;
+    k.k += l * P.k.ld_layer;
+    k.v += l * P.k.ld_layer;
+    P.shape.gq = (const uint16_t*)bb->layers[l].gq;
+    P.shape.gk = (const uint16_t*)bb->layers[l].gk;
+    JN_TRACED(c, JN_OP_KV_APPEND, T, (int32_t)P.args.ld_in, 0,
+              launch_kv_append(s, k, P.b, P.shape, bb->rope_theta > 0.f, (const uint16_t*)qkv, (uint16_t*)qkv),
+              "keys and values to the cache");
+    P.at.q = (const uint16_t*)qkv;
+    P.at.out = (uint16_t*)att;
+    JN_TRACED(c, JN_OP_KV_ATTENTION, T, d, bb->n_heads, launch_kv_attention(s, k, P.b, P.at, (char*)ws + P.attn),
+              "attention over the cache");
+    return JN_OK;
+  });
 }
 
 // ----------------------------------------------------------- token heads ---
@@ -1598,6 +1930,88 @@ jn_status jn_tenant_tokens_decode(jn_ctx* c, const void* hidden, int32_t T, int3
   if (!c) return JN_EINVAL;
   if (!heads || !io || G < 1 || G > (1 << 16)) return fail(c, JN_EINVAL, "null token heads or no tenant");
   return guarded(c, [&]() { return tokens_run(c, hidden, T, d, heads, entries(io, G), false, ws, ws_bytes); });
+}
+
+// -------------------------------------------------- verification of drafts ---
+
+extern "C++" {
+namespace {
+
+jn_status check_verify(jn_ctx* c, const jn_token_verify* v, int32_t G) {
+  if (!v || G < 1) return fail(c, JN_EINVAL, "no tenants");
+  int64_t trees = 0;
+  for (int32_t g = 0; g < G; ++g) {
+    const jn_token_verify& t = v[g];
+    if (t.n_trees < 0 || t.n < 0 || t.max_path < 1) return fail(c, JN_EINVAL, "tenant %d: negative counts, or no path", g);
+    if (t.vocab < 1 || t.vocab > 1 << 24) return fail(c, JN_ESHAPE, "tenant %d: vocabulary of %d", g, t.vocab);
+    if ((int64_t)t.n * t.vocab >= 1ll << 40 || (int64_t)t.n_trees * t.max_path > 1ll << 30)
+      return fail(c, JN_ESHAPE, "tenant %d: %d nodes, %d trees of %d", g, t.n, t.n_trees, t.max_path);
+    trees += t.n_trees;
+    if (t.n_trees == 0) continue;
+    if (!t.cu_nodes || !t.path || !t.n_path || !t.next || (t.n > 0 && !t.tokens))
+      return fail(c, JN_EINVAL, "tenant %d: null trees or outputs", g);
+    if (t.p ? t.greedy != nullptr || !t.r || (t.n > 0 && !t.u) : t.q || (t.n > 0 && !t.greedy))
+      return fail(c, JN_EINVAL, "tenant %d: p with u and r, or greedy alone", g);
+    if ((t.p && t.ld_p < t.vocab) || (t.q && t.ld_q < t.vocab))
+      return fail(c, JN_EINVAL, "tenant %d: rows of probabilities hold no %d", g, t.vocab);
+    if ((t.p && t.ld_p >= 1ll << 40) || (t.q && t.ld_q >= 1ll << 40)) return fail(c, JN_ESHAPE, "tenant %d: row strides", g);
+    const uintptr_t all = (uintptr_t)t.cu_nodes | (uintptr_t)t.parents | (uintptr_t)t.tokens | (uintptr_t)t.p |
+                          (uintptr_t)t.q | (uintptr_t)t.greedy | (uintptr_t)t.u | (uintptr_t)t.r | (uintptr_t)t.path |
+                          (uintptr_t)t.n_path | (uintptr_t)t.next;
+    if (all % 4 != 0) return fail(c, JN_EINVAL, "tenant %d: buffers not 4-byte aligned", g);
+  }
+  if (trees > kMostBlocks / 16) return fail(c, JN_ESHAPE, "%lld trees in a call", (long long)trees);
+  return JN_OK;
+}
+
+}  // namespace
+}
+
+jn_status jn_tokens_verify_workspace_size(const jn_token_verify* v, int32_t G, size_t* bytes) {
+  if (!bytes) return JN_EINVAL;
+  const jn_status st = check_verify(nullptr, v, G);
+  if (st == JN_OK) *bytes = 0;
+  return st;
+}
+
+jn_status jn_tenant_tokens_verify(jn_ctx* c, const jn_token_verify* v, int32_t G, void* ws, size_t ws_bytes) {
+  if (!c) return JN_EINVAL;
+  jn_status st = check_verify(c, v, G);
+  if (st != JN_OK) return st;
+  (void)ws;
+  (void)ws_bytes;
+  if ((st = check_device(c)) != JN_OK) return st;
+  for (int32_t g = 0; g < G;) {
+    TokVerifySet set{};
+    int64_t nodes = 0;
+    for (; g < G && set.G < kVerifyTenants; ++g) {
+      const jn_token_verify& t = v[g];
+      if (t.n_trees == 0) continue;
+      nodes += t.n;
+      TokVerify& d = set.t[set.G++];
+      d.cu = t.cu_nodes;
+      d.parents = t.parents;
+      d.tokens = t.tokens;
+      d.p = t.p;
+      d.q = t.q;
+      d.greedy = t.greedy;
+      d.u = t.u;
+      d.r = t.r;
+      d.path = t.path;
+      d.n_path = t.n_path;
+      d.next = t.next;
+      d.ldp = t.ld_p;
+      d.ldq = t.ld_q;
+      d.n = t.n;
+      d.vocab = t.vocab;
+      d.max_path = t.max_path;
+      d.tree0 = set.trees;
+      set.trees += t.n_trees;
+    }
+    if (set.trees == 0) break;
+    JN_TRACED(c, JN_OP_TOKEN_VERIFY, nodes, set.t[0].vocab, 0, launch_tok_verify(c->stream, set), "verification of drafts");
+  }
+  return JN_OK;
 }
 
 // ----------------------------------------------------------------- heads ---

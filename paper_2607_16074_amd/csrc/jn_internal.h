@@ -508,6 +508,64 @@ constexpr int kXLossParts = 64;
 hipError_t launch_xloss(hipStream_t s, const XLossDesc* d, const int32_t* roff, int32_t G, const float* pred_pad,
                         int32_t ldp, uint16_t* dpred_pad, float* part);
 
+// ------------------------------- keys and values of earlier rows (jn_kv.h) ---
+// A layer of the cache, and the new rows of its sequences, by value in kernel
+// arguments; places = max_pages * page_size.
+struct KvCache {
+  uint16_t* k;
+  uint16_t* v;
+  int64_t ld_page, ld_layer;
+  int32_t n_layers, n_pages, page_log2, kv, hd;
+};
+struct KvBatch {
+  const int32_t* pages;
+  const int32_t* past;
+  const int32_t* cu;
+  const int32_t* parents;
+  int32_t n_seqs, max_pages, rows, max_new, places, whole;
+};
+// q: rows of b at a.ldy (null where a.heads is 0); a.pos null: places
+// (along the branches of a tree) with a.axes 1; `rope` and a.gq say what is done.
+hipError_t launch_kv_append(hipStream_t s, const KvCache& c, const KvBatch& b, const QkShape& a, bool rope,
+                            const uint16_t* x, uint16_t* q);
+struct KvAttn {
+  const uint16_t* q;
+  uint16_t* out;
+  int64_t ldq, ldo;
+  int32_t heads;
+  float scale_log2;   // of the scores, times log2(e)
+};
+size_t kv_attention_bytes(const KvCache& c, const KvBatch& b, int32_t heads);
+hipError_t launch_kv_attention(hipStream_t s, const KvCache& c, const KvBatch& b, const KvAttn& a, void* ws);
+// Workgroups of a sequence's move.
+inline int64_t kv_keep_blocks(const KvCache& c) { return ((int64_t)c.n_layers * 2 * c.kv * (c.hd / 8) + 255) / 256; }
+hipError_t launch_kv_keep(hipStream_t s, const KvCache& c, const KvBatch& b, const int32_t* path, int32_t max_path,
+                          const int32_t* n_path, int32_t* past_out);
+// Tenants of a verification, by value in kernel arguments; tree0: first tree of the
+// launch's.
+struct TokVerify {
+  const int32_t* cu;
+  const int32_t* parents;
+  const int32_t* tokens;
+  const float* p;
+  const float* q;
+  const int32_t* greedy;
+  const float* u;
+  const float* r;
+  int32_t* path;
+  int32_t* n_path;
+  int32_t* next;
+  int64_t ldp, ldq;
+  int32_t n, vocab, max_path, tree0;
+};
+constexpr int32_t kVerifyTenants = 24;  // of one launch
+struct TokVerifySet {
+  TokVerify t[kVerifyTenants];
+  int32_t G, trees;
+};
+static_assert(sizeof(TokVerifySet) <= 3400, "kernel arguments");
+hipError_t launch_tok_verify(hipStream_t s, const TokVerifySet& set);
+
 // ------------------------------------------------------------ optimizer ---
 
 struct AdamwTensor {

@@ -38,6 +38,7 @@
 // query rows and v_mfma_f32_16x16x32_bf16 (two waves per SIMD).
 #include "jn_device.h"
 #include "jn_internal.h"
+#include "jn_kv.h"
 
 namespace jnx {
 
@@ -744,6 +745,68 @@ hipError_t launch_rope(hipStream_t s, void* qkv, int32_t ld, const int32_t* toke
                        int32_t hd, float theta) {
   if (T < 1 || heads < 1 || hd % 4 != 0 || hd / 4 > 256 || !(theta > 0.f)) return hipErrorInvalidValue;
   rope_kernel<<<T, 256, 0, s>>>(reinterpret_cast<uint16_t*>(qkv), ld, token_pos, heads, hd, log2f(theta));
+  return hipGetLastError();
+}
+
+// ------------------------------------------- attention over a paged cache ---
+// One wavefront per new row and query head: 64 keys a step, a key a lane for the
+// scores, then a head-dim column (or four) a lane for the sum of the values seen.
+__global__ __launch_bounds__(64) void kv_attn_plain_kernel(KvCache c, KvBatch b, KvAttn a) {
+  __shared__ float qs[256], ps[64];
+  __shared__ int64_t at[64];
+  const int lane = threadIdx.x;
+  const int32_t row = blockIdx.x / a.heads, h = blockIdx.x - row * a.heads, kvh = h / (a.heads / c.kv);
+  const int32_t seq = kv_find(b, row, lane);
+  if (seq >= b.n_seqs) return;
+  const KvSeq sq = kv_seq(b, seq);
+  const int32_t j = row - sq.row0;
+  if (j < 0 || j >= sq.n) return;
+  const int32_t* const pages = b.pages + (int64_t)seq * b.max_pages;
+  for (int e = lane; e < c.hd; e += 64) qs[e] = bf2f(a.q[row * a.ldq + (int64_t)h * c.hd + e]);
+  uint64_t sees[4] = {0, 0, 0, 0};  // a tree's row: itself and its ancestors
+  if (b.parents)
+    for (int32_t k = j; k >= 0; k = kv_parent(b.parents + sq.row0, k)) sees[k >> 6] |= 1ull << (k & 63);
+  const int32_t end = sq.past + (b.whole ? sq.n : j + 1);
+  float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  __syncthreads();
+  for (int32_t t0 = 0; t0 < end; t0 += 64) {
+    const int32_t t = t0 + lane, k = t - sq.past;
+    bool on = t < end;
+    if (on && b.parents && k >= 0) on = (sees[k >> 6] >> (k & 63)) & 1;
+    const int32_t page = on ? kv_page(b, c, pages, t) : -1;
+    on = page >= 0;
+    float s = -INFINITY;
+    if (on) {
+      at[lane] = kv_at(c, page, kvh, t);
+      float z = 0.f;
+      for (int e = 0; e < c.hd; ++e) z = fmaf(qs[e], bf2f(c.k[at[lane] + e]), z);
+      s = z * a.scale_log2;
+    }
+    const float m2 = fmaxf(m, wave_max(s)), alpha = m2 == -INFINITY ? 1.f : exp2f(m - m2);
+    m = m2;
+    const float p = s == -INFINITY ? 0.f : exp2f(s - m);
+    l = l * alpha + wave_sum(p);
+    ps[lane] = on ? bf2f(f2bf(p)) : -1.f;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      o[e] *= alpha;
+      const int col = lane + 64 * e;
+      if (col < c.hd)
+        for (int i = 0; i < 64; ++i)
+          if (ps[i] >= 0.f) o[e] = fmaf(ps[i], bf2f(c.v[at[i] + col]), o[e]);
+    }
+    __syncthreads();
+  }
+  for (int e = 0; e < 4; ++e)
+    if (lane + 64 * e < c.hd)
+      a.out[row * a.ldo + (int64_t)h * c.hd + lane + 64 * e] = f2bf(l == 0.f ? 0.f : o[e] / l);
+}
+
+size_t kv_attention_bytes(const KvCache& c, const KvBatch& b, int32_t heads) { return 0; }
+
+hipError_t launch_kv_attention(hipStream_t s, const KvCache& c, const KvBatch& b, const KvAttn& a, void* ws) {
+  kv_attn_plain_kernel<<<(unsigned)((int64_t)b.rows * a.heads), 64, 0, s>>>(c, b, a);
   return hipGetLastError();
 }
 

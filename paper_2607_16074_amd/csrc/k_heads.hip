@@ -13,6 +13,7 @@
 
 #include "jn_device.h"
 #include "jn_internal.h"
+#include "jn_kv.h"
 
 namespace jnx {
 
@@ -1396,6 +1397,147 @@ hipError_t launch_small_pick(hipStream_t s, const TokSmallSet& all, int32_t ldz,
     small_pick_kernel<C><<<dim3(set.G, ldz / 16), kSmallThreads, 0, s>>>(set, T);
     return hipGetLastError();
   });
+}
+
+// ------------------------------------------------ verification of drafts ---
+// A workgroup walks a tree.  Rejecting children drawn from q leaves max(p_k - q, 0)
+// / T of the node's distribution p_k; with p_k = max(p - a q, 0) / T that is max(p -
+// (a + T) q, 0) over its sum, so that a node's state is the two numbers a and T, and
+// each rejection of a drawn child is one pass over the node's rows for the next T.
+// All sums are formed in 64 bits: a border between two tokens lies where the
+// definition has it, whatever order the terms are added in.
+constexpr int kVerifyThreads = 1024;
+
+__device__ __forceinline__ double wave_sum64(double v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+  return v;
+}
+
+__global__ __launch_bounds__(kVerifyThreads) void tok_verify_kernel(TokVerifySet set) {
+  __shared__ double part[16];
+  __shared__ int32_t gone[JN_KV_TREE_ROWS];  // rejected tokens of picked drafts
+  __shared__ int32_t pick[2];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  int32_t g = 0;
+  while (g + 1 < set.G && set.t[g + 1].tree0 <= (int32_t)blockIdx.x) ++g;
+  const TokVerify& d = set.t[g];
+  const int32_t t = blockIdx.x - d.tree0, V = d.vocab;
+  const int32_t first = min(max(d.cu[t], 0), d.n);
+  const int32_t n = min(max(min(d.cu[t + 1], d.n) - first, 0), d.parents ? JN_KV_TREE_ROWS : d.max_path);
+  int32_t* const path = d.path + (int64_t)t * d.max_path;
+  for (int32_t k = tid; k < d.max_path; k += kVerifyThreads) path[k] = -1;
+  if (n == 0) {
+    if (tid == 0) d.n_path[t] = 0, d.next[t] = -1;
+    return;
+  }
+  // sum over the row c of w_i, by all threads, the same in all of them
+  auto weight = [&](int32_t c, double a, int32_t ngone, int32_t i) {
+    double x = d.p[(first + c) * d.ldp + i];
+    if (d.q) {
+      x -= a * d.q[(first + c) * d.ldq + i];
+    } else {
+      for (int32_t k = 0; k < ngone; ++k)
+        if (gone[k] == i) x = 0.;
+    }
+    return x > 0. ? x : 0.;
+  };
+  auto row_sum = [&](int32_t c, double a, int32_t ngone) {
+    double v = 0.;
+    for (int32_t i = tid; i < V; i += kVerifyThreads) v += weight(c, a, ngone, i);
+    v = wave_sum64(v);
+    __syncthreads();
+    if (lane == 0) part[w] = v;
+    __syncthreads();
+    v = 0.;
+    for (int k = 0; k < 16; ++k) v += part[k];
+    return v;
+  };
+  int32_t cur = 0, count = 1, ngone = 0;
+  double a = 0., before = 0., T = 1.;
+  __syncthreads();
+  if (tid == 0) path[0] = 0;
+  for (int32_t j = 1; j < n && count < d.max_path; ++j) {
+    if ((d.parents ? kv_parent(d.parents + first, j) : j - 1) != cur) continue;
+    const int32_t x = d.tokens[first + j];
+    if (x < 0 || x >= V) continue;
+    bool stands;
+    if (!d.p) {
+      stands = d.greedy[first + cur] == x;
+    } else {
+      const double u = d.u[first + j], px = weight(cur, a, ngone, x);
+      if (d.q) {
+        stands = u * d.q[(first + cur) * d.ldq + x] * T < px;
+        if (!stands && T > 0.) {
+          before = a;
+          a += T;
+          T = row_sum(cur, a, 0);
+        }
+      } else {
+        stands = u * T < px;
+        if (!stands) {
+          T -= px;
+          __syncthreads();
+          if (tid == 0) gone[ngone] = x;
+          ++ngone;
+          __syncthreads();
+        }
+      }
+    }
+    if (stands) {
+      if (tid == 0) path[count] = j;
+      ++count;
+      cur = j;
+      a = before = 0.;
+      T = 1.;
+      ngone = 0;
+    }
+  }
+  if (tid == 0) d.n_path[t] = count;
+  if (!d.p) {
+    if (tid == 0) d.next[t] = d.greedy[first + cur];
+    return;
+  }
+  // the next token: every thread sums a run of the row, then the run that passes r
+  // of the whole is walked again
+  double all = row_sum(cur, a, ngone);
+  if (d.q && all == 0.) a = before, all = row_sum(cur, a, ngone);
+  const double want = (double)d.r[t] * all;
+  const int32_t run = (V + kVerifyThreads - 1) / kVerifyThreads, i0 = min(tid * run, V), i1 = min(i0 + run, V);
+  double own = 0.;
+  for (int32_t i = i0; i < i1; ++i) own += weight(cur, a, ngone, i);
+  double up = own;  // of the wavefront's runs up to this one
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double v = __shfl_up(up, o, kWave);
+    if (lane >= o) up += v;
+  }
+  __syncthreads();
+  if (lane == 63) part[w] = up;
+  if (tid == 0) pick[0] = pick[1] = -1;
+  __syncthreads();
+  double base = 0.;
+  for (int k = 0; k < w; ++k) base += part[k];
+  up = base + (up - own);
+  int32_t last = -1, hit = -1;
+  for (int32_t i = i0; i < i1; ++i) {
+    const double x = weight(cur, a, ngone, i);
+    if (x > 0.) {
+      up += x;
+      last = i;
+      if (hit < 0 && up > want) hit = i;
+    }
+  }
+  // (the lowest hit; the last positive weight where rounding leaves none)
+  if (last >= 0) atomicMax(&pick[1], last);
+  if (hit >= 0) atomicMin((uint32_t*)&pick[0], (uint32_t)hit);
+  __syncthreads();
+  if (tid == 0) d.next[t] = pick[0] >= 0 ? pick[0] : pick[1];
+}
+
+hipError_t launch_tok_verify(hipStream_t s, const TokVerifySet& set) {
+  tok_verify_kernel<<<set.trees, kVerifyThreads, 0, s>>>(set);
+  return hipGetLastError();
 }
 
 }  // namespace jnx

@@ -6,6 +6,7 @@
 
 #include "jn_device.h"
 #include "jn_internal.h"
+#include "jn_kv.h"
 
 namespace jnx {
 
@@ -286,6 +287,21 @@ __device__ __forceinline__ void row_turns(const QkShape& a, int64_t row, int lan
   __builtin_amdgcn_wave_barrier();  // the line's last readers are done (a wave's LDS operations stay in order)
   for (int i = lane; i < half; i += 64) {
     const double t = (double)a.pos[row * a.axes + a.axis[i]] * a.freq[i];
+    float sn, cs;
+    sincospif((float)(2.0 * (t - rint(t))), &sn, &cs);
+    line[i] = cs;
+    line[128 + i] = sn;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// The same for one position of all pairs.
+__device__ __forceinline__ void place_turns(const QkShape& a, int32_t place, int lane, float* line) {
+  const int half = a.hd >> 1;
+  __builtin_amdgcn_wave_barrier();
+  for (int i = lane; i < half; i += 64) {
+    const double t = (double)place * a.freq[i];
     float sn, cs;
     sincospif((float)(2.0 * (t - rint(t))), &sn, &cs);
     line[i] = cs;
@@ -647,6 +663,136 @@ hipError_t launch_qk_bwd(hipStream_t s, const QkShape& a, const uint16_t* x, con
   if (!a.gq) return hipSuccess;
   qk_gain_kernel<<<2 * a.hd / 16, 1024, 0, s>>>(part, blocks, a.hd, dgq, dgk);
   return hipGetLastError();
+}
+
+// ----------------------------------- keys and values to a paged cache ---
+// The rows of qk_fwd_kernel with value heads behind their keys (same steps, same
+// arithmetic, so that a key has the bits that jn_qk_norm_rope gives it): queries go
+// to rows of y, keys and values to their places.  A wavefront finds its row's sequence
+// and page once, from all lanes (kv_find).  pos null: the place, of a tree's row
+// past + the depth of its branch.
+template <int E, int P2, bool NORM, bool ROPE, bool ONCE>
+__global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvBatch b, QkShape a, const uint16_t* x, uint16_t* y,
+                                                        int32_t parts) {
+  __shared__ __attribute__((aligned(16))) float lines[4][256];
+  constexpr int PER = 64 / P2;  // heads per step
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane % P2, slot = lane / P2;
+  const int64_t item = (int64_t)blockIdx.x * 4 + w;
+  const int32_t row = (int32_t)(item / parts);
+  if (row >= b.rows) return;
+  const int32_t heads = a.heads + 2 * a.kv, half = a.hd >> 1;
+  const int steps = (heads + PER - 1) / PER, part = (int)(item - (int64_t)row * parts);
+  const int s0 = steps * part / parts, s1 = steps * (part + 1) / parts;
+  const bool live = E * q < half;
+  const uint16_t* const xr = x + row * a.ldx + E * q;
+  QkRaw<E> v[kQkStep][2];
+  auto fetch = [&](int s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < kQkStep; ++j) {
+      const int h = (s + j) * PER + slot;
+      v[j][0] = v[j][1] = QkRaw<E>{};
+      if (s + j < s1 && live && h < heads) {
+        v[j][0] = raw<E>(xr + h * a.hd);
+        v[j][1] = raw<E>(xr + half + h * a.hd);
+      }
+    }
+  };
+  fetch(s0);  // in flight under the search and the sines
+  const int32_t seq = kv_find(b, row, lane);
+  if (seq >= b.n_seqs) return;
+  const KvSeq sq = kv_seq(b, seq);
+  const int32_t j0 = row - sq.row0;
+  if (j0 < 0 || j0 >= sq.n) return;
+  const int32_t place = sq.past + j0;
+  const int32_t page = kv_page(b, c, b.pages + (int64_t)seq * b.max_pages, place);
+  const int64_t at = kv_at(c, max(page, 0), 0, place) + E * q, per_head = (int64_t)a.hd << c.page_log2;
+  QkGains<E> g;
+  if constexpr (NORM) g.load(a, live ? E * q : 0);
+  const float* const line = lines[w] + (live ? E * q : 0);
+  const float part_of = 1.f / (float)a.hd;
+  if constexpr (ROPE) {
+    if (a.pos) {
+      row_turns(a, row, lane, lines[w]);
+    } else {
+      int32_t deep = j0;
+      if (b.parents) {
+        deep = 0;
+        for (int32_t p = kv_parent(b.parents + sq.row0, j0); p >= 0; p = kv_parent(b.parents + sq.row0, p)) ++deep;
+      }
+      place_turns(a, sq.past + deep, lane, lines[w]);
+    }
+  }
+  for (int s = s0; s < s1; s += kQkStep) {
+    if (s > s0) fetch(s);
+#pragma unroll
+    for (int j = 0; j < kQkStep; ++j) {
+      if (s + j >= s1) break;
+      const int h = (s + j) * PER + slot;
+      float u[2 * E];
+      widen<E>(v[j][0], u);
+      widen<E>(v[j][1], u + E);
+      const bool value = h >= a.heads + a.kv;
+      if constexpr (NORM) {
+        float ss = 0.f, gv[2 * E];
+#pragma unroll
+        for (int k = 0; k < 2 * E; ++k) ss = fmaf(u[k], u[k], ss);
+        const float r = rsqrtf(fmaf(head_sum<P2>(ss), part_of, a.eps));
+        g.get((s + j + 1) * PER > a.heads, h >= a.heads, gv);
+#pragma unroll
+        for (int k = 0; k < 2 * E; ++k) u[k] = value ? u[k] : u[k] * r * gv[k];
+      }
+      if constexpr (ROPE) {
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+          const float p = u[k], o = u[E + k], cs = line[k], sn = line[128 + k];
+          u[k] = value ? p : p * cs - o * sn;
+          u[E + k] = value ? o : o * cs + p * sn;
+        }
+      }
+      if (!live || h >= heads) continue;
+      if (h < a.heads) {
+        uint16_t* const to = y + row * a.ldy + (int64_t)h * a.hd + E * q;
+        put_bf<E, ONCE>(to, u);
+        put_bf<E, ONCE>(to + half, u + E);
+      } else if (page >= 0) {
+        uint16_t* const to = (value ? c.v : c.k) + at + (h - a.heads - (value ? a.kv : 0)) * per_head;
+        if (value) {  // as they came: no NaN is made another
+          *reinterpret_cast<uint2*>(to) = __builtin_bit_cast(uint2, v[j][0]);
+          *reinterpret_cast<uint2*>(to + half) = __builtin_bit_cast(uint2, v[j][1]);
+        } else {
+          put_bf<E, false>(to, u);
+          put_bf<E, false>(to + half, u + E);
+        }
+      }
+    }
+  }
+}
+
+hipError_t launch_kv_append(hipStream_t s, const KvCache& c, const KvBatch& b, const QkShape& a, bool rope,
+                            const uint16_t* x, uint16_t* q) {
+  if (b.rows < 1 || a.hd < 16 || a.hd > 256 || a.hd % 16 != 0 || !a.gq != !a.gk) return hipErrorInvalidValue;
+  auto go = [&](auto p2, auto norm, auto rot, auto once) {
+    constexpr int PER = 64 / decltype(p2)::value;
+    const int32_t steps = (a.heads + 2 * a.kv + PER - 1) / PER;
+    const int32_t parts = b.rows < kQkFewRows ? steps : 1;
+    const int64_t blocks = ((int64_t)b.rows * parts + 3) / 4;
+    kv_append_kernel<kQkFwdE, p2(), norm(), rot(), once()><<<(unsigned)blocks, 256, 0, s>>>(c, b, a, x, q, parts);
+    return hipGetLastError();
+  };
+  auto kind = [&](auto p2, auto once) {
+    const std::true_type yes;
+    const std::false_type no;
+    if (a.gq) return rope ? go(p2, yes, yes, once) : go(p2, yes, no, once);
+    return rope ? go(p2, no, yes, once) : go(p2, no, no, once);
+  };
+  auto width = [&](auto p2) {
+    return (int64_t)b.rows * a.heads * a.hd * 2 > kStreamBytes ? kind(p2, std::true_type()) : kind(p2, std::false_type());
+  };
+  constexpr int M = 16 / kQkFwdE;
+  if (a.hd <= 32) return width(std::integral_constant<int, M>());
+  if (a.hd <= 64) return width(std::integral_constant<int, 2 * M>());
+  if (a.hd <= 128) return width(std::integral_constant<int, 4 * M>());
+  return width(std::integral_constant<int, 8 * M>());
 }
 
 }  // namespace jnx

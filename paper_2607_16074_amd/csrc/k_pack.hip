@@ -5,6 +5,7 @@
 
 #include "jn_device.h"
 #include "jn_internal.h"
+#include "jn_kv.h"
 
 namespace jnx {
 
@@ -254,6 +255,65 @@ hipError_t launch_unpack(hipStream_t s, const ReqEntry* req_table, int32_t R, co
                                     : go(v, std::false_type(), std::false_type());
   };
   return vec16 ? form(u32x4p()) : form(uint32_t());
+}
+
+// ------------------------------------------ the branch of a tree that stays ---
+// Row past + path[k] of every head and layer to row past + k, keys and values.  A
+// thread owns 16 bytes of a head's rows and takes the path in order, eight rows at a
+// time: path[k] >= k ascends, so a row that a later step reads is not one that an
+// earlier step wrote, and within a step every load stands before the stores.
+constexpr int kKeepStep = 8;
+__global__ __launch_bounds__(256) void kv_keep_kernel(KvCache c, KvBatch b, const int32_t* __restrict__ path,
+                                                      int32_t max_path, const int32_t* __restrict__ n_path,
+                                                      int32_t* past_out, int32_t per) {
+  const int32_t s = blockIdx.x / per, part = blockIdx.x - s * per;
+  const int32_t past = min(max(b.past[s], 0), b.places), n = min(max(n_path[s], 0), max_path);
+  if (past_out && part == 0 && threadIdx.x == 0) past_out[s] = past + n;
+  const int32_t chunks = c.hd >> 3;
+  const int64_t items = (int64_t)c.n_layers * 2 * c.kv * chunks, i = (int64_t)part * 256 + threadIdx.x;
+  if (i >= items) return;
+  const int32_t chunk = (int32_t)(i % chunks), h = (int32_t)(i / chunks % c.kv);
+  const int64_t lv = i / chunks / c.kv;
+  uint16_t* const base = ((lv & 1) ? c.v : c.k) + (lv >> 1) * c.ld_layer + 8 * chunk;
+  const int32_t* const pages = b.pages + (int64_t)s * b.max_pages;
+  int32_t last = -1;
+  for (int32_t k0 = 0; k0 < n; k0 += kKeepStep) {
+    uint4 v[kKeepStep];
+    int64_t to[kKeepStep];
+#pragma unroll
+    for (int e = 0; e < kKeepStep; ++e) {
+      const int32_t k = k0 + e, j = k < n ? path[(int64_t)s * max_path + k] : -1;
+      to[e] = -1;
+      if (j <= last || j < k || j >= b.max_new) continue;
+      last = j;
+      if (j == k) continue;
+      const int32_t from = kv_page(b, c, pages, past + j), into = kv_page(b, c, pages, past + k);
+      if (from < 0 || into < 0) continue;
+      v[e] = *reinterpret_cast<const uint4*>(base + kv_at(c, from, h, past + j));
+      to[e] = kv_at(c, into, h, past + k);
+    }
+#pragma unroll
+    for (int e = 0; e < kKeepStep; ++e)
+      if (to[e] >= 0) *reinterpret_cast<uint4*>(base + to[e]) = v[e];
+  }
+}
+
+// past_out where it is past itself, which other workgroups of the move read.
+__global__ __launch_bounds__(256) void kv_past_kernel(KvBatch b, int32_t max_path, const int32_t* __restrict__ n_path,
+                                                      int32_t* past) {
+  const int32_t s = blockIdx.x * 256 + threadIdx.x;
+  if (s < b.n_seqs) past[s] = min(max(past[s], 0), b.places) + min(max(n_path[s], 0), max_path);
+}
+
+hipError_t launch_kv_keep(hipStream_t s, const KvCache& c, const KvBatch& b, const int32_t* path, int32_t max_path,
+                          const int32_t* n_path, int32_t* past_out) {
+  const int64_t per = kv_keep_blocks(c);
+  if (b.n_seqs < 1 || per * b.n_seqs > kMostBlocks) return hipErrorInvalidValue;
+  const bool own = past_out == b.past;
+  kv_keep_kernel<<<(unsigned)(per * b.n_seqs), 256, 0, s>>>(c, b, path, max_path, n_path, own ? nullptr : past_out,
+                                                            (int32_t)per);
+  if (own) kv_past_kernel<<<(b.n_seqs + 255) / 256, 256, 0, s>>>(b, max_path, n_path, past_out);
+  return hipGetLastError();
 }
 
 }  // namespace jnx
