@@ -36,6 +36,9 @@
 // head-dim row, as the MFMA wants.  Statistics in fp32, P rounded to bf16.
 // Head width 256 runs attn16_fwd_kernel: the same algorithm with 8 waves x 16
 // query rows and v_mfma_f32_16x16x32_bf16 (two waves per SIMD).
+#include <algorithm>
+#include <type_traits>
+
 #include "jn_device.h"
 #include "jn_internal.h"
 #include "jn_kv.h"
@@ -749,6 +752,591 @@ hipError_t launch_rope(hipStream_t s, void* qkv, int32_t ld, const int32_t* toke
 }
 
 // ------------------------------------------- attention over a paged cache ---
+// A sequence's new rows j and the query heads g of one key head h are the query rows
+// r = j G + g of a unit (sequence, key head); all of them read the same keys and
+// values, the cached rows and (as the mask says) the new ones. How many keys each unit
+// has is known on the device only, so the units' key tiles are laid end to end and
+// every workgroup takes an equal run of them: whatever the lengths, all finish
+// together. A unit that several workgroups hold is left as partial results (O, m, l)
+// which kv_join_kernel adds. A workgroup finds its run from the sequences' lengths by
+// itself (KvWalk), so there is no planning launch; at most two of its units are
+// not whole, the first (slot 0) and the last (slot 1).
+struct KvDesc {          // of a slot of a workgroup: its part of a unit
+  int32_t seq, h, wa, wb;  // held by workgroups wa .. wb; wb < 0: nothing
+};
+struct KvWork {
+  KvDesc* desc;          // [P][2]
+  float2* ml;            // [P][2][rows]
+  float* o;              // [P][2][rows][HD]
+  int32_t P;             // workgroups, a multiple of 8
+  int32_t group;         // query heads of a key head
+};
+
+// x * P / total and the like for x, P <= total * 1024: in 32 bits where it fits.
+__device__ __forceinline__ int64_t kv_div(int64_t a, int64_t b) {
+  if (a < (1ll << 32) && b < (1ll << 32)) return (int64_t)((uint32_t)a / (uint32_t)b);
+  return a / b;
+}
+
+__device__ __forceinline__ int64_t wave_scan64(int64_t v, int lane) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t u = __shfl_up(v, o, kWave);
+    if (lane >= o) v += u;
+  }
+  return v;
+}
+
+// Lane l's value, known to be the same for all lanes (in scalar registers).
+__device__ __forceinline__ int64_t wave_get64(int64_t v, int l) {
+  const uint32_t lo = __builtin_amdgcn_readlane((int32_t)v, l), hi = __builtin_amdgcn_readlane((int32_t)(v >> 32), l);
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// The run of tiles [pos, end) of workgroup p, walked unit by unit. KT keys a tile.
+template <int KT>
+struct KvWalk {
+  int64_t total, pos, end, unit0;  // unit0: first tile of the current unit
+  int32_t P, p;                    // workgroups with work, and this one's place in their order
+  int32_t seq, h, tiles;           // tiles of a unit of the current sequence
+  KvSeq sq;
+  int32_t kend;                    // keys of the sequence, cached and new
+
+  static __device__ __forceinline__ int32_t keys(const KvBatch& b, const KvSeq& q) {
+    return q.n > 0 ? min(q.past + q.n, b.places) : 0;
+  }
+  static __device__ __forceinline__ int32_t tiles_of(int32_t keys) { return (keys + KT - 1) / KT; }
+
+  // Runs that follow each other go to one XCD, whose workgroups are every eighth; with
+  // fewer tiles than workgroups a tile each, so that no run between two others is empty.
+  __device__ __forceinline__ bool start(const KvBatch& b, int32_t kv, int32_t most, int lane) {
+    int64_t all = 0;
+    int32_t mine = 0;
+    for (int32_t s0 = 0; s0 < b.n_seqs; s0 += 64) {
+      mine = s0 + lane < b.n_seqs ? tiles_of(keys(b, kv_seq(b, s0 + lane))) : 0;
+      all += mine;
+    }
+    int64_t scan = wave_scan64(all, lane);
+    total = wave_get64(scan, 63) * kv;
+    p = total < most ? blockIdx.x : (blockIdx.x & 7) * (most >> 3) + (blockIdx.x >> 3);
+    P = (int32_t)min(total, (int64_t)most);
+    if (p >= P) return false;
+    pos = kv_div(total * p, P);
+    end = kv_div(total * (p + 1), P);
+    int64_t before = 0;
+    seq = 0;
+    for (int32_t s0 = 0;; s0 += 64) {
+      if (b.n_seqs > 64) {
+        mine = s0 + lane < b.n_seqs ? tiles_of(keys(b, kv_seq(b, s0 + lane))) : 0;
+        scan = wave_scan64(mine, lane);
+      }
+      const int32_t c = __builtin_popcountll(__ballot((before + scan) * kv <= pos));
+      if (c < 64) {
+        seq = s0 + c;
+        before += wave_get64(scan - mine, c);
+        break;
+      }
+      before += wave_get64(scan, 63);
+    }
+    take(b);
+    const int64_t rest = pos - before * kv;
+    h = (int32_t)kv_div(rest, tiles);
+    unit0 = before * kv + (int64_t)h * tiles;
+    return true;
+  }
+  __device__ __forceinline__ void take(const KvBatch& b) {
+    const KvSeq q = kv_seq(b, seq);
+    sq = KvSeq{__builtin_amdgcn_readfirstlane(q.past), __builtin_amdgcn_readfirstlane(q.row0),
+               __builtin_amdgcn_readfirstlane(q.n)};
+    kend = keys(b, sq);
+    tiles = tiles_of(kend);
+  }
+  // To the unit behind the current one (pos < end: there is one).
+  __device__ __forceinline__ void next(const KvBatch& b, int32_t kv) {
+    unit0 += tiles;
+    if (++h < kv) return;
+    h = 0;
+    do {
+      ++seq;
+      take(b);
+    } while (tiles == 0);
+  }
+  __device__ __forceinline__ int32_t holder(int64_t x) const { return (int32_t)kv_div((x + 1) * P - 1, total); }
+};
+
+// s_waitcnt vmcnt(N) alone.
+template <int N>
+__device__ __forceinline__ void kv_wait_vmcnt() {
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Four (two) V^T fragments of 16 columns x 32 keys of a V tile: rows a and a + 16 of
+// two transposed reads each, at LDS byte addresses at[t] + off. The wait stands in the
+// same statement: a read in flight never outlives it (and the compiler's own form would
+// wait for every prefetch in flight).
+template <int HD>
+__device__ __forceinline__ void kv_read_v(const uint32_t* at, uint32_t off, bf16x8 (&v)[4]) {
+  uint64_t r[8];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8\n\t"
+      "ds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %2, %9\n\t"
+      "ds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %4, %10\n\t"
+      "ds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %6, %11\n\t"
+      "ds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+      : "v"(at[0] + off), "v"(at[1] + off), "v"(at[2] + off), "v"(at[3] + off), "n"(16 * HD * 2)
+      : "memory");
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const bf16x4 lo = __builtin_bit_cast(bf16x4, r[2 * t]), hi = __builtin_bit_cast(bf16x4, r[2 * t + 1]);
+    v[t] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+}
+template <int HD>
+__device__ __forceinline__ void kv_read_v(const uint32_t* at, uint32_t off, bf16x8 (&v)[2]) {
+  uint64_t r[4];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %4\n\t"
+      "ds_read_b64_tr_b16 %1, %4 offset:%6\n\t"
+      "ds_read_b64_tr_b16 %2, %5\n\t"
+      "ds_read_b64_tr_b16 %3, %5 offset:%6\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3])
+      : "v"(at[0] + off), "v"(at[1] + off), "n"(16 * HD * 2)
+      : "memory");
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const bf16x4 lo = __builtin_bit_cast(bf16x4, r[2 * t]), hi = __builtin_bit_cast(bf16x4, r[2 * t + 1]);
+    v[t] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+}
+
+__device__ __forceinline__ uint32_t kv_lds(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+
+// What the new rows of a tree see, as bits of the new rows: row j itself and its
+// ancestors. All threads of the workgroup; rows j0 .. j0 + rows - 1.
+struct KvTree {
+  uint16_t up[JN_KV_TREE_ROWS];
+  uint64_t seen[128][JN_KV_TREE_ROWS / 64];
+};
+template <int THREADS>
+__device__ __forceinline__ void kv_tree(KvTree& t, const KvBatch& b, const KvSeq& sq, int32_t j0, int32_t rows) {
+  for (int32_t j = threadIdx.x; j < sq.n; j += THREADS) t.up[j] = (uint16_t)kv_parent(b.parents + sq.row0, j);
+  __syncthreads();
+  for (int32_t i = threadIdx.x; i < rows && j0 + i < sq.n; i += THREADS) {
+    uint64_t w[4] = {0, 0, 0, 0};
+    for (uint32_t j = j0 + i; j != 0xffffu; j = t.up[j]) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if ((j >> 6) == (uint32_t)k) w[k] |= 1ull << (j & 63);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) t.seen[i][k] = w[k];
+  }
+  __syncthreads();
+}
+// Bits of new rows k .. k + 31 (k may be below 0 or beyond the last).
+__device__ __forceinline__ uint32_t kv_seen(const uint64_t* w, int32_t k) {
+  if (k <= -32 || k >= JN_KV_TREE_ROWS) return 0;
+  if (k < 0) return (uint32_t)w[0] << -k;
+  const int i = k >> 6, s = k & 63;
+  uint64_t v = w[i] >> s;
+  if (s > 32 && i + 1 < JN_KV_TREE_ROWS / 64) v |= w[i + 1] << (64 - s);
+  return (uint32_t)v;
+}
+
+// ---- few query rows (a unit has at most 16 NB) ----
+// The time is the reading of keys and values, each read once: four wavefronts, each
+// with 32 keys of a 128-key tile and all query rows. Keys go from the cache to
+// registers in the layout that the product takes (16 keys a fragment: 16 bytes a
+// lane of a row), values by DMA to the wavefront's own LDS tile, from which
+// transposed reads make V^T; the next step's are in flight under each step, and
+// nothing waits for another wavefront before the unit's end, where their O, m and l are
+// added in LDS.
+//   S^T = K Q^T, O^T += V^T P^T as in attn16_fwd_kernel.
+// A key's page is the same for the 16 keys of a fragment (pages are multiples of 16),
+// so page numbers are read once for all lanes. Values of places that no row sees are set to zero
+// in LDS (0 * NaN is NaN); a value that some rows of a tile see and others do not, and
+// that is not finite, is taken out of the product and added where it is seen.
+template <int HD, int NB>
+__global__ __launch_bounds__(256, HD * NB >= 256 ? 1 : 2) void kv_few_kernel(KvCache c, KvBatch b, KvAttn a, KvWork wk) {
+  constexpr int R = 16 * NB, KT = 128;
+  constexpr int NC = HD / 32, NT = HD / 16, CPR = HD / 8, RPI = 512 / HD;
+  constexpr int NV = 32 / RPI, NK = 2 * NC;  // DMA instructions and key loads of a step
+  constexpr int TG = NT < 4 ? NT : 4;        // V^T fragments read together
+  constexpr int LD = HD + 4;
+  __shared__ __attribute__((aligned(1024))) uint16_t vt[4][2][32 * HD];
+  __shared__ KvTree tree;
+  __shared__ float sm[4][R], sl[4][R];
+  static_assert(4 * 16 * LD * 4 <= sizeof(vt), "the sums use the tiles' memory");
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int j16 = lane & 15, quad = lane >> 4;
+  KvWalk<KT> run;
+  const bool any = run.start(b, c.kv, wk.P, lane);
+  const int32_t p = run.p;
+  if (tid < 2) wk.desc[2 * p + tid].wb = -1;
+  if (!any) return;
+  const int32_t G = wk.group;
+
+  const int vrow = 4 * quad + (j16 >> 2), vswz = attn_swz<HD>(vrow);
+  uint32_t vat[NT];  // the lane's transposed reads of the first tile
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int col = t * 16 + 4 * (j16 & 3);
+    vat[t] = kv_lds(&vt[wave][0][vrow * HD + (((col >> 3) ^ vswz) * 8) + (col & 7)]);
+  }
+  const int drow = lane / CPR;  // of a DMA instruction
+  int32_t doff[RPI >= 16 ? 1 : 16 / RPI];
+#pragma unroll
+  for (int v = 0; v < 16 / RPI; ++v) {
+    const int r = v * RPI + drow;
+    doff[v] = r * HD + (((lane % CPR) ^ attn_swz<HD>(r)) * 8);
+  }
+  const int32_t koff = j16 * HD + quad * 8;
+
+  while (true) {
+    const KvSeq sq = run.sq;
+    const int32_t M = sq.n * G, kend = run.kend;
+    const int32_t ta = (int32_t)(run.pos - run.unit0);
+    const int32_t tb = (int32_t)min((int64_t)run.tiles, run.end - run.unit0);
+    const int32_t* const pages = b.pages + (int64_t)run.seq * b.max_pages;
+    const bool masks = tb * KT > sq.past;
+    if (b.parents && masks) kv_tree<256>(tree, b, sq, 0, R);
+
+    bf16x8 qf[NC][NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int32_t r = nb * 16 + j16, j = r / G;
+      const uint16_t* const qr = a.q + (int64_t)(sq.row0 + (r < M ? j : 0)) * a.ldq +
+                                 ((int64_t)run.h * G + (r < M ? r - j * G : 0)) * HD + quad * 8;
+#pragma unroll
+      for (int k = 0; k < NC; ++k) qf[k][nb] = *reinterpret_cast<const bf16x8*>(qr + k * 32);
+    }
+    f32x4 o[NT][NB];
+    float m_run[NB], l_run[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      m_run[nb] = -INFINITY;
+      l_run[nb] = 0.f;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) o[t][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    const int32_t steps = tb - ta;
+    // of a step: its keys' page numbers and their heads' offsets
+    struct Pages {
+      int32_t page[2];
+      int64_t at[2];
+    };
+    auto pages_of = [&](int32_t i) __attribute__((always_inline)) {
+      Pages x;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int32_t t = (ta + i) * KT + wave * 32 + 16 * e;
+        x.page[e] = __builtin_amdgcn_readfirstlane(t < kend ? kv_page(b, c, pages, t) : -1);
+        x.at[e] = x.page[e] >= 0 ? kv_at(c, x.page[e], run.h, t) : 0;
+      }
+      return x;
+    };
+    auto fetch_v = [&](const Pages& x, int stage) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int v = 0; v < 16 / RPI; ++v)
+          __builtin_amdgcn_global_load_lds(JN_GPTR(c.v + x.at[e] + doff[v]),
+                                           JN_LPTR(&vt[wave][stage][e * 16 * HD + v * 512]), 16, 0, 0);
+    };
+    bf16x8 kf[2][NC];
+    auto fetch_k = [&](const Pages& x) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int n = 0; n < NC; ++n) kf[e][n] = *reinterpret_cast<const bf16x8*>(c.k + x.at[e] + koff + n * 32);
+    };
+    Pages use = pages_of(0), next = use;
+    fetch_v(use, 0);
+    fetch_k(use);
+    for (int32_t i = 0; i < steps; ++i) {
+      const int32_t t = (ta + i) * KT + wave * 32;
+      const bool more = i + 1 < steps;
+      const uint32_t stage = (i & 1) * (32 * HD * 2);
+      if (more) {
+        next = pages_of(i + 1);
+        fetch_v(next, (i + 1) & 1);
+      }
+      f32x4 s[2][NB];
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) s[e][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int n = 0; n < NC; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+            s[e][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[e][n], qf[n][nb], s[e][nb], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if (more) fetch_k(next);  // into the registers that the product has read
+      __builtin_amdgcn_sched_barrier(0);
+      const bool hole = use.page[0] < 0 || use.page[1] < 0 || t + 32 > kend;  // places that no row sees
+      const bool mask = t + 32 > sq.past;                                   // or not every row
+      if (hole || mask) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const int32_t j = (nb * 16 + j16) / G;
+          uint32_t bits = 0xffffffffu;  // of keys t .. t + 31
+          if (mask && !b.whole) {
+            const int32_t seen = sq.past + j + 1 - t;  // a chain's row sees keys below this
+            bits = seen >= 32 ? 0xffffffffu : seen <= 0 ? 0u : (1u << seen) - 1;
+            if (b.parents) {
+              const int32_t old = sq.past - t;  // keys below this are cached rows
+              bits = (old >= 32 ? 0xffffffffu : old <= 0 ? 0u : (1u << old) - 1) |
+                     kv_seen(tree.seen[min(j, sq.n - 1)], t - sq.past);
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int32_t x = e * 16 + quad * 4 + k;
+              if (use.page[e] < 0 || t + x >= kend || !((bits >> x) & 1)) s[e][nb][k] = -INFINITY;
+            }
+        }
+      }
+      bf16x8 pf[NB];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) top = fmaxf(top, s[e][nb][k]);
+        top = max_xor32(max_xor16(top)) * a.scale_log2;
+        if (__any(top > m_run[nb] + kRescale)) {
+          const float m_new = fmaxf(m_run[nb], top);
+          const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[nb] - m_new);
+          l_run[nb] *= alpha;
+          m_run[nb] = m_new;
+#pragma unroll
+          for (int t2 = 0; t2 < NT; ++t2) o[t2][nb] *= alpha;
+        }
+        const float m = m_run[nb] == -INFINITY ? 0.f : m_run[nb];  // (a row that has seen nothing yet)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[e][nb][k], a.scale_log2, -m));
+            l_run[nb] += x;
+            pf[nb][4 * e + k] = (__bf16)x;
+          }
+      }
+      if (more)
+        kv_wait_vmcnt<NK + NV>();  // this step's values have landed; the next step's loads may be in flight
+      else
+        kv_wait_vmcnt<0>();
+      if (hole || mask) {
+        // rows of the tile that nobody sees become zeros, others that are not finite too
+        // once the rows that see them have them: a lane holds one query row of a product, so
+        // what a product with this key alone gives is taken where its probability is not zero
+        const int32_t r = lane >> 1;
+        const bool none = (r < 16 ? use.page[0] : use.page[1]) < 0 || t + r >= kend;
+        bool bad = false;
+        uint16_t* const row = &vt[wave][i & 1][r * HD + (lane & 1) * (HD / 2)];
+#pragma unroll 1
+        for (int e = 0; e < HD / 2; e += 8) {
+          const uint4 v = *reinterpret_cast<const uint4*>(row + e);
+          const uint32_t x = v.x & 0x7fff7fffu, y = v.y & 0x7fff7fffu, z = v.z & 0x7fff7fffu, w = v.w & 0x7fff7fffu;
+          bad |= (((x + 0x00800080u) | (y + 0x00800080u) | (z + 0x00800080u) | (w + 0x00800080u)) & 0x80008000u) != 0;
+        }
+        uint64_t odd = __ballot(!none && bad);
+        const bool zero = none || ((odd >> (lane & ~1)) & 3) != 0;
+#pragma unroll 1
+        while (odd != 0) {
+          const int k = __builtin_ctzll(odd) >> 1;
+          odd &= ~(3ull << (2 * k));
+          // key k is element 4 (k / 16) + k % 4 of quad (k / 4) % 4
+          const int slot = quad == ((k >> 2) & 3) ? 4 * (k >> 4) + (k & 3) : -1;
+          bool sees[NB];
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            bool x = false;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x |= e == slot && (float)pf[nb][e] != 0.f;
+            sees[nb] = (__ballot(x) >> (((k >> 2) & 3) * 16 + j16)) & 1;
+          }
+#pragma unroll
+          for (int t0 = 0; t0 < NT; t0 += TG) {
+            bf16x8 vf[TG];
+            kv_read_v<HD>(vat + t0, stage, vf);
+#pragma unroll
+            for (int x = 0; x < TG; ++x) {
+              bf16x8 only;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) only[e] = e == slot ? vf[x][e] : (__bf16)0.f;
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) {
+                const f32x4 v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(only, pf[nb], o[t0 + x][nb], 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[t0 + x][nb][e] = sees[nb] ? v[e] : o[t0 + x][nb][e];
+              }
+            }
+          }
+        }
+        if (zero)
+#pragma unroll 1
+          for (int e = 0; e < HD / 2; e += 8) *reinterpret_cast<uint4*>(row + e) = make_uint4(0, 0, 0, 0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      }
+#pragma unroll
+      for (int t0 = 0; t0 < NT; t0 += TG) {
+        bf16x8 vf[TG];
+        kv_read_v<HD>(vat + t0, stage, vf);
+#pragma unroll
+        for (int k = 0; k < TG; ++k)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+            o[t0 + k][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[k], pf[nb], o[t0 + k][nb], 0, 0, 0);
+      }
+      use = next;
+    }
+
+    // the wavefronts' results, added
+    const bool whole = ta == 0 && tb == run.tiles;
+    const int slot = ta > 0 ? 0 : 1;
+    if (!whole && tid == 0) {
+      KvDesc d{run.seq, run.h, run.holder(run.unit0), run.holder(run.unit0 + run.tiles - 1)};
+      wk.desc[2 * p + slot] = d;
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const float l = sum_xor32(sum_xor16(l_run[nb]));
+      if (quad == 0) {
+        sm[wave][nb * 16 + j16] = m_run[nb];
+        sl[wave][nb * 16 + j16] = l;
+      }
+    }
+    float* const sums = reinterpret_cast<float*>(&vt[0][0][0]);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      if (nb * 16 >= M) break;
+      __syncthreads();  // m and l are there; the tiles, or the last rows' sums, are read
+      const int r = nb * 16 + j16;
+      const float top = fmaxf(fmaxf(sm[0][r], sm[1][r]), fmaxf(sm[2][r], sm[3][r]));
+      const float f = m_run[nb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[nb] - top);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        *reinterpret_cast<f32x4*>(&sums[(wave * 16 + j16) * LD + t * 16 + quad * 4]) = o[t][nb] * f;
+      __syncthreads();
+      for (int i = tid; i < 16 * CPR; i += 256) {
+        const int row = i / CPR, col = (i % CPR) * 8, rr = nb * 16 + row;
+        if (rr >= M) break;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] += sums[(w * 16 + row) * LD + col + e];
+        const float mt = fmaxf(fmaxf(sm[0][rr], sm[1][rr]), fmaxf(sm[2][rr], sm[3][rr]));
+        float l = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) l += sm[w][rr] == -INFINITY ? 0.f : sl[w][rr] * __builtin_amdgcn_exp2f(sm[w][rr] - mt);
+        if (whole) {
+          const float inv = l == 0.f ? 0.f : 1.f / l;
+          uint4 x;
+          x.x = pack_bf2(v[0] * inv, v[1] * inv);
+          x.y = pack_bf2(v[2] * inv, v[3] * inv);
+          x.z = pack_bf2(v[4] * inv, v[5] * inv);
+          x.w = pack_bf2(v[6] * inv, v[7] * inv);
+          const int32_t j = rr / G;
+          *reinterpret_cast<uint4*>(a.out + (int64_t)(sq.row0 + j) * a.ldo + ((int64_t)run.h * G + rr - j * G) * HD + col) = x;
+        } else {
+          const int64_t at = (int64_t)(2 * p + slot) * R + rr;
+          float4* const to = reinterpret_cast<float4*>(wk.o + at * HD + col);
+          to[0] = make_float4(v[0], v[1], v[2], v[3]);
+          to[1] = make_float4(v[4], v[5], v[6], v[7]);
+          if (col == 0) wk.ml[at] = make_float2(mt, l);
+        }
+      }
+    }
+    run.pos = run.unit0 + tb;
+    if (run.pos >= run.end) break;
+    __syncthreads();  // the sums are read before the next unit's tiles overwrite them
+    run.next(b, c.kv);
+  }
+}
+
+// Partial results of units that several workgroups hold: workgroup p adds rows p - wa,
+// p - wa + parts, ... of the units of its two slots, so that all that took part in a
+// unit share its rows. `rows`: of a slot.
+template <int HD>
+__global__ __launch_bounds__(256) void kv_join_kernel(KvBatch b, KvAttn a, KvWork wk, int32_t rows) {
+  constexpr int LN = HD / 4, GR = 256 / LN;  // lanes of a row, groups that share the parts
+  __shared__ float4 so[GR][LN];
+  __shared__ float sl[GR], tops[4];
+  const int tid = threadIdx.x, ln = tid % LN, gr = tid / LN;
+  const int32_t p = blockIdx.x, G = wk.group;
+  for (int slot = 0; slot < 2; ++slot) {
+    const KvDesc d = wk.desc[2 * p + slot];
+    if (d.wb < 0) continue;
+    const KvSeq sq = kv_seq(b, d.seq);
+    const int32_t parts = d.wb - d.wa + 1, M = min(sq.n * G, rows);
+    auto part = [&](int32_t k) { return (int64_t)(2 * (d.wa + k) + (k == 0 ? 1 : 0)) * rows; };
+    for (int32_t r = p - d.wa; r < M; r += parts) {
+      float top = -INFINITY;
+      for (int32_t k = tid; k < parts; k += 256) top = fmaxf(top, wk.ml[part(k) + r].x);
+      top = wave_max(top);
+      if ((tid & 63) == 0) tops[tid >> 6] = top;
+      __syncthreads();
+      top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      float l = 0.f;
+#pragma unroll 4
+      for (int32_t k = gr; k < parts; k += GR) {
+        const int64_t at = part(k) + r;
+        const float2 ml = wk.ml[at];
+        const float4 x = *reinterpret_cast<const float4*>(wk.o + at * HD + 4 * ln);
+        const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+        l = fmaf(f, ml.y, l);
+        v.x = fmaf(f, x.x, v.x);
+        v.y = fmaf(f, x.y, v.y);
+        v.z = fmaf(f, x.z, v.z);
+        v.w = fmaf(f, x.w, v.w);
+      }
+      so[gr][ln] = v;
+      if (ln == 0) sl[gr] = l;
+      __syncthreads();
+      if (gr == 0) {
+#pragma unroll
+        for (int k = 1; k < GR; ++k) {
+          const float4 x = so[k][ln];
+          v.x += x.x;
+          v.y += x.y;
+          v.z += x.z;
+          v.w += x.w;
+          l += sl[k];
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const int32_t j = r / G;
+        *reinterpret_cast<uint2*>(a.out + (int64_t)(sq.row0 + j) * a.ldo + ((int64_t)d.h * G + r - j * G) * HD + 4 * ln) =
+            make_uint2(pack_bf2(v.x * inv, v.y * inv), pack_bf2(v.z * inv, v.w * inv));
+      }
+      __syncthreads();
+    }
+  }
+}
+
 // One wavefront per new row and query head: 64 keys a step, a key a lane for the
 // scores, then a head-dim column (or four) a lane for the sum of the values seen.
 __global__ __launch_bounds__(64) void kv_attn_plain_kernel(KvCache c, KvBatch b, KvAttn a) {
@@ -803,11 +1391,60 @@ __global__ __launch_bounds__(64) void kv_attn_plain_kernel(KvCache c, KvBatch b,
       a.out[row * a.ldo + (int64_t)h * c.hd + lane + 64 * e] = f2bf(l == 0.f ? 0.f : o[e] / l);
 }
 
-size_t kv_attention_bytes(const KvCache& c, const KvBatch& b, int32_t heads) { return 0; }
+// Query rows of a unit's tile, and workgroups: as many as are resident together, and no
+// more than the batch can have tiles.
+struct KvPlan {
+  int32_t rows, P;
+  size_t desc, ml, total;
+};
+static KvPlan kv_plan(const KvCache& c, const KvBatch& b, int32_t heads) {
+  const int32_t G = heads / c.kv;
+  const int64_t M = (int64_t)std::min(b.max_new, b.rows) * G;
+  KvPlan k{};
+  if (M > (c.hd == 256 ? 32 : 64)) return k;
+  k.rows = M <= 16 ? 16 : M <= 32 ? 32 : 64;
+  const int64_t tiles = (int64_t)b.n_seqs * c.kv * ((b.places + 127) / 128);
+  const int64_t P = 256 * (c.hd == 256 ? 1 : 2);
+  k.P = (int32_t)std::min((tiles + 7) / 8 * 8, P);
+  k.desc = ((size_t)k.P * 2 * sizeof(KvDesc) + 255) / 256 * 256;
+  k.ml = ((size_t)k.P * 2 * k.rows * sizeof(float2) + 255) / 256 * 256;
+  k.total = k.desc + k.ml + (size_t)k.P * 2 * k.rows * c.hd * sizeof(float);
+  return k;
+}
+
+size_t kv_attention_bytes(const KvCache& c, const KvBatch& b, int32_t heads) { return kv_plan(c, b, heads).total; }
 
 hipError_t launch_kv_attention(hipStream_t s, const KvCache& c, const KvBatch& b, const KvAttn& a, void* ws) {
-  kv_attn_plain_kernel<<<(unsigned)((int64_t)b.rows * a.heads), 64, 0, s>>>(c, b, a);
-  return hipGetLastError();
+  const KvPlan k = kv_plan(c, b, a.heads);
+  if (k.P == 0) {
+    kv_attn_plain_kernel<<<(unsigned)((int64_t)b.rows * a.heads), 64, 0, s>>>(c, b, a);
+    return hipGetLastError();
+  }
+  KvWork w{};
+  w.desc = (KvDesc*)ws;
+  w.ml = (float2*)((char*)ws + k.desc);
+  w.o = (float*)((char*)ws + k.desc + k.ml);
+  w.P = k.P;
+  w.group = a.heads / c.kv;
+  auto go = [&](auto hd, auto nb) {
+    kv_few_kernel<hd(), nb()><<<k.P, 256, 0, s>>>(c, b, a, w);
+    kv_join_kernel<hd()><<<k.P, 256, 0, s>>>(b, a, w, 16 * nb());
+    return hipGetLastError();
+  };
+  auto rows = [&](auto hd) {
+    if (k.rows == 16) return go(hd, std::integral_constant<int, 1>());
+    if (k.rows == 32) return go(hd, std::integral_constant<int, 2>());
+    if constexpr (decltype(hd)::value < 256)
+      if (k.rows == 64) return go(hd, std::integral_constant<int, 4>());
+    return hipErrorInvalidValue;
+  };
+  switch (c.hd) {
+    case 32: return rows(std::integral_constant<int, 32>());
+    case 64: return rows(std::integral_constant<int, 64>());
+    case 128: return rows(std::integral_constant<int, 128>());
+    case 256: return rows(std::integral_constant<int, 256>());
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace jnx
