@@ -761,8 +761,8 @@ hipError_t launch_rope(hipStream_t s, void* qkv, int32_t ld, const int32_t* toke
 // which kv_join_kernel adds. A workgroup finds its run from the sequences' lengths by
 // itself (KvWalk), so there is no planning launch; at most two of its units are
 // not whole, the first (slot 0) and the last (slot 1).
-struct KvDesc {          // of a slot of a workgroup: its part of a unit
-  int32_t seq, h, wa, wb;  // held by workgroups wa .. wb; wb < 0: nothing
+struct KvDesc {                // of a slot of a workgroup: its part of a unit
+  int32_t seq, h, qt, wa, wb;  // held by workgroups wa .. wb; wb < 0: nothing
 };
 struct KvWork {
   KvDesc* desc;          // [P][2]
@@ -793,27 +793,47 @@ __device__ __forceinline__ int64_t wave_get64(int64_t v, int l) {
   return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
-// The run of tiles [pos, end) of workgroup p, walked unit by unit. KT keys a tile.
-template <int KT>
+// The run of tiles [pos, end) of a workgroup, walked unit by unit. KT keys a tile; R
+// query rows a tile of a unit (0: a unit has one tile of rows), a unit is then
+// (sequence, key head, row tile), and a chain's row tiles end at their last row's keys.
+template <int KT, int R>
 struct KvWalk {
   int64_t total, pos, end, unit0;  // unit0: first tile of the current unit
   int32_t P, p;                    // workgroups with work, and this one's place in their order
-  int32_t seq, h, tiles;           // tiles of a unit of the current sequence
+  int32_t seq, h, qt, tiles;       // the current unit, and its tiles
+  int32_t group;
   KvSeq sq;
-  int32_t kend;                    // keys of the sequence, cached and new
+  int32_t kend;                    // keys of the unit
 
-  static __device__ __forceinline__ int32_t keys(const KvBatch& b, const KvSeq& q) {
-    return q.n > 0 ? min(q.past + q.n, b.places) : 0;
+  static __device__ __forceinline__ int32_t row_tiles(const KvSeq& q, int32_t G) {
+    return R ? (int32_t)(((int64_t)q.n * G + R - 1) / R) : q.n > 0;
+  }
+  static __device__ __forceinline__ int32_t keys(const KvBatch& b, const KvSeq& q, int32_t G, int32_t qt) {
+    int32_t n = q.n;
+    if constexpr (R != 0)
+      if (!b.whole && !b.parents) n = min(n, (int32_t)(((int64_t)qt * R + R - 1) / G) + 1);
+    return min(q.past + n, b.places);
   }
   static __device__ __forceinline__ int32_t tiles_of(int32_t keys) { return (keys + KT - 1) / KT; }
+  // Tiles of a key head of sequence s.
+  static __device__ __forceinline__ int64_t of_seq(const KvBatch& b, int32_t G, int32_t s) {
+    if (s >= b.n_seqs) return 0;
+    const KvSeq q = kv_seq(b, s);
+    const int32_t nq = row_tiles(q, G);
+    if (nq == 0) return 0;
+    if (R == 0 || b.whole || b.parents) return (int64_t)nq * tiles_of(keys(b, q, G, 0));
+    int64_t sum = 0;
+    for (int32_t i = 0; i < nq; ++i) sum += tiles_of(keys(b, q, G, i));
+    return sum;
+  }
 
   // Runs that follow each other go to one XCD, whose workgroups are every eighth; with
   // fewer tiles than workgroups a tile each, so that no run between two others is empty.
-  __device__ __forceinline__ bool start(const KvBatch& b, int32_t kv, int32_t most, int lane) {
-    int64_t all = 0;
-    int32_t mine = 0;
+  __device__ __forceinline__ bool start(const KvBatch& b, int32_t kv, int32_t G, int32_t most, int lane) {
+    group = G;
+    int64_t all = 0, mine = 0;
     for (int32_t s0 = 0; s0 < b.n_seqs; s0 += 64) {
-      mine = s0 + lane < b.n_seqs ? tiles_of(keys(b, kv_seq(b, s0 + lane))) : 0;
+      mine = of_seq(b, G, s0 + lane);
       all += mine;
     }
     int64_t scan = wave_scan64(all, lane);
@@ -827,39 +847,66 @@ struct KvWalk {
     seq = 0;
     for (int32_t s0 = 0;; s0 += 64) {
       if (b.n_seqs > 64) {
-        mine = s0 + lane < b.n_seqs ? tiles_of(keys(b, kv_seq(b, s0 + lane))) : 0;
+        mine = of_seq(b, G, s0 + lane);
         scan = wave_scan64(mine, lane);
       }
       const int32_t c = __builtin_popcountll(__ballot((before + scan) * kv <= pos));
       if (c < 64) {
         seq = s0 + c;
         before += wave_get64(scan - mine, c);
+        mine = wave_get64(mine, c);
         break;
       }
       before += wave_get64(scan, 63);
     }
     take(b);
-    const int64_t rest = pos - before * kv;
-    h = (int32_t)kv_div(rest, tiles);
-    unit0 = before * kv + (int64_t)h * tiles;
+    int64_t rest = pos - before * kv;
+    h = (int32_t)kv_div(rest, mine);
+    rest -= h * mine;
+    unit0 = pos - rest;
+    qt = 0;
+    if constexpr (R != 0) {
+      const int32_t nq = row_tiles(sq, G);
+      for (int32_t q0 = 0;; q0 += 64) {
+        const int64_t t = q0 + lane < nq ? tiles_of(keys(b, sq, G, q0 + lane)) : 0;
+        const int64_t up = wave_scan64(t, lane);
+        const int32_t c = __builtin_popcountll(__ballot(up <= rest));
+        if (c < 64) {
+          qt = q0 + c;
+          unit0 += wave_get64(up - t, c);
+          break;
+        }
+        unit0 += wave_get64(up, 63);
+        rest -= wave_get64(up, 63);
+      }
+      unit(b);
+    }
     return true;
+  }
+  __device__ __forceinline__ void unit(const KvBatch& b) {
+    kend = keys(b, sq, group, qt);
+    tiles = tiles_of(kend);
   }
   __device__ __forceinline__ void take(const KvBatch& b) {
     const KvSeq q = kv_seq(b, seq);
     sq = KvSeq{__builtin_amdgcn_readfirstlane(q.past), __builtin_amdgcn_readfirstlane(q.row0),
                __builtin_amdgcn_readfirstlane(q.n)};
-    kend = keys(b, sq);
-    tiles = tiles_of(kend);
+    qt = 0;
+    unit(b);
   }
   // To the unit behind the current one (pos < end: there is one).
   __device__ __forceinline__ void next(const KvBatch& b, int32_t kv) {
     unit0 += tiles;
-    if (++h < kv) return;
+    if (R != 0 && ++qt < row_tiles(sq, group)) return unit(b);
+    if (++h < kv) {
+      qt = 0;
+      return unit(b);
+    }
     h = 0;
     do {
       ++seq;
       take(b);
-    } while (tiles == 0);
+    } while (sq.n == 0);
   }
   __device__ __forceinline__ int32_t holder(int64_t x) const { return (int32_t)kv_div((x + 1) * P - 1, total); }
 };
@@ -981,8 +1028,8 @@ __global__ __launch_bounds__(256, HD * NB >= 256 ? 1 : 2) void kv_few_kernel(KvC
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j16 = lane & 15, quad = lane >> 4;
-  KvWalk<KT> run;
-  const bool any = run.start(b, c.kv, wk.P, lane);
+  KvWalk<KT, 0> run;
+  const bool any = run.start(b, c.kv, wk.group, wk.P, lane);
   const int32_t p = run.p;
   if (tid < 2) wk.desc[2 * p + tid].wb = -1;
   if (!any) return;
@@ -1215,7 +1262,7 @@ __global__ __launch_bounds__(256, HD * NB >= 256 ? 1 : 2) void kv_few_kernel(KvC
     const bool whole = ta == 0 && tb == run.tiles;
     const int slot = ta > 0 ? 0 : 1;
     if (!whole && tid == 0) {
-      KvDesc d{run.seq, run.h, run.holder(run.unit0), run.holder(run.unit0 + run.tiles - 1)};
+      KvDesc d{run.seq, run.h, 0, run.holder(run.unit0), run.holder(run.unit0 + run.tiles - 1)};
       wk.desc[2 * p + slot] = d;
     }
 #pragma unroll
@@ -1277,6 +1324,290 @@ __global__ __launch_bounds__(256, HD * NB >= 256 ? 1 : 2) void kv_few_kernel(KvC
   }
 }
 
+// ---- many query rows ----
+// W wavefronts of 16 NB rows each share tiles of 64 keys in LDS: the next tile's rows
+// are loaded to registers a whole tile ahead and written to the other buffer as the
+// current one is multiplied, one barrier a tile. LDS rows as in attn16_fwd_kernel
+// (16-byte chunks permuted), and its products. Values of places that nobody sees are written
+// as zeros; where a masked tile holds a value that is not finite its key's bit is set,
+// and its products take that key out and add it to the rows that see it.
+template <int HD, int NB, int W>
+__global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b, KvAttn a, KvWork wk) {
+  constexpr int R = 16 * NB * W, KT = 64, THREADS = 64 * W;
+  constexpr int NC = HD / 32, NT = HD / 16, CPR = HD / 8;
+  constexpr int NL = KT * CPR / THREADS;  // 16-byte loads of a thread for a tile of keys, and of values
+  constexpr int RPL = THREADS / CPR;      // rows of one
+  static_assert(NL * THREADS == KT * CPR && (64 / CPR <= 16 || CPR == 4), "a wavefront's load lies in 16 rows");
+  __shared__ __attribute__((aligned(1024))) uint16_t kt[2][KT * HD], vt[2][KT * HD];
+  __shared__ KvTree tree;
+  __shared__ uint32_t odds[3][2];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int j16 = lane & 15, quad = lane >> 4;
+  const int32_t G = wk.group;
+  KvWalk<KT, R> run;
+  const bool any = run.start(b, c.kv, G, wk.P, lane);
+  const int32_t p = run.p;
+  if (tid < 2) wk.desc[2 * p + tid].wb = -1;
+  if (!any) return;
+
+  const int lrow = tid / CPR, lchunk = tid % CPR;
+  const int kswz = attn_swz<HD>(j16);
+  const int vrow = 4 * quad + (j16 >> 2), vswz = attn_swz<HD>(vrow);
+
+  while (true) {
+    const KvSeq sq = run.sq;
+    const int64_t all = (int64_t)sq.n * G;
+    const int32_t r0 = run.qt * R, M = (int32_t)min(all - r0, (int64_t)R);  // the unit's rows r0 .. r0 + M - 1
+    const int32_t kend = run.kend;
+    const int32_t ta = (int32_t)(run.pos - run.unit0);
+    const int32_t tb = (int32_t)min((int64_t)run.tiles, run.end - run.unit0);
+    const int32_t* const pages = b.pages + (int64_t)run.seq * b.max_pages;
+    const int32_t jfirst = r0 / G;
+    if (b.parents && tb * KT > sq.past) kv_tree<THREADS>(tree, b, sq, jfirst, min(R, 128));
+    if (tid < 6) odds[tid >> 1][tid & 1] = 0;
+
+    const int32_t rw = wave * 16 * NB;  // the wavefront's first row of the tile
+    const bool active = rw < M;
+    const int32_t jw = (r0 + rw) / G;   // and its place behind the cached rows, the lowest of its rows'
+    bf16x8 qf[NC][NB];
+    int32_t jr[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int32_t r = min(rw + nb * 16 + j16, M - 1) + r0;
+      jr[nb] = r / G;
+      const uint16_t* const qr = a.q + (int64_t)(sq.row0 + jr[nb]) * a.ldq + ((int64_t)run.h * G + r - jr[nb] * G) * HD + quad * 8;
+#pragma unroll
+      for (int k = 0; k < NC; ++k) qf[k][nb] = *reinterpret_cast<const bf16x8*>(qr + k * 32);
+    }
+    f32x4 o[NT][NB];
+    float m_run[NB], l_run[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      m_run[nb] = -INFINITY;
+      l_run[nb] = 0.f;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) o[t][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    uint4 kr[NL], vr[NL];
+    auto load = [&](int32_t i) __attribute__((always_inline)) {
+#pragma unroll
+      for (int k = 0; k < NL; ++k) {
+        const int32_t t = (ta + i) * KT + ((k * RPL + wave * (64 / CPR)) & ~15);  // 16 keys of one page
+        const int32_t g = __builtin_amdgcn_readfirstlane(t < kend ? kv_page(b, c, pages, t) : -1);
+        const int64_t at = g >= 0 ? kv_at(c, g, run.h, t) : 0;
+        const int32_t off = ((k * RPL + lrow) & 15) * HD + lchunk * 8;
+        kr[k] = *reinterpret_cast<const uint4*>(c.k + at + off);
+        vr[k] = *reinterpret_cast<const uint4*>(c.v + at + off);
+        if (g < 0 || (ta + i) * KT + k * RPL + lrow >= kend) vr[k] = make_uint4(0, 0, 0, 0);
+      }
+    };
+    auto store = [&](int32_t i) __attribute__((always_inline)) {
+      const int st = i & 1;
+#pragma unroll
+      for (int k = 0; k < NL; ++k) {
+        const int row = k * RPL + lrow;
+        const int at = row * HD + ((lchunk ^ attn_swz<HD>(row & 15)) * 8);
+        *reinterpret_cast<uint4*>(&kt[st][at]) = kr[k];
+        *reinterpret_cast<uint4*>(&vt[st][at]) = vr[k];
+      }
+      if ((ta + i + 1) * KT > sq.past) {  // rows of the tile that some query rows may not see
+        if (tid < 2) odds[(i + 1) % 3][tid] = 0;  // (read a tile ago, set a tile later)
+#pragma unroll
+        for (int k = 0; k < NL; ++k) {
+          const uint4 v = vr[k];
+          const uint32_t x = v.x & 0x7fff7fffu, y = v.y & 0x7fff7fffu, z = v.z & 0x7fff7fffu, w = v.w & 0x7fff7fffu;
+          const int row = k * RPL + lrow;
+          if ((((x + 0x00800080u) | (y + 0x00800080u) | (z + 0x00800080u) | (w + 0x00800080u)) & 0x80008000u) != 0)
+            atomicOr(&odds[i % 3][row >> 5], 1u << (row & 31));
+        }
+      }
+    };
+    const int32_t steps = tb - ta;
+    load(0);
+    __syncthreads();  // odds are zero
+    store(0);
+    if (steps > 1) load(1);
+    __syncthreads();
+    for (int32_t i = 0; i < steps; ++i) {
+      if (i + 1 < steps) store(i + 1);
+      if (i + 2 < steps) load(i + 2);
+      const int32_t t = (ta + i) * KT;
+      const bool mask = t + KT > sq.past;
+      // (a chain's rows before all keys of the tile have nothing to do)
+      if (active && (b.whole || b.parents || t <= sq.past + (r0 + min(rw + 16 * NB, M) - 1) / G)) {
+        const uint16_t* const Ks = kt[i & 1];
+        const uint16_t* const Vs = vt[i & 1];
+        f32x4 s[4][NB];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) s[e][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bf16x8 kf = *reinterpret_cast<const bf16x8*>(Ks + (e * 16 + j16) * HD + (((4 * n + quad) ^ kswz) * 8));
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+              s[e][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][nb], s[e][nb], 0, 0, 0);
+          }
+        uint64_t odd = 0;
+        uint32_t page = 0xfu;  // 16-key blocks that are in a page
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (t + 16 * e >= kend || kv_page(b, c, pages, t + 16 * e) < 0) page &= ~(1u << e);
+        page = __builtin_amdgcn_readfirstlane(page);
+        if (mask || page != 0xfu || t + KT > kend) {
+          if (mask) odd = odds[i % 3][0] | (uint64_t)odds[i % 3][1] << 32;
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            uint64_t bits = ~0ull;  // of keys t .. t + 63
+            auto below = [](int32_t x) { return x >= 64 ? ~0ull : x <= 0 ? 0ull : (1ull << x) - 1; };
+            if (mask && b.parents) {
+              const uint64_t* const w = tree.seen[jr[nb] - jfirst];
+              bits = below(sq.past - t) | kv_seen(w, t - sq.past) | (uint64_t)kv_seen(w, t + 32 - sq.past) << 32;
+            } else if (mask && !b.whole) {
+              bits = below(sq.past + jr[nb] + 1 - t);
+            }
+            bits &= below(kend - t);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                if (!((page >> e) & 1) || !((bits >> (e * 16 + quad * 4 + k)) & 1)) s[e][nb][k] = -INFINITY;
+          }
+          odd = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(odd >> 32)) << 32 |
+                (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)odd);
+        }
+        bf16x8 pf[2][NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) top = fmaxf(top, s[e][nb][k]);
+          top = max_xor32(max_xor16(top)) * a.scale_log2;
+          if (__any(top > m_run[nb] + kRescale)) {
+            const float m_new = fmaxf(m_run[nb], top);
+            const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[nb] - m_new);
+            l_run[nb] *= alpha;
+            m_run[nb] = m_new;
+#pragma unroll
+            for (int t2 = 0; t2 < NT; ++t2) o[t2][nb] *= alpha;
+          }
+          const float m = m_run[nb] == -INFINITY ? 0.f : m_run[nb];  // (a row that has seen nothing yet)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float x = __builtin_amdgcn_exp2f(fmaf(s[e][nb][k], a.scale_log2, -m));
+              l_run[nb] += x;
+              pf[e >> 1][nb][4 * (e & 1) + k] = (__bf16)x;
+            }
+        }
+        auto read_v = [&](int t2, int x) __attribute__((always_inline)) {
+          const int col = t2 * 16 + 4 * (j16 & 3), r = x * 32 + vrow;
+          const int at = (((col >> 3) ^ vswz) * 8) + (col & 7);
+          const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+              (__attribute__((address_space(3))) bf16x4*)(Vs + r * HD + at));
+          const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+              (__attribute__((address_space(3))) bf16x4*)(Vs + (r + 16) * HD + at));
+          return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        if (odd == 0) {
+#pragma unroll
+          for (int t2 = 0; t2 < NT; ++t2)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const bf16x8 vf = read_v(t2, x);
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb)
+                o[t2][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[x][nb], o[t2][nb], 0, 0, 0);
+            }
+        } else {
+          // bit 8 x + k of `mine`: the lane's element k of chunk x (key 32 x + 16 (k / 4) + 4
+          // quad + k % 4) is such a value
+          uint32_t mine = 0;
+#pragma unroll
+          for (int k = 0; k < 16; ++k)
+            mine |= (uint32_t)((odd >> ((k >> 3) * 32 + ((k >> 2) & 1) * 16 + quad * 4 + (k & 3))) & 1) << k;
+#pragma unroll
+          for (int t2 = 0; t2 < NT; ++t2)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const bf16x8 raw = read_v(t2, x);
+              bf16x8 vf = raw;
+#pragma unroll
+              for (int k = 0; k < 8; ++k) vf[k] = (mine >> (8 * x + k)) & 1 ? (__bf16)0.f : raw[k];
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb)
+                o[t2][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[x][nb], o[t2][nb], 0, 0, 0);
+#pragma unroll 1
+              for (int q = 0; q < 4; ++q)
+#pragma unroll 1
+                for (int k = 0; k < 8; ++k) {
+                  if (!((odd >> (x * 32 + (k >> 2) * 16 + q * 4 + (k & 3))) & 1)) continue;
+                  const int slot = quad == q ? k : -1;
+                  bf16x8 only;
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) only[e] = e == slot ? raw[e] : (__bf16)0.f;
+#pragma unroll
+                  for (int nb = 0; nb < NB; ++nb) {
+                    bool y = false;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y |= e == slot && (float)pf[x][nb][e] != 0.f;
+                    const bool sees = (__ballot(y) >> (q * 16 + j16)) & 1;
+                    const f32x4 v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(only, pf[x][nb], o[t2][nb], 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[t2][nb][e] = sees ? v[e] : o[t2][nb][e];
+                  }
+                }
+            }
+        }
+      }
+      __syncthreads();  // the tile is read, the next one written
+    }
+
+    const bool whole = ta == 0 && tb == run.tiles;
+    const int slot = ta > 0 ? 0 : 1;
+    if (!whole && tid == 0) {
+      KvDesc d{run.seq, run.h, run.qt, run.holder(run.unit0), run.holder(run.unit0 + run.tiles - 1)};
+      wk.desc[2 * p + slot] = d;
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const float l = sum_xor32(sum_xor16(l_run[nb]));
+      const int32_t r = rw + nb * 16 + j16;
+      if (whole) {
+        // 16 bytes a lane after a lane swap, as in attn16_fwd_kernel
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        uint16_t* const to = a.out + (int64_t)(sq.row0 + jr[nb]) * a.ldo +
+                             ((int64_t)run.h * G + r0 + r - jr[nb] * G) * HD + 16 * (quad & 1) + 8 * (quad >> 1);
+#pragma unroll
+        for (int t = 0; t < NT; t += 2) {
+          const auto x = __builtin_amdgcn_permlane16_swap(pack_bf2(o[t][nb][0] * inv, o[t][nb][1] * inv),
+                                                          pack_bf2(o[t + 1][nb][0] * inv, o[t + 1][nb][1] * inv), false, false);
+          const auto y = __builtin_amdgcn_permlane16_swap(pack_bf2(o[t][nb][2] * inv, o[t][nb][3] * inv),
+                                                          pack_bf2(o[t + 1][nb][2] * inv, o[t + 1][nb][3] * inv), false, false);
+          if (r < M) *reinterpret_cast<uint4*>(to + t * 16) = make_uint4(x[0], y[0], x[1], y[1]);
+        }
+      } else if (r < M) {
+        const int64_t at = (int64_t)(2 * p + slot) * R + r;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+          *reinterpret_cast<f32x4*>(wk.o + at * HD + t * 16 + quad * 4) = o[t][nb];
+        if (quad == 0) wk.ml[at] = make_float2(m_run[nb], l);
+      }
+    }
+    run.pos = run.unit0 + tb;
+    if (run.pos >= run.end) break;
+    run.next(b, c.kv);
+  }
+}
+
 // Partial results of units that several workgroups hold: workgroup p adds rows p - wa,
 // p - wa + parts, ... of the units of its two slots, so that all that took part in a
 // unit share its rows. `rows`: of a slot.
@@ -1291,7 +1622,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvBatch b, KvAttn a, KvWor
     const KvDesc d = wk.desc[2 * p + slot];
     if (d.wb < 0) continue;
     const KvSeq sq = kv_seq(b, d.seq);
-    const int32_t parts = d.wb - d.wa + 1, M = min(sq.n * G, rows);
+    const int32_t parts = d.wb - d.wa + 1, M = (int32_t)min((int64_t)sq.n * G - (int64_t)d.qt * rows, (int64_t)rows);
     auto part = [&](int32_t k) { return (int64_t)(2 * (d.wa + k) + (k == 0 ? 1 : 0)) * rows; };
     for (int32_t r = p - d.wa; r < M; r += parts) {
       float top = -INFINITY;
@@ -1328,8 +1659,8 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvBatch b, KvAttn a, KvWor
           l += sl[k];
         }
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        const int32_t j = r / G;
-        *reinterpret_cast<uint2*>(a.out + (int64_t)(sq.row0 + j) * a.ldo + ((int64_t)d.h * G + r - j * G) * HD + 4 * ln) =
+        const int32_t rr = d.qt * rows + r, j = rr / G;
+        *reinterpret_cast<uint2*>(a.out + (int64_t)(sq.row0 + j) * a.ldo + ((int64_t)d.h * G + rr - j * G) * HD + 4 * ln) =
             make_uint2(pack_bf2(v.x * inv, v.y * inv), pack_bf2(v.z * inv, v.w * inv));
       }
       __syncthreads();
@@ -1337,63 +1668,10 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvBatch b, KvAttn a, KvWor
   }
 }
 
-// One wavefront per new row and query head: 64 keys a step, a key a lane for the
-// scores, then a head-dim column (or four) a lane for the sum of the values seen.
-__global__ __launch_bounds__(64) void kv_attn_plain_kernel(KvCache c, KvBatch b, KvAttn a) {
-  __shared__ float qs[256], ps[64];
-  __shared__ int64_t at[64];
-  const int lane = threadIdx.x;
-  const int32_t row = blockIdx.x / a.heads, h = blockIdx.x - row * a.heads, kvh = h / (a.heads / c.kv);
-  const int32_t seq = kv_find(b, row, lane);
-  if (seq >= b.n_seqs) return;
-  const KvSeq sq = kv_seq(b, seq);
-  const int32_t j = row - sq.row0;
-  if (j < 0 || j >= sq.n) return;
-  const int32_t* const pages = b.pages + (int64_t)seq * b.max_pages;
-  for (int e = lane; e < c.hd; e += 64) qs[e] = bf2f(a.q[row * a.ldq + (int64_t)h * c.hd + e]);
-  uint64_t sees[4] = {0, 0, 0, 0};  // a tree's row: itself and its ancestors
-  if (b.parents)
-    for (int32_t k = j; k >= 0; k = kv_parent(b.parents + sq.row0, k)) sees[k >> 6] |= 1ull << (k & 63);
-  const int32_t end = sq.past + (b.whole ? sq.n : j + 1);
-  float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  __syncthreads();
-  for (int32_t t0 = 0; t0 < end; t0 += 64) {
-    const int32_t t = t0 + lane, k = t - sq.past;
-    bool on = t < end;
-    if (on && b.parents && k >= 0) on = (sees[k >> 6] >> (k & 63)) & 1;
-    const int32_t page = on ? kv_page(b, c, pages, t) : -1;
-    on = page >= 0;
-    float s = -INFINITY;
-    if (on) {
-      at[lane] = kv_at(c, page, kvh, t);
-      float z = 0.f;
-      for (int e = 0; e < c.hd; ++e) z = fmaf(qs[e], bf2f(c.k[at[lane] + e]), z);
-      s = z * a.scale_log2;
-    }
-    const float m2 = fmaxf(m, wave_max(s)), alpha = m2 == -INFINITY ? 1.f : exp2f(m - m2);
-    m = m2;
-    const float p = s == -INFINITY ? 0.f : exp2f(s - m);
-    l = l * alpha + wave_sum(p);
-    ps[lane] = on ? bf2f(f2bf(p)) : -1.f;
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      o[e] *= alpha;
-      const int col = lane + 64 * e;
-      if (col < c.hd)
-        for (int i = 0; i < 64; ++i)
-          if (ps[i] >= 0.f) o[e] = fmaf(ps[i], bf2f(c.v[at[i] + col]), o[e]);
-    }
-    __syncthreads();
-  }
-  for (int e = 0; e < 4; ++e)
-    if (lane + 64 * e < c.hd)
-      a.out[row * a.ldo + (int64_t)h * c.hd + lane + 64 * e] = f2bf(l == 0.f ? 0.f : o[e] / l);
-}
-
 // Query rows of a unit's tile, and workgroups: as many as are resident together, and no
 // more than the batch can have tiles.
 struct KvPlan {
+  bool many;
   int32_t rows, P;
   size_t desc, ml, total;
 };
@@ -1401,9 +1679,11 @@ static KvPlan kv_plan(const KvCache& c, const KvBatch& b, int32_t heads) {
   const int32_t G = heads / c.kv;
   const int64_t M = (int64_t)std::min(b.max_new, b.rows) * G;
   KvPlan k{};
-  if (M > (c.hd == 256 ? 32 : 64)) return k;
-  k.rows = M <= 16 ? 16 : M <= 32 ? 32 : 64;
-  const int64_t tiles = (int64_t)b.n_seqs * c.kv * ((b.places + 127) / 128);
+  k.many = M > (c.hd == 256 ? 32 : 64);
+  k.rows = k.many ? 128 : M <= 16 ? 16 : M <= 32 ? 32 : 64;
+  const int32_t keys = k.many ? 64 : 128;
+  const int64_t units = (int64_t)b.n_seqs * c.kv * ((M + k.rows - 1) / k.rows);
+  const int64_t tiles = std::min<int64_t>(units * ((b.places + keys - 1) / keys), 1 << 20);
   const int64_t P = 256 * (c.hd == 256 ? 1 : 2);
   k.P = (int32_t)std::min((tiles + 7) / 8 * 8, P);
   k.desc = ((size_t)k.P * 2 * sizeof(KvDesc) + 255) / 256 * 256;
@@ -1416,10 +1696,6 @@ size_t kv_attention_bytes(const KvCache& c, const KvBatch& b, int32_t heads) { r
 
 hipError_t launch_kv_attention(hipStream_t s, const KvCache& c, const KvBatch& b, const KvAttn& a, void* ws) {
   const KvPlan k = kv_plan(c, b, a.heads);
-  if (k.P == 0) {
-    kv_attn_plain_kernel<<<(unsigned)((int64_t)b.rows * a.heads), 64, 0, s>>>(c, b, a);
-    return hipGetLastError();
-  }
   KvWork w{};
   w.desc = (KvDesc*)ws;
   w.ml = (float2*)((char*)ws + k.desc);
@@ -1432,6 +1708,12 @@ hipError_t launch_kv_attention(hipStream_t s, const KvCache& c, const KvBatch& b
     return hipGetLastError();
   };
   auto rows = [&](auto hd) {
+    if (k.many) {
+      constexpr int HD = decltype(hd)::value, NB = HD == 256 ? 1 : 2, W = HD == 256 ? 8 : 4;
+      kv_many_kernel<HD, NB, W><<<k.P, 64 * W, 0, s>>>(c, b, a, w);
+      kv_join_kernel<HD><<<k.P, 256, 0, s>>>(b, a, w, 128);
+      return hipGetLastError();
+    }
     if (k.rows == 16) return go(hd, std::integral_constant<int, 1>());
     if (k.rows == 32) return go(hd, std::integral_constant<int, 2>());
     if constexpr (decltype(hd)::value < 256)
