@@ -7,12 +7,18 @@
 
 namespace jnx {
 
+// The caller's tables are not written while a kernel reads them, so that what a whole
+// wavefront reads of them alike comes by the scalar cache.
+typedef const __attribute__((address_space(4))) int32_t* KvTable;
+__device__ __forceinline__ KvTable kv_table(const int32_t* p) { return (KvTable)(uintptr_t)p; }
+
 struct KvSeq {
   int32_t past, row0, n;  // cached rows, first new row of the call, new rows
 };
 __device__ __forceinline__ KvSeq kv_seq(const KvBatch& b, int32_t s) {
-  const int32_t row0 = min(max(b.cu[s], 0), b.rows), end = min(b.cu[s + 1], b.rows);
-  return KvSeq{min(max(b.past[s], 0), b.places), row0, min(max(end - row0, 0), b.max_new)};
+  const KvTable cu = kv_table(b.cu) + s;
+  const int32_t row0 = min(max(cu[0], 0), b.rows), end = min(cu[1], b.rows);
+  return KvSeq{min(max(kv_table(b.past)[s], 0), b.places), row0, min(max(end - row0, 0), b.max_new)};
 }
 
 // Sequence of a call's row by all lanes of a wavefront (n_seqs: the row is in none):

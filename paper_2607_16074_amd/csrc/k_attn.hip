@@ -965,6 +965,14 @@ __device__ __forceinline__ void kv_read_v(const uint32_t* at, uint32_t off, bf16
   }
 }
 
+// x, as a value that the compiler knows nothing of: what is made of it is made where it
+// is used and not kept in registers through the loops around (the masks' bits, the
+// ends of units: 60 registers of the loops below).
+__device__ __forceinline__ int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 __device__ __forceinline__ uint32_t kv_lds(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
@@ -1001,6 +1009,55 @@ __device__ __forceinline__ uint32_t kv_seen(const uint64_t* w, int32_t k) {
   return (uint32_t)v;
 }
 
+// Values that are not finite in rows that only some query rows see: 0 * inf is NaN, so
+// the products take them as zeros, and here they are added to the query rows that see
+// them, whose probability p of the key is not zero. Keys t0 .. t1 - 1, a key after the
+// other: such values are rare, and the products' loop stays free of them.
+template <int HD, int NB, typename See>
+__device__ __forceinline__ void kv_add_odd(const KvBatch& b, const KvCache& c, KvTable pages, int32_t h, int32_t t0,
+                                           int32_t t1, const bf16x8 (&qf)[HD / 32][NB], const float (&m)[NB], float scale,
+                                           f32x4 (&o)[HD / 16][NB], int lane, See&& sees) {
+  const int quad = lane >> 4;
+#pragma unroll 1
+  for (int32_t t = t0; t < t1; ++t) {
+    const int32_t g = pages[t >> c.page_log2];
+    if ((uint32_t)g >= (uint32_t)c.n_pages) continue;
+    const int64_t at = kv_at(c, g, h, t);
+    bool bad = false;
+    for (int e = lane; e < HD; e += 64) bad |= (c.v[at + e] & 0x7f80) == 0x7f80;
+    if (!__any(bad)) continue;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      float z = 0.f;
+#pragma unroll
+      for (int n = 0; n < HD / 32; ++n)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z = fmaf((float)qf[n][nb][e], bf2f(c.k[at + n * 32 + quad * 8 + e]), z);
+      z = sum_xor32(sum_xor16(z));
+      const float p = sees(nb, t) ? __builtin_amdgcn_exp2f(fmaf(z, scale, -m[nb])) : 0.f;
+#pragma unroll
+      for (int x = 0; x < HD / 16; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint16_t v = c.v[at + x * 16 + quad * 4 + e];
+          if ((v & 0x7f80) == 0x7f80 && p != 0.f) o[x][nb][e] = fmaf(p, bf2f(v), o[x][nb][e]);
+        }
+    }
+  }
+}
+// v with zeros for its elements that are not finite, and whether there are any.
+__device__ __forceinline__ bool kv_finite(uint4& v) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w}, any = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t odd = ((w[k] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;  // (no carry: 0x7fff + 0x80 < 2^16)
+    any |= odd;
+    w[k] &= ~((odd >> 15) * 0xffffu);
+  }
+  v = make_uint4(w[0], w[1], w[2], w[3]);
+  return any != 0;
+}
+
 // ---- few query rows (a unit has at most 16 NB) ----
 // The time is the reading of keys and values, each read once: four wavefronts, each
 // with 32 keys of a 128-key tile and all query rows. Keys go from the cache to
@@ -1012,10 +1069,9 @@ __device__ __forceinline__ uint32_t kv_seen(const uint64_t* w, int32_t k) {
 //   S^T = K Q^T, O^T += V^T P^T as in attn16_fwd_kernel.
 // A key's page is the same for the 16 keys of a fragment (pages are multiples of 16),
 // so page numbers are read once for all lanes. Values of places that no row sees are set to zero
-// in LDS (0 * NaN is NaN); a value that some rows of a tile see and others do not, and
-// that is not finite, is taken out of the product and added where it is seen.
+// in LDS (0 * NaN is NaN).
 template <int HD, int NB>
-__global__ __launch_bounds__(256, HD * NB >= 256 ? 1 : 2) void kv_few_kernel(KvCache c, KvBatch b, KvAttn a, KvWork wk) {
+__global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void kv_few_kernel(KvCache c, KvBatch b, KvAttn a, KvWork wk) {
   constexpr int R = 16 * NB, KT = 128;
   constexpr int NC = HD / 32, NT = HD / 16, CPR = HD / 8, RPI = 512 / HD;
   constexpr int NV = 32 / RPI, NK = 2 * NC;  // DMA instructions and key loads of a step
@@ -1056,7 +1112,7 @@ __global__ __launch_bounds__(256, HD * NB >= 256 ? 1 : 2) void kv_few_kernel(KvC
     const int32_t M = sq.n * G, kend = run.kend;
     const int32_t ta = (int32_t)(run.pos - run.unit0);
     const int32_t tb = (int32_t)min((int64_t)run.tiles, run.end - run.unit0);
-    const int32_t* const pages = b.pages + (int64_t)run.seq * b.max_pages;
+    const KvTable pages = kv_table(b.pages) + (int64_t)run.seq * b.max_pages;
     const bool masks = tb * KT > sq.past;
     if (b.parents && masks) kv_tree<256>(tree, b, sq, 0, R);
 
@@ -1080,17 +1136,21 @@ __global__ __launch_bounds__(256, HD * NB >= 256 ? 1 : 2) void kv_few_kernel(KvC
     }
 
     const int32_t steps = tb - ta;
-    // of a step: its keys' page numbers and their heads' offsets
+    // of a step: its keys' page numbers, read a step before they are needed, and their
+    // heads' offsets
     struct Pages {
       int32_t page[2];
       int64_t at[2];
     };
-    auto pages_of = [&](int32_t i) __attribute__((always_inline)) {
+    auto page_id = [&](int32_t i, int e) __attribute__((always_inline)) {
+      return pages[min(((ta + i) * KT + wave * 32 + 16 * e) >> c.page_log2, b.max_pages - 1)];
+    };
+    auto pages_of = [&](int32_t i, int32_t id0, int32_t id1) __attribute__((always_inline)) {
       Pages x;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int32_t t = (ta + i) * KT + wave * 32 + 16 * e;
-        x.page[e] = __builtin_amdgcn_readfirstlane(t < kend ? kv_page(b, c, pages, t) : -1);
+        const int32_t t = (ta + i) * KT + wave * 32 + 16 * e, id = e ? id1 : id0;
+        x.page[e] = t < kend && (uint32_t)id < (uint32_t)c.n_pages ? id : -1;
         x.at[e] = x.page[e] >= 0 ? kv_at(c, x.page[e], run.h, t) : 0;
       }
       return x;
@@ -1110,7 +1170,9 @@ __global__ __launch_bounds__(256, HD * NB >= 256 ? 1 : 2) void kv_few_kernel(KvC
 #pragma unroll
         for (int n = 0; n < NC; ++n) kf[e][n] = *reinterpret_cast<const bf16x8*>(c.k + x.at[e] + koff + n * 32);
     };
-    Pages use = pages_of(0), next = use;
+    Pages use = pages_of(0, page_id(0, 0), page_id(0, 1)), next = use;
+    int32_t id0 = page_id(1, 0), id1 = page_id(1, 1);
+    bool odd = false;
     fetch_v(use, 0);
     fetch_k(use);
     for (int32_t i = 0; i < steps; ++i) {
@@ -1118,7 +1180,9 @@ __global__ __launch_bounds__(256, HD * NB >= 256 ? 1 : 2) void kv_few_kernel(KvC
       const bool more = i + 1 < steps;
       const uint32_t stage = (i & 1) * (32 * HD * 2);
       if (more) {
-        next = pages_of(i + 1);
+        next = pages_of(i + 1, id0, id1);
+        id0 = page_id(i + 2, 0);
+        id1 = page_id(i + 2, 1);
         fetch_v(next, (i + 1) & 1);
       }
       f32x4 s[2][NB];
@@ -1139,9 +1203,10 @@ __global__ __launch_bounds__(256, HD * NB >= 256 ? 1 : 2) void kv_few_kernel(KvC
       const bool hole = use.page[0] < 0 || use.page[1] < 0 || t + 32 > kend;  // places that no row sees
       const bool mask = t + 32 > sq.past;                                   // or not every row
       if (hole || mask) {
+        const int l = here(lane), q4 = (l >> 4) * 4;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          const int32_t j = (nb * 16 + j16) / G;
+          const int32_t j = (nb * 16 + (l & 15)) / G;
           uint32_t bits = 0xffffffffu;  // of keys t .. t + 31
           if (mask && !b.whole) {
             const int32_t seen = sq.past + j + 1 - t;  // a chain's row sees keys below this
@@ -1156,7 +1221,7 @@ __global__ __launch_bounds__(256, HD * NB >= 256 ? 1 : 2) void kv_few_kernel(KvC
           for (int e = 0; e < 2; ++e)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const int32_t x = e * 16 + quad * 4 + k;
+              const int32_t x = e * 16 + q4 + k;
               if (use.page[e] < 0 || t + x >= kend || !((bits >> x) & 1)) s[e][nb][k] = -INFINITY;
             }
         }
@@ -1193,56 +1258,19 @@ __global__ __launch_bounds__(256, HD * NB >= 256 ? 1 : 2) void kv_few_kernel(KvC
       else
         kv_wait_vmcnt<0>();
       if (hole || mask) {
-        // rows of the tile that nobody sees become zeros, others that are not finite too
-        // once the rows that see them have them: a lane holds one query row of a product, so
-        // what a product with this key alone gives is taken where its probability is not zero
-        const int32_t r = lane >> 1;
+        // rows of the tile that nobody sees become zeros, and values that are not finite
+        const int l = here(lane);
+        const int32_t r = l >> 1;
         const bool none = (r < 16 ? use.page[0] : use.page[1]) < 0 || t + r >= kend;
+        uint16_t* const row = &vt[wave][i & 1][r * HD + (l & 1) * (HD / 2)];
         bool bad = false;
-        uint16_t* const row = &vt[wave][i & 1][r * HD + (lane & 1) * (HD / 2)];
 #pragma unroll 1
         for (int e = 0; e < HD / 2; e += 8) {
-          const uint4 v = *reinterpret_cast<const uint4*>(row + e);
-          const uint32_t x = v.x & 0x7fff7fffu, y = v.y & 0x7fff7fffu, z = v.z & 0x7fff7fffu, w = v.w & 0x7fff7fffu;
-          bad |= (((x + 0x00800080u) | (y + 0x00800080u) | (z + 0x00800080u) | (w + 0x00800080u)) & 0x80008000u) != 0;
+          uint4 v = *reinterpret_cast<const uint4*>(row + e);
+          bad |= kv_finite(v);
+          *reinterpret_cast<uint4*>(row + e) = none ? make_uint4(0, 0, 0, 0) : v;
         }
-        uint64_t odd = __ballot(!none && bad);
-        const bool zero = none || ((odd >> (lane & ~1)) & 3) != 0;
-#pragma unroll 1
-        while (odd != 0) {
-          const int k = __builtin_ctzll(odd) >> 1;
-          odd &= ~(3ull << (2 * k));
-          // key k is element 4 (k / 16) + k % 4 of quad (k / 4) % 4
-          const int slot = quad == ((k >> 2) & 3) ? 4 * (k >> 4) + (k & 3) : -1;
-          bool sees[NB];
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            bool x = false;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x |= e == slot && (float)pf[nb][e] != 0.f;
-            sees[nb] = (__ballot(x) >> (((k >> 2) & 3) * 16 + j16)) & 1;
-          }
-#pragma unroll
-          for (int t0 = 0; t0 < NT; t0 += TG) {
-            bf16x8 vf[TG];
-            kv_read_v<HD>(vat + t0, stage, vf);
-#pragma unroll
-            for (int x = 0; x < TG; ++x) {
-              bf16x8 only;
-#pragma unroll
-              for (int e = 0; e < 8; ++e) only[e] = e == slot ? vf[x][e] : (__bf16)0.f;
-#pragma unroll
-              for (int nb = 0; nb < NB; ++nb) {
-                const f32x4 v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(only, pf[nb], o[t0 + x][nb], 0, 0, 0);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[t0 + x][nb][e] = sees[nb] ? v[e] : o[t0 + x][nb][e];
-              }
-            }
-          }
-        }
-        if (zero)
-#pragma unroll 1
-          for (int e = 0; e < HD / 2; e += 8) *reinterpret_cast<uint4*>(row + e) = make_uint4(0, 0, 0, 0);
+        odd |= __any(bad && !none);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       }
 #pragma unroll
@@ -1257,8 +1285,18 @@ __global__ __launch_bounds__(256, HD * NB >= 256 ? 1 : 2) void kv_few_kernel(KvC
       }
       use = next;
     }
+    if (odd)
+      for (int32_t i = max(0, (sq.past - 31 - wave * 32) / KT - ta); i < steps; ++i) {
+        const int32_t t = (ta + i) * KT + wave * 32;
+        kv_add_odd<HD, NB>(b, c, pages, run.h, t, min(t + 32, kend), qf, m_run, a.scale_log2, o, here(lane), [&](int nb, int32_t x) {
+          const int32_t j = (nb * 16 + (here(lane) & 15)) / G, k = x - sq.past;
+          if (k < 0 || b.whole) return true;
+          return b.parents ? (kv_seen(tree.seen[min(j, sq.n - 1)], k) & 1) != 0 : k <= j;
+        });
+      }
 
     // the wavefronts' results, added
+    const int el = here(lane), ej = el & 15, eq = el >> 4, et = wave * 64 + el;
     const bool whole = ta == 0 && tb == run.tiles;
     const int slot = ta > 0 ? 0 : 1;
     if (!whole && tid == 0) {
@@ -1268,9 +1306,9 @@ __global__ __launch_bounds__(256, HD * NB >= 256 ? 1 : 2) void kv_few_kernel(KvC
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       const float l = sum_xor32(sum_xor16(l_run[nb]));
-      if (quad == 0) {
-        sm[wave][nb * 16 + j16] = m_run[nb];
-        sl[wave][nb * 16 + j16] = l;
+      if (eq == 0) {
+        sm[wave][nb * 16 + ej] = m_run[nb];
+        sl[wave][nb * 16 + ej] = l;
       }
     }
     float* const sums = reinterpret_cast<float*>(&vt[0][0][0]);
@@ -1278,14 +1316,14 @@ __global__ __launch_bounds__(256, HD * NB >= 256 ? 1 : 2) void kv_few_kernel(KvC
     for (int nb = 0; nb < NB; ++nb) {
       if (nb * 16 >= M) break;
       __syncthreads();  // m and l are there; the tiles, or the last rows' sums, are read
-      const int r = nb * 16 + j16;
+      const int r = nb * 16 + ej;
       const float top = fmaxf(fmaxf(sm[0][r], sm[1][r]), fmaxf(sm[2][r], sm[3][r]));
       const float f = m_run[nb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[nb] - top);
 #pragma unroll
       for (int t = 0; t < NT; ++t)
-        *reinterpret_cast<f32x4*>(&sums[(wave * 16 + j16) * LD + t * 16 + quad * 4]) = o[t][nb] * f;
+        *reinterpret_cast<f32x4*>(&sums[(wave * 16 + ej) * LD + t * 16 + eq * 4]) = o[t][nb] * f;
       __syncthreads();
-      for (int i = tid; i < 16 * CPR; i += 256) {
+      for (int i = et; i < 16 * CPR; i += 256) {
         const int row = i / CPR, col = (i % CPR) * 8, rr = nb * 16 + row;
         if (rr >= M) break;
         float v[8];
@@ -1329,8 +1367,7 @@ __global__ __launch_bounds__(256, HD * NB >= 256 ? 1 : 2) void kv_few_kernel(KvC
 // are loaded to registers a whole tile ahead and written to the other buffer as the
 // current one is multiplied, one barrier a tile. LDS rows as in attn16_fwd_kernel
 // (16-byte chunks permuted), and its products. Values of places that nobody sees are written
-// as zeros; where a masked tile holds a value that is not finite its key's bit is set,
-// and its products take that key out and add it to the rows that see it.
+// as zeros, as are those of masked tiles that are not finite (kv_add_odd).
 template <int HD, int NB, int W>
 __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b, KvAttn a, KvWork wk) {
   constexpr int R = 16 * NB * W, KT = 64, THREADS = 64 * W;
@@ -1340,7 +1377,6 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
   static_assert(NL * THREADS == KT * CPR && (64 / CPR <= 16 || CPR == 4), "a wavefront's load lies in 16 rows");
   __shared__ __attribute__((aligned(1024))) uint16_t kt[2][KT * HD], vt[2][KT * HD];
   __shared__ KvTree tree;
-  __shared__ uint32_t odds[3][2];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j16 = lane & 15, quad = lane >> 4;
@@ -1362,10 +1398,9 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
     const int32_t kend = run.kend;
     const int32_t ta = (int32_t)(run.pos - run.unit0);
     const int32_t tb = (int32_t)min((int64_t)run.tiles, run.end - run.unit0);
-    const int32_t* const pages = b.pages + (int64_t)run.seq * b.max_pages;
+    const KvTable pages = kv_table(b.pages) + (int64_t)run.seq * b.max_pages;
     const int32_t jfirst = r0 / G;
     if (b.parents && tb * KT > sq.past) kv_tree<THREADS>(tree, b, sq, jfirst, min(R, 128));
-    if (tid < 6) odds[tid >> 1][tid & 1] = 0;
 
     const int32_t rw = wave * 16 * NB;  // the wavefront's first row of the tile
     const bool active = rw < M;
@@ -1391,20 +1426,57 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
     }
 
     uint4 kr[NL], vr[NL];
+    // of a tile: its four 16-key blocks' page numbers, read a tile before they are needed,
+    // and as bits which blocks have one
+    int32_t id[4];
+    auto ids = [&](int32_t i) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) id[e] = pages[min(((ta + i) * KT + 16 * e) >> c.page_log2, b.max_pages - 1)];
+    };
+    uint32_t on[3] = {0, 0, 0};  // of the current tile and the next two
+    bool odd = false;
     auto load = [&](int32_t i) __attribute__((always_inline)) {
+      on[0] = on[1];
+      on[1] = on[2];
+      on[2] = 0;
+      int64_t at[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int32_t t = (ta + i) * KT + 16 * e;
+        const bool ok = t < kend && (uint32_t)id[e] < (uint32_t)c.n_pages;
+        on[2] |= (uint32_t)ok << e;
+        at[e] = ok ? kv_at(c, id[e], run.h, t) : 0;
+      }
 #pragma unroll
       for (int k = 0; k < NL; ++k) {
-        const int32_t t = (ta + i) * KT + ((k * RPL + wave * (64 / CPR)) & ~15);  // 16 keys of one page
-        const int32_t g = __builtin_amdgcn_readfirstlane(t < kend ? kv_page(b, c, pages, t) : -1);
-        const int64_t at = g >= 0 ? kv_at(c, g, run.h, t) : 0;
+        int e = (k * RPL) >> 4;  // the wavefront's block of this load
+        int64_t from = at[e & 3];
+        if constexpr (RPL > 16) {
+          const int w = wave * (64 / CPR) >> 4;
+#pragma unroll
+          for (int x = 1; x < RPL / 16; ++x) from = w == x ? at[(e + x) & 3] : from;
+          e += w;
+        }
         const int32_t off = ((k * RPL + lrow) & 15) * HD + lchunk * 8;
-        kr[k] = *reinterpret_cast<const uint4*>(c.k + at + off);
-        vr[k] = *reinterpret_cast<const uint4*>(c.v + at + off);
-        if (g < 0 || (ta + i) * KT + k * RPL + lrow >= kend) vr[k] = make_uint4(0, 0, 0, 0);
+        kr[k] = *reinterpret_cast<const uint4*>(c.k + from + off);
+        vr[k] = *reinterpret_cast<const uint4*>(c.v + from + off);
       }
     };
-    auto store = [&](int32_t i) __attribute__((always_inline)) {
+    // tile i, whose blocks `on` says, from the registers to its buffer
+    auto store = [&](int32_t i, uint32_t has) __attribute__((always_inline)) {
       const int st = i & 1;
+      const int32_t t = (ta + i) * KT;
+      const bool edge = has != 0xfu || t + KT > kend, mask = t + KT > sq.past;
+      if (edge || mask) {
+#pragma unroll
+        for (int k = 0; k < NL; ++k) {
+          const int row = k * RPL + lrow;
+          const bool none = !((has >> (row >> 4)) & 1) || t + row >= kend;
+          const bool bad = kv_finite(vr[k]);
+          odd |= bad && !none;
+          if (none) vr[k] = make_uint4(0, 0, 0, 0);
+        }
+      }
 #pragma unroll
       for (int k = 0; k < NL; ++k) {
         const int row = k * RPL + lrow;
@@ -1412,27 +1484,27 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
         *reinterpret_cast<uint4*>(&kt[st][at]) = kr[k];
         *reinterpret_cast<uint4*>(&vt[st][at]) = vr[k];
       }
-      if ((ta + i + 1) * KT > sq.past) {  // rows of the tile that some query rows may not see
-        if (tid < 2) odds[(i + 1) % 3][tid] = 0;  // (read a tile ago, set a tile later)
-#pragma unroll
-        for (int k = 0; k < NL; ++k) {
-          const uint4 v = vr[k];
-          const uint32_t x = v.x & 0x7fff7fffu, y = v.y & 0x7fff7fffu, z = v.z & 0x7fff7fffu, w = v.w & 0x7fff7fffu;
-          const int row = k * RPL + lrow;
-          if ((((x + 0x00800080u) | (y + 0x00800080u) | (z + 0x00800080u) | (w + 0x00800080u)) & 0x80008000u) != 0)
-            atomicOr(&odds[i % 3][row >> 5], 1u << (row & 31));
-        }
-      }
     };
     const int32_t steps = tb - ta;
+    ids(0);
     load(0);
-    __syncthreads();  // odds are zero
-    store(0);
-    if (steps > 1) load(1);
+    ids(1);
+    store(0, on[2]);
+    if (steps > 1) {
+      load(1);
+      ids(2);
+    } else {
+      on[1] = on[2];
+    }
     __syncthreads();
+    // on[1], on[2]: of tiles i and i + 1 at the top of step i
     for (int32_t i = 0; i < steps; ++i) {
-      if (i + 1 < steps) store(i + 1);
-      if (i + 2 < steps) load(i + 2);
+      const uint32_t has = i + 1 < steps ? on[1] : (steps > 1 ? on[2] : on[1]);
+      if (i + 1 < steps) store(i + 1, on[2]);
+      if (i + 2 < steps) {
+        load(i + 2);
+        ids(i + 3);
+      }
       const int32_t t = (ta + i) * KT;
       const bool mask = t + KT > sq.past;
       // (a chain's rows before all keys of the tile have nothing to do)
@@ -1453,14 +1525,8 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
             for (int nb = 0; nb < NB; ++nb)
               s[e][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][nb], s[e][nb], 0, 0, 0);
           }
-        uint64_t odd = 0;
-        uint32_t page = 0xfu;  // 16-key blocks that are in a page
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (t + 16 * e >= kend || kv_page(b, c, pages, t + 16 * e) < 0) page &= ~(1u << e);
-        page = __builtin_amdgcn_readfirstlane(page);
-        if (mask || page != 0xfu || t + KT > kend) {
-          if (mask) odd = odds[i % 3][0] | (uint64_t)odds[i % 3][1] << 32;
+        if (mask || has != 0xfu || t + KT > kend) {
+          const int q4 = (here(lane) >> 4) * 4;
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) {
             uint64_t bits = ~0ull;  // of keys t .. t + 63
@@ -1476,10 +1542,8 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
             for (int e = 0; e < 4; ++e)
 #pragma unroll
               for (int k = 0; k < 4; ++k)
-                if (!((page >> e) & 1) || !((bits >> (e * 16 + quad * 4 + k)) & 1)) s[e][nb][k] = -INFINITY;
+                if (!((has >> e) & 1) || !((bits >> (e * 16 + q4 + k)) & 1)) s[e][nb][k] = -INFINITY;
           }
-          odd = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(odd >> 32)) << 32 |
-                (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)odd);
         }
         bf16x8 pf[2][NB];
 #pragma unroll
@@ -1517,62 +1581,29 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
               (__attribute__((address_space(3))) bf16x4*)(Vs + (r + 16) * HD + at));
           return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         };
-        if (odd == 0) {
 #pragma unroll
-          for (int t2 = 0; t2 < NT; ++t2)
+        for (int t2 = 0; t2 < NT; ++t2)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const bf16x8 vf = read_v(t2, x);
+          for (int x = 0; x < 2; ++x) {
+            const bf16x8 vf = read_v(t2, x);
 #pragma unroll
-              for (int nb = 0; nb < NB; ++nb)
-                o[t2][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[x][nb], o[t2][nb], 0, 0, 0);
-            }
-        } else {
-          // bit 8 x + k of `mine`: the lane's element k of chunk x (key 32 x + 16 (k / 4) + 4
-          // quad + k % 4) is such a value
-          uint32_t mine = 0;
-#pragma unroll
-          for (int k = 0; k < 16; ++k)
-            mine |= (uint32_t)((odd >> ((k >> 3) * 32 + ((k >> 2) & 1) * 16 + quad * 4 + (k & 3))) & 1) << k;
-#pragma unroll
-          for (int t2 = 0; t2 < NT; ++t2)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const bf16x8 raw = read_v(t2, x);
-              bf16x8 vf = raw;
-#pragma unroll
-              for (int k = 0; k < 8; ++k) vf[k] = (mine >> (8 * x + k)) & 1 ? (__bf16)0.f : raw[k];
-#pragma unroll
-              for (int nb = 0; nb < NB; ++nb)
-                o[t2][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[x][nb], o[t2][nb], 0, 0, 0);
-#pragma unroll 1
-              for (int q = 0; q < 4; ++q)
-#pragma unroll 1
-                for (int k = 0; k < 8; ++k) {
-                  if (!((odd >> (x * 32 + (k >> 2) * 16 + q * 4 + (k & 3))) & 1)) continue;
-                  const int slot = quad == q ? k : -1;
-                  bf16x8 only;
-#pragma unroll
-                  for (int e = 0; e < 8; ++e) only[e] = e == slot ? raw[e] : (__bf16)0.f;
-#pragma unroll
-                  for (int nb = 0; nb < NB; ++nb) {
-                    bool y = false;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) y |= e == slot && (float)pf[x][nb][e] != 0.f;
-                    const bool sees = (__ballot(y) >> (q * 16 + j16)) & 1;
-                    const f32x4 v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(only, pf[x][nb], o[t2][nb], 0, 0, 0);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[t2][nb][e] = sees ? v[e] : o[t2][nb][e];
-                  }
-                }
-            }
-        }
+            for (int nb = 0; nb < NB; ++nb)
+              o[t2][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[x][nb], o[t2][nb], 0, 0, 0);
+          }
       }
       __syncthreads();  // the tile is read, the next one written
     }
+    if (__syncthreads_or(odd) && active)
+      kv_add_odd<HD, NB>(b, c, pages, run.h, max(ta * KT, sq.past / KT * KT), min(tb * KT, kend), qf, m_run, a.scale_log2, o,
+                         here(lane), [&](int nb, int32_t x) {
+                           const int32_t k = x - sq.past;
+                           if (k < 0 || b.whole) return true;
+                           return b.parents ? (kv_seen(tree.seen[jr[nb] - jfirst], k) & 1) != 0 : k <= jr[nb];
+                         });
 
     const bool whole = ta == 0 && tb == run.tiles;
     const int slot = ta > 0 ? 0 : 1;
+    const int el = here(lane), ej = el & 15, eq = el >> 4;
     if (!whole && tid == 0) {
       KvDesc d{run.seq, run.h, run.qt, run.holder(run.unit0), run.holder(run.unit0 + run.tiles - 1)};
       wk.desc[2 * p + slot] = d;
@@ -1580,12 +1611,12 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       const float l = sum_xor32(sum_xor16(l_run[nb]));
-      const int32_t r = rw + nb * 16 + j16;
+      const int32_t r = rw + nb * 16 + ej;
       if (whole) {
         // 16 bytes a lane after a lane swap, as in attn16_fwd_kernel
         const float inv = l == 0.f ? 0.f : 1.f / l;
         uint16_t* const to = a.out + (int64_t)(sq.row0 + jr[nb]) * a.ldo +
-                             ((int64_t)run.h * G + r0 + r - jr[nb] * G) * HD + 16 * (quad & 1) + 8 * (quad >> 1);
+                             ((int64_t)run.h * G + r0 + r - jr[nb] * G) * HD + 16 * (eq & 1) + 8 * (eq >> 1);
 #pragma unroll
         for (int t = 0; t < NT; t += 2) {
           const auto x = __builtin_amdgcn_permlane16_swap(pack_bf2(o[t][nb][0] * inv, o[t][nb][1] * inv),
@@ -1598,8 +1629,8 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
         const int64_t at = (int64_t)(2 * p + slot) * R + r;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
-          *reinterpret_cast<f32x4*>(wk.o + at * HD + t * 16 + quad * 4) = o[t][nb];
-        if (quad == 0) wk.ml[at] = make_float2(m_run[nb], l);
+          *reinterpret_cast<f32x4*>(wk.o + at * HD + t * 16 + eq * 4) = o[t][nb];
+        if (eq == 0) wk.ml[at] = make_float2(m_run[nb], l);
       }
     }
     run.pos = run.unit0 + tb;
@@ -1608,29 +1639,25 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
   }
 }
 
-// Partial results of units that several workgroups hold: workgroup p adds rows p - wa,
-// p - wa + parts, ... of the units of its two slots, so that all that took part in a
-// unit share its rows. `rows`: of a slot.
+// Partial results of units that several workgroups hold: the wavefronts of workgroup
+// p add rows of the units of its two slots, which all that took part in a unit share. A
+// wavefront takes a row: HD / 4 lanes, and what lanes are left share the parts. `rows`: of a slot.
 template <int HD>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvBatch b, KvAttn a, KvWork wk, int32_t rows) {
-  constexpr int LN = HD / 4, GR = 256 / LN;  // lanes of a row, groups that share the parts
-  __shared__ float4 so[GR][LN];
-  __shared__ float sl[GR], tops[4];
-  const int tid = threadIdx.x, ln = tid % LN, gr = tid / LN;
-  const int32_t p = blockIdx.x, G = wk.group;
+  constexpr int LN = HD / 4, GR = 64 / LN;  // lanes of a row, groups that share the parts
+  const int lane = threadIdx.x & 63, ln = lane % LN, gr = lane / LN;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int32_t p = blockIdx.x, G = wk.group, first = blockIdx.y * 4 + wave, share = gridDim.y * 4;
   for (int slot = 0; slot < 2; ++slot) {
     const KvDesc d = wk.desc[2 * p + slot];
     if (d.wb < 0) continue;
     const KvSeq sq = kv_seq(b, d.seq);
     const int32_t parts = d.wb - d.wa + 1, M = (int32_t)min((int64_t)sq.n * G - (int64_t)d.qt * rows, (int64_t)rows);
     auto part = [&](int32_t k) { return (int64_t)(2 * (d.wa + k) + (k == 0 ? 1 : 0)) * rows; };
-    for (int32_t r = p - d.wa; r < M; r += parts) {
+    for (int32_t r = (p - d.wa) * share + first; r < M; r += parts * share) {
       float top = -INFINITY;
-      for (int32_t k = tid; k < parts; k += 256) top = fmaxf(top, wk.ml[part(k) + r].x);
+      for (int32_t k = lane; k < parts; k += 64) top = fmaxf(top, wk.ml[part(k) + r].x);
       top = wave_max(top);
-      if ((tid & 63) == 0) tops[tid >> 6] = top;
-      __syncthreads();
-      top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       float l = 0.f;
 #pragma unroll 4
@@ -1645,25 +1672,20 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvBatch b, KvAttn a, KvWor
         v.z = fmaf(f, x.z, v.z);
         v.w = fmaf(f, x.w, v.w);
       }
-      so[gr][ln] = v;
-      if (ln == 0) sl[gr] = l;
-      __syncthreads();
-      if (gr == 0) {
 #pragma unroll
-        for (int k = 1; k < GR; ++k) {
-          const float4 x = so[k][ln];
-          v.x += x.x;
-          v.y += x.y;
-          v.z += x.z;
-          v.w += x.w;
-          l += sl[k];
-        }
+      for (int e = LN; e < 64; e <<= 1) {
+        v.x += __shfl_xor(v.x, e, kWave);
+        v.y += __shfl_xor(v.y, e, kWave);
+        v.z += __shfl_xor(v.z, e, kWave);
+        v.w += __shfl_xor(v.w, e, kWave);
+        l += __shfl_xor(l, e, kWave);
+      }
+      if (gr == 0) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const int32_t rr = d.qt * rows + r, j = rr / G;
         *reinterpret_cast<uint2*>(a.out + (int64_t)(sq.row0 + j) * a.ldo + ((int64_t)d.h * G + rr - j * G) * HD + 4 * ln) =
             make_uint2(pack_bf2(v.x * inv, v.y * inv), pack_bf2(v.z * inv, v.w * inv));
       }
-      __syncthreads();
     }
   }
 }
@@ -1679,8 +1701,8 @@ static KvPlan kv_plan(const KvCache& c, const KvBatch& b, int32_t heads) {
   const int32_t G = heads / c.kv;
   const int64_t M = (int64_t)std::min(b.max_new, b.rows) * G;
   KvPlan k{};
-  k.many = M > (c.hd == 256 ? 32 : 64);
-  k.rows = k.many ? 128 : M <= 16 ? 16 : M <= 32 ? 32 : 64;
+  k.many = M > (c.hd == 256 ? 16 : 32);
+  k.rows = M <= 16 ? 16 : M <= 32 && !k.many ? 32 : M <= 64 ? 64 : 128;
   const int32_t keys = k.many ? 64 : 128;
   const int64_t units = (int64_t)b.n_seqs * c.kv * ((M + k.rows - 1) / k.rows);
   const int64_t tiles = std::min<int64_t>(units * ((b.places + keys - 1) / keys), 1 << 20);
@@ -1702,23 +1724,19 @@ hipError_t launch_kv_attention(hipStream_t s, const KvCache& c, const KvBatch& b
   w.o = (float*)((char*)ws + k.desc + k.ml);
   w.P = k.P;
   w.group = a.heads / c.kv;
-  auto go = [&](auto hd, auto nb) {
-    kv_few_kernel<hd(), nb()><<<k.P, 256, 0, s>>>(c, b, a, w);
-    kv_join_kernel<hd()><<<k.P, 256, 0, s>>>(b, a, w, 16 * nb());
-    return hipGetLastError();
-  };
   auto rows = [&](auto hd) {
-    if (k.many) {
-      constexpr int HD = decltype(hd)::value, NB = HD == 256 ? 1 : 2, W = HD == 256 ? 8 : 4;
+    constexpr int HD = decltype(hd)::value, NB = HD == 256 ? 1 : 2, W = HD == 256 ? 8 : 4;
+    static_assert(16 * NB * W == 128, "rows of the largest tile");
+    if (k.rows == 128)
       kv_many_kernel<HD, NB, W><<<k.P, 64 * W, 0, s>>>(c, b, a, w);
-      kv_join_kernel<HD><<<k.P, 256, 0, s>>>(b, a, w, 128);
-      return hipGetLastError();
-    }
-    if (k.rows == 16) return go(hd, std::integral_constant<int, 1>());
-    if (k.rows == 32) return go(hd, std::integral_constant<int, 2>());
-    if constexpr (decltype(hd)::value < 256)
-      if (k.rows == 64) return go(hd, std::integral_constant<int, 4>());
-    return hipErrorInvalidValue;
+    else if (k.many)
+      kv_many_kernel<HD, 1, 4><<<k.P, 256, 0, s>>>(c, b, a, w);
+    else if (k.rows == 16)
+      kv_few_kernel<HD, 1><<<k.P, 256, 0, s>>>(c, b, a, w);
+    else if constexpr (HD < 256)
+      kv_few_kernel<HD, 2><<<k.P, 256, 0, s>>>(c, b, a, w);
+    kv_join_kernel<HD><<<dim3(k.P, (k.rows + 31) / 32), 256, 0, s>>>(b, a, w, k.rows);
+    return hipGetLastError();
   };
   switch (c.hd) {
     case 32: return rows(std::integral_constant<int, 32>());
