@@ -793,6 +793,10 @@ __device__ __forceinline__ int64_t wave_get64(int64_t v, int l) {
   return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
+// The same value in all lanes, said so.
+__device__ __forceinline__ int32_t wave_same(int32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t wave_same64(int64_t v) { return wave_get64(v, 0); }
+
 // The run of tiles [pos, end) of a workgroup, walked unit by unit. KT keys a tile; R
 // query rows a tile of a unit (0: a unit has one tile of rows), a unit is then
 // (sequence, key head, row tile), and a chain's row tiles end at their last row's keys.
@@ -838,11 +842,12 @@ struct KvWalk {
     }
     int64_t scan = wave_scan64(all, lane);
     total = wave_get64(scan, 63) * kv;
+    total = wave_same64(total);
     p = total < most ? blockIdx.x : (blockIdx.x & 7) * (most >> 3) + (blockIdx.x >> 3);
     P = (int32_t)min(total, (int64_t)most);
     if (p >= P) return false;
-    pos = kv_div(total * p, P);
-    end = kv_div(total * (p + 1), P);
+    pos = wave_same64(kv_div(total * p, P));
+    end = wave_same64(kv_div(total * (p + 1), P));
     int64_t before = 0;
     seq = 0;
     for (int32_t s0 = 0;; s0 += 64) {
@@ -861,9 +866,9 @@ struct KvWalk {
     }
     take(b);
     int64_t rest = pos - before * kv;
-    h = (int32_t)kv_div(rest, mine);
+    h = wave_same((int32_t)kv_div(rest, mine));
     rest -= h * mine;
-    unit0 = pos - rest;
+    unit0 = wave_same64(pos - rest);
     qt = 0;
     if constexpr (R != 0) {
       const int32_t nq = row_tiles(sq, G);
@@ -872,7 +877,7 @@ struct KvWalk {
         const int64_t up = wave_scan64(t, lane);
         const int32_t c = __builtin_popcountll(__ballot(up <= rest));
         if (c < 64) {
-          qt = q0 + c;
+          qt = wave_same(q0 + c);
           unit0 += wave_get64(up - t, c);
           break;
         }
@@ -884,7 +889,7 @@ struct KvWalk {
     return true;
   }
   __device__ __forceinline__ void unit(const KvBatch& b) {
-    kend = keys(b, sq, group, qt);
+    kend = wave_same(keys(b, sq, group, qt));
     tiles = tiles_of(kend);
   }
   __device__ __forceinline__ void take(const KvBatch& b) {
@@ -1046,15 +1051,15 @@ __device__ __forceinline__ void kv_add_odd(const KvBatch& b, const KvCache& c, K
   }
 }
 // v with zeros for its elements that are not finite, and whether there are any.
-__device__ __forceinline__ bool kv_finite(uint4& v) {
-  uint32_t w[4] = {v.x, v.y, v.z, v.w}, any = 0;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ bool kv_finite(u32x4& v) {
+  uint32_t any = 0;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const uint32_t odd = ((w[k] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;  // (no carry: 0x7fff + 0x80 < 2^16)
+    const uint32_t odd = ((v[k] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;  // (no carry: 0x7fff + 0x80 < 2^16)
     any |= odd;
-    w[k] &= ~((odd >> 15) * 0xffffu);
+    v[k] &= ~((odd >> 15) * 0xffffu);
   }
-  v = make_uint4(w[0], w[1], w[2], w[3]);
   return any != 0;
 }
 
@@ -1110,9 +1115,9 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void kv_few_kernel(KvCache 
   while (true) {
     const KvSeq sq = run.sq;
     const int32_t M = sq.n * G, kend = run.kend;
-    const int32_t ta = (int32_t)(run.pos - run.unit0);
-    const int32_t tb = (int32_t)min((int64_t)run.tiles, run.end - run.unit0);
-    const KvTable pages = kv_table(b.pages) + (int64_t)run.seq * b.max_pages;
+    const int32_t ta = wave_same((int32_t)(run.pos - run.unit0));
+    const int32_t tb = wave_same((int32_t)min((int64_t)run.tiles, run.end - run.unit0));
+    const KvTable pages = kv_table(b.pages) + (int64_t)wave_same(run.seq) * b.max_pages;
     const bool masks = tb * KT > sq.past;
     if (b.parents && masks) kv_tree<256>(tree, b, sq, 0, R);
 
@@ -1266,9 +1271,9 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void kv_few_kernel(KvCache 
         bool bad = false;
 #pragma unroll 1
         for (int e = 0; e < HD / 2; e += 8) {
-          uint4 v = *reinterpret_cast<const uint4*>(row + e);
+          u32x4 v = *reinterpret_cast<const u32x4*>(row + e);
           bad |= kv_finite(v);
-          *reinterpret_cast<uint4*>(row + e) = none ? make_uint4(0, 0, 0, 0) : v;
+          *reinterpret_cast<u32x4*>(row + e) = none ? u32x4{0, 0, 0, 0} : v;
         }
         odd |= __any(bad && !none);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -1396,9 +1401,9 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
     const int64_t all = (int64_t)sq.n * G;
     const int32_t r0 = run.qt * R, M = (int32_t)min(all - r0, (int64_t)R);  // the unit's rows r0 .. r0 + M - 1
     const int32_t kend = run.kend;
-    const int32_t ta = (int32_t)(run.pos - run.unit0);
-    const int32_t tb = (int32_t)min((int64_t)run.tiles, run.end - run.unit0);
-    const KvTable pages = kv_table(b.pages) + (int64_t)run.seq * b.max_pages;
+    const int32_t ta = wave_same((int32_t)(run.pos - run.unit0));
+    const int32_t tb = wave_same((int32_t)min((int64_t)run.tiles, run.end - run.unit0));
+    const KvTable pages = kv_table(b.pages) + (int64_t)wave_same(run.seq) * b.max_pages;
     const int32_t jfirst = r0 / G;
     if (b.parents && tb * KT > sq.past) kv_tree<THREADS>(tree, b, sq, jfirst, min(R, 128));
 
@@ -1425,7 +1430,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
       for (int t = 0; t < NT; ++t) o[t][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    uint4 kr[NL], vr[NL];
+    u32x4 kr[NL], vr[NL];
     // of a tile: its four 16-key blocks' page numbers, read a tile before they are needed,
     // and as bits which blocks have one
     int32_t id[4];
@@ -1458,8 +1463,8 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
           e += w;
         }
         const int32_t off = ((k * RPL + lrow) & 15) * HD + lchunk * 8;
-        kr[k] = *reinterpret_cast<const uint4*>(c.k + from + off);
-        vr[k] = *reinterpret_cast<const uint4*>(c.v + from + off);
+        kr[k] = *reinterpret_cast<const u32x4*>(c.k + from + off);
+        vr[k] = *reinterpret_cast<const u32x4*>(c.v + from + off);
       }
     };
     // tile i, whose blocks `on` says, from the registers to its buffer
@@ -1474,15 +1479,15 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
           const bool none = !((has >> (row >> 4)) & 1) || t + row >= kend;
           const bool bad = kv_finite(vr[k]);
           odd |= bad && !none;
-          if (none) vr[k] = make_uint4(0, 0, 0, 0);
+          if (none) vr[k] = u32x4{0, 0, 0, 0};
         }
       }
 #pragma unroll
       for (int k = 0; k < NL; ++k) {
         const int row = k * RPL + lrow;
         const int at = row * HD + ((lchunk ^ attn_swz<HD>(row & 15)) * 8);
-        *reinterpret_cast<uint4*>(&kt[st][at]) = kr[k];
-        *reinterpret_cast<uint4*>(&vt[st][at]) = vr[k];
+        *reinterpret_cast<u32x4*>(&kt[st][at]) = kr[k];
+        *reinterpret_cast<u32x4*>(&vt[st][at]) = vr[k];
       }
     };
     const int32_t steps = tb - ta;
