@@ -660,7 +660,8 @@ jn_status jn_tenant_tokens_decode(jn_ctx* ctx, const void* hidden, int32_t T, in
  * node 0 alone draws a token from p.  Weights that are NaN or negative count as 0; children
  * whose token is outside [0, vocab) are passed over.  Products and sums are formed in 64 bits, in a fixed order. */
 typedef struct jn_token_verify {
-  int32_t n_trees, n;      /* n: nodes of all trees, with n * vocab < 2^40 (JN_ESHAPE) */
+  int32_t n_trees, n;      /* n: nodes of all trees, with n * vocab < 2^40; at most 65,536 trees of all
+                              tenants of a call (JN_ESHAPE) */
   int32_t vocab;           /* 1 .. 2^24 */
   int32_t max_path;        /* >= 1 */
   int64_t ld_p, ld_q;      /* elements between rows of p and q, >= vocab */

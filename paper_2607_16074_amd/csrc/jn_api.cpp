@@ -1960,57 +1960,89 @@ jn_status check_verify(jn_ctx* c, const jn_token_verify* v, int32_t G) {
                           (uintptr_t)t.n_path | (uintptr_t)t.next;
     if (all % 4 != 0) return fail(c, JN_EINVAL, "tenant %d: buffers not 4-byte aligned", g);
   }
-  if (trees > kMostBlocks / 16) return fail(c, JN_ESHAPE, "%lld trees in a call", (long long)trees);
+  if (trees > 1 << 16) return fail(c, JN_ESHAPE, "%lld trees in a call", (long long)trees);
   return JN_OK;
 }
 
 }  // namespace
 }
 
+// A launch's tenants: from v[g] on, behind which g stands then.
+extern "C++" {
+namespace {
+struct VerifyPlan {
+  TokVerifySet set;
+  int32_t phases;
+  int64_t nodes;
+  size_t bytes;
+};
+bool verify_plan(const jn_token_verify* v, int32_t G, int32_t* g, VerifyPlan* P) {
+  TokVerifySet& set = P->set;
+  set = TokVerifySet{};
+  P->nodes = 0;
+  P->phases = 0;
+  int32_t vocab = 1;
+  for (; *g < G && set.G < kVerifyTenants; ++*g) {
+    const jn_token_verify& t = v[*g];
+    if (t.n_trees == 0) continue;
+    P->nodes += t.n;
+    TokVerify& d = set.t[set.G++];
+    d.cu = t.cu_nodes;
+    d.parents = t.parents;
+    d.tokens = t.tokens;
+    d.p = t.p;
+    d.q = t.q;
+    d.greedy = t.greedy;
+    d.u = t.u;
+    d.r = t.r;
+    d.path = t.path;
+    d.n_path = t.n_path;
+    d.next = t.next;
+    d.ldp = t.ld_p;
+    d.ldq = t.ld_q;
+    d.n = t.n;
+    d.vocab = t.vocab;
+    d.max_path = t.max_path;
+    d.tree0 = set.trees;
+    set.trees += t.n_trees;
+    if (!t.p) continue;
+    vocab = std::max(vocab, t.vocab);
+    // a chain has one sum, a tree of drawn drafts one more for every rejection but a node's last
+    const bool more = t.q && t.parents && t.vocab >= kVerifyLongRow && t.n > 2ll * t.n_trees;
+    P->phases = std::max(P->phases, more ? 3 : 1);
+  }
+  if (set.trees == 0) return false;
+  const int32_t most = (vocab + 1023) / 1024;
+  set.chunks = std::min({std::max(1, (kVerifyGroups + set.trees - 1) / set.trees), most, kVerifyChunks});
+  P->bytes = (size_t)P->phases * set.trees * set.chunks * sizeof(double);
+  return true;
+}
+}  // namespace
+}
+
 jn_status jn_tokens_verify_workspace_size(const jn_token_verify* v, int32_t G, size_t* bytes) {
   if (!bytes) return JN_EINVAL;
   const jn_status st = check_verify(nullptr, v, G);
-  if (st == JN_OK) *bytes = 0;
-  return st;
+  if (st != JN_OK) return st;
+  VerifyPlan P;
+  *bytes = 0;
+  for (int32_t g = 0; verify_plan(v, G, &g, &P);) *bytes = std::max(*bytes, P.bytes);
+  return JN_OK;
 }
 
 jn_status jn_tenant_tokens_verify(jn_ctx* c, const jn_token_verify* v, int32_t G, void* ws, size_t ws_bytes) {
   if (!c) return JN_EINVAL;
   jn_status st = check_verify(c, v, G);
   if (st != JN_OK) return st;
-  (void)ws;
-  (void)ws_bytes;
+  size_t need = 0;
+  jn_tokens_verify_workspace_size(v, G, &need);
+  if (need > 0 && (!ws || ws_bytes < need)) return fail(c, JN_ENOSPACE, "workspace %zu B < %zu B", ws ? ws_bytes : 0, need);
+  if (need > 0 && (uintptr_t)ws % 16 != 0) return fail(c, JN_EUNSUPPORTED, "workspace not 16-byte aligned");
   if ((st = check_device(c)) != JN_OK) return st;
-  for (int32_t g = 0; g < G;) {
-    TokVerifySet set{};
-    int64_t nodes = 0;
-    for (; g < G && set.G < kVerifyTenants; ++g) {
-      const jn_token_verify& t = v[g];
-      if (t.n_trees == 0) continue;
-      nodes += t.n;
-      TokVerify& d = set.t[set.G++];
-      d.cu = t.cu_nodes;
-      d.parents = t.parents;
-      d.tokens = t.tokens;
-      d.p = t.p;
-      d.q = t.q;
-      d.greedy = t.greedy;
-      d.u = t.u;
-      d.r = t.r;
-      d.path = t.path;
-      d.n_path = t.n_path;
-      d.next = t.next;
-      d.ldp = t.ld_p;
-      d.ldq = t.ld_q;
-      d.n = t.n;
-      d.vocab = t.vocab;
-      d.max_path = t.max_path;
-      d.tree0 = set.trees;
-      set.trees += t.n_trees;
-    }
-    if (set.trees == 0) break;
-    JN_TRACED(c, JN_OP_TOKEN_VERIFY, nodes, set.t[0].vocab, 0, launch_tok_verify(c->stream, set), "verification of drafts");
-  }
+  VerifyPlan P;
+  for (int32_t g = 0; verify_plan(v, G, &g, &P);)
+    JN_TRACED(c, JN_OP_TOKEN_VERIFY, P.nodes, P.set.t[0].vocab, 0,
+              launch_tok_verify(c->stream, P.set, P.phases, (double*)ws), "verification of drafts");
   return JN_OK;
 }
 

@@ -559,12 +559,16 @@ struct TokVerify {
   int32_t n, vocab, max_path, tree0;
 };
 constexpr int32_t kVerifyTenants = 24;  // of one launch
+constexpr int32_t kVerifyChunks = 256;  // most pieces of a row
+constexpr int32_t kVerifyGroups = 512;  // workgroups of a launch over pieces, about
+constexpr int32_t kVerifyLongRow = 1 << 16;
 struct TokVerifySet {
   TokVerify t[kVerifyTenants];
-  int32_t G, trees;
+  int32_t G, trees, chunks;
 };
 static_assert(sizeof(TokVerifySet) <= 3400, "kernel arguments");
-hipError_t launch_tok_verify(hipStream_t s, const TokVerifySet& set);
+// part: [phases][trees][chunks]
+hipError_t launch_tok_verify(hipStream_t s, const TokVerifySet& set, int32_t phases, double* part);
 
 // ------------------------------------------------------------ optimizer ---
 

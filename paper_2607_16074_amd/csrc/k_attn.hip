@@ -764,12 +764,14 @@ hipError_t launch_rope(hipStream_t s, void* qkv, int32_t ld, const int32_t* toke
 struct KvDesc {                // of a slot of a workgroup: its part of a unit
   int32_t seq, h, qt, wa, wb;  // held by workgroups wa .. wb; wb < 0: nothing
 };
+constexpr int32_t kKvJoinMany = 16;
 struct KvWork {
   KvDesc* desc;          // [P][2]
   float2* ml;            // [P][2][rows]
   float* o;              // [P][2][rows][HD]
   int32_t P;             // workgroups, a multiple of 8
   int32_t group;         // query heads of a key head
+  int32_t least;         // tiles of a workgroup, where there are so many
 };
 
 // x * P / total and the like for x, P <= total * 1024: in 32 bits where it fits.
@@ -819,10 +821,9 @@ struct KvWalk {
     return min(q.past + n, b.places);
   }
   static __device__ __forceinline__ int32_t tiles_of(int32_t keys) { return (keys + KT - 1) / KT; }
-  // Tiles of a key head of sequence s.
-  static __device__ __forceinline__ int64_t of_seq(const KvBatch& b, int32_t G, int32_t s) {
+  // Tiles of a key head of sequence s, which is q.
+  static __device__ __forceinline__ int64_t of_seq(const KvBatch& b, const KvSeq& q, int32_t G, int32_t s) {
     if (s >= b.n_seqs) return 0;
-    const KvSeq q = kv_seq(b, s);
     const int32_t nq = row_tiles(q, G);
     if (nq == 0) return 0;
     if (R == 0 || b.whole || b.parents) return (int64_t)nq * tiles_of(keys(b, q, G, 0));
@@ -831,20 +832,23 @@ struct KvWalk {
     return sum;
   }
 
-  // Runs that follow each other go to one XCD, whose workgroups are every eighth; with
-  // fewer tiles than workgroups a tile each, so that no run between two others is empty.
-  __device__ __forceinline__ bool start(const KvBatch& b, int32_t kv, int32_t G, int32_t most, int lane) {
+  // At most `most` workgroups, of `least` tiles each where there are so many. Runs that
+  // follow each other go to one XCD, whose workgroups are every eighth.
+  __device__ __forceinline__ bool start(const KvBatch& b, int32_t kv, int32_t G, int32_t most, int32_t least, int lane) {
     group = G;
     int64_t all = 0, mine = 0;
+    KvSeq q{};
     for (int32_t s0 = 0; s0 < b.n_seqs; s0 += 64) {
-      mine = of_seq(b, G, s0 + lane);
+      if (s0 + lane < b.n_seqs) q = kv_seq(b, s0 + lane);
+      mine = of_seq(b, q, G, s0 + lane);
       all += mine;
     }
     int64_t scan = wave_scan64(all, lane);
     total = wave_get64(scan, 63) * kv;
     total = wave_same64(total);
-    p = total < most ? blockIdx.x : (blockIdx.x & 7) * (most >> 3) + (blockIdx.x >> 3);
-    P = (int32_t)min(total, (int64_t)most);
+    const bool all_run = total >= (int64_t)most * least;
+    p = all_run ? (blockIdx.x & 7) * (most >> 3) + (blockIdx.x >> 3) : blockIdx.x;
+    P = all_run ? most : (int32_t)((total + least - 1) / least);
     if (p >= P) return false;
     pos = wave_same64(kv_div(total * p, P));
     end = wave_same64(kv_div(total * (p + 1), P));
@@ -852,7 +856,8 @@ struct KvWalk {
     seq = 0;
     for (int32_t s0 = 0;; s0 += 64) {
       if (b.n_seqs > 64) {
-        mine = of_seq(b, G, s0 + lane);
+        if (s0 + lane < b.n_seqs) q = kv_seq(b, s0 + lane);
+        mine = of_seq(b, q, G, s0 + lane);
         scan = wave_scan64(mine, lane);
       }
       const int32_t c = __builtin_popcountll(__ballot((before + scan) * kv <= pos));
@@ -860,16 +865,18 @@ struct KvWalk {
         seq = s0 + c;
         before += wave_get64(scan - mine, c);
         mine = wave_get64(mine, c);
+        sq = KvSeq{__builtin_amdgcn_readlane(q.past, c), __builtin_amdgcn_readlane(q.row0, c),
+                   __builtin_amdgcn_readlane(q.n, c)};
         break;
       }
       before += wave_get64(scan, 63);
     }
-    take(b);
+    qt = 0;
+    unit(b);
     int64_t rest = pos - before * kv;
     h = wave_same((int32_t)kv_div(rest, mine));
     rest -= h * mine;
     unit0 = wave_same64(pos - rest);
-    qt = 0;
     if constexpr (R != 0) {
       const int32_t nq = row_tiles(sq, G);
       for (int32_t q0 = 0;; q0 += 64) {
@@ -1090,7 +1097,7 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void kv_few_kernel(KvCache 
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j16 = lane & 15, quad = lane >> 4;
   KvWalk<KT, 0> run;
-  const bool any = run.start(b, c.kv, wk.group, wk.P, lane);
+  const bool any = run.start(b, c.kv, wk.group, wk.P, wk.least, lane);
   const int32_t p = run.p;
   if (tid < 2) wk.desc[2 * p + tid].wb = -1;
   if (!any) return;
@@ -1387,7 +1394,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
   const int j16 = lane & 15, quad = lane >> 4;
   const int32_t G = wk.group;
   KvWalk<KT, R> run;
-  const bool any = run.start(b, c.kv, G, wk.P, lane);
+  const bool any = run.start(b, c.kv, G, wk.P, wk.least, lane);
   const int32_t p = run.p;
   if (tid < 2) wk.desc[2 * p + tid].wb = -1;
   if (!any) return;
@@ -1405,21 +1412,21 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
     const int32_t tb = wave_same((int32_t)min((int64_t)run.tiles, run.end - run.unit0));
     const KvTable pages = kv_table(b.pages) + (int64_t)wave_same(run.seq) * b.max_pages;
     const int32_t jfirst = r0 / G;
-    if (b.parents && tb * KT > sq.past) kv_tree<THREADS>(tree, b, sq, jfirst, min(R, 128));
-
     const int32_t rw = wave * 16 * NB;  // the wavefront's first row of the tile
     const bool active = rw < M;
     const int32_t jw = (r0 + rw) / G;   // and its place behind the cached rows, the lowest of its rows'
     bf16x8 qf[NC][NB];
     int32_t jr[NB];
+    auto load_q = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      const int32_t r = min(rw + nb * 16 + j16, M - 1) + r0;
-      jr[nb] = r / G;
-      const uint16_t* const qr = a.q + (int64_t)(sq.row0 + jr[nb]) * a.ldq + ((int64_t)run.h * G + r - jr[nb] * G) * HD + quad * 8;
+      for (int nb = 0; nb < NB; ++nb) {
+        const int32_t r = min(rw + nb * 16 + j16, M - 1) + r0;
+        jr[nb] = r / G;
+        const uint16_t* const qr = a.q + (int64_t)(sq.row0 + jr[nb]) * a.ldq + ((int64_t)run.h * G + r - jr[nb] * G) * HD + quad * 8;
 #pragma unroll
-      for (int k = 0; k < NC; ++k) qf[k][nb] = *reinterpret_cast<const bf16x8*>(qr + k * 32);
-    }
+        for (int k = 0; k < NC; ++k) qf[k][nb] = *reinterpret_cast<const bf16x8*>(qr + k * 32);
+      }
+    };
     f32x4 o[NT][NB];
     float m_run[NB], l_run[NB];
 #pragma unroll
@@ -1494,6 +1501,8 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
     ids(0);
     load(0);
     ids(1);
+    load_q();  // (under the first tile's loads, as the tree's bits)
+    if (b.parents && tb * KT > sq.past) kv_tree<THREADS>(tree, b, sq, jfirst, min(R, 128));
     store(0, on[2]);
     if (steps > 1) {
       load(1);
@@ -1644,20 +1653,25 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
   }
 }
 
-// Partial results of units that several workgroups hold: the wavefronts of workgroup
-// p add rows of the units of its two slots, which all that took part in a unit share. A
-// wavefront takes a row: HD / 4 lanes, and what lanes are left share the parts. `rows`: of a slot.
+// Partial results of units that several workgroups hold: workgroup p adds rows of the
+// units of its two slots, which all that took part in a unit share. A row is a
+// wavefront's (HD / 4 lanes, and what lanes are left share the parts), of units in many parts the
+// whole workgroup's. `rows`: of a slot.
 template <int HD>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvBatch b, KvAttn a, KvWork wk, int32_t rows) {
   constexpr int LN = HD / 4, GR = 64 / LN;  // lanes of a row, groups that share the parts
+  __shared__ float4 so[4][LN];
+  __shared__ float sl[4];
   const int lane = threadIdx.x & 63, ln = lane % LN, gr = lane / LN;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int32_t p = blockIdx.x, G = wk.group, first = blockIdx.y * 4 + wave, share = gridDim.y * 4;
+  const int32_t p = blockIdx.x, G = wk.group;
   for (int slot = 0; slot < 2; ++slot) {
     const KvDesc d = wk.desc[2 * p + slot];
     if (d.wb < 0) continue;
     const KvSeq sq = kv_seq(b, d.seq);
     const int32_t parts = d.wb - d.wa + 1, M = (int32_t)min((int64_t)sq.n * G - (int64_t)d.qt * rows, (int64_t)rows);
+    const bool all = parts >= kKvJoinMany;  // four wavefronts a row
+    const int32_t share = gridDim.y * (all ? 1 : 4), first = blockIdx.y * (all ? 1 : 4) + (all ? 0 : wave);
     auto part = [&](int32_t k) { return (int64_t)(2 * (d.wa + k) + (k == 0 ? 1 : 0)) * rows; };
     for (int32_t r = (p - d.wa) * share + first; r < M; r += parts * share) {
       float top = -INFINITY;
@@ -1665,8 +1679,9 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvBatch b, KvAttn a, KvWor
       top = wave_max(top);
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       float l = 0.f;
-#pragma unroll 4
-      for (int32_t k = gr; k < parts; k += GR) {
+      const int32_t step = all ? 4 * GR : GR;
+#pragma unroll 8
+      for (int32_t k = all ? wave * GR + gr : gr; k < parts; k += step) {
         const int64_t at = part(k) + r;
         const float2 ml = wk.ml[at];
         const float4 x = *reinterpret_cast<const float4*>(wk.o + at * HD + 4 * ln);
@@ -1685,6 +1700,22 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvBatch b, KvAttn a, KvWor
         v.w += __shfl_xor(v.w, e, kWave);
         l += __shfl_xor(l, e, kWave);
       }
+      if (all) {
+        __syncthreads();  // the last row's sums are read
+        if (gr == 0) so[wave][ln] = v;
+        if (lane == 0) sl[wave] = l;
+        __syncthreads();
+        if (wave > 0) continue;
+#pragma unroll
+        for (int k = 1; k < 4; ++k) {
+          const float4 x = so[k][ln];
+          v.x += x.x;
+          v.y += x.y;
+          v.z += x.z;
+          v.w += x.w;
+          l += sl[k];
+        }
+      }
       if (gr == 0) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const int32_t rr = d.qt * rows + r, j = rr / G;
@@ -1692,11 +1723,16 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvBatch b, KvAttn a, KvWor
             make_uint2(pack_bf2(v.x * inv, v.y * inv), pack_bf2(v.z * inv, v.w * inv));
       }
     }
+    __syncthreads();  // so and sl are read
   }
 }
 
 // Query rows of a unit's tile, and workgroups: as many as are resident together, and no
 // more than the batch can have tiles.
+// (Tiles of a workgroup, where there are so many: with one tile of 64 keys each of 128
+// rows leaves as much as partial results as it reads of keys and values. 8 trees of 25
+// rows over 2,000 rows: 1, 2, 4, 8 tiles 40.4, 38.2, 40.4, 53 us. One row: 1 tile.)
+constexpr int32_t kKvLeastMany = 2, kKvLeastFew = 1;
 struct KvPlan {
   bool many;
   int32_t rows, P;
@@ -1729,6 +1765,7 @@ hipError_t launch_kv_attention(hipStream_t s, const KvCache& c, const KvBatch& b
   w.o = (float*)((char*)ws + k.desc + k.ml);
   w.P = k.P;
   w.group = a.heads / c.kv;
+  w.least = k.many ? kKvLeastMany : kKvLeastFew;
   auto rows = [&](auto hd) {
     constexpr int HD = decltype(hd)::value, NB = HD == 256 ? 1 : 2, W = HD == 256 ? 8 : 4;
     static_assert(16 * NB * W == 128, "rows of the largest tile");

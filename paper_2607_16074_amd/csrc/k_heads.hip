@@ -1400,13 +1400,22 @@ hipError_t launch_small_pick(hipStream_t s, const TokSmallSet& all, int32_t ldz,
 }
 
 // ------------------------------------------------ verification of drafts ---
-// A workgroup walks a tree.  Rejecting children drawn from q leaves max(p_k - q, 0)
-// / T of the node's distribution p_k; with p_k = max(p - a q, 0) / T that is max(p -
-// (a + T) q, 0) over its sum, so that a node's state is the two numbers a and T, and
-// each rejection of a drawn child is one pass over the node's rows for the next T.
+// Rejecting children drawn from q leaves max(p_k - q, 0) / T of the node's
+// distribution p_k; with p_k = max(p - a q, 0) / T that is max(p - (a + T) q, 0) over its
+// sum, so that a node's state is the two numbers a and T, and a rejected drawn child costs
+// one pass over the node's rows for the next T. Drafts that were picked need no pass:
+// their p is taken off T. At last the next token needs one pass over the last node's row.
+// A pass over a row by one workgroup would take 25 us for 160,001 tokens of p and q, so passes
+// are launches of their own: tok_sums_kernel, `chunks` workgroups to a tree, each of
+// which walks the tree for itself as far as the sums of the launches before it reach, and sums
+// its piece of the row that the walk then needs. tok_pick_next_kernel walks to the end (with
+// passes of its own where the launches were too few) and finds the token in the pieces.
+// What a walk needs of a node is one entry of its parent's rows: all nodes' are
+// fetched together, then the walk is a wavefront's, a child after the other.
 // All sums are formed in 64 bits: a border between two tokens lies where the
 // definition has it, whatever order the terms are added in.
-constexpr int kVerifyThreads = 1024;
+constexpr int kSumThreads = 256, kPickThreads = 1024;
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 
 __device__ __forceinline__ double wave_sum64(double v) {
 #pragma unroll
@@ -1414,129 +1423,362 @@ __device__ __forceinline__ double wave_sum64(double v) {
   return v;
 }
 
-__global__ __launch_bounds__(kVerifyThreads) void tok_verify_kernel(TokVerifySet set) {
-  __shared__ double part[16];
-  __shared__ int32_t gone[JN_KV_TREE_ROWS];  // rejected tokens of picked drafts
-  __shared__ int32_t pick[2];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  int32_t g = 0;
-  while (g + 1 < set.G && set.t[g + 1].tree0 <= (int32_t)blockIdx.x) ++g;
-  const TokVerify& d = set.t[g];
-  const int32_t t = blockIdx.x - d.tree0, V = d.vocab;
-  const int32_t first = min(max(d.cu[t], 0), d.n);
-  const int32_t n = min(max(min(d.cu[t + 1], d.n) - first, 0), d.parents ? JN_KV_TREE_ROWS : d.max_path);
-  int32_t* const path = d.path + (int64_t)t * d.max_path;
-  for (int32_t k = tid; k < d.max_path; k += kVerifyThreads) path[k] = -1;
-  if (n == 0) {
-    if (tid == 0) d.n_path[t] = 0, d.next[t] = -1;
-    return;
-  }
-  // sum over the row c of w_i, by all threads, the same in all of them
-  auto weight = [&](int32_t c, double a, int32_t ngone, int32_t i) {
-    double x = d.p[(first + c) * d.ldp + i];
-    if (d.q) {
-      x -= a * d.q[(first + c) * d.ldq + i];
-    } else {
-      for (int32_t k = 0; k < ngone; ++k)
-        if (gone[k] == i) x = 0.;
-    }
-    return x > 0. ? x : 0.;
-  };
-  auto row_sum = [&](int32_t c, double a, int32_t ngone) {
-    double v = 0.;
-    for (int32_t i = tid; i < V; i += kVerifyThreads) v += weight(c, a, ngone, i);
-    v = wave_sum64(v);
+// Elements of a row's piece: pieces are whole multiples of 4.
+__device__ __forceinline__ int32_t verify_piece(int32_t vocab, int32_t chunks) {
+  return ((vocab + chunks - 1) / chunks + 3) / 4 * 4;
+}
+
+struct VerifyWalk {
+  // of the standing branch's last node: what is left of its distribution
+  int32_t cur, count, ngone;
+  double a, before, T;
+  bool waits;   // for T, the sum of what is left at a
+  int32_t used; // sums that the walk has taken
+};
+// Shared by a workgroup: the window's nodes, rejected tokens.
+struct VerifyNodes {
+  int32_t parent[JN_KV_TREE_ROWS], token[JN_KV_TREE_ROWS];
+  float u[JN_KV_TREE_ROWS], p[JN_KV_TREE_ROWS], q[JN_KV_TREE_ROWS];
+  int32_t gone[JN_KV_TREE_ROWS];
+  VerifyWalk walk;
+};
+
+// Sum `k` of the launches before, from its pieces, by a wavefront.
+__device__ __forceinline__ double verify_sum(const double* part, int32_t chunks, int lane) {
+  double v = 0.;
+  for (int32_t c = lane; c < chunks; c += 64) v += part[c];
+  return wave_sum64(v);
+}
+
+// The walk of a tree of n nodes by the first wavefront, which takes sum k from
+// sums[k * stride] (`have` of them) or stops and waits for it; every thread gets the end from
+// s.walk. path (or null) receives the standing nodes.
+template <int THREADS>
+__device__ void verify_walk(VerifyNodes& s, const TokVerify& d, int32_t first, int32_t n, const double* sums,
+                            int64_t stride, int32_t chunks, int32_t have, int32_t* path) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  VerifyWalk w{0, 1, 0, 0., 0., 1., false, 0};
+  bool over = d.max_path == 1;
+  for (int32_t w0 = 0; w0 < n; w0 += JN_KV_TREE_ROWS) {  // (a chain may be longer than a window)
+    const int32_t m = min(n - w0, JN_KV_TREE_ROWS);
     __syncthreads();
-    if (lane == 0) part[w] = v;
-    __syncthreads();
-    v = 0.;
-    for (int k = 0; k < 16; ++k) v += part[k];
-    return v;
-  };
-  int32_t cur = 0, count = 1, ngone = 0;
-  double a = 0., before = 0., T = 1.;
-  __syncthreads();
-  if (tid == 0) path[0] = 0;
-  for (int32_t j = 1; j < n && count < d.max_path; ++j) {
-    if ((d.parents ? kv_parent(d.parents + first, j) : j - 1) != cur) continue;
-    const int32_t x = d.tokens[first + j];
-    if (x < 0 || x >= V) continue;
-    bool stands;
-    if (!d.p) {
-      stands = d.greedy[first + cur] == x;
-    } else {
-      const double u = d.u[first + j], px = weight(cur, a, ngone, x);
-      if (d.q) {
-        stands = u * d.q[(first + cur) * d.ldq + x] * T < px;
-        if (!stands && T > 0.) {
-          before = a;
-          a += T;
-          T = row_sum(cur, a, 0);
-        }
+    for (int32_t i = tid; i < m; i += THREADS) {
+      const int32_t j = w0 + i, up = j == 0 ? -1 : d.parents ? kv_parent(d.parents + first, j) : j - 1;
+      const int32_t x = d.tokens[first + j];
+      const bool on = up >= 0 && x >= 0 && x < d.vocab;
+      s.parent[i] = on ? up : -1;
+      s.token[i] = x;
+      if (d.p) {
+        s.u[i] = on ? d.u[first + j] : 0.f;
+        s.p[i] = on ? d.p[(first + up) * d.ldp + x] : 0.f;
+        s.q[i] = on && d.q ? d.q[(first + up) * d.ldq + x] : 0.f;
       } else {
-        stands = u * T < px;
-        if (!stands) {
-          T -= px;
-          __syncthreads();
-          if (tid == 0) gone[ngone] = x;
-          ++ngone;
-          __syncthreads();
+        s.p[i] = on && d.greedy[first + up] == x ? 1.f : 0.f;
+      }
+    }
+    __syncthreads();
+    if (tid >= 64) continue;
+#pragma unroll 1
+    for (int32_t b0 = 0; b0 < m && !over; b0 += 64) {
+      const int32_t i = b0 + lane;
+      const bool in = i < m;
+      const int32_t parent = in ? s.parent[i] : -1, token = in ? s.token[i] : -1;
+      const float pv = in ? s.p[i] : 0.f, qv = in ? s.q[i] : 0.f, uv = in && d.p ? s.u[i] : 0.f;
+      uint64_t left = ~0ull;
+      while (true) {
+        const uint64_t kids = __ballot(parent == w.cur) & left;
+        if (kids == 0) break;
+        const int k = __builtin_ctzll(kids);
+        left = k == 63 ? 0 : ~0ull << (k + 1);
+        const int32_t j = w0 + b0 + k, x = __builtin_amdgcn_readlane(token, k);
+        const double p = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(pv), k));
+        const double q = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(qv), k));
+        const double u = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(uv), k));
+        bool stands;
+        if (!d.p) {
+          stands = p > 0.;
+        } else if (d.q) {
+          const double rest = p - w.a * q;
+          stands = u * q * w.T < (rest > 0. ? rest : 0.);
+          if (!stands && w.T > 0.) {
+            w.before = w.a;
+            w.a += w.T;
+            if (w.used == have) {
+              w.waits = over = true;
+              break;
+            }
+            w.T = verify_sum(sums + w.used * stride, chunks, lane);
+            ++w.used;
+          }
+        } else {
+          bool was = false;
+          for (int32_t g = lane; g < w.ngone; g += 64) was |= s.gone[g] == x;
+          const double rest = __any(was) || !(p > 0.) ? 0. : p;
+          stands = u * w.T < rest;
+          if (!stands) {
+            w.T -= rest;
+            if (lane == 0) s.gone[w.ngone] = x;
+            ++w.ngone;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          }
+        }
+        if (stands) {
+          if (path && lane == 0) path[w.count] = j;
+          w.cur = j;
+          ++w.count;
+          w.ngone = 0;
+          w.a = w.before = 0.;
+          w.T = 1.;
+          if (w.count == d.max_path) {
+            over = true;
+            break;
+          }
         }
       }
     }
-    if (stands) {
-      if (tid == 0) path[count] = j;
-      ++count;
-      cur = j;
-      a = before = 0.;
-      T = 1.;
-      ngone = 0;
-    }
+    if (lane == 0) s.walk = w;
   }
-  if (tid == 0) d.n_path[t] = count;
-  if (!d.p) {
-    if (tid == 0) d.next[t] = d.greedy[first + cur];
+  __syncthreads();
+}
+
+// Weights of elements i .. i + 3 of the row of node c.
+__device__ __forceinline__ void verify_weights(const TokVerify& d, const VerifyNodes& s, int64_t row, double a,
+                                               int32_t ngone, int32_t i, double (&w)[4]) {
+  const float* const p = d.p + row * d.ldp + i;
+  f32x4u x{0.f, 0.f, 0.f, 0.f}, y{0.f, 0.f, 0.f, 0.f};
+  const bool whole = i + 4 <= d.vocab;
+  if (whole) {
+    x = *reinterpret_cast<const f32x4u*>(p);
+    if (d.q) y = *reinterpret_cast<const f32x4u*>(d.q + row * d.ldq + i);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (i + e < d.vocab) {
+        x[e] = p[e];
+        if (d.q) y[e] = d.q[row * d.ldq + i + e];
+      }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const double v = d.q ? (double)x[e] - a * (double)y[e] : (double)x[e];
+    w[e] = v > 0. ? v : 0.;
+  }
+  for (int32_t g = 0; g < ngone; ++g) {
+    const uint32_t e = s.gone[g] - i;
+    if (e < 4u) w[e] = 0.;
+  }
+}
+
+__device__ __forceinline__ const TokVerify& verify_tenant(const TokVerifySet& set, int32_t tree) {
+  int32_t g = 0;
+  while (g + 1 < set.G && set.t[g + 1].tree0 <= tree) ++g;
+  return set.t[g];
+}
+__device__ __forceinline__ int32_t verify_nodes(const TokVerify& d, int32_t t, int32_t& first) {
+  first = min(max(d.cu[t], 0), d.n);
+  return min(max(min(d.cu[t + 1], d.n) - first, 0), d.parents ? JN_KV_TREE_ROWS : d.max_path);
+}
+
+// Sum `phase` of every tree that needs one, in pieces: part [phase][tree][chunk].
+__global__ __launch_bounds__(kSumThreads) void tok_sums_kernel(TokVerifySet set, double* __restrict__ part, int32_t phase) {
+  __shared__ VerifyNodes s;
+  __shared__ double red[4];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int32_t tree = blockIdx.x / set.chunks, c = blockIdx.x - tree * set.chunks;
+  const TokVerify& d = verify_tenant(set, tree);
+  int32_t first;
+  const int32_t n = verify_nodes(d, tree - d.tree0, first);
+  if (n == 0 || !d.p) return;
+  const int64_t stride = (int64_t)set.trees * set.chunks;
+  double* const mine = part + (int64_t)tree * set.chunks;
+  verify_walk<kSumThreads>(s, d, first, n, mine, stride, set.chunks, phase, nullptr);
+  const VerifyWalk w = s.walk;
+  // (the sum that the walk waits for; at its end the next token's, unless that is the last one taken)
+  if (!w.waits && (w.used < phase || (d.q && w.a > 0.))) return;
+  const int32_t piece = verify_piece(d.vocab, set.chunks), i0 = min(c * piece, d.vocab), i1 = min(i0 + piece, d.vocab);
+  double v = 0.;
+#pragma unroll 4
+  for (int32_t i = i0 + 4 * tid; i < i1; i += 4 * kSumThreads) {
+    double x[4];
+    verify_weights(d, s, first + w.cur, w.a, w.ngone, i, x);
+    v += (x[0] + x[1]) + (x[2] + x[3]);
+  }
+  v = wave_sum64(v);
+  if (lane == 0) red[tid >> 6] = v;
+  __syncthreads();
+  if (tid == 0) mine[phase * stride + c] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+__global__ __launch_bounds__(kPickThreads) void tok_pick_next_kernel(TokVerifySet set, const double* __restrict__ part,
+                                                                    int32_t phases) {
+  __shared__ VerifyNodes s;
+  __shared__ double sums[kVerifyChunks], red[16], own[JN_KV_TREE_ROWS];
+  __shared__ int32_t pick[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int32_t tree = blockIdx.x;
+  const TokVerify& d = verify_tenant(set, tree);
+  const int32_t t = tree - d.tree0;
+  int32_t first;
+  const int32_t n = verify_nodes(d, t, first);
+  int32_t* const path = d.path + (int64_t)t * d.max_path;
+  for (int32_t k = tid; k < d.max_path; k += kPickThreads) path[k] = k == 0 && n > 0 ? 0 : -1;
+  if (n == 0) {
+    if (tid == 0) {
+      d.n_path[t] = 0;
+      d.next[t] = -1;
+    }
     return;
   }
-  // the next token: every thread sums a run of the row, then the run that passes r
-  // of the whole is walked again
-  double all = row_sum(cur, a, ngone);
-  if (d.q && all == 0.) a = before, all = row_sum(cur, a, ngone);
-  const double want = (double)d.r[t] * all;
-  const int32_t run = (V + kVerifyThreads - 1) / kVerifyThreads, i0 = min(tid * run, V), i1 = min(i0 + run, V);
-  double own = 0.;
-  for (int32_t i = i0; i < i1; ++i) own += weight(cur, a, ngone, i);
-  double up = own;  // of the wavefront's runs up to this one
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double v = __shfl_up(up, o, kWave);
-    if (lane >= o) up += v;
+  const int64_t stride = (int64_t)set.trees * set.chunks;
+  const double* const mine = part + (int64_t)tree * set.chunks;
+  const int32_t piece = verify_piece(d.vocab, set.chunks);
+  // pieces' sums of what is left at (c, a), the same grouping whoever forms them
+  auto pieces = [&](const VerifyWalk& w, double a) {
+    for (int32_t c = wave; c < set.chunks; c += 16) {
+      const int32_t i0 = min(c * piece, d.vocab), i1 = min(i0 + piece, d.vocab);
+      double v = 0.;
+#pragma unroll 4
+      for (int32_t i = i0 + 4 * lane; i < i1; i += 256) {
+        double x[4];
+        verify_weights(d, s, first + w.cur, a, w.ngone, i, x);
+        v += (x[0] + x[1]) + (x[2] + x[3]);
+      }
+      v = wave_sum64(v);
+      if (lane == 0) sums[c] = v;
+    }
+    __syncthreads();
+  };
+  // The sums that there are, then those that the walk goes on to need. `own` holds them all:
+  // a walk is begun again with one more each time.
+  int32_t have = d.p ? phases : 0;
+  for (int32_t k = wave; k < have; k += 16) {
+    const double v = verify_sum(mine + k * stride, set.chunks, lane);
+    if (lane == 0) own[k] = v;
   }
-  __syncthreads();
-  if (lane == 63) part[w] = up;
-  if (tid == 0) pick[0] = pick[1] = -1;
-  __syncthreads();
-  double base = 0.;
-  for (int k = 0; k < w; ++k) base += part[k];
-  up = base + (up - own);
-  int32_t last = -1, hit = -1;
-  for (int32_t i = i0; i < i1; ++i) {
-    const double x = weight(cur, a, ngone, i);
-    if (x > 0.) {
-      up += x;
-      last = i;
-      if (hit < 0 && up > want) hit = i;
+  bool here = false;  // `sums` are of the walk's last sum
+  while (true) {
+    verify_walk<kPickThreads>(s, d, first, n, own, 1, 1, have, path);
+    if (!s.walk.waits) break;
+    const VerifyWalk w = s.walk;
+    pieces(w, w.a);
+    if (wave == 0) {
+      const double v = verify_sum(sums, set.chunks, lane);
+      if (lane == 0) own[have] = v;
+    }
+    ++have;
+    here = true;
+    __syncthreads();
+  }
+  const VerifyWalk w = s.walk;
+  if (tid == 0) d.n_path[t] = w.count;
+  if (!d.p) {
+    if (tid == 0) d.next[t] = d.greedy[first + w.cur];
+    return;
+  }
+  double a = w.a;
+  if (d.q && a > 0. && w.T == 0.) {
+    a = w.before;
+    pieces(w, a);
+  } else if (d.q && a > 0.) {
+    if (!here || w.used != have) {
+      // (the last sum taken is number used - 1, of a launch)
+      __syncthreads();
+      for (int32_t c = tid; c < set.chunks; c += kPickThreads) sums[c] = mine[(w.used - 1) * stride + c];
+      __syncthreads();
+    }
+  } else if (w.used < phases) {
+    __syncthreads();
+    for (int32_t c = tid; c < set.chunks; c += kPickThreads) sums[c] = mine[w.used * stride + c];
+    __syncthreads();
+  } else {
+    pieces(w, a);
+  }
+  // the piece that passes r of the whole, and in it every thread's run
+  if (wave == 0) {
+    double up = 0.;  // before the lane's pieces
+    const int32_t per = (set.chunks + 63) / 64, c0 = min(lane * per, set.chunks), c1 = min(c0 + per, set.chunks);
+    double v = 0.;
+    for (int32_t c = c0; c < c1; ++c) v += sums[c];
+    up = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const double x = __shfl_up(up, o, kWave);
+      if (lane >= o) up += x;
+    }
+    const double want = (double)d.r[t] * __shfl(up, 63, kWave);
+    double at = up - v;
+    int32_t hit = -1, last = -1;
+    double base = 0., lbase = 0.;
+    for (int32_t c = c0; c < c1; ++c) {
+      if (sums[c] > 0.) {
+        last = c;
+        lbase = at;
+      }
+      at += sums[c];
+      if (hit < 0 && sums[c] > 0. && at > want) {
+        hit = c;
+        base = at - sums[c];
+      }
+    }
+    // the first such piece; where rounding leaves none the last one with a weight
+    const uint64_t hits = __ballot(hit >= 0), some = __ballot(last >= 0);
+    const int l = hits ? __builtin_ctzll(hits) : some ? 63 - __builtin_clzll(some) : 0;
+    if (lane == l) {
+      pick[0] = hits ? hit : last;
+      pick[1] = hits != 0;
+      red[0] = want - (hits ? base : lbase);
     }
   }
-  // (the lowest hit; the last positive weight where rounding leaves none)
+  __syncthreads();
+  const int32_t c = pick[0];
+  const bool found = pick[1] != 0;
+  const double want = red[0];
+  __syncthreads();
+  if (c < 0) {
+    if (tid == 0) d.next[t] = -1;
+    return;
+  }
+  const int32_t i0 = c * piece, i1 = min(i0 + piece, d.vocab);
+  const int32_t run = ((i1 - i0 + kPickThreads - 1) / kPickThreads + 3) / 4 * 4;
+  const int32_t r0 = min(i0 + tid * run, i1), r1 = min(r0 + run, i1);
+  double v = 0., x[4];
+  for (int32_t i = r0; i < r1; i += 4) {
+    verify_weights(d, s, first + w.cur, a, w.ngone, i, x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v += i + e < i1 ? x[e] : 0.;
+  }
+  double up = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double y = __shfl_up(up, o, kWave);
+    if (lane >= o) up += y;
+  }
+  if (lane == 63) red[wave] = up;
+  if (tid == 0) pick[0] = pick[1] = -1;
+  __syncthreads();
+  double at = 0.;
+  for (int k = 0; k < wave; ++k) at += red[k];
+  at += up - v;
+  int32_t last = -1, hit = -1;
+  for (int32_t i = r0; i < r1; i += 4) {
+    verify_weights(d, s, first + w.cur, a, w.ngone, i, x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (i + e < i1 && x[e] > 0.) {
+        at += x[e];
+        last = i + e;
+        if (hit < 0 && at > want) hit = i + e;
+      }
+  }
   if (last >= 0) atomicMax(&pick[1], last);
-  if (hit >= 0) atomicMin((uint32_t*)&pick[0], (uint32_t)hit);
+  if (hit >= 0 && found) atomicMin((uint32_t*)&pick[0], (uint32_t)hit);
   __syncthreads();
   if (tid == 0) d.next[t] = pick[0] >= 0 ? pick[0] : pick[1];
 }
 
-hipError_t launch_tok_verify(hipStream_t s, const TokVerifySet& set) {
-  tok_verify_kernel<<<set.trees, kVerifyThreads, 0, s>>>(set);
+hipError_t launch_tok_verify(hipStream_t s, const TokVerifySet& set, int32_t phases, double* part) {
+  for (int32_t k = 0; k < phases; ++k) tok_sums_kernel<<<set.trees * set.chunks, kSumThreads, 0, s>>>(set, part, k);
+  tok_pick_next_kernel<<<set.trees, kPickThreads, 0, s>>>(set, part, phases);
   return hipGetLastError();
 }
 
