@@ -1974,7 +1974,7 @@ struct VerifyPlan {
   TokVerifySet set;
   int32_t phases;
   int64_t nodes;
-  size_t bytes;
+  size_t state, gone, part, bytes;
 };
 bool verify_plan(const jn_token_verify* v, int32_t G, int32_t* g, VerifyPlan* P) {
   TokVerifySet& set = P->set;
@@ -2014,7 +2014,10 @@ bool verify_plan(const jn_token_verify* v, int32_t G, int32_t* g, VerifyPlan* P)
   if (set.trees == 0) return false;
   const int32_t most = (vocab + 1023) / 1024;
   set.chunks = std::min({std::max(1, (kVerifyGroups + set.trees - 1) / set.trees), most, kVerifyChunks});
-  P->bytes = (size_t)P->phases * set.trees * set.chunks * sizeof(double);
+  P->state = 0;
+  P->gone = align_up(2 * (size_t)set.trees * sizeof(VerifyState), 256);
+  P->part = P->gone + align_up((size_t)set.trees * JN_KV_TREE_ROWS * sizeof(int32_t), 256);
+  P->bytes = P->phases > 0 ? P->part + 2 * (size_t)set.trees * set.chunks * sizeof(double) : 0;
   return true;
 }
 }  // namespace
@@ -2040,9 +2043,11 @@ jn_status jn_tenant_tokens_verify(jn_ctx* c, const jn_token_verify* v, int32_t G
   if (need > 0 && (uintptr_t)ws % 16 != 0) return fail(c, JN_EUNSUPPORTED, "workspace not 16-byte aligned");
   if ((st = check_device(c)) != JN_OK) return st;
   VerifyPlan P;
-  for (int32_t g = 0; verify_plan(v, G, &g, &P);)
-    JN_TRACED(c, JN_OP_TOKEN_VERIFY, P.nodes, P.set.t[0].vocab, 0,
-              launch_tok_verify(c->stream, P.set, P.phases, (double*)ws), "verification of drafts");
+  for (int32_t g = 0; verify_plan(v, G, &g, &P);) {
+    const VerifySums sums{(VerifyState*)((char*)ws + P.state), (int32_t*)((char*)ws + P.gone), (double*)((char*)ws + P.part)};
+    JN_TRACED(c, JN_OP_TOKEN_VERIFY, P.nodes, P.set.t[0].vocab, 0, launch_tok_verify(c->stream, P.set, P.phases, sums),
+              "verification of drafts");
+  }
   return JN_OK;
 }
 

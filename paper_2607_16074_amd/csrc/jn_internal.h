@@ -567,8 +567,25 @@ struct TokVerifySet {
   int32_t G, trees, chunks;
 };
 static_assert(sizeof(TokVerifySet) <= 3400, "kernel arguments");
-// part: [phases][trees][chunks]
-hipError_t launch_tok_verify(hipStream_t s, const TokVerifySet& set, int32_t phases, double* part);
+// Where a tree's walk is: its last standing node and what is left there, max(p - a q,
+// 0) with sum T (before: a before the last rejection) or p without `ngone` tokens.
+struct VerifyState {
+  double a, before, T;
+  int32_t cur, count, ngone;
+  int32_t at;     // node to go on with
+  int32_t waits;  // for T
+  int32_t over;   // no node is tried any more
+  int32_t ends;   // so after a launch: nothing but the next token is missing
+  int32_t slot;   // which of `part` holds the last sum's pieces
+};
+// state [2][trees], gone [trees][JN_KV_TREE_ROWS], part [2][trees][chunks]: a launch
+// reads what the one before it wrote beside.
+struct VerifySums {
+  VerifyState* state;
+  int32_t* gone;
+  double* part;
+};
+hipError_t launch_tok_verify(hipStream_t s, const TokVerifySet& set, int32_t phases, const VerifySums& v);
 
 // ------------------------------------------------------------ optimizer ---
 

@@ -1407,9 +1407,9 @@ hipError_t launch_small_pick(hipStream_t s, const TokSmallSet& all, int32_t ldz,
 // their p is taken off T. At last the next token needs one pass over the last node's row.
 // A pass over a row by one workgroup would take 25 us for 160,001 tokens of p and q, so passes
 // are launches of their own: tok_sums_kernel, `chunks` workgroups to a tree, each of
-// which walks the tree for itself as far as the sums of the launches before it reach, and sums
-// its piece of the row that the walk then needs. tok_pick_next_kernel walks to the end (with
-// passes of its own where the launches were too few) and finds the token in the pieces.
+// which walks the tree for itself until it needs a sum, and sums its piece of that row.
+// The next launch goes on from there (VerifyState), and tok_pick_next_kernel to the end,
+// with passes of its own where the launches were too few; it finds the token in the pieces.
 // What a walk needs of a node is one entry of its parent's rows: all nodes' are
 // fetched together, then the walk is a wavefront's, a child after the other.
 // All sums are formed in 64 bits: a border between two tokens lies where the
@@ -1428,38 +1428,35 @@ __device__ __forceinline__ int32_t verify_piece(int32_t vocab, int32_t chunks) {
   return ((vocab + chunks - 1) / chunks + 3) / 4 * 4;
 }
 
-struct VerifyWalk {
-  // of the standing branch's last node: what is left of its distribution
-  int32_t cur, count, ngone;
-  double a, before, T;
-  bool waits;   // for T, the sum of what is left at a
-  int32_t used; // sums that the walk has taken
-};
-// Shared by a workgroup: the window's nodes, rejected tokens.
+// Shared by a workgroup: the window's nodes, rejected tokens, where the walk is.
 struct VerifyNodes {
   int32_t parent[JN_KV_TREE_ROWS], token[JN_KV_TREE_ROWS];
   float u[JN_KV_TREE_ROWS], p[JN_KV_TREE_ROWS], q[JN_KV_TREE_ROWS];
   int32_t gone[JN_KV_TREE_ROWS];
-  VerifyWalk walk;
+  VerifyState walk;
 };
 
-// Sum `k` of the launches before, from its pieces, by a wavefront.
-__device__ __forceinline__ double verify_sum(const double* part, int32_t chunks, int lane) {
+__device__ __forceinline__ VerifyState verify_start(const TokVerify& d) {
+  VerifyState w{};
+  w.count = 1;
+  w.T = 1.;
+  w.over = d.max_path == 1;
+  return w;
+}
+
+// Sum of pieces by a wavefront.
+__device__ __forceinline__ double verify_sum(const double* part, int32_t chunks, int32_t lane) {
   double v = 0.;
   for (int32_t c = lane; c < chunks; c += 64) v += part[c];
   return wave_sum64(v);
 }
 
-// The walk of a tree of n nodes by the first wavefront, which takes sum k from
-// sums[k * stride] (`have` of them) or stops and waits for it; every thread gets the end from
-// s.walk. path (or null) receives the standing nodes.
+// The walk of a tree of n nodes by the first wavefront, on from w, until it needs a sum
+// (w.waits) or is over; every thread gets the end. path (or null) receives standing nodes.
 template <int THREADS>
-__device__ void verify_walk(VerifyNodes& s, const TokVerify& d, int32_t first, int32_t n, const double* sums,
-                            int64_t stride, int32_t chunks, int32_t have, int32_t* path) {
+__device__ VerifyState verify_walk(VerifyNodes& s, const TokVerify& d, int32_t first, int32_t n, VerifyState w, int32_t* path) {
   const int tid = threadIdx.x, lane = tid & 63;
-  VerifyWalk w{0, 1, 0, 0., 0., 1., false, 0};
-  bool over = d.max_path == 1;
-  for (int32_t w0 = 0; w0 < n; w0 += JN_KV_TREE_ROWS) {  // (a chain may be longer than a window)
+  for (int32_t w0 = w.at / JN_KV_TREE_ROWS * JN_KV_TREE_ROWS; w0 < n; w0 += JN_KV_TREE_ROWS) {  // (of a long chain)
     const int32_t m = min(n - w0, JN_KV_TREE_ROWS);
     __syncthreads();
     for (int32_t i = tid; i < m; i += THREADS) {
@@ -1479,18 +1476,20 @@ __device__ void verify_walk(VerifyNodes& s, const TokVerify& d, int32_t first, i
     __syncthreads();
     if (tid >= 64) continue;
 #pragma unroll 1
-    for (int32_t b0 = 0; b0 < m && !over; b0 += 64) {
+    for (int32_t b0 = max(0, w.at - w0) & ~63; b0 < m && !w.over && !w.waits; b0 += 64) {
       const int32_t i = b0 + lane;
       const bool in = i < m;
       const int32_t parent = in ? s.parent[i] : -1, token = in ? s.token[i] : -1;
       const float pv = in ? s.p[i] : 0.f, qv = in ? s.q[i] : 0.f, uv = in && d.p ? s.u[i] : 0.f;
-      uint64_t left = ~0ull;
+      const int32_t done = w.at - w0 - b0;  // nodes of the block before the one to go on with
+      uint64_t left = done <= 0 ? ~0ull : ~0ull << done;
       while (true) {
         const uint64_t kids = __ballot(parent == w.cur) & left;
         if (kids == 0) break;
         const int k = __builtin_ctzll(kids);
         left = k == 63 ? 0 : ~0ull << (k + 1);
         const int32_t j = w0 + b0 + k, x = __builtin_amdgcn_readlane(token, k);
+        w.at = j + 1;
         const double p = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(pv), k));
         const double q = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(qv), k));
         const double u = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(uv), k));
@@ -1503,12 +1502,8 @@ __device__ void verify_walk(VerifyNodes& s, const TokVerify& d, int32_t first, i
           if (!stands && w.T > 0.) {
             w.before = w.a;
             w.a += w.T;
-            if (w.used == have) {
-              w.waits = over = true;
-              break;
-            }
-            w.T = verify_sum(sums + w.used * stride, chunks, lane);
-            ++w.used;
+            w.waits = 1;
+            break;
           }
         } else {
           bool was = false;
@@ -1530,15 +1525,19 @@ __device__ void verify_walk(VerifyNodes& s, const TokVerify& d, int32_t first, i
           w.a = w.before = 0.;
           w.T = 1.;
           if (w.count == d.max_path) {
-            over = true;
+            w.over = 1;
             break;
           }
         }
       }
     }
+  }
+  if (tid < 64) {
+    if (!w.waits) w.over = 1;
     if (lane == 0) s.walk = w;
   }
   __syncthreads();
+  return s.walk;
 }
 
 // Weights of elements i .. i + 3 of the row of node c.
@@ -1579,41 +1578,60 @@ __device__ __forceinline__ int32_t verify_nodes(const TokVerify& d, int32_t t, i
   return min(max(min(d.cu[t + 1], d.n) - first, 0), d.parents ? JN_KV_TREE_ROWS : d.max_path);
 }
 
-// Sum `phase` of every tree that needs one, in pieces: part [phase][tree][chunk].
-__global__ __launch_bounds__(kSumThreads) void tok_sums_kernel(TokVerifySet set, double* __restrict__ part, int32_t phase) {
+// Launch `phase`: every tree's walk on to the next sum that it needs, and its pieces.
+__global__ __launch_bounds__(kSumThreads) void tok_sums_kernel(TokVerifySet set, VerifySums v, int32_t phase) {
   __shared__ VerifyNodes s;
   __shared__ double red[4];
   const int tid = threadIdx.x, lane = tid & 63;
   const int32_t tree = blockIdx.x / set.chunks, c = blockIdx.x - tree * set.chunks;
   const TokVerify& d = verify_tenant(set, tree);
+  const int32_t t = tree - d.tree0;
   int32_t first;
-  const int32_t n = verify_nodes(d, tree - d.tree0, first);
+  const int32_t n = verify_nodes(d, t, first);
   if (n == 0 || !d.p) return;
-  const int64_t stride = (int64_t)set.trees * set.chunks;
-  double* const mine = part + (int64_t)tree * set.chunks;
-  verify_walk<kSumThreads>(s, d, first, n, mine, stride, set.chunks, phase, nullptr);
-  const VerifyWalk w = s.walk;
-  // (the sum that the walk waits for; at its end the next token's, unless that is the last one taken)
-  if (!w.waits && (w.used < phase || (d.q && w.a > 0.))) return;
+  const int now = phase & 1;
+  VerifyState w = phase == 0 ? verify_start(d) : v.state[(now ^ 1) * set.trees + tree];
+  int32_t* const path = c == 0 ? d.path + (int64_t)t * d.max_path : nullptr;
+  if (path && phase == 0)
+    for (int32_t k = tid; k < d.max_path; k += kSumThreads) path[k] = k == 0 ? 0 : -1;
+  bool sum = false;
+  if (!w.ends) {
+    if (phase > 0) {
+      w.T = verify_sum(v.part + ((int64_t)(now ^ 1) * set.trees + tree) * set.chunks, set.chunks, lane);
+      w.waits = 0;
+      w.slot = now ^ 1;
+    }
+    const double a = w.a;
+    w = verify_walk<kSumThreads>(s, d, first, n, w, path);
+    // at its end it needs the next token's sum, unless that is the one it has just taken
+    w.ends = !w.waits;
+    sum = w.waits || !(d.q && w.a > 0. && w.a == a);
+    if (sum) w.slot = now;
+  }
+  if (c == 0) {
+    if (tid == 0) v.state[now * set.trees + tree] = w;
+    if (phase == 0 && w.ngone > 0)
+      for (int32_t k = tid; k < w.ngone; k += kSumThreads) v.gone[(int64_t)tree * JN_KV_TREE_ROWS + k] = s.gone[k];
+  }
+  if (!sum) return;
   const int32_t piece = verify_piece(d.vocab, set.chunks), i0 = min(c * piece, d.vocab), i1 = min(i0 + piece, d.vocab);
-  double v = 0.;
+  double y = 0.;
 #pragma unroll 4
   for (int32_t i = i0 + 4 * tid; i < i1; i += 4 * kSumThreads) {
     double x[4];
     verify_weights(d, s, first + w.cur, w.a, w.ngone, i, x);
-    v += (x[0] + x[1]) + (x[2] + x[3]);
+    y += (x[0] + x[1]) + (x[2] + x[3]);
   }
-  v = wave_sum64(v);
-  if (lane == 0) red[tid >> 6] = v;
+  y = wave_sum64(y);
+  if (lane == 0) red[tid >> 6] = y;
   __syncthreads();
-  if (tid == 0) mine[phase * stride + c] = (red[0] + red[1]) + (red[2] + red[3]);
+  if (tid == 0) v.part[((int64_t)now * set.trees + tree) * set.chunks + c] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-__global__ __launch_bounds__(kPickThreads) void tok_pick_next_kernel(TokVerifySet set, const double* __restrict__ part,
-                                                                    int32_t phases) {
+__global__ __launch_bounds__(kPickThreads) void tok_pick_next_kernel(TokVerifySet set, VerifySums vs, int32_t phases) {
   __shared__ VerifyNodes s;
-  __shared__ double sums[kVerifyChunks], red[16], own[JN_KV_TREE_ROWS];
-  __shared__ int32_t pick[2];
+  __shared__ double sums[kVerifyChunks], red[16];
+  __shared__ int32_t pick[2], lasts[16], hits16[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t tree = blockIdx.x;
   const TokVerify& d = verify_tenant(set, tree);
@@ -1621,7 +1639,9 @@ __global__ __launch_bounds__(kPickThreads) void tok_pick_next_kernel(TokVerifySe
   int32_t first;
   const int32_t n = verify_nodes(d, t, first);
   int32_t* const path = d.path + (int64_t)t * d.max_path;
-  for (int32_t k = tid; k < d.max_path; k += kPickThreads) path[k] = k == 0 && n > 0 ? 0 : -1;
+  const bool begun = phases > 0 && d.p && n > 0;
+  if (!begun)
+    for (int32_t k = tid; k < d.max_path; k += kPickThreads) path[k] = k == 0 && n > 0 ? 0 : -1;
   if (n == 0) {
     if (tid == 0) {
       d.n_path[t] = 0;
@@ -1629,11 +1649,10 @@ __global__ __launch_bounds__(kPickThreads) void tok_pick_next_kernel(TokVerifySe
     }
     return;
   }
-  const int64_t stride = (int64_t)set.trees * set.chunks;
-  const double* const mine = part + (int64_t)tree * set.chunks;
   const int32_t piece = verify_piece(d.vocab, set.chunks);
-  // pieces' sums of what is left at (c, a), the same grouping whoever forms them
-  auto pieces = [&](const VerifyWalk& w, double a) {
+  // pieces' sums of what is left at (c, a)
+  auto pieces = [&](const VerifyState& w, double a) {
+    __syncthreads();
     for (int32_t c = wave; c < set.chunks; c += 16) {
       const int32_t i0 = min(c * piece, d.vocab), i1 = min(i0 + piece, d.vocab);
       double v = 0.;
@@ -1648,51 +1667,37 @@ __global__ __launch_bounds__(kPickThreads) void tok_pick_next_kernel(TokVerifySe
     }
     __syncthreads();
   };
-  // The sums that there are, then those that the walk goes on to need. `own` holds them all:
-  // a walk is begun again with one more each time.
-  int32_t have = d.p ? phases : 0;
-  for (int32_t k = wave; k < have; k += 16) {
-    const double v = verify_sum(mine + k * stride, set.chunks, lane);
-    if (lane == 0) own[k] = v;
-  }
-  bool here = false;  // `sums` are of the walk's last sum
-  while (true) {
-    verify_walk<kPickThreads>(s, d, first, n, own, 1, 1, have, path);
-    if (!s.walk.waits) break;
-    const VerifyWalk w = s.walk;
-    pieces(w, w.a);
-    if (wave == 0) {
-      const double v = verify_sum(sums, set.chunks, lane);
-      if (lane == 0) own[have] = v;
-    }
-    ++have;
-    here = true;
+  VerifyState w;
+  if (begun) {
+    w = vs.state[((phases - 1) & 1) * set.trees + tree];
+    const double* const from = vs.part + ((int64_t)w.slot * set.trees + tree) * set.chunks;
+    for (int32_t c = tid; c < set.chunks; c += kPickThreads) sums[c] = from[c];
+    for (int32_t k = tid; k < w.ngone; k += kPickThreads) s.gone[k] = vs.gone[(int64_t)tree * JN_KV_TREE_ROWS + k];
     __syncthreads();
+  } else {
+    w = verify_walk<kPickThreads>(s, d, first, n, verify_start(d), path);
+    if (!d.p) {
+      if (tid == 0) {
+        d.n_path[t] = w.count;
+        d.next[t] = d.greedy[first + w.cur];
+      }
+      return;
+    }
+    pieces(w, w.a);
   }
-  const VerifyWalk w = s.walk;
-  if (tid == 0) d.n_path[t] = w.count;
-  if (!d.p) {
-    if (tid == 0) d.next[t] = d.greedy[first + w.cur];
-    return;
+  while (w.waits) {  // more sums than launches: `sums` are what it waits for
+    const double a = w.a;
+    w.T = verify_sum(sums, set.chunks, lane);
+    w.waits = 0;
+    w = verify_walk<kPickThreads>(s, d, first, n, w, path);
+    if (w.waits || w.a != a || !(w.a > 0.)) pieces(w, w.a);
   }
   double a = w.a;
   if (d.q && a > 0. && w.T == 0.) {
     a = w.before;
     pieces(w, a);
-  } else if (d.q && a > 0.) {
-    if (!here || w.used != have) {
-      // (the last sum taken is number used - 1, of a launch)
-      __syncthreads();
-      for (int32_t c = tid; c < set.chunks; c += kPickThreads) sums[c] = mine[(w.used - 1) * stride + c];
-      __syncthreads();
-    }
-  } else if (w.used < phases) {
-    __syncthreads();
-    for (int32_t c = tid; c < set.chunks; c += kPickThreads) sums[c] = mine[w.used * stride + c];
-    __syncthreads();
-  } else {
-    pieces(w, a);
   }
+  if (tid == 0) d.n_path[t] = w.count;
   // the piece that passes r of the whole, and in it every thread's run
   if (wave == 0) {
     double up = 0.;  // before the lane's pieces
@@ -1754,7 +1759,6 @@ __global__ __launch_bounds__(kPickThreads) void tok_pick_next_kernel(TokVerifySe
     if (lane >= o) up += y;
   }
   if (lane == 63) red[wave] = up;
-  if (tid == 0) pick[0] = pick[1] = -1;
   __syncthreads();
   double at = 0.;
   for (int k = 0; k < wave; ++k) at += red[k];
@@ -1770,15 +1774,23 @@ __global__ __launch_bounds__(kPickThreads) void tok_pick_next_kernel(TokVerifySe
         if (hit < 0 && at > want) hit = i + e;
       }
   }
-  if (last >= 0) atomicMax(&pick[1], last);
-  if (hit >= 0 && found) atomicMin((uint32_t*)&pick[0], (uint32_t)hit);
+  // runs ascend with the threads: the first with a hit has the lowest, the last with a weight the highest
+  const uint64_t some = __ballot(last >= 0), ones = __ballot(hit >= 0 && found);
+  if (lane == 0) lasts[wave] = hits16[wave] = -1;
+  if (some != 0 && lane == 63 - __builtin_clzll(some)) lasts[wave] = last;
+  if (ones != 0 && lane == __builtin_ctzll(ones)) hits16[wave] = hit;
   __syncthreads();
-  if (tid == 0) d.next[t] = pick[0] >= 0 ? pick[0] : pick[1];
+  if (tid == 0) {
+    int32_t next = -1;
+    for (int k = 0; k < 16; ++k) next = max(next, lasts[k]);
+    for (int k = 15; k >= 0; --k) next = hits16[k] >= 0 ? hits16[k] : next;
+    d.next[t] = next;
+  }
 }
 
-hipError_t launch_tok_verify(hipStream_t s, const TokVerifySet& set, int32_t phases, double* part) {
-  for (int32_t k = 0; k < phases; ++k) tok_sums_kernel<<<set.trees * set.chunks, kSumThreads, 0, s>>>(set, part, k);
-  tok_pick_next_kernel<<<set.trees, kPickThreads, 0, s>>>(set, part, phases);
+hipError_t launch_tok_verify(hipStream_t s, const TokVerifySet& set, int32_t phases, const VerifySums& v) {
+  for (int32_t k = 0; k < phases; ++k) tok_sums_kernel<<<set.trees * set.chunks, kSumThreads, 0, s>>>(set, v, k);
+  tok_pick_next_kernel<<<set.trees, kPickThreads, 0, s>>>(set, v, phases);
   return hipGetLastError();
 }
 
