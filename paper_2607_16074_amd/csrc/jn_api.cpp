@@ -2007,9 +2007,12 @@ bool verify_plan(const jn_token_verify* v, int32_t G, int32_t* g, VerifyPlan* P)
     set.trees += t.n_trees;
     if (!t.p) continue;
     vocab = std::max(vocab, t.vocab);
-    // a chain has one sum, a tree of drawn drafts one more for every rejection but a node's last
-    const bool more = t.q && t.parents && t.vocab >= kVerifyLongRow && t.n > 2ll * t.n_trees;
-    P->phases = std::max(P->phases, more ? 3 : 1);
+    // A chain has one sum, a tree of drawn drafts one more for every rejection but a node's
+    // last: a launch for each node of a mean tree, where rows are long. 16 trees of up to 9
+    // nodes over 160,001: 1, 2, 4, 5, 6, 8 launches 70, 57, 36, 37, 40, 44 us; 6 of up to
+    // 25 nodes 112, 92, 55, 47, 39, 44; 16 of 25 over 32,003: 1, 6 launches 73, 59.
+    const bool more = t.q && t.parents && t.vocab >= kVerifyLongRow;
+    P->phases = std::max(P->phases, more ? (int32_t)std::min<int64_t>(std::max<int64_t>(t.n / t.n_trees, 1), 6) : 1);
   }
   if (set.trees == 0) return false;
   const int32_t most = (vocab + 1023) / 1024;

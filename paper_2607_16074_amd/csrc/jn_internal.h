@@ -561,7 +561,7 @@ struct TokVerify {
 constexpr int32_t kVerifyTenants = 24;  // of one launch
 constexpr int32_t kVerifyChunks = 256;  // most pieces of a row
 constexpr int32_t kVerifyGroups = 512;  // workgroups of a launch over pieces, about
-constexpr int32_t kVerifyLongRow = 1 << 16;
+constexpr int32_t kVerifyLongRow = 1 << 13;
 struct TokVerifySet {
   TokVerify t[kVerifyTenants];
   int32_t G, trees, chunks;
