@@ -982,7 +982,7 @@ jn_status kv_batch(jn_ctx* c, const jn_kv_batch* b, const jn_kv_cache* k, KvBatc
   out->n_seqs = b->n_seqs;
   out->max_pages = b->max_pages;
   out->rows = b->rows;
-  out->max_new = b->max_new;
+  out->max_new = std::min(b->max_new, 1 << 26);  // (a place stays below 2^31)
   out->places = b->max_pages * k->page_size;
   out->whole = b->whole;
   return JN_OK;
@@ -1118,6 +1118,7 @@ jn_status jn_kv_keep(jn_ctx* c, const jn_kv_cache* cache, const jn_kv_batch* bat
   if (st == JN_OK) st = kv_batch(c, batch, cache, &b);
   if (st != JN_OK) return st;
   if (max_path < 1) return fail(c, JN_EINVAL, "paths of %d rows", max_path);
+  if (max_path > 1 << 26) return fail(c, JN_ESHAPE, "paths of %d rows", max_path);
   if (((uintptr_t)path | (uintptr_t)n_path | (uintptr_t)past_out) % 4 != 0)
     return fail(c, JN_EINVAL, "paths not 4-byte aligned");
   if (b.n_seqs == 0) return JN_OK;

@@ -1070,6 +1070,18 @@ __device__ __forceinline__ bool kv_finite(u32x4& v) {
   return any != 0;
 }
 
+// Chunk permutation of LDS row r for the products below: 16 rows read at one chunk (K)
+// and 4 rows x 2 chunks a 16-lane group (V^T), where groups q and q ^ 1, and q and q ^ 2, are
+// served together. attn_swz has that at head width 256; at 128 its rule is for 32 x 32
+// products and puts rows r and r ^ 4 on one slot pair.
+template <int HD>
+__device__ __forceinline__ int kv_swz(int r) {
+  const int q = (r >> 2) & 3, e = r & 3, pair = (q ^ (q >> 1)) & 1, low = q >> 1;
+  if constexpr (HD == 32) return pair << 1 | low;
+  if constexpr (HD == 64) return ((e >> 1) << 1 | pair) << 1 | low;
+  return (e | pair << 2) << 1 | low;
+}
+
 // ---- few query rows (a unit has at most 16 NB) ----
 // The time is the reading of keys and values, each read once: four wavefronts, each
 // with 32 keys of a 128-key tile and all query rows. Keys go from the cache to
@@ -1103,7 +1115,7 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void kv_few_kernel(KvCache 
   if (!any) return;
   const int32_t G = wk.group;
 
-  const int vrow = 4 * quad + (j16 >> 2), vswz = attn_swz<HD>(vrow);
+  const int vrow = 4 * quad + (j16 >> 2), vswz = kv_swz<HD>(vrow);
   uint32_t vat[NT];  // the lane's transposed reads of the first tile
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -1115,7 +1127,7 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void kv_few_kernel(KvCache 
 #pragma unroll
   for (int v = 0; v < 16 / RPI; ++v) {
     const int r = v * RPI + drow;
-    doff[v] = r * HD + (((lane % CPR) ^ attn_swz<HD>(r)) * 8);
+    doff[v] = r * HD + (((lane % CPR) ^ kv_swz<HD>(r)) * 8);
   }
   const int32_t koff = j16 * HD + quad * 8;
 
@@ -1400,8 +1412,8 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
   if (!any) return;
 
   const int lrow = tid / CPR, lchunk = tid % CPR;
-  const int kswz = attn_swz<HD>(j16);
-  const int vrow = 4 * quad + (j16 >> 2), vswz = attn_swz<HD>(vrow);
+  const int kswz = kv_swz<HD>(j16);
+  const int vrow = 4 * quad + (j16 >> 2), vswz = kv_swz<HD>(vrow);
 
   while (true) {
     const KvSeq sq = run.sq;
@@ -1492,7 +1504,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
 #pragma unroll
       for (int k = 0; k < NL; ++k) {
         const int row = k * RPL + lrow;
-        const int at = row * HD + ((lchunk ^ attn_swz<HD>(row & 15)) * 8);
+        const int at = row * HD + ((lchunk ^ kv_swz<HD>(row & 15)) * 8);
         *reinterpret_cast<u32x4*>(&kt[st][at]) = kr[k];
         *reinterpret_cast<u32x4*>(&vt[st][at]) = vr[k];
       }
@@ -1530,15 +1542,25 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
         for (int e = 0; e < 4; ++e)
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) s[e][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        // (a chunk's fragments are read under the products of the chunk before)
+        auto read_k = [&](int n, bf16x8 (&kf)[4]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int n = 0; n < NC; ++n)
+          for (int e = 0; e < 4; ++e)
+            kf[e] = *reinterpret_cast<const bf16x8*>(Ks + (e * 16 + j16) * HD + (((4 * n + quad) ^ kswz) * 8));
+        };
+        bf16x8 kf[2][4];
+        read_k(0, kf[0]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const bf16x8 kf = *reinterpret_cast<const bf16x8*>(Ks + (e * 16 + j16) * HD + (((4 * n + quad) ^ kswz) * 8));
+        for (int n = 0; n < NC; ++n) {
+          if (n + 1 < NC) read_k(n + 1, kf[(n + 1) & 1]);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
-              s[e][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][nb], s[e][nb], 0, 0, 0);
-          }
+              s[e][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[n & 1][e], qf[n][nb], s[e][nb], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
         if (mask || has != 0xfu || t + KT > kend) {
           const int q4 = (here(lane) >> 4) * 4;
 #pragma unroll
@@ -1595,15 +1617,23 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
               (__attribute__((address_space(3))) bf16x4*)(Vs + (r + 16) * HD + at));
           return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         };
+        bf16x8 vf[2][2];
+        vf[0][0] = read_v(0, 0);
+        vf[0][1] = read_v(0, 1);
 #pragma unroll
-        for (int t2 = 0; t2 < NT; ++t2)
+        for (int t2 = 0; t2 < NT; ++t2) {
+          if (t2 + 1 < NT) {
+            vf[(t2 + 1) & 1][0] = read_v(t2 + 1, 0);
+            vf[(t2 + 1) & 1][1] = read_v(t2 + 1, 1);
+          }
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const bf16x8 vf = read_v(t2, x);
+          for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
-              o[t2][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[x][nb], o[t2][nb], 0, 0, 0);
-          }
+              o[t2][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[t2 & 1][x], pf[x][nb], o[t2][nb], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
       __syncthreads();  // the tile is read, the next one written
     }

@@ -261,40 +261,46 @@ hipError_t launch_unpack(hipStream_t s, const ReqEntry* req_table, int32_t R, co
 // Row past + path[k] of every head and layer to row past + k, keys and values.  A
 // thread owns 16 bytes of a head's rows and takes the path in order, eight rows at a
 // time: path[k] >= k ascends, so a row that a later step reads is not one that an
-// earlier step wrote, and within a step every load stands before the stores.
+// earlier step wrote, and within a step every load stands before the stores. Where they
+// lie is the same for a workgroup and found in scalar registers.
 constexpr int kKeepStep = 8;
 __global__ __launch_bounds__(256) void kv_keep_kernel(KvCache c, KvBatch b, const int32_t* __restrict__ path,
                                                       int32_t max_path, const int32_t* __restrict__ n_path,
                                                       int32_t* past_out, int32_t per) {
   const int32_t s = blockIdx.x / per, part = blockIdx.x - s * per;
-  const int32_t past = min(max(b.past[s], 0), b.places), n = min(max(n_path[s], 0), max_path);
+  const KvTable row = kv_table(path) + (int64_t)s * max_path, pages = kv_table(b.pages) + (int64_t)s * b.max_pages;
+  const int32_t past = min(max(kv_table(b.past)[s], 0), b.places), n = min(max(kv_table(n_path)[s], 0), max_path);
   if (past_out && part == 0 && threadIdx.x == 0) past_out[s] = past + n;
-  const int32_t chunks = c.hd >> 3;
-  const int64_t items = (int64_t)c.n_layers * 2 * c.kv * chunks, i = (int64_t)part * 256 + threadIdx.x;
-  if (i >= items) return;
-  const int32_t chunk = (int32_t)(i % chunks), h = (int32_t)(i / chunks % c.kv);
-  const int64_t lv = i / chunks / c.kv;
-  uint16_t* const base = ((lv & 1) ? c.v : c.k) + (lv >> 1) * c.ld_layer + 8 * chunk;
-  const int32_t* const pages = b.pages + (int64_t)s * b.max_pages;
+  const uint32_t chunks = c.hd >> 3, items = (uint32_t)c.n_layers * 2 * c.kv * chunks, i = part * 256u + threadIdx.x;
+  const uint32_t lvh = i / chunks, lv = lvh / c.kv, h = lvh - lv * c.kv;
+  uint16_t* const base = ((lv & 1) ? c.v : c.k) + (lv >> 1) * c.ld_layer + 8 * (i - lvh * chunks);
+  const int64_t head = (int64_t)h * c.hd << c.page_log2;
+  const int32_t mask = (1 << c.page_log2) - 1;
   int32_t last = -1;
   for (int32_t k0 = 0; k0 < n; k0 += kKeepStep) {
     uint4 v[kKeepStep];
-    int64_t to[kKeepStep];
+    int64_t to[kKeepStep], from[kKeepStep];
+    int32_t j[kKeepStep];
+#pragma unroll
+    for (int e = 0; e < kKeepStep; ++e) j[e] = row[min(k0 + e, max_path - 1)];
 #pragma unroll
     for (int e = 0; e < kKeepStep; ++e) {
-      const int32_t k = k0 + e, j = k < n ? path[(int64_t)s * max_path + k] : -1;
-      to[e] = -1;
-      if (j <= last || j < k || j >= b.max_new) continue;
-      last = j;
-      if (j == k) continue;
-      const int32_t from = kv_page(b, c, pages, past + j), into = kv_page(b, c, pages, past + k);
-      if (from < 0 || into < 0) continue;
-      v[e] = *reinterpret_cast<const uint4*>(base + kv_at(c, from, h, past + j));
-      to[e] = kv_at(c, into, h, past + k);
+      const int32_t k = k0 + e;
+      const bool is = k < n && j[e] > last && j[e] >= k && j[e] < b.max_new;
+      last = is ? j[e] : last;
+      const int32_t x = past + (is ? j[e] : 0), y = past + (is ? k : 0);
+      const int32_t gx = pages[min(x >> c.page_log2, b.max_pages - 1)], gy = pages[min(y >> c.page_log2, b.max_pages - 1)];
+      const bool move = is && x != y && x < b.places && (uint32_t)gx < (uint32_t)c.n_pages && (uint32_t)gy < (uint32_t)c.n_pages;
+      from[e] = gx * c.ld_page + (int64_t)(x & mask) * c.hd;
+      to[e] = move ? gy * c.ld_page + (int64_t)(y & mask) * c.hd : -1;
     }
+    if (i >= items) continue;
 #pragma unroll
     for (int e = 0; e < kKeepStep; ++e)
-      if (to[e] >= 0) *reinterpret_cast<uint4*>(base + to[e]) = v[e];
+      if (to[e] >= 0) v[e] = *reinterpret_cast<const uint4*>(base + from[e] + head);
+#pragma unroll
+    for (int e = 0; e < kKeepStep; ++e)
+      if (to[e] >= 0) *reinterpret_cast<uint4*>(base + to[e] + head) = v[e];
   }
 }
 
