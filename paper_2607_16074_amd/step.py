@@ -16,6 +16,9 @@ resident by ``jn_infer_plan_create`` (pack, shared encode, split, forward-only
 decode), launched eagerly or replayed as a captured HIP graph.
 ``DecodeStep`` is the token-predicting tenants' counterpart: the likeliest next
 token behind every sample's last row.
+``SpeculativeStep`` writes tokens: sequences of such tenants stay in a paged
+cache, and a run takes each one's drafted tokens through the backbone, finds
+which of them stand and keeps those.
 ``isolated_runs`` builds one such step per tenant over the same device
 weights: the serial-execution comparator of grouped execution, using the
 same kernels and the same tile rule.
@@ -26,9 +29,10 @@ from typing import Dict, List, Optional, Sequence
 
 import numpy as np
 
-from . import (EXPERT_LAYER_FIELDS, AdamWTenant, Backbone, Context, Expert, ExpertIO, Head, HeadIO, InferPlan,
-               Request, Tenant, TokenHead, TokenIO, TokenPick, jn_adamw_workspace_size, jn_infer_workspace_size,
-               jn_backbone_forward, jn_backbone_workspace_size, jn_experts_workspace_size, jn_heads_workspace_size,
+from . import (EXPERT_LAYER_FIELDS, AdamWTenant, Backbone, Context, Expert, ExpertIO, Head, HeadIO, InferPlan, KVBatch,
+               KVCache, Request, Tenant, TokenHead, TokenIO, TokenPick, TokenVerify, jn_adamw_workspace_size,
+               jn_infer_workspace_size, jn_backbone_extend, jn_backbone_extend_workspace_size, jn_kv_keep,
+               jn_tenant_tokens_verify, jn_tokens_verify_workspace_size, jn_backbone_forward, jn_backbone_workspace_size, jn_experts_workspace_size, jn_heads_workspace_size,
                jn_pack_group, jn_pack_maps_host, jn_pack_plan, jn_pack_tenant_sizes, jn_tenant_adamw_step,
                jn_tenant_experts_fwd_bwd, jn_tenant_heads_fwd_bwd, jn_tenant_tokens_decode, jn_tenant_tokens_fwd_bwd,
                jn_tokens_decode_workspace_size, jn_tokens_workspace_size, jn_unpack)
@@ -317,6 +321,111 @@ class DecodeStep:
         packed = jn_pack_group(self.ctx, self.requests, self.table, d, self.align, self.maps, self.packed_tokens)
         jn_backbone_forward(self.ctx, self.model.backbone, packed, self.hidden, self.bb_ws, self.pos)
         jn_tenant_tokens_decode(self.ctx, self.hidden, self.heads, self.picks, self.ws)
+
+
+class SpeculativeStep:
+    """Token streams over a paged cache: ``streams[k]`` sequences of tenant ``tenants[k]``, each with room for
+    ``max_len`` rows.  ``prefill`` takes the sequences' prompts; a ``run`` then takes ``nodes`` rows of every sequence (its
+    last token and drafts behind it; ``parents``: a tree of them, the same for all sequences, none: a chain; one row:
+    plain decoding) through the backbone, the likeliest token behind each row (``jn_tenant_tokens_decode``), which drafts
+    stand (``jn_tenant_tokens_verify``), and keeps these (``jn_kv_keep``).  Before a run ``embeds`` [sequences * nodes, d]
+    and ``tokens`` [sequences * nodes] hold the rows and what they stand for; after it ``path`` and ``n_path`` hold the
+    standing rows of every sequence, ``next`` the token behind them, ``past`` the rows in its cache.  ``sample`` instead
+    of ``choose`` verifies against probabilities of the caller's.  Everything is enqueued on the context's stream and
+    reads its buffers when it runs, so a run may be captured and replayed."""
+
+    def __init__(self, model: Model, tenants: Sequence[int], streams: Sequence[int], max_len: int, nodes: int = 1,
+                 parents: Optional[Sequence[int]] = None, page_size: int = 64, ctx: Optional[Context] = None, device="cuda"):
+        import torch
+        bb = model.backbone
+        self.model, self.ctx = model, ctx or Context()
+        self.heads = [model.token_heads[g] for g in tenants]
+        if any(h is None for h in self.heads):
+            raise ValueError("SpeculativeStep serves token-predicting tenants")
+        if parents is not None and len(parents) != nodes:
+            raise ValueError("one parent for every node")
+        if not bb.causal:
+            raise ValueError("tokens are written by a causal backbone")
+        if bb.struct.rope_axes > 1:
+            raise ValueError("rows with several positions have no place of their own to be turned by")
+        n, per = int(sum(streams)), (max_len + page_size - 1) // page_size
+        self.n, self.nodes, self.max_len = n, int(nodes), int(max_len)
+        kv, hd = bb.n_kv_heads or bb.n_heads, bb.d // bb.n_heads
+        shape = (len(bb.layers), n * per, kv, page_size, hd)
+        self.cache = KVCache(torch.zeros(shape, dtype=torch.bfloat16, device=device),
+                             torch.zeros(shape, dtype=torch.bfloat16, device=device))
+        i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device=device)  # noqa: E731
+        self.pages = torch.arange(n * per, dtype=torch.int32, device=device).view(n, per)
+        self.past = i32(n)
+        rows = n * self.nodes
+        cu = torch.arange(n + 1, dtype=torch.int32, device=device) * self.nodes
+        self.tree = torch.tensor(list(parents) * n, dtype=torch.int32, device=device) if parents is not None else None
+        self.batch = KVBatch(self.pages, self.past, cu, rows, self.nodes, self.tree)
+        self.embeds = torch.zeros(rows, bb.d, dtype=torch.bfloat16, device=device)
+        self.hidden = torch.zeros(rows, bb.d, dtype=torch.bfloat16, device=device)
+        self.tokens, self.greedy, self.logp = i32(rows), i32(rows), torch.zeros(rows, device=device)
+        self.path, self.n_path, self.next = i32(n, self.nodes), i32(n), i32(n)
+        self.ws = torch.empty(jn_backbone_extend_workspace_size(bb, self.cache, self.batch), dtype=torch.uint8, device=device)
+        self.picks, self.trees, self.slices, first = [], [], [], 0
+        index = torch.arange(rows, dtype=torch.int32, device=device)
+        for h, m in zip(self.heads, streams):
+            s, r = slice(first, first + m), slice(first * self.nodes, (first + m) * self.nodes)
+            self.picks.append(TokenPick(index[r], self.greedy[r], self.logp[r]))
+            self.trees.append(self._verify(s, r, cu, greedy=self.greedy[r], vocab=h.shape[0]))
+            self.slices.append((s, r))
+            first += m
+        self.cu = cu
+        self.head_ws = torch.empty(jn_tokens_decode_workspace_size(self.heads, self.picks), dtype=torch.uint8, device=device)
+        self.tree_ws = torch.empty(jn_tokens_verify_workspace_size(self.trees), dtype=torch.uint8, device=device)
+
+    def _verify(self, seqs, rows, cu, **against):
+        # (a tenant's nodes are rows of its own: its trees begin at 0)
+        at = cu[: seqs.stop - seqs.start + 1]
+        return TokenVerify(at, self.tokens[rows], self.path[seqs], self.n_path[seqs], self.next[seqs],
+                           parents=self.tree[rows] if self.tree is not None else None, **against)
+
+    def prefill(self, embeds, lengths: Sequence[int]):
+        """Appends ``lengths[i]`` rows to sequence i (``embeds``: device bf16 [sum, d], sequence after sequence); returns
+        their hidden rows."""
+        import torch
+        lengths = [int(x) for x in lengths]
+        if len(lengths) != self.n or min(lengths) < 0 or sum(lengths) != embeds.shape[0]:
+            raise ValueError("one length for every sequence, and as many rows")
+        if max(lengths) == 0:
+            return embeds
+        new = torch.tensor(lengths, dtype=torch.int32, device=embeds.device)
+        cu = torch.cat([new.new_zeros(1), new.cumsum(0, dtype=torch.int32)])
+        b = KVBatch(self.pages, self.past, cu, embeds.shape[0], max(lengths))
+        ws = torch.empty(jn_backbone_extend_workspace_size(self.model.backbone, self.cache, b), dtype=torch.uint8,
+                         device=embeds.device)
+        hidden = torch.empty_like(embeds)
+        jn_backbone_extend(self.ctx, self.model.backbone, self.cache, b, embeds, hidden, ws)
+        self.past += new
+        return hidden
+
+    def extend(self):
+        jn_backbone_extend(self.ctx, self.model.backbone, self.cache, self.batch, self.embeds, self.hidden, self.ws)
+
+    def choose(self):
+        jn_tenant_tokens_decode(self.ctx, self.hidden, self.heads, self.picks, self.head_ws)
+        jn_tenant_tokens_verify(self.ctx, self.trees, self.tree_ws)
+
+    def sample(self, p: Sequence, u, r, q: Optional[Sequence] = None):
+        """Instead of ``choose``: ``p[k]`` (and ``q[k]``, of drafts that were drawn) fp32 [tenant k's rows, vocab], numbers
+        ``u`` [rows] and ``r`` [sequences]."""
+        import torch
+        trees = [self._verify(s, rows, self.cu, p=p[k], q=q[k] if q is not None else None, u=u[rows], r=r[s])
+                 for k, (s, rows) in enumerate(self.slices)]
+        ws = torch.empty(jn_tokens_verify_workspace_size(trees), dtype=torch.uint8, device=self.tokens.device)
+        jn_tenant_tokens_verify(self.ctx, trees, ws)
+
+    def keep(self):
+        jn_kv_keep(self.ctx, self.cache, self.batch, self.path, self.n_path, self.past)
+
+    def run(self):
+        self.extend()
+        self.choose()
+        self.keep()
 
 
 class TenantOptimizer:

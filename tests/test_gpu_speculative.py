@@ -1,0 +1,286 @@
+"""The backbone over cached sequences against the same backbone over whole ones, and the calls over a cache together."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+BF16, I32 = torch.bfloat16, torch.int32
+
+
+def backbone(lib, seed, d, heads, kv, layers=2, ffn=256, theta=1e4, norm=False, causal=True, glu=True, sections=()):
+    gen = torch.Generator().manual_seed(seed)
+    hd, kvn = d // heads, kv or heads
+    w = lambda *n: (torch.randn(*n, generator=gen) / n[-1] ** 0.5).to(BF16).cuda()  # noqa: E731
+    g = lambda n: (1 + 0.1 * torch.randn(n, generator=gen)).to(BF16).cuda()  # noqa: E731
+    ls = []
+    for _ in range(layers):
+        L = dict(wqkv=w((heads + 2 * kvn) * hd, d), wo=w(d, d), w_up=w(ffn, d), w_down=w(d, ffn), g1=g(d), g2=g(d))
+        if glu:
+            L["w_gate"] = w(ffn, d)
+        if norm:
+            L["gq"], L["gk"] = g(hd), g(hd)
+        ls.append(L)
+    return lib.Backbone(ls, g(d), heads, 1e-6, kv, causal, theta, sections), gen
+
+
+def whole(lib, ctx, bb, seqs, pos=None):
+    """jn_backbone_forward of whole sequences (device bf16 [n, d] each), one list of hidden rows."""
+    lens = [x.shape[0] for x in seqs]
+    emb = torch.zeros(len(seqs), max(lens), bb.d, dtype=BF16, device="cuda")
+    for i, x in enumerate(seqs):
+        emb[i, : x.shape[0]] = x
+    reqs, ten = [lib.Request(0, emb, lens)], [lib.Tenant(1, bb.d)]
+    sz = lib.jn_pack_plan(reqs, ten, bb.d)
+    maps = torch.empty(int(sz.map_bytes), dtype=torch.uint8, device="cuda")
+    tokens, hidden = (torch.empty(sz.T, bb.d, dtype=BF16, device="cuda") for _ in range(2))
+    packed = lib.jn_pack_group(ctx, reqs, ten, bb.d, 1, maps, tokens)
+    ws = torch.empty(lib.jn_backbone_workspace_size(bb, sz.T), dtype=torch.uint8, device="cuda")
+    lib.jn_backbone_forward(ctx, bb, packed, hidden, ws, torch.cat(pos) if pos is not None else None)
+    torch.cuda.synchronize()
+    return list(hidden.float().cpu().split(lens))
+
+
+class Streams:
+    """Sequences in a cache, extended a batch at a time."""
+
+    def __init__(self, lib, bb, n, room, page=16):
+        self.lib, self.bb, self.ctx = lib, bb, lib.Context()
+        per = (room + page - 1) // page
+        hd, kv = bb.d // bb.n_heads, bb.n_kv_heads or bb.n_heads
+        mk = lambda: torch.full((len(bb.layers), n * per + 1, kv, page, hd), float("nan"), dtype=BF16, device="cuda")  # noqa: E731
+        self.cache = lib.KVCache(mk(), mk())
+        self.pages = torch.randperm(n * per + 1)[: n * per].view(n, per).to(I32).cuda()
+        self.past = torch.zeros(n, dtype=I32, device="cuda")
+
+    def extend(self, rows, parents=None, pad=0, pos=None):
+        """rows: per sequence device bf16 [n, d]; their hidden rows on the CPU."""
+        lib, bb, new = self.lib, self.bb, [r.shape[0] for r in rows]
+        x = torch.cat(rows + [torch.full((pad, bb.d), float("nan"), dtype=BF16, device="cuda")])
+        cu = torch.tensor([0] + list(np.cumsum(new)), dtype=I32).cuda()
+        up = torch.tensor(sum(parents, []) + [-1] * pad, dtype=I32).cuda() if parents is not None else None
+        b = lib.KVBatch(self.pages, self.past, cu, x.shape[0], max(1, max(new)), up, not bb.causal)
+        ws = torch.empty(lib.jn_backbone_extend_workspace_size(bb, self.cache, b, pos), dtype=torch.uint8, device="cuda")
+        ws.fill_(0xff)
+        hidden = torch.empty_like(x)
+        lib.jn_backbone_extend(self.ctx, bb, self.cache, b, x, hidden, ws, pos)
+        torch.cuda.synchronize()
+        return list(hidden[: sum(new)].float().cpu().split(new)), b
+
+
+def near(got, want, bar=2e-2):
+    """The backbone's own bar: max error over max value, of a sample."""
+    for g, w in zip(got, want):
+        if w.numel():
+            assert float((g - w).abs().max()) <= bar * float(w.abs().max())
+
+
+CASES = [dict(d=256, heads=8, kv=2, norm=True), dict(d=256, heads=4, kv=0), dict(d=512, heads=4, kv=1, glu=False),
+         dict(d=512, heads=2, kv=1, norm=True, theta=1e6), dict(d=256, heads=2, kv=2, theta=0.0)]
+
+
+@pytest.mark.parametrize("kw", CASES)
+def test_pieces_and_single_rows(lib, kw):
+    """Prompts in pieces of uneven lengths, then a row at a time, with and without rows behind the last sequence's."""
+    bb, gen = backbone(lib, 1, **kw)
+    lens = [70, 3, 150]
+    seqs = [torch.randn(n, bb.d, generator=gen).to(BF16).cuda() for n in lens]
+    want = whole(lib, lib.Context(), bb, seqs)
+    st = Streams(lib, bb, 3, 160)
+    got, at = [[] for _ in lens], [0, 0, 0]
+    for step in ([40, 0, 100], [28, 1, 47], [1, 1, 1], [1, 1, 1], [0, 0, 1]):
+        out, _ = st.extend([s[a: a + n] for s, a, n in zip(seqs, at, step)], pad=step[0] % 3)
+        for g, o in zip(got, out):
+            g.append(o)
+        at = [a + n for a, n in zip(at, step)]
+        st.past.copy_(torch.tensor(at, dtype=I32))
+    assert at == lens
+    near([torch.cat(g) for g in got], want)
+
+
+def test_a_prefix_that_sees_itself(lib):
+    """A backbone that is not causal: new rows see all of the call's and the cached ones."""
+    bb, gen = backbone(lib, 2, 256, 4, 2, causal=False)
+    seqs = [torch.randn(n, bb.d, generator=gen).to(BF16).cuda() for n in (90, 17)]
+    st = Streams(lib, bb, 2, 100)
+    got, _ = st.extend(seqs)
+    near(got, whole(lib, lib.Context(), bb, seqs))
+
+
+def test_positions_of_several_axes(lib):
+    bb, gen = backbone(lib, 3, 256, 4, 2, norm=True, sections=(16, 8, 8))
+    lens = [33, 8]
+    seqs = [torch.randn(n, bb.d, generator=gen).to(BF16).cuda() for n in lens]
+    pos = [torch.randint(0, 500, (n, 3), generator=gen, dtype=torch.int32).cuda() for n in lens]
+    want = whole(lib, lib.Context(), bb, seqs, pos)
+    st = Streams(lib, bb, 2, 40)
+    a, _ = st.extend([s[:5] for s in seqs], pos=torch.cat([p[:5] for p in pos]))
+    st.past.fill_(5)
+    b, _ = st.extend([s[5:] for s in seqs], pos=torch.cat([p[5:] for p in pos]))
+    near([torch.cat(x) for x in zip(a, b)], want)
+
+
+@pytest.mark.parametrize("kw", CASES[:3])
+def test_every_branch_of_a_tree_is_its_sequence(lib, kw):
+    """A row of a tree has the hidden state that its branch alone gives it; a kept branch goes on as if it had come so."""
+    bb, gen = backbone(lib, 4, **kw)
+    prompt = [torch.randn(n, bb.d, generator=gen).to(BF16).cuda() for n in (50, 4)]
+    up = [[-1, 0, 0, 1, 2, 2, 4, 3], [-1, 0, 1, 1, 0]]
+    nodes = [torch.randn(len(u), bb.d, generator=gen).to(BF16).cuda() for u in up]
+    tail = [torch.randn(2, bb.d, generator=gen).to(BF16).cuda() for _ in up]
+    st = Streams(lib, bb, 2, 64)
+    st.extend(prompt)
+    st.past.copy_(torch.tensor([50, 4], dtype=I32))
+    got, batch = st.extend(nodes, up)
+
+    def branch(u, j):
+        return (branch(u, u[j]) if u[j] >= 0 else []) + [j]
+
+    ctx = lib.Context()
+    for s in range(2):
+        want = whole(lib, ctx, bb, [torch.cat([prompt[s], nodes[s][branch(up[s], j)]]) for j in range(len(up[s]))])
+        near([got[s][j: j + 1] for j in range(len(up[s]))], [w[-1:] for w in want])
+    path = torch.tensor([[0, 2, 4, 6], [0, 1, 3, -1]], dtype=I32).cuda()
+    count = torch.tensor([4, 3], dtype=I32).cuda()
+    lib.jn_kv_keep(st.ctx, st.cache, batch, path, count, st.past)
+    assert st.past.tolist() == [54, 7]
+    got, _ = st.extend(tail)
+    for s, b in enumerate(([0, 2, 4, 6], [0, 1, 3])):
+        near([got[s]], [whole(lib, ctx, bb, [torch.cat([prompt[s], nodes[s][b], tail[s]])])[0][-2:]])
+
+
+def test_refusals(lib):
+    bb, gen = backbone(lib, 5, 256, 4, 2)
+    st = Streams(lib, bb, 1, 32)
+    x = torch.zeros(2, 256, dtype=BF16, device="cuda")
+    i = lambda *v: torch.tensor(v, dtype=I32).cuda()  # noqa: E731
+    whole_batch = lib.KVBatch(st.pages, st.past, i(0, 2), 2, 2, whole=True)
+    b = lib.KVBatch(st.pages, st.past, i(0, 2), 2, 2)
+    other, _ = backbone(lib, 5, 256, 4, 2, layers=3)
+    ws = torch.empty(lib.jn_backbone_extend_workspace_size(bb, st.cache, b), dtype=torch.uint8, device="cuda")
+    wide = torch.empty(ws.numel() + 256, dtype=torch.uint8, device="cuda")
+    for status, call in (("EINVAL", lambda: lib.jn_backbone_extend(st.ctx, bb, st.cache, whole_batch, x, x.clone(), ws)),
+                         ("EINCOMPAT", lambda: lib.jn_backbone_extend(st.ctx, other, st.cache, b, x, x.clone(), ws)),
+                         ("ENOSPACE", lambda: lib.jn_backbone_extend(st.ctx, bb, st.cache, b, x, x.clone(), ws[:1024])),
+                         ("EUNSUPPORTED", lambda: lib.jn_backbone_extend(st.ctx, bb, st.cache, b, x, x.clone(), wide[16:]))):
+        with pytest.raises(lib.JNError, match=status):
+            call()
+
+
+class Speaker:
+    """Two tenants' token heads over one backbone, with embeddings of their tokens, and the tokens that the backbone
+    over whole sequences writes."""
+
+    def __init__(self, lib, seed=7, vocabs=(40, 33)):
+        from paper_2607_16074_amd import step
+        self.lib, (self.bb, gen) = lib, backbone(lib, seed, 256, 8, 2, norm=True)
+        self.heads = [lib.TokenHead((2 * torch.randn(v, 256, generator=gen)).to(BF16).cuda()) for v in vocabs]
+        self.table = [torch.randn(v, 256, generator=gen).to(BF16).cuda() for v in vocabs]
+        self.model = step.Model(self.bb, [None, None], [{}, {}], 1, token_heads=self.heads)
+        self.ctx = lib.Context()
+
+    def logits(self, tenant, rows):
+        """Behind the last row."""
+        h = whole(self.lib, self.ctx, self.bb, [rows])[0][-1].cuda()
+        return h.double() @ self.heads[tenant].W.double().T
+
+    def sure(self, z):
+        """Whether the likeliest token is ahead by more than the backbone's bar (2e-2 of a feature's largest value, over 256
+        features of deviation 2) makes two runs differ, with room."""
+        a, b = z.topk(2)[0].tolist()
+        return a - b > 4.0
+
+
+@pytest.mark.parametrize("parents", [None, [-1, 0, 0, 1, 1, 2]])
+@pytest.mark.parametrize("captured", [False, True])
+def test_speculative_steps_write_the_backbones_tokens(lib, parents, captured):
+    from paper_2607_16074_amd import step
+    sp = Speaker(lib)
+    gen = torch.Generator().manual_seed(9)
+    streams, nodes = [2, 1], len(parents) if parents else 4
+    side = torch.cuda.Stream()
+    ctx = lib.Context(side)
+    with torch.cuda.stream(side):
+        st = step.SpeculativeStep(sp.model, [0, 1], streams, 128, nodes, parents, 16, ctx)
+        tenant = [0, 0, 1]
+        lens = [30, 5, 17]
+        seqs = [torch.randn(n, 256, generator=gen).to(BF16).cuda() for n in lens]
+        st.prefill(torch.cat([s[:-1] for s in seqs]), [n - 1 for n in lens])
+        side.synchronize()
+        graph = None
+        if captured:
+            past = st.past.clone()
+            st.run()  # (everything is loaded before a capture)
+            st.past.copy_(past)
+            side.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                st.run()
+        last = [s[-1] for s in seqs]  # the standing token that is not in the cache yet
+        seqs = [s[:-1] for s in seqs]
+        checked = 0
+        for turn in range(3):
+            tokens = torch.randint(0, 33, (3, nodes), generator=gen)
+            emb = torch.zeros(3, nodes, 256, dtype=BF16, device="cuda")
+            for i in range(3):
+                # the first child of the root is right in two turns of three, and the chain behind it in one
+                z = sp.logits(tenant[i], torch.cat([seqs[i], last[i][None]]))
+                if turn < 2:
+                    tokens[i, 1] = int(z.argmax())
+                if turn == 0 and parents is None:
+                    z = sp.logits(tenant[i], torch.cat([seqs[i], last[i][None], sp.table[tenant[i]][tokens[i, 1]][None]]))
+                    tokens[i, 2] = int(z.argmax())
+                emb[i, 0] = last[i]
+                emb[i, 1:] = sp.table[tenant[i]][tokens[i, 1:].cuda()]
+            st.embeds.copy_(emb.view(-1, 256))
+            st.tokens.copy_(tokens.view(-1).to(I32))
+            before = st.past.tolist()
+            graph.replay() if graph else st.run()
+            side.synchronize()
+            up = parents or list(range(-1, nodes - 1))
+            for i in range(3):
+                c = st.n_path.tolist()[i]
+                path = st.path.tolist()[i][:c]
+                assert path[0] == 0 and all(up[b] == a for a, b in zip(path, path[1:]))
+                assert st.past.tolist()[i] == before[i] + c
+                # every standing draft, and the token behind them, is what the backbone over the whole sequence writes
+                rows = torch.cat([seqs[i], last[i][None]])
+                for k in range(c):
+                    z = sp.logits(tenant[i], rows)
+                    token = int(tokens[i, path[k + 1]]) if k + 1 < c else int(st.next[i])
+                    if sp.sure(z):
+                        assert token == int(z.argmax())
+                        checked += 1
+                    rows = torch.cat([rows, sp.table[tenant[i]][token][None]])
+                kids = [j for j in range(1, nodes) if up[j] == path[-1]]
+                assert all(int(tokens[i, j]) != int(st.next[i]) for j in kids)
+                seqs[i], last[i] = rows[:-1], rows[-1]
+        assert checked >= 6
+
+
+def test_sampled_steps_follow_their_probabilities(lib):
+    """Drawn drafts against the probabilities of the caller's: as verification by itself says, and the cache goes on from there."""
+    import kv_plain as plain
+    from paper_2607_16074_amd import step
+    sp = Speaker(lib, 11)
+    gen = torch.Generator().manual_seed(3)
+    parents = [-1, 0, 0, 1, 2]
+    st = step.SpeculativeStep(sp.model, [0, 1], [1, 2], 64, 5, parents, 16)
+    st.prefill(torch.randn(9, 256, generator=gen).to(BF16).cuda(), [4, 0, 5])
+    st.embeds.copy_(torch.randn(15, 256, generator=gen).to(BF16))
+    rows = [5, 10]
+    q = [torch.softmax(torch.randn(n, h.shape[0], generator=gen), 1) for n, h in zip(rows, sp.heads)]
+    p = [torch.softmax(2 * torch.randn(n, h.shape[0], generator=gen), 1) for n, h in zip(rows, sp.heads)]
+    u, r = torch.rand(15, generator=gen), torch.rand(3, generator=gen)
+    st.tokens.copy_(torch.randint(0, 33, (15,), generator=gen))
+    st.extend()
+    st.sample([x.cuda() for x in p], u.cuda(), r.cuda(), [x.cuda() for x in q])
+    st.keep()
+    got = [x[:c] for x, c in zip(st.path.tolist(), st.n_path.tolist())]
+    want, first = [], 0
+    for k, (t0, trees) in enumerate(((0, 1), (1, 2))):
+        n = 5 * trees
+        w = plain.verify([5 * i for i in range(trees + 1)], st.tokens.cpu()[5 * t0: 5 * t0 + n], torch.tensor(parents * trees), p[k],
+                         q[k], None, u[5 * t0: 5 * t0 + n], r[t0: t0 + trees], sp.heads[k].shape[0], 5, n)
+        want += list(zip(w[0], w[1]))
+    assert [(g, x) for g, x in zip(got, st.next.tolist())] == want
+    assert st.past.tolist() == [4 + len(got[0]), len(got[1]), 5 + len(got[2])]
