@@ -932,6 +932,12 @@ __device__ __forceinline__ void kv_wait_vmcnt() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// 16 bytes a lane from `src` to 1 KB of LDS at `dst` (the same for all lanes), which only
+// this wavefront reads: it waits by kv_wait_vmcnt, and no barrier stands between.
+__device__ __forceinline__ void kv_dma(const uint16_t* src, uint16_t* dst) {
+  __builtin_amdgcn_global_load_lds(JN_GPTR(src), JN_LPTR(dst), 16, 0, 0);
+}
+
 // Four (two) V^T fragments of 16 columns x 32 keys of a V tile: rows a and a + 16 of
 // two transposed reads each, at LDS byte addresses at[t] + off. The wait stands in the
 // same statement: a read in flight never outlives it (and the compiler's own form would
@@ -1184,8 +1190,7 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void kv_few_kernel(KvCache 
       for (int e = 0; e < 2; ++e)
 #pragma unroll
         for (int v = 0; v < 16 / RPI; ++v)
-          __builtin_amdgcn_global_load_lds(JN_GPTR(c.v + x.at[e] + doff[v]),
-                                           JN_LPTR(&vt[wave][stage][e * 16 * HD + v * 512]), 16, 0, 0);
+          kv_dma(c.v + x.at[e] + doff[v], &vt[wave][stage][e * 16 * HD + v * 512]);
     };
     bf16x8 kf[2][NC];
     auto fetch_k = [&](const Pages& x) __attribute__((always_inline)) {
