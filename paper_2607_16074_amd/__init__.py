@@ -419,8 +419,7 @@ class KVCache:
         self.k, self.v = k, v
         s = jn_kv_cache()
         s.n_layers, s.n_pages, s.page_size, s.n_kv_heads, s.head_dim = layers, pages, size, kv, hd
-        # (of one page or layer any distance: nothing is that far away)
-        s.ld_page = ld_page if pages > 1 else max(ld_page, kv * size * hd)
+        s.ld_page = ld_page if pages > 1 else kv * size * hd  # (of one page any distance: nothing is that far away)
         s.ld_layer = ld_layer
         s.k, s.v = k.data_ptr(), v.data_ptr()
         self.struct = s

@@ -838,6 +838,7 @@ struct KvWalk {
     group = G;
     int64_t all = 0, mine = 0;
     KvSeq q{};
+#pragma unroll 4
     for (int32_t s0 = 0; s0 < b.n_seqs; s0 += 64) {
       if (s0 + lane < b.n_seqs) q = kv_seq(b, s0 + lane);
       mine = of_seq(b, q, G, s0 + lane);
@@ -1287,7 +1288,8 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void kv_few_kernel(KvCache 
       else
         kv_wait_vmcnt<0>();
       if (hole || mask) {
-        // rows of the tile that nobody sees become zeros, and values that are not finite
+        // rows of the tile that nobody sees become zeros, and, where not every query row sees
+        // all of it, values that are not finite
         const int l = here(lane);
         const int32_t r = l >> 1;
         const bool none = (r < 16 ? use.page[0] : use.page[1]) < 0 || t + r >= kend;
@@ -1296,7 +1298,7 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void kv_few_kernel(KvCache 
 #pragma unroll 1
         for (int e = 0; e < HD / 2; e += 8) {
           u32x4 v = *reinterpret_cast<const u32x4*>(row + e);
-          bad |= kv_finite(v);
+          if (mask) bad |= kv_finite(v);
           *reinterpret_cast<u32x4*>(row + e) = none ? u32x4{0, 0, 0, 0} : v;
         }
         odd |= __any(bad && !none);
@@ -1315,8 +1317,9 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void kv_few_kernel(KvCache 
       use = next;
     }
     if (odd)
-      for (int32_t i = max(0, (sq.past - 31 - wave * 32) / KT - ta); i < steps; ++i) {
+      for (int32_t i = 0; i < steps; ++i) {
         const int32_t t = (ta + i) * KT + wave * 32;
+        if (t + 32 <= sq.past) continue;  // (as they are in the product: every row sees them)
         kv_add_odd<HD, NB>(b, c, pages, run.h, t, min(t + 32, kend), qf, m_run, a.scale_log2, o, here(lane), [&](int nb, int32_t x) {
           const int32_t j = (nb * 16 + (here(lane) & 15)) / G, k = x - sq.past;
           if (k < 0 || b.whole) return true;
@@ -1501,7 +1504,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b
         for (int k = 0; k < NL; ++k) {
           const int row = k * RPL + lrow;
           const bool none = !((has >> (row >> 4)) & 1) || t + row >= kend;
-          const bool bad = kv_finite(vr[k]);
+          const bool bad = mask && kv_finite(vr[k]);
           odd |= bad && !none;
           if (none) vr[k] = u32x4{0, 0, 0, 0};
         }

@@ -163,6 +163,21 @@ def test_what_a_row_does_not_see_leaves_it_alone(lib, margin, heads, kv, hd, new
         assert bool(torch.isnan(last).all() if s == 0 else (last == float("inf")).all())
 
 
+@pytest.mark.parametrize("heads,kv,new", [(4, 1, 2), (4, 1, 40)])
+def test_values_that_all_rows_see_stay_what_they_are(lib, heads, kv, new):
+    """An infinity among the cached rows reaches every row, also beside a page that is none."""
+    b, k, v, gen = make(12, kv, 64, 16, [100], [new], bad=[(0, 2, -1)], pad=0)
+    g, r = plain.place(b, k.shape[1], 0, 50)  # (the bad page holds places 32 .. 47)
+    v[0][g, :, r, 3], v[0][g, :, r, 40] = float("inf"), -float("inf")
+    q = torch.randn(b["rows"], heads * 64, generator=gen).to(BF16)
+    got = attend(lib, b, k, v, q, heads).double().view(new, heads, 64)
+    want, tol = plain.attention(b, k[0], v[0], q, heads, torch.full((new, heads * 64), float("nan")))
+    want, tol = want.view(got.shape), tol.view(got.shape)
+    assert bool((got[..., 3] == float("inf")).all() and (got[..., 40] == -float("inf")).all())
+    rest = [i for i in range(64) if i not in (3, 40)]
+    assert bool(((got - want).abs()[..., rest] <= tol[..., rest]).all())
+
+
 def test_infinite_keys(lib):
     """A key of +inf where the query is positive: NaN, as a softmax of an infinite score is; a key of -inf is nothing."""
     b, k, v, gen = make(6, 1, 64, 16, [40], [1], pad=0)
