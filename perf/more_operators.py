@@ -406,11 +406,12 @@ def _call(s: dict):
     if c["kind"] == "append":
         qk = jn.QKNormRope(c["heads"], c["kv"], c["hd"], EPS, s["gq"], s["gk"], c["theta"],
                            _sections(c) if s["pos"] is not None else ())
-        pos = s["pos"][:rows] if s["pos"] is not None else None
-        return (lambda: jn.jn_kv_append(ctx, cache, 0, batch, qk, s["x"][:rows], pos, s["q"][:rows]),
+        x, q, pos = s["x"][:rows], s["q"][:rows], s["pos"][:rows] if s["pos"] is not None else None
+        return (lambda: jn.jn_kv_append(ctx, cache, 0, batch, qk, x, pos, q),
                 {"q": s["q"], "k": s["k"], "v": s["v"]})
     ws = torch.empty(jn.jn_kv_attention_workspace_size(cache, batch, c["heads"]), dtype=torch.uint8, device=DEV)
-    return lambda: jn.jn_kv_attention(ctx, cache, 0, batch, c["heads"], s["q"][:rows], s["out"][:rows], ws), s["out"]
+    q, out = s["q"][:rows], s["out"][:rows]
+    return lambda: jn.jn_kv_attention(ctx, cache, 0, batch, c["heads"], q, out, ws), s["out"]
 
 
 _contexts: dict = {}
