@@ -1414,6 +1414,9 @@ hipError_t launch_small_pick(hipStream_t s, const TokSmallSet& all, int32_t ldz,
 // fetched together, then the walk is a wavefront's, a child after the other.
 // All sums are formed in 64 bits: a border between two tokens lies where the
 // definition has it, whatever order the terms are added in.
+// Bound by latency: a chain over 32,003 tokens 5.7 + 5.0 us, 64 trees of 25 picked drafts
+// 13.3 (their scattered entries) + 7.6, 16 trees of 9 drawn ones over 160,001 five launches of
+// 3.5 to 10 and 7.6. (One workgroup a tree for everything took 78, 75 and 439.)
 constexpr int kSumThreads = 256, kPickThreads = 1024;
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 
