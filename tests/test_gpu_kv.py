@@ -210,6 +210,60 @@ def test_equal_scores_give_the_mean(lib):
     assert bool((got == 0.5).all())
 
 
+def test_sequences_that_share_pages(lib, margin):
+    """A common prompt is read by all of its sequences from the same pages."""
+    b, k, v, gen = make(13, 2, 64, 32, [64, 64, 90], [5, 1, 40])
+    b["pages"][1, :2] = b["pages"][0, :2]
+    b["pages"][2, :2] = b["pages"][0, :2]
+    attention_case(lib, margin, b, k, v, gen, 8)
+
+
+def test_many_sequences(lib, margin):
+    """More than a search's 64, uneven, some of them empty."""
+    past, new = [(37 * i) % 200 for i in range(150)], [(i % 4 != 1) * (1 + i % 3) for i in range(150)]
+    b, k, v, gen = make(14, 1, 32, 16, past, new)
+    attention_case(lib, margin, b, k, v, gen, 4)
+    b, k, v, gen = make(15, 1, 32, 16, past[:80], [i % 40 for i in range(80)])
+    attention_case(lib, margin, b, k, v, gen, 4)
+
+
+def test_calls_of_nothing(lib):
+    b, k, v, gen = make(16, 2, 64, 16, [5], [2], pad=0)
+    ctx, cache = lib.Context(), lib.KVCache(k.cuda(), v.cuda())
+    i = lambda *n: torch.zeros(n, dtype=I32, device="cuda")  # noqa: E731
+    for bt in (lib.KVBatch(i(0, 3), i(0), i(1), 4, 1), lib.KVBatch(i(2, 3), i(2), i(3), 0, 1)):
+        rows = bt.struct.rows
+        x, q, out = (torch.ones(rows, w, dtype=BF16, device="cuda") for w in (512, 256, 256))
+        assert lib.jn_kv_attention_workspace_size(cache, bt, 4) == 0
+        lib.jn_kv_append(ctx, cache, 0, bt, lib.QKNormRope(4, 2, 64, theta=1e4), x, None, q)
+        lib.jn_kv_attention(ctx, cache, 0, bt, 4, q, out, None)
+        lib.jn_kv_keep(ctx, cache, bt, i(bt.struct.n_seqs, 2), i(bt.struct.n_seqs))
+        torch.cuda.synchronize()
+        assert bool((out == 1).all() and (q == 1).all())
+    # a batch whose sequences have no rows
+    bt = lib.KVBatch(i(2, 3), i(2), i(3), 4, 2)
+    q, out = (torch.ones(4, 256, dtype=BF16, device="cuda") for _ in range(2))
+    ws = torch.empty(lib.jn_kv_attention_workspace_size(cache, bt, 4), dtype=torch.uint8, device="cuda").fill_(0xff)
+    lib.jn_kv_attention(ctx, cache, 0, bt, 4, q, out, ws)
+    torch.cuda.synchronize()
+    assert bool((out == 1).all()) and torch.equal(cache.k.cpu(), k)
+
+
+def test_the_launch_trace_names_the_calls(lib):
+    b, k, v, gen = make(17, 2, 64, 16, [5], [2], pad=0)
+    ctx, cache, bt = lib.Context(), lib.KVCache(k.cuda(), v.cuda()), batch(lib, b)
+    x = torch.randn(2, 8 * 64, generator=gen).to(BF16).cuda()
+    q, out = (torch.zeros(2, 4 * 64, dtype=BF16, device="cuda") for _ in range(2))
+    ws = torch.empty(lib.jn_kv_attention_workspace_size(cache, bt, 4), dtype=torch.uint8, device="cuda")
+    ctx.set_trace(True)
+    lib.jn_kv_append(ctx, cache, 0, bt, lib.QKNormRope(4, 2, 64, theta=1e4), x, None, q)
+    lib.jn_kv_attention(ctx, cache, 0, bt, 4, q, out, ws)
+    lib.jn_kv_keep(ctx, cache, bt, torch.zeros(1, 1, dtype=I32, device="cuda"), torch.ones(1, dtype=I32, device="cuda"))
+    got = ctx.trace_read()
+    assert [(e[0], e[1], e[2]) for e in got] == [("kv_append", 2, 512), ("kv_attention", 2, 256), ("kv_keep", 1, 128)]
+    assert all(0 < e[4] < 1000 for e in got)
+
+
 def test_strided_rows_cache_and_layers(lib, margin):
     """Rows inside wider ones, layers of a page together, the second layer."""
     heads, kv, hd = 4, 2, 64
