@@ -393,7 +393,8 @@ jn_status jn_kv_append(jn_ctx* ctx, const jn_kv_cache* cache, int32_t layer, con
 
 typedef struct jn_kv_attn {
   int32_t n_heads;         /* a multiple of the cache's n_kv_heads: query head h reads
-                              key head h / (n_heads / n_kv_heads)                   */
+                              key head h / (n_heads / n_kv_heads); at most 2^26 query rows of a
+                              key head, max_new (or rows) times that (JN_ESHAPE)    */
   float scale;             /* of the scores, finite and >= 0; 0: 1 / sqrt(head_dim) */
   int64_t ld_q, ld_out;    /* elements between rows, multiples of 8 (JN_EUNSUPPORTED) */
 } jn_kv_attn;

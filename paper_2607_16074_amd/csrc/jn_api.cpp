@@ -1036,10 +1036,11 @@ jn_status kv_attn(jn_ctx* c, const KvCache& k, const KvBatch& b, const jn_kv_att
   if (a->ld_q < width || a->ld_out < width) return fail(c, JN_EINVAL, "rows hold no %lld elements", (long long)width);
   if ((a->ld_q | a->ld_out) % 8 != 0) return fail(c, JN_EUNSUPPORTED, "row strides not multiples of 8");
   if (!(a->scale >= 0.f) || std::isinf(a->scale)) return fail(c, JN_EINVAL, "scale must be finite and >= 0");
-  // query tiles of a launch, for the smallest tile (16 rows)
-  const int64_t tiles = ((int64_t)std::min(b.max_new, std::max(b.rows, 1)) * (a->n_heads / k.kv) + 15) / 16;
-  if (tiles * k.kv * std::max(b.n_seqs, 1) > kMostBlocks)
-    return fail(c, JN_ESHAPE, "%d sequences of %d new rows exceed one launch's grid", b.n_seqs, b.max_new);
+  // query rows of a key head, and key tiles of all units, in the kernels' integers
+  const int64_t rows = (int64_t)std::min(b.max_new, std::max(b.rows, 1)) * (a->n_heads / k.kv);
+  const int64_t units = (rows + 15) / 16 * k.kv * std::max(b.n_seqs, 1);
+  if (rows > 1 << 26 || units > (1ll << 53) / (b.places / 64 + 1))
+    return fail(c, JN_ESHAPE, "%d sequences of %d new rows, %d heads", b.n_seqs, b.max_new, a->n_heads);
   *out = KvAttn{};
   out->ldq = a->ld_q;
   out->ldo = a->ld_out;

@@ -821,15 +821,40 @@ struct KvWalk {
     return min(q.past + n, b.places);
   }
   static __device__ __forceinline__ int32_t tiles_of(int32_t keys) { return (keys + KT - 1) / KT; }
+  // Tiles of the first k <= row_tiles row tiles of a key head. A chain's row tile i has
+  // min(floor((R i + B) / (KT G)), C) tiles, B = R - 1 + G (past + KT), C those of its last
+  // row: those below C are summed as the steps of the Euclidean algorithm (count, modulus,
+  // slope and offset below), the rest are C each. All in 32 bits but the sum: G n <= 2^26,
+  // and past is taken modulo KT. (Row tile after row tile instead, the search made two
+  // pieces of 2,048 rows take 329 us, with this 313.)
+  static __device__ __forceinline__ int64_t upto(const KvBatch& b, const KvSeq& q, int32_t G, int32_t k) {
+    const int32_t last = tiles_of(min(q.past + q.n, b.places));
+    if constexpr (R == 0) return (int64_t)k * last;
+    if (b.whole || b.parents || k <= 1) {
+      return (int64_t)k * tiles_of(keys(b, q, G, 0));
+    } else {
+      const int32_t x = q.past / KT, y = q.past % KT, rise = G * KT * (last - x - 1) - G * y - (R - 1);
+      const int32_t below = rise <= 0 ? 0 : min(k, (rise + R - 1) / R);
+      int64_t sum = (int64_t)(k - below) * last + (int64_t)below * (x + 1);
+      uint32_t t = below, m = KT * G, a = R, o = R - 1 + G * y;
+      while (true) {
+        const uint32_t qa = a / m, qo = o / m;
+        sum += (int64_t)t * (t - 1) / 2 * qa + (int64_t)t * qo;
+        a -= qa * m;
+        o -= qo * m;
+        const uint32_t top = a * t + o;
+        if (top < m) return sum;
+        t = top / m;
+        o = top - t * m;
+        const uint32_t was = m;
+        m = a;
+        a = was;
+      }
+    }
+  }
   // Tiles of a key head of sequence s, which is q.
   static __device__ __forceinline__ int64_t of_seq(const KvBatch& b, const KvSeq& q, int32_t G, int32_t s) {
-    if (s >= b.n_seqs) return 0;
-    const int32_t nq = row_tiles(q, G);
-    if (nq == 0) return 0;
-    if (R == 0 || b.whole || b.parents) return (int64_t)nq * tiles_of(keys(b, q, G, 0));
-    int64_t sum = 0;
-    for (int32_t i = 0; i < nq; ++i) sum += tiles_of(keys(b, q, G, i));
-    return sum;
+    return s < b.n_seqs ? upto(b, q, G, row_tiles(q, G)) : 0;
   }
 
   // At most `most` workgroups, of `least` tiles each where there are so many. Runs that
@@ -879,19 +904,17 @@ struct KvWalk {
     rest -= h * mine;
     unit0 = wave_same64(pos - rest);
     if constexpr (R != 0) {
-      const int32_t nq = row_tiles(sq, G);
-      for (int32_t q0 = 0;; q0 += 64) {
-        const int64_t t = q0 + lane < nq ? tiles_of(keys(b, sq, G, q0 + lane)) : 0;
-        const int64_t up = wave_scan64(t, lane);
-        const int32_t c = __builtin_popcountll(__ballot(up <= rest));
-        if (c < 64) {
-          qt = wave_same(q0 + c);
-          unit0 += wave_get64(up - t, c);
-          break;
-        }
-        unit0 += wave_get64(up, 63);
-        rest -= wave_get64(up, 63);
+      // the last row tile that begins at or before `rest`, 64 of them at a time
+      int32_t len = row_tiles(sq, G);
+      while (len > 0) {
+        const int32_t stride = (len + 63) >> 6, k = (lane + 1) * stride;
+        const bool before = k <= len && upto(b, sq, G, qt + k) <= rest;
+        const int32_t c = __builtin_popcountll(__ballot(before)) * stride;
+        qt += c;
+        len = min(len - c, stride - 1);
       }
+      qt = wave_same(qt);
+      unit0 += wave_same64(upto(b, sq, G, qt));
       unit(b);
     }
     return true;
@@ -1407,8 +1430,8 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void kv_few_kernel(KvCache 
 // 32 rows a wavefront (head width 256: 16, whose registers leave two wavefronts a SIMD;
 // 32 there took twice as long), 128 rows a workgroup, which halves the LDS reads of a
 // product against 16 rows; 64 rows where a unit has no more. Two pieces of 2,048 rows behind 6,001, 16
-// query heads of 128: 327 us with the join, 0.56 PFLOP/s, the matrix cores 28 % busy beside
-// 350 vector instructions a tile and wavefront; 61 rows over 131,070 of 8 heads: 106 us, 5.1 TB/s.
+// query heads of 128: 313 us with the join, 0.59 PFLOP/s, the matrix cores 30 % busy beside
+// 200 other vector instructions a tile and wavefront; 61 rows over 131,070 of 8 heads: 106 us, 5.1 TB/s.
 template <int HD, int NB, int W>
 __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b, KvAttn a, KvWork wk) {
   constexpr int R = 16 * NB * W, KT = 64, THREADS = 64 * W;

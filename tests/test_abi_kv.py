@@ -72,6 +72,13 @@ def test_refusals_before_anything_runs(lib):
     refused(lib, "JN_ESHAPE", set_(max_new=1 << 22, rows=1 << 22, n_seqs=60000), heads=64)
 
 
+def test_sizes_beyond_a_batch_are_taken(lib):
+    """What a batch may hold at most: 256 sequences in buffers for 75,529 rows, each allowed all of them."""
+    cache, b = parts(lib, kv=4, seqs=256, rows=75529, new=75529)
+    assert 0 < lib.jn_kv_attention_workspace_size(cache, b, 16) < 1 << 28
+    refused(lib, "JN_ESHAPE", lambda c, x: setattr(x, "max_new", x.rows), heads=4096, kv=2, rows=(1 << 15) + 1)
+
+
 def test_the_cache_and_batch_binding_checks_types(lib):
     k = torch.zeros(1, 4, 2, 16, 64, dtype=BF16)
     for bad in ((k.float(), k.float()), (k, k[:, :3]), (k[0], k[0]), (k[..., ::2], k[..., ::2]), (k, k.transpose(2, 3).contiguous().transpose(2, 3))):

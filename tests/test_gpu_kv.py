@@ -227,6 +227,22 @@ def test_many_sequences(lib, margin):
     attention_case(lib, margin, b, k, v, gen, 4)
 
 
+@pytest.mark.parametrize("heads,kv", [(2, 2), (6, 2), (5, 1), (14, 2), (32, 1)])
+@pytest.mark.parametrize("cut", [0, 9])
+def test_long_pieces_of_odd_head_groups(lib, margin, heads, kv, cut):
+    """Chains of many row tiles, with `cut` pages too few for the last rows: the tiles of a run are counted by a formula."""
+    b, k, v, gen = make(heads, kv, 32, 16, [700, 61, 0, 5], [601, 1, 333, 1240], "chain")
+    b["pages"] = b["pages"][:, : b["pages"].shape[1] - cut].contiguous()
+    attention_case(lib, margin, b, k, v, gen, heads)
+
+
+def test_sizes_far_beyond_what_a_batch_holds(lib, margin):
+    """A program's buffers and max_new are made for its largest call."""
+    b, k, v, gen = make(3, 2, 32, 16, [s % 40 for s in range(300)], [1 + s % 3 for s in range(300)], "chain", pad=70000,
+                        max_new=70000)
+    attention_case(lib, margin, b, k, v, gen, 16)
+
+
 def test_calls_of_nothing(lib):
     b, k, v, gen = make(16, 2, 64, 16, [5], [2], pad=0)
     ctx, cache = lib.Context(), lib.KVCache(k.cuda(), v.cuda())
