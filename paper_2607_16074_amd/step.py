@@ -377,6 +377,7 @@ class SpeculativeStep:
         self.cu = cu
         self.head_ws = torch.empty(jn_tokens_decode_workspace_size(self.heads, self.picks), dtype=torch.uint8, device=device)
         self.tree_ws = torch.empty(jn_tokens_verify_workspace_size(self.trees), dtype=torch.uint8, device=device)
+        self.ctx.stream.wait_stream(torch.cuda.current_stream())  # (the buffers are filled there)
 
     def _verify(self, seqs, rows, cu, **against):
         # (a tenant's nodes are rows of its own: its trees begin at 0)
@@ -386,13 +387,25 @@ class SpeculativeStep:
 
     def prefill(self, embeds, lengths: Sequence[int]):
         """Appends ``lengths[i]`` rows to sequence i (``embeds``: device bf16 [sum, d], sequence after sequence); returns
-        their hidden rows."""
+        their hidden rows.  Follows the current stream, and is followed by it, where the context's is another."""
         import torch
         lengths = [int(x) for x in lengths]
         if len(lengths) != self.n or min(lengths) < 0 or sum(lengths) != embeds.shape[0]:
             raise ValueError("one length for every sequence, and as many rows")
+        if max(lengths) > self.max_len:
+            raise ValueError(f"{max(lengths)} rows of a sequence with room for {self.max_len}")
         if max(lengths) == 0:
             return embeds
+        here = torch.cuda.current_stream(embeds.device)
+        self.ctx.stream.wait_stream(here)
+        with torch.cuda.stream(self.ctx.stream):
+            hidden = self._prefill(embeds, lengths)
+        here.wait_stream(self.ctx.stream)
+        hidden.record_stream(here)
+        return hidden
+
+    def _prefill(self, embeds, lengths):
+        import torch
         new = torch.tensor(lengths, dtype=torch.int32, device=embeds.device)
         cu = torch.cat([new.new_zeros(1), new.cumsum(0, dtype=torch.int32)])
         b = KVBatch(self.pages, self.past, cu, embeds.shape[0], max(lengths))
@@ -416,7 +429,8 @@ class SpeculativeStep:
         import torch
         trees = [self._verify(s, rows, self.cu, p=p[k], q=q[k] if q is not None else None, u=u[rows], r=r[s])
                  for k, (s, rows) in enumerate(self.slices)]
-        ws = torch.empty(jn_tokens_verify_workspace_size(trees), dtype=torch.uint8, device=self.tokens.device)
+        with torch.cuda.stream(self.ctx.stream):  # whose memory it is: the next call may have it again
+            ws = torch.empty(jn_tokens_verify_workspace_size(trees), dtype=torch.uint8, device=self.tokens.device)
         jn_tenant_tokens_verify(self.ctx, trees, ws)
 
     def keep(self):

@@ -284,3 +284,29 @@ def test_sampled_steps_follow_their_probabilities(lib):
         want += list(zip(w[0], w[1]))
     assert [(g, x) for g, x in zip(got, st.next.tolist())] == want
     assert st.past.tolist() == [4 + len(got[0]), len(got[1]), 5 + len(got[2])]
+
+
+def test_prompts_from_another_stream_than_the_contexts(lib):
+    """A prompt's length reaches the cache's lengths behind its rows, though the context's stream is far behind."""
+    from paper_2607_16074_amd import step
+    sp = Speaker(lib)
+    gen = torch.Generator().manual_seed(12)
+    x = torch.randn(21, 256, generator=gen).to(BF16).cuda()
+    hidden, caches = [], []
+    for ctx in (sp.ctx, lib.Context(torch.cuda.Stream())):
+        st = step.SpeculativeStep(sp.model, [0], [1], 48, 1, page_size=16, ctx=ctx)
+        if ctx is not sp.ctx:
+            ctx.stream.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(ctx.stream):
+                busy = torch.zeros(4096, 4096, device="cuda")
+                for _ in range(50):
+                    busy = busy @ busy
+        parts = [st.prefill(x[:9].clone(), [9]), st.prefill(x[9:].clone(), [12])]
+        hidden.append(torch.cat(parts))
+        torch.cuda.synchronize()
+        assert st.past.tolist() == [21]
+        caches.append((st.cache.k.clone(), st.cache.v.clone()))
+    assert torch.equal(hidden[0], hidden[1])
+    assert all(torch.equal(a, b) for a, b in zip(*caches))
+    with pytest.raises(ValueError, match="room"):
+        st.prefill(torch.zeros(49, 256, dtype=BF16, device="cuda"), [49])
