@@ -415,8 +415,9 @@ jn_status jn_kv_attention(jn_ctx* ctx, const jn_kv_cache* cache, int32_t layer, 
 /* Keeps a branch of every sequence's new rows, in all layers: keys and values of new
  * row path[s][k] move to place past[s] + k for k < n_path[s] (n_path taken within [0,
  * max_path]), and past_out[s] = past[s] + n_path[s] (past_out may be past, or NULL).
- * max_path: 1 .. 2^26 (JN_ESHAPE).  A path ascends, path[s][k] >= k, as those of jn_tenant_tokens_verify do; an entry outside
- * k .. max_new - 1, or below an earlier one, moves nothing. */
+ * max_path: 1 .. 2^26 (JN_ESHAPE).  A path ascends, path[s][k] >= k, as those of
+ * jn_tenant_tokens_verify do; an entry outside k .. max_new - 1, or below an earlier one,
+ * moves nothing. */
 jn_status jn_kv_keep(jn_ctx* ctx, const jn_kv_cache* cache, const jn_kv_batch* b, const int32_t* path, int32_t max_path,
                      const int32_t* n_path, int32_t* past_out);
 

@@ -667,11 +667,10 @@ hipError_t launch_qk_bwd(hipStream_t s, const QkShape& a, const uint16_t* x, con
 
 // ----------------------------------- keys and values to a paged cache ---
 // The rows of qk_fwd_kernel with value heads behind their keys (same steps, same
-// arithmetic): queries go
-// to rows of y, keys and values to their places.  A wavefront finds its row's sequence
-// and page once, from all lanes (kv_find).  pos null: the place, of a tree's row
-// past + the depth of its branch.  Bound by HBM: 40,726 rows of 20 heads of 128 take 66
-// us, 6.3 TB/s; 8 rows 4.7, a chain of loads (lengths, page, row, gains).
+// arithmetic): queries go to rows of y, keys and values to their places.  A wavefront
+// finds its row's sequence and page once, from all lanes (kv_find).  pos null: the place,
+// of a tree's row past + the depth of its branch.  Bound by HBM: 40,726 rows of 20 heads
+// of 128 take 66 us, 6.3 TB/s; 8 rows 4.7, a chain of loads (lengths, page, row, gains).
 template <int E, int P2, bool NORM, bool ROPE, bool ONCE>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvBatch b, QkShape a, const uint16_t* x, uint16_t* y,
                                                         int32_t parts) {

@@ -32,7 +32,8 @@ import numpy as np
 from . import (EXPERT_LAYER_FIELDS, AdamWTenant, Backbone, Context, Expert, ExpertIO, Head, HeadIO, InferPlan, KVBatch,
                KVCache, Request, Tenant, TokenHead, TokenIO, TokenPick, TokenVerify, jn_adamw_workspace_size,
                jn_infer_workspace_size, jn_backbone_extend, jn_backbone_extend_workspace_size, jn_kv_keep,
-               jn_tenant_tokens_verify, jn_tokens_verify_workspace_size, jn_backbone_forward, jn_backbone_workspace_size, jn_experts_workspace_size, jn_heads_workspace_size,
+               jn_tenant_tokens_verify, jn_tokens_verify_workspace_size, jn_backbone_forward, jn_backbone_workspace_size,
+               jn_experts_workspace_size, jn_heads_workspace_size,
                jn_pack_group, jn_pack_maps_host, jn_pack_plan, jn_pack_tenant_sizes, jn_tenant_adamw_step,
                jn_tenant_experts_fwd_bwd, jn_tenant_heads_fwd_bwd, jn_tenant_tokens_decode, jn_tenant_tokens_fwd_bwd,
                jn_tokens_decode_workspace_size, jn_tokens_workspace_size, jn_unpack)
