@@ -333,7 +333,11 @@ class SpeculativeStep:
     and ``tokens`` [sequences * nodes] hold the rows and what they stand for; after it ``path`` and ``n_path`` hold the
     standing rows of every sequence, ``next`` the token behind them, ``past`` the rows in its cache.  ``sample`` instead
     of ``choose`` verifies against probabilities of the caller's.  Everything is enqueued on the context's stream and
-    reads its buffers when it runs, so a run may be captured and replayed."""
+    reads its buffers when it runs, so a run may be captured and replayed.
+
+    A run takes sequences of fewer than ``max_len`` rows (all of its rows have places: the pages hold ``nodes`` - 1 more).
+    One that has ``max_len`` or more is full and stays as it is: ``n_path`` 0, ``path`` and ``next`` -1.  ``prefill`` refuses
+    rows beyond ``max_len``."""
 
     def __init__(self, model: Model, tenants: Sequence[int], streams: Sequence[int], max_len: int, nodes: int = 1,
                  parents: Optional[Sequence[int]] = None, page_size: int = 64, ctx: Optional[Context] = None, device="cuda"):
@@ -349,7 +353,8 @@ class SpeculativeStep:
             raise ValueError("tokens are written by a causal backbone")
         if bb.struct.rope_axes > 1:
             raise ValueError("rows with several positions have no place of their own to be turned by")
-        n, per = int(sum(streams)), (max_len + page_size - 1) // page_size
+        # (row j of a tree lies at place past + j, whatever its depth: a run from max_len - 1 on ends at max_len + nodes - 2)
+        n, per = int(sum(streams)), (int(max_len) + int(nodes) - 1 + page_size - 1) // page_size
         self.n, self.nodes, self.max_len = n, int(nodes), int(max_len)
         kv, hd = bb.n_kv_heads or bb.n_heads, bb.d // bb.n_heads
         shape = (len(bb.layers), n * per, kv, page_size, hd)
@@ -357,7 +362,7 @@ class SpeculativeStep:
                              torch.zeros(shape, dtype=torch.bfloat16, device=device))
         i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device=device)  # noqa: E731
         self.pages = torch.arange(n * per, dtype=torch.int32, device=device).view(n, per)
-        self.past = i32(n)
+        self.past, self.full = i32(n), torch.zeros(n, dtype=torch.bool, device=device)
         rows = n * self.nodes
         cu = torch.arange(n + 1, dtype=torch.int32, device=device) * self.nodes
         self.tree = torch.tensor(list(parents) * n, dtype=torch.int32, device=device) if parents is not None else None
@@ -388,7 +393,8 @@ class SpeculativeStep:
 
     def prefill(self, embeds, lengths: Sequence[int]):
         """Appends ``lengths[i]`` rows to sequence i (``embeds``: device bf16 [sum, d], sequence after sequence); returns
-        their hidden rows.  Follows the current stream, and is followed by it, where the context's is another."""
+        their hidden rows.  Follows the current stream, and is followed by it, where the context's is another; waits for
+        both, to see how many rows the sequences have."""
         import torch
         lengths = [int(x) for x in lengths]
         if len(lengths) != self.n or min(lengths) < 0 or sum(lengths) != embeds.shape[0]:
@@ -400,6 +406,9 @@ class SpeculativeStep:
         here = torch.cuda.current_stream(embeds.device)
         self.ctx.stream.wait_stream(here)
         with torch.cuda.stream(self.ctx.stream):
+            for i, (past, new) in enumerate(zip(self.past.tolist(), lengths)):
+                if new > 0 and past + new > self.max_len:
+                    raise ValueError(f"{new} rows behind {past} of sequence {i} with room for {self.max_len}")
             hidden = self._prefill(embeds, lengths)
         here.wait_stream(self.ctx.stream)
         hidden.record_stream(here)
@@ -423,6 +432,16 @@ class SpeculativeStep:
     def choose(self):
         jn_tenant_tokens_decode(self.ctx, self.hidden, self.heads, self.picks, self.head_ws)
         jn_tenant_tokens_verify(self.ctx, self.trees, self.tree_ws)
+        self._hold()
+
+    def _hold(self):
+        """Nothing stands of sequences that are full.  By what `past` says on the device, which a replay has too."""
+        import torch
+        with torch.cuda.stream(self.ctx.stream):
+            torch.ge(self.past, self.max_len, out=self.full)
+            self.n_path.masked_fill_(self.full, 0)
+            self.next.masked_fill_(self.full, -1)
+            self.path.masked_fill_(self.full[:, None], -1)
 
     def sample(self, p: Sequence, u, r, q: Optional[Sequence] = None):
         """Instead of ``choose``: ``p[k]`` (and ``q[k]``, of drafts that were drawn) fp32 [tenant k's rows, vocab], numbers
@@ -433,6 +452,7 @@ class SpeculativeStep:
         with torch.cuda.stream(self.ctx.stream):  # whose memory it is: the next call may have it again
             ws = torch.empty(jn_tokens_verify_workspace_size(trees), dtype=torch.uint8, device=self.tokens.device)
         jn_tenant_tokens_verify(self.ctx, trees, ws)
+        self._hold()
 
     def keep(self):
         jn_kv_keep(self.ctx, self.cache, self.batch, self.path, self.n_path, self.past)
