@@ -445,8 +445,13 @@ class SpeculativeStep:
 
     def sample(self, p: Sequence, u, r, q: Optional[Sequence] = None):
         """Instead of ``choose``: ``p[k]`` (and ``q[k]``, of drafts that were drawn) fp32 [tenant k's rows, vocab], numbers
-        ``u`` [rows] and ``r`` [sequences]."""
+        ``u`` [rows] and ``r`` [sequences].  Follows the current stream where the context's is another."""
         import torch
+        here = torch.cuda.current_stream(self.tokens.device)
+        if here != self.ctx.stream:
+            self.ctx.stream.wait_stream(here)
+            for t in (*p, *(q or ()), u, r):  # (the caller may let go of them before they are read)
+                t.record_stream(self.ctx.stream)
         trees = [self._verify(s, rows, self.cu, p=p[k], q=q[k] if q is not None else None, u=u[rows], r=r[s])
                  for k, (s, rows) in enumerate(self.slices)]
         with torch.cuda.stream(self.ctx.stream):  # whose memory it is: the next call may have it again
