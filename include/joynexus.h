@@ -657,8 +657,8 @@ jn_status jn_tenant_tokens_decode(jn_ctx* ctx, const void* hidden, int32_t T, in
  *   likeliest tokens (p NULL): x stands if x == greedy[c].
  * So a standing token's chance is the target's p.  Behind the last standing node comes
  * `next`: the lowest token i with sum_{k <= i} w_k > r sum_k w_k for the tree's number r, w
- * what is left of p[c] (its max(p - a q, 0), or p without the rejected tokens; the w before
- * the last rejection where that leaves nothing), or greedy[c]; -1 where no w is positive.  A
+ * what is left of p[c] (its max(p - a q, 0), or p without the rejected tokens; where that is
+ * nothing, the w before the last rejection that took some of it), or greedy[c]; -1 where no w is positive.  A
  * node 0 alone draws a token from p.  Weights that are NaN or negative count as 0; children
  * whose token is outside [0, vocab) are passed over.  Products and sums are formed in 64 bits, in a fixed order. */
 typedef struct jn_token_verify {

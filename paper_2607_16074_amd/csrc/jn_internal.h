@@ -568,7 +568,8 @@ struct TokVerifySet {
 };
 static_assert(sizeof(TokVerifySet) <= 3400, "kernel arguments");
 // Where a tree's walk is: its last standing node and what is left there, max(p - a q,
-// 0) with sum T (before: a before the last rejection) or p without `ngone` tokens.
+// 0) with sum T (before: a before the last rejection) or p without `ngone` tokens, in the
+// order of their rejections.
 struct VerifyState {
   double a, before, T;
   int32_t cur, count, ngone;

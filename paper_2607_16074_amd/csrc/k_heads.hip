@@ -1513,7 +1513,7 @@ __device__ VerifyState verify_walk(VerifyNodes& s, const TokVerify& d, int32_t f
           for (int32_t g = lane; g < w.ngone; g += 64) was |= s.gone[g] == x;
           const double rest = __any(was) || !(p > 0.) ? 0. : p;
           stands = u * w.T < rest;
-          if (!stands) {
+          if (!stands && rest > 0.) {  // (of others nothing is taken: the last one gone is the last that had a weight)
             w.T -= rest;
             if (lane == 0) s.gone[w.ngone] = x;
             ++w.ngone;
@@ -1742,8 +1742,8 @@ __global__ __launch_bounds__(kPickThreads) void tok_pick_next_kernel(TokVerifySe
   const bool found = pick[1] != 0;
   const double want = red[0];
   __syncthreads();
-  if (c < 0) {
-    if (tid == 0) d.next[t] = -1;
+  if (c < 0) {  // (of picked drafts the token that was taken last is all that was there before)
+    if (tid == 0) d.next[t] = !d.q && w.ngone > 0 ? s.gone[w.ngone - 1] : -1;
     return;
   }
   const int32_t i0 = c * piece, i1 = min(i0 + piece, d.vocab);
