@@ -372,7 +372,11 @@ typedef struct jn_kv_batch {
   int32_t max_pages;       /* >= 1; max_pages * page_size <= 2^30 (JN_ESHAPE)   */
   int32_t rows;            /* rows of the call, 0 .. 2^26 - 4 (JN_ESHAPE)       */
   int32_t max_new;         /* >= 1: the most new rows of a sequence; with parents at most
-                              JN_KV_TREE_ROWS (JN_EUNSUPPORTED)                 */
+                              JN_KV_TREE_ROWS (JN_EUNSUPPORTED).  min(max_new, rows) times the
+                              query heads of a key head picks attention's kernel: beyond 32 (16 of
+                              head width 256) it works on 64 or 128 query rows at a time, which
+                              makes single tokens slower (8 heads a key head, width 128: one 12 ->
+                              16 us, of 64 streams 110 -> 125), so name the call's own        */
   int32_t whole;
   int32_t reserved;
   const int32_t* pages;    /* device int32 [n_seqs][max_pages] */
@@ -414,7 +418,9 @@ jn_status jn_kv_attention(jn_ctx* ctx, const jn_kv_cache* cache, int32_t layer, 
 
 /* Keeps a branch of every sequence's new rows, in all layers: keys and values of new
  * row path[s][k] move to place past[s] + k for k < n_path[s] (n_path taken within [0,
- * max_path]), and past_out[s] = past[s] + n_path[s] (past_out may be past, or NULL).
+ * max_path]), and past_out[s] = past[s] + n_path[s] (past_out may be past, or NULL): rows
+ * that had no place are counted too, so a caller keeps past + max_new within max_pages *
+ * page_size (row j lies at past + j, whatever its depth in a tree), or stops there.
  * max_path: 1 .. 2^26 (JN_ESHAPE).  A path ascends, path[s][k] >= k, as those of
  * jn_tenant_tokens_verify do; an entry outside k .. max_new - 1, or below an earlier one,
  * moves nothing. */

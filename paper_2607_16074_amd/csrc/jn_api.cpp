@@ -2012,7 +2012,10 @@ bool verify_plan(const jn_token_verify* v, int32_t G, int32_t* g, VerifyPlan* P)
     // A chain has one sum, a tree of drawn drafts one more for every rejection but a node's
     // last: a launch for each node of a mean tree, where rows are long. 16 trees of up to 9
     // nodes over 160,001: 1, 2, 4, 5, 6, 8 launches 70, 57, 36, 37, 40, 44 us; 6 of up to
-    // 25 nodes 112, 92, 55, 47, 39, 44; 16 of 25 over 32,003: 1, 6 launches 73, 59.
+    // 25 nodes 112, 92, 55, 47, 39, 44; 16 of 25 over 32,003: 1, 6 launches 73, 59. Below some
+    // 30,000 one launch is the faster or as fast, by up to 10 us: 16 of up to 9 nodes over 4,001, 8,001,
+    // 16,001, 32,003: 23, 27, 32, 32 with one, 33, 34, 35, 32 with more; 64 of 25: 51, 59, 50, 83 and 57, 63,
+    // 52, 78. The border stands lower than that.
     const bool more = t.q && t.parents && t.vocab >= kVerifyLongRow;
     P->phases = std::max(P->phases, more ? (int32_t)std::min<int64_t>(std::max<int64_t>(t.n / t.n_trees, 1), 6) : 1);
   }

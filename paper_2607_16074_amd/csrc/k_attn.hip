@@ -826,7 +826,7 @@ struct KvWalk {
   // row: those below C are summed as the steps of the Euclidean algorithm (count, modulus,
   // slope and offset below), the rest are C each. All in 32 bits but the sum: G n <= 2^26,
   // and past is taken modulo KT. (Row tile after row tile instead, the search made two
-  // pieces of 2,048 rows take 329 us, with this 313.)
+  // pieces of 2,048 and 1,792 rows take 329 us, with this 312.)
   static __device__ __forceinline__ int64_t upto(const KvBatch& b, const KvSeq& q, int32_t G, int32_t k) {
     const int32_t last = tiles_of(min(q.past + q.n, b.places));
     if constexpr (R == 0) return (int64_t)k * last;
@@ -1121,6 +1121,9 @@ __device__ __forceinline__ int kv_swz(int r) {
 // nothing waits for another wavefront before the unit's end, where their O, m and l are
 // added in LDS.
 //   S^T = K Q^T, O^T += V^T P^T as in attn16_fwd_kernel.
+// P is rounded to bf16 for its product, here and in kv_many_kernel (l sums it before that):
+// results are 1.9e-3 to 2.3e-3 from 64 bits, relative, where rounding them alone gives 1.7e-3;
+// P as two bf16 would double the second product.
 // A key's page is the same for the 16 keys of a fragment (pages are multiples of 16),
 // so page numbers are read once for all lanes, a step ahead. Values of places that no row
 // sees are set to zero in LDS (0 * NaN is NaN).
@@ -1429,9 +1432,10 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void kv_few_kernel(KvCache 
 // as zeros, as are those of masked tiles that are not finite (kv_add_odd).
 // 32 rows a wavefront (head width 256: 16, whose registers leave two wavefronts a SIMD;
 // 32 there took twice as long), 128 rows a workgroup, which halves the LDS reads of a
-// product against 16 rows; 64 rows where a unit has no more. Two pieces of 2,048 rows behind 6,001, 16
-// query heads of 128: 313 us with the join, 0.59 PFLOP/s, the matrix cores 30 % busy beside
-// 200 other vector instructions a tile and wavefront; 61 rows over 131,070 of 8 heads: 106 us, 5.1 TB/s.
+// product against 16 rows; 64 rows where a unit has no more. Pieces of 2,048 rows behind 6,001 and of
+// 1,792 behind 3,563, 16 query heads of 128: 286 us, 0.64 PFLOP/s (312 and 0.59 with the join), the matrix
+// cores 30 % busy beside 200 other vector instructions a tile and wavefront; where all rows see each other
+// 369 with the join, 0.58. 61 rows over 131,070 of 8 heads: 105 us, 5.1 TB/s.
 template <int HD, int NB, int W>
 __global__ __launch_bounds__(64 * W, 2) void kv_many_kernel(KvCache c, KvBatch b, KvAttn a, KvWork wk) {
   constexpr int R = 16 * NB * W, KT = 64, THREADS = 64 * W;
