@@ -89,3 +89,49 @@ def test_probabilities_of_another_stream_than_the_contexts(lib):
     got = [x[:c] for x, c in zip(st.path.tolist(), st.n_path.tolist())]
     assert [(g, x) for g, x in zip(got, st.next.tolist())] == want
     assert all(bool((x == 0.5).all()) for x in again)
+
+
+@pytest.mark.gpu
+def test_a_captured_sampled_run_follows_its_buffers(lib):
+    """Extend, sample and keep in one graph, replayed over new probabilities, against the same run eagerly."""
+    from paper_2607_16074_amd import step
+    from test_gpu_speculative import Speaker
+    sp, gen = Speaker(lib, 14), torch.Generator().manual_seed(6)
+    side = torch.cuda.Stream()
+    parents = [-1, 0, 0, 1, 2]
+    with torch.cuda.stream(side):
+        steps = [step.SpeculativeStep(sp.model, [0, 1], [1, 2], 24, 5, parents, 16, lib.Context(side)) for _ in range(2)]
+        x = torch.randn(20, 256, generator=gen).to(torch.bfloat16).cuda()
+        for st in steps:
+            st.prefill(x, [14, 0, 6])
+        p, q = ([torch.zeros(n, h.shape[0], device="cuda") for n, h in zip((5, 10), sp.heads)] for _ in range(2))
+        u, r = torch.zeros(15, device="cuda"), torch.zeros(3, device="cuda")
+
+        def run(st):
+            st.extend()
+            st.sample(p, u, r, q)
+            st.keep()
+
+        past = steps[0].past.clone()
+        run(steps[0])  # (everything is loaded before a capture)
+        steps[0].past.copy_(past)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            run(steps[0])
+        for turn in range(12):
+            for t in (*p, *q):
+                t.copy_(torch.softmax(torch.randn(t.shape, generator=gen), 1))
+            u.copy_(torch.rand(15, generator=gen))
+            r.copy_(torch.rand(3, generator=gen))
+            rows, tokens = torch.randn(15, 256, generator=gen), torch.randint(0, 33, (15,), generator=gen)
+            for st in steps:
+                st.embeds.copy_(rows)
+                st.tokens.copy_(tokens)
+            graph.replay()
+            run(steps[1])
+            side.synchronize()
+            for name in ("past", "path", "n_path", "next"):
+                assert torch.equal(getattr(steps[0], name), getattr(steps[1], name)), (turn, name)
+            assert torch.equal(steps[0].cache.k, steps[1].cache.k) and torch.equal(steps[0].cache.v, steps[1].cache.v)
+        assert steps[0].past.tolist()[0] >= 24 and steps[0].n_path.tolist()[0] == 0
